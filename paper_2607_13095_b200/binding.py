@@ -28,7 +28,8 @@ EXPORTS = [
     "hswa_window_safe_len", "hswa_swa_window_gather", "hswa_swa_window_scatter",
     "hswa_decode_workspace_need", "hswa_selftest_wait_timeout", "hswa_set_overlap",
     "hswa_swa_release", "hswa_swa_valid_mask", "hswa_prefix_hit_len", "hswa_set_prefill_order", "hswa_set_block_trace",
-    "hswa_probe_read_stream",
+    "hswa_probe_read_stream", "hswa_cross_attn", "hswa_cross_workspace_need", "hswa_attn_weights", "hswa_evict_select",
+    "hswa_evict_compact",
 ]
 
 
@@ -109,6 +110,16 @@ def load(build_if_missing: bool = True) -> C.CDLL:
     lib.hswa_prefill_attn.restype = C.c_int
     lib.hswa_prefill_attn.argtypes = [vp, C.POINTER(hswa_layer), C.POINTER(hswa_batch), vp, vp, vp, i32, vp, vp, vp,
                                       sz, vp]
+    lib.hswa_cross_workspace_need.restype = sz
+    lib.hswa_cross_workspace_need.argtypes = [vp, i32, i32, i32, i32]
+    lib.hswa_cross_attn.restype = C.c_int
+    lib.hswa_cross_attn.argtypes = [vp, C.POINTER(hswa_layer), C.POINTER(hswa_batch), vp, vp, vp, vp, sz, vp]
+    lib.hswa_attn_weights.restype = C.c_int
+    lib.hswa_attn_weights.argtypes = [vp, C.POINTER(hswa_layer), C.POINTER(hswa_batch), i32, vp, vp, C.c_float, vp, i64, vp]
+    lib.hswa_evict_select.restype = C.c_int
+    lib.hswa_evict_select.argtypes = [vp, i32, vp, i32, vp, i64, vp, i32, i32, i32, vp, vp, vp]
+    lib.hswa_evict_compact.restype = C.c_int
+    lib.hswa_evict_compact.argtypes = [vp, C.POINTER(hswa_layer), C.POINTER(hswa_batch), vp, vp, i32, vp, i32, vp, i64, vp, i64, vp]
     lib.hswa_window_safe_len.restype = C.c_int64
     lib.hswa_window_safe_len.argtypes = [C.c_int64, i32, vp]
     lib.hswa_swa_window_gather.restype = C.c_int
@@ -296,6 +307,53 @@ def hswa_prefill_attn(h: Handle, layer: Layer, batch: Batch, q, k_new, v_new, fu
     _check(load().hswa_prefill_attn(h.ptr, C.byref(layer.c), C.byref(batch.c), _ptr(q), _ptr(k_new), _ptr(v_new),
                                     int(bool(fuse_append)), _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes,
                                     _stream()), "hswa_prefill_attn")
+
+
+def hswa_cross_workspace_need(h: Handle, batch: int, total_q: int, max_q_len: int, max_ctx_len: int) -> int:
+    return int(load().hswa_cross_workspace_need(h.ptr, batch, total_q, max_q_len, max_ctx_len))
+
+
+def hswa_cross_attn(h: Handle, layer: Layer, batch: Batch, q, out, lse=None, workspace=None):
+    """Attention of q [T][Hq][D] to all ctx_len[r] cached states of each request (no causal mask, nothing appended)."""
+    assert q.dtype == torch.bfloat16 and out.dtype == h.out_dtype and (lse is None or lse.dtype == torch.float32)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(load().hswa_cross_attn(h.ptr, C.byref(layer.c), C.byref(batch.c), _ptr(q), _ptr(out), _ptr(lse), _ptr(workspace),
+                                  ws_bytes, _stream()), "hswa_cross_attn")
+
+
+def hswa_attn_weights(h: Handle, layer: Layer, batch: Batch, causal: bool, q, lse, decay: float, weights: torch.Tensor):
+    """weights: fp32 CUDA tensor [B][Hkv][stride], updated in place with the attention weights of q's rows (lse: theirs)."""
+    assert q.dtype == torch.bfloat16 and lse.dtype == torch.float32
+    assert weights.dtype == torch.float32 and weights.dim() == 3 and tuple(weights.shape[:2]) == (batch.batch, h.cfg.num_kv_heads)
+    _check(load().hswa_attn_weights(h.ptr, C.byref(layer.c), C.byref(batch.c), int(bool(causal)), _ptr(q), _ptr(lse), float(decay),
+                                    _ptr(weights), int(weights.shape[2]), _stream()), "hswa_attn_weights")
+
+
+def hswa_evict_select(h: Handle, batch: int, ctx_len: torch.Tensor, max_ctx_len: int, weights: torch.Tensor, keep_len: torch.Tensor,
+                      keep_idx: torch.Tensor, kept_len: torch.Tensor, *, protect_first: int = 0, protect_last: int = 0):
+    """keep_idx: int32 CUDA tensor [B][Hkv][max_keep], filled with the positions of largest weight, ascending, then -1."""
+    for t in (ctx_len, keep_len, keep_idx, kept_len):
+        assert t.dtype == torch.int32
+    assert weights.dtype == torch.float32 and weights.dim() == 3 and tuple(weights.shape[:2]) == (batch, h.cfg.num_kv_heads)
+    assert keep_idx.dim() == 3 and tuple(keep_idx.shape[:2]) == (batch, h.cfg.num_kv_heads)
+    _check(load().hswa_evict_select(h.ptr, batch, _ptr(ctx_len), int(max_ctx_len), _ptr(weights), int(weights.shape[2]),
+                                    _ptr(keep_len), int(keep_idx.shape[2]), int(protect_first), int(protect_last), _ptr(keep_idx),
+                                    _ptr(kept_len), _stream()), "hswa_evict_select")
+
+
+def hswa_evict_compact(h: Handle, layer: Layer, batch: Batch, keep_idx: torch.Tensor, kept_len: torch.Tensor,
+                       dst_block_table: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                       weights_out: Optional[torch.Tensor] = None):
+    """Copies the kept K/V rows (and weights) of batch's block table to the pages of dst_block_table [B][blocks]."""
+    for t in (keep_idx, kept_len, dst_block_table):
+        assert t.dtype == torch.int32
+    assert keep_idx.dim() == 3 and dst_block_table.dim() == 2
+    for t in (weights, weights_out):
+        assert t is None or (t.dtype == torch.float32 and t.dim() == 3)
+    _check(load().hswa_evict_compact(h.ptr, C.byref(layer.c), C.byref(batch.c), _ptr(keep_idx), _ptr(kept_len),
+                                     int(keep_idx.shape[2]), _ptr(dst_block_table), int(dst_block_table.shape[1]), _ptr(weights),
+                                     0 if weights is None else int(weights.shape[2]), _ptr(weights_out),
+                                     0 if weights_out is None else int(weights_out.shape[2]), _stream()), "hswa_evict_compact")
 
 
 def hswa_window_safe_len(match_len: int, window: int, swa_valid) -> int:

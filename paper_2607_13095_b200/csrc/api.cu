@@ -129,6 +129,43 @@ bool plan_decode(const hswa_handle* h, int is_swa, int batch, int max_ctx_len, i
   return true;
 }
 
+// Cross attention: how one call is laid out, from host-known values only.  One token per request streams the cache like a
+// decode step; anything else goes to the tile kernel, whose key slices fill the machine when the rows alone do not.
+struct CrossPlan {
+  bool decode;
+  DecodePlan dec;
+  int row_tiles, slices, slice_len;
+  size_t o_bytes, ml_bytes;
+};
+
+bool plan_cross(const hswa_handle* h, int batch, int total_q, int max_q_len, int max_ctx_len, CrossPlan* pl) {
+  CrossPlan c = {};
+  c.decode = max_q_len == 1 && total_q == batch;
+  if (c.decode) {
+    if (!plan_decode(h, 0, batch, max_ctx_len > 0 ? max_ctx_len - 1 : 0, 0, 1, &c.dec)) return false;
+    c.o_bytes = c.dec.o_bytes;
+    c.ml_bytes = c.dec.ml_bytes;
+  } else {
+    const int64_t rows = (int64_t)max_q_len * h->group;
+    c.row_tiles = (int)((rows + hswa_cross_mma_rows() - 1) / hswa_cross_mma_rows());
+    const int64_t blocks = (int64_t)c.row_tiles * h->cfg.num_kv_heads * batch;
+    const int64_t want = (4LL * h->num_sms + blocks - 1) / blocks, most = (max_ctx_len + 511) / 512;
+    int64_t slices = want < most ? want : most;
+    if (slices < 1) slices = 1;
+    c.slice_len = (int)((((int64_t)max_ctx_len + slices - 1) / slices + 127) / 128 * 128);
+    if (c.slice_len < 128) c.slice_len = 128;
+    c.slices = max_ctx_len > 0 ? (max_ctx_len + c.slice_len - 1) / c.slice_len : 1;
+    if (blocks * c.slices > INT32_MAX) return false;
+    if (c.slices > 1) {
+      const size_t n = (size_t)total_q * h->cfg.num_q_heads * c.slices;
+      c.o_bytes = (n * h->cfg.head_dim * sizeof(float) + 255) & ~size_t(255);
+      c.ml_bytes = (n * sizeof(float2) + 255) & ~size_t(255);
+    }
+  }
+  *pl = c;
+  return true;
+}
+
 // 4-D view of a pool for TMA: {D, P, 2 * Hkv, num_pages}, box {64, box_slots, 1, 1} (0: a whole page),
 // 128-byte swizzle.
 hswa_status make_pool_map(const hswa_handle* h, const hswa_layer* layer, CUtensorMap* tm, int box_slots = 0) {
@@ -422,7 +459,7 @@ static hswa_status decode_impl(hswa_handle* h, const hswa_layer* layer, const hs
   // that the combine, which waits for the suffix kernel, finds both sets of partials complete.
   p.late_dep_wait = cascade ? 1 : 0;
   if (hswa_launch_decode(h, tm, p, early || cascade, (cudaStream_t)stream) != cudaSuccess) return HSWA_ERR_CUDA;
-  if (p.max_splits > 1 && hswa_launch_combine(p, (cudaStream_t)stream) != cudaSuccess) return HSWA_ERR_CUDA;
+  if (p.max_splits > 1 && hswa_launch_combine(p, false, (cudaStream_t)stream) != cudaSuccess) return HSWA_ERR_CUDA;
   if (k_new != nullptr) {
     h->chain_ok = 1;
     h->chain_stream = stream;
@@ -516,7 +553,7 @@ hswa_status hswa_decode_attn_mtp(hswa_handle* h, const hswa_layer* layer, const 
     if (hswa_launch_decode_mtp_tc(tm, tm_q, p, h->num_sms, workspace, (cudaStream_t)stream) != cudaSuccess) return HSWA_ERR_CUDA;
   } else {
     if (hswa_launch_decode_mtp(h, tm, p, early, (cudaStream_t)stream) != cudaSuccess) return HSWA_ERR_CUDA;
-    if (p.max_splits > 1 && hswa_launch_combine(p, (cudaStream_t)stream) != cudaSuccess) return HSWA_ERR_CUDA;
+    if (p.max_splits > 1 && hswa_launch_combine(p, false, (cudaStream_t)stream) != cudaSuccess) return HSWA_ERR_CUDA;
   }
   h->chain_ok = 1;  // none of these kernels writes the batch arrays or another layer's pool
   h->chain_stream = stream;
@@ -616,6 +653,168 @@ hswa_status hswa_prefill_attn(hswa_handle* h, const hswa_layer* layer, const hsw
     if (hswa_launch_append(a, (cudaStream_t)stream) != cudaSuccess) return HSWA_ERR_CUDA;
   }
   return HSWA_OK;
+}
+
+size_t hswa_cross_workspace_need(const hswa_handle* h, int32_t batch, int32_t total_q, int32_t max_q_len, int32_t max_ctx_len) {
+  CrossPlan pl;
+  if (!h || batch <= 0 || total_q <= 0 || max_q_len <= 0 || max_q_len > total_q || max_ctx_len < 0 ||
+      !plan_cross(h, batch, total_q, max_q_len, max_ctx_len, &pl))
+    return 0;
+  return pl.o_bytes + pl.ml_bytes;
+}
+
+hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_batch* b, const void* q, void* out, float* lse,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+  if (h) h->chain_ok = 0;
+  hswa_status st = check_common(h, layer, b);
+  if (st != HSWA_OK) return st;
+  if (b->batch == 0 || b->total_q == 0) return HSWA_OK;
+  if (layer->is_swa || b->max_q_len == 0) return HSWA_ERR_INVALID_ARG;
+  if (!q || !out || !aligned16(q) || !aligned16(out)) return HSWA_ERR_INVALID_ARG;
+  if ((int64_t)b->max_ctx_len > (int64_t)b->max_blocks * h->cfg.page_size) return HSWA_ERR_INVALID_ARG;
+  CrossPlan pl;
+  if (!plan_cross(h, b->batch, b->total_q, b->max_q_len, b->max_ctx_len, &pl)) return HSWA_ERR_UNSUPPORTED;
+  if (pl.o_bytes > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < pl.o_bytes + pl.ml_bytes))
+    return HSWA_ERR_WORKSPACE;
+  if (cudaSetDevice(h->device) != cudaSuccess) return HSWA_ERR_CUDA;
+  float* part_o = pl.o_bytes > 0 ? static_cast<float*>(workspace) : nullptr;
+  float2* part_ml = pl.o_bytes > 0 ? reinterpret_cast<float2*>(static_cast<char*>(workspace) + pl.o_bytes) : nullptr;
+  cudaStream_t s = (cudaStream_t)stream;
+  if (pl.decode) {
+    DecodeParams p = {};
+    p.m = model_params(h);
+    p.b = batch_params(b);
+    p.pool = static_cast<__nv_bfloat16*>(layer->pool);
+    p.num_pages = layer->num_pages;
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.out = out;
+    p.lse = lse;
+    p.split_len = pl.dec.split_len;
+    p.max_splits = pl.dec.max_splits;
+    p.grid_splits = pl.dec.grid_splits;
+    p.nq = 1;
+    p.max_ctx_len = b->max_ctx_len;
+    p.part_o = part_o;
+    p.part_ml = part_ml;
+    p.err = h->err;
+    CUtensorMap tm;
+    if ((st = make_pool_map(h, layer, &tm)) != HSWA_OK) return st;
+    if (hswa_launch_decode_cross(tm, p, s) != cudaSuccess) return HSWA_ERR_CUDA;
+    if (p.max_splits > 1 && hswa_launch_combine(p, true, s) != cudaSuccess) return HSWA_ERR_CUDA;
+    return HSWA_OK;
+  }
+  CrossParams p = {};
+  p.m = model_params(h);
+  p.b = batch_params(b);
+  p.pool = static_cast<const __nv_bfloat16*>(layer->pool);
+  p.num_pages = layer->num_pages;
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.out = out;
+  p.lse = lse;
+  p.total_q = b->total_q;
+  p.max_q_len = b->max_q_len;
+  p.max_ctx_len = b->max_ctx_len;
+  p.row_tiles = pl.row_tiles;
+  p.slices = pl.slices;
+  p.slice_len = pl.slice_len;
+  p.part_o = part_o;
+  p.part_ml = part_ml;
+  p.err = h->err;
+  if (hswa_launch_cross_mma(p, s) != cudaSuccess) return HSWA_ERR_CUDA;
+  if (p.slices > 1 && hswa_launch_cross_combine(p, s) != cudaSuccess) return HSWA_ERR_CUDA;
+  return HSWA_OK;
+}
+
+hswa_status hswa_attn_weights(hswa_handle* h, const hswa_layer* layer, const hswa_batch* b, int32_t causal, const void* q,
+                              const float* lse, float decay, float* weights, int64_t weights_stride, void* stream) {
+  if (h) h->chain_ok = 0;
+  hswa_status st = check_common(h, layer, b);
+  if (st != HSWA_OK) return st;
+  if (b->batch == 0) return HSWA_OK;
+  if (layer->is_swa || weights_stride < 0 || !(decay >= 0.f) || std::isinf(decay)) return HSWA_ERR_INVALID_ARG;
+  // (the longest context and the longest step need not belong to one request: their sum is checked per request)
+  if ((int64_t)b->max_ctx_len > (int64_t)b->max_blocks * h->cfg.page_size || b->max_ctx_len > weights_stride) return HSWA_ERR_INVALID_ARG;
+  if (b->max_ctx_len == 0 && (!causal || b->max_q_len == 0)) return HSWA_OK;
+  if (!weights || (b->total_q > 0 && (!q || !lse || !aligned16(q)))) return HSWA_ERR_INVALID_ARG;
+  if (b->batch > 65535 || h->cfg.num_kv_heads > 65535) return HSWA_ERR_UNSUPPORTED;
+  if (cudaSetDevice(h->device) != cudaSuccess) return HSWA_ERR_CUDA;
+  WeightsParams p = {};
+  p.m = model_params(h);
+  p.b = batch_params(b);
+  p.pool = static_cast<const __nv_bfloat16*>(layer->pool);
+  p.num_pages = layer->num_pages;
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.lse = lse;
+  p.weights = weights;
+  p.stride = weights_stride;
+  p.decay = decay;
+  p.causal = causal != 0;
+  p.max_q_len = b->max_q_len;
+  p.max_ctx_len = b->max_ctx_len;
+  p.err = h->err;
+  return hswa_launch_attn_weights(p, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+}
+
+hswa_status hswa_evict_select(hswa_handle* h, int32_t batch, const int32_t* ctx_len, int32_t max_ctx_len, const float* weights,
+                              int64_t weights_stride, const int32_t* keep_len, int32_t max_keep, int32_t protect_first,
+                              int32_t protect_last, int32_t* keep_idx, int32_t* kept_len, void* stream) {
+  if (h) h->chain_ok = 0;
+  if (!h || batch < 0 || max_ctx_len < 0 || max_keep < 0 || protect_first < 0 || protect_last < 0 || weights_stride < max_ctx_len)
+    return HSWA_ERR_INVALID_ARG;
+  if (batch == 0) return HSWA_OK;
+  if (!ctx_len || !keep_len || !kept_len || (max_keep > 0 && !keep_idx) || (max_ctx_len > 0 && !weights)) return HSWA_ERR_INVALID_ARG;
+  if ((int64_t)batch * h->cfg.num_kv_heads > INT32_MAX) return HSWA_ERR_UNSUPPORTED;
+  if (cudaSetDevice(h->device) != cudaSuccess) return HSWA_ERR_CUDA;
+  SelectParams p = {};
+  p.B = batch;
+  p.Hkv = h->cfg.num_kv_heads;
+  p.ctx_len = ctx_len;
+  p.max_ctx_len = max_ctx_len;
+  p.weights = weights;
+  p.stride = weights_stride;
+  p.keep_len = keep_len;
+  p.max_keep = max_keep;
+  p.protect_first = protect_first;
+  p.protect_last = protect_last;
+  p.keep_idx = keep_idx;
+  p.kept_len = kept_len;
+  p.err = h->err;
+  return hswa_launch_evict_select(p, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+}
+
+hswa_status hswa_evict_compact(hswa_handle* h, const hswa_layer* layer, const hswa_batch* b, const int32_t* keep_idx,
+                               const int32_t* kept_len, int32_t max_keep, const int32_t* dst_block_table, int32_t dst_max_blocks,
+                               const float* weights, int64_t weights_stride, float* weights_out, int64_t weights_out_stride,
+                               void* stream) {
+  if (h) h->chain_ok = 0;
+  hswa_status st = check_common(h, layer, b);
+  if (st != HSWA_OK) return st;
+  if (max_keep < 0 || dst_max_blocks < 0) return HSWA_ERR_INVALID_ARG;
+  if (b->batch == 0 || max_keep == 0) return HSWA_OK;
+  if (layer->is_swa || !keep_idx || !kept_len || !dst_block_table) return HSWA_ERR_INVALID_ARG;
+  if ((int64_t)max_keep > (int64_t)dst_max_blocks * h->cfg.page_size) return HSWA_ERR_INVALID_ARG;
+  if ((int64_t)b->max_ctx_len > (int64_t)b->max_blocks * h->cfg.page_size) return HSWA_ERR_INVALID_ARG;
+  if ((weights == nullptr) != (weights_out == nullptr)) return HSWA_ERR_INVALID_ARG;
+  if (weights && (weights_stride < b->max_ctx_len || weights_out_stride < max_keep || weights == weights_out)) return HSWA_ERR_INVALID_ARG;
+  if (b->batch > 65535 || h->cfg.num_kv_heads > 65535) return HSWA_ERR_UNSUPPORTED;
+  if (cudaSetDevice(h->device) != cudaSuccess) return HSWA_ERR_CUDA;
+  CompactParams p = {};
+  p.m = model_params(h);
+  p.b = batch_params(b);
+  p.pool = static_cast<__nv_bfloat16*>(layer->pool);
+  p.num_pages = layer->num_pages;
+  p.max_ctx_len = b->max_ctx_len;
+  p.keep_idx = keep_idx;
+  p.kept_len = kept_len;
+  p.max_keep = max_keep;
+  p.dst_block_table = dst_block_table;
+  p.dst_max_blocks = dst_max_blocks;
+  p.weights = weights;
+  p.stride = weights_stride;
+  p.weights_out = weights_out;
+  p.out_stride = weights_out_stride;
+  p.err = h->err;
+  return hswa_launch_evict_compact(p, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
 }
 
 static hswa_status window_move(hswa_handle* h, const hswa_layer* layer, const hswa_batch* b, void* buf, int gather,

@@ -50,7 +50,11 @@ struct KeyRange {
 //                     only on tiles that have such rows: right for Full layers, where that is the last tile);
 //   REG_MASK = true   zero them in the A fragments after ldmatrix (four logic ops per fragment on every tile, no
 //                     pass over shared memory: right for rings, where most tiles have such rows).
-template <int D, bool REG_MASK = false>
+// The row sum takes the probabilities as the tensor core multiplies them (rounded to bf16), so that a row's weights add
+// up to one exactly; with EXACT_SUM it takes the fp32 values instead, for callers whose log-sum-exp is itself a result
+// that later kernels exponentiate again (a rounded sum is up to 2^-9 off on a row of one key, and averages out only
+// with the number of keys).
+template <int D, bool REG_MASK = false, bool EXACT_SUM = false>
 __device__ __forceinline__ void consume_tile(uint8_t* sV, uint32_t aK, uint32_t aV, uint32_t vm0, uint32_t vm1, bool wrote,
                                              const uint32_t (&qf)[D / 16][2], float scale_log2, float (&m_run)[2],
                                              float (&l_run)[2], float (&o)[D / 16][4], int lane, uint32_t zm0, uint32_t zm1) {
@@ -126,9 +130,14 @@ __device__ __forceinline__ void consume_tile(uint8_t* sV, uint32_t aK, uint32_t 
     uint32_t pk[8];
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) {
-      pk[2 * kb] = pack_bf16x2(fast_exp2(s[kb][0] - m_use[0]), fast_exp2(s[kb][1] - m_use[1]));
-      pk[2 * kb + 1] = pack_bf16x2(fast_exp2(s[kb][2] - m_use[0]), fast_exp2(s[kb][3] - m_use[1]));
-      const float2 f0 = unpack_bf16x2(pk[2 * kb]), f1 = unpack_bf16x2(pk[2 * kb + 1]);
+      float2 f0 = make_float2(fast_exp2(s[kb][0] - m_use[0]), fast_exp2(s[kb][1] - m_use[1]));
+      float2 f1 = make_float2(fast_exp2(s[kb][2] - m_use[0]), fast_exp2(s[kb][3] - m_use[1]));
+      pk[2 * kb] = pack_bf16x2(f0.x, f0.y);
+      pk[2 * kb + 1] = pack_bf16x2(f1.x, f1.y);
+      if constexpr (!EXACT_SUM) {
+        f0 = unpack_bf16x2(pk[2 * kb]);
+        f1 = unpack_bf16x2(pk[2 * kb + 1]);
+      }
       l_run[0] += f0.x + f1.x;  // sum the values the tensor core will actually multiply
       l_run[1] += f0.y + f1.y;
     }
@@ -165,7 +174,10 @@ __device__ __forceinline__ void consume_tile(uint8_t* sV, uint32_t aK, uint32_t 
   }
 }
 
-template <int D, int P, int NS, int NW>
+// CROSS = true: attention to an encoder's states (hswa_cross_attn with one token per request).  All ctx keys and no
+// others are visible -- there is no new token, and a request may have none at all, whose block still writes its rows
+// (zeros, log-sum-exp minus infinity).  Lengths are clamped to the host's bound.
+template <int D, int P, int NS, int NW, bool CROSS = false>
 __global__ void __launch_bounds__((NW + 1) * 32, 2)
 decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p) {
   constexpr int HALVES = D / 64;
@@ -191,7 +203,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const ModelParams& M = p.m;
   const int ctx = p.b.ctx_len[r];
-  const int kv_len = ctx + 1;
+  const int kv_len = CROSS ? max(0, min(ctx, p.max_ctx_len)) : ctx + 1;
   // the grid was sized from the host's bound: a longer context would silently lose its tail
   if (threadIdx.x == 0 && split == 0 && kh == 0 && ctx > p.max_ctx_len) record_error(p.err, HSWA_ERR_BOUNDS, r, -1, ctx);
 
@@ -204,7 +216,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p)
   int k_begin = 0;
   if (!p.is_swa) {
     k_begin = p.k_start + split * p.split_len;
-    if (k_begin >= kv_len) return;
+    if (k_begin >= kv_len && (!CROSS || split > 0)) return;
     kr.span = min(kv_len, k_begin + p.split_len) - k_begin;
   } else {
     if (split > 0) return;
@@ -363,7 +375,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p)
       // validity of the tile's 64 keys
       const uint32_t vm0 = __ballot_sync(0xffffffffu, kr.valid(tile_lo + lane));
       const uint32_t vm1 = __ballot_sync(0xffffffffu, kr.valid(tile_lo + 32 + lane));
-      consume_tile<D>(sV, aK, aV, vm0, vm1, wrote, qf, M.scale_log2, m_run, l_run, o, lane, vm0, vm1);
+      consume_tile<D, false, CROSS>(sV, aK, aV, vm0, vm1, wrote, qf, M.scale_log2, m_run, l_run, o, lane, vm0, vm1);
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&bars[NS + stage]));
     }
@@ -416,12 +428,13 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p)
     }
     const int64_t row = (int64_t)r * M.Hq + kh * M.G + g;
     if (p.max_splits == 1) {
-      const float val = L > 0.f ? O / L : 0.f;
+      const bool some = CROSS ? L != 0.f : L > 0.f;  // (CROSS: a NaN among the inputs shows in the output)
+      const float val = some ? O / L : 0.f;
       if (M.out_fp32)
         reinterpret_cast<float*>(p.out)[row * D + d] = val;
       else
         reinterpret_cast<__nv_bfloat16*>(p.out)[row * D + d] = __float2bfloat16_rn(val);
-      if (d == 0 && p.lse) p.lse[row] = L > 0.f ? (mm + log2f(L)) * 0.6931471805599453f : -INFINITY;
+      if (d == 0 && p.lse) p.lse[row] = some ? (mm + log2f(L)) * 0.6931471805599453f : -INFINITY;
     } else {
       p.part_o[(row * p.max_splits + p.split_base + split) * D + d] = O;
       if (d == 0) p.part_ml[row * p.max_splits + p.split_base + split] = make_float2(mm, L);
@@ -433,7 +446,8 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p)
 }
 
 // Merge split-K partials: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  One warp per (request, head).
-template <int D>
+// CROSS: as for decode_kernel, the keys are the ctx cached ones; a row without keys has no partials and gets zeros.
+template <int D, bool CROSS = false>
 __global__ void __launch_bounds__(128) combine_kernel(const DecodeParams p) {
   const int warp_global = (blockIdx.x * blockDim.x + threadIdx.x) >> 5;
   const int lane = threadIdx.x & 31;
@@ -443,7 +457,7 @@ __global__ void __launch_bounds__(128) combine_kernel(const DecodeParams p) {
   if (warp_global >= p.b.B * p.nq * M.Hq) return;
   const int r = warp_global / (p.nq * M.Hq);
   const int64_t row = warp_global;
-  const int kv_len = p.b.ctx_len[r] + p.nq;
+  const int kv_len = CROSS ? max(0, min(p.b.ctx_len[r], p.max_ctx_len)) : p.b.ctx_len[r] + p.nq;
   const int n_splits = min(p.max_splits, p.split_base + (kv_len - p.k_start + p.split_len - 1) / p.split_len);
   const float2* ml = p.part_ml + row * p.max_splits;
   const float* po = p.part_o + row * p.max_splits * D;
@@ -474,7 +488,8 @@ __global__ void __launch_bounds__(128) combine_kernel(const DecodeParams p) {
       }
     }
   }
-  const float inv = L > 0.f ? 1.f / L : 0.f;
+  const bool some = CROSS ? L != 0.f : L > 0.f;
+  const float inv = some ? 1.f / L : 0.f;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const float val = acc[i] * inv;
@@ -483,7 +498,7 @@ __global__ void __launch_bounds__(128) combine_kernel(const DecodeParams p) {
     else
       reinterpret_cast<__nv_bfloat16*>(p.out)[row * D + lane * PER + i] = __float2bfloat16_rn(val);
   }
-  if (lane == 0 && p.lse) p.lse[row] = L > 0.f ? (mm + log2f(L)) * 0.6931471805599453f : -INFINITY;
+  if (lane == 0 && p.lse) p.lse[row] = some ? (mm + log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -1147,12 +1162,12 @@ cudaError_t launch_mtp_t(const CUtensorMap& tm, const DecodeParams& p, cudaStrea
   return cudaGetLastError();
 }
 
-template <int D, int P, int NS, int NW>
+template <int D, int P, int NS, int NW, bool CROSS = false>
 cudaError_t launch_decode_t(const CUtensorMap& tm, const DecodeParams& p, bool early_start, cudaStream_t s) {
   constexpr int STAGE_BYTES = 2 * (D / 64) * TK * 128;
   constexpr int SMEM = NS * STAGE_BYTES + 2 * NS * 8 + 16;  // stage buffers, barriers
   static_assert(NW * 8 * D * 4 + NW * 64 <= NS * STAGE_BYTES, "merge scratch must fit the stage buffers");
-  auto kern = decode_kernel<D, P, NS, NW>;
+  auto kern = decode_kernel<D, P, NS, NW, CROSS>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -1200,7 +1215,19 @@ cudaError_t hswa_launch_decode(const hswa_handle* h, const CUtensorMap& tm_pool,
   return cudaErrorInvalidValue;
 }
 
-cudaError_t hswa_launch_combine(const DecodeParams& p, cudaStream_t s) {
+cudaError_t hswa_launch_decode_cross(const CUtensorMap& tm_pool, const DecodeParams& p, cudaStream_t s) {
+  if (p.b.B == 0) return cudaSuccess;
+  const int D = p.m.D, P = p.m.P;
+  if (D == 128 && P == 64) return launch_decode_t<128, 64, 3, 3, true>(tm_pool, p, false, s);
+  if (D == 128 && P == 32) return launch_decode_t<128, 32, 3, 3, true>(tm_pool, p, false, s);
+  if (D == 128 && P == 16) return launch_decode_t<128, 16, 3, 3, true>(tm_pool, p, false, s);
+  if (D == 64 && P == 64) return launch_decode_t<64, 64, 3, 3, true>(tm_pool, p, false, s);
+  if (D == 64 && P == 32) return launch_decode_t<64, 32, 3, 3, true>(tm_pool, p, false, s);
+  if (D == 64 && P == 16) return launch_decode_t<64, 16, 3, 3, true>(tm_pool, p, false, s);
+  return cudaErrorInvalidValue;
+}
+
+cudaError_t hswa_launch_combine(const DecodeParams& p, bool cross, cudaStream_t s) {
   const int rows = p.b.B * p.nq * p.m.Hq;
   if (rows == 0) return cudaSuccess;
   const int blocks = (rows * 32 + 127) / 128;
@@ -1214,6 +1241,8 @@ cudaError_t hswa_launch_combine(const DecodeParams& p, cudaStream_t s) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
+  if (cross)
+    return p.m.D == 128 ? cudaLaunchKernelEx(&cfg, combine_kernel<128, true>, p) : cudaLaunchKernelEx(&cfg, combine_kernel<64, true>, p);
   return p.m.D == 128 ? cudaLaunchKernelEx(&cfg, combine_kernel<128>, p) : cudaLaunchKernelEx(&cfg, combine_kernel<64>, p);
 }
 

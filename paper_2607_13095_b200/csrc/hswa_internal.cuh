@@ -115,13 +115,88 @@ struct PrefillParams {
   float2* part_ml;
 };
 
+// Cross attention over an encoder's cached states.  Rows are packed: row rho of (request, KV head) is token rho / G,
+// query head kh * G + rho % G, so that the heads of a group share every K/V tile.
+struct CrossParams {
+  ModelParams m;
+  BatchParams b;
+  const __nv_bfloat16* pool;
+  int64_t num_pages;
+  const __nv_bfloat16* q;  // [T][Hq][D]
+  void* out;               // [T][Hq][D]
+  float* lse;              // [T][Hq] or null
+  int32_t total_q, max_q_len, max_ctx_len;
+  int32_t row_tiles;   // row tiles per (request, KV head)
+  int32_t slices;      // key slices; 1 = write the output directly
+  int32_t slice_len;   // keys per slice (multiple of 128)
+  float* part_o;       // [T * Hq][slices][D]
+  float2* part_ml;     // [T * Hq][slices] (m in log2 units, l; l = 0: the slice holds no key of the row)
+  int32_t* err;
+};
+
+struct WeightsParams {
+  ModelParams m;
+  BatchParams b;
+  const __nv_bfloat16* pool;
+  int64_t num_pages;
+  const __nv_bfloat16* q;  // [T][Hq][D]
+  const float* lse;        // [T][Hq]
+  float* weights;          // [B][Hkv][stride]
+  int64_t stride;
+  float decay;
+  int32_t causal;
+  int32_t max_q_len, max_ctx_len;
+  int32_t* err;
+};
+
+struct SelectParams {
+  int32_t B, Hkv;
+  const int32_t* ctx_len;
+  int32_t max_ctx_len;
+  const float* weights;  // [B][Hkv][stride]
+  int64_t stride;
+  const int32_t* keep_len;
+  int32_t max_keep, protect_first, protect_last;
+  int32_t* keep_idx;  // [B][Hkv][max_keep]
+  int32_t* kept_len;  // [B]
+  int32_t* err;
+};
+
+struct CompactParams {
+  ModelParams m;
+  BatchParams b;
+  __nv_bfloat16* pool;
+  int64_t num_pages;
+  int32_t max_ctx_len;
+  const int32_t* keep_idx;  // [B][Hkv][max_keep]
+  const int32_t* kept_len;  // [B]
+  int32_t max_keep;
+  const int32_t* dst_block_table;  // [B][dst_max_blocks]
+  int32_t dst_max_blocks;
+  const float* weights;  // [B][Hkv][stride] or null
+  int64_t stride;
+  float* weights_out;    // [B][Hkv][out_stride]
+  int64_t out_stride;
+  int32_t* err;
+};
+
 // Launchers implemented in the kernel translation units.
 cudaError_t hswa_launch_append(const AppendParams& p, cudaStream_t s);
 // Slots per TMA box of the persistent ring decode kernel (its tensor map is built with this box height).
 #define HSWA_RING_GRANULE 16
 cudaError_t hswa_launch_decode(const hswa_handle* h, const CUtensorMap& tm_pool, const DecodeParams& p, bool early_start,
                                cudaStream_t s);
-cudaError_t hswa_launch_combine(const DecodeParams& p, cudaStream_t s);
+cudaError_t hswa_launch_combine(const DecodeParams& p, bool cross, cudaStream_t s);
+// Cross attention, one token per request: the streaming decode kernel without a new token
+cudaError_t hswa_launch_decode_cross(const CUtensorMap& tm_pool, const DecodeParams& p, cudaStream_t s);
+// Cross attention, any number of tokens per request: warp-level tile kernel, and the join of key slices
+cudaError_t hswa_launch_cross_mma(const CrossParams& p, cudaStream_t s);
+cudaError_t hswa_launch_cross_combine(const CrossParams& p, cudaStream_t s);
+int hswa_cross_mma_rows();  // packed (token, head) rows per block
+// Eviction: accumulated attention weights, choice of the kept positions, compaction
+cudaError_t hswa_launch_attn_weights(const WeightsParams& p, cudaStream_t s);
+cudaError_t hswa_launch_evict_select(const SelectParams& p, cudaStream_t s);
+cudaError_t hswa_launch_evict_compact(const CompactParams& p, cudaStream_t s);
 // SWA layers whose window fits shared memory: one block per (request, KV head) over a compact copy of the window
 bool hswa_ring_compact_supported(const ModelParams& m, int nq);
 cudaError_t hswa_launch_decode_ring_compact(const hswa_handle* h, const CUtensorMap& tm_pool, const DecodeParams& p,
