@@ -752,7 +752,13 @@ hswa_status hswa_attn_weights(hswa_handle* h, const hswa_layer* layer, const hsw
   p.max_q_len = b->max_q_len;
   p.max_ctx_len = b->max_ctx_len;
   p.err = h->err;
-  return hswa_launch_attn_weights(p, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+  CUtensorMap tm, tm_q;
+  if ((st = make_pool_map(h, layer, &tm)) != HSWA_OK) return st;
+  tm_q = tm;  // a step without rows reads none
+  if (b->total_q > 0 &&
+      (st = make_rows_map(h, q, h->cfg.num_q_heads, b->total_q, hswa_attn_weights_tile_tokens(p.m, p.max_q_len), &tm_q, h->group)) != HSWA_OK)
+    return st;
+  return hswa_launch_attn_weights(tm, tm_q, p, h->num_sms, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
 }
 
 hswa_status hswa_evict_select(hswa_handle* h, int32_t batch, const int32_t* ctx_len, int32_t max_ctx_len, const float* weights,

@@ -1,89 +1,10 @@
-// Eviction from a Full layer's cache by accumulated attention weight: the weights of the cached keys, the choice of the
-// positions that stay, and their move to the head of fresh pages (paper Sec. 3.1.3: pages may be shared between
+// Eviction from a Full layer's cache by accumulated attention weight: the choice of the positions that stay, and their move
+// to the head of fresh pages (paper Sec. 3.1.3: pages may be shared between
 // requests, so kept rows are copied to pages of the request's own, never moved inside pages that another one reads).
 #include "hswa_internal.cuh"
 
 namespace {
 using namespace hswa_dev;
-
-// weights[r][kh][j] = decay * weights[r][kh][j] + sum over the step's tokens i and the heads g of the group of
-// exp(scale q_{i,g}.k_j - lse_{i,g}).  One thread per key: its K row stays in registers, the query rows go through
-// shared memory, and the sum needs no exchange and no atomics.
-constexpr int WK = 128;  // keys per block
-constexpr int WR = 16;   // query rows staged at a time
-
-// Index of the error word for a request that the host's bounds, the block table or the weights do not cover; 0 if fine.
-__device__ __forceinline__ int weights_request_error(const WeightsParams& p, int ctx, int n) {
-  if (ctx < 0 || ctx > p.max_ctx_len) return -1;
-  if (n < 0 || n > p.max_q_len) return -2;
-  const int64_t keys = (int64_t)ctx + (p.causal ? n : 0);
-  return keys > p.stride || keys > (int64_t)p.b.max_blocks * p.m.P ? -3 : 0;
-}
-
-template <int D>
-__global__ void __launch_bounds__(WK) attn_weights_kernel(const WeightsParams p) {
-  __shared__ float sq[WR][D];
-  __shared__ float sl[WR];
-  const ModelParams& M = p.m;
-  const int kh = blockIdx.y, r = blockIdx.z;
-  const int t0 = p.b.q_indptr ? p.b.q_indptr[r] : r;
-  const int n = p.b.q_indptr ? p.b.q_indptr[r + 1] - t0 : 1;
-  const int ctx = p.b.ctx_len[r];
-  const int bad = weights_request_error(p, ctx, n);
-  if (bad != 0) {
-    if (threadIdx.x == 0 && blockIdx.x == 0 && kh == 0) record_error(p.err, HSWA_ERR_BOUNDS, r, bad, bad == -1 ? ctx : bad == -2 ? n : ctx + n);
-    return;
-  }
-  const int kv_len = ctx + (p.causal ? n : 0);
-  const int j0 = blockIdx.x * WK, j = j0 + threadIdx.x;
-  if (j0 >= kv_len) return;
-  uint32_t kr[D / 2];
-  const __nv_bfloat16* krow = nullptr;
-  if (j < kv_len) {
-    const int page = p.b.block_table[(int64_t)r * p.b.max_blocks + j / M.P];
-    if (page < 0 || page >= p.num_pages)
-      record_error(p.err, HSWA_ERR_BOUNDS, r, j / M.P, page);
-    else
-      krow = p.pool + (((int64_t)page * 2 * M.Hkv + kh) * M.P + j % M.P) * D;
-  }
-#pragma unroll
-  for (int c = 0; c < D / 8; ++c) {
-    const uint4 v = krow ? *reinterpret_cast<const uint4*>(krow + c * 8) : make_uint4(0, 0, 0, 0);
-    kr[4 * c] = v.x;
-    kr[4 * c + 1] = v.y;
-    kr[4 * c + 2] = v.z;
-    kr[4 * c + 3] = v.w;
-  }
-  const int rows = n * M.G;
-  float sum = 0.f;
-  for (int row0 = 0; row0 < rows; row0 += WR) {
-    __syncthreads();
-    for (int idx = threadIdx.x; idx < WR * D; idx += WK) {
-      const int row = row0 + idx / D;
-      if (row < rows) sq[idx / D][idx % D] = __bfloat162float(p.q[((int64_t)(t0 + row / M.G) * M.Hq + kh * M.G + row % M.G) * D + idx % D]);
-    }
-    if (threadIdx.x < WR && row0 + (int)threadIdx.x < rows) {
-      const int row = row0 + threadIdx.x;
-      sl[threadIdx.x] = p.lse[(int64_t)(t0 + row / M.G) * M.Hq + kh * M.G + row % M.G];
-    }
-    __syncthreads();
-    for (int i = 0; i < min(WR, rows - row0); ++i) {
-      if (p.causal && j > ctx + (row0 + i) / M.G) continue;
-      if (sl[i] == -INFINITY) continue;  // a row that saw nothing
-      float dot = 0.f;
-#pragma unroll
-      for (int c = 0; c < D / 2; ++c) {
-        const float2 kv = unpack_bf16x2(kr[c]);
-        dot += kv.x * sq[i][2 * c] + kv.y * sq[i][2 * c + 1];
-      }
-      sum += expf(dot * (M.scale_log2 * 0.6931471805599453f) - sl[i]);
-    }
-  }
-  if (j < kv_len) {
-    float* w = p.weights + ((int64_t)r * M.Hkv + kh) * p.stride + j;
-    *w = j < ctx && p.decay != 0.f ? p.decay * *w + sum : sum;
-  }
-}
 
 // ---------------------------------------------------------------------------------------------------------------------
 // Order-preserving map of a weight to 32 bits: NaN lowest, -0 and +0 alike, protected positions above everything.
@@ -207,17 +128,6 @@ __global__ void __launch_bounds__(256) evict_compact_kernel(const CompactParams 
 }
 
 }  // namespace
-
-cudaError_t hswa_launch_attn_weights(const WeightsParams& p, cudaStream_t s) {
-  const int keys = p.max_ctx_len + (p.causal ? p.max_q_len : 0);
-  if (p.b.B == 0 || keys == 0) return cudaSuccess;
-  dim3 grid((keys + WK - 1) / WK, p.m.Hkv, p.b.B);
-  if (p.m.D == 128)
-    attn_weights_kernel<128><<<grid, WK, 0, s>>>(p);
-  else
-    attn_weights_kernel<64><<<grid, WK, 0, s>>>(p);
-  return cudaGetLastError();
-}
 
 cudaError_t hswa_launch_evict_select(const SelectParams& p, cudaStream_t s) {
   if (p.B == 0) return cudaSuccess;
