@@ -7,12 +7,16 @@
 // read from memory once.
 //
 // Bounds.  One row group (a decode step) is bound by reading K.  With many rows the exponentials bound it: 16 per clock
-// and SM against 32 score elements per clock from the tensor core at D = 128.
+// and SM from the special-function units against 32 score elements per clock from the tensor core at D = 128.  The
+// exponentials of the many-row form are therefore shared between the special-function unit and the FMA pipes.
 //
-// Warp roles: warps 0-3 and 4-7 sum the even and the odd key tiles of the block's key range, warp 8 loads (TMA) and stages
-// the rows' log-sum-exps, warp 9 issues the MMAs.  Each of the two summing groups has two TMEM accumulators.  The Q tiles
-// (up to 128 rows) stay in shared memory for the block's whole key range when they all fit (up to 512 rows), else they are
-// streamed from L2 once per pair of key tiles.
+// Warp roles: warps 0-3 and 4-7 sum the even and the odd key tiles of a segment, warp 8 loads (TMA) and stages the rows'
+// log-sum-exps, warp 9 issues the MMAs.  Each of the two summing groups has two TMEM accumulators.
+//
+// Blocks are persistent: all key tiles of the batch, weighted with the Q tiles they meet, are cut into equal shares, and a
+// block walks the segments (request, KV head, range of key tiles) of its share with every pipeline running on across
+// them.  The Q tiles of a segment (up to 128 rows each) stay in shared memory while it lasts when they all fit, else they
+// are streamed from L2 once per pair of key tiles.
 #include "hswa_internal.cuh"
 #include "tc_primitives.cuh"
 
@@ -20,20 +24,25 @@ namespace {
 using namespace hswa_dev;
 
 constexpr int TKEYS = 128;       // keys per tile
-constexpr int THREADS = 320;     // two summing groups, loader, MMA issuer
+// Summing warps per group: four cover the 128 keys of a tile.  The many-row form has twice as many, each with half of the
+// columns: two warps per scheduler leave the pipes idle most of the time behind TMEM reads and dependent steps (100 us on
+// the 64-token observation window of 8 prompts, 78 us with four).
+constexpr int group_warps(bool wide) { return wide ? 8 : 4; }
+constexpr int block_threads(bool wide) { return (2 * group_warps(wide) + 2) * 32; }
 constexpr int MAX_NSQ = 4, MAX_NSK = 6;
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr float NO_ROW = -1e30f;  // in the place of an absent row's value, or of a row's that saw nothing: 2^that = 0
+constexpr int FMA_SHARE = 3;     // of eight exponentials of the many-row form, those taken on the FMA pipes
 
 // Barriers
 enum { B_QFULL = 0, B_LFULL = B_QFULL + MAX_NSQ, B_QEMPTY = B_LFULL + MAX_NSQ, B_KFULL = B_QEMPTY + MAX_NSQ,
-       B_KEMPTY = B_KFULL + MAX_NSK, B_SFULL = B_KEMPTY + MAX_NSK /* [group][buffer] */, B_SEMPTY = B_SFULL + 4, NUM_BARS = B_SEMPTY + 4 };
+       B_KEMPTY = B_KFULL + MAX_NSK, B_SFULL = B_KEMPTY + MAX_NSK /* [group][buffer] */, B_SEMPTY = B_SFULL + 4,
+       B_PFULL = B_SEMPTY + 4 /* [group][buffer]: the upper columns' sums are in TMEM */, NUM_BARS = B_PFULL + 4 };
 
 struct WeightsPlan {
   int n_cols;       // N of the MMA: rows of a Q tile, rounded up
   int tile_tokens;  // tokens per Q tile
   int nsq, nsk;     // Q and K stages
-  int resident;     // the Q tiles of a request all fit the Q stages
-  int block_tiles;  // key tiles per block
   int tmem_cols;
 };
 
@@ -48,81 +57,206 @@ __device__ __forceinline__ int weights_request_error(const WeightsParams& p, int
 // A warp's bounded wait: one answer for all lanes.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)); }
 
+// 2^x for a pair of columns, added to acc, on the FMA and integer pipes instead of the special-function unit: x = n + f with
+// n the nearest integer (found by adding 1.5 * 2^23, which leaves n in the low mantissa bits; + 127 makes them the exponent
+// field of 2^n), 2^f by a polynomial of degree 5 that is minimax in the relative error on [-1/2, 1/2] (Remez exchange;
+// 2.1e-7 at most with its coefficients and steps in fp32), and the product with 2^n is the fma that adds it to the sum.
+// Finite x down to any size (2^n is 0 from -127 on), up to 127: a probability's x is at most 0 but for rounding.
+__device__ __forceinline__ float2 add_exp2_fma(float2 x, float2 acc) {
+  const float2 magic = make_float2(12583039.f, 12583039.f), neg_magic = make_float2(-12583039.f, -12583039.f);
+  const float2 t = __fadd2_rn(x, magic);
+  const float2 n = __fadd2_rn(t, neg_magic);
+  const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
+  float2 q = make_float2(0.0013276467798277736f, 0.0013276467798277736f);
+  q = __ffma2_rn(q, f, make_float2(0.009675540961325169f, 0.009675540961325169f));
+  q = __ffma2_rn(q, f, make_float2(0.05550713464617729f, 0.05550713464617729f));
+  q = __ffma2_rn(q, f, make_float2(0.24022120237350464f, 0.24022120237350464f));
+  q = __ffma2_rn(q, f, make_float2(0.6931469440460205f, 0.6931469440460205f));
+  q = __ffma2_rn(q, f, make_float2(1.0000001192092896f, 1.0000001192092896f));
+  const int low = 0x4b400000;  // the bits of 1.5 * 2^23: an exponent field of 0
+  const float2 scale = make_float2(__int_as_float(max(__float_as_int(t.x), low) << 23), __int_as_float(max(__float_as_int(t.y), low) << 23));
+  return __ffma2_rn(q, scale, acc);
+}
+
 // One thread's sum over CHUNK score columns.  nl: minus the rows' log-sum-exps in log2 units; a column that does not count
-// (an absent row) has minus infinity there and a finite score.  MASKED: columns outside [c_lo, c_hi) are dropped whatever
-// their score is.
-template <int CHUNK, bool MASKED>
+// (an absent row) has NO_ROW there and a finite score.  MASKED: columns outside [c_lo, c_hi) are dropped whatever
+// their score is.  FMA_OF_8: of every eight column pairs, how many take their exponential on the FMA pipes.
+template <int CHUNK, bool MASKED, int FMA_OF_8>
 __device__ __forceinline__ void sum_chunk(const uint32_t (&v)[CHUNK], const float* nl, float scale_log2, int c0, int c_lo, int c_hi,
                                           float2 (&acc)[4]) {
   const float2 sc2 = make_float2(scale_log2, scale_log2);
 #pragma unroll
   for (int k = 0; k < CHUNK; k += 4) {
     const float4 l4 = *reinterpret_cast<const float4*>(nl + k);
-    const float2 x0 = __ffma2_rn(make_float2(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), sc2, make_float2(l4.x, l4.y));
-    const float2 x1 = __ffma2_rn(make_float2(__uint_as_float(v[k + 2]), __uint_as_float(v[k + 3])), sc2, make_float2(l4.z, l4.w));
-    float2 e0 = make_float2(fast_exp2(x0.x), fast_exp2(x0.y)), e1 = make_float2(fast_exp2(x1.x), fast_exp2(x1.y));
-    if constexpr (MASKED) {
-      e0.x = c0 + k >= c_lo && c0 + k < c_hi ? e0.x : 0.f;
-      e0.y = c0 + k + 1 >= c_lo && c0 + k + 1 < c_hi ? e0.y : 0.f;
-      e1.x = c0 + k + 2 >= c_lo && c0 + k + 2 < c_hi ? e1.x : 0.f;
-      e1.y = c0 + k + 3 >= c_lo && c0 + k + 3 < c_hi ? e1.y : 0.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int c = k + 2 * h, pair = c >> 1;
+      const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2,
+                                  h ? make_float2(l4.z, l4.w) : make_float2(l4.x, l4.y));
+      float2& a = acc[pair & 3];
+      if (!MASKED && ((pair & 7) * FMA_OF_8) % 8 + FMA_OF_8 > 7) {  // spread evenly
+        a = add_exp2_fma(x, a);
+      } else {
+        float2 e = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+        if constexpr (MASKED) {
+          e.x = c0 + c >= c_lo && c0 + c < c_hi ? e.x : 0.f;
+          e.y = c0 + c + 1 >= c_lo && c0 + c + 1 < c_hi ? e.y : 0.f;
+        }
+        a = __fadd2_rn(a, e);
+      }
     }
-    acc[(k >> 1) & 3] = __fadd2_rn(acc[(k >> 1) & 3], e0);
-    acc[((k >> 1) + 1) & 3] = __fadd2_rn(acc[((k >> 1) + 1) & 3], e1);
   }
 }
 
-// WIDE: one block per SM, Q tiles of up to 128 rows; else two blocks per SM (at most 64 rows), which hide each other's
-// start and end.
+// Position in a ring of stages: the slot, and the parity of the phase in which it is next filled.
+struct Ring {
+  int slot = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void step(int stages) {
+    if (++slot == stages) {
+      slot = 0;
+      phase ^= 1u;
+    }
+  }
+  __device__ __forceinline__ void step(int stages, int by) {  // by <= stages
+    slot += by;
+    if (slot >= stages) {
+      slot -= stages;
+      phase ^= 1u;
+    }
+  }
+};
+
+// A stretch of the block's share: key tiles [t_lo, t_hi) of one (request, KV head).
+struct Segment {
+  int r, kh, t0, n, ctx, kv_len, t_lo, t_hi, n_qt;
+};
+
+// Walks a block's share [lo, hi) of the batch's total cost.  A key tile costs one unit per 32 rows of the request (at least
+// one), the first tile of a (request, KV head) twice that (its Q tiles come in, and the pipeline runs empty behind the
+// segment before: 4 us against 3 for a tile of 512 rows).  The tiles follow one another by KV head; a tile belongs to the share in which it begins.  Every role walks by itself.
+struct Walker {
+  int r;
+  int64_t base, lo, hi;  // base: cost of all requests before r
+  int kh;
+
+  __device__ __forceinline__ static void request(const WeightsParams& p, const WeightsPlan& pl, int r, Segment& s, int& tiles, int& q) {
+    s.r = r;
+    s.t0 = p.b.q_indptr ? p.b.q_indptr[r] : r;
+    s.n = p.b.q_indptr ? p.b.q_indptr[r + 1] - s.t0 : 1;
+    s.ctx = p.b.ctx_len[r];
+    tiles = 0;
+    q = 1;
+    if (weights_request_error(p, s.ctx, s.n) != 0) return;
+    s.kv_len = s.ctx + (p.causal ? s.n : 0);
+    s.n_qt = (s.n + pl.tile_tokens - 1) / pl.tile_tokens;
+    tiles = (s.kv_len + TKEYS - 1) / TKEYS;
+    q = max(1, (s.n_qt - 1) * (pl.tile_tokens * p.m.G + 31) / 32 + ((s.n - (s.n_qt - 1) * pl.tile_tokens) * p.m.G + 31) / 32);
+  }
+
+  // Tiles of a (request, KV head) that begin before cost c of it: tile 0 at 0, tile i at (i + 1) q.
+  __device__ __forceinline__ static int tiles_before(int64_t c, int tiles, int q) {
+    if (c <= 0) return 0;
+    const int64_t i = (c + q - 1) / q - 1;
+    return (int)(i < 1 ? 1 : (i < tiles ? i : tiles));
+  }
+
+  __device__ __forceinline__ bool next(const WeightsParams& p, const WeightsPlan& pl, Segment& s) {
+    for (; r < p.b.B && base < hi; ++r, kh = 0) {
+      int tiles, q;
+      request(p, pl, r, s, tiles, q);
+      const int64_t head_cost = tiles > 0 ? (int64_t)(tiles + 1) * q : 0, all = head_cost * p.m.Hkv;
+      if (lo < base + all) {
+        if (lo > base + kh * head_cost) kh = (int)((lo - base) / head_cost);
+        for (; kh < p.m.Hkv; ++kh) {
+          const int64_t c0 = base + kh * head_cost;
+          if (c0 >= hi) return false;
+          s.t_lo = tiles_before(lo - c0, tiles, q);
+          s.t_hi = tiles_before(hi - c0, tiles, q);
+          if (s.t_lo < s.t_hi) {
+            s.kh = kh++;
+            return true;
+          }
+        }
+      }
+      base += all;
+    }
+    return false;
+  }
+};
+
+// WIDE: one block per SM, Q tiles of up to 128 rows; else two blocks per SM (at most 64 rows).
 template <int D, bool WIDE>
-__global__ void __launch_bounds__(THREADS, WIDE ? 1 : 2)
+__global__ void __launch_bounds__(block_threads(WIDE), WIDE ? 1 : 2)
 attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_constant__ CUtensorMap tm_q, const WeightsParams p,
                     const WeightsPlan pl) {
   constexpr int HALVES = D / 64;
   constexpr int K_HALF = TKEYS * 128, K_BYTES = HALVES * K_HALF;
+  constexpr int GW = group_warps(WIDE), LOADER = 2 * GW, ISSUER = 2 * GW + 1, THREADS = block_threads(WIDE);
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sbase = smem_u32(smem);
   const ModelParams& M = p.m;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int kh = blockIdx.y, r = blockIdx.z;
   const int N = pl.n_cols;
   const uint32_t q_half = (uint32_t)N * 128, q_bytes = q_half * HALVES;
   const uint32_t off_k = pl.nsq * q_bytes, off_lse = off_k + pl.nsk * K_BYTES;
   float* s_nl = reinterpret_cast<float*>(smem + off_lse);                            // [nsq][N]
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + off_lse + pl.nsq * N * 4);     // [NUM_BARS]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + NUM_BARS);
+  int64_t* s_base = reinterpret_cast<int64_t*>(bars + NUM_BARS);                     // [2]: base and total
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_base + 2);
+  int* s_r = reinterpret_cast<int*>(tmem_slot + 1);
   auto bar = [&](int i) { return smem_u32(&bars[i]); };
 
-  const int t0 = p.b.q_indptr ? p.b.q_indptr[r] : r;
-  const int n = p.b.q_indptr ? p.b.q_indptr[r + 1] - t0 : 1;
-  const int ctx = p.b.ctx_len[r];
-  const int bad = weights_request_error(p, ctx, n);
-  if (bad != 0) {
-    if (threadIdx.x == 0 && blockIdx.x == 0 && kh == 0) record_error(p.err, HSWA_ERR_BOUNDS, r, bad, bad == -1 ? ctx : bad == -2 ? n : ctx + n);
-    return;
+  // ---- this block's share ----
+  if (warp == 0) {
+    auto cost_of = [&](int r) {
+      if (r >= p.b.B) return (int64_t)0;
+      Segment s;
+      int tiles, q;
+      Walker::request(p, pl, r, s, tiles, q);
+      return tiles > 0 ? (int64_t)(tiles + 1) * q * M.Hkv : (int64_t)0;
+    };
+    int64_t total = 0;
+    for (int r = lane; r < p.b.B; r += 32) total += cost_of(r);
+#pragma unroll
+    for (int sh = 16; sh; sh >>= 1) total += __shfl_xor_sync(0xffffffffu, total, sh);
+    const int64_t lo = total * blockIdx.x / gridDim.x;
+    int64_t base = 0;
+    int at = p.b.B;
+    for (int r0 = 0; r0 < p.b.B; r0 += 32) {
+      const int64_t c = cost_of(r0 + lane);
+      int64_t incl = c;
+#pragma unroll
+      for (int sh = 1; sh < 32; sh <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, incl, sh);
+        if (lane >= sh) incl += v;
+      }
+      const unsigned hit = __ballot_sync(0xffffffffu, base + incl > lo);  // the first request whose tiles reach past lo
+      if (hit) {
+        const int sel = __ffs(hit) - 1;
+        at = r0 + sel;
+        base += __shfl_sync(0xffffffffu, incl - c, sel);
+        break;
+      }
+      base += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) {
+      s_base[0] = base;
+      s_base[1] = total;
+      *s_r = at;
+    }
+  } else if (warp == 1 && blockIdx.x == 0) {
+    for (int r = lane; r < p.b.B; r += 32) {
+      const int t0 = p.b.q_indptr ? p.b.q_indptr[r] : r, n = p.b.q_indptr ? p.b.q_indptr[r + 1] - t0 : 1, ctx = p.b.ctx_len[r];
+      const int bad = weights_request_error(p, ctx, n);
+      if (bad != 0) record_error(p.err, HSWA_ERR_BOUNDS, r, bad, bad == -1 ? ctx : bad == -2 ? n : ctx + n);
+    }
   }
-  const int kv_len = ctx + (p.causal ? n : 0);
-  const int k_begin = blockIdx.x * pl.block_tiles * TKEYS;
-  if (k_begin >= kv_len) return;
-  const int k_end = min(kv_len, k_begin + pl.block_tiles * TKEYS);
-  const int n_tiles = (k_end - k_begin + TKEYS - 1) / TKEYS;
-  const int n_qt = (n + pl.tile_tokens - 1) / pl.tile_tokens;
-  float* w_row = p.weights + ((int64_t)r * M.Hkv + kh) * p.stride;
-  if (n == 0) {  // no rows: the old weights only decay
-    for (int j = k_begin + threadIdx.x; j < k_end; j += THREADS) w_row[j] = p.decay != 0.f ? p.decay * w_row[j] : 0.f;
-    return;
-  }
-  // Q tiles that come before the first token which sees any key of tile t (causal: token i sees j <= ctx + i)
-  auto first_qt = [&](int t) {
-    const int over = k_begin + t * TKEYS - ctx;
-    return p.causal && over > 0 ? over / pl.tile_tokens : 0;
-  };
-
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 64) {
     for (int i = 0; i < pl.nsq; ++i) {
       mbar_init(bar(B_QFULL + i), 1);
       mbar_init(bar(B_LFULL + i), 1);
-      mbar_init(bar(B_QEMPTY + i), 9);  // the MMA commit and eight summing warps
+      mbar_init(bar(B_QEMPTY + i), 1 + 2 * GW);  // the MMA commit and the summing warps
     }
     for (int i = 0; i < pl.nsk; ++i) {
       mbar_init(bar(B_KFULL + i), 1);
@@ -130,19 +264,22 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar(B_SFULL + i), 1);
-      mbar_init(bar(B_SEMPTY + i), 4);
+      mbar_init(bar(B_SEMPTY + i), GW);
+      mbar_init(bar(B_PFULL + i), 4);
     }
     mbar_fence_init();
+    tma_prefetch_desc(&tm_pool);
+    tma_prefetch_desc(&tm_q);
     if (sbase & 1023u) record_error(p.err, HSWA_ERR_CUDA, -1, (int)(sbase & 1023u), 16);  // tiles would be misread
   }
-  // rows of a Q tile that no load fills (a group that does not divide 128): zeros, so that their scores are finite
+  // rows of a Q tile that no load fills (a group that does not divide the tile): zeros, so that their scores are finite
   const int q_rows = pl.tile_tokens * M.G;
   for (int i = threadIdx.x; i < pl.nsq * HALVES * (N - q_rows) * 8; i += THREADS) {
     const int ch = i & 7, row = q_rows + (i >> 3) % (N - q_rows), hs = (i >> 3) / (N - q_rows);
     *reinterpret_cast<uint4*>(smem + (hs / HALVES) * q_bytes + (hs % HALVES) * q_half + row * 128 + ch * 16) = make_uint4(0, 0, 0, 0);
   }
   fence_proxy_async_smem();
-  if (warp == 9) {
+  if (warp == ISSUER) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(pl.tmem_cols)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -151,243 +288,319 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  Walker walk;
+  walk.r = *s_r;
+  walk.kh = 0;
+  walk.base = s_base[0];
+  walk.lo = s_base[1] * blockIdx.x / gridDim.x;
+  walk.hi = s_base[1] * (blockIdx.x + 1) / gridDim.x;
+  Segment sg;
+  // first Q tile with a token that sees any key of tile t (causal: token i sees j <= ctx + i)
+  auto first_qt = [&](int t) {
+    const int over = t * TKEYS - sg.ctx;
+    return p.causal && over > 0 ? over / pl.tile_tokens : 0;
+  };
 
-  if (warp == 8) {
+  if (warp == LOADER) {
     // ======================= loader =======================
-    if (lane == 0) {
-      tma_prefetch_desc(&tm_pool);
-      tma_prefetch_desc(&tm_q);
-    }
-    const int n_pages = (k_end - k_begin + M.P - 1) / M.P, ppt = TKEYS / M.P;
-    const int32_t* tbl = p.b.block_table + (int64_t)r * p.b.max_blocks + k_begin / M.P;
-    int pid_next = lane < ppt && lane < n_pages ? tbl[lane] : 0;
+    const int ppt = TKEYS / M.P;
     bool ok = true;
-    auto load_k = [&](int t) {
-      if (t >= n_tiles || !ok) return;
-      const int stage = t % pl.nsk;
-      const int pid = pid_next, pgi = t * ppt + lane;
-      const int nx = pgi + ppt;
-      pid_next = lane < ppt && nx < n_pages ? tbl[nx] : 0;
-      if (t >= pl.nsk && !warp_wait(bar(B_KEMPTY + stage), ((t / pl.nsk) - 1) & 1)) {
-        if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, t, 90);
-        ok = false;
-        return;
-      }
-      bool mine = lane < ppt && pgi < n_pages;
-      if (mine && (pid < 0 || pid >= p.num_pages)) {
-        record_error(p.err, HSWA_ERR_BOUNDS, r, k_begin / M.P + pgi, pid);
-        mine = false;
-      }
-      const int pages = __popc(__ballot_sync(0xffffffffu, mine));
-      if (lane == 0) {
-        if (pages == 0)
-          mbar_arrive(bar(B_KFULL + stage));
-        else
-          mbar_arrive_expect_tx(bar(B_KFULL + stage), pages * M.P * 128 * HALVES);
-      }
-      __syncwarp();
-      if (mine) {
-        const uint32_t dst = sbase + off_k + stage * K_BYTES + lane * M.P * 128;
+    Ring kr, qr;
+    bool k_used = false, q_used = false;  // the ring has been filled once: its slots have to be released first
+    while (ok && walk.next(p, pl, sg)) {
+      if (sg.n == 0) continue;
+      const int32_t* tbl = p.b.block_table + (int64_t)sg.r * p.b.max_blocks;
+      const int n_pages = (sg.kv_len + M.P - 1) / M.P;
+      auto page_of = [&](int t) { return lane < ppt && t * ppt + lane < n_pages ? tbl[t * ppt + lane] : 0; };
+      int pid_next = page_of(sg.t_lo);
+      auto load_k = [&](int t) {
+        if (t >= sg.t_hi || !ok) return;
+        const int stage = kr.slot, pid = pid_next, pgi = t * ppt + lane;
+        pid_next = page_of(t + 1);
+        if (k_used && !warp_wait(bar(B_KEMPTY + stage), kr.phase ^ 1u)) {
+          if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, sg.r, t, 90);
+          ok = false;
+          return;
+        }
+        bool mine = lane < ppt && pgi < n_pages;
+        if (mine && (pid < 0 || pid >= p.num_pages)) {
+          record_error(p.err, HSWA_ERR_BOUNDS, sg.r, pgi, pid);
+          mine = false;
+        }
+        const int pages = __popc(__ballot_sync(0xffffffffu, mine));
+        if (lane == 0) {
+          if (pages == 0)
+            mbar_arrive(bar(B_KFULL + stage));
+          else
+            mbar_arrive_expect_tx(bar(B_KFULL + stage), pages * M.P * 128 * HALVES);
+        }
+        __syncwarp();
+        if (mine) {
+          const uint32_t dst = sbase + off_k + stage * K_BYTES + lane * M.P * 128;
 #pragma unroll
-        for (int hf = 0; hf < HALVES; ++hf) tma_load_4d(dst + hf * K_HALF, &tm_pool, bar(B_KFULL + stage), hf * 64, 0, kh, pid);
-      }
-      __syncwarp();
-    };
-    // lane's four rows of Q tile qt: minus their log-sum-exps in log2 units (absent rows, and rows that saw nothing: minus
-    // infinity, so that they add exp2(-inf) = 0)
-    auto fetch_lse = [&](int qt, float (&x)[4]) {
+          for (int hf = 0; hf < HALVES; ++hf) tma_load_4d(dst + hf * K_HALF, &tm_pool, bar(B_KFULL + stage), hf * 64, 0, sg.kh, pid);
+        }
+        __syncwarp();
+        kr.step(pl.nsk);
+        k_used |= kr.slot == 0;
+      };
+      // lane's four rows of Q tile qt: minus their log-sum-exps in log2 units
+      float x[4];
+      auto fetch_lse = [&](int qt) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int col = u * 32 + lane, tok = qt * pl.tile_tokens + col / M.G;
-        const float v = col < q_rows && tok < n ? p.lse[(int64_t)(t0 + tok) * M.Hq + kh * M.G + col % M.G] : -INFINITY;
-        x[u] = v == -INFINITY ? -INFINITY : -v * LOG2E;
-      }
-    };
-    auto load_q = [&](int qt, int stage, const float (&x)[4]) {
-      if (lane == 0) {
-        mbar_arrive_expect_tx(bar(B_QFULL + stage), q_rows * 128 * HALVES);
+        for (int u = 0; u < 4; ++u) {
+          const int col = u * 32 + lane, tok = qt * pl.tile_tokens + col / M.G;
+          const float v = col < q_rows && tok < sg.n ? p.lse[(int64_t)(sg.t0 + tok) * M.Hq + sg.kh * M.G + col % M.G] : -INFINITY;
+          x[u] = v == -INFINITY ? NO_ROW : -v * LOG2E;
+        }
+      };
+      auto load_q = [&](int qt, int next_qt) {
+        const int stage = qr.slot;
+        if (q_used && !warp_wait(bar(B_QEMPTY + stage), qr.phase ^ 1u)) {
+          if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, sg.r, qt, 91);
+          ok = false;
+          return;
+        }
+        if (lane == 0) {
+          mbar_arrive_expect_tx(bar(B_QFULL + stage), q_rows * 128 * HALVES);
 #pragma unroll
-        for (int hf = 0; hf < HALVES; ++hf)
-          tma_load_3d(sbase + stage * q_bytes + hf * q_half, &tm_q, bar(B_QFULL + stage), hf * 64, kh * M.G, t0 + qt * pl.tile_tokens);
-      }
+          for (int hf = 0; hf < HALVES; ++hf)
+            tma_load_3d(sbase + stage * q_bytes + hf * q_half, &tm_q, bar(B_QFULL + stage), hf * 64, sg.kh * M.G, sg.t0 + qt * pl.tile_tokens);
+        }
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (u * 32 + lane < N) s_nl[stage * N + u * 32 + lane] = x[u];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(B_LFULL + stage));
-    };
-    float x[4];
-    if (pl.resident) {
-      load_k(0);
-      for (int qt = 0; qt < n_qt; ++qt) {
-        fetch_lse(qt, x);
-        load_q(qt, qt, x);
-        if (qt == 0) load_k(1);
-      }
-      for (int t = 2; t < n_tiles && ok; ++t) load_k(t);
-    } else {
-      load_k(0);
-      load_k(1);
-      int qi = 0;
-      fetch_lse(first_qt(0), x);
-      for (int t = 0; t < n_tiles && ok; t += 2) {
-        const int lo = first_qt(t);
-        for (int qt = lo; qt < n_qt && ok; ++qt, ++qi) {
-          const int stage = qi % pl.nsq;
-          if (qi >= pl.nsq && !warp_wait(bar(B_QEMPTY + stage), ((qi / pl.nsq) - 1) & 1)) {
-            if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, qi, 91);
-            ok = false;
-            break;
-          }
-          load_q(qt, stage, x);
-          fetch_lse(qt + 1 < n_qt ? qt + 1 : first_qt(t + 2), x);  // the next one's values are under way meanwhile
-          if (qt == lo) {  // the next pair of key tiles, behind this pair's first Q tile
-            load_k(t + 2);
-            load_k(t + 3);
+        for (int u = 0; u < 4; ++u)
+          if (u * 32 + lane < N) s_nl[stage * N + u * 32 + lane] = x[u];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_LFULL + stage));
+        if (next_qt < sg.n_qt) fetch_lse(next_qt);  // under way while other things are loaded
+        qr.step(pl.nsq);
+        q_used |= qr.slot == 0;
+      };
+      const int lo = first_qt(sg.t_lo);
+      fetch_lse(lo);
+      load_k(sg.t_lo);
+      if (sg.n_qt - lo <= pl.nsq) {
+        for (int qt = lo; qt < sg.n_qt && ok; ++qt) {
+          load_q(qt, qt + 1);
+          if (qt == lo) load_k(sg.t_lo + 1);
+        }
+        for (int t = sg.t_lo + 2; t < sg.t_hi && ok; ++t) load_k(t);
+      } else {
+        load_k(sg.t_lo + 1);
+        for (int t = sg.t_lo; t < sg.t_hi && ok; t += 2) {
+          const int first = first_qt(t), then = t + 2 < sg.t_hi ? first_qt(t + 2) : sg.n_qt;
+          for (int qt = first; qt < sg.n_qt && ok; ++qt) {
+            load_q(qt, qt + 1 < sg.n_qt ? qt + 1 : then);
+            if (qt == first) {  // the next pair of key tiles, behind this pair's first Q tile
+              load_k(t + 2);
+              load_k(t + 3);
+            }
           }
         }
       }
     }
-  } else if (warp == 9) {
+  } else if (warp == ISSUER) {
     // ======================= MMA issuer =======================
-    const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(TKEYS >> 4) << 24);
+    const uint32_t idesc0 = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TKEYS >> 4) << 24);
     const uint64_t dQ0 = smem_desc(sbase, 16), dK0 = smem_desc(sbase + off_k, 16);
     bool ok = true;
-    int qi = 0, units[2] = {0, 0};
-    for (int t = 0; t < n_tiles && ok; t += 2) {
-      const int lo = first_qt(t);
-      for (int qt = lo; qt < n_qt && ok; ++qt, ++qi) {
-        const int qs = pl.resident ? qt : qi % pl.nsq;
-        ok = warp_wait(bar(B_QFULL + qs), pl.resident ? 0 : (qi / pl.nsq) & 1);
+    Ring kr, qr;
+    int units[2] = {0, 0};
+    while (ok && walk.next(p, pl, sg)) {
+      if (sg.n == 0) continue;
+      const int lo = first_qt(sg.t_lo);
+      const bool resident = sg.n_qt - lo <= pl.nsq;
+      for (int t = sg.t_lo; t < sg.t_hi && ok; t += 2) {
+        const int first = first_qt(t);
+        Ring k2 = kr, q = qr;  // the pair's second K tile; resident: the segment's Q tiles from its first one on
+        k2.step(pl.nsk);
+        if (resident) q.step(pl.nsq, first - lo);
+        for (int qt = first; qt < sg.n_qt && ok; ++qt) {
+          const int qs = q.slot;
+          if (!resident || t == sg.t_lo) ok = warp_wait(bar(B_QFULL + qs), q.phase);
+          // a request's last Q tile: no more columns than the sums look at
+          const int cols = min(pl.tile_tokens, sg.n - qt * pl.tile_tokens) * M.G;
+          const uint32_t idesc = idesc0 | ((uint32_t)(min(N, (cols + 31) & ~31) >> 3) << 17);
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          if (t + g >= n_tiles || !ok) continue;
-          const int ks = (t + g) % pl.nsk, buf = units[g] & 1;
-          if (qt == lo) ok = warp_wait(bar(B_KFULL + ks), ((t + g) / pl.nsk) & 1);
-          if (ok && units[g] >= 2) ok = warp_wait(bar(B_SEMPTY + g * 2 + buf), ((units[g] >> 1) - 1) & 1);
-          if (!ok) continue;
-          tc_fence_after();
-          if (elect_one()) {
-            const uint64_t dk = desc_advance(dK0, ks * K_BYTES), dq = desc_advance(dQ0, qs * q_bytes);
+          for (int g = 0; g < 2; ++g) {
+            if (t + g >= sg.t_hi || !ok) continue;
+            const int ks = g ? k2.slot : kr.slot, buf = units[g] & 1;
+            if (qt == first) ok = warp_wait(bar(B_KFULL + ks), g ? k2.phase : kr.phase);
+            if (ok && units[g] >= 2) ok = warp_wait(bar(B_SEMPTY + g * 2 + buf), ((units[g] >> 1) - 1) & 1);
+            if (!ok) continue;
+            tc_fence_after();
+            if (elect_one()) {
+              const uint64_t dk = desc_advance(dK0, ks * K_BYTES), dq = desc_advance(dQ0, qs * q_bytes);
 #pragma unroll
-            for (int s = 0; s < D / 16; ++s)
-              tc_mma_ss(tmem + (g * 2 + buf) * N, desc_advance(dk, (s >> 2) * K_HALF + (s & 3) * 32),
-                        desc_advance(dq, (s >> 2) * q_half + (s & 3) * 32), idesc, s > 0);
-            tc_commit(bar(B_SFULL + g * 2 + buf));
-            if (qt == n_qt - 1) tc_commit(bar(B_KEMPTY + ks));
+              for (int s = 0; s < D / 16; ++s)
+                tc_mma_ss(tmem + (g * 2 + buf) * N, desc_advance(dk, (s >> 2) * K_HALF + (s & 3) * 32),
+                          desc_advance(dq, (s >> 2) * q_half + (s & 3) * 32), idesc, s > 0);
+              tc_commit(bar(B_SFULL + g * 2 + buf));
+              if (qt == sg.n_qt - 1) tc_commit(bar(B_KEMPTY + ks));
+            }
+            __syncwarp();
+            ++units[g];
           }
-          __syncwarp();
-          ++units[g];
+          if (ok && !resident) {
+            if (elect_one()) tc_commit(bar(B_QEMPTY + qs));
+            __syncwarp();
+          }
+          q.step(pl.nsq);
         }
-        if (ok && !pl.resident) {
-          if (elect_one()) tc_commit(bar(B_QEMPTY + qs));
+        if (!resident) qr = q;
+        kr = k2;
+        if (t + 1 < sg.t_hi) kr.step(pl.nsk);
+      }
+      if (ok && resident) {
+        for (int qt = lo; qt < sg.n_qt; ++qt) {
+          if (elect_one()) tc_commit(bar(B_QEMPTY + qr.slot));
           __syncwarp();
+          qr.step(pl.nsq);
         }
       }
     }
-    if (!ok && lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, qi, 92);
+    if (!ok && lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, sg.r, sg.kh, 92);
   } else {
     // ======================= sums =======================
-    const int g = warp >> 2, quad = warp & 3;
+    const int g = warp / GW, half = (warp % GW) >> 2, quad = warp & 3;
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     bool ok = true;
-    int qi = 0, units = 0;
-    uint32_t seen_l = 0;  // resident: bit qt = the tile's log-sum-exps have been waited for
-    float old_next = 0.f;
-    auto fetch_old = [&](int t) {
-      const int j = k_begin + t * TKEYS + quad * 32 + lane;
-      return t < n_tiles && j < k_end && j < ctx && p.decay != 0.f ? w_row[j] : 0.f;
-    };
-    old_next = fetch_old(g);
-    for (int t = 0; t < n_tiles && ok; t += 2) {
-      const bool mine = t + g < n_tiles;
-      const int j = k_begin + (t + g) * TKEYS + quad * 32 + lane;
-      const float old = old_next;
-      old_next = fetch_old(t + 2 + g);
-      const int last_key = k_begin + (t + g) * TKEYS + TKEYS - 1;
-      float sum = 0.f;
-      for (int qt = first_qt(t); qt < n_qt && ok; ++qt, ++qi) {
-        const int qs = pl.resident ? qt : qi % pl.nsq;
-        if (!pl.resident) {
-          ok = warp_wait(bar(B_LFULL + qs), (qi / pl.nsq) & 1);
-        } else if (!((seen_l >> qt) & 1u)) {
-          ok = warp_wait(bar(B_LFULL + qs), 0);
-          seen_l |= 1u << qt;
-        }
-        if (mine) {
-          const int buf = units & 1;
-          if (ok) ok = warp_wait(bar(B_SFULL + g * 2 + buf), (units >> 1) & 1);
-          if (!ok) break;
-          ++units;
-          tc_fence_after();
-          const uint32_t ts = tmem + lane_addr + (g * 2 + buf) * N;
-          const float* nl = s_nl + qs * N;
-          const int tok0 = qt * pl.tile_tokens;
-          const int cols = min(pl.tile_tokens, n - tok0) * M.G;
-          // rows of another request behind this one's last token, or keys ahead of some of the tile's tokens
-          const bool masked = cols < q_rows || (p.causal && last_key > ctx + tok0);
-          const int c_lo = p.causal ? (j - ctx - tok0) * M.G : 0;
-          float2 acc[4];
+    Ring qr;
+    int units = 0;
+    uint32_t joined = 0;  // bit b: parity of the next joining in accumulator b
+    while (ok && walk.next(p, pl, sg)) {
+      float* w_row = p.weights + ((int64_t)sg.r * M.Hkv + sg.kh) * p.stride;
+      const int own = g * TKEYS + quad * 32 + lane;
+      auto fetch_old = [&](int t) {  // positions of this step start at nothing
+        const int j = t * TKEYS + own;
+        return half == 0 && t + g < sg.t_hi && j < sg.ctx && p.decay != 0.f ? w_row[j] : 0.f;
+      };
+      float old_next = fetch_old(sg.t_lo);
+      const int lo = first_qt(sg.t_lo);
+      const bool resident = sg.n_qt - lo <= pl.nsq;
+      for (int t = sg.t_lo; t < sg.t_hi && ok; t += 2) {
+        const bool mine = t + g < sg.t_hi;
+        const int j = t * TKEYS + own;
+        const float old = old_next;
+        old_next = fetch_old(t + 2);
+        float sum = 0.f;
+        const int first = first_qt(t);
+        Ring q = qr;
+        if (resident) q.step(pl.nsq, first - lo);
+        for (int qt = first; qt < sg.n_qt && ok; ++qt) {
+          const int qs = q.slot;
+          if (!resident || t == sg.t_lo) ok = warp_wait(bar(B_LFULL + qs), q.phase);
+          if (mine) {
+            const int buf = units & 1;
+            if (ok) ok = warp_wait(bar(B_SFULL + g * 2 + buf), (units >> 1) & 1);
+            if (!ok) break;
+            ++units;
+            tc_fence_after();
+            const uint32_t ts = tmem + lane_addr + (g * 2 + buf) * N;
+            const float* nl = s_nl + qs * N;
+            const int tok0 = qt * pl.tile_tokens;
+            const int cols = min(pl.tile_tokens, sg.n - tok0) * M.G;
+            const int full_cols = cols == q_rows ? N : cols;  // (the rows up to N are zeros there)
+            // Columns [c_lo, cols) count: behind cols are rows of another request, before c_lo tokens that come before the
+            // key.  Chunks that every lane of the warp sees whole take the short way, chunks that none sees are passed over.
+            const int c_lo = p.causal ? (j - sg.ctx - tok0) * M.G : 0;
+            const int warp_lo = max(0, __shfl_sync(0xffffffffu, c_lo, 0)), warp_hi = __shfl_sync(0xffffffffu, c_lo, 31);
+            float2 acc[4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) acc[c] = make_float2(0.f, 0.f);
-          if (N == 16) {
-            uint32_t v[16];
-            tmem_ld16(ts, v);
-            tc_wait_ld();
-            if (masked) sum_chunk<16, true>(v, nl, M.scale_log2, 0, c_lo, cols, acc);
-            else sum_chunk<16, false>(v, nl, M.scale_log2, 0, c_lo, cols, acc);
-          } else if (masked) {
-            for (int c0 = 0; c0 < N; c0 += 32) {
-              uint32_t v[32];
-              tmem_ld32(ts + c0, v);
+            for (int c = 0; c < 4; ++c) acc[c] = make_float2(0.f, 0.f);
+            const int c_begin = WIDE ? half * 64 : 0, c_end = WIDE ? min(cols, half * 64 + 64) : cols;
+            if (WIDE && warp_hi <= c_begin && full_cols >= c_begin + 64) {
+              // all 64 columns count: the next sixteen are read from TMEM while these are worked on
+              uint32_t va[16], vb[16];
+              tmem_ld16(ts + c_begin, va);
               tc_wait_ld();
-              sum_chunk<32, true>(v, nl + c0, M.scale_log2, c0, c_lo, cols, acc);
-            }
-          } else {
-            for (int c0 = 0; c0 < N; c0 += 32) {
-              uint32_t v[32];
-              tmem_ld32(ts + c0, v);
+              tmem_ld16(ts + c_begin + 16, vb);
+              sum_chunk<16, false, FMA_SHARE>(va, nl + c_begin, M.scale_log2, 0, 0, 0, acc);
               tc_wait_ld();
-              sum_chunk<32, false>(v, nl + c0, M.scale_log2, c0, c_lo, cols, acc);
+              tmem_ld16(ts + c_begin + 32, va);
+              sum_chunk<16, false, FMA_SHARE>(vb, nl + c_begin + 16, M.scale_log2, 0, 0, 0, acc);
+              tc_wait_ld();
+              tmem_ld16(ts + c_begin + 48, vb);
+              sum_chunk<16, false, FMA_SHARE>(va, nl + c_begin + 32, M.scale_log2, 0, 0, 0, acc);
+              tc_wait_ld();
+              sum_chunk<16, false, FMA_SHARE>(vb, nl + c_begin + 48, M.scale_log2, 0, 0, 0, acc);
+            } else {
+#pragma unroll 1
+              for (int c0 = max(warp_lo & ~15, c_begin); c0 < c_end; c0 += 16) {
+                uint32_t v[16];
+                tmem_ld16(ts + c0, v);
+                tc_wait_ld();
+                if (c0 >= warp_hi && c0 + 16 <= full_cols)
+                  sum_chunk<16, false, 0>(v, nl + c0, M.scale_log2, 0, 0, 0, acc);
+                else
+                  sum_chunk<16, true, 0>(v, nl + c0, M.scale_log2, c0, c_lo, cols, acc);
+              }
             }
+            const float2 a = __fadd2_rn(__fadd2_rn(acc[0], acc[1]), __fadd2_rn(acc[2], acc[3]));
+            sum += a.x + a.y;
+            if (WIDE && qt == sg.n_qt - 1) {
+              // The key's two sums meet: the upper columns' goes through the first of those columns, which its warps have
+              // read by now.  The accumulator is free again when both halves have arrived below.
+              if (half == 1) {
+                tmem_st1(ts + 64, __float_as_uint(sum));
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(B_PFULL + g * 2 + buf));
+              } else {
+                ok = warp_wait(bar(B_PFULL + g * 2 + buf), (joined >> buf) & 1);
+                joined ^= 1u << buf;
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t other;
+                tmem_ld1(ts + 64, other);
+                tc_wait_ld();
+                sum += __uint_as_float(other);
+              }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(B_SEMPTY + g * 2 + buf));
           }
-          const float2 a = __fadd2_rn(__fadd2_rn(acc[0], acc[1]), __fadd2_rn(acc[2], acc[3]));
-          sum += a.x + a.y;
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(B_SEMPTY + g * 2 + buf));
+          if (!resident) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(B_QEMPTY + qs));
+          }
+          q.step(pl.nsq);
         }
-        if (!pl.resident) {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(B_QEMPTY + qs));
+        if (!resident) qr = q;
+        if (ok && half == 0 && mine && j < sg.kv_len) w_row[j] = p.decay != 0.f && j < sg.ctx ? fmaf(p.decay, old, sum) : sum;
+      }
+      if (ok && resident) {
+        __syncwarp();
+        for (int qt = lo; qt < sg.n_qt; ++qt) {
+          if (lane == 0) mbar_arrive(bar(B_QEMPTY + qr.slot));
+          qr.step(pl.nsq);
         }
       }
-      if (ok && mine && j < k_end) w_row[j] = p.decay != 0.f && j < ctx ? fmaf(p.decay, old, sum) : sum;
     }
-    if (!ok && lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, qi, 93 + g);
+    if (!ok && lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, sg.r, sg.kh, 93 + g);
   }
   // A role that gave up may leave TMA loads in flight towards this block's shared memory; outwait them.
   if (*reinterpret_cast<volatile int32_t*>(p.err) == HSWA_ERR_TIMEOUT) __nanosleep(100000);
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == ISSUER) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(pl.tmem_cols) : "memory");
   }
 }
 
 template <int D, bool WIDE>
-cudaError_t launch_t(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const WeightsParams& p, const WeightsPlan& pl, cudaStream_t s) {
+cudaError_t launch_t(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const WeightsParams& p, const WeightsPlan& pl, int blocks,
+                     cudaStream_t s) {
   constexpr int HALVES = D / 64;
-  int smem = pl.nsq * pl.n_cols * 128 * HALVES + pl.nsk * TKEYS * 128 * HALVES + pl.nsq * pl.n_cols * 4 + NUM_BARS * 8 + 16;
+  int smem = pl.nsq * pl.n_cols * 128 * HALVES + pl.nsk * TKEYS * 128 * HALVES + pl.nsq * pl.n_cols * 4 + NUM_BARS * 8 + 32;
   if (WIDE && smem < 120 * 1024) smem = 120 * 1024;  // one block per SM: it takes all of its TMEM
   auto kern = attn_weights_kernel<D, WIDE>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  const int64_t keys = (int64_t)p.max_ctx_len + (p.causal ? p.max_q_len : 0);
-  const int64_t tiles = (keys + TKEYS - 1) / TKEYS;
-  dim3 grid((unsigned)((tiles + pl.block_tiles - 1) / pl.block_tiles), p.m.Hkv, p.b.B);
-  kern<<<grid, THREADS, smem, s>>>(tm_pool, tm_q, p, pl);
+  kern<<<blocks, block_threads(WIDE), smem, s>>>(tm_pool, tm_q, p, pl);
   return cudaGetLastError();
 }
 
@@ -407,18 +620,21 @@ cudaError_t hswa_launch_attn_weights(const CUtensorMap& tm_pool, const CUtensorM
   pl.tmem_cols = 4 * pl.n_cols;
   const int max_qt = (p.max_q_len + pl.tile_tokens - 1) / pl.tile_tokens;
   const bool wide = pl.n_cols > 64;
-  pl.resident = max_qt <= MAX_NSQ;
-  pl.nsq = max_qt < 1 ? 1 : (pl.resident ? max_qt : 3);
-  const int tile_kb = p.m.D / 4;  // a 128-row tile
-  // shared memory: 224 KB of tiles in one block per SM, 96 KB of K tiles beside one small Q tile in each of two
-  pl.nsk = wide ? (224 - pl.nsq * tile_kb) / tile_kb : 96 / tile_kb;
+  const int tile_kb = p.m.D / 4;  // a tile of 128 rows
+  if (wide) {
+    // 224 KB of tiles, one block per SM: a Q stage more than a request has Q tiles (the next segment's first one) up to
+    // four, three when they are streamed; K takes the rest
+    pl.nsq = max_qt < MAX_NSQ ? max_qt + 1 : (max_qt == MAX_NSQ ? MAX_NSQ : 3);
+    pl.nsk = (224 - pl.nsq * tile_kb) / tile_kb;
+  } else {
+    // two blocks per SM with 96 KB of K tiles each, beside one or two Q tiles of at most 16 KB
+    pl.nsq = pl.n_cols == 64 && p.m.D == 128 ? 1 : 2;
+    pl.nsk = 96 / tile_kb;
+  }
   if (pl.nsk > MAX_NSK) pl.nsk = MAX_NSK;
-  // Key tiles per block: long enough to pay for a block's start, short enough to fill the machine
   const int64_t keys = (int64_t)p.max_ctx_len + (p.causal ? p.max_q_len : 0);
-  const int64_t tiles = (keys + TKEYS - 1) / TKEYS;
-  int per = 32;
-  while (per > 2 && (int64_t)p.b.B * p.m.Hkv * ((tiles + per - 1) / per) < 4LL * num_sms) per >>= 1;
-  pl.block_tiles = per;
-  if (p.m.D == 128) return wide ? launch_t<128, true>(tm_pool, tm_q, p, pl, s) : launch_t<128, false>(tm_pool, tm_q, p, pl, s);
-  return wide ? launch_t<64, true>(tm_pool, tm_q, p, pl, s) : launch_t<64, false>(tm_pool, tm_q, p, pl, s);
+  const int64_t tiles = (keys + TKEYS - 1) / TKEYS * p.m.Hkv * p.b.B, most = (wide ? 1 : 2) * (int64_t)num_sms;
+  const int blocks = (int)(2 * tiles < most ? 2 * tiles : most);  // (a share ends between tiles: half of few blocks may be idle)
+  if (p.m.D == 128) return wide ? launch_t<128, true>(tm_pool, tm_q, p, pl, blocks, s) : launch_t<128, false>(tm_pool, tm_q, p, pl, blocks, s);
+  return wide ? launch_t<64, true>(tm_pool, tm_q, p, pl, blocks, s) : launch_t<64, false>(tm_pool, tm_q, p, pl, blocks, s);
 }
