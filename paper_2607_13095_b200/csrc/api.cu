@@ -820,7 +820,7 @@ hswa_status hswa_evict_compact(hswa_handle* h, const hswa_layer* layer, const hs
   p.weights_out = weights_out;
   p.out_stride = weights_out_stride;
   p.err = h->err;
-  return hswa_launch_evict_compact(p, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+  return hswa_launch_evict_compact(p, h->num_sms, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
 }
 
 static hswa_status window_move(hswa_handle* h, const hswa_layer* layer, const hswa_batch* b, void* buf, int gather,

@@ -16,16 +16,103 @@ __device__ __forceinline__ uint32_t rank_key(float w, int j, int ctx, int first,
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// One block per (request, KV head): the keep-th largest key by four passes over 8-bit digits, then the kept positions in
-// ascending order, ties taken from the lowest index on.
-constexpr int ST = 1024;
-__global__ void __launch_bounds__(ST) evict_select_kernel(const SelectParams p) {
-  __shared__ int hist[256];
-  __shared__ uint32_t s_prefix;
-  __shared__ int s_want;
-  __shared__ int warp_gt[ST / 32], warp_eq[ST / 32];
-  const int kh = blockIdx.x % p.Hkv, r = blockIdx.x / p.Hkv;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+// The choice for one row (request, KV head), by one block.  The keep-th largest key is found by digits of 11, 11 and 10 bits.
+// The first pass over the weights counts the top digit; the second collects, in order of position, the few keys whose top
+// digit reaches the one found -- all that stay are among them -- in shared memory, where the other digits are counted and
+// the positions written from.  So the weights are read twice, the second time mostly from L2; a list that does not fit
+// (many equal weights) is done without: the later passes then read the row.
+//
+// Bound by what one SM can load (a row is one block's): two passes at about 100 GB/s per SM.
+constexpr int SEL_BINS = 2048;
+constexpr int SEL_QUADS = 4;  // quads of keys a thread has in hand
+
+// Counters of a block-wide step.
+template <int T>
+struct SelectShared {
+  uint32_t hist[SEL_BINS];
+  uint32_t warp_sum[2][T / 32];   // packed counts per warp, two buffers in turn
+  uint32_t warp_sum2[2][T / 32];
+  uint32_t digit, want;
+};
+
+// Position of a block-wide ordered step: thread-order prefix sums of four counts per thread (each at most 4), tile by tile.
+// In: c = the counts of tiles 0..3 in bytes.  Out: per tile the sum over all threads before this one, tile 0's threads
+// first; returns the grand total.  One barrier; `turn` alternates.
+template <int T>
+__device__ __forceinline__ uint32_t block_offsets(uint32_t (&sums)[2][T / 32], int turn, uint32_t c, uint32_t (&at)[SEL_QUADS]) {
+  constexpr int NW = T / 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint32_t incl = c;  // a warp's byte sums are at most 128
+#pragma unroll
+  for (int sh = 1; sh < 32; sh <<= 1) {
+    const uint32_t v = __shfl_up_sync(0xffffffffu, incl, sh);
+    if (lane >= sh) incl += v;
+  }
+  if (lane == 31) sums[turn][warp] = incl;
+  __syncthreads();
+  const uint32_t w = lane < NW ? sums[turn][lane] : 0u;
+  uint32_t even = w & 0x00ff00ffu, odd = (w >> 8) & 0x00ff00ffu;  // 16 bits each: at most 4096
+#pragma unroll
+  for (int sh = 1; sh < 32; sh <<= 1) {
+    const uint32_t a = __shfl_up_sync(0xffffffffu, even, sh), b = __shfl_up_sync(0xffffffffu, odd, sh);
+    if (lane >= sh) {
+      even += a;
+      odd += b;
+    }
+  }
+  const uint32_t te = __shfl_sync(0xffffffffu, even, 31), to = __shfl_sync(0xffffffffu, odd, 31);
+  uint32_t be = __shfl_sync(0xffffffffu, even, warp > 0 ? warp - 1 : 0), bo = __shfl_sync(0xffffffffu, odd, warp > 0 ? warp - 1 : 0);
+  if (warp == 0) be = bo = 0;
+  const uint32_t mine = incl - c;
+  const uint32_t t0 = te & 0xffff, t1 = to & 0xffff, t2 = te >> 16, t3 = to >> 16;
+  at[0] = (be & 0xffff) + (mine & 0xff);
+  at[1] = t0 + (bo & 0xffff) + ((mine >> 8) & 0xff);
+  at[2] = t0 + t1 + (be >> 16) + ((mine >> 16) & 0xff);
+  at[3] = t0 + t1 + t2 + (bo >> 16) + (mine >> 24);
+  return t0 + t1 + t2 + t3;
+}
+
+// The highest digit at which the count from the top reaches `want`; `want` becomes the rank inside it.
+template <int T>
+__device__ __forceinline__ uint32_t find_digit(SelectShared<T>& sh, int bins, uint32_t& want) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int PER = SEL_BINS / T;  // bins per thread, from the top down
+  const int top = bins - 1 - (int)threadIdx.x * PER;
+  uint32_t mine[PER], sum = 0;
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    mine[u] = top - u >= 0 ? sh.hist[top - u] : 0u;
+    sum += mine[u];
+  }
+  uint32_t incl = sum;
+#pragma unroll
+  for (int s = 1; s < 32; s <<= 1) {
+    const uint32_t v = __shfl_up_sync(0xffffffffu, incl, s);
+    if (lane >= s) incl += v;
+  }
+  if (lane == 31) sh.warp_sum[0][warp] = incl;
+  __syncthreads();
+  uint32_t b = incl - sum;
+  for (int i = 0; i < warp; ++i) b += sh.warp_sum[0][i];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    if (want > b && want <= b + mine[u]) {
+      sh.digit = (uint32_t)(top - u);
+      sh.want = want - b;
+    }
+    b += mine[u];
+  }
+  __syncthreads();
+  want = sh.want;
+  return sh.digit;
+}
+
+template <int T>
+__global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, const int capacity) {
+  extern __shared__ __align__(16) uint32_t list[];  // [capacity] keys, then [capacity] positions
+  __shared__ SelectShared<T> sh;
+  const int row = blockIdx.x, kh = row % p.Hkv, r = row / p.Hkv;
+  const int tid = threadIdx.x;
   int ctx = p.ctx_len[r];
   int keep = p.keep_len[r];
   if (ctx < 0 || ctx > p.max_ctx_len || keep < 0 || keep > p.max_keep) {
@@ -35,109 +122,281 @@ __global__ void __launch_bounds__(ST) evict_select_kernel(const SelectParams p) 
     keep = max(0, min(keep, p.max_keep));
   }
   keep = min(keep, ctx);
-  const float* w = p.weights + ((int64_t)r * p.Hkv + kh) * p.stride;
-  int32_t* out = p.keep_idx + ((int64_t)r * p.Hkv + kh) * p.max_keep;
+  const float* w = p.weights + (int64_t)row * p.stride;
+  int32_t* out = p.keep_idx + (int64_t)row * p.max_keep;
   if (tid == 0 && kh == 0) p.kept_len[r] = keep;
-  for (int i = keep + tid; i < p.max_keep; i += ST) out[i] = -1;
+  for (int i = keep + tid; i < p.max_keep; i += T) out[i] = -1;
   if (keep == 0) return;
-  if (tid == 0) {
-    s_prefix = 0;
-    s_want = keep;
+  if (keep == ctx) {  // everything stays
+    for (int i = tid; i < keep; i += T) out[i] = i;
+    return;
   }
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += ST) hist[i] = 0;
-    __syncthreads();
-    const uint32_t prefix = s_prefix;
-    for (int j = tid; j < ctx; j += ST) {
-      const uint32_t k = rank_key(w[j], j, ctx, p.protect_first, p.protect_last);
-      if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1);
-    }
-    __syncthreads();
-    if (tid == 0) {
-      int want = s_want, d = 255;
-      while (want > hist[d]) want -= hist[d--];
-      s_want = want;
-      s_prefix = (prefix << 8) | (uint32_t)d;
-    }
-    __syncthreads();
-  }
-  const uint32_t thr = s_prefix;
-  const int ties = s_want;  // positions with exactly the threshold that stay
-  int gt_base = 0, eq_base = 0;
-  for (int j0 = 0; j0 < ctx; j0 += ST) {
-    const int j = j0 + tid;
-    const uint32_t k = j < ctx ? rank_key(w[j], j, ctx, p.protect_first, p.protect_last) : 0u;
-    const unsigned gt = __ballot_sync(0xffffffffu, j < ctx && k > thr), eq = __ballot_sync(0xffffffffu, j < ctx && k == thr);
-    if (lane == 0) {
-      warp_gt[warp] = __popc(gt);
-      warp_eq[warp] = __popc(eq);
-    }
-    __syncthreads();
-    int g = gt_base, e = eq_base, gt_all = 0, eq_all = 0;
-    for (int i = 0; i < ST / 32; ++i) {
-      if (i < warp) {
-        g += warp_gt[i];
-        e += warp_eq[i];
+  for (int i = tid; i < SEL_BINS; i += T) sh.hist[i] = 0;
+  __syncthreads();
+
+  // The row in quads on 16-byte boundaries; the first one may begin up to three places before the row
+  const int mis = (int)((reinterpret_cast<uintptr_t>(w) >> 2) & 3);
+  const int quads = (ctx + mis + 3) / 4;
+  auto quad_inside = [&](int q) {  // which of a quad's four places lie in the row
+    const int j = q * 4 - mis;
+    uint32_t in = 15u;
+    if (j < 0) in &= 15u << -j;
+    if (j + 4 > ctx) in &= 15u >> (j + 4 - ctx);
+    return in;
+  };
+  auto load_quad = [&](int q) {
+    const int j = q * 4 - mis;
+    if (j >= 0 && j + 4 <= ctx) return __ldg(reinterpret_cast<const float4*>(w + j));
+    float4 v;
+    v.x = j >= 0 ? w[j] : 0.f;  // (the row is not empty, and a quad holds at least one place of it)
+    v.y = j + 1 >= 0 && j + 1 < ctx ? w[j + 1] : 0.f;
+    v.z = j + 2 >= 0 && j + 2 < ctx ? w[j + 2] : 0.f;
+    v.w = j + 3 >= 0 && j + 3 < ctx ? w[j + 3] : 0.f;
+    return v;
+  };
+  auto keys_of = [&](const float4& v, int q, uint32_t (&k)[4]) {
+    const int j = q * 4 - mis;
+    k[0] = rank_key(v.x, j, ctx, p.protect_first, p.protect_last);
+    k[1] = rank_key(v.y, j + 1, ctx, p.protect_first, p.protect_last);
+    k[2] = rank_key(v.z, j + 2, ctx, p.protect_first, p.protect_last);
+    k[3] = rank_key(v.w, j + 3, ctx, p.protect_first, p.protect_last);
+  };
+
+  // ---- the top digit ----
+  for (int q0 = tid; q0 < quads; q0 += SEL_QUADS * T) {
+    float4 v[SEL_QUADS];
+#pragma unroll
+    for (int u = 0; u < SEL_QUADS; ++u)
+      if (q0 + u * T < quads) v[u] = load_quad(q0 + u * T);
+#pragma unroll
+    for (int u = 0; u < SEL_QUADS; ++u) {
+      const int q = q0 + u * T;
+      if (q < quads) {
+        uint32_t k[4];
+        keys_of(v[u], q, k);
+        const uint32_t in = quad_inside(q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if ((in >> e) & 1u) atomicAdd(&sh.hist[k[e] >> 21], 1u);
       }
-      gt_all += warp_gt[i];
-      eq_all += warp_eq[i];
     }
-    const unsigned below = (1u << lane) - 1;
-    const int gr = g + __popc(gt & below), er = e + __popc(eq & below);
-    const bool is_gt = (gt >> lane) & 1u, is_eq = (eq >> lane) & 1u;
-    if (is_gt || (is_eq && er < ties)) out[gr + min(er, ties)] = j;
-    gt_base += gt_all;
-    eq_base += eq_all;
+  }
+  __syncthreads();
+  uint32_t want = (uint32_t)keep;
+  const uint32_t d1 = find_digit<T>(sh, SEL_BINS, want);
+  const uint32_t n_list = (uint32_t)keep - want + sh.hist[d1];  // keys above the digit, and all that have it
+  const bool listed = n_list <= (uint32_t)capacity;
+  uint32_t* l_key = list;
+  int32_t* l_pos = reinterpret_cast<int32_t*>(list + capacity);
+
+  // ---- collect ----
+  int turn = 0;
+  if (listed) {
+    uint32_t base = 0;
+    float4 v[SEL_QUADS];
+#pragma unroll
+    for (int u = 0; u < SEL_QUADS; ++u)
+      if (tid + u * T < quads) v[u] = load_quad(tid + u * T);
+    for (int q0 = 0; q0 < quads; q0 += SEL_QUADS * T) {
+      uint32_t k[SEL_QUADS][4], take[SEL_QUADS], c = 0;
+#pragma unroll
+      for (int u = 0; u < SEL_QUADS; ++u) {
+        const int q = q0 + u * T + tid;
+        take[u] = 0;
+        if (q < quads) {
+          keys_of(v[u], q, k[u]);
+          const uint32_t in = quad_inside(q);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) take[u] |= ((k[u][e] >> 21) >= d1 ? 1u : 0u) << e;
+          take[u] &= in;
+        }
+        c |= (uint32_t)__popc(take[u]) << (8 * u);
+        const int nq = q + SEL_QUADS * T;  // the next round's loads are under way meanwhile
+        if (nq < quads) v[u] = load_quad(nq);
+      }
+      uint32_t at[SEL_QUADS];
+      const uint32_t all = block_offsets<T>(sh.warp_sum, turn, c, at);
+      turn ^= 1;
+#pragma unroll
+      for (int u = 0; u < SEL_QUADS; ++u) {
+        uint32_t slot = base + at[u];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if ((take[u] >> e) & 1u) {
+            if (slot < (uint32_t)capacity) {
+              l_key[slot] = k[u][e];
+              l_pos[slot] = (q0 + u * T + tid) * 4 - mis + e;
+            }
+            ++slot;
+          }
+      }
+      base += all;
+    }
+  }
+  __syncthreads();
+
+  // ---- the other digits, over the list or over the row ----
+  const int n_quads = listed ? (int)(n_list + 3) / 4 : quads;
+  auto get = [&](int q, uint32_t (&k)[4]) -> uint32_t {  // a quad's keys; which of its places count
+    if (listed) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k[e] = q * 4 + e < (int)n_list ? l_key[q * 4 + e] : 0u;
+      return q * 4 + 4 <= (int)n_list ? 15u : 15u >> (q * 4 + 4 - (int)n_list);
+    }
+    keys_of(load_quad(q), q, k);
+    return quad_inside(q);
+  };
+  uint32_t thr = d1 << 21;
+#pragma unroll 1
+  for (int pass = 1; pass < 3; ++pass) {
+    const int shift = pass == 1 ? 10 : 0, above = pass == 1 ? 21 : 10, bins = pass == 1 ? 2048 : 1024;
+    for (int i = tid; i < SEL_BINS; i += T) sh.hist[i] = 0;
     __syncthreads();
+    for (int q = tid; q < n_quads; q += T) {
+      uint32_t k[4];
+      const uint32_t in = get(q, k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (((in >> e) & 1u) && (k[e] >> above) == (thr >> above)) atomicAdd(&sh.hist[(k[e] >> shift) & (uint32_t)(bins - 1)], 1u);
+    }
+    __syncthreads();
+    thr |= find_digit<T>(sh, bins, want) << shift;
+  }
+
+  // ---- the kept positions: keys above the threshold, and the first `want` of those equal to it ----
+  uint32_t base_gt = 0, base_eq = 0;
+  for (int q0 = 0; q0 < n_quads; q0 += SEL_QUADS * T) {
+    uint32_t gt[SEL_QUADS], eq[SEL_QUADS], c_gt = 0, c_eq = 0;
+#pragma unroll
+    for (int u = 0; u < SEL_QUADS; ++u) {
+      const int q = q0 + u * T + tid;
+      gt[u] = eq[u] = 0;
+      if (q < n_quads) {
+        uint32_t k[4];
+        const uint32_t in = get(q, k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          gt[u] |= (k[e] > thr ? 1u : 0u) << e;
+          eq[u] |= (k[e] == thr ? 1u : 0u) << e;
+        }
+        gt[u] &= in;
+        eq[u] &= in;
+      }
+      c_gt |= (uint32_t)__popc(gt[u]) << (8 * u);
+      c_eq |= (uint32_t)__popc(eq[u]) << (8 * u);
+    }
+    uint32_t at_gt[SEL_QUADS], at_eq[SEL_QUADS];
+    const uint32_t all_gt = block_offsets<T>(sh.warp_sum, turn, c_gt, at_gt);
+    const uint32_t all_eq = block_offsets<T>(sh.warp_sum2, turn, c_eq, at_eq);
+    turn ^= 1;
+#pragma unroll
+    for (int u = 0; u < SEL_QUADS; ++u) {
+      uint32_t g = base_gt + at_gt[u], e_rank = base_eq + at_eq[u];
+      const int q = q0 + u * T + tid;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool is_gt = (gt[u] >> e) & 1u, is_eq = (eq[u] >> e) & 1u;
+        const uint32_t slot = g + min(e_rank, want);
+        if ((is_gt || (is_eq && e_rank < want)) && slot < (uint32_t)keep) out[slot] = listed ? l_pos[q * 4 + e] : q * 4 - mis + e;
+        g += is_gt;
+        e_rank += is_eq;
+      }
+    }
+    base_gt += all_gt;
+    base_eq += all_eq;
   }
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
 // Kept row i of (request, KV head) goes from the storage of position keep_idx[i] to that of position i behind the new
-// block table.  One warp per kept row, K and V.
-__global__ void __launch_bounds__(256) evict_compact_kernel(const CompactParams p) {
+// block table.  A warp takes `rows` consecutive kept rows: lane l looks up row l's source and destination, then the warp
+// copies the rows with 16 bytes per lane, eight loads in flight before the first store.  Bound by memory: 2 x 4 D bytes per
+// row (source rows are gathered 2 D bytes at a time, destinations are consecutive).
+template <int D>
+__global__ void __launch_bounds__(256) evict_compact_kernel(const CompactParams p, const int rows) {
+  constexpr int LPR = D / 4;         // lanes per row: K and V, 16 bytes each
+  constexpr int RPS = 32 / LPR;      // rows per step
+  constexpr int STEPS = 8;
   const ModelParams& M = p.m;
   const int kh = blockIdx.y, r = blockIdx.z, lane = threadIdx.x & 31;
-  const int i = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int i0 = (blockIdx.x * 8 + (threadIdx.x >> 5)) * rows;
   int kept = p.kept_len[r];
-  const int ctx = min(p.b.ctx_len[r], p.max_ctx_len);
   if (kept < 0 || kept > p.max_keep) {
     if (threadIdx.x == 0 && blockIdx.x == 0 && kh == 0) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, kept);
     kept = min(kept, p.max_keep);
   }
-  if (i >= kept) return;
+  if (i0 >= kept) return;
+  const int ctx = min(p.b.ctx_len[r], p.max_ctx_len);
   const int64_t pair = (int64_t)r * M.Hkv + kh;
-  const int j = p.keep_idx[pair * p.max_keep + i];
-  if (j < 0 || j >= ctx) {
-    if (lane == 0) record_error(p.err, HSWA_ERR_BOUNDS, r, i, j);
-    return;
+  const int i = i0 + lane;
+  int64_t src = -1, dst = -1;  // element offsets of the K rows; -1: nothing to copy
+  if (lane < rows && i < kept) {
+    const int j = p.keep_idx[pair * p.max_keep + i];
+    if (j < 0 || j >= ctx) {
+      record_error(p.err, HSWA_ERR_BOUNDS, r, i, j);
+    } else {
+      const int from = p.b.block_table[(int64_t)r * p.b.max_blocks + j / M.P];
+      const int to = p.dst_block_table[(int64_t)r * p.dst_max_blocks + i / M.P];
+      if (from < 0 || from >= p.num_pages || to < 0 || to >= p.num_pages) {
+        record_error(p.err, HSWA_ERR_BOUNDS, r, i, from < 0 || from >= p.num_pages ? from : to);
+      } else {
+        src = (((int64_t)from * 2 * M.Hkv + kh) * M.P + j % M.P) * D;
+        dst = (((int64_t)to * 2 * M.Hkv + kh) * M.P + i % M.P) * D;
+        if (p.weights) p.weights_out[pair * p.out_stride + i] = p.weights[pair * p.stride + j];
+      }
+    }
   }
-  const int src = p.b.block_table[(int64_t)r * p.b.max_blocks + j / M.P];
-  const int dst = p.dst_block_table[(int64_t)r * p.dst_max_blocks + i / M.P];
-  if (src < 0 || src >= p.num_pages || dst < 0 || dst >= p.num_pages) {
-    if (lane == 0) record_error(p.err, HSWA_ERR_BOUNDS, r, i, src < 0 || src >= p.num_pages ? src : dst);
-    return;
+  // K in the lower half of a row's lanes, V (Hkv * P rows further on) in the upper half
+  const int64_t mine = (int64_t)(lane % LPR / (LPR / 2)) * M.Hkv * M.P * D + lane % (LPR / 2) * 8;
+  for (int l0 = 0; l0 < rows; l0 += STEPS * RPS) {
+    uint4 v[STEPS];
+    int64_t to[STEPS];
+#pragma unroll
+    for (int u = 0; u < STEPS; ++u) {
+      const int l = l0 + u * RPS + lane / LPR;  // the lane that looked this row up (rows is a multiple of STEPS * RPS)
+      const int64_t from = __shfl_sync(0xffffffffu, src, l);
+      to[u] = __shfl_sync(0xffffffffu, dst, l);
+      if (from >= 0) v[u] = __ldcs(reinterpret_cast<const uint4*>(p.pool + from + mine));
+    }
+#pragma unroll
+    for (int u = 0; u < STEPS; ++u)
+      if (to[u] >= 0) *reinterpret_cast<uint4*>(p.pool + to[u] + mine) = v[u];
   }
-  const int chunks = M.D / 8;
-  for (int c = lane; c < 2 * chunks; c += 32) {
-    const int kv = c / chunks, ch = c % chunks;
-    const uint4 v = *reinterpret_cast<const uint4*>(p.pool + ((((int64_t)src * 2 + kv) * M.Hkv + kh) * M.P + j % M.P) * M.D + ch * 8);
-    *reinterpret_cast<uint4*>(p.pool + ((((int64_t)dst * 2 + kv) * M.Hkv + kh) * M.P + i % M.P) * M.D + ch * 8) = v;
-  }
-  if (p.weights && lane == 0) p.weights_out[pair * p.out_stride + i] = p.weights[pair * p.stride + j];
 }
 
 }  // namespace
 
-cudaError_t hswa_launch_evict_select(const SelectParams& p, cudaStream_t s) {
-  if (p.B == 0) return cudaSuccess;
-  evict_select_kernel<<<p.B * p.Hkv, ST, 0, s>>>(p);
+template <int T>
+static cudaError_t launch_select_t(const SelectParams& p, int64_t rows, int capacity, cudaStream_t s) {
+  const int smem = capacity * 8;
+  cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  evict_select_kernel<T><<<(unsigned)rows, T, smem, s>>>(p, capacity);
   return cudaGetLastError();
 }
 
-cudaError_t hswa_launch_evict_compact(const CompactParams& p, cudaStream_t s) {
+cudaError_t hswa_launch_evict_select(const SelectParams& p, cudaStream_t s) {
+  if (p.B == 0) return cudaSuccess;
+  const int64_t rows = (int64_t)p.B * p.Hkv;
+  // room in the list for what stays and for an eighth of the row beside it (keys that share the threshold's top digit)
+  int64_t capacity = (int64_t)p.max_keep + p.max_ctx_len / 8 + 1024;
+  if (capacity > p.max_ctx_len) capacity = p.max_ctx_len;
+  if (capacity > 26000) capacity = 26000;
+  capacity = (capacity + 3) / 4 * 4;
+  if (p.max_ctx_len > 32768) return launch_select_t<1024>(p, rows, (int)capacity, s);
+  return launch_select_t<512>(p, rows, (int)capacity, s);
+}
+
+cudaError_t hswa_launch_evict_compact(const CompactParams& p, int num_sms, cudaStream_t s) {
   if (p.b.B == 0 || p.max_keep == 0) return cudaSuccess;
-  dim3 grid((p.max_keep + 7) / 8, p.m.Hkv, p.b.B);
-  evict_compact_kernel<<<grid, 256, 0, s>>>(p);
+  // 32 kept rows per warp, fewer while the warps do not fill the machine
+  int rows = 32;
+  const int least = p.m.D == 128 ? 8 : 16;
+  while (rows > least && (int64_t)p.b.B * p.m.Hkv * ((p.max_keep + rows - 1) / rows) < 32LL * num_sms) rows /= 2;
+  dim3 grid((p.max_keep + 8 * rows - 1) / (8 * rows), p.m.Hkv, p.b.B);
+  if (p.m.D == 128)
+    evict_compact_kernel<128><<<grid, 256, 0, s>>>(p, rows);
+  else
+    evict_compact_kernel<64><<<grid, 256, 0, s>>>(p, rows);
   return cudaGetLastError();
 }

@@ -198,7 +198,7 @@ int hswa_attn_weights_tile_tokens(const ModelParams& m, int max_q_len);  // toke
 cudaError_t hswa_launch_attn_weights(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const WeightsParams& p, int num_sms,
                                      cudaStream_t s);
 cudaError_t hswa_launch_evict_select(const SelectParams& p, cudaStream_t s);
-cudaError_t hswa_launch_evict_compact(const CompactParams& p, cudaStream_t s);
+cudaError_t hswa_launch_evict_compact(const CompactParams& p, int num_sms, cudaStream_t s);
 // SWA layers whose window fits shared memory: one block per (request, KV head) over a compact copy of the window
 bool hswa_ring_compact_supported(const ModelParams& m, int nq);
 cudaError_t hswa_launch_decode_ring_compact(const hswa_handle* h, const CUtensorMap& tm_pool, const DecodeParams& p,
