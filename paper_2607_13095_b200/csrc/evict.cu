@@ -17,13 +17,18 @@ __device__ __forceinline__ uint32_t rank_key(float w, int j, int ctx, int first,
 }
 
 // The choice for one row (request, KV head), by one block.  The keep-th largest key is found by digits of 11, 11 and 10 bits.
-// The first pass over the weights counts the top digit; the second collects, in order of position, the few keys whose top
-// digit reaches the one found -- all that stay are among them -- in shared memory, where the other digits are counted and
-// the positions written from.  So the weights are read twice, the second time mostly from L2; a list that does not fit
-// (many equal weights) is done without: the later passes then read the row.
 //
-// Bound by what one SM can load (a row is one block's): two passes at about 100 GB/s per SM.
+// Counting every key of a long row in shared memory would cost more than reading it (an atomic per key, several keys of a
+// warp in one bin), so long rows are sampled first: 4096 keys spread over the row say below which top digit nothing can
+// matter, with a margin of four standard deviations.  One pass then collects the keys from that digit on, in order of
+// position, in shared memory, where the digits are counted and from where the positions are written: the weights are read
+// once.  The sample decides nothing: when the list turns out to hold fewer keys than are to stay, or does not fit, and on
+// short rows, the top digit is counted over the whole row and the list begins at the digit found.  A list that does not fit
+// even then (many equal weights) is done without: the later passes read the row.
+//
+// Bound by what one SM can load (a row is one block's): about 100 GB/s per SM.
 constexpr int SEL_BINS = 2048;
+constexpr int SEL_SAMPLE = 1024;  // quads of keys in a long row's sample
 constexpr int SEL_QUADS = 4;  // quads of keys a thread has in hand
 
 // Counters of a block-wide step.
@@ -131,8 +136,6 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
     for (int i = tid; i < keep; i += T) out[i] = i;
     return;
   }
-  for (int i = tid; i < SEL_BINS; i += T) sh.hist[i] = 0;
-  __syncthreads();
 
   // The row in quads on 16-byte boundaries; the first one may begin up to three places before the row
   const int mis = (int)((reinterpret_cast<uintptr_t>(w) >> 2) & 3);
@@ -162,36 +165,11 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
     k[3] = rank_key(v.w, j + 3, ctx, p.protect_first, p.protect_last);
   };
 
-  // ---- the top digit ----
-  for (int q0 = tid; q0 < quads; q0 += SEL_QUADS * T) {
-    float4 v[SEL_QUADS];
-#pragma unroll
-    for (int u = 0; u < SEL_QUADS; ++u)
-      if (q0 + u * T < quads) v[u] = load_quad(q0 + u * T);
-#pragma unroll
-    for (int u = 0; u < SEL_QUADS; ++u) {
-      const int q = q0 + u * T;
-      if (q < quads) {
-        uint32_t k[4];
-        keys_of(v[u], q, k);
-        const uint32_t in = quad_inside(q);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if ((in >> e) & 1u) atomicAdd(&sh.hist[k[e] >> 21], 1u);
-      }
-    }
-  }
-  __syncthreads();
-  uint32_t want = (uint32_t)keep;
-  const uint32_t d1 = find_digit<T>(sh, SEL_BINS, want);
-  const uint32_t n_list = (uint32_t)keep - want + sh.hist[d1];  // keys above the digit, and all that have it
-  const bool listed = n_list <= (uint32_t)capacity;
   uint32_t* l_key = list;
   int32_t* l_pos = reinterpret_cast<int32_t*>(list + capacity);
-
-  // ---- collect ----
   int turn = 0;
-  if (listed) {
+  // Keys whose top digit is at least `digit`, in order of position: into the list as far as they fit; returns their number.
+  auto collect = [&](uint32_t digit) {
     uint32_t base = 0;
     float4 v[SEL_QUADS];
 #pragma unroll
@@ -207,7 +185,7 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
           keys_of(v[u], q, k[u]);
           const uint32_t in = quad_inside(q);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) take[u] |= ((k[u][e] >> 21) >= d1 ? 1u : 0u) << e;
+          for (int e = 0; e < 4; ++e) take[u] |= ((k[u][e] >> 21) >= digit ? 1u : 0u) << e;
           take[u] &= in;
         }
         c |= (uint32_t)__popc(take[u]) << (8 * u);
@@ -232,8 +210,70 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
       }
       base += all;
     }
+    __syncthreads();
+    return base;
+  };
+  auto clear_hist = [&]() {
+    for (int i = tid; i < SEL_BINS; i += T) sh.hist[i] = 0;
+    __syncthreads();
+  };
+
+  uint32_t want = (uint32_t)keep, n_list = 0, thr = 0;
+  bool listed = false;
+  int first_pass = 0;  // the digits before it are in thr
+  // ---- long rows: a sample's word on where the list may begin ----
+  if (quads >= 2 * SEL_SAMPLE) {
+    const int step = quads / SEL_SAMPLE;
+    const float share = 4.f * SEL_SAMPLE * (float)keep / (float)ctx;  // of the sample, what would stay
+    const uint32_t rank = (uint32_t)(share + 4.f * sqrtf(share) + 8.f);
+    if (rank <= 2 * SEL_SAMPLE) {  // at most half of it
+      clear_hist();
+#pragma unroll
+      for (int u = 0; u < SEL_SAMPLE / T; ++u) {
+        const int q = (u * T + tid) * step + step / 2;
+        uint32_t k[4];
+        keys_of(load_quad(q), q, k);
+        const uint32_t in = quad_inside(q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if ((in >> e) & 1u) atomicAdd(&sh.hist[k[e] >> 21], 1u);
+      }
+      __syncthreads();
+      uint32_t in_digit = rank;
+      n_list = collect(find_digit<T>(sh, SEL_BINS, in_digit));
+      listed = n_list >= (uint32_t)keep && n_list <= (uint32_t)capacity;
+    }
   }
-  __syncthreads();
+  // ---- the top digit, counted over the row ----
+  if (!listed) {
+    clear_hist();
+    for (int q0 = tid; q0 < quads; q0 += SEL_QUADS * T) {
+      float4 v[SEL_QUADS];
+#pragma unroll
+      for (int u = 0; u < SEL_QUADS; ++u)
+        if (q0 + u * T < quads) v[u] = load_quad(q0 + u * T);
+#pragma unroll
+      for (int u = 0; u < SEL_QUADS; ++u) {
+        const int q = q0 + u * T;
+        if (q < quads) {
+          uint32_t k[4];
+          keys_of(v[u], q, k);
+          const uint32_t in = quad_inside(q);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if ((in >> e) & 1u) atomicAdd(&sh.hist[k[e] >> 21], 1u);
+        }
+      }
+    }
+    __syncthreads();
+    const uint32_t d1 = find_digit<T>(sh, SEL_BINS, want);
+    thr = d1 << 21;
+    first_pass = 1;
+    n_list = (uint32_t)keep - want + sh.hist[d1];  // keys above the digit, and all that have it
+    listed = n_list <= (uint32_t)capacity;
+    __syncthreads();  // everybody has read the bin
+    if (listed) collect(d1);
+  }
 
   // ---- the other digits, over the list or over the row ----
   const int n_quads = listed ? (int)(n_list + 3) / 4 : quads;
@@ -246,18 +286,16 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
     keys_of(load_quad(q), q, k);
     return quad_inside(q);
   };
-  uint32_t thr = d1 << 21;
 #pragma unroll 1
-  for (int pass = 1; pass < 3; ++pass) {
-    const int shift = pass == 1 ? 10 : 0, above = pass == 1 ? 21 : 10, bins = pass == 1 ? 2048 : 1024;
-    for (int i = tid; i < SEL_BINS; i += T) sh.hist[i] = 0;
-    __syncthreads();
+  for (int pass = first_pass; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 1 ? 21 : 10, bins = pass == 2 ? 1024 : 2048;
+    clear_hist();
     for (int q = tid; q < n_quads; q += T) {
       uint32_t k[4];
       const uint32_t in = get(q, k);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (((in >> e) & 1u) && (k[e] >> above) == (thr >> above)) atomicAdd(&sh.hist[(k[e] >> shift) & (uint32_t)(bins - 1)], 1u);
+        if (((in >> e) & 1u) && (pass == 0 || (k[e] >> above) == (thr >> above))) atomicAdd(&sh.hist[(k[e] >> shift) & (uint32_t)(bins - 1)], 1u);
     }
     __syncthreads();
     thr |= find_digit<T>(sh, bins, want) << shift;
