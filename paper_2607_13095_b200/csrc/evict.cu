@@ -168,25 +168,34 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
   uint32_t* l_key = list;
   int32_t* l_pos = reinterpret_cast<int32_t*>(list + capacity);
   int turn = 0;
-  // Keys whose top digit is at least `digit`, in order of position: into the list as far as they fit; returns their number.
+  // Positions whose key's top digit is at least `digit`, in ascending order: into the list as far as they fit, with their
+  // keys; returns their number.
   auto collect = [&](uint32_t digit) {
+    // The digit as a weight: above zero one comparison per weight says the same (a NaN compares false, and its digit is 0).
+    // Protected places, and rows whose list begins among negative weights, take the long way.
+    const float least = __uint_as_float((digit << 21) & 0x7fffffffu);
+    const bool plain = digit >= 0x400u;
     uint32_t base = 0;
     float4 v[SEL_QUADS];
 #pragma unroll
     for (int u = 0; u < SEL_QUADS; ++u)
       if (tid + u * T < quads) v[u] = load_quad(tid + u * T);
     for (int q0 = 0; q0 < quads; q0 += SEL_QUADS * T) {
-      uint32_t k[SEL_QUADS][4], take[SEL_QUADS], c = 0;
+      uint32_t take[SEL_QUADS], c = 0;
 #pragma unroll
       for (int u = 0; u < SEL_QUADS; ++u) {
-        const int q = q0 + u * T + tid;
+        const int q = q0 + u * T + tid, j = q * 4 - mis;
         take[u] = 0;
         if (q < quads) {
-          keys_of(v[u], q, k[u]);
-          const uint32_t in = quad_inside(q);
+          if (plain && j >= p.protect_first && j + 4 <= ctx - p.protect_last) {
+            take[u] = (v[u].x >= least ? 1u : 0u) | (v[u].y >= least ? 2u : 0u) | (v[u].z >= least ? 4u : 0u) | (v[u].w >= least ? 8u : 0u);
+          } else {
+            uint32_t k[4];
+            keys_of(v[u], q, k);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) take[u] |= ((k[u][e] >> 21) >= digit ? 1u : 0u) << e;
-          take[u] &= in;
+            for (int e = 0; e < 4; ++e) take[u] |= ((k[e] >> 21) >= digit ? 1u : 0u) << e;
+            take[u] &= quad_inside(q);
+          }
         }
         c |= (uint32_t)__popc(take[u]) << (8 * u);
         const int nq = q + SEL_QUADS * T;  // the next round's loads are under way meanwhile
@@ -198,18 +207,14 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
 #pragma unroll
       for (int u = 0; u < SEL_QUADS; ++u) {
         uint32_t slot = base + at[u];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if ((take[u] >> e) & 1u) {
-            if (slot < (uint32_t)capacity) {
-              l_key[slot] = k[u][e];
-              l_pos[slot] = (q0 + u * T + tid) * 4 - mis + e;
-            }
-            ++slot;
-          }
+        for (uint32_t m = take[u]; m != 0; m &= m - 1, ++slot)
+          if (slot < (uint32_t)capacity) l_pos[slot] = (q0 + u * T + tid) * 4 - mis + __ffs(m) - 1;
       }
       base += all;
     }
+    __syncthreads();
+    for (int i = tid; i < (int)min(base, (uint32_t)capacity); i += T)
+      l_key[i] = rank_key(__ldg(w + l_pos[i]), l_pos[i], ctx, p.protect_first, p.protect_last);
     __syncthreads();
     return base;
   };
@@ -218,9 +223,12 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
     __syncthreads();
   };
 
-  uint32_t want = (uint32_t)keep, n_list = 0, thr = 0;
+  uint32_t want = (uint32_t)keep, n_list = 0;
   bool listed = false;
-  int first_pass = 0;  // the digits before it are in thr
+  // The threshold is at least `low`, and below low + 2^bits (bits = 32: anywhere from low on); `want` of the keys in that
+  // range stay, and all keys above it.
+  uint32_t low = 0;
+  int bits = 32;
   // ---- long rows: a sample's word on where the list may begin ----
   if (quads >= 2 * SEL_SAMPLE) {
     const int step = quads / SEL_SAMPLE;
@@ -240,8 +248,10 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
       }
       __syncthreads();
       uint32_t in_digit = rank;
-      n_list = collect(find_digit<T>(sh, SEL_BINS, in_digit));
+      const uint32_t d = find_digit<T>(sh, SEL_BINS, in_digit);
+      n_list = collect(d);
       listed = n_list >= (uint32_t)keep && n_list <= (uint32_t)capacity;
+      low = d << 21;
     }
   }
   // ---- the top digit, counted over the row ----
@@ -267,39 +277,61 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
     }
     __syncthreads();
     const uint32_t d1 = find_digit<T>(sh, SEL_BINS, want);
-    thr = d1 << 21;
-    first_pass = 1;
+    low = d1 << 21;
+    bits = 21;
     n_list = (uint32_t)keep - want + sh.hist[d1];  // keys above the digit, and all that have it
     listed = n_list <= (uint32_t)capacity;
     __syncthreads();  // everybody has read the bin
     if (listed) collect(d1);
   }
 
-  // ---- the other digits, over the list or over the row ----
+  // ---- the threshold: narrowed down over the list or over the row ----
   const int n_quads = listed ? (int)(n_list + 3) / 4 : quads;
   auto get = [&](int q, uint32_t (&k)[4]) -> uint32_t {  // a quad's keys; which of its places count
     if (listed) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) k[e] = q * 4 + e < (int)n_list ? l_key[q * 4 + e] : 0u;
+      const uint4 v = reinterpret_cast<const uint4*>(l_key)[q];  // (the list's room is whole quads)
+      k[0] = v.x;
+      k[1] = v.y;
+      k[2] = v.z;
+      k[3] = v.w;
       return q * 4 + 4 <= (int)n_list ? 15u : 15u >> (q * 4 + 4 - (int)n_list);
     }
     keys_of(load_quad(q), q, k);
     return quad_inside(q);
   };
-#pragma unroll 1
-  for (int pass = first_pass; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 1 ? 21 : 10, bins = pass == 2 ? 1024 : 2048;
+  // One step: the bin of 2^shift keys that holds the threshold; false if that is the last bin of a range cut off at 2^32
+  // keys, which also holds everything beyond.
+  auto narrow = [&](int shift) {
+    const int bins = bits == 32 ? SEL_BINS : 1 << (bits - shift);
     clear_hist();
     for (int q = tid; q < n_quads; q += T) {
       uint32_t k[4];
       const uint32_t in = get(q, k);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (((in >> e) & 1u) && (pass == 0 || (k[e] >> above) == (thr >> above))) atomicAdd(&sh.hist[(k[e] >> shift) & (uint32_t)(bins - 1)], 1u);
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t b = k[e] >= low ? (k[e] - low) >> shift : 0xffffffffu;
+        if (((in >> e) & 1u) && k[e] >= low && (bits == 32 || b < (uint32_t)bins)) atomicAdd(&sh.hist[min(b, (uint32_t)bins - 1u)], 1u);
+      }
     }
     __syncthreads();
-    thr |= find_digit<T>(sh, bins, want) << shift;
+    uint32_t rank = want;
+    const uint32_t d = find_digit<T>(sh, bins, rank);
+    if (bits == 32 && shift < 21 && d == (uint32_t)bins - 1u) return false;
+    want = rank;
+    low += d << shift;
+    bits = shift;
+    return true;
+  };
+  if (bits == 32) {
+    // A list from `low` on: bins of 2^16 keys (1/128 of an octave) over 16 octaves tell most apart and keep the keys of a
+    // warp out of one bin; if the threshold lies beyond, bins of whole digits.
+    if (!narrow(16)) {
+      low = 0;
+      narrow(21);
+    }
   }
+  while (bits > 0) narrow(bits > 11 ? bits - 11 : 0);
+  const uint32_t thr = low;
 
   // ---- the kept positions: keys above the threshold, and the first `want` of those equal to it ----
   uint32_t base_gt = 0, base_eq = 0;
