@@ -16,17 +16,19 @@ __device__ __forceinline__ uint32_t rank_key(float w, int j, int ctx, int first,
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// The choice for one row (request, KV head), by one block.  The keep-th largest key is found by digits of 11, 11 and 10 bits.
+// The choice for one row (request, KV head), by one block.  The threshold, the keep-th largest key, is narrowed down by
+// counting keys in bins.
 //
 // Counting every key of a long row in shared memory would cost more than reading it (an atomic per key, several keys of a
 // warp in one bin), so long rows are sampled first: 4096 keys spread over the row say below which top digit nothing can
-// matter, with a margin of four standard deviations.  One pass then collects the keys from that digit on, in order of
-// position, in shared memory, where the digits are counted and from where the positions are written: the weights are read
-// once.  The sample decides nothing: when the list turns out to hold fewer keys than are to stay, or does not fit, and on
-// short rows, the top digit is counted over the whole row and the list begins at the digit found.  A list that does not fit
-// even then (many equal weights) is done without: the later passes read the row.
+// matter, with a margin of four standard deviations.  One pass then collects the keys from that digit on in shared memory,
+// in any order (warps do not wait for one another), and the threshold is found among them: the weights are read once.  The
+// sample decides nothing: when the list turns out to hold fewer keys than are to stay, or does not fit, and on short rows,
+// the top digit is counted over the whole row and the list begins at the digit found.  What stays is marked in a bitmap of
+// the positions, which puts it in order.  A list that does not fit even then (many equal weights) is done without: the
+// later passes read the row.
 //
-// Bound by what one SM can load (a row is one block's): about 100 GB/s per SM.
+// Bound by what one SM can load: a row is one block's.
 constexpr int SEL_BINS = 2048;
 constexpr int SEL_SAMPLE = 1024;  // quads of keys in a long row's sample
 constexpr int SEL_QUADS = 4;  // quads of keys a thread has in hand
@@ -37,7 +39,8 @@ struct SelectShared {
   uint32_t hist[SEL_BINS];
   uint32_t warp_sum[2][T / 32];   // packed counts per warp, two buffers in turn
   uint32_t warp_sum2[2][T / 32];
-  uint32_t digit, want;
+  uint32_t digit, want, n_list, n_near;
+  uint32_t near[T];               // the keys that share the threshold's bin, when they are few
 };
 
 // Position of a block-wide ordered step: thread-order prefix sums of four counts per thread (each at most 4), tile by tile.
@@ -77,6 +80,15 @@ __device__ __forceinline__ uint32_t block_offsets(uint32_t (&sums)[2][T / 32], i
   return t0 + t1 + t2 + t3;
 }
 
+// Place of word i of a bitmap: one word of padding per 32, so that threads with consecutive words meet no bank twice.
+__host__ __device__ __forceinline__ int map_at(int i) { return i + (i >> 5); }
+
+// Lane i holds warp i's sum: the sum over the warps before this one.
+__device__ __forceinline__ uint32_t sum_of_warps_before(uint32_t v) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  return __reduce_add_sync(0xffffffffu, lane < warp ? v : 0u);
+}
+
 // The highest digit at which the count from the top reaches `want`; `want` becomes the rank inside it.
 template <int T>
 __device__ __forceinline__ uint32_t find_digit(SelectShared<T>& sh, int bins, uint32_t& want) {
@@ -97,8 +109,7 @@ __device__ __forceinline__ uint32_t find_digit(SelectShared<T>& sh, int bins, ui
   }
   if (lane == 31) sh.warp_sum[0][warp] = incl;
   __syncthreads();
-  uint32_t b = incl - sum;
-  for (int i = 0; i < warp; ++i) b += sh.warp_sum[0][i];
+  uint32_t b = incl - sum + sum_of_warps_before(lane < T / 32 ? sh.warp_sum[0][lane] : 0u);
 #pragma unroll
   for (int u = 0; u < PER; ++u) {
     if (want > b && want <= b + mine[u]) {
@@ -113,8 +124,8 @@ __device__ __forceinline__ uint32_t find_digit(SelectShared<T>& sh, int bins, ui
 }
 
 template <int T>
-__global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, const int capacity) {
-  extern __shared__ __align__(16) uint32_t list[];  // [capacity] keys, then [capacity] positions
+__global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, const int capacity, const int words) {
+  extern __shared__ __align__(16) uint32_t list[];  // [capacity] keys, [capacity] positions, [2] padded bitmaps of `words`
   __shared__ SelectShared<T> sh;
   const int row = blockIdx.x, kh = row % p.Hkv, r = row / p.Hkv;
   const int tid = threadIdx.x;
@@ -168,55 +179,70 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
   uint32_t* l_key = list;
   int32_t* l_pos = reinterpret_cast<int32_t*>(list + capacity);
   int turn = 0;
-  // Positions whose key's top digit is at least `digit`, in ascending order: into the list as far as they fit, with their
-  // keys; returns their number.
+  uint32_t* map_gt = list + 2 * capacity;
+  uint32_t* map_eq = map_gt + map_at(words);
+  const int lane = tid & 31;
+  // Keys whose top digit is at least `digit`, and their positions, into the list as far as they fit; returns their number.
   auto collect = [&](uint32_t digit) {
     // The digit as a weight: above zero one comparison per weight says the same (a NaN compares false, and its digit is 0).
     // Protected places, and rows whose list begins among negative weights, take the long way.
     const float least = __uint_as_float((digit << 21) & 0x7fffffffu);
     const bool plain = digit >= 0x400u;
-    uint32_t base = 0;
-    float4 v[SEL_QUADS];
+    if (tid == 0) sh.n_list = 0;
+    __syncthreads();
+    for (int q0 = tid - lane; q0 < quads; q0 += SEL_QUADS * T) {  // (the same for the lanes of a warp)
+      float4 v[SEL_QUADS];
 #pragma unroll
-    for (int u = 0; u < SEL_QUADS; ++u)
-      if (tid + u * T < quads) v[u] = load_quad(tid + u * T);
-    for (int q0 = 0; q0 < quads; q0 += SEL_QUADS * T) {
-      uint32_t take[SEL_QUADS], c = 0;
+      for (int u = 0; u < SEL_QUADS; ++u)
+        if (q0 + u * T + lane < quads) v[u] = load_quad(q0 + u * T + lane);
+      uint32_t take = 0;  // four bits per quad
 #pragma unroll
       for (int u = 0; u < SEL_QUADS; ++u) {
-        const int q = q0 + u * T + tid, j = q * 4 - mis;
-        take[u] = 0;
+        const int q = q0 + u * T + lane, j = q * 4 - mis;
         if (q < quads) {
+          uint32_t t;
           if (plain && j >= p.protect_first && j + 4 <= ctx - p.protect_last) {
-            take[u] = (v[u].x >= least ? 1u : 0u) | (v[u].y >= least ? 2u : 0u) | (v[u].z >= least ? 4u : 0u) | (v[u].w >= least ? 8u : 0u);
+            t = (v[u].x >= least ? 1u : 0u) | (v[u].y >= least ? 2u : 0u) | (v[u].z >= least ? 4u : 0u) | (v[u].w >= least ? 8u : 0u);
           } else {
             uint32_t k[4];
             keys_of(v[u], q, k);
+            t = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) take[u] |= ((k[e] >> 21) >= digit ? 1u : 0u) << e;
-            take[u] &= quad_inside(q);
+            for (int e = 0; e < 4; ++e) t |= ((k[e] >> 21) >= digit ? 1u : 0u) << e;
+            t &= quad_inside(q);
           }
+          take |= t << (4 * u);
         }
-        c |= (uint32_t)__popc(take[u]) << (8 * u);
-        const int nq = q + SEL_QUADS * T;  // the next round's loads are under way meanwhile
-        if (nq < quads) v[u] = load_quad(nq);
       }
-      uint32_t at[SEL_QUADS];
-      const uint32_t all = block_offsets<T>(sh.warp_sum, turn, c, at);
-      turn ^= 1;
+      const uint32_t mine = __popc(take);
+      uint32_t incl = mine;
 #pragma unroll
-      for (int u = 0; u < SEL_QUADS; ++u) {
-        uint32_t slot = base + at[u];
-        for (uint32_t m = take[u]; m != 0; m &= m - 1, ++slot)
-          if (slot < (uint32_t)capacity) l_pos[slot] = (q0 + u * T + tid) * 4 - mis + __ffs(m) - 1;
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += x;
       }
-      base += all;
+      uint32_t base = 0;
+      if (lane == 31 && incl > 0) base = atomicAdd(&sh.n_list, incl);
+      uint32_t slot = __shfl_sync(0xffffffffu, base, 31) + incl - mine;
+      for (uint32_t m = take; m != 0; m &= m - 1, ++slot) {
+        const int b = __ffs(m) - 1;
+        if (slot < (uint32_t)capacity) l_pos[slot] = (q0 + (b >> 2) * T + lane) * 4 - mis + (b & 3);
+      }
     }
     __syncthreads();
-    for (int i = tid; i < (int)min(base, (uint32_t)capacity); i += T)
-      l_key[i] = rank_key(__ldg(w + l_pos[i]), l_pos[i], ctx, p.protect_first, p.protect_last);
+    const uint32_t n = sh.n_list;
+    // the keys, read again (from L2) for the few that are listed: four at a time
+    const int n_in = (int)min(n, (uint32_t)capacity);
+    for (int i0 = tid; i0 < n_in; i0 += 4 * T) {
+      float x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u] = i0 + u * T < n_in ? __ldg(w + l_pos[i0 + u * T]) : 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (i0 + u * T < n_in) l_key[i0 + u * T] = rank_key(x[u], l_pos[i0 + u * T], ctx, p.protect_first, p.protect_last);
+    }
     __syncthreads();
-    return base;
+    return n;
   };
   auto clear_hist = [&]() {
     for (int i = tid; i < SEL_BINS; i += T) sh.hist[i] = 0;
@@ -330,10 +356,97 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
       narrow(21);
     }
   }
-  while (bits > 0) narrow(bits > 11 ? bits - 11 : 0);
-  const uint32_t thr = low;
+  uint32_t thr = low;
+  while (bits > 0) {
+    const uint32_t near = sh.hist[sh.digit];  // (as the last step, or the count of the top digit, left them)
+    __syncthreads();
+    if (near <= (uint32_t)T) {
+      // few keys share the bin: each is ranked among them
+      if (tid == 0) sh.n_near = 0;
+      __syncthreads();
+      for (int q = tid; q < n_quads; q += T) {
+        uint32_t k[4];
+        const uint32_t in = get(q, k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (((in >> e) & 1u) && k[e] >= low && ((k[e] - low) >> bits) == 0) {
+            const uint32_t at = atomicAdd(&sh.n_near, 1u);
+            if (at < (uint32_t)T) sh.near[at] = k[e];
+          }
+      }
+      __syncthreads();
+      if (tid < (int)near) {
+        const uint32_t k = sh.near[tid];
+        uint32_t above = 0, same = 0;
+        for (int i = 0; i < (int)near; ++i) {
+          above += sh.near[i] > k;
+          same += sh.near[i] == k;
+        }
+        if (above < want && want <= above + same) {  // equal keys write equal values
+          sh.digit = k;
+          sh.want = want - above;
+        }
+      }
+      __syncthreads();
+      thr = sh.digit;
+      want = sh.want;
+      break;
+    }
+    narrow(bits > 11 ? bits - 11 : 0);
+    thr = low;
+  }
 
   // ---- the kept positions: keys above the threshold, and the first `want` of those equal to it ----
+  if (listed) {
+    uint32_t done_gt = 0, done_eq = 0;
+    for (int i = tid; i < (int)n_list; i += T) {  // what stays, by kind, in the positions' sign bits: the keys' room is wanted
+      const uint32_t k = l_key[i];
+      l_pos[i] = k < thr ? -1 : (k > thr ? l_pos[i] : l_pos[i] | (int)0x80000000);
+    }
+    int32_t* in_order = reinterpret_cast<int32_t*>(l_key);  // [keep]
+    __syncthreads();
+    for (int win = 0; win < ctx; win += words * 32) {  // positions a bitmap at a time
+      const int n_words = min(words, (ctx - win + 31) / 32), each = (n_words + T - 1) / T;
+      for (int i = tid; i < map_at(n_words); i += T) map_gt[i] = map_eq[i] = 0;
+      __syncthreads();
+      for (int i = tid; i < (int)n_list; i += T) {
+        const int at = l_pos[i], j = (at & 0x7fffffff) - win;
+        if (at != -1 && j >= 0 && j < n_words * 32) atomicOr((at >= 0 ? map_gt : map_eq) + map_at(j >> 5), 1u << (j & 31));
+      }
+      __syncthreads();
+      // a thread's words are consecutive; counts of both kinds in one number (a list is shorter than 2^16)
+      const int w_lo = min(tid * each, n_words), w_hi = min(w_lo + each, n_words);
+      uint32_t c = 0;
+      for (int i = w_lo; i < w_hi; ++i) c += __popc(map_gt[map_at(i)]) | __popc(map_eq[map_at(i)]) << 16;
+      uint32_t incl = c;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += x;
+      }
+      if (lane == 31) sh.warp_sum[0][tid >> 5] = incl;
+      __syncthreads();
+      const uint32_t of_warp = lane < T / 32 ? sh.warp_sum[0][lane] : 0u;
+      const uint32_t before = incl - c + sum_of_warps_before(of_warp), all = __reduce_add_sync(0xffffffffu, of_warp);
+      uint32_t g = done_gt + (before & 0xffff), e_rank = done_eq + (before >> 16);
+      for (int i = w_lo; i < w_hi; ++i) {
+        const uint32_t gt = map_gt[map_at(i)];
+        for (uint32_t m = gt | map_eq[map_at(i)]; m != 0; m &= m - 1) {
+          const int b = __ffs(m) - 1;
+          const bool is_gt = (gt >> b) & 1u;
+          const uint32_t slot = g + min(e_rank, want);
+          if ((is_gt || e_rank < want) && slot < (uint32_t)keep) in_order[slot] = win + i * 32 + b;
+          g += is_gt;
+          e_rank += !is_gt;
+        }
+      }
+      done_gt += all & 0xffff;
+      done_eq += all >> 16;
+      __syncthreads();
+    }
+    for (int i = tid; i < keep; i += T) out[i] = in_order[i];
+    return;
+  }
   uint32_t base_gt = 0, base_eq = 0;
   for (int q0 = 0; q0 < n_quads; q0 += SEL_QUADS * T) {
     uint32_t gt[SEL_QUADS], eq[SEL_QUADS], c_gt = 0, c_eq = 0;
@@ -367,7 +480,7 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
       for (int e = 0; e < 4; ++e) {
         const bool is_gt = (gt[u] >> e) & 1u, is_eq = (eq[u] >> e) & 1u;
         const uint32_t slot = g + min(e_rank, want);
-        if ((is_gt || (is_eq && e_rank < want)) && slot < (uint32_t)keep) out[slot] = listed ? l_pos[q * 4 + e] : q * 4 - mis + e;
+        if ((is_gt || (is_eq && e_rank < want)) && slot < (uint32_t)keep) out[slot] = q * 4 - mis + e;
         g += is_gt;
         e_rank += is_eq;
       }
@@ -437,11 +550,11 @@ __global__ void __launch_bounds__(256) evict_compact_kernel(const CompactParams 
 }  // namespace
 
 template <int T>
-static cudaError_t launch_select_t(const SelectParams& p, int64_t rows, int capacity, cudaStream_t s) {
-  const int smem = capacity * 8;
+static cudaError_t launch_select_t(const SelectParams& p, int64_t rows, int capacity, int words, cudaStream_t s) {
+  const int smem = (capacity + map_at(words)) * 8;
   cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  evict_select_kernel<T><<<(unsigned)rows, T, smem, s>>>(p, capacity);
+  evict_select_kernel<T><<<(unsigned)rows, T, smem, s>>>(p, capacity, words);
   return cudaGetLastError();
 }
 
@@ -451,10 +564,12 @@ cudaError_t hswa_launch_evict_select(const SelectParams& p, cudaStream_t s) {
   // room in the list for what stays and for an eighth of the row beside it (keys that share the threshold's top digit)
   int64_t capacity = (int64_t)p.max_keep + p.max_ctx_len / 8 + 1024;
   if (capacity > p.max_ctx_len) capacity = p.max_ctx_len;
-  if (capacity > 26000) capacity = 26000;
+  if (capacity > 18176) capacity = 18176;
   capacity = (capacity + 3) / 4 * 4;
-  if (p.max_ctx_len > 32768) return launch_select_t<1024>(p, rows, (int)capacity, s);
-  return launch_select_t<512>(p, rows, (int)capacity, s);
+  int words = (p.max_ctx_len + 31) / 32;
+  if (words > 8192) words = 8192;
+  if (p.max_ctx_len > 32768) return launch_select_t<1024>(p, rows, (int)capacity, words, s);
+  return launch_select_t<512>(p, rows, (int)capacity, words, s);
 }
 
 cudaError_t hswa_launch_evict_compact(const CompactParams& p, int num_sms, cudaStream_t s) {
