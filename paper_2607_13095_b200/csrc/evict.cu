@@ -20,8 +20,8 @@ __device__ __forceinline__ uint32_t rank_key(float w, int j, int ctx, int first,
 // counting keys in bins.
 //
 // Counting every key of a long row in shared memory would cost more than reading it (an atomic per key, several keys of a
-// warp in one bin), so long rows are sampled first: 4096 keys spread over the row say below which top digit nothing can
-// matter, with a margin of four standard deviations.  One pass then collects the keys from that digit on in shared memory,
+// warp in one bin), so long rows are sampled first: eight keys per thread, spread over the row, say below which key nothing
+// can matter, with a margin of four standard deviations.  One pass then collects the keys from that one on in shared memory,
 // in any order (warps do not wait for one another), and the threshold is found among them: the weights are read once.  The
 // sample decides nothing: when the list turns out to hold fewer keys than are to stay, or does not fit, and on short rows,
 // the top digit is counted over the whole row and the list begins at the digit found.  What stays is marked in a bitmap of
@@ -30,8 +30,7 @@ __device__ __forceinline__ uint32_t rank_key(float w, int j, int ctx, int first,
 //
 // Bound by what one SM can load: a row is one block's.
 constexpr int SEL_BINS = 2048;
-constexpr int SEL_SAMPLE = 1024;  // quads of keys in a long row's sample
-constexpr int SEL_QUADS = 4;  // quads of keys a thread has in hand
+constexpr int SEL_QUADS = 4;  // quads of keys a thread has in hand in a step of the whole block
 
 // Counters of a block-wide step.
 template <int T>
@@ -123,9 +122,10 @@ __device__ __forceinline__ uint32_t find_digit(SelectShared<T>& sh, int bins, ui
   return sh.digit;
 }
 
-template <int T>
-__global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, const int capacity, const int words) {
-  extern __shared__ __align__(16) uint32_t list[];  // [capacity] keys, [capacity] positions, [2] padded bitmaps of `words`
+// T threads; CQ quads of keys per thread in flight while as many are looked at.
+template <int T, int CQ>
+__global__ void __launch_bounds__(T, T == 256 ? 4 : 1) evict_select_kernel(const SelectParams p, const int capacity, const int words) {
+  extern __shared__ __align__(16) uint32_t list[];  // [capacity] keys, [capacity] positions, [3] padded arrays of `words`
   __shared__ SelectShared<T> sh;
   const int row = blockIdx.x, kh = row % p.Hkv, r = row / p.Hkv;
   const int tid = threadIdx.x;
@@ -181,34 +181,42 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
   int turn = 0;
   uint32_t* map_gt = list + 2 * capacity;
   uint32_t* map_eq = map_gt + map_at(words);
+  uint32_t* map_before = map_eq + map_at(words);
   const int lane = tid & 31;
-  // Keys whose top digit is at least `digit`, and their positions, into the list as far as they fit; returns their number.
-  auto collect = [&](uint32_t digit) {
-    // The digit as a weight: above zero one comparison per weight says the same (a NaN compares false, and its digit is 0).
+  // Keys from `least_key` on, and their positions, into the list as far as they fit; returns their number.
+  auto collect = [&](uint32_t least_key) {
+    // The key as a weight: from zero on one comparison per weight says the same (a NaN compares false, and its key is 0).
     // Protected places, and rows whose list begins among negative weights, take the long way.
-    const float least = __uint_as_float((digit << 21) & 0x7fffffffu);
-    const bool plain = digit >= 0x400u;
+    const float least = __uint_as_float(least_key & 0x7fffffffu);
+    const bool plain = least_key >= 0x80000000u;
     if (tid == 0) sh.n_list = 0;
     __syncthreads();
-    for (int q0 = tid - lane; q0 < quads; q0 += SEL_QUADS * T) {  // (the same for the lanes of a warp)
-      float4 v[SEL_QUADS];
+    float4 v[CQ];
+    auto fetch = [&](int q0) {
 #pragma unroll
-      for (int u = 0; u < SEL_QUADS; ++u)
+      for (int u = 0; u < CQ; ++u)
         if (q0 + u * T + lane < quads) v[u] = load_quad(q0 + u * T + lane);
-      uint32_t take = 0;  // four bits per quad
+    };
+    fetch(tid - lane);
+    for (int q0 = tid - lane; q0 < quads; q0 += CQ * T) {  // (the same for the lanes of a warp)
+      float4 x[CQ];
 #pragma unroll
-      for (int u = 0; u < SEL_QUADS; ++u) {
+      for (int u = 0; u < CQ; ++u) x[u] = v[u];
+      fetch(q0 + CQ * T);  // the next round's loads are under way meanwhile
+      uint32_t take = 0;   // four bits per quad
+#pragma unroll
+      for (int u = 0; u < CQ; ++u) {
         const int q = q0 + u * T + lane, j = q * 4 - mis;
         if (q < quads) {
           uint32_t t;
           if (plain && j >= p.protect_first && j + 4 <= ctx - p.protect_last) {
-            t = (v[u].x >= least ? 1u : 0u) | (v[u].y >= least ? 2u : 0u) | (v[u].z >= least ? 4u : 0u) | (v[u].w >= least ? 8u : 0u);
+            t = (x[u].x >= least ? 1u : 0u) | (x[u].y >= least ? 2u : 0u) | (x[u].z >= least ? 4u : 0u) | (x[u].w >= least ? 8u : 0u);
           } else {
             uint32_t k[4];
-            keys_of(v[u], q, k);
+            keys_of(x[u], q, k);
             t = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) t |= ((k[e] >> 21) >= digit ? 1u : 0u) << e;
+            for (int e = 0; e < 4; ++e) t |= (k[e] >= least_key ? 1u : 0u) << e;
             t &= quad_inside(q);
           }
           take |= t << (4 * u);
@@ -218,8 +226,8 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
       uint32_t incl = mine;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xffffffffu, incl, d);
-        if (lane >= d) incl += x;
+        const uint32_t y = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += y;
       }
       uint32_t base = 0;
       if (lane == 31 && incl > 0) base = atomicAdd(&sh.n_list, incl);
@@ -256,28 +264,32 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
   uint32_t low = 0;
   int bits = 32;
   // ---- long rows: a sample's word on where the list may begin ----
-  if (quads >= 2 * SEL_SAMPLE) {
-    const int step = quads / SEL_SAMPLE;
-    const float share = 4.f * SEL_SAMPLE * (float)keep / (float)ctx;  // of the sample, what would stay
-    const uint32_t rank = (uint32_t)(share + 4.f * sqrtf(share) + 8.f);
-    if (rank <= 2 * SEL_SAMPLE) {  // at most half of it
-      clear_hist();
+  if (quads >= 4 * T) {
+    const int step = quads / (2 * T);
+    const float share = 8.f * T * (float)keep / (float)ctx;  // of the sample's 8 T keys, those that would stay
+    uint32_t rank = (uint32_t)(share + 4.f * sqrtf(share) + 8.f);
+    if (rank <= 4 * T) {  // at most half of it
+      uint32_t k[2][4], in[2];
 #pragma unroll
-      for (int u = 0; u < SEL_SAMPLE / T; ++u) {
+      for (int u = 0; u < 2; ++u) {
         const int q = (u * T + tid) * step + step / 2;
-        uint32_t k[4];
-        keys_of(load_quad(q), q, k);
-        const uint32_t in = quad_inside(q);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if ((in >> e) & 1u) atomicAdd(&sh.hist[k[e] >> 21], 1u);
+        keys_of(load_quad(q), q, k[u]);
+        in[u] = quad_inside(q);
       }
-      __syncthreads();
-      uint32_t in_digit = rank;
-      const uint32_t d = find_digit<T>(sh, SEL_BINS, in_digit);
-      n_list = collect(d);
+#pragma unroll
+      for (int digit = 0; digit < 2; ++digit) {  // 22 bits of it
+        clear_hist();
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (((in[u] >> e) & 1u) && (digit == 0 || (k[u][e] >> 21) == (low >> 21)))
+              atomicAdd(&sh.hist[digit == 0 ? k[u][e] >> 21 : (k[u][e] >> 10) & 2047u], 1u);
+        __syncthreads();
+        low |= find_digit<T>(sh, SEL_BINS, rank) << (digit == 0 ? 21 : 10);
+      }
+      n_list = collect(low);
       listed = n_list >= (uint32_t)keep && n_list <= (uint32_t)capacity;
-      low = d << 21;
     }
   }
   // ---- the top digit, counted over the row ----
@@ -308,7 +320,7 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
     n_list = (uint32_t)keep - want + sh.hist[d1];  // keys above the digit, and all that have it
     listed = n_list <= (uint32_t)capacity;
     __syncthreads();  // everybody has read the bin
-    if (listed) collect(d1);
+    if (listed) collect(low);
   }
 
   // ---- the threshold: narrowed down over the list or over the row ----
@@ -428,17 +440,26 @@ __global__ void __launch_bounds__(T) evict_select_kernel(const SelectParams p, c
       __syncthreads();
       const uint32_t of_warp = lane < T / 32 ? sh.warp_sum[0][lane] : 0u;
       const uint32_t before = incl - c + sum_of_warps_before(of_warp), all = __reduce_add_sync(0xffffffffu, of_warp);
-      uint32_t g = done_gt + (before & 0xffff), e_rank = done_eq + (before >> 16);
-      for (int i = w_lo; i < w_hi; ++i) {
-        const uint32_t gt = map_gt[map_at(i)];
-        for (uint32_t m = gt | map_eq[map_at(i)]; m != 0; m &= m - 1) {
-          const int b = __ffs(m) - 1;
-          const bool is_gt = (gt >> b) & 1u;
-          const uint32_t slot = g + min(e_rank, want);
-          if ((is_gt || e_rank < want) && slot < (uint32_t)keep) in_order[slot] = win + i * 32 + b;
-          g += is_gt;
-          e_rank += !is_gt;
+      uint32_t at = done_gt + (before & 0xffff), at_eq = done_eq + (before >> 16);
+      for (int i = w_lo; i < w_hi; ++i) {  // where each word's positions go: ties that stay are among the first `want`
+        map_before[map_at(i)] = at + min(at_eq, want);
+        const uint32_t eq = map_eq[map_at(i)];
+        const int room = (int)want - (int)min(at_eq, want);  // drop the ties that do not
+        uint32_t stay = eq;
+        if (__popc(eq) > room) {
+          stay = 0;
+          uint32_t m = eq;
+          for (int k = 0; k < room; ++k, m &= m - 1) stay |= m & (0u - m);
         }
+        at += __popc(map_gt[map_at(i)]);
+        at_eq += __popc(eq);
+        map_eq[map_at(i)] = stay;
+      }
+      __syncthreads();
+      for (int i = tid; i < n_words; i += T) {  // full words next to one another fall to different threads
+        uint32_t slot = map_before[map_at(i)];
+        for (uint32_t m = map_gt[map_at(i)] | map_eq[map_at(i)]; m != 0; m &= m - 1, ++slot)
+          if (slot < (uint32_t)keep) in_order[slot] = win + i * 32 + __ffs(m) - 1;
       }
       done_gt += all & 0xffff;
       done_eq += all >> 16;
@@ -549,27 +570,29 @@ __global__ void __launch_bounds__(256) evict_compact_kernel(const CompactParams 
 
 }  // namespace
 
-template <int T>
+template <int T, int CQ>
 static cudaError_t launch_select_t(const SelectParams& p, int64_t rows, int capacity, int words, cudaStream_t s) {
-  const int smem = (capacity + map_at(words)) * 8;
-  cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const int smem = capacity * 8 + map_at(words) * 12;
+  cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<T, CQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  evict_select_kernel<T><<<(unsigned)rows, T, smem, s>>>(p, capacity, words);
+  evict_select_kernel<T, CQ><<<(unsigned)rows, T, smem, s>>>(p, capacity, words);
   return cudaGetLastError();
 }
 
 cudaError_t hswa_launch_evict_select(const SelectParams& p, cudaStream_t s) {
   if (p.B == 0) return cudaSuccess;
   const int64_t rows = (int64_t)p.B * p.Hkv;
-  // room in the list for what stays and for an eighth of the row beside it (keys that share the threshold's top digit)
-  int64_t capacity = (int64_t)p.max_keep + p.max_ctx_len / 8 + 1024;
+  // room in the list for what stays and for what the sample's margin and the threshold's bin bring with them
+  int64_t capacity = (int64_t)p.max_keep + p.max_keep / 4 * 3 + 2048;
   if (capacity > p.max_ctx_len) capacity = p.max_ctx_len;
-  if (capacity > 18176) capacity = 18176;
+  if (capacity > 18432) capacity = 18432;
   capacity = (capacity + 3) / 4 * 4;
   int words = (p.max_ctx_len + 31) / 32;
-  if (words > 8192) words = 8192;
-  if (p.max_ctx_len > 32768) return launch_select_t<1024>(p, rows, (int)capacity, words, s);
-  return launch_select_t<512>(p, rows, (int)capacity, words, s);
+  if (words > 4096) words = 4096;
+  // Long rows: one block per SM with as many loads in flight as its registers hold; short rows: several blocks per SM,
+  // whose steps overlap.
+  if (p.max_ctx_len > 32768) return launch_select_t<512, 8>(p, rows, (int)capacity, words, s);
+  return launch_select_t<256, 4>(p, rows, (int)capacity, words, s);
 }
 
 cudaError_t hswa_launch_evict_compact(const CompactParams& p, int num_sms, cudaStream_t s) {
