@@ -411,19 +411,22 @@ __global__ void __launch_bounds__(T, T == 256 ? 4 : 1) evict_select_kernel(const
   // ---- the kept positions: keys above the threshold, and the first `want` of those equal to it ----
   if (listed) {
     uint32_t done_gt = 0, done_eq = 0;
-    for (int i = tid; i < (int)n_list; i += T) {  // what stays, by kind, in the positions' sign bits: the keys' room is wanted
-      const uint32_t k = l_key[i];
-      l_pos[i] = k < thr ? -1 : (k > thr ? l_pos[i] : l_pos[i] | (int)0x80000000);
+    int32_t* in_order = reinterpret_cast<int32_t*>(l_key);  // [keep]: written when the keys have been looked at
+    const bool windows = ctx > words * 32;
+    if (windows) {  // the list is gone through more than once: what stays, by kind, goes into the positions' sign bits
+      for (int i = tid; i < (int)n_list; i += T) {
+        const uint32_t k = l_key[i];
+        l_pos[i] = k < thr ? -1 : (k > thr ? l_pos[i] : l_pos[i] | (int)0x80000000);
+      }
     }
-    int32_t* in_order = reinterpret_cast<int32_t*>(l_key);  // [keep]
-    __syncthreads();
     for (int win = 0; win < ctx; win += words * 32) {  // positions a bitmap at a time
       const int n_words = min(words, (ctx - win + 31) / 32), each = (n_words + T - 1) / T;
       for (int i = tid; i < map_at(n_words); i += T) map_gt[i] = map_eq[i] = 0;
       __syncthreads();
       for (int i = tid; i < (int)n_list; i += T) {
         const int at = l_pos[i], j = (at & 0x7fffffff) - win;
-        if (at != -1 && j >= 0 && j < n_words * 32) atomicOr((at >= 0 ? map_gt : map_eq) + map_at(j >> 5), 1u << (j & 31));
+        const bool above = windows ? at >= 0 : l_key[i] > thr, counts = windows ? at != -1 : l_key[i] >= thr;
+        if (counts && j >= 0 && j < n_words * 32) atomicOr((above ? map_gt : map_eq) + map_at(j >> 5), 1u << (j & 31));
       }
       __syncthreads();
       // a thread's words are consecutive; counts of both kinds in one number (a list is shorter than 2^16)
@@ -583,12 +586,12 @@ cudaError_t hswa_launch_evict_select(const SelectParams& p, cudaStream_t s) {
   if (p.B == 0) return cudaSuccess;
   const int64_t rows = (int64_t)p.B * p.Hkv;
   // room in the list for what stays and for what the sample's margin and the threshold's bin bring with them
-  int64_t capacity = (int64_t)p.max_keep + p.max_keep / 4 * 3 + 2048;
+  int64_t capacity = (int64_t)p.max_keep + p.max_keep / 2 + 2048;
   if (capacity > p.max_ctx_len) capacity = p.max_ctx_len;
-  if (capacity > 18432) capacity = 18432;
+  if (capacity > 14848) capacity = 14848;  // (with the bitmaps of 262144 positions, one SM's shared memory)
   capacity = (capacity + 3) / 4 * 4;
   int words = (p.max_ctx_len + 31) / 32;
-  if (words > 4096) words = 4096;
+  if (words > 8192) words = 8192;
   // Long rows: one block per SM with as many loads in flight as its registers hold; short rows: several blocks per SM,
   // whose steps overlap.
   if (p.max_ctx_len > 32768) return launch_select_t<512, 8>(p, rows, (int)capacity, words, s);

@@ -107,9 +107,10 @@ struct PrefillParams {
   int32_t order_mode;    // block order of the Full-layer tile kernel (hswa_set_prefill_order)
   long long* trace;      // per-block {start ns, end ns, SM id, request << 32 | tile} (hswa_set_block_trace) or null
   int64_t trace_cap;
-  // shared-prefix stage of cascade decode only
+  int32_t max_ctx_len;   // cross attention only: host-known bound of ctx_len
+  // shared-prefix stage of cascade decode and cross attention only
   int32_t prefix_len;              // shared tokens (multiple of the page size)
-  int32_t prefix_tiles_per_split;  // 128-key tiles per prefix slice
+  int32_t prefix_tiles_per_split;  // 128-key tiles per prefix slice (cross attention: per key slice)
   int32_t max_splits;              // partial slots per (request, head) row
   float* part_o;
   float2* part_ml;
@@ -192,6 +193,10 @@ cudaError_t hswa_launch_decode_cross(const CUtensorMap& tm_pool, const DecodePar
 // Cross attention, any number of tokens per request: warp-level tile kernel, and the join of key slices
 cudaError_t hswa_launch_cross_mma(const CrossParams& p, cudaStream_t s);
 cudaError_t hswa_launch_cross_combine(const CrossParams& p, cudaStream_t s);
+bool hswa_cross_tc_supported(const ModelParams& m);
+int hswa_cross_tc_tile_tokens(const ModelParams& m);  // tokens per Q tile (box height of tm_q); two tiles per block
+cudaError_t hswa_launch_cross_tc(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const PrefillParams& p, int row_tiles,
+                                 cudaStream_t s);
 int hswa_cross_mma_rows();  // packed (token, head) rows per block
 // Eviction: accumulated attention weights, choice of the kept positions, compaction
 int hswa_attn_weights_tile_tokens(const ModelParams& m, int max_q_len);  // tokens per Q tile (box height of tm_q)

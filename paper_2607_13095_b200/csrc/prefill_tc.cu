@@ -222,6 +222,13 @@ __device__ __forceinline__ void linger_after_error(const int32_t* err) {
 // 3.1.4: requests that share a system prompt share its pages): the 128 rows of a Q tile are 16 requests x
 // the 8 query heads of one KV head, the keys are a slice of the shared prefix pages, nothing is masked, and
 // the block writes an unnormalised (m, l, o) partial per row for the split-K combine instead of an output.
+//
+// MODE_CROSS turns it into cross attention to cached encoder states (hswa_cross_attn): every cached key is visible to every
+// row, so the (token, head) rows of a GQA group are interchangeable, and a Q tile takes 128 / G tokens x the G query heads of
+// one KV head; the two tiles of a block follow one another in the request's tokens.  The keys may be cut into slices
+// (blockIdx.x / row tiles), which leave partials like the prefix stage's.  A block whose tokens fit one Q tile runs with
+// one MMA issuer and one softmax group.
+enum { MODE_PREFILL = 0, MODE_PREFIX = 1, MODE_CROSS = 2 };
 // Does cached tile j (of nA) of a request with ctx cached tokens hold rows that no row of the block can see?  On a
 // Full layer: the last tile when ctx ends inside it.  On an SWA layer: every ring tile (slots older than the window,
 // never written, or past the ring's last page).
@@ -229,7 +236,7 @@ __device__ __forceinline__ bool v_tile_needs_patch(int is_swa, int ctx, int j) {
 
 // STAGES = depth of the K and of the V tile ring: 2 for prefill; 1 for the shared-prefix stage, whose block then leaves
 // room on its SM for a block of the suffix decode kernel that streams beside it.
-template <bool PREFIX, int STAGES>
+template <int MODE, int STAGES>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_constant__ CUtensorMap tm_q,
                   const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
@@ -237,6 +244,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
   // All shared memory is one dynamic window (no static part, so that it starts on the 1 KB boundary the swizzled tiles
   // need without slack): Q tiles | K ring | V ring | barriers and flags.
   extern __shared__ __align__(1024) uint8_t smem[];
+  constexpr bool PREFIX = MODE == MODE_PREFIX, CROSS = MODE == MODE_CROSS;
   constexpr int OFF_V = OFF_K + STAGES * TILE_BYTES;
   constexpr int OFF_STATE = OFF_V + STAGES * TILE_BYTES;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + OFF_STATE);                     // [NUM_BARS]
@@ -250,6 +258,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int pair = blockIdx.x, kh = blockIdx.y;
   int r, b, t0, n, ctx, head, h0, page_off = 0;
+  int tok_tile = 0, nq_tiles = 2, slice = 0;  // CROSS: tokens per Q tile, Q tiles with tokens, key slice
   TileSeq seq;
   if constexpr (PREFIX) {
     // the suffix decode kernel that follows on the stream reads nothing this kernel writes before its own
@@ -271,6 +280,45 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     page_off = 2 * tile_begin;
     ctx = p.prefix_len - tile_begin * BN;  // keys from this slice's first tile to the end of the prefix
     if (seq.nA <= 0) return;               // the host plans slices so that none is empty
+  } else if constexpr (CROSS) {
+    // blockIdx.x = row tile + max_tiles * slice, blockIdx.z = request
+    r = blockIdx.z;
+    b = blockIdx.x % max_tiles;
+    slice = blockIdx.x / max_tiles;
+    t0 = p.b.q_indptr ? p.b.q_indptr[r] : r;
+    n = p.b.q_indptr ? p.b.q_indptr[r + 1] - t0 : 1;
+    const int len = p.b.ctx_len[r];
+    if (threadIdx.x == 0 && blockIdx.x == 0 && kh == 0) {  // the grid was sized from the host's bounds
+      if (len < 0 || len > p.max_ctx_len) record_error(p.err, HSWA_ERR_BOUNDS, r, -1, len);
+      if (n < 0 || n > p.max_q_len) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, n);
+    }
+    head = 0;
+    h0 = kh * M.G;
+    tok_tile = BM / M.G;
+    if (b * 2 * tok_tile >= n) return;  // uniform for the block
+    nq_tiles = (b * 2 + 1) * tok_tile < n ? 2 : 1;
+    const int tile_begin = slice * p.prefix_tiles_per_split;
+    ctx = max(0, min(len, p.max_ctx_len) - tile_begin * BN);  // keys from this slice's first tile to the end
+    seq.nA = min(p.prefix_tiles_per_split, (ctx + BN - 1) / BN);
+    seq.c_lo = 0;
+    seq.nB = 0;
+    page_off = 2 * tile_begin;
+    if (seq.nA <= 0) {
+      // no key here: zeros (no states at all), or a partial that the join passes over
+      const int rows = min(2 * tok_tile, n - b * 2 * tok_tile) * M.G;
+      for (int row = threadIdx.x; row < rows; row += NUM_THREADS) {
+        const int64_t orow = (int64_t)(t0 + b * 2 * tok_tile + row / M.G) * M.Hq + h0 + row % M.G;
+        if (p.max_splits > 1) {
+          p.part_ml[orow * p.max_splits + slice] = make_float2(-INFINITY, 0.f);
+          continue;
+        }
+        uint4* dst = M.out_fp32 ? reinterpret_cast<uint4*>(reinterpret_cast<float*>(p.out) + orow * HD)
+                                : reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + orow * HD);
+        for (int k = 0; k < (M.out_fp32 ? 32 : 16); ++k) dst[k] = make_uint4(0, 0, 0, 0);
+        if (p.lse) p.lse[orow] = -INFINITY;
+      }
+      return;
+    }
   } else {
     if (p.order_mode >= 2 && !p.is_swa) {
       // longest request first (2) or globally longest tile first (3); on SWA layers every tile costs the same and the
@@ -307,7 +355,8 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
   // An earlier block gave up: do not queue behind it.  One thread reads the error word so that the whole block
   // takes the same decision (the MMA issuers below wait for each other on counted barriers).
   if (threadIdx.x == 0) {
-    mma_abort = *reinterpret_cast<volatile int32_t*>(p.err) != 0;
+    const int32_t recorded = *reinterpret_cast<volatile int32_t*>(p.err);
+    mma_abort = CROSS ? recorded == HSWA_ERR_TIMEOUT : recorded != 0;
     if (sbase & 1023u) {  // the swizzled tile addressing assumes a 1 KB-aligned window
       record_error(p.err, HSWA_ERR_CUDA, -1, (int)(sbase & 1023u), 14);
       mma_abort = 1;
@@ -326,9 +375,9 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     mbar_init(bar(BAR_Q), 1);
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(bar(BAR_KFULL + s), 1);
-      mbar_init(bar(BAR_KEMPTY + s), 2);  // one commit per MMA issuer
+      mbar_init(bar(BAR_KEMPTY + s), CROSS ? nq_tiles : 2);  // one commit per MMA issuer
       mbar_init(bar(BAR_VFULL + s), 1);
-      mbar_init(bar(BAR_VEMPTY + s), 2);
+      mbar_init(bar(BAR_VEMPTY + s), CROSS ? nq_tiles : 2);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(BAR_SFULL + i), 1);
@@ -362,10 +411,12 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       tma_prefetch_desc(&tm_q);
       tma_prefetch_desc(&tm_k);
       tma_prefetch_desc(&tm_v);
-      mbar_arrive_expect_tx(bar(BAR_Q), 2 * TILE_BYTES);
-      for (int i = 0; i < 2; ++i)
+      mbar_arrive_expect_tx(bar(BAR_Q), CROSS ? nq_tiles * 2 * tok_tile * M.G * 128 : 2 * TILE_BYTES);
+      for (int i = 0; i < nq_tiles; ++i)
         for (int hf = 0; hf < 2; ++hf) {
-          if constexpr (PREFIX)  // box {64, 8 heads, 16 requests} over q [B][Hq][D]
+          if constexpr (CROSS)  // box {64, G heads, tok_tile tokens} over q [T][Hq][D]
+            tma_load_3d(sbase + OFF_Q + i * TILE_BYTES + hf * HALF_BYTES, &tm_q, bar(BAR_Q), hf * 64, h0, t0 + (2 * b + i) * tok_tile);
+          else if constexpr (PREFIX)  // box {64, 8 heads, 16 requests} over q [B][Hq][D]
             tma_load_3d(sbase + OFF_Q + i * TILE_BYTES + hf * HALF_BYTES, &tm_q, bar(BAR_Q), hf * 64, h0, r + 16 * i);
           else
             tma_load_3d(sbase + OFF_Q + i * TILE_BYTES + hf * HALF_BYTES, &tm_q, bar(BAR_Q), hf * 64, h0 + i, t0 + b * BM);
@@ -434,7 +485,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_SERVICE) : "memory");
     // ======================= MMA issuer =======================
     // The whole warp walks the loop converged (waits, descriptor arithmetic); one elected lane issues.
-    {
+    if (!CROSS || warp - 9 < nq_tiles) {
       bool ok = mbar_wait(bar(BAR_Q), 0);
       const uint64_t dQ0 = smem_desc(sbase + OFF_Q, 16), dQ1 = smem_desc(sbase + OFF_Q + TILE_BYTES, 16);
       const uint64_t dK0 = smem_desc(sbase + OFF_K, 16), dV0 = smem_desc(sbase + OFF_V, HALF_BYTES);
@@ -471,8 +522,12 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       // passing the token, and passes it whenever it finds the abort flag set, so neither can wait forever.
       const int i = warp - 9;
       const int tok_in = i == 0 ? 2 : 1, tok_out = i == 0 ? 1 : 2;
-      auto token_wait = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(tok_in) : "memory"); };
+      auto token_wait = [&]() {
+        if (CROSS && nq_tiles == 1) return;  // a single issuer has every turn
+        asm volatile("bar.sync %0, 64;" ::"r"(tok_in) : "memory");
+      };
       auto token_pass = [&]() {
+        if (CROSS && nq_tiles == 1) return;
         __threadfence_block();  // the abort flag, if set, is visible to the warp this releases
         asm volatile("bar.arrive %0, 64;" ::"r"(tok_out) : "memory");
       };
@@ -571,11 +626,12 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     const uint32_t tS = tmem + lane_addr + i * 128;
     const uint32_t tO = tmem + lane_addr + 256 + i * 128;
+    const bool here = !CROSS || i < nq_tiles;   // (a Q tile without tokens has no work)
     const int ri = b * BM + rr;                 // chunk-relative row
     const int pos = ctx + ri;                   // absolute position
     float m_st = -INFINITY, l_run = 0.f;
     bool ok = true;
-    for (int j = 0; j < n_tiles; ++j) {
+    for (int j = 0; j < (here ? n_tiles : 0); ++j) {
       ok = __all_sync(0xffffffffu, mbar_wait(bar(BAR_SFULL + i), j & 1));  // warp-uniform: TMEM ops are warp-wide
       if (!ok) {
         if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, j, 30 + i);
@@ -715,15 +771,19 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       l_run += (a01.x + a01.y) + (a23.x + a23.y);
     }
     // ---- epilogue: O / l -> global ----
-    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(BAR_OFINAL + i), 0));
+    if (ok && here) ok = __all_sync(0xffffffffu, mbar_wait(bar(BAR_OFINAL + i), 0));
     if (!ok && lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, b, 40 + i);
     tc_fence_after();
     const float l_tot = l_run;
-    if constexpr (PREFIX) {
-      // partial for the split-K combine: row = (request, head), unnormalised o with its (m, l)
+    const int tok = CROSS ? (2 * b + i) * tok_tile + rr / M.G : 0;  // CROSS: this row's token and its output row
+    const bool tok_ok = CROSS && here && rr < tok_tile * M.G && tok < n;
+    const int64_t cross_row = CROSS ? (int64_t)(t0 + tok) * M.Hq + h0 + rr % M.G : 0;
+    if (PREFIX || (CROSS && p.max_splits > 1)) {
+      // partial for the split-K combine: row = (request, head) or (token, head), unnormalised o with its (m, l)
       const int rq = r + 16 * i + (rr >> 3);
-      const bool row_ok = ok && rq < p.b.B;
-      const int64_t prow = ((int64_t)rq * M.Hq + kh * M.G + (rr & 7)) * p.max_splits + blockIdx.x;
+      const bool row_ok = ok && (CROSS ? tok_ok : rq < p.b.B);
+      const int64_t prow = CROSS ? cross_row * p.max_splits + slice
+                                 : ((int64_t)rq * M.Hq + kh * M.G + (rr & 7)) * p.max_splits + blockIdx.x;
 #pragma unroll 1
       for (int c4 = 0; c4 < 4; ++c4) {
         uint32_t w[32];
@@ -739,9 +799,10 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       }
       if (row_ok) p.part_ml[prow] = make_float2(m_st, l_tot);
     } else {
-      const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-      const bool row_ok = ok && ri < n;
-      const int64_t orow = ((int64_t)(t0 + ri) * M.Hq + (h0 + i));
+      const bool some = CROSS ? l_tot != 0.f : l_tot > 0.f;  // (CROSS: a NaN among the inputs shows in the output)
+      const float inv = some ? 1.f / l_tot : 0.f;
+      const bool row_ok = ok && (CROSS ? tok_ok : ri < n);
+      const int64_t orow = CROSS ? cross_row : ((int64_t)(t0 + ri) * M.Hq + (h0 + i));
 #pragma unroll 1
       for (int c4 = 0; c4 < 4; ++c4) {
         uint32_t w[32];
@@ -769,7 +830,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
           }
         }
       }
-      if (row_ok && p.lse) p.lse[orow] = l_tot > 0.f ? (m_st + log2f(l_tot)) * 0.6931471805599453f : -INFINITY;
+      if (row_ok && p.lse) p.lse[orow] = some ? (m_st + log2f(l_tot)) * 0.6931471805599453f : -INFINITY;
     }
   }
 
@@ -1534,7 +1595,7 @@ cudaError_t hswa_launch_prefill_tc(const CUtensorMap& tm_pool, const CUtensorMap
                                    const CUtensorMap& tm_v, const PrefillParams& p, int tile_limit, cudaStream_t s) {
   if (p.b.B == 0 || p.total_q == 0 || p.max_q_len == 0) return cudaSuccess;
   constexpr int SMEM_BYTES = tile_kernel_smem(KV_STAGES);
-  auto kern = prefill_tc_kernel<false, KV_STAGES>;
+  auto kern = prefill_tc_kernel<MODE_PREFILL, KV_STAGES>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
   if (e != cudaSuccess) return e;
   static const cudaError_t budget = check_register_budget(kern, NUM_THREADS);
@@ -1554,7 +1615,7 @@ cudaError_t hswa_launch_decode_prefix(const CUtensorMap& tm_pool, const CUtensor
   if (p.b.B == 0 || n_slices <= 0) return cudaSuccess;
   constexpr int PREFIX_STAGES = KV_STAGES;
   constexpr int SMEM_BYTES = tile_kernel_smem(PREFIX_STAGES);
-  auto kern = prefill_tc_kernel<true, PREFIX_STAGES>;
+  auto kern = prefill_tc_kernel<MODE_PREFIX, PREFIX_STAGES>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
   if (e != cudaSuccess) return e;
   e = cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
@@ -1563,6 +1624,22 @@ cudaError_t hswa_launch_decode_prefix(const CUtensorMap& tm_pool, const CUtensor
   if (budget != cudaSuccess) return budget;
   dim3 grid(n_slices, p.m.Hkv, (p.b.B + 31) / 32);
   kern<<<grid, NUM_THREADS, SMEM_BYTES, s>>>(tm_pool, tm_q, tm_pool, tm_pool, p, 1);
+  return cudaGetLastError();
+}
+
+// Cross attention: grid (row tiles x key slices, KV heads, requests).  tm_q has box {64, G heads, 128 / G tokens} over q
+// [T][Hq][D]; p carries the host's bounds, the slice plan and, for more than one slice, the partial buffers.
+bool hswa_cross_tc_supported(const ModelParams& m) { return m.D == 128 && m.P == 64; }
+int hswa_cross_tc_tile_tokens(const ModelParams& m) { return BM / m.G; }
+cudaError_t hswa_launch_cross_tc(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const PrefillParams& p, int row_tiles, cudaStream_t s) {
+  constexpr int SMEM_BYTES = tile_kernel_smem(KV_STAGES);
+  auto kern = prefill_tc_kernel<MODE_CROSS, KV_STAGES>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+  if (e != cudaSuccess) return e;
+  static const cudaError_t budget = check_register_budget(kern, NUM_THREADS);
+  if (budget != cudaSuccess) return budget;
+  dim3 grid(row_tiles * p.max_splits, p.m.Hkv, p.b.B);
+  kern<<<grid, NUM_THREADS, SMEM_BYTES, s>>>(tm_pool, tm_q, tm_pool, tm_pool, p, row_tiles);
   return cudaGetLastError();
 }
 
