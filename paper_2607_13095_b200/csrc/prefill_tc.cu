@@ -142,11 +142,10 @@ __device__ __forceinline__ bool pick_longest_first(const BatchParams& bp, int id
 // tiles_r (ties: ascending request), and inside a request the longest tile goes first, so that the launch ends on the
 // shortest tiles of the shortest request.  Same search as above on T(w) = number of tiles of all requests whose key
 // is >= w.
-__device__ __forceinline__ bool pick_longest_request_first(const BatchParams& bp, int idx, int lane, int* r_out, int* b_out) {
-  auto tiles_of = [&](int r, int& key, int& nt) {
-    nt = (bp.q_indptr[r + 1] - bp.q_indptr[r] + BM - 1) / BM;
-    key = nt > 0 ? (bp.ctx_len[r] + BN - 1) / BN + nt : 0;
-  };
+// tiles_of(r, key, nt) gives a request's key and number of tiles (0: it has none and its key is 0).
+template <typename TilesOf>
+__device__ __forceinline__ bool pick_longest_request_first(const BatchParams& bp, int idx, int lane, TilesOf tiles_of, int* r_out,
+                                                           int* b_out) {
   auto tiles_ge = [&](int w) {
     int c = 0;
     for (int r = lane; r < bp.B; r += 32) {
@@ -281,8 +280,24 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     ctx = p.prefix_len - tile_begin * BN;  // keys from this slice's first tile to the end of the prefix
     if (seq.nA <= 0) return;               // the host plans slices so that none is empty
   } else if constexpr (CROSS) {
-    // blockIdx.x = row tile + max_tiles * slice, blockIdx.z = request
-    r = blockIdx.z;
+    // blockIdx.x = row tile + max_tiles * slice, blockIdx.z = request: the one with most keys first, so that the launch
+    // ends on short blocks
+    if (gridDim.z > 1) {
+      if (warp == 0) {
+        int pr = -1, pb = 0;
+        auto one_each = [&](int rq, int& key, int& nt) {
+          nt = 1;
+          key = 1 + (max(0, min(p.b.ctx_len[rq], p.max_ctx_len)) + BN - 1) / BN;
+        };
+        pick_longest_request_first(p.b, (int)blockIdx.z, lane, one_each, &pr, &pb);
+        if (lane == 0) picked[0] = pr;
+      }
+      __syncthreads();
+      r = picked[0];
+      if (r < 0) return;  // uniform for the block
+    } else {
+      r = 0;
+    }
     b = blockIdx.x % max_tiles;
     slice = blockIdx.x / max_tiles;
     t0 = p.b.q_indptr ? p.b.q_indptr[r] : r;
@@ -302,7 +317,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     seq.nA = min(p.prefix_tiles_per_split, (ctx + BN - 1) / BN);
     seq.c_lo = 0;
     seq.nB = 0;
-    page_off = 2 * tile_begin;
+    page_off = BN / M.P * tile_begin;
     if (seq.nA <= 0) {
       // no key here: zeros (no states at all), or a partial that the join passes over
       const int rows = min(2 * tok_tile, n - b * 2 * tok_tile) * M.G;
@@ -325,7 +340,11 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       // order does not matter
       if (warp == 0) {
         int pr = -1, pb = 0;
-        const bool got = p.order_mode == 2 ? pick_longest_request_first(p.b, (int)blockIdx.z, lane, &pr, &pb)
+        auto tiles_of = [&](int rq, int& key, int& nt) {
+          nt = (p.b.q_indptr[rq + 1] - p.b.q_indptr[rq] + BM - 1) / BM;
+          key = nt > 0 ? (p.b.ctx_len[rq] + BN - 1) / BN + nt : 0;
+        };
+        const bool got = p.order_mode == 2 ? pick_longest_request_first(p.b, (int)blockIdx.z, lane, tiles_of, &pr, &pb)
                                            : pick_longest_first(p.b, (int)blockIdx.z, lane, &pr, &pb);
         if (!got) pr = -1;
         if (lane == 0) {
@@ -424,11 +443,40 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     }
     // page ids of the cached tiles, 32 at a time
     const int32_t* tbl = p.is_swa ? p.b.ring_table + (int64_t)r * M.R : p.b.block_table + (int64_t)r * p.b.max_blocks + page_off;
-    const int n_pages = p.is_swa ? M.R : (ctx + PG - 1) / PG;
-    int pid_next = lane < n_pages ? tbl[lane] : 0;
+    const int n_pages = p.is_swa ? M.R : (ctx + (CROSS ? M.P : PG) - 1) / (CROSS ? M.P : PG);
+    const int ppt = CROSS ? BN / M.P : 2;  // pages per tile
+    auto page_of = [&](int j) { return tbl[min(j * ppt + (lane & (ppt - 1)), n_pages - 1)]; };  // a missing page repeats the last
+    int pid_next = CROSS ? page_of(0) : (lane < n_pages ? tbl[lane] : 0);
     int pid_cur = 0;
     bool ok = true;
-    for (int j = 0; j < n_tiles && ok; ++j) {
+    if constexpr (CROSS) {
+      // any page size: lane i < ppt loads page i of the tile
+      for (int j = 0; j < n_tiles && ok; ++j) {
+        const int stage = j % STAGES;
+        int page = pid_next;
+        pid_next = page_of(j + 1);
+        if (lane < ppt && (page < 0 || page >= p.num_pages)) {
+          record_error(p.err, HSWA_ERR_BOUNDS, r, page_off + min(j * ppt + lane, n_pages - 1), page);
+          page = 0;
+        }
+        const uint32_t par = ((j / STAGES) - 1) & 1;
+        for (int kv = 0; kv < 2 && ok; ++kv) {
+          if (j >= STAGES && !__all_sync(0xffffffffu, mbar_wait(bar((kv ? BAR_VEMPTY : BAR_KEMPTY) + stage), par))) {
+            if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, j, 10 + kv);
+            ok = false;
+            break;
+          }
+          const uint32_t full = kv && v_tile_needs_patch(0, ctx, j) ? bar(BAR_VPATCH + stage) : bar((kv ? BAR_VFULL : BAR_KFULL) + stage);
+          if (lane == 0) mbar_arrive_expect_tx(full, TILE_BYTES);
+          __syncwarp();
+          if (lane < ppt) {
+            const uint32_t dst = sbase + (kv ? OFF_V : OFF_K) + stage * TILE_BYTES + lane * M.P * 128;
+            for (int hf = 0; hf < 2; ++hf) tma_load_4d(dst + hf * HALF_BYTES, &tm_pool, full, hf * 64, 0, kv * M.Hkv + kh, page);
+          }
+        }
+      }
+    }
+    for (int j = 0; !CROSS && j < n_tiles && ok; ++j) {
       const int stage = j % STAGES;
       int pg[2] = {0, 0};
       // Rows of a cached tile that no row of this block can see (the tail of the last page of a Full layer; ring
@@ -1629,7 +1677,7 @@ cudaError_t hswa_launch_decode_prefix(const CUtensorMap& tm_pool, const CUtensor
 
 // Cross attention: grid (row tiles x key slices, KV heads, requests).  tm_q has box {64, G heads, 128 / G tokens} over q
 // [T][Hq][D]; p carries the host's bounds, the slice plan and, for more than one slice, the partial buffers.
-bool hswa_cross_tc_supported(const ModelParams& m) { return m.D == 128 && m.P == 64; }
+bool hswa_cross_tc_supported(const ModelParams& m) { return m.D == 128; }
 int hswa_cross_tc_tile_tokens(const ModelParams& m) { return BM / m.G; }
 cudaError_t hswa_launch_cross_tc(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const PrefillParams& p, int row_tiles, cudaStream_t s) {
   constexpr int SMEM_BYTES = tile_kernel_smem(KV_STAGES);
