@@ -156,7 +156,7 @@ bool plan_cross(const hswa_handle* h, int batch, int total_q, int max_q_len, int
       c.row_tiles = (int)((rows + hswa_cross_mma_rows() - 1) / hswa_cross_mma_rows());
     }
     const int64_t blocks = (int64_t)c.row_tiles * h->cfg.num_kv_heads * batch;
-    const int64_t want = ((c.tc ? 2LL : 4LL) * h->num_sms + blocks - 1) / blocks, most = (max_ctx_len + 511) / 512;
+    const int64_t want = ((c.tc ? 1LL : 4LL) * h->num_sms + blocks - 1) / blocks, most = (max_ctx_len + 511) / 512;
     int64_t slices = want < most ? want : most;
     if (slices < 1) slices = 1;
     c.slice_len = (int)((((int64_t)max_ctx_len + slices - 1) / slices + 127) / 128 * 128);
