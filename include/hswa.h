@@ -253,6 +253,8 @@ hswa_status hswa_prefill_attn(hswa_handle* h, const hswa_layer* layer, const hsw
  * (HSWA_ERR_INVALID_ARG).  A request longer than max_ctx_len or max_q_len is recorded as HSWA_ERR_BOUNDS (index -1 / -2)
  * and what the bounds cover is computed.
  *
+ * This call and the eviction calls below refuse a current device other than the handle's (HSWA_ERR_INVALID_ARG).
+ *
  * hswa_cross_workspace_need: exact bytes for a call with these host-known fields; pure host arithmetic. */
 size_t hswa_cross_workspace_need(const hswa_handle* h, int32_t batch, int32_t total_q, int32_t max_q_len, int32_t max_ctx_len);
 hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_batch* batch, const void* q, void* out,

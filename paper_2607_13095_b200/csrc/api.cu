@@ -56,6 +56,12 @@ hswa_status check_common(const hswa_handle* h, const hswa_layer* layer, const hs
   return HSWA_OK;
 }
 
+// The launches go to the current device, whose stream the caller passes: it has to be the handle's.
+bool device_is_current(const hswa_handle* h) {
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess && dev == h->device;
+}
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // Keys per split for Full-layer decode: long enough that the partial (m, l, o) traffic stays below one
@@ -683,7 +689,7 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
   if (!plan_cross(h, b->batch, b->total_q, b->max_q_len, b->max_ctx_len, &pl)) return HSWA_ERR_UNSUPPORTED;
   if (pl.o_bytes > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < pl.o_bytes + pl.ml_bytes))
     return HSWA_ERR_WORKSPACE;
-  if (cudaSetDevice(h->device) != cudaSuccess) return HSWA_ERR_CUDA;
+  if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
   float* part_o = pl.o_bytes > 0 ? static_cast<float*>(workspace) : nullptr;
   float2* part_ml = pl.o_bytes > 0 ? reinterpret_cast<float2*>(static_cast<char*>(workspace) + pl.o_bytes) : nullptr;
   cudaStream_t s = (cudaStream_t)stream;
@@ -767,7 +773,7 @@ hswa_status hswa_attn_weights(hswa_handle* h, const hswa_layer* layer, const hsw
   if (b->max_ctx_len == 0 && (!causal || b->max_q_len == 0)) return HSWA_OK;
   if (!weights || (b->total_q > 0 && (!q || !lse || !aligned16(q)))) return HSWA_ERR_INVALID_ARG;
   if (b->batch > 65535 || h->cfg.num_kv_heads > 65535) return HSWA_ERR_UNSUPPORTED;
-  if (cudaSetDevice(h->device) != cudaSuccess) return HSWA_ERR_CUDA;
+  if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
   WeightsParams p = {};
   p.m = model_params(h);
   p.b = batch_params(b);
@@ -800,7 +806,7 @@ hswa_status hswa_evict_select(hswa_handle* h, int32_t batch, const int32_t* ctx_
   if (batch == 0) return HSWA_OK;
   if (!ctx_len || !keep_len || !kept_len || (max_keep > 0 && !keep_idx) || (max_ctx_len > 0 && !weights)) return HSWA_ERR_INVALID_ARG;
   if ((int64_t)batch * h->cfg.num_kv_heads > INT32_MAX) return HSWA_ERR_UNSUPPORTED;
-  if (cudaSetDevice(h->device) != cudaSuccess) return HSWA_ERR_CUDA;
+  if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
   SelectParams p = {};
   p.B = batch;
   p.Hkv = h->cfg.num_kv_heads;
@@ -833,7 +839,7 @@ hswa_status hswa_evict_compact(hswa_handle* h, const hswa_layer* layer, const hs
   if ((weights == nullptr) != (weights_out == nullptr)) return HSWA_ERR_INVALID_ARG;
   if (weights && (weights_stride < b->max_ctx_len || weights_out_stride < max_keep || weights == weights_out)) return HSWA_ERR_INVALID_ARG;
   if (b->batch > 65535 || h->cfg.num_kv_heads > 65535) return HSWA_ERR_UNSUPPORTED;
-  if (cudaSetDevice(h->device) != cudaSuccess) return HSWA_ERR_CUDA;
+  if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
   CompactParams p = {};
   p.m = model_params(h);
   p.b = batch_params(b);
