@@ -39,7 +39,8 @@ struct SelectShared {
   uint32_t warp_sum[2][T / 32];   // packed counts per warp, two buffers in turn
   uint32_t warp_sum2[2][T / 32];
   uint32_t digit, want, n_list, n_near;
-  uint32_t near[T];               // the keys that share the threshold's bin, when they are few
+  uint32_t near[T];               // the keys that share the threshold's bin, when they are few, and their positions
+  int near_pos[T], last;
 };
 
 // Position of a block-wide ordered step: thread-order prefix sums of four counts per thread (each at most 4), tile by tile.
@@ -125,7 +126,7 @@ __device__ __forceinline__ uint32_t find_digit(SelectShared<T>& sh, int bins, ui
 // T threads; CQ quads of keys per thread in flight while as many are looked at.
 template <int T, int CQ>
 __global__ void __launch_bounds__(T, T == 256 ? 4 : 1) evict_select_kernel(const SelectParams p, const int capacity, const int words) {
-  extern __shared__ __align__(16) uint32_t list[];  // [capacity] keys, [capacity] positions, [3] padded arrays of `words`
+  extern __shared__ __align__(16) uint32_t list[];  // [capacity] keys, [capacity] positions, [2] padded arrays of `words`
   __shared__ SelectShared<T> sh;
   const int row = blockIdx.x, kh = row % p.Hkv, r = row / p.Hkv;
   const int tid = threadIdx.x;
@@ -179,9 +180,8 @@ __global__ void __launch_bounds__(T, T == 256 ? 4 : 1) evict_select_kernel(const
   uint32_t* l_key = list;
   int32_t* l_pos = reinterpret_cast<int32_t*>(list + capacity);
   int turn = 0;
-  uint32_t* map_gt = list + 2 * capacity;
-  uint32_t* map_eq = map_gt + map_at(words);
-  uint32_t* map_before = map_eq + map_at(words);
+  uint32_t* map = list + 2 * capacity;                // the positions that stay, a bit each
+  uint32_t* map_before = map + map_at(words);         // how many come before a word's
   const int lane = tid & 31;
   // Keys from `least_key` on, and their positions, into the list as far as they fit; returns their number.
   auto collect = [&](uint32_t least_key) {
@@ -191,11 +191,21 @@ __global__ void __launch_bounds__(T, T == 256 ? 4 : 1) evict_select_kernel(const
     const bool plain = least_key >= 0x80000000u;
     if (tid == 0) sh.n_list = 0;
     __syncthreads();
+    // Quads [q_in, q_out) lie in the row and hold no protected place; a warp's round is mostly made of such.
+    const int q_in = (min(max(p.protect_first, 0), ctx) + mis + 3) / 4;
+    const int q_out = max(0, ctx - min(p.protect_last, ctx) + mis) / 4;
+    const float4* row4 = reinterpret_cast<const float4*>(w - mis);
+    auto all_in = [&](int q0) { return q0 >= q_in && q0 + (CQ - 1) * T + 32 <= q_out; };
     float4 v[CQ];
     auto fetch = [&](int q0) {
+      if (all_in(q0)) {
 #pragma unroll
-      for (int u = 0; u < CQ; ++u)
-        if (q0 + u * T + lane < quads) v[u] = load_quad(q0 + u * T + lane);
+        for (int u = 0; u < CQ; ++u) v[u] = __ldg(row4 + q0 + u * T + lane);
+      } else {
+#pragma unroll
+        for (int u = 0; u < CQ; ++u)
+          if (q0 + u * T + lane < quads) v[u] = load_quad(q0 + u * T + lane);
+      }
     };
     fetch(tid - lane);
     for (int q0 = tid - lane; q0 < quads; q0 += CQ * T) {  // (the same for the lanes of a warp)
@@ -204,24 +214,25 @@ __global__ void __launch_bounds__(T, T == 256 ? 4 : 1) evict_select_kernel(const
       for (int u = 0; u < CQ; ++u) x[u] = v[u];
       fetch(q0 + CQ * T);  // the next round's loads are under way meanwhile
       uint32_t take = 0;   // four bits per quad
+      if (plain && all_in(q0)) {
 #pragma unroll
-      for (int u = 0; u < CQ; ++u) {
-        const int q = q0 + u * T + lane, j = q * 4 - mis;
-        if (q < quads) {
-          uint32_t t;
-          if (plain && j >= p.protect_first && j + 4 <= ctx - p.protect_last) {
-            t = (x[u].x >= least ? 1u : 0u) | (x[u].y >= least ? 2u : 0u) | (x[u].z >= least ? 4u : 0u) | (x[u].w >= least ? 8u : 0u);
-          } else {
-            uint32_t k[4];
-            keys_of(x[u], q, k);
-            t = 0;
+        for (int u = 0; u < CQ; ++u)
+          take |= (x[u].x >= least ? 1u << (4 * u) : 0u) | (x[u].y >= least ? 2u << (4 * u) : 0u) |
+                  (x[u].z >= least ? 4u << (4 * u) : 0u) | (x[u].w >= least ? 8u << (4 * u) : 0u);
+      } else {
+#pragma unroll 1
+        for (int u = 0; u < CQ; ++u) {
+          const int q = q0 + u * T + lane;
+          if (q >= quads) break;
+          uint32_t k[4], t = 0;
+          keys_of(load_quad(q), q, k);  // (loaded again: this is the row's two ends)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) t |= (k[e] >= least_key ? 1u : 0u) << e;
-            t &= quad_inside(q);
-          }
-          take |= t << (4 * u);
+          for (int e = 0; e < 4; ++e) t |= (k[e] >= least_key ? 1u : 0u) << e;
+          take |= (t & quad_inside(q)) << (4 * u);
         }
+        __syncwarp();
       }
+      if (!__any_sync(0xffffffffu, take != 0)) continue;
       const uint32_t mine = __popc(take);
       uint32_t incl = mine;
 #pragma unroll
@@ -339,12 +350,21 @@ __global__ void __launch_bounds__(T, T == 256 ? 4 : 1) evict_select_kernel(const
   };
   // One step: the bin of 2^shift keys that holds the threshold; false if that is the last bin of a range cut off at 2^32
   // keys, which also holds everything beyond.
-  auto narrow = [&](int shift) {
+  // by_pos: among the listed keys equal to `thr`, the same for their positions from the lowest on (as their complements).
+  uint32_t thr = 0;
+  auto narrow = [&](int shift, bool by_pos) {
     const int bins = bits == 32 ? SEL_BINS : 1 << (bits - shift);
     clear_hist();
     for (int q = tid; q < n_quads; q += T) {
       uint32_t k[4];
-      const uint32_t in = get(q, k);
+      uint32_t in = get(q, k);
+      if (by_pos) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (k[e] != thr) in &= ~(1u << e);
+          k[e] = ~(uint32_t)l_pos[q * 4 + e];
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const uint32_t b = k[e] >= low ? (k[e] - low) >> shift : 0xffffffffu;
@@ -363,76 +383,89 @@ __global__ void __launch_bounds__(T, T == 256 ? 4 : 1) evict_select_kernel(const
   if (bits == 32) {
     // A list from `low` on: bins of 2^16 keys (1/128 of an octave) over 16 octaves tell most apart and keep the keys of a
     // warp out of one bin; if the threshold lies beyond, bins of whole digits.
-    if (!narrow(16)) {
+    if (!narrow(16, false)) {
       low = 0;
-      narrow(21);
+      narrow(21, false);
     }
   }
-  uint32_t thr = low;
+  int last_tie = -1;  // listed: of the keys equal to the threshold, those up to this position stay
   while (bits > 0) {
     const uint32_t near = sh.hist[sh.digit];  // (as the last step, or the count of the top digit, left them)
     __syncthreads();
-    if (near <= (uint32_t)T) {
-      // few keys share the bin: each is ranked among them
-      if (tid == 0) sh.n_near = 0;
-      __syncthreads();
-      for (int q = tid; q < n_quads; q += T) {
-        uint32_t k[4];
-        const uint32_t in = get(q, k);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (((in >> e) & 1u) && k[e] >= low && ((k[e] - low) >> bits) == 0) {
-            const uint32_t at = atomicAdd(&sh.n_near, 1u);
-            if (at < (uint32_t)T) sh.near[at] = k[e];
-          }
-      }
-      __syncthreads();
-      if (tid < (int)near) {
-        const uint32_t k = sh.near[tid];
-        uint32_t above = 0, same = 0;
-        for (int i = 0; i < (int)near; ++i) {
-          above += sh.near[i] > k;
-          same += sh.near[i] == k;
-        }
-        if (above < want && want <= above + same) {  // equal keys write equal values
-          sh.digit = k;
-          sh.want = want - above;
-        }
-      }
-      __syncthreads();
-      thr = sh.digit;
-      want = sh.want;
-      break;
+    if (near > (uint32_t)T) {
+      narrow(bits > 11 ? bits - 11 : 0, false);
+      continue;
     }
-    narrow(bits > 11 ? bits - 11 : 0);
-    thr = low;
+    // few keys share the bin: each is ranked among them, equal ones by position
+    if (tid == 0) sh.n_near = 0;
+    __syncthreads();
+    for (int q = tid; q < n_quads; q += T) {
+      uint32_t k[4];
+      const uint32_t in = get(q, k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (((in >> e) & 1u) && k[e] >= low && ((k[e] - low) >> bits) == 0) {
+          const uint32_t at = atomicAdd(&sh.n_near, 1u);
+          if (at < (uint32_t)T) {
+            sh.near[at] = k[e];
+            sh.near_pos[at] = listed ? l_pos[q * 4 + e] : q * 4 - mis + e;
+          }
+        }
+    }
+    __syncthreads();
+    if (tid < (int)near) {
+      const uint32_t k = sh.near[tid];
+      const int pos = sh.near_pos[tid];
+      uint32_t above = 0, before = 0;  // larger keys; equal ones at lower positions
+      for (int i = 0; i < (int)near; ++i) {
+        above += sh.near[i] > k;
+        before += sh.near[i] == k && sh.near_pos[i] < pos;
+      }
+      if (above + before == want - 1) {  // the last one that stays
+        sh.digit = k;
+        sh.want = before + 1;
+        sh.last = pos;
+      }
+    }
+    __syncthreads();
+    low = sh.digit;
+    want = sh.want;
+    last_tie = sh.last;
+    break;
+  }
+  thr = low;
+  if (listed && bits == 0) {  // many equal keys
+    low = 0;
+    bits = 32;
+    narrow(21, true);
+    narrow(10, true);
+    narrow(0, true);
+    last_tie = (int)~low;
   }
 
   // ---- the kept positions: keys above the threshold, and the first `want` of those equal to it ----
   if (listed) {
-    uint32_t done_gt = 0, done_eq = 0;
+    uint32_t done = 0;
     int32_t* in_order = reinterpret_cast<int32_t*>(l_key);  // [keep]: written when the keys have been looked at
     const bool windows = ctx > words * 32;
-    if (windows) {  // the list is gone through more than once: what stays, by kind, goes into the positions' sign bits
-      for (int i = tid; i < (int)n_list; i += T) {
-        const uint32_t k = l_key[i];
-        l_pos[i] = k < thr ? -1 : (k > thr ? l_pos[i] : l_pos[i] | (int)0x80000000);
-      }
+    auto stays = [&](int i) { return l_key[i] > thr || (l_key[i] == thr && l_pos[i] <= last_tie); };
+    if (windows) {  // the list is gone through more than once: what goes loses its position
+      for (int i = tid; i < (int)n_list; i += T)
+        if (!stays(i)) l_pos[i] = -1;
     }
     for (int win = 0; win < ctx; win += words * 32) {  // positions a bitmap at a time
       const int n_words = min(words, (ctx - win + 31) / 32), each = (n_words + T - 1) / T;
-      for (int i = tid; i < map_at(n_words); i += T) map_gt[i] = map_eq[i] = 0;
+      for (int i = tid; i < map_at(n_words); i += T) map[i] = 0;
       __syncthreads();
       for (int i = tid; i < (int)n_list; i += T) {
-        const int at = l_pos[i], j = (at & 0x7fffffff) - win;
-        const bool above = windows ? at >= 0 : l_key[i] > thr, counts = windows ? at != -1 : l_key[i] >= thr;
-        if (counts && j >= 0 && j < n_words * 32) atomicOr((above ? map_gt : map_eq) + map_at(j >> 5), 1u << (j & 31));
+        const int j = l_pos[i] - win;
+        if (j >= 0 && j < n_words * 32 && (windows || stays(i))) atomicOr(map + map_at(j >> 5), 1u << (j & 31));
       }
       __syncthreads();
-      // a thread's words are consecutive; counts of both kinds in one number (a list is shorter than 2^16)
+      // a thread counts consecutive words
       const int w_lo = min(tid * each, n_words), w_hi = min(w_lo + each, n_words);
       uint32_t c = 0;
-      for (int i = w_lo; i < w_hi; ++i) c += __popc(map_gt[map_at(i)]) | __popc(map_eq[map_at(i)]) << 16;
+      for (int i = w_lo; i < w_hi; ++i) c += __popc(map[map_at(i)]);
       uint32_t incl = c;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
@@ -442,30 +475,18 @@ __global__ void __launch_bounds__(T, T == 256 ? 4 : 1) evict_select_kernel(const
       if (lane == 31) sh.warp_sum[0][tid >> 5] = incl;
       __syncthreads();
       const uint32_t of_warp = lane < T / 32 ? sh.warp_sum[0][lane] : 0u;
-      const uint32_t before = incl - c + sum_of_warps_before(of_warp), all = __reduce_add_sync(0xffffffffu, of_warp);
-      uint32_t at = done_gt + (before & 0xffff), at_eq = done_eq + (before >> 16);
-      for (int i = w_lo; i < w_hi; ++i) {  // where each word's positions go: ties that stay are among the first `want`
-        map_before[map_at(i)] = at + min(at_eq, want);
-        const uint32_t eq = map_eq[map_at(i)];
-        const int room = (int)want - (int)min(at_eq, want);  // drop the ties that do not
-        uint32_t stay = eq;
-        if (__popc(eq) > room) {
-          stay = 0;
-          uint32_t m = eq;
-          for (int k = 0; k < room; ++k, m &= m - 1) stay |= m & (0u - m);
-        }
-        at += __popc(map_gt[map_at(i)]);
-        at_eq += __popc(eq);
-        map_eq[map_at(i)] = stay;
+      uint32_t at = done + incl - c + sum_of_warps_before(of_warp);
+      done += __reduce_add_sync(0xffffffffu, of_warp);
+      for (int i = w_lo; i < w_hi; ++i) {
+        map_before[map_at(i)] = at;
+        at += __popc(map[map_at(i)]);
       }
       __syncthreads();
       for (int i = tid; i < n_words; i += T) {  // full words next to one another fall to different threads
         uint32_t slot = map_before[map_at(i)];
-        for (uint32_t m = map_gt[map_at(i)] | map_eq[map_at(i)]; m != 0; m &= m - 1, ++slot)
+        for (uint32_t m = map[map_at(i)]; m != 0; m &= m - 1, ++slot)
           if (slot < (uint32_t)keep) in_order[slot] = win + i * 32 + __ffs(m) - 1;
       }
-      done_gt += all & 0xffff;
-      done_eq += all >> 16;
       __syncthreads();
     }
     for (int i = tid; i < keep; i += T) out[i] = in_order[i];
@@ -575,7 +596,7 @@ __global__ void __launch_bounds__(256) evict_compact_kernel(const CompactParams 
 
 template <int T, int CQ>
 static cudaError_t launch_select_t(const SelectParams& p, int64_t rows, int capacity, int words, cudaStream_t s) {
-  const int smem = capacity * 8 + map_at(words) * 12;
+  const int smem = (capacity + map_at(words)) * 8;
   cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<T, CQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   evict_select_kernel<T, CQ><<<(unsigned)rows, T, smem, s>>>(p, capacity, words);
@@ -585,16 +606,19 @@ static cudaError_t launch_select_t(const SelectParams& p, int64_t rows, int capa
 cudaError_t hswa_launch_evict_select(const SelectParams& p, cudaStream_t s) {
   if (p.B == 0) return cudaSuccess;
   const int64_t rows = (int64_t)p.B * p.Hkv;
-  // room in the list for what stays and for what the sample's margin and the threshold's bin bring with them
-  int64_t capacity = (int64_t)p.max_keep + p.max_keep / 2 + 2048;
+  // Room in the list for what stays and for what the sample's margin and the threshold's bin bring with them (1.2 to 1.4
+  // times what stays).  Long rows: one block per SM with as many loads in flight as its registers hold; the data of a load
+  // in flight needs room in L1, which shares its memory with this one: 213 KB of shared memory instead of 195 or less
+  // took 16 rows of 8 heads and up to 262144 positions from 54 to 71 us.  Short rows: four blocks per SM, whose steps overlap
+  // (36.5 us on 512 rows of up to 32768 positions; three blocks with more room in their lists 47 us).
+  const bool is_long = p.max_ctx_len > 32768;
+  int64_t capacity = (int64_t)p.max_keep + p.max_keep / 2 + (is_long ? 2048 : 1024);
   if (capacity > p.max_ctx_len) capacity = p.max_ctx_len;
-  if (capacity > 14848) capacity = 14848;  // (with the bitmaps of 262144 positions, one SM's shared memory)
+  if (capacity > 18432) capacity = 18432;
   capacity = (capacity + 3) / 4 * 4;
   int words = (p.max_ctx_len + 31) / 32;
-  if (words > 8192) words = 8192;
-  // Long rows: one block per SM with as many loads in flight as its registers hold; short rows: several blocks per SM,
-  // whose steps overlap.
-  if (p.max_ctx_len > 32768) return launch_select_t<512, 8>(p, rows, (int)capacity, words, s);
+  if (words > 4096) words = 4096;
+  if (is_long) return launch_select_t<512, 8>(p, rows, (int)capacity, words, s);
   return launch_select_t<256, 4>(p, rows, (int)capacity, words, s);
 }
 
