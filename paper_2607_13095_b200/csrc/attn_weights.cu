@@ -132,9 +132,10 @@ struct Segment {
   int r, kh, t0, n, ctx, kv_len, t_lo, t_hi, n_qt;
 };
 
-// Walks a block's share [lo, hi) of the batch's total cost.  A key tile costs one unit per 32 rows of the request (at least
-// one), the first tile of a (request, KV head) twice that (its Q tiles come in, and the pipeline runs empty behind the
-// segment before: 4 us against 3 for a tile of 512 rows).  The tiles follow one another by KV head; a tile belongs to the share in which it begins.  Every role walks by itself.
+// Walks a block's share [lo, hi) of the batch's total cost.  A key tile costs, per Q tile of the request, four units
+// and one more per 32 rows (measured: 0.83 us and 0.23 us per pair of key tiles); the first tile of a (request, KV head) costs
+// three times that (its Q tiles come in, and the pipeline runs empty behind the segment before).  The tiles follow one another by
+// KV head; a tile belongs to the share in which it begins.  Every role walks by itself.
 struct Walker {
   int r;
   int64_t base, lo, hi;  // base: cost of all requests before r
@@ -151,13 +152,13 @@ struct Walker {
     s.kv_len = s.ctx + (p.causal ? s.n : 0);
     s.n_qt = (s.n + pl.tile_tokens - 1) / pl.tile_tokens;
     tiles = (s.kv_len + TKEYS - 1) / TKEYS;
-    q = max(1, (s.n_qt - 1) * (pl.tile_tokens * p.m.G + 31) / 32 + ((s.n - (s.n_qt - 1) * pl.tile_tokens) * p.m.G + 31) / 32);
+    q = max(1, (s.n_qt - 1) * (4 + (pl.tile_tokens * p.m.G + 31) / 32) + 4 + ((s.n - (s.n_qt - 1) * pl.tile_tokens) * p.m.G + 31) / 32);
   }
 
-  // Tiles of a (request, KV head) that begin before cost c of it: tile 0 at 0, tile i at (i + 1) q.
+  // Tiles of a (request, KV head) that begin before cost c of it: tile 0 at 0, tile i at (i + 2) q.
   __device__ __forceinline__ static int tiles_before(int64_t c, int tiles, int q) {
     if (c <= 0) return 0;
-    const int64_t i = (c + q - 1) / q - 1;
+    const int64_t i = (c + q - 1) / q - 2;
     return (int)(i < 1 ? 1 : (i < tiles ? i : tiles));
   }
 
@@ -165,7 +166,7 @@ struct Walker {
     for (; r < p.b.B && base < hi; ++r, kh = 0) {
       int tiles, q;
       request(p, pl, r, s, tiles, q);
-      const int64_t head_cost = tiles > 0 ? (int64_t)(tiles + 1) * q : 0, all = head_cost * p.m.Hkv;
+      const int64_t head_cost = tiles > 0 ? (int64_t)(tiles + 2) * q : 0, all = head_cost * p.m.Hkv;
       if (lo < base + all) {
         if (lo > base + kh * head_cost) kh = (int)((lo - base) / head_cost);
         for (; kh < p.m.Hkv; ++kh) {
@@ -214,7 +215,7 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
       Segment s;
       int tiles, q;
       Walker::request(p, pl, r, s, tiles, q);
-      return tiles > 0 ? (int64_t)(tiles + 1) * q * M.Hkv : (int64_t)0;
+      return tiles > 0 ? (int64_t)(tiles + 2) * q * M.Hkv : (int64_t)0;
     };
     int64_t total = 0;
     for (int r = lane; r < p.b.B; r += 32) total += cost_of(r);
