@@ -283,11 +283,12 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
  *   ascending order; entries from kept to max_keep are set to -1, kept_len[r] = kept.  The first protect_first and the
  *   last protect_last positions rank above all others; equal weights are taken from the lowest position on; NaN ranks
  *   lowest.  ctx_len, keep_len, kept_len: device int32 [B]; weights as above; keep_idx: device int32 [B][Hkv][max_keep].
- *   ctx_len is the length AFTER the step (call it behind hswa_step_advance).  A ctx_len outside [0, max_ctx_len] or a
+ *   ctx_len is the length AFTER the step (call it behind hswa_step_advance); kept_len must be another array
+ *   (HSWA_ERR_INVALID_ARG), and max_ctx_len at most 2^30 (HSWA_ERR_UNSUPPORTED).  A ctx_len outside [0, max_ctx_len] or a
  *   keep_len outside [0, max_keep] is recorded as HSWA_ERR_BOUNDS (index -1 / -2) and clamped.
  *
  * hswa_evict_compact: copies K and V of position keep_idx[r][kh][i], i < kept_len[r], to position i behind
- *   dst_block_table (device int32 [B][dst_max_blocks], pages of the same pool), and its weight (weights and weights_out
+ *   dst_block_table (device int32 [B][dst_max_blocks], another array, pages of the same pool), and its weight (weights and weights_out
  *   both given or both NULL; different arrays) to weights_out[r][kh][i].  Nothing else is written.  The caller guarantees
  *   that the destination pages are pages of no block table in use, this batch's included: source pages, which other
  *   requests may share, are only read.  Afterwards dst_block_table and kept_len take the place of block_table and ctx_len

@@ -772,7 +772,6 @@ hswa_status hswa_attn_weights(hswa_handle* h, const hswa_layer* layer, const hsw
   if ((int64_t)b->max_ctx_len > (int64_t)b->max_blocks * h->cfg.page_size || b->max_ctx_len > weights_stride) return HSWA_ERR_INVALID_ARG;
   if (b->max_ctx_len == 0 && (!causal || b->max_q_len == 0)) return HSWA_OK;
   if (!weights || (b->total_q > 0 && (!q || !lse || !aligned16(q)))) return HSWA_ERR_INVALID_ARG;
-  if (b->batch > 65535 || h->cfg.num_kv_heads > 65535) return HSWA_ERR_UNSUPPORTED;
   if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
   WeightsParams p = {};
   p.m = model_params(h);
@@ -805,6 +804,8 @@ hswa_status hswa_evict_select(hswa_handle* h, int32_t batch, const int32_t* ctx_
     return HSWA_ERR_INVALID_ARG;
   if (batch == 0) return HSWA_OK;
   if (!ctx_len || !keep_len || !kept_len || (max_keep > 0 && !keep_idx) || (max_ctx_len > 0 && !weights)) return HSWA_ERR_INVALID_ARG;
+  if (kept_len == ctx_len) return HSWA_ERR_INVALID_ARG;  // the heads of a request read its length while one of them writes it
+  if (max_ctx_len > (1 << 30)) return HSWA_ERR_UNSUPPORTED;
   if ((int64_t)batch * h->cfg.num_kv_heads > INT32_MAX) return HSWA_ERR_UNSUPPORTED;
   if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
   SelectParams p = {};
@@ -833,7 +834,7 @@ hswa_status hswa_evict_compact(hswa_handle* h, const hswa_layer* layer, const hs
   if (st != HSWA_OK) return st;
   if (max_keep < 0 || dst_max_blocks < 0) return HSWA_ERR_INVALID_ARG;
   if (b->batch == 0 || max_keep == 0) return HSWA_OK;
-  if (layer->is_swa || !keep_idx || !kept_len || !dst_block_table) return HSWA_ERR_INVALID_ARG;
+  if (layer->is_swa || !keep_idx || !kept_len || !dst_block_table || dst_block_table == b->block_table) return HSWA_ERR_INVALID_ARG;
   if ((int64_t)max_keep > (int64_t)dst_max_blocks * h->cfg.page_size) return HSWA_ERR_INVALID_ARG;
   if ((int64_t)b->max_ctx_len > (int64_t)b->max_blocks * h->cfg.page_size) return HSWA_ERR_INVALID_ARG;
   if ((weights == nullptr) != (weights_out == nullptr)) return HSWA_ERR_INVALID_ARG;

@@ -126,6 +126,30 @@ def test_cross_few_requests(d, ctx, n):
         check_cross(c, *run_cross(c, single=False))
 
 
+@pytest.mark.parametrize("d", [dims(8, 128, 64, 4), dims(3, 128, 16, 2), dims(6, 64, 32)], ids=str)
+def test_cross_many_requests(d):
+    rng = np.random.default_rng(40)
+    B = 60
+    c = Case(d, np.where(rng.random(B) < 0.2, 0, rng.integers(1, 900, B)), rng.integers(0, 40, B), seed=41)
+    check_cross(c, *run_cross(c))
+    c = Case(d, np.where(rng.random(B) < 0.2, 0, rng.integers(1, 900, B)), np.ones(B, np.int32), seed=42)
+    check_cross(c, *run_cross(c))
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(4, 64, 16, 1)], ids=str)
+@pytest.mark.parametrize("n", [1, 3, 70])
+def test_cross_shows_a_nan_among_its_inputs(d, n):
+    """A NaN in a cached state shows in the rows of its KV head and nowhere else."""
+    c = Case(d, [300, 200], [n, n], seed=43)
+    kh = d.num_kv_heads - 1
+    c.pool[c.table[0, 100 // d.page_size], 0, kh, 100 % d.page_size, 5] = NAN_BITS
+    out, lse = run_cross(c)
+    hit = slice(kh * d.group, (kh + 1) * d.group)
+    assert np.isnan(out[:n, hit]).all() and np.isnan(lse[:n, hit]).all()
+    out[:n, hit] = lse[:n, hit] = 0
+    assert np.isfinite(out).all() and np.isfinite(lse).all()
+
+
 def test_cross_bounds_wider_than_the_batch():
     d = dims(8, 128, 64)
     c = Case(d, [100, 0, 700], [5, 2, 0], seed=4, spare_blocks=40)
@@ -193,6 +217,24 @@ def test_weights_long(causal, ctx, n):
     got = run_weights(c, 1.0, lse, old)
     check_weights(c, 1.0, lse, old.copy(), got)
     assert np.array_equal(got, run_weights(c, 1.0, lse, old)), "repeated calls differ"
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64, 8), dims(5, 64, 16, 3), dims(7, 128, 32, 8)], ids=str)
+@pytest.mark.parametrize("kind", ["single", "few", "many", "mixed"])
+@pytest.mark.parametrize("causal", [False, True])
+def test_weights_many_requests(d, kind, causal):
+    """More (request, KV head) pairs than blocks: a block's share crosses requests, with and without rows, whose Q tiles fit
+    shared memory or are streamed."""
+    rng = np.random.default_rng(70)
+    B = 50
+    n = {"single": np.ones(B), "few": rng.integers(0, 9, B), "many": rng.integers(0, 70, B),
+         "mixed": np.where(rng.random(B) < 0.3, 0, np.where(rng.random(B) < 0.1, rng.integers(90, 200, B), rng.integers(1, 30, B)))}[kind]
+    ctx = np.where(rng.random(B) < 0.2, rng.integers(0, 3, B), rng.integers(1, 700, B))
+    c = Case(d, ctx, n.astype(np.int32), seed=71, causal=causal)
+    lse, old = weights_inputs(c, 72)
+    got = run_weights(c, 0.5, lse, old)
+    check_weights(c, 0.5, lse, old.copy(), got)
+    assert np.array_equal(got, run_weights(c, 0.5, lse, old)), "repeated calls differ"
 
 
 def test_weights_of_a_causal_step_add_up_to_its_rows():
@@ -522,6 +564,8 @@ def test_refusals():
     refused(INV, hb.hswa_evict_select, h, 2, ctx, 9003, w, keep, idx, kept)
     refused(INV, hb.hswa_evict_select, h, 2, ctx, 9000, w, keep, idx, kept, protect_first=-1)
     refused(INV, hb.hswa_evict_select, h, 2, ctx, 9000, w, keep, idx, kept, protect_last=-1)
+    refused(INV, hb.hswa_evict_select, h, 2, ctx, 9000, w, keep, idx, ctx)
+    refused(INV, hb.hswa_evict_compact, h, layer, b, idx, kept, b.block_table)
     refused(INV, hb.hswa_evict_compact, h, swa, b, idx, kept, dev_i32([[0], [1]]))
     refused(INV, hb.hswa_evict_compact, h, layer, b, idx, kept, dev_i32(np.zeros((2, 0))))
     refused(INV, hb.hswa_evict_compact, h, layer, b, idx, kept, dev_i32([[0], [1]]), w, None)
