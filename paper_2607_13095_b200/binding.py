@@ -150,12 +150,12 @@ def _ptr(t: Optional[torch.Tensor]):
     if t is None:
         return None
     assert t.is_cuda and t.is_contiguous(), "device tensors must be contiguous CUDA tensors"
-    return C.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _stream():
     # (the stream's handle without the Stream object around it: 0.2 us a call instead of 3.4 us)
-    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _check(status: int, what: str):
@@ -325,36 +325,37 @@ def hswa_cross_attn(h: Handle, layer: Layer, batch: Batch, q, out, lse=None, wor
 def hswa_attn_weights(h: Handle, layer: Layer, batch: Batch, causal: bool, q, lse, decay: float, weights: torch.Tensor):
     """weights: fp32 CUDA tensor [B][Hkv][stride], updated in place with the attention weights of q's rows (lse: theirs)."""
     assert q.dtype == torch.bfloat16 and lse.dtype == torch.float32
-    assert weights.dtype == torch.float32 and weights.dim() == 3 and tuple(weights.shape[:2]) == (batch.batch, h.cfg.num_kv_heads)
-    _check(load().hswa_attn_weights(h.ptr, C.byref(layer.c), C.byref(batch.c), int(bool(causal)), _ptr(q), _ptr(lse), float(decay),
-                                    _ptr(weights), int(weights.shape[2]), _stream()), "hswa_attn_weights")
+    B, heads, stride = weights.shape
+    assert weights.dtype == torch.float32 and B == batch.batch and heads == h.cfg.num_kv_heads
+    _check(load().hswa_attn_weights(h.ptr, C.byref(layer.c), C.byref(batch.c), bool(causal), _ptr(q), _ptr(lse), decay, _ptr(weights),
+                                    stride, _stream()), "hswa_attn_weights")
 
 
 def hswa_evict_select(h: Handle, batch: int, ctx_len: torch.Tensor, max_ctx_len: int, weights: torch.Tensor, keep_len: torch.Tensor,
                       keep_idx: torch.Tensor, kept_len: torch.Tensor, *, protect_first: int = 0, protect_last: int = 0):
     """keep_idx: int32 CUDA tensor [B][Hkv][max_keep], filled with the positions of largest weight, ascending, then -1."""
-    for t in (ctx_len, keep_len, keep_idx, kept_len):
-        assert t.dtype == torch.int32
-    assert weights.dtype == torch.float32 and weights.dim() == 3 and tuple(weights.shape[:2]) == (batch, h.cfg.num_kv_heads)
-    assert keep_idx.dim() == 3 and tuple(keep_idx.shape[:2]) == (batch, h.cfg.num_kv_heads)
-    _check(load().hswa_evict_select(h.ptr, batch, _ptr(ctx_len), int(max_ctx_len), _ptr(weights), int(weights.shape[2]),
-                                    _ptr(keep_len), int(keep_idx.shape[2]), int(protect_first), int(protect_last), _ptr(keep_idx),
-                                    _ptr(kept_len), _stream()), "hswa_evict_select")
+    i32, heads = torch.int32, h.cfg.num_kv_heads
+    assert ctx_len.dtype == i32 and keep_len.dtype == i32 and keep_idx.dtype == i32 and kept_len.dtype == i32
+    w_batch, w_heads, stride = weights.shape
+    k_batch, k_heads, max_keep = keep_idx.shape
+    assert weights.dtype == torch.float32 and w_batch == k_batch == batch and w_heads == k_heads == heads
+    _check(load().hswa_evict_select(h.ptr, batch, _ptr(ctx_len), max_ctx_len, _ptr(weights), stride, _ptr(keep_len), max_keep,
+                                    protect_first, protect_last, _ptr(keep_idx), _ptr(kept_len), _stream()), "hswa_evict_select")
 
 
 def hswa_evict_compact(h: Handle, layer: Layer, batch: Batch, keep_idx: torch.Tensor, kept_len: torch.Tensor,
                        dst_block_table: torch.Tensor, weights: Optional[torch.Tensor] = None,
                        weights_out: Optional[torch.Tensor] = None):
     """Copies the kept K/V rows (and weights) of batch's block table to the pages of dst_block_table [B][blocks]."""
-    for t in (keep_idx, kept_len, dst_block_table):
-        assert t.dtype == torch.int32
-    assert keep_idx.dim() == 3 and dst_block_table.dim() == 2
-    for t in (weights, weights_out):
-        assert t is None or (t.dtype == torch.float32 and t.dim() == 3)
-    _check(load().hswa_evict_compact(h.ptr, C.byref(layer.c), C.byref(batch.c), _ptr(keep_idx), _ptr(kept_len),
-                                     int(keep_idx.shape[2]), _ptr(dst_block_table), int(dst_block_table.shape[1]), _ptr(weights),
-                                     0 if weights is None else int(weights.shape[2]), _ptr(weights_out),
-                                     0 if weights_out is None else int(weights_out.shape[2]), _stream()), "hswa_evict_compact")
+    i32, f32 = torch.int32, torch.float32
+    assert keep_idx.dtype == i32 and kept_len.dtype == i32 and dst_block_table.dtype == i32
+    assert (weights is None or weights.dtype == f32) and (weights_out is None or weights_out.dtype == f32)
+    _, _, max_keep = keep_idx.shape
+    _, dst_blocks = dst_block_table.shape
+    _check(load().hswa_evict_compact(h.ptr, C.byref(layer.c), C.byref(batch.c), _ptr(keep_idx), _ptr(kept_len), max_keep,
+                                     _ptr(dst_block_table), dst_blocks, _ptr(weights), 0 if weights is None else weights.shape[2],
+                                     _ptr(weights_out), 0 if weights_out is None else weights_out.shape[2], _stream()),
+           "hswa_evict_compact")
 
 
 def hswa_window_safe_len(match_len: int, window: int, swa_valid) -> int:

@@ -8,6 +8,9 @@
 namespace {
 
 constexpr int kMinSplitLen = 256;
+// Cross attention of single tokens: up to this many states are one block's.  Two requests of up to 512 states: 8.9 us by one
+// launch; in two splits 7.7 us on the device, but 10.5 us of the host's time for two launches.
+constexpr int kUnsplitLen = 512;
 constexpr int kMaxSplitLen = 4096;  // measured on configs 2, 4 and 5: 4096-8192 beat 2048 (fewer block prologues) and 16384 (tail)
 
 ModelParams model_params(const hswa_handle* h) {
@@ -149,6 +152,11 @@ bool plan_cross(const hswa_handle* h, int batch, int total_q, int max_q_len, int
   c.decode = max_q_len == 1 && total_q == batch;
   if (c.decode) {
     if (!plan_decode(h, 0, batch, max_ctx_len > 0 ? max_ctx_len - 1 : 0, 0, 1, &c.dec)) return false;
+    if (max_ctx_len <= kUnsplitLen) {  // a second launch costs more than the few tiles that it would spare a block
+      c.dec.split_len = kUnsplitLen;
+      c.dec.grid_splits = c.dec.max_splits = 1;
+      c.dec.o_bytes = c.dec.ml_bytes = 0;
+    }
     c.o_bytes = c.dec.o_bytes;
     c.ml_bytes = c.dec.ml_bytes;
   } else {
