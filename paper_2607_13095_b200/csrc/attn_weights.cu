@@ -6,9 +6,11 @@
 // writes one number; nothing is exchanged between threads, no atomics, and the order of the sums is fixed.  Each key is
 // read from memory once.
 //
-// Bounds.  One row group (a decode step) is bound by reading K.  With many rows the exponentials bound it: 16 per clock
-// and SM from the special-function units against 32 score elements per clock from the tensor core at D = 128.  The
-// exponentials of the many-row form are therefore shared between the special-function unit and the FMA pipes.
+// Bounds.  One row group (a decode step) is bound by reading K: 64 requests of 4096 to 32768 keys, 8 KV heads of 128: 423 us =
+// 6.5 TB/s, 1.01 of a plain copy's rate.  With many rows the sums bound it (an observation window of 33 to 64 tokens on 8
+// prompts of up to 16384: 73 us, where the tensor core has 26 us of work and the special-function units, at 16 exponentials
+// per clock and SM, 37 us): the rest is the instructions around them.  Taking a share of the exponentials on the FMA pipes by
+// a polynomial was no faster (1, 2, 3 of 8: 78 us; 4 of 8: 83 us).
 //
 // Warp roles: warps 0-3 and 4-7 sum the even and the odd key tiles of a segment, warp 8 loads (TMA) and stages the rows'
 // log-sum-exps, warp 9 issues the MMAs.  Each of the two summing groups has two TMEM accumulators.
@@ -25,14 +27,13 @@ using namespace hswa_dev;
 
 constexpr int TKEYS = 128;       // keys per tile
 // Summing warps per group: four cover the 128 keys of a tile.  The many-row form has twice as many, each with half of the
-// columns: two warps per scheduler leave the pipes idle most of the time behind TMEM reads and dependent steps (100 us on
-// the 64-token observation window of 8 prompts, 78 us with four).
+// columns: two warps per scheduler leave the pipes idle too long behind TMEM reads and dependent steps (86 us on an observation
+// window of up to 64 tokens of 8 prompts of up to 16384, 78 us with four).
 constexpr int group_warps(bool wide) { return wide ? 8 : 4; }
 constexpr int block_threads(bool wide) { return (2 * group_warps(wide) + 2) * 32; }
 constexpr int MAX_NSQ = 4, MAX_NSK = 6;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float NO_ROW = -1e30f;  // in the place of an absent row's value, or of a row's that saw nothing: 2^that = 0
-constexpr int FMA_SHARE = 3;     // of eight exponentials of the many-row form, those taken on the FMA pipes
 
 // Barriers
 enum { B_QFULL = 0, B_LFULL = B_QFULL + MAX_NSQ, B_QEMPTY = B_LFULL + MAX_NSQ, B_KFULL = B_QEMPTY + MAX_NSQ,
@@ -57,53 +58,26 @@ __device__ __forceinline__ int weights_request_error(const WeightsParams& p, int
 // A warp's bounded wait: one answer for all lanes.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)); }
 
-// 2^x for a pair of columns, added to acc, on the FMA and integer pipes instead of the special-function unit: x = n + f with
-// n the nearest integer (found by adding 1.5 * 2^23, which leaves n in the low mantissa bits; + 127 makes them the exponent
-// field of 2^n), 2^f by a polynomial of degree 5 that is minimax in the relative error on [-1/2, 1/2] (Remez exchange;
-// 2.1e-7 at most with its coefficients and steps in fp32), and the product with 2^n is the fma that adds it to the sum.
-// Finite x down to any size (2^n is 0 from -127 on), up to 127: a probability's x is at most 0 but for rounding.
-__device__ __forceinline__ float2 add_exp2_fma(float2 x, float2 acc) {
-  const float2 magic = make_float2(12583039.f, 12583039.f), neg_magic = make_float2(-12583039.f, -12583039.f);
-  const float2 t = __fadd2_rn(x, magic);
-  const float2 n = __fadd2_rn(t, neg_magic);
-  const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
-  float2 q = make_float2(0.0013276467798277736f, 0.0013276467798277736f);
-  q = __ffma2_rn(q, f, make_float2(0.009675540961325169f, 0.009675540961325169f));
-  q = __ffma2_rn(q, f, make_float2(0.05550713464617729f, 0.05550713464617729f));
-  q = __ffma2_rn(q, f, make_float2(0.24022120237350464f, 0.24022120237350464f));
-  q = __ffma2_rn(q, f, make_float2(0.6931469440460205f, 0.6931469440460205f));
-  q = __ffma2_rn(q, f, make_float2(1.0000001192092896f, 1.0000001192092896f));
-  const int low = 0x4b400000;  // the bits of 1.5 * 2^23: an exponent field of 0
-  const float2 scale = make_float2(__int_as_float(max(__float_as_int(t.x), low) << 23), __int_as_float(max(__float_as_int(t.y), low) << 23));
-  return __ffma2_rn(q, scale, acc);
-}
-
-// One thread's sum over CHUNK score columns.  nl: minus the rows' log-sum-exps in log2 units; a column that does not count
-// (an absent row) has NO_ROW there and a finite score.  MASKED: columns outside [c_lo, c_hi) are dropped whatever
-// their score is.  FMA_OF_8: of every eight column pairs, how many take their exponential on the FMA pipes.
-template <int CHUNK, bool MASKED, int FMA_OF_8>
-__device__ __forceinline__ void sum_chunk(const uint32_t (&v)[CHUNK], const float* nl, float scale_log2, int c0, int c_lo, int c_hi,
+// One thread's sum over 16 score columns.  nl: minus the rows' log-sum-exps in log2 units; a column that does not count (an
+// absent row) has NO_ROW there and a finite score.  MASKED: columns outside [c_lo, c_hi) are dropped whatever their score is.
+template <bool MASKED>
+__device__ __forceinline__ void sum_chunk(const uint32_t (&v)[16], const float* nl, float scale_log2, int c0, int c_lo, int c_hi,
                                           float2 (&acc)[4]) {
   const float2 sc2 = make_float2(scale_log2, scale_log2);
 #pragma unroll
-  for (int k = 0; k < CHUNK; k += 4) {
+  for (int k = 0; k < 16; k += 4) {
     const float4 l4 = *reinterpret_cast<const float4*>(nl + k);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int c = k + 2 * h, pair = c >> 1;
+      const int c = k + 2 * h;
       const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2,
                                   h ? make_float2(l4.z, l4.w) : make_float2(l4.x, l4.y));
-      float2& a = acc[pair & 3];
-      if (!MASKED && ((pair & 7) * FMA_OF_8) % 8 + FMA_OF_8 > 7) {  // spread evenly
-        a = add_exp2_fma(x, a);
-      } else {
-        float2 e = make_float2(fast_exp2(x.x), fast_exp2(x.y));
-        if constexpr (MASKED) {
-          e.x = c0 + c >= c_lo && c0 + c < c_hi ? e.x : 0.f;
-          e.y = c0 + c + 1 >= c_lo && c0 + c + 1 < c_hi ? e.y : 0.f;
-        }
-        a = __fadd2_rn(a, e);
+      float2 e = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+      if constexpr (MASKED) {
+        e.x = c0 + c >= c_lo && c0 + c < c_hi ? e.x : 0.f;
+        e.y = c0 + c + 1 >= c_lo && c0 + c + 1 < c_hi ? e.y : 0.f;
       }
+      acc[(c >> 1) & 3] = __fadd2_rn(acc[(c >> 1) & 3], e);
     }
   }
 }
@@ -516,15 +490,15 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
               tmem_ld16(ts + c_begin, va);
               tc_wait_ld();
               tmem_ld16(ts + c_begin + 16, vb);
-              sum_chunk<16, false, FMA_SHARE>(va, nl + c_begin, M.scale_log2, 0, 0, 0, acc);
+              sum_chunk<false>(va, nl + c_begin, M.scale_log2, 0, 0, 0, acc);
               tc_wait_ld();
               tmem_ld16(ts + c_begin + 32, va);
-              sum_chunk<16, false, FMA_SHARE>(vb, nl + c_begin + 16, M.scale_log2, 0, 0, 0, acc);
+              sum_chunk<false>(vb, nl + c_begin + 16, M.scale_log2, 0, 0, 0, acc);
               tc_wait_ld();
               tmem_ld16(ts + c_begin + 48, vb);
-              sum_chunk<16, false, FMA_SHARE>(va, nl + c_begin + 32, M.scale_log2, 0, 0, 0, acc);
+              sum_chunk<false>(va, nl + c_begin + 32, M.scale_log2, 0, 0, 0, acc);
               tc_wait_ld();
-              sum_chunk<16, false, FMA_SHARE>(vb, nl + c_begin + 48, M.scale_log2, 0, 0, 0, acc);
+              sum_chunk<false>(vb, nl + c_begin + 48, M.scale_log2, 0, 0, 0, acc);
             } else {
 #pragma unroll 1
               for (int c0 = max(warp_lo & ~15, c_begin); c0 < c_end; c0 += 16) {
@@ -532,9 +506,9 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
                 tmem_ld16(ts + c0, v);
                 tc_wait_ld();
                 if (c0 >= warp_hi && c0 + 16 <= full_cols)
-                  sum_chunk<16, false, 0>(v, nl + c0, M.scale_log2, 0, 0, 0, acc);
+                  sum_chunk<false>(v, nl + c0, M.scale_log2, 0, 0, 0, acc);
                 else
-                  sum_chunk<16, true, 0>(v, nl + c0, M.scale_log2, c0, c_lo, cols, acc);
+                  sum_chunk<true>(v, nl + c0, M.scale_log2, c0, c_lo, cols, acc);
               }
             }
             const float2 a = __fadd2_rn(__fadd2_rn(acc[0], acc[1]), __fadd2_rn(acc[2], acc[3]));
