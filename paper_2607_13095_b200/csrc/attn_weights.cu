@@ -12,8 +12,8 @@
 // per clock and SM, 37 us): the rest is the instructions around them.  Taking a share of the exponentials on the FMA pipes by
 // a polynomial was no faster (1, 2, 3 of 8: 78 us; 4 of 8: 83 us).
 //
-// Warp roles: warps 0-3 and 4-7 sum the even and the odd key tiles of a segment, warp 8 loads (TMA) and stages the rows'
-// log-sum-exps, warp 9 issues the MMAs.  Each of the two summing groups has two TMEM accumulators.
+// Warp roles: two groups of summing warps (four or eight each) take the even and the odd key tiles of a segment, one warp
+// loads (TMA) and stages the rows' log-sum-exps, one issues the MMAs.  Each group has two TMEM accumulators.
 //
 // Blocks are persistent: all key tiles of the batch, weighted with the Q tiles they meet, are cut into equal shares, and a
 // block walks the segments (request, KV head, range of key tiles) of its share with every pipeline running on across
@@ -31,7 +31,7 @@ constexpr int TKEYS = 128;       // keys per tile
 // window of up to 64 tokens of 8 prompts of up to 16384, 78 us with four).
 constexpr int group_warps(bool wide) { return wide ? 8 : 4; }
 constexpr int block_threads(bool wide) { return (2 * group_warps(wide) + 2) * 32; }
-constexpr int MAX_NSQ = 4, MAX_NSK = 6;
+constexpr int MAX_NSQ = 8, MAX_NSK = 6;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float NO_ROW = -1e30f;  // in the place of an absent row's value, or of a row's that saw nothing: 2^that = 0
 
@@ -280,6 +280,13 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
     // ======================= loader =======================
     const int ppt = TKEYS / M.P;
     bool ok = true;
+    int row_tok[4], row_at[4];  // of the lane's four rows of a Q tile: the token in the tile, the place of its log-sum-exp
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int col = u * 32 + lane;
+      row_tok[u] = col < q_rows ? col / M.G : INT32_MAX;
+      row_at[u] = col / M.G * M.Hq + col % M.G;
+    }
     Ring kr, qr;
     bool k_used = false, q_used = false;  // the ring has been filled once: its slots have to be released first
     while (ok && walk.next(p, pl, sg)) {
@@ -320,16 +327,30 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
         k_used |= kr.slot == 0;
       };
       // lane's four rows of Q tile qt: minus their log-sum-exps in log2 units
-      float x[4];
-      auto fetch_lse = [&](int qt) {
+      auto fetch_lse = [&](int qt, float(&x)[4]) {
+        const float* lse = p.lse + (int64_t)(sg.t0 + qt * pl.tile_tokens) * M.Hq + sg.kh * M.G;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const int col = u * 32 + lane, tok = qt * pl.tile_tokens + col / M.G;
-          const float v = col < q_rows && tok < sg.n ? p.lse[(int64_t)(sg.t0 + tok) * M.Hq + sg.kh * M.G + col % M.G] : -INFINITY;
+          const float v = row_tok[u] < sg.n - qt * pl.tile_tokens ? lse[row_at[u]] : -INFINITY;
           x[u] = v == -INFINITY ? NO_ROW : -v * LOG2E;
         }
       };
-      auto load_q = [&](int qt, int next_qt) {
+      // The values of the next three Q tiles are on their way while one is staged (reading them one by one costs a memory
+      // latency per Q tile).  fq: the next one to read, in the order in which the tiles are loaded.
+      const int lo = first_qt(sg.t_lo);
+      const bool resident = sg.n_qt - lo <= pl.nsq;
+      float x[3][4];
+      int fq = lo, ft = sg.t_lo;
+      auto fetch_next = [&](float(&y)[4]) {
+        if (fq < 0) return;
+        fetch_lse(fq, y);
+        if (++fq < sg.n_qt) return;
+        ft += 2;
+        fq = resident || ft >= sg.t_hi ? -1 : first_qt(ft);
+      };
+#pragma unroll
+      for (int d = 0; d < 3; ++d) fetch_next(x[d]);
+      auto load_q = [&](int qt) {
         const int stage = qr.slot;
         if (q_used && !warp_wait(bar(B_QEMPTY + stage), qr.phase ^ 1u)) {
           if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, sg.r, qt, 91);
@@ -344,28 +365,31 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-          if (u * 32 + lane < N) s_nl[stage * N + u * 32 + lane] = x[u];
+          if (u * 32 + lane < N) s_nl[stage * N + u * 32 + lane] = x[0][u];
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(B_LFULL + stage));
-        if (next_qt < sg.n_qt) fetch_lse(next_qt);  // under way while other things are loaded
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          x[0][u] = x[1][u];
+          x[1][u] = x[2][u];
+        }
+        fetch_next(x[2]);
         qr.step(pl.nsq);
         q_used |= qr.slot == 0;
       };
-      const int lo = first_qt(sg.t_lo);
-      fetch_lse(lo);
       load_k(sg.t_lo);
-      if (sg.n_qt - lo <= pl.nsq) {
+      if (resident) {
         for (int qt = lo; qt < sg.n_qt && ok; ++qt) {
-          load_q(qt, qt + 1);
+          load_q(qt);
           if (qt == lo) load_k(sg.t_lo + 1);
         }
         for (int t = sg.t_lo + 2; t < sg.t_hi && ok; ++t) load_k(t);
       } else {
         load_k(sg.t_lo + 1);
         for (int t = sg.t_lo; t < sg.t_hi && ok; t += 2) {
-          const int first = first_qt(t), then = t + 2 < sg.t_hi ? first_qt(t + 2) : sg.n_qt;
+          const int first = first_qt(t);
           for (int qt = first; qt < sg.n_qt && ok; ++qt) {
-            load_q(qt, qt + 1 < sg.n_qt ? qt + 1 : then);
+            load_q(qt);
             if (qt == first) {  // the next pair of key tiles, behind this pair's first Q tile
               load_k(t + 2);
               load_k(t + 3);
@@ -597,10 +621,14 @@ cudaError_t hswa_launch_attn_weights(const CUtensorMap& tm_pool, const CUtensorM
   const bool wide = pl.n_cols > 64;
   const int tile_kb = p.m.D / 4;  // a tile of 128 rows
   if (wide) {
-    // 224 KB of tiles, one block per SM: a Q stage more than a request has Q tiles (the next segment's first one) up to
-    // four, three when they are streamed; K takes the rest
-    pl.nsq = max_qt < MAX_NSQ ? max_qt + 1 : (max_qt == MAX_NSQ ? MAX_NSQ : 3);
-    pl.nsk = (224 - pl.nsq * tile_kb) / tile_kb;
+    // One block per SM, as many tiles as its shared memory holds: a Q stage more than a request has Q tiles (the next segment's first one) as long as
+    // three K stages are left; where Q tiles are streamed, four K stages (the next pair's are loaded while this one is
+    // multiplied) and the rest for Q
+    const int stages = p.m.D == 128 ? 7 : 13;
+    pl.nsq = max_qt + 1 < MAX_NSQ ? max_qt + 1 : MAX_NSQ;
+    if (pl.nsq > stages - 3) pl.nsq = stages - 3;
+    if (max_qt > pl.nsq && pl.nsq > stages - 4) pl.nsq = stages - 4;
+    pl.nsk = stages - pl.nsq;
   } else {
     // two blocks per SM with 96 KB of K tiles each, beside one or two Q tiles of at most 16 KB
     pl.nsq = pl.n_cols == 64 && p.m.D == 128 ? 1 : 2;
