@@ -161,8 +161,9 @@ bool plan_cross(const hswa_handle* h, int batch, int total_q, int max_q_len, int
     c.ml_bytes = c.dec.ml_bytes;
   } else {
     const ModelParams m = model_params(h);
-    c.tc = hswa_cross_tc_supported(m) && batch <= 65535 && h->cfg.num_kv_heads <= 65535;
+    c.tc = hswa_cross_tc_supported(m);
     if (c.tc) {
+      if (batch > 65535 || h->cfg.num_kv_heads > 65535) return false;  // grid extents
       const int tokens = 2 * hswa_cross_tc_tile_tokens(m);
       c.row_tiles = (max_q_len + tokens - 1) / tokens;
     } else {

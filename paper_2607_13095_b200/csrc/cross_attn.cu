@@ -2,8 +2,8 @@
 // paged storage): softmax(scale q K^T) V over all len_r cached positions of the request, no causal mask, any number of
 // query tokens per request; a request without states gives zeros and a log-sum-exp of minus infinity.
 //
-// General tile kernel on warp-level tensor-core MMA, for every supported shape.  No mask depends on the query, so the
-// (token, head) rows of a GQA group are interchangeable: a block takes 64 packed rows of one (request, KV head) -- 8
+// Tile kernel on warp-level tensor-core MMA for head_dim 64 (head_dim 128 takes the tcgen05 tile kernel, single tokens the
+// streaming decode kernel).  No mask depends on the query, so the (token, head) rows of a GQA group are interchangeable: a block takes 64 packed rows of one (request, KV head) -- 8
 // tokens at a group of 8 -- and the whole group shares each K/V tile.  Few rows against many keys do not fill the
 // machine by themselves: the keys are then cut into slices whose (m, l, o) partials a second kernel joins.
 #include "hswa_internal.cuh"
@@ -302,7 +302,6 @@ cudaError_t launch_mma_t(const CrossParams& p, cudaStream_t s) {
 int hswa_cross_mma_rows() { return BM; }
 
 cudaError_t hswa_launch_cross_mma(const CrossParams& p, cudaStream_t s) {
-  if (p.m.D == 128) return launch_mma_t<128>(p, s);
   if (p.m.D == 64) return launch_mma_t<64>(p, s);
   return cudaErrorInvalidValue;
 }
