@@ -141,7 +141,7 @@ bool plan_decode(const hswa_handle* h, int is_swa, int batch, int max_ctx_len, i
 // Cross attention: how one call is laid out, from host-known values only.  One token per request streams the cache like a
 // decode step; anything else goes to the tile kernel, whose key slices fill the machine when the rows alone do not.
 struct CrossPlan {
-  bool decode, tc;
+  bool decode;
   DecodePlan dec;
   int row_tiles, slices, slice_len;
   size_t o_bytes, ml_bytes;
@@ -160,18 +160,11 @@ bool plan_cross(const hswa_handle* h, int batch, int total_q, int max_q_len, int
     c.o_bytes = c.dec.o_bytes;
     c.ml_bytes = c.dec.ml_bytes;
   } else {
-    const ModelParams m = model_params(h);
-    c.tc = hswa_cross_tc_supported(m);
-    if (c.tc) {
-      if (batch > 65535 || h->cfg.num_kv_heads > 65535) return false;  // grid extents
-      const int tokens = 2 * hswa_cross_tc_tile_tokens(m);
-      c.row_tiles = (max_q_len + tokens - 1) / tokens;
-    } else {
-      const int64_t rows = (int64_t)max_q_len * h->group;
-      c.row_tiles = (int)((rows + hswa_cross_mma_rows() - 1) / hswa_cross_mma_rows());
-    }
+    if (batch > 65535 || h->cfg.num_kv_heads > 65535) return false;  // grid extents
+    const int tokens = 2 * hswa_cross_tile_tokens(model_params(h));
+    c.row_tiles = (max_q_len + tokens - 1) / tokens;
     const int64_t blocks = (int64_t)c.row_tiles * h->cfg.num_kv_heads * batch;
-    const int64_t want = ((c.tc ? 1LL : 4LL) * h->num_sms + blocks - 1) / blocks, most = (max_ctx_len + 511) / 512;
+    const int64_t want = (h->num_sms + blocks - 1) / blocks, most = (max_ctx_len + 511) / 512;  // one wave of blocks
     int64_t slices = want < most ? want : most;
     if (slices < 1) slices = 1;
     c.slice_len = (int)((((int64_t)max_ctx_len + slices - 1) / slices + 127) / 128 * 128);
@@ -725,48 +718,30 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
     if (p.max_splits > 1 && hswa_launch_combine(p, true, s) != cudaSuccess) return HSWA_ERR_CUDA;
     return HSWA_OK;
   }
-  CrossParams p = {};  // (the join of the slices takes it on both paths)
-  p.m = model_params(h);
-  p.b = batch_params(b);
-  p.pool = static_cast<const __nv_bfloat16*>(layer->pool);
-  p.num_pages = layer->num_pages;
-  p.q = static_cast<const __nv_bfloat16*>(q);
-  p.out = out;
-  p.lse = lse;
-  p.total_q = b->total_q;
-  p.max_q_len = b->max_q_len;
-  p.max_ctx_len = b->max_ctx_len;
-  p.row_tiles = pl.row_tiles;
-  p.slices = pl.slices;
-  p.slice_len = pl.slice_len;
-  p.part_o = part_o;
-  p.part_ml = part_ml;
-  p.err = h->err;
-  if (pl.tc) {
-    PrefillParams t = {};
-    t.m = p.m;
-    t.b = p.b;
-    t.pool = static_cast<__nv_bfloat16*>(layer->pool);
-    t.num_pages = p.num_pages;
-    t.q = p.q;
-    t.out = out;
-    t.lse = lse;
-    t.total_q = p.total_q;
-    t.max_q_len = p.max_q_len;
-    t.max_ctx_len = p.max_ctx_len;
-    t.prefix_tiles_per_split = pl.slice_len / 128;
-    t.max_splits = pl.slices;
-    t.part_o = part_o;
-    t.part_ml = part_ml;
-    t.err = h->err;
-    CUtensorMap tm, tm_q;
-    if ((st = make_pool_map(h, layer, &tm)) != HSWA_OK) return st;
-    if ((st = make_rows_map(h, q, h->cfg.num_q_heads, b->total_q, hswa_cross_tc_tile_tokens(p.m), &tm_q, h->group)) != HSWA_OK) return st;
-    if (hswa_launch_cross_tc(tm, tm_q, t, pl.row_tiles, s) != cudaSuccess) return HSWA_ERR_CUDA;
-  } else if (hswa_launch_cross_mma(p, s) != cudaSuccess) {
-    return HSWA_ERR_CUDA;
+  PrefillParams t = {};
+  t.m = model_params(h);
+  t.b = batch_params(b);
+  t.pool = static_cast<__nv_bfloat16*>(layer->pool);
+  t.num_pages = layer->num_pages;
+  t.q = static_cast<const __nv_bfloat16*>(q);
+  t.out = out;
+  t.lse = lse;
+  t.total_q = b->total_q;
+  t.max_q_len = b->max_q_len;
+  t.max_ctx_len = b->max_ctx_len;
+  t.prefix_tiles_per_split = pl.slice_len / 128;
+  t.max_splits = pl.slices;
+  t.part_o = part_o;
+  t.part_ml = part_ml;
+  t.err = h->err;
+  CUtensorMap tm, tm_q;
+  if ((st = make_pool_map(h, layer, &tm)) != HSWA_OK) return st;
+  if ((st = make_rows_map(h, q, h->cfg.num_q_heads, b->total_q, hswa_cross_tile_tokens(t.m), &tm_q, h->group)) != HSWA_OK) return st;
+  if (hswa_launch_cross_tc(tm, tm_q, t, pl.row_tiles, s) != cudaSuccess) return HSWA_ERR_CUDA;
+  if (pl.slices > 1) {
+    const CrossParams p = {t.m, out, lse, b->total_q, pl.slices, part_o, part_ml};
+    if (hswa_launch_cross_combine(p, s) != cudaSuccess) return HSWA_ERR_CUDA;
   }
-  if (p.slices > 1 && hswa_launch_cross_combine(p, s) != cudaSuccess) return HSWA_ERR_CUDA;
   return HSWA_OK;
 }
 

@@ -116,23 +116,15 @@ struct PrefillParams {
   float2* part_ml;
 };
 
-// Cross attention over an encoder's cached states.  Rows are packed: row rho of (request, KV head) is token rho / G,
-// query head kh * G + rho % G, so that the heads of a group share every K/V tile.
+// Join of the key slices of cross attention.
 struct CrossParams {
   ModelParams m;
-  BatchParams b;
-  const __nv_bfloat16* pool;
-  int64_t num_pages;
-  const __nv_bfloat16* q;  // [T][Hq][D]
-  void* out;               // [T][Hq][D]
-  float* lse;              // [T][Hq] or null
-  int32_t total_q, max_q_len, max_ctx_len;
-  int32_t row_tiles;   // row tiles per (request, KV head)
-  int32_t slices;      // key slices; 1 = write the output directly
-  int32_t slice_len;   // keys per slice (multiple of 128)
-  float* part_o;       // [T * Hq][slices][D]
-  float2* part_ml;     // [T * Hq][slices] (m in log2 units, l; l = 0: the slice holds no key of the row)
-  int32_t* err;
+  void* out;   // [T][Hq][D]
+  float* lse;  // [T][Hq] or null
+  int32_t total_q;
+  int32_t slices;
+  const float* part_o;    // [T * Hq][slices][D]
+  const float2* part_ml;  // [T * Hq][slices] (m in log2 units, l; l = 0: the slice holds no key of the row)
 };
 
 struct WeightsParams {
@@ -190,14 +182,12 @@ cudaError_t hswa_launch_decode(const hswa_handle* h, const CUtensorMap& tm_pool,
 cudaError_t hswa_launch_combine(const DecodeParams& p, bool cross, cudaStream_t s);
 // Cross attention, one token per request: the streaming decode kernel without a new token
 cudaError_t hswa_launch_decode_cross(const CUtensorMap& tm_pool, const DecodeParams& p, cudaStream_t s);
-// Cross attention, any number of tokens per request: warp-level tile kernel, and the join of key slices
-cudaError_t hswa_launch_cross_mma(const CrossParams& p, cudaStream_t s);
-cudaError_t hswa_launch_cross_combine(const CrossParams& p, cudaStream_t s);
-bool hswa_cross_tc_supported(const ModelParams& m);
-int hswa_cross_tc_tile_tokens(const ModelParams& m);  // tokens per Q tile (box height of tm_q); two tiles per block
+// Cross attention, any number of tokens per request: the tile kernel, two Q tiles of hswa_cross_tile_tokens tokens (the box
+// height of tm_q) per block, and the join of its key slices
+int hswa_cross_tile_tokens(const ModelParams& m);
 cudaError_t hswa_launch_cross_tc(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const PrefillParams& p, int row_tiles,
                                  cudaStream_t s);
-int hswa_cross_mma_rows();  // packed (token, head) rows per block
+cudaError_t hswa_launch_cross_combine(const CrossParams& p, cudaStream_t s);
 // Eviction: accumulated attention weights, choice of the kept positions, compaction
 int hswa_attn_weights_tile_tokens(const ModelParams& m, int max_q_len);  // tokens per Q tile (box height of tm_q)
 cudaError_t hswa_launch_attn_weights(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const WeightsParams& p, int num_sms,

@@ -236,7 +236,8 @@ __device__ __forceinline__ bool v_tile_needs_patch(int is_swa, int ctx, int j) {
 
 // STAGES = depth of the K and of the V tile ring: 2 for prefill; 1 for the shared-prefix stage, whose block then leaves
 // room on its SM for a block of the suffix decode kernel that streams beside it.
-template <int MODE, int STAGES>
+// DH = head dim; a tile keeps room for two 64-element halves whatever DH is.
+template <int MODE, int STAGES, int DH = HD>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_constant__ CUtensorMap tm_q,
                   const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
@@ -245,6 +246,9 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
   // need without slack): Q tiles | K ring | V ring | barriers and flags.
   extern __shared__ __align__(1024) uint8_t smem[];
   constexpr bool PREFIX = MODE == MODE_PREFIX, CROSS = MODE == MODE_CROSS;
+  constexpr int HALVES = DH / 64;
+  static_assert(DH == HD || CROSS, "other head dims only for cross attention");
+  constexpr uint32_t IDESC_O = (IDESC_PV & ~(0x3fu << 17)) | ((uint32_t)(DH >> 3) << 17);
   constexpr int OFF_V = OFF_K + STAGES * TILE_BYTES;
   constexpr int OFF_STATE = OFF_V + STAGES * TILE_BYTES;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + OFF_STATE);                     // [NUM_BARS]
@@ -328,9 +332,9 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
           p.part_ml[orow * p.max_splits + slice] = make_float2(-INFINITY, 0.f);
           continue;
         }
-        uint4* dst = M.out_fp32 ? reinterpret_cast<uint4*>(reinterpret_cast<float*>(p.out) + orow * HD)
-                                : reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + orow * HD);
-        for (int k = 0; k < (M.out_fp32 ? 32 : 16); ++k) dst[k] = make_uint4(0, 0, 0, 0);
+        uint4* dst = M.out_fp32 ? reinterpret_cast<uint4*>(reinterpret_cast<float*>(p.out) + orow * DH)
+                                : reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + orow * DH);
+        for (int k = 0; k < (M.out_fp32 ? DH / 4 : DH / 8); ++k) dst[k] = make_uint4(0, 0, 0, 0);
         if (p.lse) p.lse[orow] = -INFINITY;
       }
       return;
@@ -431,9 +435,9 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       tma_prefetch_desc(&tm_q);
       tma_prefetch_desc(&tm_k);
       tma_prefetch_desc(&tm_v);
-      mbar_arrive_expect_tx(bar(BAR_Q), CROSS ? nq_tiles * 2 * tok_tile * M.G * 128 : 2 * TILE_BYTES);
+      mbar_arrive_expect_tx(bar(BAR_Q), CROSS ? nq_tiles * HALVES * tok_tile * M.G * 128 : 2 * TILE_BYTES);
       for (int i = 0; i < nq_tiles; ++i)
-        for (int hf = 0; hf < 2; ++hf) {
+        for (int hf = 0; hf < HALVES; ++hf) {
           if constexpr (CROSS)  // box {64, G heads, tok_tile tokens} over q [T][Hq][D]
             tma_load_3d(sbase + OFF_Q + i * TILE_BYTES + hf * HALF_BYTES, &tm_q, bar(BAR_Q), hf * 64, h0, t0 + (2 * b + i) * tok_tile);
           else if constexpr (PREFIX)  // box {64, 8 heads, 16 requests} over q [B][Hq][D]
@@ -468,11 +472,11 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
             break;
           }
           const uint32_t full = kv && v_tile_needs_patch(0, ctx, j) ? bar(BAR_VPATCH + stage) : bar((kv ? BAR_VFULL : BAR_KFULL) + stage);
-          if (lane == 0) mbar_arrive_expect_tx(full, TILE_BYTES);
+          if (lane == 0) mbar_arrive_expect_tx(full, HALVES * HALF_BYTES);
           __syncwarp();
           if (lane < ppt) {
             const uint32_t dst = sbase + (kv ? OFF_V : OFF_K) + stage * TILE_BYTES + lane * M.P * 128;
-            for (int hf = 0; hf < 2; ++hf) tma_load_4d(dst + hf * HALF_BYTES, &tm_pool, full, hf * 64, 0, kv * M.Hkv + kh, page);
+            for (int hf = 0; hf < HALVES; ++hf) tma_load_4d(dst + hf * HALF_BYTES, &tm_pool, full, hf * 64, 0, kv * M.Hkv + kh, page);
           }
         }
       }
@@ -543,7 +547,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
         const uint64_t dq = i ? dQ1 : dQ0, dk = desc_advance(dK0, stage * TILE_BYTES);
         if (elect_one()) {
 #pragma unroll
-          for (int ks = 0; ks < HD / 16; ++ks) {
+          for (int ks = 0; ks < DH / 16; ++ks) {
             const uint32_t off = (ks >> 2) * HALF_BYTES + (ks & 3) * 32;
             tc_mma_ss(tmem + i * 128, desc_advance(dq, off), desc_advance(dk, off), IDESC_S, ks > 0);
           }
@@ -560,7 +564,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
         if (elect_one()) {
 #pragma unroll
           for (int q = 0; q < KSTEPS; ++q)
-            tc_mma_ts(tmem + 256 + i * 128, tp + q * 8, desc_advance(dv, q * 2048), IDESC_PV, !(first && part == 0 && q == 0));
+            tc_mma_ts(tmem + 256 + i * 128, tp + q * 8, desc_advance(dv, q * 2048), IDESC_O, !(first && part == 0 && q == 0));
         }
         __syncwarp();
       };
@@ -643,7 +647,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
         }
         n_patched ^= 1u << stage;
         uint8_t* sV = smem + OFF_V + stage * TILE_BYTES;
-        for (int idx = lane; idx < BN * 16; idx += 32) {  // 16-byte chunks: 128 rows x 2 halves x 8
+        for (int idx = lane; idx < BN * 8 * HALVES; idx += 32) {  // 16-byte chunks: 128 rows x halves x 8
           const int row = (idx >> 3) & (BN - 1), hf = idx >> 10, ch = idx & 7;
           bool live;
           if (!p.is_swa) {
@@ -770,7 +774,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
           const float m_new = grow ? mx_s : m_st;
           const float alpha = (m_new == -INFINITY) ? 1.f : fast_exp2(m_st - m_new);
 #pragma unroll 1
-          for (int c16 = 0; c16 < 8; ++c16) {
+          for (int c16 = 0; c16 < DH / 16; ++c16) {
             uint32_t w[16];
             tmem_ld16(tO + c16 * 16, w);
             tc_wait_ld();
@@ -834,12 +838,12 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       const int64_t prow = CROSS ? cross_row * p.max_splits + slice
                                  : ((int64_t)rq * M.Hq + kh * M.G + (rr & 7)) * p.max_splits + blockIdx.x;
 #pragma unroll 1
-      for (int c4 = 0; c4 < 4; ++c4) {
+      for (int c4 = 0; c4 < DH / 32; ++c4) {
         uint32_t w[32];
         tmem_ld32(tO + c4 * 32, w);
         tc_wait_ld();
         if (row_ok) {
-          float4* dst = reinterpret_cast<float4*>(p.part_o + prow * HD + c4 * 32);
+          float4* dst = reinterpret_cast<float4*>(p.part_o + prow * DH + c4 * 32);
 #pragma unroll
           for (int k = 0; k < 8; ++k)
             dst[k] = make_float4(__uint_as_float(w[4 * k]), __uint_as_float(w[4 * k + 1]), __uint_as_float(w[4 * k + 2]),
@@ -853,20 +857,20 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       const bool row_ok = ok && (CROSS ? tok_ok : ri < n);
       const int64_t orow = CROSS ? cross_row : ((int64_t)(t0 + ri) * M.Hq + (h0 + i));
 #pragma unroll 1
-      for (int c4 = 0; c4 < 4; ++c4) {
+      for (int c4 = 0; c4 < DH / 32; ++c4) {
         uint32_t w[32];
         tmem_ld32(tO + c4 * 32, w);
         tc_wait_ld();
         if (row_ok) {
           const int col0 = c4 * 32;
           if (M.out_fp32) {
-            float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + orow * HD + col0);
+            float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + orow * DH + col0);
 #pragma unroll
             for (int k = 0; k < 8; ++k)
               dst[k] = make_float4(__uint_as_float(w[4 * k]) * inv, __uint_as_float(w[4 * k + 1]) * inv,
                                    __uint_as_float(w[4 * k + 2]) * inv, __uint_as_float(w[4 * k + 3]) * inv);
           } else {
-            uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + orow * HD + col0);
+            uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + orow * DH + col0);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               uint4 u;
@@ -1678,11 +1682,11 @@ cudaError_t hswa_launch_decode_prefix(const CUtensorMap& tm_pool, const CUtensor
 
 // Cross attention: grid (row tiles x key slices, KV heads, requests).  tm_q has box {64, G heads, 128 / G tokens} over q
 // [T][Hq][D]; p carries the host's bounds, the slice plan and, for more than one slice, the partial buffers.
-bool hswa_cross_tc_supported(const ModelParams& m) { return m.D == 128; }
-int hswa_cross_tc_tile_tokens(const ModelParams& m) { return BM / m.G; }
-cudaError_t hswa_launch_cross_tc(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const PrefillParams& p, int row_tiles, cudaStream_t s) {
+int hswa_cross_tile_tokens(const ModelParams& m) { return BM / m.G; }
+template <int DH>
+static cudaError_t launch_cross_t(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const PrefillParams& p, int row_tiles, cudaStream_t s) {
   constexpr int SMEM_BYTES = tile_kernel_smem(KV_STAGES);
-  auto kern = prefill_tc_kernel<MODE_CROSS, KV_STAGES>;
+  auto kern = prefill_tc_kernel<MODE_CROSS, KV_STAGES, DH>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
   if (e != cudaSuccess) return e;
   static const cudaError_t budget = check_register_budget(kern, NUM_THREADS);
@@ -1690,6 +1694,9 @@ cudaError_t hswa_launch_cross_tc(const CUtensorMap& tm_pool, const CUtensorMap& 
   dim3 grid(row_tiles * p.max_splits, p.m.Hkv, p.b.B);
   kern<<<grid, NUM_THREADS, SMEM_BYTES, s>>>(tm_pool, tm_q, tm_pool, tm_pool, p, row_tiles);
   return cudaGetLastError();
+}
+cudaError_t hswa_launch_cross_tc(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const PrefillParams& p, int row_tiles, cudaStream_t s) {
+  return p.m.D == 128 ? launch_cross_t<128>(tm_pool, tm_q, p, row_tiles, s) : launch_cross_t<64>(tm_pool, tm_q, p, row_tiles, s);
 }
 
 // Streaming SWA kernel (GQA group of 8, window 128): every token from the 129th of each request on.  tm_q has box
