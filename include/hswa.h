@@ -247,11 +247,12 @@ hswa_status hswa_prefill_attn(hswa_handle* h, const hswa_layer* layer, const hsw
  * tokens to ALL of its ctx_len[r] cached positions: no causal mask, nothing is appended.  ctx_len[r] = 0 gives zeros and
  * an lse of minus infinity; n[r] = 0 leaves nothing to do for the request.
  * q: device bf16 [T][Hq][D]; out: device [T][Hq][D] in cfg.out_dtype; lse: device fp32 [T][Hq] or NULL.
- * batch->q_indptr may be NULL (one token per request, the serving step).  Probabilities enter the PV product as bf16; row
- * sums and lse are taken over the fp32 values.  Workspace: hswa_cross_workspace_need bytes (0: none needed), else
+ * batch->q_indptr may be NULL (one token per request, the serving step); with it, rows of q behind the last request's do
+ * not matter and those of out and lse are left as they were.  Probabilities enter the PV product as bf16; row sums and
+ * lse are taken over the fp32 values.  Workspace: hswa_cross_workspace_need bytes (0: none needed), else
  * HSWA_ERR_WORKSPACE.  The block table must cover max_ctx_len and the layer must not be an SWA layer
- * (HSWA_ERR_INVALID_ARG).  A request longer than max_ctx_len or max_q_len is recorded as HSWA_ERR_BOUNDS (index -1 / -2)
- * and what the bounds cover is computed.
+ * (HSWA_ERR_INVALID_ARG); max_ctx_len is at most 2^30 (HSWA_ERR_UNSUPPORTED, the need is then 0).  A request longer than
+ * max_ctx_len or max_q_len is recorded as HSWA_ERR_BOUNDS (index -1 / -2) and what the bounds cover is computed.
  *
  * This call and the eviction calls below refuse a current device other than the handle's (HSWA_ERR_INVALID_ARG).
  *
@@ -275,9 +276,10 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
  *   prompt by its last n tokens only, pass those tokens' q and lse with ctx_len reduced by n.
  *   q: device bf16 [T][Hq][D]; lse: device fp32 [T][Hq]; weights: device fp32 [B][Hkv][weights_stride], columns at or
  *   past the request's last position are not touched.  weights_stride and the block table must cover max_ctx_len, decay
- *   must be finite and >= 0: HSWA_ERR_INVALID_ARG.  A request longer than max_ctx_len or max_q_len, or whose ctx + n passes
- *   weights_stride or the block table, is recorded as HSWA_ERR_BOUNDS (index -1 / -2 / -3) and left out.  Sums are in fp32 in a fixed order: repeated
- *   calls on equal inputs agree bit for bit.
+ *   must be finite and >= 0: HSWA_ERR_INVALID_ARG; max_ctx_len + max_q_len is at most 2^30: HSWA_ERR_UNSUPPORTED.  A
+ *   request longer than max_ctx_len or max_q_len, or whose ctx + n passes weights_stride or the block table, is recorded as
+ *   HSWA_ERR_BOUNDS (index -1 / -2 / -3) and left out.  Sums are in fp32 in a fixed order: repeated calls on equal inputs
+ *   agree bit for bit.
  *
  * hswa_evict_select: keep_idx[r][kh][0 .. kept) = the kept = min(keep_len[r], ctx_len[r]) positions of largest weight, in
  *   ascending order; entries from kept to max_keep are set to -1, kept_len[r] = kept.  The first protect_first and the

@@ -59,6 +59,9 @@ hswa_status check_common(const hswa_handle* h, const hswa_layer* layer, const hs
   return HSWA_OK;
 }
 
+// Positions of a request that the calls on Full layers' contexts below take: positions and the steps past them fit 32 bits.
+constexpr int kMaxPositions = 1 << 30;
+
 // The launches go to the current device, whose stream the caller passes: it has to be the handle's.
 bool device_is_current(const hswa_handle* h) {
   int dev = -1;
@@ -149,7 +152,8 @@ struct CrossPlan {
 
 bool plan_cross(const hswa_handle* h, int batch, int total_q, int max_q_len, int max_ctx_len, CrossPlan* pl) {
   CrossPlan c = {};
-  c.decode = max_q_len == 1 && total_q == batch;
+  if (max_ctx_len > kMaxPositions) return false;
+  c.decode = max_q_len == 1;
   if (c.decode) {
     if (!plan_decode(h, 0, batch, max_ctx_len > 0 ? max_ctx_len - 1 : 0, 0, 1, &c.dec)) return false;
     if (max_ctx_len <= kUnsplitLen) {  // a second launch costs more than the few tiles that it would spare a block
@@ -162,7 +166,7 @@ bool plan_cross(const hswa_handle* h, int batch, int total_q, int max_q_len, int
   } else {
     if (batch > 65535 || h->cfg.num_kv_heads > 65535) return false;  // grid extents
     const int tokens = 2 * hswa_cross_tile_tokens(model_params(h));
-    c.row_tiles = (max_q_len + tokens - 1) / tokens;
+    c.row_tiles = (int)(((int64_t)max_q_len + tokens - 1) / tokens);
     const int64_t blocks = (int64_t)c.row_tiles * h->cfg.num_kv_heads * batch;
     const int64_t want = (h->num_sms + blocks - 1) / blocks, most = (max_ctx_len + 511) / 512;  // one wave of blocks
     int64_t slices = want < most ? want : most;
@@ -739,7 +743,7 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
   if ((st = make_rows_map(h, q, h->cfg.num_q_heads, b->total_q, hswa_cross_tile_tokens(t.m), &tm_q, h->group)) != HSWA_OK) return st;
   if (hswa_launch_cross_tc(tm, tm_q, t, pl.row_tiles, s) != cudaSuccess) return HSWA_ERR_CUDA;
   if (pl.slices > 1) {
-    const CrossParams p = {t.m, out, lse, b->total_q, pl.slices, part_o, part_ml};
+    const CrossParams p = {t.m, out, lse, b->total_q, b->q_indptr ? b->q_indptr + b->batch : nullptr, pl.slices, part_o, part_ml};
     if (hswa_launch_cross_combine(p, s) != cudaSuccess) return HSWA_ERR_CUDA;
   }
   return HSWA_OK;
@@ -754,6 +758,7 @@ hswa_status hswa_attn_weights(hswa_handle* h, const hswa_layer* layer, const hsw
   if (layer->is_swa || weights_stride < 0 || !(decay >= 0.f) || std::isinf(decay)) return HSWA_ERR_INVALID_ARG;
   // (the longest context and the longest step need not belong to one request: their sum is checked per request)
   if ((int64_t)b->max_ctx_len > (int64_t)b->max_blocks * h->cfg.page_size || b->max_ctx_len > weights_stride) return HSWA_ERR_INVALID_ARG;
+  if ((int64_t)b->max_ctx_len + b->max_q_len > kMaxPositions) return HSWA_ERR_UNSUPPORTED;
   if (b->max_ctx_len == 0 && (!causal || b->max_q_len == 0)) return HSWA_OK;
   if (!weights || (b->total_q > 0 && (!q || !lse || !aligned16(q)))) return HSWA_ERR_INVALID_ARG;
   if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
@@ -789,7 +794,7 @@ hswa_status hswa_evict_select(hswa_handle* h, int32_t batch, const int32_t* ctx_
   if (batch == 0) return HSWA_OK;
   if (!ctx_len || !keep_len || !kept_len || (max_keep > 0 && !keep_idx) || (max_ctx_len > 0 && !weights)) return HSWA_ERR_INVALID_ARG;
   if (kept_len == ctx_len) return HSWA_ERR_INVALID_ARG;  // the heads of a request read its length while one of them writes it
-  if (max_ctx_len > (1 << 30)) return HSWA_ERR_UNSUPPORTED;
+  if (max_ctx_len > kMaxPositions) return HSWA_ERR_UNSUPPORTED;
   if ((int64_t)batch * h->cfg.num_kv_heads > INT32_MAX) return HSWA_ERR_UNSUPPORTED;
   if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
   SelectParams p = {};
@@ -819,6 +824,7 @@ hswa_status hswa_evict_compact(hswa_handle* h, const hswa_layer* layer, const hs
   if (max_keep < 0 || dst_max_blocks < 0) return HSWA_ERR_INVALID_ARG;
   if (b->batch == 0 || max_keep == 0) return HSWA_OK;
   if (layer->is_swa || !keep_idx || !kept_len || !dst_block_table || dst_block_table == b->block_table) return HSWA_ERR_INVALID_ARG;
+  if (max_keep > kMaxPositions) return HSWA_ERR_UNSUPPORTED;
   if ((int64_t)max_keep > (int64_t)dst_max_blocks * h->cfg.page_size) return HSWA_ERR_INVALID_ARG;
   if ((int64_t)b->max_ctx_len > (int64_t)b->max_blocks * h->cfg.page_size) return HSWA_ERR_INVALID_ARG;
   if ((weights == nullptr) != (weights_out == nullptr)) return HSWA_ERR_INVALID_ARG;

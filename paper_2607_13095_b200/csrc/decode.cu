@@ -176,7 +176,8 @@ __device__ __forceinline__ void consume_tile(uint8_t* sV, uint32_t aK, uint32_t 
 
 // CROSS = true: attention to an encoder's states (hswa_cross_attn with one token per request).  All ctx keys and no
 // others are visible -- there is no new token, and a request may have none at all, whose block still writes its rows
-// (zeros, log-sum-exp minus infinity).  Lengths are clamped to the host's bound.
+// (zeros, log-sum-exp minus infinity).  Lengths are clamped to the host's bound.  With row offsets (q_indptr) a request may
+// also have no token, and its row need not be the r-th; partials stay by request.
 template <int D, int P, int NS, int NW, bool CROSS = false>
 __global__ void __launch_bounds__((NW + 1) * 32, 2)
 decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p) {
@@ -205,7 +206,17 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p)
   const int ctx = p.b.ctx_len[r];
   const int kv_len = CROSS ? max(0, min(ctx, p.max_ctx_len)) : ctx + 1;
   // the grid was sized from the host's bound: a longer context would silently lose its tail
-  if (threadIdx.x == 0 && split == 0 && kh == 0 && ctx > p.max_ctx_len) record_error(p.err, HSWA_ERR_BOUNDS, r, -1, ctx);
+  if (threadIdx.x == 0 && split == 0 && kh == 0 && (ctx > p.max_ctx_len || (CROSS && ctx < 0)))
+    record_error(p.err, HSWA_ERR_BOUNDS, r, -1, ctx);
+  int row_r = r;  // the request's row of q and out
+  if constexpr (CROSS) {
+    if (p.b.q_indptr) {
+      row_r = p.b.q_indptr[r];
+      const int n = p.b.q_indptr[r + 1] - row_r;
+      if (threadIdx.x == 0 && split == 0 && kh == 0 && (n < 0 || n > 1)) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, n);
+      if (n <= 0) return;
+    }
+  }
 
   KeyRange kr;
   kr.is_swa = p.is_swa;
@@ -326,7 +337,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p)
     if (!p.late_dep_wait) griddep_wait();
     griddep_launch_dependents();
     {
-      const __nv_bfloat16* qrow = p.q + ((int64_t)r * M.Hq + kh * M.G + g_row) * D;
+      const __nv_bfloat16* qrow = p.q + ((int64_t)row_r * M.Hq + kh * M.G + g_row) * D;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         qf[ks][0] = g_row < M.G ? *reinterpret_cast<const uint32_t*>(qrow + ks * 16 + qd) : 0u;
@@ -426,7 +437,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p)
         O += f * sc_o[(w * 8 + g) * D + d];
       }
     }
-    const int64_t row = (int64_t)r * M.Hq + kh * M.G + g;
+    const int64_t row = (int64_t)(p.max_splits == 1 ? row_r : r) * M.Hq + kh * M.G + g;
     if (p.max_splits == 1) {
       const bool some = CROSS ? L != 0.f : L > 0.f;  // (CROSS: a NaN among the inputs shows in the output)
       const float val = some ? O / L : 0.f;
@@ -457,6 +468,14 @@ __global__ void __launch_bounds__(128) combine_kernel(const DecodeParams p) {
   if (warp_global >= p.b.B * p.nq * M.Hq) return;
   const int r = warp_global / (p.nq * M.Hq);
   const int64_t row = warp_global;
+  int64_t out_row = row;
+  if constexpr (CROSS) {
+    if (p.b.q_indptr) {
+      const int t0 = p.b.q_indptr[r];
+      if (p.b.q_indptr[r + 1] <= t0) return;
+      out_row = (int64_t)t0 * M.Hq + (warp_global - r * M.Hq);
+    }
+  }
   const int kv_len = CROSS ? max(0, min(p.b.ctx_len[r], p.max_ctx_len)) : p.b.ctx_len[r] + p.nq;
   const int n_splits = min(p.max_splits, p.split_base + (kv_len - p.k_start + p.split_len - 1) / p.split_len);
   const float2* ml = p.part_ml + row * p.max_splits;
@@ -494,11 +513,11 @@ __global__ void __launch_bounds__(128) combine_kernel(const DecodeParams p) {
   for (int i = 0; i < PER; ++i) {
     const float val = acc[i] * inv;
     if (M.out_fp32)
-      reinterpret_cast<float*>(p.out)[row * D + lane * PER + i] = val;
+      reinterpret_cast<float*>(p.out)[out_row * D + lane * PER + i] = val;
     else
-      reinterpret_cast<__nv_bfloat16*>(p.out)[row * D + lane * PER + i] = __float2bfloat16_rn(val);
+      reinterpret_cast<__nv_bfloat16*>(p.out)[out_row * D + lane * PER + i] = __float2bfloat16_rn(val);
   }
-  if (lane == 0 && p.lse) p.lse[row] = some ? (mm + log2f(L)) * 0.6931471805599453f : -INFINITY;
+  if (lane == 0 && p.lse) p.lse[out_row] = some ? (mm + log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------------------------------------

@@ -156,6 +156,59 @@ def test_cross_bounds_wider_than_the_batch():
     check_cross(c, *run_cross(c, max_ctx=3000, max_q=7))
 
 
+def no_rings(d, B):
+    return torch.zeros((B, d.ring_pages), dtype=torch.int32, device="cuda"), torch.zeros((B,), dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(3, 64, 16)], ids=str)
+@pytest.mark.parametrize("ctx,n", [([100, 300, 40], [1, 0, 1]), ([100, 300, 0, 40, 5], [0, 1, 1, 0, 1]), ([9000, 700, 4100], [0, 1, 1]),
+                                   ([300, 9000, 20], [1, 0, 1]), ([100, 300], [0, 0]), ([600, 40, 9], [5, 0, 2])])
+@pytest.mark.parametrize("pad", ["batch", "more"])
+def test_cross_and_weights_of_a_padded_batch(d, ctx, n, pad):
+    """Requests without a token, and rows behind the last request's: those rows are left as they were."""
+    c = Case(d, ctx, n, seed=9)
+    used = int(c.indptr[-1])
+    total = max(used, len(ctx)) + (0 if pad == "batch" else 3)
+    h = make_handle(d)
+    b = hb.Batch(dev_i32(c.ctx), dev_i32(c.table), *no_rings(d, len(ctx)), dev_i32(c.indptr), max_q_len=max(1, int(c.n.max())), total_q=total,
+                 max_ctx_len=int(c.ctx.max()))
+    q = np.full((total, d.num_q_heads, d.head_dim), NAN_BITS, np.uint16)
+    q[:used] = c.q
+    out = torch.full((total, d.num_q_heads, d.head_dim), 7.0, device="cuda")
+    lse = torch.full((total, d.num_q_heads), 7.0, device="cuda")
+    layer = hb.Layer(to_dev_bf16(c.pool), False)
+    hb.hswa_cross_attn(h, layer, b, to_dev_bf16(q), out, lse, workspace(h, b))
+    no_error(h)
+    assert (out[used:] == 7).all() and (lse[used:] == 7).all()
+    check_cross(c, out[:used].double().cpu().numpy(), lse[:used].double().cpu().numpy())
+    old = np.random.default_rng(9).random((len(ctx), d.num_kv_heads, int(c.ctx.max()) + 3)).astype(np.float32)
+    w = torch.from_numpy(old).cuda()
+    lse[used:] = float("nan")
+    hb.hswa_attn_weights(h, layer, b, False, to_dev_bf16(q), lse, 0.5, w)
+    no_error(h)
+    check_weights(c, 0.5, lse[:used].cpu().numpy(), old, w.cpu().numpy())
+
+
+def test_cross_single_tokens_record_values_out_of_range():
+    d = dims(8, 128, 64)
+    c = Case(d, [100, 300], [1, 1], seed=10)
+    h = make_handle(d)
+    for ctx, indptr, index, value in ([[-5, 300], None, -1, -5], [[100, 301], None, -1, 301], [[100, 300], [0, 2, 2], -2, 2]):
+        b = hb.Batch(dev_i32(np.asarray(ctx, np.int32)), dev_i32(c.table), *no_rings(d, 2),
+                     None if indptr is None else dev_i32(np.asarray(indptr, np.int32)), max_q_len=1, total_q=2, max_ctx_len=300)
+        out = torch.zeros((2, d.num_q_heads, d.head_dim), device="cuda")
+        hb.hswa_cross_attn(h, hb.Layer(to_dev_bf16(c.pool), False), b, to_dev_bf16(c.q), out, None, workspace(h, b))
+        st = hb.hswa_get_async_error(h)
+        assert st[0] == hb.HSWA_ERR_BOUNDS and st[2] == index and st[3] == value, st
+
+
+def test_lengths_past_the_limit_are_refused():
+    d = dims(8, 128, 64)
+    h = make_handle(d)
+    assert hb.hswa_cross_workspace_need(h, 1, 1, 1, 2 ** 30 + 1) == 0
+    assert hb.hswa_cross_workspace_need(h, 1, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1) == 0
+
+
 def run_weights(c, decay, lse, old, stride_extra=3, single=None, **bounds):
     h = make_handle(c.d)
     w = torch.from_numpy(old).cuda()
