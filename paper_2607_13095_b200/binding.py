@@ -317,6 +317,9 @@ def hswa_cross_workspace_need(h: Handle, batch: int, total_q: int, max_q_len: in
 def hswa_cross_attn(h: Handle, layer: Layer, batch: Batch, q, out, lse=None, workspace=None):
     """Attention of q [T][Hq][D] to all ctx_len[r] cached states of each request (no causal mask, nothing appended)."""
     assert q.dtype == torch.bfloat16 and out.dtype == h.out_dtype and (lse is None or lse.dtype == torch.float32)
+    rows = batch.total_q * h.cfg.num_q_heads
+    n = rows * h.cfg.head_dim
+    assert q.numel() >= n and out.numel() >= n and (lse is None or lse.numel() >= rows), "fewer rows than total_q"
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(load().hswa_cross_attn(h.ptr, C.byref(layer.c), C.byref(batch.c), _ptr(q), _ptr(out), _ptr(lse), _ptr(workspace),
                                   ws_bytes, _stream()), "hswa_cross_attn")
@@ -327,6 +330,8 @@ def hswa_attn_weights(h: Handle, layer: Layer, batch: Batch, causal: bool, q, ls
     assert q.dtype == torch.bfloat16 and lse.dtype == torch.float32
     B, heads, stride = weights.shape
     assert weights.dtype == torch.float32 and B == batch.batch and heads == h.cfg.num_kv_heads
+    rows = batch.total_q * h.cfg.num_q_heads
+    assert q.numel() >= rows * h.cfg.head_dim and lse.numel() >= rows, "fewer rows than total_q"
     _check(load().hswa_attn_weights(h.ptr, C.byref(layer.c), C.byref(batch.c), bool(causal), _ptr(q), _ptr(lse), decay, _ptr(weights),
                                     stride, _stream()), "hswa_attn_weights")
 
@@ -339,6 +344,7 @@ def hswa_evict_select(h: Handle, batch: int, ctx_len: torch.Tensor, max_ctx_len:
     w_batch, w_heads, stride = weights.shape
     k_batch, k_heads, max_keep = keep_idx.shape
     assert weights.dtype == torch.float32 and w_batch == k_batch == batch and w_heads == k_heads == heads
+    assert ctx_len.numel() >= batch and keep_len.numel() >= batch and kept_len.numel() >= batch
     _check(load().hswa_evict_select(h.ptr, batch, _ptr(ctx_len), max_ctx_len, _ptr(weights), stride, _ptr(keep_len), max_keep,
                                     protect_first, protect_last, _ptr(keep_idx), _ptr(kept_len), _stream()), "hswa_evict_select")
 
@@ -350,8 +356,10 @@ def hswa_evict_compact(h: Handle, layer: Layer, batch: Batch, keep_idx: torch.Te
     i32, f32 = torch.int32, torch.float32
     assert keep_idx.dtype == i32 and kept_len.dtype == i32 and dst_block_table.dtype == i32
     assert (weights is None or weights.dtype == f32) and (weights_out is None or weights_out.dtype == f32)
-    _, _, max_keep = keep_idx.shape
-    _, dst_blocks = dst_block_table.shape
+    B, heads, max_keep = keep_idx.shape
+    dst_batch, dst_blocks = dst_block_table.shape
+    assert B == dst_batch == batch.batch and heads == h.cfg.num_kv_heads and kept_len.numel() >= B
+    assert all(w is None or (w.dim() == 3 and w.shape[0] == B and w.shape[1] == heads) for w in (weights, weights_out))
     _check(load().hswa_evict_compact(h.ptr, C.byref(layer.c), C.byref(batch.c), _ptr(keep_idx), _ptr(kept_len), max_keep,
                                      _ptr(dst_block_table), dst_blocks, _ptr(weights), 0 if weights is None else weights.shape[2],
                                      _ptr(weights_out), 0 if weights_out is None else weights_out.shape[2], _stream()),

@@ -692,3 +692,27 @@ def test_empty_calls():
     want = torch.full((1, 2, 200), 2.0)
     want[..., :100] = 1.0
     assert torch.equal(w.cpu(), want)
+
+
+def test_tensors_too_small_for_the_batch_are_refused():
+    d = dims(8, 128, 64)
+    c = Case(d, [100, 200], [1, 1], seed=20)
+    h, layer, b = make_handle(d), hb.Layer(to_dev_bf16(c.pool), False), c.batch()
+    q, out, lse = to_dev_bf16(c.q), torch.zeros((2, 16, 128), device="cuda"), torch.zeros((2, 16), device="cuda")
+    w, idx, kept = torch.zeros((2, 2, 200), device="cuda"), dev_i32(np.zeros((2, 2, 4), np.int32)), dev_i32([1, 1])
+    dst = dev_i32([[0], [1]])
+    for bad in ((q[:1], out, lse), (q, out[:1], lse), (q, out, lse[:1])):
+        with pytest.raises(AssertionError):
+            hb.hswa_cross_attn(h, layer, b, *bad)
+    for bad in ((q[:1], lse, 0.0, w), (q, lse[:1], 0.0, w), (q, lse, 0.0, w[:1]), (q, lse, 0.0, w[:, :1])):
+        with pytest.raises(AssertionError):
+            hb.hswa_attn_weights(h, layer, b, False, *bad)
+    for bad in ((kept[:1], 200, w, kept, idx, kept.clone()), (kept, 200, w, kept[:1], idx, kept.clone()), (kept, 200, w, kept, idx, kept[:1]),
+                (kept, 200, w[:1], kept, idx, kept.clone()), (kept, 200, w, kept, idx[:, :1], kept.clone())):
+        with pytest.raises(AssertionError):
+            hb.hswa_evict_select(h, 2, *bad)
+    for bad in ((idx[:1], kept, dst), (idx[:, :1], kept, dst), (idx, kept[:1], dst), (idx, kept, dst[:1]), (idx, kept, dst, w[:1], w.clone()),
+                (idx, kept, dst, w, w[:, :1].clone())):
+        with pytest.raises(AssertionError):
+            hb.hswa_evict_compact(h, layer, b, *bad)
+    no_error(h)
