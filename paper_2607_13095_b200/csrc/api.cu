@@ -146,7 +146,7 @@ bool plan_decode(const hswa_handle* h, int is_swa, int batch, int max_ctx_len, i
 struct CrossPlan {
   bool decode;
   DecodePlan dec;
-  int row_tiles, slices, slice_len;
+  int q_tiles, row_tiles, slices, slice_len;  // the tile kernel: Q tiles per block, blocks per (request, KV head), key slices
   size_t o_bytes, ml_bytes;
 };
 
@@ -165,10 +165,16 @@ bool plan_cross(const hswa_handle* h, int batch, int total_q, int max_q_len, int
     c.ml_bytes = c.dec.ml_bytes;
   } else {
     if (batch > 65535 || h->cfg.num_kv_heads > 65535) return false;  // grid extents
-    const int tokens = 2 * hswa_cross_tile_tokens(model_params(h));
+    const int tile = hswa_cross_tile_tokens(model_params(h));
+    // Blocks of one Q tile, two per SM, when no request has more rows than that: two chains of loads, MMAs and softmax run
+    // beside one another (32 requests of 4 tokens, 4096 to 32768 states, 64 / 8 heads: 363 us, blocks of two tiles 428).
+    // Longer ones share each K / V tile between two Q tiles (16 requests of 2 to 37 tokens, 25 to a tile: 42 us against 46).
+    c.q_tiles = max_q_len <= tile ? 1 : 2;
+    const int tokens = c.q_tiles * tile;
     c.row_tiles = (int)(((int64_t)max_q_len + tokens - 1) / tokens);
     const int64_t blocks = (int64_t)c.row_tiles * h->cfg.num_kv_heads * batch;
-    const int64_t want = (h->num_sms + blocks - 1) / blocks, most = (max_ctx_len + 511) / 512;  // one wave of blocks
+    const int64_t wave = (c.q_tiles == 1 ? 2 : 1) * (int64_t)h->num_sms;
+    const int64_t want = (wave + blocks - 1) / blocks, most = (max_ctx_len + 511) / 512;  // one wave of blocks
     int64_t slices = want < most ? want : most;
     if (slices < 1) slices = 1;
     c.slice_len = (int)((((int64_t)max_ctx_len + slices - 1) / slices + 127) / 128 * 128);
@@ -741,7 +747,7 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
   CUtensorMap tm, tm_q;
   if ((st = make_pool_map(h, layer, &tm)) != HSWA_OK) return st;
   if ((st = make_rows_map(h, q, h->cfg.num_q_heads, b->total_q, hswa_cross_tile_tokens(t.m), &tm_q, h->group)) != HSWA_OK) return st;
-  if (hswa_launch_cross_tc(tm, tm_q, t, pl.row_tiles, s) != cudaSuccess) return HSWA_ERR_CUDA;
+  if (hswa_launch_cross_tc(tm, tm_q, t, pl.row_tiles, pl.q_tiles, s) != cudaSuccess) return HSWA_ERR_CUDA;
   if (pl.slices > 1) {
     const CrossParams p = {t.m, out, lse, b->total_q, b->q_indptr ? b->q_indptr + b->batch : nullptr, pl.slices, part_o, part_ml};
     if (hswa_launch_cross_combine(p, s) != cudaSuccess) return HSWA_ERR_CUDA;

@@ -183,11 +183,11 @@ cudaError_t hswa_launch_decode(const hswa_handle* h, const CUtensorMap& tm_pool,
 cudaError_t hswa_launch_combine(const DecodeParams& p, bool cross, cudaStream_t s);
 // Cross attention, one token per request: the streaming decode kernel without a new token
 cudaError_t hswa_launch_decode_cross(const CUtensorMap& tm_pool, const DecodeParams& p, cudaStream_t s);
-// Cross attention, any number of tokens per request: the tile kernel, two Q tiles of hswa_cross_tile_tokens tokens (the box
-// height of tm_q) per block, and the join of its key slices
+// Cross attention, any number of tokens per request: the tile kernel, one or two Q tiles of hswa_cross_tile_tokens tokens (the
+// box height of tm_q) per block, and the join of its key slices
 int hswa_cross_tile_tokens(const ModelParams& m);
 cudaError_t hswa_launch_cross_tc(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const PrefillParams& p, int row_tiles,
-                                 cudaStream_t s);
+                                 int q_tiles, cudaStream_t s);
 cudaError_t hswa_launch_cross_combine(const CrossParams& p, cudaStream_t s);
 // Eviction: accumulated attention weights, choice of the kept positions, compaction
 int hswa_attn_weights_tile_tokens(const ModelParams& m, int max_q_len);  // tokens per Q tile (box height of tm_q)

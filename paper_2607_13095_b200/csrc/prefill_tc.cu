@@ -35,15 +35,16 @@ constexpr int PG = 64;                // page size
 constexpr int HALF_BYTES = 128 * 128; // [128 rows][128 B]: one 64-element half of a 128-row tile
 constexpr int TILE_BYTES = 2 * HALF_BYTES;
 constexpr int KV_STAGES = 2;
-constexpr int NUM_THREADS = 384;  // 8 softmax warps + producer + one MMA issuer per Q tile + the patch warp
+constexpr int tile_threads(int q_tiles) { return (4 * q_tiles + 4) * 32; }  // softmax warps + producer, two MMA issuers, patch warp
+constexpr int NUM_THREADS = tile_threads(2);
 // Registers per thread after the roles have split; the sum over the block must not pass what the launch gave
 // (384 x 168), or the softmax warps' request would never be granted: checked against the compiled kernel before launch.
 constexpr int REGS_SERVICE = 56, REGS_SOFTMAX = 224;
+constexpr int REGS_SERVICE_ONE = 80, REGS_SOFTMAX_ONE = 176;  // blocks of one Q tile, two per SM: 256 x 128 at launch
 
 // shared memory map (offsets from a 1024-byte aligned base)
-constexpr int OFF_Q = 0;                                  // 2 Q tiles
-constexpr int OFF_K = OFF_Q + 2 * TILE_BYTES;             // the K ring, then the V ring (both `stages` tiles deep)
-constexpr int tile_kernel_smem(int stages) { return OFF_K + 2 * stages * TILE_BYTES + 256; }  // + barriers and flags
+constexpr int OFF_Q = 0;  // the Q tiles, then the K ring, then the V ring (both `stages` tiles deep)
+constexpr int tile_kernel_smem(int stages, int q_tiles = 2) { return (q_tiles + 2 * stages) * TILE_BYTES + 256; }  // + barriers and flags
 
 constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
 constexpr uint32_t IDESC_PV = IDESC_S | (1u << 16);  // B (= V) is MN-major: [key][d] with d contiguous
@@ -225,8 +226,9 @@ __device__ __forceinline__ void linger_after_error(const int32_t* err) {
 // MODE_CROSS turns it into cross attention to cached encoder states (hswa_cross_attn): every cached key is visible to every
 // row, so the (token, head) rows of a GQA group are interchangeable, and a Q tile takes 128 / G tokens x the G query heads of
 // one KV head; the two tiles of a block follow one another in the request's tokens.  The keys may be cut into slices
-// (blockIdx.x / row tiles), which leave partials like the prefix stage's.  A block whose tokens fit one Q tile runs with
-// one MMA issuer and one softmax group.  8 requests, 257 to 512 tokens, up to 8192 states, 64 / 8 heads: 354 us = 990 TFLOP/s
+// (blockIdx.x / row tiles), which leave partials like the prefix stage's.  A block of two Q tiles whose
+// tokens fit one runs with one MMA issuer and one softmax group; NQ = 1 is for batches whose requests all do: half the
+// threads, shared memory (one K and one V stage) and TMEM columns, so that an SM holds two blocks.  8 requests, 257 to 512 tokens, up to 8192 states, 64 / 8 heads: 354 us = 990 TFLOP/s
 // under a sustained load (1136 in short bursts), 53 % of the tensor pipe; the warp-level kernel took 2137 us.
 enum { MODE_PREFILL = 0, MODE_PREFIX = 1, MODE_CROSS = 2 };
 // Does cached tile j (of nA) of a request with ctx cached tokens hold rows that no row of the block can see?  On a
@@ -237,8 +239,9 @@ __device__ __forceinline__ bool v_tile_needs_patch(int is_swa, int ctx, int j) {
 // STAGES = depth of the K and of the V tile ring: 2 for prefill; 1 for the shared-prefix stage, whose block then leaves
 // room on its SM for a block of the suffix decode kernel that streams beside it.
 // DH = head dim; a tile keeps room for two 64-element halves whatever DH is.
-template <int MODE, int STAGES, int DH = HD>
-__global__ void __launch_bounds__(NUM_THREADS, 1)
+// NQ = Q tiles per block; 1 only for cross attention.
+template <int MODE, int STAGES, int DH = HD, int NQ = 2>
+__global__ void __launch_bounds__(tile_threads(NQ), NQ == 1 ? 2 : 1)
 prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_constant__ CUtensorMap tm_q,
                   const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const PrefillParams p, const int max_tiles) {  // tiles b < max_tiles only
@@ -249,6 +252,11 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
   constexpr int HALVES = DH / 64;
   static_assert(DH == HD || CROSS, "other head dims only for cross attention");
   constexpr uint32_t IDESC_O = (IDESC_PV & ~(0x3fu << 17)) | ((uint32_t)(DH >> 3) << 17);
+  static_assert(NQ == 2 || (NQ == 1 && CROSS), "one Q tile only for cross attention");
+  constexpr int THREADS = (4 * NQ + 4) * 32, SERVICE = 4 * NQ;  // the first service warp
+  constexpr int REGS_ROWS = NQ == 1 ? REGS_SOFTMAX_ONE : REGS_SOFTMAX, REGS_OTHER = NQ == 1 ? REGS_SERVICE_ONE : REGS_SERVICE;
+  constexpr int TM_O = NQ * 128, TM_COLS = NQ * 256;  // TMEM: S of each Q tile, then O of each
+  constexpr int OFF_K = OFF_Q + NQ * TILE_BYTES;
   constexpr int OFF_V = OFF_K + STAGES * TILE_BYTES;
   constexpr int OFF_STATE = OFF_V + STAGES * TILE_BYTES;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + OFF_STATE);                     // [NUM_BARS]
@@ -262,7 +270,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int pair = blockIdx.x, kh = blockIdx.y;
   int r, b, t0, n, ctx, head, h0, page_off = 0;
-  int tok_tile = 0, nq_tiles = 2, slice = 0;  // CROSS: tokens per Q tile, Q tiles with tokens, key slice
+  int tok_tile = 0, nq_tiles = NQ, slice = 0;  // CROSS: tokens per Q tile, Q tiles with tokens, key slice
   TileSeq seq;
   if constexpr (PREFIX) {
     // the suffix decode kernel that follows on the stream reads nothing this kernel writes before its own
@@ -315,8 +323,8 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     head = 0;
     h0 = kh * M.G;
     tok_tile = BM / M.G;
-    if (b * 2 * tok_tile >= n) return;  // uniform for the block
-    nq_tiles = (b * 2 + 1) * tok_tile < n ? 2 : 1;
+    if (b * NQ * tok_tile >= n) return;  // uniform for the block
+    nq_tiles = NQ == 2 && (b * 2 + 1) * tok_tile < n ? 2 : 1;
     const int tile_begin = slice * p.prefix_tiles_per_split;
     ctx = max(0, min(len, p.max_ctx_len) - tile_begin * BN);  // keys from this slice's first tile to the end
     seq.nA = min(p.prefix_tiles_per_split, (ctx + BN - 1) / BN);
@@ -325,9 +333,9 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     page_off = BN / M.P * tile_begin;
     if (seq.nA <= 0) {
       // no key here: zeros (no states at all), or a partial that the join passes over
-      const int rows = min(2 * tok_tile, n - b * 2 * tok_tile) * M.G;
-      for (int row = threadIdx.x; row < rows; row += NUM_THREADS) {
-        const int64_t orow = (int64_t)(t0 + b * 2 * tok_tile + row / M.G) * M.Hq + h0 + row % M.G;
+      const int rows = min(NQ * tok_tile, n - b * NQ * tok_tile) * M.G;
+      for (int row = threadIdx.x; row < rows; row += THREADS) {
+        const int64_t orow = (int64_t)(t0 + b * NQ * tok_tile + row / M.G) * M.Hq + h0 + row % M.G;
         if (p.max_splits > 1) {
           p.part_ml[orow * p.max_splits + slice] = make_float2(-INFINITY, 0.f);
           continue;
@@ -414,8 +422,8 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     mbar_init(bar(BAR_VPATCH + 1), 1);
     mbar_fence_init();
   }
-  if (warp == 8) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(512)
+  if (warp == SERVICE) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(TM_COLS)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -426,9 +434,9 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
 
   // Registers move from the service warps (one warpgroup: producer, two MMA issuers and the patch warp; the
   // exchange is made by whole warpgroups) to the softmax warps, whose threads hold a row of 128 scores:
-  // 8 x 32 x 224 + 4 x 32 x 56 = 384 x 168.  Each role's branch changes its own allotment.
-  if (warp == 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_SERVICE) : "memory");
+  // 8 x 32 x 224 + 4 x 32 x 56 = 384 x 168 (one Q tile: 4 x 32 x 176 + 4 x 32 x 80 = 256 x 128).  Each role's branch changes its own allotment.
+  if (warp == SERVICE) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER) : "memory");
     // ======================= TMA producer =======================
     if (lane == 0) {
       tma_prefetch_desc(&tm_pool);
@@ -439,7 +447,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       for (int i = 0; i < nq_tiles; ++i)
         for (int hf = 0; hf < HALVES; ++hf) {
           if constexpr (CROSS)  // box {64, G heads, tok_tile tokens} over q [T][Hq][D]
-            tma_load_3d(sbase + OFF_Q + i * TILE_BYTES + hf * HALF_BYTES, &tm_q, bar(BAR_Q), hf * 64, h0, t0 + (2 * b + i) * tok_tile);
+            tma_load_3d(sbase + OFF_Q + i * TILE_BYTES + hf * HALF_BYTES, &tm_q, bar(BAR_Q), hf * 64, h0, t0 + (NQ * b + i) * tok_tile);
           else if constexpr (PREFIX)  // box {64, 8 heads, 16 requests} over q [B][Hq][D]
             tma_load_3d(sbase + OFF_Q + i * TILE_BYTES + hf * HALF_BYTES, &tm_q, bar(BAR_Q), hf * 64, h0, r + 16 * i);
           else
@@ -488,7 +496,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       // slots never written, past the ring's last page, or older than the first row's window, which a ring seeded
       // with a window only never filled) may hold anything, patterns of NaN included.  Their probabilities are exactly
       // 0, but 0 x NaN would still reach the output through the PV MMA (paper Sec. 3.1.3: attention must not be
-      // affected by invalid slots).  The V half of such a tile lands on a barrier that the patch warp (warp 11)
+      // affected by invalid slots).  The V half of such a tile lands on a barrier that the patch warp (the last one)
       // waits on; that warp zeroes the dead rows and only then hands the tile to the MMA issuers.
       const bool patch = !PREFIX && j < seq.nA && v_tile_needs_patch(p.is_swa, ctx, j);
       if (j < seq.nA) {
@@ -534,11 +542,11 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       }
       ok = __shfl_sync(0xffffffffu, ok, 0);
     }
-  } else if (warp == 9 || warp == 10) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_SERVICE) : "memory");
+  } else if (warp == SERVICE + 1 || warp == SERVICE + 2) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER) : "memory");
     // ======================= MMA issuer =======================
     // The whole warp walks the loop converged (waits, descriptor arithmetic); one elected lane issues.
-    if (!CROSS || warp - 9 < nq_tiles) {
+    if (!CROSS || warp - SERVICE - 1 < nq_tiles) {
       bool ok = mbar_wait(bar(BAR_Q), 0);
       const uint64_t dQ0 = smem_desc(sbase + OFF_Q, 16), dQ1 = smem_desc(sbase + OFF_Q + TILE_BYTES, 16);
       const uint64_t dK0 = smem_desc(sbase + OFF_K, 16), dV0 = smem_desc(sbase + OFF_V, HALF_BYTES);
@@ -564,7 +572,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
         if (elect_one()) {
 #pragma unroll
           for (int q = 0; q < KSTEPS; ++q)
-            tc_mma_ts(tmem + 256 + i * 128, tp + q * 8, desc_advance(dv, q * 2048), IDESC_O, !(first && part == 0 && q == 0));
+            tc_mma_ts(tmem + TM_O + i * 128, tp + q * 8, desc_advance(dv, q * 2048), IDESC_O, !(first && part == 0 && q == 0));
         }
         __syncwarp();
       };
@@ -573,7 +581,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       // the tensor queue is the one that keeps the tiles half a step apart, while each issuer polls the
       // mbarriers of its next group during the other issuer's turn.  A warp leaves the loop only right after
       // passing the token, and passes it whenever it finds the abort flag set, so neither can wait forever.
-      const int i = warp - 9;
+      const int i = warp - SERVICE - 1;
       const int tok_in = i == 0 ? 2 : 1, tok_out = i == 0 ? 1 : 2;
       auto token_wait = [&]() {
         if (CROSS && nq_tiles == 1) return;  // a single issuer has every turn
@@ -630,8 +638,8 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       if (elect_one()) tc_commit(bar(BAR_OFINAL + i));
       __syncwarp();
     }
-  } else if (warp == 11) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_SERVICE) : "memory");
+  } else if (warp == SERVICE + 3) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER) : "memory");
     // ======================= patch warp =======================
     // (see the producer: dead rows of a cached V tile are zeroed between the tile's arrival and its hand-over)
     if constexpr (!PREFIX) {
@@ -667,7 +675,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX) : "memory");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_ROWS) : "memory");
     // ======================= softmax warps =======================
     // 4 warps per Q tile: TMEM lane = row = thread, which holds all 128 scores of its row in registers, so row
     // maxima and sums need no exchange.  P is written to TMEM in four quarters of 32 keys and posted to the MMA
@@ -678,7 +686,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     const int rr = quad * 32 + lane;            // row in the tile = TMEM lane
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     const uint32_t tS = tmem + lane_addr + i * 128;
-    const uint32_t tO = tmem + lane_addr + 256 + i * 128;
+    const uint32_t tO = tmem + lane_addr + TM_O + i * 128;
     const bool here = !CROSS || i < nq_tiles;   // (a Q tile without tokens has no work)
     const int ri = b * BM + rr;                 // chunk-relative row
     const int pos = ctx + ri;                   // absolute position
@@ -828,7 +836,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     if (!ok && lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, b, 40 + i);
     tc_fence_after();
     const float l_tot = l_run;
-    const int tok = CROSS ? (2 * b + i) * tok_tile + rr / M.G : 0;  // CROSS: this row's token and its output row
+    const int tok = CROSS ? (NQ * b + i) * tok_tile + rr / M.G : 0;  // CROSS: this row's token and its output row
     const bool tok_ok = CROSS && here && rr < tok_tile * M.G && tok < n;
     const int64_t cross_row = CROSS ? (int64_t)(t0 + tok) * M.Hq + h0 + rr % M.G : 0;
     if (PREFIX || (CROSS && p.max_splits > 1)) {
@@ -891,9 +899,9 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
   linger_after_error(p.err);
   tc_fence_before();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == SERVICE) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TM_COLS) : "memory");
   }
   if (traced && threadIdx.x == 0) {
     unsigned sm;
@@ -1599,14 +1607,14 @@ prefill_swa_stream_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid
   }
 }
 
-// The role split asks for 8 x 32 x REGS_SOFTMAX + 4 x 32 x REGS_SERVICE registers; a block that was launched with
+// The role split asks for `regs` registers (8 x 32 x REGS_SOFTMAX + 4 x 32 x REGS_SERVICE); a block that was launched with
 // fewer would wait for them for ever.
 template <typename Kernel>
-cudaError_t check_register_budget(Kernel kernel, int threads) {
+cudaError_t check_register_budget(Kernel kernel, int threads, int regs = 256 * REGS_SOFTMAX + 128 * REGS_SERVICE) {
   cudaFuncAttributes attr;
   cudaError_t e = cudaFuncGetAttributes(&attr, kernel);
   if (e != cudaSuccess) return e;
-  return attr.numRegs * threads < 128 * REGS_SERVICE + 256 * REGS_SOFTMAX ? cudaErrorLaunchOutOfResources : cudaSuccess;
+  return attr.numRegs * threads < regs ? cudaErrorLaunchOutOfResources : cudaSuccess;
 }
 
 cudaError_t launch_stream(const CUtensorMap& tm_q, const CUtensorMap& tm_k16, const CUtensorMap& tm_v16, const CUtensorMap& tm_out,
@@ -1680,23 +1688,32 @@ cudaError_t hswa_launch_decode_prefix(const CUtensorMap& tm_pool, const CUtensor
   return cudaGetLastError();
 }
 
-// Cross attention: grid (row tiles x key slices, KV heads, requests).  tm_q has box {64, G heads, 128 / G tokens} over q
-// [T][Hq][D]; p carries the host's bounds, the slice plan and, for more than one slice, the partial buffers.
+// Cross attention: grid (row tiles x key slices, KV heads, requests), NQ Q tiles per row tile.  tm_q has box {64, G heads,
+// 128 / G tokens} over q [T][Hq][D]; p carries the host's bounds, the slice plan and, for more than one slice, the partial
+// buffers.
 int hswa_cross_tile_tokens(const ModelParams& m) { return BM / m.G; }
-template <int DH>
+template <int DH, int NQ>
 static cudaError_t launch_cross_t(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const PrefillParams& p, int row_tiles, cudaStream_t s) {
-  constexpr int SMEM_BYTES = tile_kernel_smem(KV_STAGES);
-  auto kern = prefill_tc_kernel<MODE_CROSS, KV_STAGES, DH>;
+  constexpr int STAGES = NQ == 1 ? 1 : KV_STAGES, THREADS = tile_threads(NQ);
+  constexpr int SMEM_BYTES = tile_kernel_smem(STAGES, NQ);
+  auto kern = prefill_tc_kernel<MODE_CROSS, STAGES, DH, NQ>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
   if (e != cudaSuccess) return e;
-  static const cudaError_t budget = check_register_budget(kern, NUM_THREADS);
+  if (NQ == 1) {
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    if (e != cudaSuccess) return e;
+  }
+  static const cudaError_t budget = NQ == 1 ? check_register_budget(kern, THREADS, 128 * (REGS_SOFTMAX_ONE + REGS_SERVICE_ONE)) : check_register_budget(kern, THREADS);
   if (budget != cudaSuccess) return budget;
   dim3 grid(row_tiles * p.max_splits, p.m.Hkv, p.b.B);
-  kern<<<grid, NUM_THREADS, SMEM_BYTES, s>>>(tm_pool, tm_q, tm_pool, tm_pool, p, row_tiles);
+  kern<<<grid, THREADS, SMEM_BYTES, s>>>(tm_pool, tm_q, tm_pool, tm_pool, p, row_tiles);
   return cudaGetLastError();
 }
-cudaError_t hswa_launch_cross_tc(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const PrefillParams& p, int row_tiles, cudaStream_t s) {
-  return p.m.D == 128 ? launch_cross_t<128>(tm_pool, tm_q, p, row_tiles, s) : launch_cross_t<64>(tm_pool, tm_q, p, row_tiles, s);
+cudaError_t hswa_launch_cross_tc(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const PrefillParams& p, int row_tiles, int q_tiles,
+                                 cudaStream_t s) {
+  if (q_tiles == 1)
+    return p.m.D == 128 ? launch_cross_t<128, 1>(tm_pool, tm_q, p, row_tiles, s) : launch_cross_t<64, 1>(tm_pool, tm_q, p, row_tiles, s);
+  return p.m.D == 128 ? launch_cross_t<128, 2>(tm_pool, tm_q, p, row_tiles, s) : launch_cross_t<64, 2>(tm_pool, tm_q, p, row_tiles, s);
 }
 
 // Streaming SWA kernel (GQA group of 8, window 128): every token from the 129th of each request on.  tm_q has box

@@ -156,6 +156,18 @@ def test_cross_bounds_wider_than_the_batch():
     check_cross(c, *run_cross(c, max_ctx=3000, max_q=7))
 
 
+@pytest.mark.parametrize("d", SHAPES, ids=str)
+def test_cross_requests_of_one_tile(d):
+    """No request has more rows than a tile: two blocks to an SM, many key tiles through one stage, with and without slices."""
+    rng = np.random.default_rng(43)
+    most = 128 // d.group
+    for B, top in ((2, 5000), (40, 700), (90, 300)):
+        n = np.minimum(rng.integers(0, most + 1, B), 16)
+        n[0] = min(most, 37)
+        c = Case(d, np.where(rng.random(B) < 0.2, 0, rng.integers(1, top, B)), n, seed=44)
+        check_cross(c, *run_cross(c))
+
+
 def no_rings(d, B):
     return torch.zeros((B, d.ring_pages), dtype=torch.int32, device="cuda"), torch.zeros((B,), dtype=torch.int32, device="cuda")
 
