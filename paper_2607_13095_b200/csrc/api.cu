@@ -817,7 +817,7 @@ hswa_status hswa_evict_select(hswa_handle* h, int32_t batch, const int32_t* ctx_
   p.keep_idx = keep_idx;
   p.kept_len = kept_len;
   p.err = h->err;
-  return hswa_launch_evict_select(p, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+  return hswa_launch_evict_select(p, h->num_sms, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
 }
 
 hswa_status hswa_evict_compact(hswa_handle* h, const hswa_layer* layer, const hswa_batch* b, const int32_t* keep_idx,

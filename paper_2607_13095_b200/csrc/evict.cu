@@ -21,7 +21,7 @@ __device__ __forceinline__ uint32_t rank_key(float w, int j, int ctx, int first,
 //
 // Counting every key of a long row in shared memory would cost more than reading it (an atomic per key, several keys of a
 // warp in one bin), so long rows are sampled first: eight keys per thread, spread over the row, say below which key nothing
-// can matter, with a margin of four standard deviations.  One pass then collects the keys from that one on in shared memory,
+// can matter, with a margin of three standard deviations and more.  One pass then collects the keys from that one on in shared memory,
 // in any order (warps do not wait for one another), and the threshold is found among them: the weights are read once.  The
 // sample decides nothing: when the list turns out to hold fewer keys than are to stay, or does not fit, and on short rows,
 // the top digit is counted over the whole row and the list begins at the digit found.  What stays is marked in a bitmap of
@@ -124,9 +124,12 @@ __device__ __forceinline__ uint32_t find_digit(SelectShared<T>& sh, int bins, ui
   return sh.digit;
 }
 
+// Of the sample's keys, `share` should be among those that stay: the rank in the sample of a key that is below the threshold.
+__host__ __device__ __forceinline__ float sample_rank(float share) { return share + 3.f * sqrtf(share) + 8.f; }
+
 // T threads; CQ quads of keys per thread in flight while as many are looked at.
 template <int T, int CQ>
-__global__ void __launch_bounds__(T, T == 256 ? 4 : 1) evict_select_kernel(const SelectParams p, const int capacity, const int words) {
+__global__ void __launch_bounds__(T, T == 256 ? 4 : CQ == 4 ? 2 : 1) evict_select_kernel(const SelectParams p, const int capacity, const int words) {
   extern __shared__ __align__(16) uint32_t list[];  // [capacity] keys, [capacity] positions, [2] padded arrays of `words`
   __shared__ SelectShared<T> sh;
   const int row = blockIdx.x, kh = row % p.Hkv, r = row / p.Hkv;
@@ -279,7 +282,7 @@ __global__ void __launch_bounds__(T, T == 256 ? 4 : 1) evict_select_kernel(const
   if (quads >= 4 * T) {
     const int step = quads / (2 * T);
     const float share = 8.f * T * (float)keep / (float)ctx;  // of the sample's 8 T keys, those that would stay
-    uint32_t rank = (uint32_t)(share + 4.f * sqrtf(share) + 8.f);
+    uint32_t rank = (uint32_t)sample_rank(share);
     if (rank <= 4 * T) {  // at most half of it
       uint32_t k[2][4], in[2];
 #pragma unroll
@@ -596,32 +599,52 @@ __global__ void __launch_bounds__(256) evict_compact_kernel(const CompactParams 
 
 }  // namespace
 
-template <int T, int CQ>
-static cudaError_t launch_select_t(const SelectParams& p, int64_t rows, int capacity, int words, cudaStream_t s) {
-  const int smem = (capacity + map_at(words)) * 8;
-  cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<T, CQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
-  evict_select_kernel<T, CQ><<<(unsigned)rows, T, smem, s>>>(p, capacity, words);
-  return cudaGetLastError();
-}
+namespace {
+// Shared memory of a block: the list and the bitmap of positions with a number per word.
+struct SelectRoom {
+  int capacity, words;
+  int bytes() const { return (capacity + map_at(words)) * 8; }
+};
 
-cudaError_t hswa_launch_evict_select(const SelectParams& p, cudaStream_t s) {
-  if (p.B == 0) return cudaSuccess;
-  const int64_t rows = (int64_t)p.B * p.Hkv;
-  // Room in the list for what stays and for what the sample's margin and the threshold's bin bring with them (1.2 to 1.4
-  // times what stays).  Long rows: one block per SM with as many loads in flight as its registers hold; the data of a load
-  // in flight needs room in L1, which shares its memory with this one: 213 KB of shared memory instead of 195 or less
-  // took 128 rows of up to 262144 positions from 54 to 70 us.  Short rows: four blocks per SM, whose steps overlap (43 us on
-  // 512 rows of up to 32768 positions; three blocks with more room in their lists 48 us).
-  const bool is_long = p.max_ctx_len > 32768;
-  int64_t capacity = (int64_t)p.max_keep + p.max_keep / 2 + (is_long ? 2048 : 1024);
+// Room in the list for what stays and for what the threshold's bin brings with it, and for what a sample of 8 T keys brings
+// with it when its rank is four standard deviations off.  A list that does not fit costs passes over the row.
+SelectRoom select_room(const SelectParams& p, int T) {
+  SelectRoom room;
+  const float share = 8.f * T * (float)p.max_keep / (float)(p.max_ctx_len > 0 ? p.max_ctx_len : 1), rank = sample_rank(share);
+  int64_t capacity = (int64_t)p.max_keep + p.max_keep / 2 + (T == 512 ? 2048 : 1024);
+  const int64_t sampled = (int64_t)((rank + 4.f * sqrtf(rank)) * (float)p.max_ctx_len / (8.f * T));
+  if (rank <= 4 * T && capacity < sampled) capacity = sampled;
   if (capacity > p.max_ctx_len) capacity = p.max_ctx_len;
   if (capacity > 18432) capacity = 18432;
-  capacity = (capacity + 3) / 4 * 4;
-  int words = (p.max_ctx_len + 31) / 32;
-  if (words > 4096) words = 4096;
-  if (is_long) return launch_select_t<512, 8>(p, rows, (int)capacity, words, s);
-  return launch_select_t<256, 4>(p, rows, (int)capacity, words, s);
+  room.capacity = (int)((capacity + 3) / 4 * 4);
+  room.words = (p.max_ctx_len + 31) / 32;
+  if (room.words > 4096) room.words = 4096;
+  return room;
+}
+
+template <int T, int CQ>
+cudaError_t launch_select_t(const SelectParams& p, int64_t rows, cudaStream_t s) {
+  const SelectRoom room = select_room(p, T);
+  cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<T, CQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, room.bytes());
+  if (e != cudaSuccess) return e;
+  evict_select_kernel<T, CQ><<<(unsigned)rows, T, room.bytes(), s>>>(p, room.capacity, room.words);
+  return cudaGetLastError();
+}
+}  // namespace
+
+cudaError_t hswa_launch_evict_select(const SelectParams& p, int num_sms, cudaStream_t s) {
+  if (p.B == 0) return cudaSuccess;
+  const int64_t rows = (int64_t)p.B * p.Hkv;
+  // Blocks.  More rows than SMs, up to 32768 positions: four small blocks per SM, whose steps overlap (512 rows, 2048 kept:
+  // 34 us; two larger blocks 41).  Else two blocks of 512 threads per SM, where their lists leave L1 the room that the data of
+  // loads in flight needs (512 rows of 30000 to 60000, 4096 kept: 66 us; four small blocks 76, one block 99), or one where there
+  // is one row per SM at most (128 rows of 16000 to 32000: 19 us; small blocks 25).  The longest rows and lists: one block per
+  // SM with as many loads in flight as its registers hold (128 rows of 65536 to 262144, 8191 kept: 54 us; with half of them
+  // in flight 59; with 213 KB of shared memory instead of 195 or less, so that L1 is short of room, 70).
+  if (rows > num_sms && p.max_ctx_len <= 32768) return launch_select_t<256, 4>(p, rows, s);
+  const bool two_fit = select_room(p, 512).bytes() + (int)sizeof(SelectShared<512>) <= 96 * 1024;
+  if (rows > num_sms ? two_fit : p.max_ctx_len <= 131072) return launch_select_t<512, 4>(p, rows, s);
+  return launch_select_t<512, 8>(p, rows, s);
 }
 
 cudaError_t hswa_launch_evict_compact(const CompactParams& p, int num_sms, cudaStream_t s) {

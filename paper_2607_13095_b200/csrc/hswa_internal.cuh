@@ -193,7 +193,7 @@ cudaError_t hswa_launch_cross_combine(const CrossParams& p, cudaStream_t s);
 int hswa_attn_weights_tile_tokens(const ModelParams& m, int max_q_len);  // tokens per Q tile (box height of tm_q)
 cudaError_t hswa_launch_attn_weights(const CUtensorMap& tm_pool, const CUtensorMap& tm_q, const WeightsParams& p, int num_sms,
                                      cudaStream_t s);
-cudaError_t hswa_launch_evict_select(const SelectParams& p, cudaStream_t s);
+cudaError_t hswa_launch_evict_select(const SelectParams& p, int num_sms, cudaStream_t s);
 cudaError_t hswa_launch_evict_compact(const CompactParams& p, int num_sms, cudaStream_t s);
 // SWA layers whose window fits shared memory: one block per (request, KV head) over a compact copy of the window
 bool hswa_ring_compact_supported(const ModelParams& m, int nq);

@@ -359,6 +359,19 @@ def test_select(first, last, kind):
     check_select(w, CTX, [3] * len(CTX), 17, first, last, max_ctx=5003)
 
 
+@pytest.mark.parametrize("batch,lo,hi,keep", [(100, 0, 3000, 300), (90, 1000, 9000, 2048), (100, 3000, 40000, 900), (85, 30000, 60000, 4096),
+                                              (80, 100000, 140000, 512), (80, 50000, 70000, 12000), (60, 2000, 30000, 64)])
+@pytest.mark.parametrize("kind", ["random", "skewed"])
+def test_select_more_rows_than_sms(batch, lo, hi, keep, kind):
+    """And just fewer: blocks of either size, several to an SM or one; weights spread evenly and as attention spreads them."""
+    rng = np.random.default_rng(12)
+    w = rng.random((batch, 2, hi + 1), dtype=np.float32)
+    if kind == "skewed":
+        w = np.exp(np.float32(9) * w) * (rng.random(w.shape, dtype=np.float32) < 0.7)
+    ctx = rng.integers(lo, hi + 1, batch).astype(np.int32)
+    check_select(w, ctx, np.where(rng.random(batch) < 0.2, keep // 3, keep), keep, 4, 64, hi)
+
+
 @pytest.mark.parametrize("ctx", [16383, 16384, 16385, 49152, 65536, 200001, 262144, 300000])
 def test_select_long(ctx):
     rng = np.random.default_rng(10)
