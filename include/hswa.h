@@ -251,8 +251,9 @@ hswa_status hswa_prefill_attn(hswa_handle* h, const hswa_layer* layer, const hsw
  * not matter and those of out and lse are left as they were.  Probabilities enter the PV product as bf16; row sums and
  * lse are taken over the fp32 values.  Workspace: hswa_cross_workspace_need bytes (0: none needed), else
  * HSWA_ERR_WORKSPACE.  The block table must cover max_ctx_len and the layer must not be an SWA layer
- * (HSWA_ERR_INVALID_ARG); max_ctx_len is at most 2^30 (HSWA_ERR_UNSUPPORTED, the need is then 0).  A request longer than
- * max_ctx_len or max_q_len is recorded as HSWA_ERR_BOUNDS (index -1 / -2) and what the bounds cover is computed.
+ * (HSWA_ERR_INVALID_ARG); max_ctx_len is at most 2^30, for single tokens 65535 * 4096 (HSWA_ERR_UNSUPPORTED, the need is
+ * then 0).  A request longer than max_ctx_len or max_q_len is recorded as HSWA_ERR_BOUNDS (index -1 / -2) and what the
+ * bounds cover is computed.
  *
  * This call and the eviction calls below refuse a current device other than the handle's (HSWA_ERR_INVALID_ARG).
  *

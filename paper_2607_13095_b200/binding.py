@@ -359,10 +359,15 @@ def hswa_evict_compact(h: Handle, layer: Layer, batch: Batch, keep_idx: torch.Te
     B, heads, max_keep = keep_idx.shape
     dst_batch, dst_blocks = dst_block_table.shape
     assert B == dst_batch == batch.batch and heads == h.cfg.num_kv_heads and kept_len.numel() >= B
-    assert all(w is None or (w.dim() == 3 and w.shape[0] == B and w.shape[1] == heads) for w in (weights, weights_out))
+    stride = out_stride = 0
+    if weights is not None:
+        w_batch, w_heads, stride = weights.shape
+        assert w_batch == B and w_heads == heads
+    if weights_out is not None:
+        w_batch, w_heads, out_stride = weights_out.shape
+        assert w_batch == B and w_heads == heads
     _check(load().hswa_evict_compact(h.ptr, C.byref(layer.c), C.byref(batch.c), _ptr(keep_idx), _ptr(kept_len), max_keep,
-                                     _ptr(dst_block_table), dst_blocks, _ptr(weights), 0 if weights is None else weights.shape[2],
-                                     _ptr(weights_out), 0 if weights_out is None else weights_out.shape[2], _stream()),
+                                     _ptr(dst_block_table), dst_blocks, _ptr(weights), stride, _ptr(weights_out), out_stride, _stream()),
            "hswa_evict_compact")
 
 

@@ -29,7 +29,7 @@ __device__ __forceinline__ uint32_t rank_key(float w, int j, int ctx, int first,
 // later passes read the row.
 //
 // Bound by what one SM can load -- a row is one block's -- and by the chain of block-wide steps around it.  512 rows of 1024 to
-// 32768 weights: 43 us for 41 MB; 128 rows of 65536 to 262144: 54 us for 83 MB, of which the longest row's 1 MB takes 32 us.
+// 32768 weights: 36 us for 41 MB (43 among other kernels); 128 rows of 65536 to 262144: 53 us for 83 MB, of which the longest row's 1 MB takes 32 us.
 constexpr int SEL_BINS = 2048;
 constexpr int SEL_QUADS = 4;  // quads of keys a thread has in hand in a step of the whole block
 
@@ -607,18 +607,21 @@ struct SelectRoom {
 };
 
 // Room in the list for what stays and for what the threshold's bin brings with it, and for what a sample of 8 T keys brings
-// with it when its rank is four standard deviations off.  A list that does not fit costs passes over the row.
+// with it when its rank is four standard deviations off.  A list that does not fit costs passes over the row: more room than
+// leaves L1 its own is taken only for that (64 rows of 65536 to 262144, 16000 kept: 75 us; at 18432 places 312).
 SelectRoom select_room(const SelectParams& p, int T) {
   SelectRoom room;
   const float share = 8.f * T * (float)p.max_keep / (float)(p.max_ctx_len > 0 ? p.max_ctx_len : 1), rank = sample_rank(share);
   int64_t capacity = (int64_t)p.max_keep + p.max_keep / 2 + (T == 512 ? 2048 : 1024);
   const int64_t sampled = (int64_t)((rank + 4.f * sqrtf(rank)) * (float)p.max_ctx_len / (8.f * T));
+  if (capacity > 18432) capacity = 18432;  // (L1 keeps enough room for loads in flight)
   if (rank <= 4 * T && capacity < sampled) capacity = sampled;
   if (capacity > p.max_ctx_len) capacity = p.max_ctx_len;
-  if (capacity > 18432) capacity = 18432;
-  room.capacity = (int)((capacity + 3) / 4 * 4);
   room.words = (p.max_ctx_len + 31) / 32;
   if (room.words > 4096) room.words = 4096;
+  const int64_t most = (227 * 1024 - (int)sizeof(SelectShared<512>) - 64) / 8 - map_at(room.words) - 4;
+  if (capacity > most) capacity = most;
+  room.capacity = (int)((capacity + 3) / 4 * 4);
   return room;
 }
 

@@ -360,7 +360,8 @@ def test_select(first, last, kind):
 
 
 @pytest.mark.parametrize("batch,lo,hi,keep", [(100, 0, 3000, 300), (90, 1000, 9000, 2048), (100, 3000, 40000, 900), (85, 30000, 60000, 4096),
-                                              (80, 100000, 140000, 512), (80, 50000, 70000, 12000), (60, 2000, 30000, 64)])
+                                              (80, 100000, 140000, 512), (80, 50000, 70000, 12000), (60, 2000, 30000, 64), (6, 100000, 200000, 18000),
+                                              (6, 20000, 50000, 24000)])
 @pytest.mark.parametrize("kind", ["random", "skewed"])
 def test_select_more_rows_than_sms(batch, lo, hi, keep, kind):
     """And just fewer: blocks of either size, several to an SM or one; weights spread evenly and as attention spreads them."""
