@@ -268,9 +268,42 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p)
       tbl = p.b.ring_table + (int64_t)r * M.R;
       n_pages = M.R;
     }
+    if constexpr (CROSS) {
+      // every page of the range counts: a lane per copy (page, K or V, half) of a tile
+      constexpr int COPIES = 2 * HALVES;  // of a page
+      const int of_tile = lane / COPIES, kv = lane / HALVES % 2, hf = lane % HALVES;
+      auto page_of = [&](int t) { return of_tile < PPT && t * PPT + of_tile < n_pages ? tbl[t * PPT + of_tile] : -1; };
+      int next = page_of(0);
+      for (int t = 0; t < n_tiles; ++t) {
+        const int stage = t % NS, page = next, pgi = t * PPT + of_tile;
+        next = page_of(t + 1);
+        if (t >= NS && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars[NS + stage]), ((t / NS) - 1) & 1))) {
+          if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, t, 1);
+          break;
+        }
+        bool mine = of_tile < PPT && pgi < n_pages;
+        if (mine && (page < 0 || page >= p.num_pages)) {
+          record_error(p.err, HSWA_ERR_BOUNDS, r, k_begin / P + pgi, page);
+          mine = false;
+        }
+        const int copies = __popc(__ballot_sync(0xffffffffu, mine));
+        const uint32_t full_bar = smem_u32(&bars[stage]);
+        if (lane == 0) {
+          if (copies == 0)
+            mbar_arrive(full_bar);
+          else
+            mbar_arrive_expect_tx(full_bar, copies * BOX_BYTES);
+        }
+        __syncwarp();
+        if (mine)
+          tma_load_4d(smem_base + stage * STAGE_BYTES + (kv * HALVES + hf) * HALF_BYTES + of_tile * BOX_BYTES, &tm_pool, full_bar, hf * 64, 0,
+                      kv * M.Hkv + kh, page);
+        __syncwarp();
+      }
+    }
     int pid_next = lane < n_pages ? tbl[lane] : 0;
     int pid_cur = 0;
-    for (int t = 0; t < n_tiles; ++t) {
+    for (int t = 0; !CROSS && t < n_tiles; ++t) {
       const int pg0 = t * PPT;
       if ((pg0 & 31) == 0) {
         pid_cur = pid_next;

@@ -157,6 +157,14 @@ def test_cross_bounds_wider_than_the_batch():
 
 
 @pytest.mark.parametrize("d", SHAPES, ids=str)
+@pytest.mark.parametrize("top", [192, 193, 512, 513])
+def test_cross_decode_of_short_states(d, top):
+    """Few requests whose states are one block's: every tile has a stage of its own, or not quite."""
+    c = Case(d, [top, 0, 1, 63, 64, 65, 150, top - 1], [1] * 8, seed=45)
+    check_cross(c, *run_cross(c))
+
+
+@pytest.mark.parametrize("d", SHAPES, ids=str)
 def test_cross_requests_of_one_tile(d):
     """No request has more rows than a tile: two blocks to an SM, many key tiles through one stage, with and without slices."""
     rng = np.random.default_rng(43)
