@@ -8,8 +8,8 @@
 namespace {
 
 constexpr int kMinSplitLen = 256;
-// Cross attention of single tokens: up to this many states are one block's.  Two requests of up to 512 states: 8.9 us by one
-// launch; in two splits 7.7 us on the device, but 10.5 us of the host's time for two launches.
+// Cross attention of single tokens: up to this many states are one block's.  Two requests of up to 512 states: 7.2 us by one
+// launch, 8.2 with the call around it; two launches cost the host alone 10.5.
 constexpr int kUnsplitLen = 512;
 constexpr int kMaxSplitLen = 4096;  // measured on configs 2, 4 and 5: 4096-8192 beat 2048 (fewer block prologues) and 16384 (tail)
 
@@ -72,10 +72,10 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 
 // Keys per split for Full-layer decode: long enough that the partial (m, l, o) traffic stays below one
 // percent of the KV bytes, short enough that the grid fills the machine.
-int plan_split_len(const hswa_handle* h, int batch, int max_ctx_len) {
+int plan_split_len(const hswa_handle* h, int batch, int max_ctx_len, int blocks_per_sm = 4) {
   const long long kv_len = (long long)max_ctx_len + 1;
   int len = kMaxSplitLen;
-  const long long want = 4LL * h->num_sms;
+  const long long want = (long long)blocks_per_sm * h->num_sms;
   while (len > kMinSplitLen && (long long)batch * h->cfg.num_kv_heads * ((kv_len + len - 1) / len) < want) len >>= 1;
   return len;
 }
@@ -145,7 +145,7 @@ bool plan_decode(const hswa_handle* h, int is_swa, int batch, int max_ctx_len, i
 // decode step; anything else goes to the tile kernel, whose key slices fill the machine when the rows alone do not.
 struct CrossPlan {
   bool decode;
-  DecodePlan dec;
+  int split_len;  // single tokens: keys per block
   int q_tiles, row_tiles, slices, slice_len;  // the tile kernel: Q tiles per block, blocks per (request, KV head), key slices
   size_t o_bytes, ml_bytes;
 };
@@ -155,14 +155,19 @@ bool plan_cross(const hswa_handle* h, int batch, int total_q, int max_q_len, int
   if (max_ctx_len > kMaxPositions) return false;
   c.decode = max_q_len == 1;
   if (c.decode) {
-    if (!plan_decode(h, 0, batch, max_ctx_len > 0 ? max_ctx_len - 1 : 0, 0, 1, &c.dec)) return false;
-    if (max_ctx_len <= kUnsplitLen) {  // a second launch costs more than the few tiles that it would spare a block
-      c.dec.split_len = kUnsplitLen;
-      c.dec.grid_splits = c.dec.max_splits = 1;
-      c.dec.o_bytes = c.dec.ml_bytes = 0;
+    const int last = max_ctx_len > 0 ? max_ctx_len - 1 : 0;
+    // As many blocks as an SM holds: two of 128 wide heads, four of 64.  (Twice as many of 128: one request of 32000 states, 64 / 8
+    // heads, 44 us against 33, 16 requests of 500 to 8000 51 against 44; half as many: 27 and 52.  60 requests of 3000 to
+    // 12000, 8 / 1 heads of 64: 25 us with four, 28 with two.)
+    const int per_sm = h->cfg.head_dim == 128 ? 2 : 4;
+    c.split_len = max_ctx_len <= kUnsplitLen ? kUnsplitLen : plan_split_len(h, batch, last, per_sm);
+    c.slices = plan_max_splits(c.split_len, last);
+    if (c.slices > 65535) return false;
+    if (c.slices > 1) {
+      const size_t rows = (size_t)batch * h->cfg.num_q_heads;
+      c.o_bytes = (rows * c.slices * h->cfg.head_dim * sizeof(float) + 255) & ~size_t(255);
+      c.ml_bytes = (rows * c.slices * sizeof(float2) + 255) & ~size_t(255);
     }
-    c.o_bytes = c.dec.o_bytes;
-    c.ml_bytes = c.dec.ml_bytes;
   } else {
     if (batch > 65535 || h->cfg.num_kv_heads > 65535) return false;  // grid extents
     const int tile = hswa_cross_tile_tokens(model_params(h));
@@ -714,9 +719,8 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
     p.q = static_cast<const __nv_bfloat16*>(q);
     p.out = out;
     p.lse = lse;
-    p.split_len = pl.dec.split_len;
-    p.max_splits = pl.dec.max_splits;
-    p.grid_splits = pl.dec.grid_splits;
+    p.split_len = pl.split_len;
+    p.max_splits = p.grid_splits = pl.slices;
     p.nq = 1;
     p.max_ctx_len = b->max_ctx_len;
     p.part_o = part_o;

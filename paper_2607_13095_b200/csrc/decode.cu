@@ -491,9 +491,12 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p)
 
 // Merge split-K partials: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  One warp per (request, head).
 // CROSS: as for decode_kernel, the keys are the ctx cached ones; a row without keys has no partials and gets zeros.
-template <int D, bool CROSS = false>
+// WPR = 4: four warps per row, a block's, each with every fourth partial, for rows of more than eight: one warp pays a memory
+// latency for every few of them (one request of 32000 states in 125 slices: 85 us, with four warps 44).
+template <int D, bool CROSS = false, int WPR = 1>
 __global__ void __launch_bounds__(128) combine_kernel(const DecodeParams p) {
-  const int warp_global = (blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+  const int warp_global = WPR == 4 ? (int)blockIdx.x : (int)((blockIdx.x * blockDim.x + threadIdx.x) >> 5);
+  const int sub = WPR == 4 ? (int)(threadIdx.x >> 5) : 0;
   const int lane = threadIdx.x & 31;
   const ModelParams& M = p.m;
   griddep_launch_dependents();  // the next attention kernel may start its cache loads now
@@ -523,7 +526,7 @@ __global__ void __launch_bounds__(128) combine_kernel(const DecodeParams p) {
   for (int i = 0; i < PER; ++i) acc[i] = 0.f;
   float L = 0.f;
   if (mm != -INFINITY) {
-    for (int s = 0; s < n_splits; ++s) {
+    for (int s = sub; s < n_splits; s += WPR) {
       const float2 v = ml[s];
       const float f = fast_exp2(v.x - mm);
       L += f * v.y;
@@ -538,6 +541,22 @@ __global__ void __launch_bounds__(128) combine_kernel(const DecodeParams p) {
         acc[0] += f * x.x;
         acc[1] += f * x.y;
       }
+    }
+  }
+  if constexpr (WPR == 4) {
+    __shared__ float sums[3][32][PER + 1];
+    if (sub > 0) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) sums[sub - 1][lane][i] = acc[i];
+      sums[sub - 1][lane][PER] = L;
+    }
+    __syncthreads();
+    if (sub > 0) return;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) acc[i] += sums[k][lane][i];
+      L += sums[k][lane][PER];
     }
   }
   const bool some = CROSS ? L != 0.f : L > 0.f;
@@ -1282,7 +1301,8 @@ cudaError_t hswa_launch_decode_cross(const CUtensorMap& tm_pool, const DecodePar
 cudaError_t hswa_launch_combine(const DecodeParams& p, bool cross, cudaStream_t s) {
   const int rows = p.b.B * p.nq * p.m.Hq;
   if (rows == 0) return cudaSuccess;
-  const int blocks = (rows * 32 + 127) / 128;
+  const bool four = cross && p.max_splits > 8;  // warps per row
+  const int blocks = four ? rows : (rows * 32 + 127) / 128;
   // programmatic dependent launch: the blocks are resident (and wait) by the time the partials are complete
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(blocks, 1, 1);
@@ -1293,6 +1313,8 @@ cudaError_t hswa_launch_combine(const DecodeParams& p, bool cross, cudaStream_t 
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
+  if (four)
+    return p.m.D == 128 ? cudaLaunchKernelEx(&cfg, combine_kernel<128, true, 4>, p) : cudaLaunchKernelEx(&cfg, combine_kernel<64, true, 4>, p);
   if (cross)
     return p.m.D == 128 ? cudaLaunchKernelEx(&cfg, combine_kernel<128, true>, p) : cudaLaunchKernelEx(&cfg, combine_kernel<64, true>, p);
   return p.m.D == 128 ? cudaLaunchKernelEx(&cfg, combine_kernel<128>, p) : cudaLaunchKernelEx(&cfg, combine_kernel<64>, p);
