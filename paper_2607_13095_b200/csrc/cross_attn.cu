@@ -8,10 +8,13 @@ namespace {
 using namespace hswa_dev;
 
 // Joins the key slices: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  One warp per (token, head); slices that hold
-// no key of the row (l = 0) are passed over.
-template <int D>
+// no key of the row (l = 0) are passed over.  WPR = 4: four warps per row, a block's, each with every fourth slice, for more
+// than eight of them: one warp pays a memory latency for every few (8 tokens against 32000 states, 32 / 8 heads of 128, 36
+// slices: 43 us, with four warps 35).
+template <int D, int WPR>
 __global__ void __launch_bounds__(128) cross_combine_kernel(const CrossParams p) {
-  const int64_t row = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+  const int64_t row = WPR == 4 ? (int64_t)blockIdx.x : ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+  const int sub = WPR == 4 ? (int)(threadIdx.x >> 5) : 0;
   const int lane = threadIdx.x & 31;
   const ModelParams& M = p.m;
   // launched early (programmatic dependent launch) behind the kernel that writes the partials
@@ -31,7 +34,7 @@ __global__ void __launch_bounds__(128) cross_combine_kernel(const CrossParams p)
 #pragma unroll
   for (int i = 0; i < PER; ++i) acc[i] = 0.f;
   float L = 0.f;
-  for (int s = 0; s < p.slices; ++s) {
+  for (int s = sub; s < p.slices; s += WPR) {
     const float2 v = ml[s];
     if (v.y == 0.f) continue;
     const float f = fast_exp2(v.x - mm);
@@ -41,6 +44,22 @@ __global__ void __launch_bounds__(128) cross_combine_kernel(const CrossParams p)
       const float2 x = *reinterpret_cast<const float2*>(po + (int64_t)s * D + lane * PER + i);
       acc[i] += f * x.x;
       acc[i + 1] += f * x.y;
+    }
+  }
+  if constexpr (WPR == 4) {
+    __shared__ float sums[3][32][PER + 1];
+    if (sub > 0) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) sums[sub - 1][lane][i] = acc[i];
+      sums[sub - 1][lane][PER] = L;
+    }
+    __syncthreads();
+    if (sub > 0) return;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) acc[i] += sums[k][lane][i];
+      L += sums[k][lane][PER];
     }
   }
   const float inv = L != 0.f ? 1.f / L : 0.f;  // (a NaN among the inputs shows in the output)
@@ -59,7 +78,8 @@ __global__ void __launch_bounds__(128) cross_combine_kernel(const CrossParams p)
 }  // namespace
 
 cudaError_t hswa_launch_cross_combine(const CrossParams& p, cudaStream_t s) {
-  const int64_t blocks = ((int64_t)p.total_q * p.m.Hq * 32 + 127) / 128;
+  const bool four = p.slices > 8;  // warps per row
+  const int64_t rows = (int64_t)p.total_q * p.m.Hq, blocks = four ? rows : (rows + 3) / 4;
   if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks, 1, 1);
@@ -70,5 +90,7 @@ cudaError_t hswa_launch_cross_combine(const CrossParams& p, cudaStream_t s) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return p.m.D == 128 ? cudaLaunchKernelEx(&cfg, cross_combine_kernel<128>, p) : cudaLaunchKernelEx(&cfg, cross_combine_kernel<64>, p);
+  if (four)
+    return p.m.D == 128 ? cudaLaunchKernelEx(&cfg, cross_combine_kernel<128, 4>, p) : cudaLaunchKernelEx(&cfg, cross_combine_kernel<64, 4>, p);
+  return p.m.D == 128 ? cudaLaunchKernelEx(&cfg, cross_combine_kernel<128, 1>, p) : cudaLaunchKernelEx(&cfg, cross_combine_kernel<64, 1>, p);
 }
