@@ -162,7 +162,7 @@ bool plan_cross(const hswa_handle* h, int batch, int total_q, int max_q_len, int
     const int per_sm = h->cfg.head_dim == 128 ? 2 : 4;
     c.split_len = max_ctx_len <= kUnsplitLen ? kUnsplitLen : plan_split_len(h, batch, last, per_sm);
     c.slices = plan_max_splits(c.split_len, last);
-    if (c.slices > 65535) return false;
+    if (c.slices > 65535 || (int64_t)batch * h->cfg.num_q_heads > INT32_MAX / 64) return false;  // grid extents, the join's rows
     if (c.slices > 1) {
       const size_t rows = (size_t)batch * h->cfg.num_q_heads;
       c.o_bytes = (rows * c.slices * h->cfg.head_dim * sizeof(float) + 255) & ~size_t(255);
