@@ -6,8 +6,8 @@
 // writes one number; nothing is exchanged between threads, no atomics, and the order of the sums is fixed.  Each key is
 // read from memory once.
 //
-// Bounds.  One row group (a decode step) is bound by reading K: 64 requests of 4096 to 32768 keys, 8 KV heads of 128: 423 us =
-// 6.5 TB/s, 1.01 of a plain copy's rate.  With many rows the sums bound it (an observation window of 33 to 64 tokens on 8
+// Bounds.  One row group (a decode step) is bound by reading K: 64 requests of 4096 to 32768 keys, 8 KV heads of 128: 423 to
+// 433 us = 6.4 to 6.5 TB/s, a plain copy's rate.  With many rows the sums bound it (an observation window of 33 to 64 tokens on 8
 // prompts of up to 16384: 73 us, where the tensor core has 26 us of work and the special-function units, at 16 exponentials
 // per clock and SM, 37 us): the rest is the instructions around them.  Taking a share of the exponentials on the FMA pipes by
 // a polynomial was no faster (1, 2, 3 of 8: 78 us; 4 of 8: 83 us).

@@ -228,8 +228,8 @@ __device__ __forceinline__ void linger_after_error(const int32_t* err) {
 // one KV head; the two tiles of a block follow one another in the request's tokens.  The keys may be cut into slices
 // (blockIdx.x / row tiles), which leave partials like the prefix stage's.  A block of two Q tiles whose
 // tokens fit one runs with one MMA issuer and one softmax group; NQ = 1 is for batches whose requests all do: half the
-// threads, shared memory (one K and one V stage) and TMEM columns, so that an SM holds two blocks.  8 requests, 257 to 512 tokens, up to 8192 states, 64 / 8 heads: 354 us = 990 TFLOP/s
-// under a sustained load (1136 in short bursts), 53 % of the tensor pipe; the warp-level kernel took 2137 us.
+// threads, shared memory (one K and one V stage) and TMEM columns, so that an SM holds two blocks.  8 requests, 257 to 512 tokens, up to 8192 states, 64 / 8 heads: 357 us = 981 TFLOP/s
+// under a sustained load (1140 in short bursts), 53 % of the tensor pipe; the warp-level kernel took 2137 us.
 enum { MODE_PREFILL = 0, MODE_PREFIX = 1, MODE_CROSS = 2 };
 // Does cached tile j (of nA) of a request with ctx cached tokens hold rows that no row of the block can see?  On a
 // Full layer: the last tile when ctx ends inside it.  On an SWA layer: every ring tile (slots older than the window,
