@@ -55,6 +55,10 @@ __device__ __forceinline__ int weights_request_error(const WeightsParams& p, int
   return keys > p.stride || keys > (int64_t)p.b.max_blocks * p.m.P ? -3 : 0;
 }
 
+// Columns that the MMA of a Q tile of `cols` rows writes, of the tile's N; those behind them hold what an earlier kernel or
+// Q tile left in TMEM, and nothing may read them.
+__device__ __forceinline__ int mma_cols(int cols, int N) { return min(N, (cols + 31) & ~31); }
+
 // A warp's bounded wait: one answer for all lanes.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)); }
 
@@ -417,9 +421,9 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
         for (int qt = first; qt < sg.n_qt && ok; ++qt) {
           const int qs = q.slot;
           if (!resident || t == sg.t_lo) ok = warp_wait(bar(B_QFULL + qs), q.phase);
-          // a request's last Q tile: no more columns than the sums look at
+          // no more columns than the sums look at
           const int cols = min(pl.tile_tokens, sg.n - qt * pl.tile_tokens) * M.G;
-          const uint32_t idesc = idesc0 | ((uint32_t)(min(N, (cols + 31) & ~31) >> 3) << 17);
+          const uint32_t idesc = idesc0 | ((uint32_t)(mma_cols(cols, N) >> 3) << 17);
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             if (t + g >= sg.t_hi || !ok) continue;
@@ -499,7 +503,7 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
             const float* nl = s_nl + qs * N;
             const int tok0 = qt * pl.tile_tokens;
             const int cols = min(pl.tile_tokens, sg.n - tok0) * M.G;
-            const int full_cols = cols == q_rows ? N : cols;  // (the rows up to N are zeros there)
+            const int full_cols = cols == q_rows ? mma_cols(cols, N) : cols;  // (a full tile's rows behind q_rows are zeros)
             // Columns [c_lo, cols) count: behind cols are rows of another request, before c_lo tokens that come before the
             // key.  Chunks that every lane of the warp sees whole take the short way, chunks that none sees are passed over.
             const int c_lo = p.causal ? (j - sg.ctx - tok0) * M.G : 0;
