@@ -506,8 +506,8 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
             const int full_cols = cols == q_rows ? mma_cols(cols, N) : cols;  // (a full tile's rows behind q_rows are zeros)
             // Columns [c_lo, cols) count: behind cols are rows of another request, before c_lo tokens that come before the
             // key.  Chunks that every lane of the warp sees whole take the short way, chunks that none sees are passed over.
-            const int c_lo = p.causal ? (j - sg.ctx - tok0) * M.G : 0;
-            const int warp_lo = max(0, __shfl_sync(0xffffffffu, c_lo, 0)), warp_hi = __shfl_sync(0xffffffffu, c_lo, 31);
+            const int c_lo = p.causal ? max(0, j - sg.ctx - tok0) * M.G : 0;  // (clamped first: G times a far context passes 32 bits)
+            const int warp_lo = __shfl_sync(0xffffffffu, c_lo, 0), warp_hi = __shfl_sync(0xffffffffu, c_lo, 31);
             float2 acc[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[c] = make_float2(0.f, 0.f);

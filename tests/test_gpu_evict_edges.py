@@ -33,3 +33,32 @@ def test_weights_of_65_to_104_rows(G, n, D, causal):
     lse, old = weights_inputs(c, 103)
     leave_nan_in_the_accumulators()
     check_weights(c, 0.5, lse, old.copy(), run_weights(c, 0.5, lse, old))
+
+
+@pytest.mark.parametrize("n", [1, 5, 20])
+def test_weights_of_the_oldest_keys_of_a_context_past_2_to_28(n):
+    """2^28 and some positions behind a block table that names eight pages over and over: positions with equal slots of equal
+    pages get equal weights, the oldest ones too."""
+    d, L, pages = dims(8, 64, 64, 1), 2 ** 28 + 200, 8
+    rng = np.random.default_rng(110)
+    pool = wl.bf16_bits_normal(111, (pages, 2, 1, 64, 64))
+    q = wl.bf16_bits_normal(112, (n, 8, 64))
+    blocks = -(-(L + n) // 64)
+    table = torch.arange(blocks, dtype=torch.int32, device="cuda") % pages
+    lse = rng.uniform(2.0, 4.0, (n, 8)).astype(np.float32)
+    b = hb.Batch(dev_i32([L]), table[None], *no_rings(d, 1), dev_i32([0, n]), max_q_len=n, total_q=n, max_ctx_len=L)
+    w = torch.full((1, 1, L + n + 5), -1.0, device="cuda")
+    h = make_handle(d)
+    hb.hswa_attn_weights(h, hb.Layer(to_dev_bf16(pool), False), b, True, to_dev_bf16(q), torch.from_numpy(lse).cuda(), 0.0, w)
+    no_error(h)
+    s = wl.bits_to_f64(q).reshape(n * 8, 64) @ wl.bits_to_f64(pool[:, 0, 0]).reshape(pages * 64, 64).T / 8.0
+    e = np.exp(s - lse.reshape(n * 8, 1))
+    want = torch.from_numpy(e.sum(axis=0)).float().cuda()
+    tol = (S_ERR + (8 * n + 4) * 2.0 ** -24) * want
+    whole = L // (pages * 64) * (pages * 64)
+    assert ((w[0, 0, :whole].view(-1, pages * 64) - want).abs_() <= tol).all()
+    new = np.arange(n)[:, None] >= np.arange(n)[None, :]  # the step's own positions: causal
+    at = (L + np.arange(n)) % (pages * 64)
+    own = (e.reshape(n, 8, -1).sum(axis=1)[:, at] * new).sum(axis=0)
+    assert np.allclose(w[0, 0, L:L + n].cpu().numpy(), own, rtol=S_ERR + (8 * n + 4) * 2.0 ** -24, atol=0)
+    assert (w[0, 0, L + n:] == -1).all()
