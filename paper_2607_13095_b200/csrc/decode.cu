@@ -459,10 +459,14 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p)
   for (int idx = threadIdx.x; idx < M.G * D; idx += blockDim.x) {
     const int g = idx / D, d = idx % D;
     float mm = -INFINITY;
+    bool sums = false;  // CROSS: scores that are all NaN leave a sum of NaN without a maximum
 #pragma unroll
-    for (int w = 0; w < NW; ++w) mm = fmaxf(mm, sc_ml[(w * 8 + g) * 2]);
+    for (int w = 0; w < NW; ++w) {
+      mm = fmaxf(mm, sc_ml[(w * 8 + g) * 2]);
+      if constexpr (CROSS) sums |= sc_ml[(w * 8 + g) * 2 + 1] != 0.f;
+    }
     float L = 0.f, O = 0.f;
-    if (mm != -INFINITY) {
+    if (mm != -INFINITY || sums) {
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
         const float f = fast_exp2(sc_ml[(w * 8 + g) * 2] - mm);
@@ -517,15 +521,21 @@ __global__ void __launch_bounds__(128) combine_kernel(const DecodeParams p) {
   const float2* ml = p.part_ml + row * p.max_splits;
   const float* po = p.part_o + row * p.max_splits * D;
   float mm = -INFINITY;
-  for (int s = lane; s < n_splits; s += 32) mm = fmaxf(mm, ml[s].x);
+  bool sums = false;  // CROSS: as in decode_kernel
+  for (int s = lane; s < n_splits; s += 32) {
+    const float2 v = ml[s];
+    mm = fmaxf(mm, v.x);
+    if constexpr (CROSS) sums |= v.y != 0.f;
+  }
 #pragma unroll
   for (int sh = 16; sh >= 1; sh >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, sh));
+  if constexpr (CROSS) sums = __any_sync(0xffffffffu, sums);
   constexpr int PER = D / 32;
   float acc[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) acc[i] = 0.f;
   float L = 0.f;
-  if (mm != -INFINITY) {
+  if (mm != -INFINITY || sums) {
     for (int s = sub; s < n_splits; s += WPR) {
       const float2 v = ml[s];
       const float f = fast_exp2(v.x - mm);

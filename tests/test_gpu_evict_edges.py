@@ -62,3 +62,28 @@ def test_weights_of_the_oldest_keys_of_a_context_past_2_to_28(n):
     own = (e.reshape(n, 8, -1).sum(axis=1)[:, at] * new).sum(axis=0)
     assert np.allclose(w[0, 0, L:L + n].cpu().numpy(), own, rtol=S_ERR + (8 * n + 4) * 2.0 ** -24, atol=0)
     assert (w[0, 0, L + n:] == -1).all()
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(3, 64, 16)], ids=str)
+@pytest.mark.parametrize("ctx", [1, 300, 9000])
+@pytest.mark.parametrize("n", [1, 3])
+def test_cross_shows_a_row_of_nan(d, ctx, n):
+    """A NaN in q makes every score of its row NaN: that row is NaN, with one slice of the keys and with many."""
+    c = Case(d, [ctx, 5], [n, 1], seed=120)
+    c.q[0, 1, 7] = NAN_BITS
+    out, lse = run_cross(c)
+    assert np.isnan(out[0, 1]).all() and np.isnan(lse[0, 1])
+    out[0, 1] = lse[0, 1] = 0
+    assert np.isfinite(out).all() and np.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(3, 64, 16)], ids=str)
+@pytest.mark.parametrize("ctx", [1, 65, 129, 4097])
+@pytest.mark.parametrize("n", [1, 3])
+def test_cross_shows_a_nan_in_the_last_key(d, ctx, n):
+    """Alone in the request, in its tile, or in its slice of the keys."""
+    c = Case(d, [ctx, 5], [n, 1], seed=121)
+    c.pool[c.table[0, (ctx - 1) // d.page_size], 0, 1, (ctx - 1) % d.page_size] = NAN_BITS
+    out, lse = run_cross(c)
+    assert np.isnan(out[:n, d.group:]).all() and np.isnan(lse[:n, d.group:]).all()
+    assert np.isfinite(out[:n, :d.group]).all() and np.isfinite(out[n:]).all()
