@@ -125,7 +125,7 @@ struct CrossParams {
   const int32_t* q_end;  // device: the last request's end (q_indptr[B]), behind which no row has partials; null: total_q
   int32_t slices;
   const float* part_o;    // [T * Hq][slices][D]
-  const float2* part_ml;  // [T * Hq][slices] (m in log2 units, l; l = 0: the slice holds no key of the row)
+  const float2* part_ml;  // [T * Hq][slices] (m in log2 units, l; l = 0: the slice holds no key of the row; l < 0 in the first: no block has the row)
 };
 
 struct WeightsParams {

@@ -323,6 +323,12 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     head = 0;
     h0 = kh * M.G;
     tok_tile = BM / M.G;
+    if (p.max_splits > 1 && b == 0 && slice == 0) {
+      // rows past the last row tile have no block: a mark tells the join to leave them alone
+      const int64_t first = (int64_t)max_tiles * NQ * tok_tile, last = min(n, p.total_q - t0);
+      for (int64_t row = first * M.G + threadIdx.x; row < last * M.G; row += THREADS)
+        p.part_ml[((t0 + row / M.G) * M.Hq + h0 + row % M.G) * p.max_splits] = make_float2(-INFINITY, -1.f);
+    }
     if (b * NQ * tok_tile >= n) return;  // uniform for the block
     nq_tiles = NQ == 2 && (b * 2 + 1) * tok_tile < n ? 2 : 1;
     const int tile_begin = slice * p.prefix_tiles_per_split;

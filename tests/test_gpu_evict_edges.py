@@ -87,3 +87,30 @@ def test_cross_shows_a_nan_in_the_last_key(d, ctx, n):
     out, lse = run_cross(c)
     assert np.isnan(out[:n, d.group:]).all() and np.isnan(lse[:n, d.group:]).all()
     assert np.isfinite(out[:n, :d.group]).all() and np.isfinite(out[n:]).all()
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(3, 64, 16)], ids=str)
+@pytest.mark.parametrize("ctx", [[300, 100, 50], [9000, 700, 0]])
+@pytest.mark.parametrize("max_q,n", [(7, [90, 5, 100]), (50, [20, 200, 3])])
+def test_cross_leaves_rows_past_the_bound_alone(d, ctx, max_q, n):
+    """Requests longer than max_q_len, with and without slices of the keys: a row is right or as it was, and what the workspace
+    held does not matter."""
+    c = Case(d, ctx, n, seed=130)
+    h, b, T = make_handle(d), c.batch(max_q=max_q), int(c.indptr[-1])
+    out = torch.full((T, d.num_q_heads, d.head_dim), 7.0, device="cuda")
+    lse = torch.full((T, d.num_q_heads), 7.0, device="cuda")
+    ws = workspace(h, b)
+    ws.view(torch.float32).fill_(float("nan"))
+    hb.hswa_cross_attn(h, hb.Layer(to_dev_bf16(c.pool), False), b, to_dev_bf16(c.q), out, lse, ws)
+    st = hb.hswa_get_async_error(h)
+    assert st[0] == hb.HSWA_ERR_BOUNDS and st[2] == -2 and st[3] == n[st[1]] > max_q, st
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    want, want_lse, mag = ref.cross_attention(c.pool, c.table, c.ctx, c.indptr, c.q, c.scale)
+    with np.errstate(invalid="ignore"):
+        right = (np.abs(out - want) <= (2.0 ** -8 + 2 * S_ERR) * mag + 1e-7).all(axis=2) & ((np.abs(lse - want_lse) <= S_ERR) | (lse == want_lse))
+    same = (out == 7).all(axis=2) & (lse == 7)
+    for r in range(3):
+        rows = slice(int(c.indptr[r]), int(c.indptr[r]) + min(int(c.n[r]), max_q))
+        assert right[rows].all(), r
+    assert (right | same).all()
+    assert same.any()
