@@ -252,8 +252,8 @@ hswa_status hswa_prefill_attn(hswa_handle* h, const hswa_layer* layer, const hsw
  * lse are taken over the fp32 values.  Workspace: hswa_cross_workspace_need bytes (0: none needed), else
  * HSWA_ERR_WORKSPACE.  The block table must cover max_ctx_len and the layer must not be an SWA layer
  * (HSWA_ERR_INVALID_ARG); max_ctx_len is at most 2^30, for single tokens 65535 * 4096 (HSWA_ERR_UNSUPPORTED, the need is
- * then 0).  A request longer than max_ctx_len or max_q_len is recorded as HSWA_ERR_BOUNDS (index -1 / -2) and what the
- * bounds cover is computed.
+ * then 0).  A request longer than max_ctx_len or max_q_len, or with row offsets outside [0, total_q], is recorded as
+ * HSWA_ERR_BOUNDS (index -1 / -2 / -2); what the bounds cover is computed, other rows of out and lse stay as they were.
  *
  * This call and the eviction calls below refuse a current device other than the handle's (HSWA_ERR_INVALID_ARG).
  *
@@ -278,8 +278,8 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
  *   q: device bf16 [T][Hq][D]; lse: device fp32 [T][Hq]; weights: device fp32 [B][Hkv][weights_stride], columns at or
  *   past the request's last position are not touched.  weights_stride and the block table must cover max_ctx_len, decay
  *   must be finite and >= 0: HSWA_ERR_INVALID_ARG; max_ctx_len + max_q_len is at most 2^30: HSWA_ERR_UNSUPPORTED.  A
- *   request longer than max_ctx_len or max_q_len, or whose ctx + n passes weights_stride or the block table, is recorded as
- *   HSWA_ERR_BOUNDS (index -1 / -2 / -3) and left out.  Sums are in fp32 in a fixed order: repeated calls on equal inputs
+ *   request longer than max_ctx_len or max_q_len, with row offsets outside [0, total_q], or whose ctx + n passes
+ *   weights_stride or the block table, is recorded as HSWA_ERR_BOUNDS (index -1 / -2 / -2 / -3) and left out.  Sums are in fp32 in a fixed order: repeated calls on equal inputs
  *   agree bit for bit.
  *
  * hswa_evict_select: keep_idx[r][kh][0 .. kept) = the kept = min(keep_len[r], ctx_len[r]) positions of largest weight, in

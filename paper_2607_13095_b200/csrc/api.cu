@@ -723,6 +723,7 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
     p.max_splits = p.grid_splits = pl.slices;
     p.nq = 1;
     p.max_ctx_len = b->max_ctx_len;
+    p.total_q = b->total_q;
     p.part_o = part_o;
     p.part_ml = part_ml;
     p.err = h->err;
@@ -784,6 +785,7 @@ hswa_status hswa_attn_weights(hswa_handle* h, const hswa_layer* layer, const hsw
   p.decay = decay;
   p.causal = causal != 0;
   p.max_q_len = b->max_q_len;
+  p.total_q = b->total_q;
   p.max_ctx_len = b->max_ctx_len;
   p.err = h->err;
   CUtensorMap tm, tm_q;

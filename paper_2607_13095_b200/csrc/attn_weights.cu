@@ -48,9 +48,9 @@ struct WeightsPlan {
 };
 
 // Index of the error word for a request that the host's bounds, the block table or the weights do not cover; 0 if fine.
-__device__ __forceinline__ int weights_request_error(const WeightsParams& p, int ctx, int n) {
+__device__ __forceinline__ int weights_request_error(const WeightsParams& p, int ctx, int t0, int n) {
   if (ctx < 0 || ctx > p.max_ctx_len) return -1;
-  if (n < 0 || n > p.max_q_len) return -2;
+  if (n < 0 || n > p.max_q_len || t0 < 0 || (int64_t)t0 + n > p.total_q) return -2;
   const int64_t keys = (int64_t)ctx + (p.causal ? n : 0);
   return keys > p.stride || keys > (int64_t)p.b.max_blocks * p.m.P ? -3 : 0;
 }
@@ -126,7 +126,7 @@ struct Walker {
     s.ctx = p.b.ctx_len[r];
     tiles = 0;
     q = 1;
-    if (weights_request_error(p, s.ctx, s.n) != 0) return;
+    if (weights_request_error(p, s.ctx, s.t0, s.n) != 0) return;
     s.kv_len = s.ctx + (p.causal ? s.n : 0);
     s.n_qt = (s.n + pl.tile_tokens - 1) / pl.tile_tokens;
     tiles = (s.kv_len + TKEYS - 1) / TKEYS;
@@ -227,7 +227,7 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
   } else if (warp == 1 && blockIdx.x == 0) {
     for (int r = lane; r < p.b.B; r += 32) {
       const int t0 = p.b.q_indptr ? p.b.q_indptr[r] : r, n = p.b.q_indptr ? p.b.q_indptr[r + 1] - t0 : 1, ctx = p.b.ctx_len[r];
-      const int bad = weights_request_error(p, ctx, n);
+      const int bad = weights_request_error(p, ctx, t0, n);
       if (bad != 0) record_error(p.err, HSWA_ERR_BOUNDS, r, bad, bad == -1 ? ctx : bad == -2 ? n : ctx + n);
     }
   }

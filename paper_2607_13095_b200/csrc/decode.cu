@@ -213,8 +213,9 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p)
     if (p.b.q_indptr) {
       row_r = p.b.q_indptr[r];
       const int n = p.b.q_indptr[r + 1] - row_r;
-      if (threadIdx.x == 0 && split == 0 && kh == 0 && (n < 0 || n > 1)) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, n);
-      if (n <= 0) return;
+      const bool inside = row_r >= 0 && (int64_t)row_r + n <= p.total_q;
+      if (threadIdx.x == 0 && split == 0 && kh == 0 && (n < 0 || n > 1 || !inside)) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, n);
+      if (n <= 0 || row_r < 0 || row_r >= p.total_q) return;
     }
   }
 
@@ -512,7 +513,7 @@ __global__ void __launch_bounds__(128) combine_kernel(const DecodeParams p) {
   if constexpr (CROSS) {
     if (p.b.q_indptr) {
       const int t0 = p.b.q_indptr[r];
-      if (p.b.q_indptr[r + 1] <= t0) return;
+      if (p.b.q_indptr[r + 1] <= t0 || t0 < 0 || t0 >= p.total_q) return;
       out_row = (int64_t)t0 * M.Hq + (warp_global - r * M.Hq);
     }
   }

@@ -318,14 +318,15 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     const int len = p.b.ctx_len[r];
     if (threadIdx.x == 0 && blockIdx.x == 0 && kh == 0) {  // the grid was sized from the host's bounds
       if (len < 0 || len > p.max_ctx_len) record_error(p.err, HSWA_ERR_BOUNDS, r, -1, len);
-      if (n < 0 || n > p.max_q_len) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, n);
+      if (n < 0 || n > p.max_q_len || t0 < 0 || (int64_t)t0 + n > p.total_q) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, n);
     }
+    n = t0 < 0 ? 0 : min(n, p.total_q - t0);  // (rows past total_q have no storage)
     head = 0;
     h0 = kh * M.G;
     tok_tile = BM / M.G;
     if (p.max_splits > 1 && b == 0 && slice == 0) {
       // rows past the last row tile have no block: a mark tells the join to leave them alone
-      const int64_t first = (int64_t)max_tiles * NQ * tok_tile, last = min(n, p.total_q - t0);
+      const int64_t first = (int64_t)max_tiles * NQ * tok_tile, last = n;
       for (int64_t row = first * M.G + threadIdx.x; row < last * M.G; row += THREADS)
         p.part_ml[((t0 + row / M.G) * M.Hq + h0 + row % M.G) * p.max_splits] = make_float2(-INFINITY, -1.f);
     }

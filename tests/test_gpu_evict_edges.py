@@ -114,3 +114,49 @@ def test_cross_leaves_rows_past_the_bound_alone(d, ctx, max_q, n):
         assert right[rows].all(), r
     assert (right | same).all()
     assert same.any()
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(3, 64, 16)], ids=str)
+@pytest.mark.parametrize("ctx", [[300, 100, 50], [9000, 700, 800]])
+@pytest.mark.parametrize("n", [[1, 1, 1], [2, 3, 20], [30, 40, 50]])
+def test_row_offsets_past_total_q_are_recorded(d, ctx, n):
+    """The last request's rows pass total_q (and one request's begin there): they are neither read nor written."""
+    c = Case(d, ctx, n, seed=140)
+    h, T, cut = make_handle(d), int(c.indptr[-1]), int(c.indptr[2])
+    q, layer = to_dev_bf16(c.q), hb.Layer(to_dev_bf16(c.pool), False)
+    want, want_lse, mag = ref.cross_attention(c.pool, c.table, c.ctx, c.indptr, c.q, c.scale)
+    for total in (cut, T - 1):
+        if total < max(n):
+            continue
+        b = hb.Batch(dev_i32(c.ctx), dev_i32(c.table), *no_rings(d, 3), dev_i32(c.indptr), max_q_len=max(n), total_q=total, max_ctx_len=max(ctx))
+        out = torch.full((T, d.num_q_heads, d.head_dim), 7.0, device="cuda")
+        lse = torch.full((T, d.num_q_heads), 7.0, device="cuda")
+        ws = torch.full((workspace(h, b).numel() // 4 + 64 * 1024,), 7.0, device="cuda")
+        need = hb.hswa_cross_workspace_need(h, 3, total, max(n), max(ctx))
+        hb.hswa_cross_attn(h, layer, b, q, out, lse, ws)
+        assert hb.hswa_get_async_error(h) == (hb.HSWA_ERR_BOUNDS, 2, -2, n[2])
+        assert (out[total:] == 7).all() and (lse[total:] == 7).all() and (ws[need // 4:] == 7).all()
+        got, got_lse = out[:cut].double().cpu().numpy(), lse[:cut].double().cpu().numpy()
+        assert (np.abs(got - want[:cut]) <= (2.0 ** -8 + 2 * S_ERR) * mag[:cut] + 1e-7).all() and (np.abs(got_lse - want_lse[:cut]) <= S_ERR).all()
+        w = torch.full((3, d.num_kv_heads, max(ctx)), 7.0, device="cuda")
+        hb.hswa_attn_weights(h, layer, b, False, q, lse, 0.0, w)
+        assert hb.hswa_get_async_error(h) == (hb.HSWA_ERR_BOUNDS, 2, -2, n[2])
+        assert (w[2] == 7).all() and not (w[:2, :, :50] == 7).any()
+
+
+def test_negative_row_offsets_are_recorded():
+    d = dims(8, 128, 64)
+    for n in ([1, 1], [4, 30]):
+        c = Case(d, [300, 100], n, seed=141)
+        h, T = make_handle(d), int(c.indptr[-1])
+        q, layer = to_dev_bf16(c.q), hb.Layer(to_dev_bf16(c.pool), False)
+        b = hb.Batch(dev_i32(c.ctx), dev_i32(c.table), *no_rings(d, 2), dev_i32([n[0] - 2 * n[0], 0, n[1]]), max_q_len=max(n), total_q=T,
+                     max_ctx_len=300)
+        out, lse = torch.full((T, 16, 128), 7.0, device="cuda"), torch.full((T, 16), 7.0, device="cuda")
+        hb.hswa_cross_attn(h, layer, b, q, out, lse, workspace(h, b))
+        assert hb.hswa_get_async_error(h) == (hb.HSWA_ERR_BOUNDS, 0, -2, n[0])
+        assert (out[n[1]:] == 7).all() and (out[:n[1]] != 7).any(dim=-1).all()
+        w = torch.full((2, 2, 300), 7.0, device="cuda")
+        hb.hswa_attn_weights(h, layer, b, False, q, lse, 0.0, w)
+        assert hb.hswa_get_async_error(h) == (hb.HSWA_ERR_BOUNDS, 0, -2, n[0])
+        assert (w[0] == 7).all() and not (w[1, :, :100] == 7).any()
