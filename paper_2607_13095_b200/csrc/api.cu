@@ -754,7 +754,7 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
   if ((st = make_rows_map(h, q, h->cfg.num_q_heads, b->total_q, hswa_cross_tile_tokens(t.m), &tm_q, h->group)) != HSWA_OK) return st;
   if (hswa_launch_cross_tc(tm, tm_q, t, pl.row_tiles, pl.q_tiles, s) != cudaSuccess) return HSWA_ERR_CUDA;
   if (pl.slices > 1) {
-    const CrossParams p = {t.m, out, lse, b->total_q, b->q_indptr ? b->q_indptr + b->batch : nullptr, pl.slices, part_o, part_ml};
+    const CrossParams p = {t.m, out, lse, b->total_q, b->q_indptr, b->batch, pl.slices, part_o, part_ml};
     if (hswa_launch_cross_combine(p, s) != cudaSuccess) return HSWA_ERR_CUDA;
   }
   return HSWA_OK;

@@ -123,7 +123,8 @@ struct CrossParams {
   void* out;   // [T][Hq][D]
   float* lse;  // [T][Hq] or null
   int32_t total_q;
-  const int32_t* q_end;  // device: the last request's end (q_indptr[B]), behind which no row has partials; null: total_q
+  const int32_t* q_indptr;  // [batch + 1]: rows before the first request's and behind the last one's have no partials
+  int32_t batch;
   int32_t slices;
   const float* part_o;    // [T * Hq][slices][D]
   const float2* part_ml;  // [T * Hq][slices] (m in log2 units, l; l = 0: the slice holds no key of the row; l < 0 in the first: no block has the row)

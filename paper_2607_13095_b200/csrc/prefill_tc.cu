@@ -313,8 +313,8 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     }
     b = blockIdx.x % max_tiles;
     slice = blockIdx.x / max_tiles;
-    t0 = p.b.q_indptr ? p.b.q_indptr[r] : r;
-    n = p.b.q_indptr ? p.b.q_indptr[r + 1] - t0 : 1;
+    t0 = p.b.q_indptr[r];
+    n = p.b.q_indptr[r + 1] - t0;
     const int len = p.b.ctx_len[r];
     if (threadIdx.x == 0 && blockIdx.x == 0 && kh == 0) {  // the grid was sized from the host's bounds
       if (len < 0 || len > p.max_ctx_len) record_error(p.err, HSWA_ERR_BOUNDS, r, -1, len);

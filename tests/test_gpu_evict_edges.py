@@ -160,3 +160,28 @@ def test_negative_row_offsets_are_recorded():
         hb.hswa_attn_weights(h, layer, b, False, q, lse, 0.0, w)
         assert hb.hswa_get_async_error(h) == (hb.HSWA_ERR_BOUNDS, 0, -2, n[0])
         assert (w[0] == 7).all() and not (w[1, :, :100] == 7).any()
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(3, 64, 16)], ids=str)
+@pytest.mark.parametrize("n", [[9, 1, 1], [9, 3, 20], [30, 40, 50]])
+def test_cross_of_the_last_requests_of_a_batch(d, n):
+    """Row offsets that do not begin at 0 (the last requests of a longer batch): the rows before them stay as they were."""
+    c = Case(d, [10, 9000, 700], n, seed=145)
+    h, T, first = make_handle(d), int(c.indptr[-1]), int(c.indptr[1])
+    q, layer, indptr = to_dev_bf16(c.q), hb.Layer(to_dev_bf16(c.pool), False), dev_i32(c.indptr)
+    b = hb.Batch(dev_i32(c.ctx[1:]), dev_i32(c.table[1:]), *no_rings(d, 2), indptr[1:], max_q_len=max(n[1:]), total_q=T, max_ctx_len=9000)
+    out, lse = torch.full((T, d.num_q_heads, d.head_dim), 7.0, device="cuda"), torch.full((T, d.num_q_heads), 7.0, device="cuda")
+    ws = workspace(h, b)
+    ws.view(torch.float32).fill_(float("nan"))
+    hb.hswa_cross_attn(h, layer, b, q, out, lse, ws)
+    no_error(h)
+    assert (out[:first] == 7).all() and (lse[:first] == 7).all()
+    want, want_lse, mag = ref.cross_attention(c.pool, c.table, c.ctx, c.indptr, c.q, c.scale)
+    got, got_lse = out.double().cpu().numpy()[first:], lse.double().cpu().numpy()[first:]
+    assert (np.abs(got - want[first:]) <= (2.0 ** -8 + 2 * S_ERR) * mag[first:] + 1e-7).all() and (np.abs(got_lse - want_lse[first:]) <= S_ERR).all()
+    w = torch.full((2, d.num_kv_heads, 9000), 7.0, device="cuda")
+    hb.hswa_attn_weights(h, layer, b, False, q, lse, 0.0, w)
+    no_error(h)
+    rows = torch.tensor(n[1:], device="cuda")[:, None] * d.group  # every row's probabilities sum to one
+    assert torch.allclose(torch.stack([w[0].double().sum(-1), w[1, :, :700].double().sum(-1)]), rows.double().expand(2, d.num_kv_heads),
+                          rtol=2 * S_ERR + 2.0 ** -11, atol=0)
