@@ -38,7 +38,7 @@ constexpr float NO_ROW = -1e30f;  // in the place of an absent row's value, or o
 // Barriers
 enum { B_QFULL = 0, B_LFULL = B_QFULL + MAX_NSQ, B_QEMPTY = B_LFULL + MAX_NSQ, B_KFULL = B_QEMPTY + MAX_NSQ,
        B_KEMPTY = B_KFULL + MAX_NSK, B_SFULL = B_KEMPTY + MAX_NSK /* [group][buffer] */, B_SEMPTY = B_SFULL + 4,
-       B_PFULL = B_SEMPTY + 4 /* [group][buffer]: the upper columns' sums are in TMEM */, NUM_BARS = B_PFULL + 4 };
+       B_PFULL = B_SEMPTY + 4 /* [group][buffer]: the upper columns' sums are in TMEM */, B_QLAND = B_PFULL + 4, NUM_BARS };
 
 struct WeightsPlan {
   int n_cols;       // N of the MMA: rows of a Q tile, rounded up
@@ -246,6 +246,7 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
       mbar_init(bar(B_SEMPTY + i), GW);
       mbar_init(bar(B_PFULL + i), 4);
     }
+    mbar_init(bar(B_QLAND), 1);
     mbar_fence_init();
     tma_prefetch_desc(&tm_pool);
     tma_prefetch_desc(&tm_q);
@@ -292,6 +293,7 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
       row_at[u] = col / M.G * M.Hq + col % M.G;
     }
     Ring kr, qr;
+    uint32_t landed = 0;                  // parity of the next Q tile that the loader itself waits for
     bool k_used = false, q_used = false;  // the ring has been filled once: its slots have to be released first
     while (ok && walk.next(p, pl, sg)) {
       if (sg.n == 0) continue;
@@ -361,11 +363,34 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
           ok = false;
           return;
         }
+        // A row whose lse is minus infinity adds nothing whatever its q holds, NaN included: it is zeroed between the tile's
+        // arrival and its hand-over, so that its scores are finite.  (The loader waits for such tiles alone; dropping the row's
+        // terms in the sums instead made every call 2 % slower.)
+        bool drop[4], any = false;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) any |= drop[u] = row_tok[u] < sg.n - qt * pl.tile_tokens && x[0][u] == NO_ROW;
+        any = __any_sync(0xffffffffu, any);
+        const uint32_t arrival = bar(any ? B_QLAND : B_QFULL + stage);
         if (lane == 0) {
-          mbar_arrive_expect_tx(bar(B_QFULL + stage), q_rows * 128 * HALVES);
+          mbar_arrive_expect_tx(arrival, q_rows * 128 * HALVES);
 #pragma unroll
           for (int hf = 0; hf < HALVES; ++hf)
-            tma_load_3d(sbase + stage * q_bytes + hf * q_half, &tm_q, bar(B_QFULL + stage), hf * 64, sg.kh * M.G, sg.t0 + qt * pl.tile_tokens);
+            tma_load_3d(sbase + stage * q_bytes + hf * q_half, &tm_q, arrival, hf * 64, sg.kh * M.G, sg.t0 + qt * pl.tile_tokens);
+        }
+        if (any) {
+          if (!warp_wait(arrival, landed)) {
+            if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, sg.r, qt, 95);
+            ok = false;
+            return;
+          }
+          landed ^= 1u;
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            for (int i = 0; drop[u] && i < 8 * HALVES; ++i)
+              *reinterpret_cast<uint4*>(smem + stage * q_bytes + (i >> 3) * q_half + (u * 32 + lane) * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(B_QFULL + stage));
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)

@@ -185,3 +185,23 @@ def test_cross_of_the_last_requests_of_a_batch(d, n):
     rows = torch.tensor(n[1:], device="cuda")[:, None] * d.group  # every row's probabilities sum to one
     assert torch.allclose(torch.stack([w[0].double().sum(-1), w[1, :, :700].double().sum(-1)]), rows.double().expand(2, d.num_kv_heads),
                           rtol=2 * S_ERR + 2.0 ** -11, atol=0)
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(3, 64, 16), dims(5, 128, 32)], ids=str)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("n", [[1, 1, 1], [4, 0, 3], [9, 12, 2], [40, 16, 64], [300, 5, 500]])
+@pytest.mark.parametrize("what", ["nan", "large"])
+def test_weights_of_rows_without_a_vote(d, causal, n, what):
+    """A row whose lse is minus infinity adds nothing, whatever its q is."""
+    c = Case(d, [700, 90, 300], n, seed=150, causal=causal)
+    lse, old = weights_inputs(c, 151)
+    rng = np.random.default_rng(152)
+    out = rng.random(lse.shape) < 0.3
+    out[0, 0] = True
+    lse[out] = -np.inf
+    q = c.q.copy()
+    q[out] = NAN_BITS if what == "nan" else wl.bf16_bits_const(3e38, (1,))[0]
+    want_q, c.q = c.q, q
+    got = run_weights(c, 0.5, lse, old)
+    c.q = want_q
+    check_weights(c, 0.5, lse, old.copy(), got)
