@@ -248,7 +248,7 @@ hswa_status hswa_prefill_attn(hswa_handle* h, const hswa_layer* layer, const hsw
  * an lse of minus infinity; n[r] = 0 leaves nothing to do for the request.
  * q: device bf16 [T][Hq][D]; out: device [T][Hq][D] in cfg.out_dtype; lse: device fp32 [T][Hq] or NULL.
  * batch->q_indptr may be NULL (one token per request, the serving step); with it, rows of q behind the last request's do
- * not matter and those of out and lse are left as they were.  Probabilities enter the PV product as bf16; row sums and
+ * not matter and those of out and lse are left as they were (max_q_len = 0: all of them).  Probabilities enter the PV product as bf16; row sums and
  * lse are taken over the fp32 values.  Workspace: hswa_cross_workspace_need bytes (0: none needed), else
  * HSWA_ERR_WORKSPACE.  The block table must cover max_ctx_len and the layer must not be an SWA layer
  * (HSWA_ERR_INVALID_ARG); max_ctx_len is at most 2^30, for single tokens 65535 * 4096 (HSWA_ERR_UNSUPPORTED, the need is

@@ -699,7 +699,8 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
   hswa_status st = check_common(h, layer, b);
   if (st != HSWA_OK) return st;
   if (b->batch == 0 || b->total_q == 0) return HSWA_OK;
-  if (layer->is_swa || b->max_q_len == 0) return HSWA_ERR_INVALID_ARG;
+  if (layer->is_swa) return HSWA_ERR_INVALID_ARG;
+  if (b->max_q_len == 0) return HSWA_OK;  // a padded batch of which no request has a token
   if (!q || !out || !aligned16(q) || !aligned16(out)) return HSWA_ERR_INVALID_ARG;
   if ((int64_t)b->max_ctx_len > (int64_t)b->max_blocks * h->cfg.page_size) return HSWA_ERR_INVALID_ARG;
   CrossPlan pl;

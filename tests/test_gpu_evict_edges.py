@@ -205,3 +205,16 @@ def test_weights_of_rows_without_a_vote(d, causal, n, what):
     got = run_weights(c, 0.5, lse, old)
     c.q = want_q
     check_weights(c, 0.5, lse, old.copy(), got)
+
+
+def test_cross_of_a_padded_batch_without_any_token():
+    """No request of the step has a token (max_q_len = 0), the tensors are padded: nothing to do, as for the weights."""
+    d = dims(8, 128, 64)
+    c = Case(d, [100, 200], [1, 1], seed=160)
+    h, layer = make_handle(d), hb.Layer(to_dev_bf16(c.pool), False)
+    b = hb.Batch(dev_i32(c.ctx), dev_i32(c.table), *no_rings(d, 2), dev_i32([0, 0, 0]), max_q_len=0, total_q=2, max_ctx_len=200)
+    out, lse = torch.full((2, 16, 128), 7.0, device="cuda"), torch.full((2, 16), 7.0, device="cuda")
+    assert hb.hswa_cross_workspace_need(h, 2, 2, 0, 200) == 0
+    hb.hswa_cross_attn(h, layer, b, to_dev_bf16(c.q), out, lse, None)
+    no_error(h)
+    assert (out == 7).all() and (lse == 7).all()
