@@ -273,8 +273,11 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
  *                       exp(sm_scale * q[r,i,h] . k[j] - lse[r,i,h])   over the rows that see position j.
  *   causal != 0 (self attention): token i sees j <= ctx[r] + i, and positions ctx[r] .. ctx[r] + n[r] - 1 are new: what
  *     their weights held before counts as 0.   causal == 0 (hswa_cross_attn): token i sees every j < ctx[r].
- *   decay = 0 reads none of the old weights.  A row whose lse is minus infinity saw nothing and adds nothing.  To judge a
- *   prompt by its last n tokens only, pass those tokens' q and lse with ctx_len reduced by n.
+ *   decay = 0 reads none of the old weights.  A row whose lse is minus infinity saw nothing and adds nothing, whatever its q
+ *   holds.  To judge a prompt by its last n tokens only, pass those tokens' q and lse with ctx_len reduced by n.
+ *   After hswa_decode_attn_mtp the batch needs row offsets, q_indptr[r] = r * q_len with max_q_len = q_len and total_q =
+ *   B * q_len: the batch of that call (q_indptr = NULL) would mean one row per request.  Rejected drafts have no vote when
+ *   their lse is set to minus infinity before the call; their positions lie behind the advanced ctx_len.
  *   q: device bf16 [T][Hq][D]; lse: device fp32 [T][Hq]; weights: device fp32 [B][Hkv][weights_stride], columns at or
  *   past the request's last position are not touched.  weights_stride and the block table must cover max_ctx_len, decay
  *   must be finite and >= 0: HSWA_ERR_INVALID_ARG; max_ctx_len + max_q_len is at most 2^30: HSWA_ERR_UNSUPPORTED.  A

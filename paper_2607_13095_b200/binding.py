@@ -314,9 +314,15 @@ def hswa_cross_workspace_need(h: Handle, batch: int, total_q: int, max_q_len: in
     return int(load().hswa_cross_workspace_need(h.ptr, batch, total_q, max_q_len, max_ctx_len))
 
 
+def _rows_are_said(batch: Batch, q):
+    # [B][q_len][Hq][D], as multi-token decode takes it: without row offsets its r-th row would count as request r's
+    assert batch.q_indptr is not None or q.dim() < 4 or q.shape[1] == 1, "several rows of q per request need q_indptr"
+
+
 def hswa_cross_attn(h: Handle, layer: Layer, batch: Batch, q, out, lse=None, workspace=None):
     """Attention of q [T][Hq][D] to all ctx_len[r] cached states of each request (no causal mask, nothing appended)."""
     assert q.dtype == torch.bfloat16 and out.dtype == h.out_dtype and (lse is None or lse.dtype == torch.float32)
+    _rows_are_said(batch, q)
     rows = batch.total_q * h.cfg.num_q_heads
     n = rows * h.cfg.head_dim
     assert q.numel() >= n and out.numel() >= n and (lse is None or lse.numel() >= rows), "fewer rows than total_q"
@@ -326,8 +332,11 @@ def hswa_cross_attn(h: Handle, layer: Layer, batch: Batch, q, out, lse=None, wor
 
 
 def hswa_attn_weights(h: Handle, layer: Layer, batch: Batch, causal: bool, q, lse, decay: float, weights: torch.Tensor):
-    """weights: fp32 CUDA tensor [B][Hkv][stride], updated in place with the attention weights of q's rows (lse: theirs)."""
+    """weights: fp32 CUDA tensor [B][Hkv][stride], updated in place with the attention weights of q's rows (lse: theirs).
+
+    After hswa_decode_attn_mtp: a Batch with q_indptr = arange(B + 1) * q_len; an lse of -inf takes a draft's vote away."""
     assert q.dtype == torch.bfloat16 and lse.dtype == torch.float32
+    _rows_are_said(batch, q)
     B, heads, stride = weights.shape
     assert weights.dtype == torch.float32 and B == batch.batch and heads == h.cfg.num_kv_heads
     rows = batch.total_q * h.cfg.num_q_heads

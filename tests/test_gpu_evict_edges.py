@@ -218,3 +218,62 @@ def test_cross_of_a_padded_batch_without_any_token():
     hb.hswa_cross_attn(h, layer, b, to_dev_bf16(c.q), out, lse, None)
     no_error(h)
     assert (out == 7).all() and (lse == 7).all()
+
+
+def drafts(d, ctx0, q_len, seed):
+    B = len(ctx0)
+    c = Case(d, ctx0, [q_len] * B, seed=seed, causal=True, spare_blocks=1)
+    kv = wl.bf16_bits_normal(seed + 1, (B, q_len, 2, d.num_kv_heads, d.head_dim))
+    return c, np.ascontiguousarray(kv[:, :, 0]), np.ascontiguousarray(kv[:, :, 1])
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(4, 64, 16)], ids=str)
+@pytest.mark.parametrize("q_len", [2, 4])
+def test_weights_of_drafts(d, q_len):
+    """Multi-token decode steps of which some drafts are rejected: a batch with row offsets says what q's rows are, and a rejected
+    draft, whose lse is set to minus infinity, has no vote."""
+    ctx0 = np.array([300, 5, 64], np.int32)
+    c, k_new, v_new = drafts(d, ctx0, q_len, 170)
+    B, h, pool = 3, make_handle(d), to_dev_bf16(c.pool)
+    layer, q = hb.Layer(pool, False), to_dev_bf16(c.q.reshape(B, q_len, d.num_q_heads, d.head_dim))
+    ctx, head = dev_i32(ctx0), torch.zeros((B,), dtype=torch.int32, device="cuda")
+    ring = torch.zeros((B, d.ring_pages), dtype=torch.int32, device="cuda")
+    b = hb.Batch(ctx, dev_i32(c.table), ring, head, None, max_ctx_len=300)
+    out = torch.zeros((B, q_len, d.num_q_heads, d.head_dim), device="cuda")
+    lse = torch.zeros((B, q_len, d.num_q_heads), device="cuda")
+    ws = torch.empty((max(256, hb.hswa_workspace_bytes(h, B, B * q_len, 300)),), dtype=torch.uint8, device="cuda")
+    hb.hswa_decode_attn_mtp(h, layer, b, q_len, q, to_dev_bf16(k_new), to_dev_bf16(v_new), out, lse, ws)
+    accepted = np.array([q_len, 1, q_len - 1], np.int32)
+    rejected = torch.arange(q_len)[None, :] >= torch.from_numpy(accepted)[:, None]
+    lse[rejected.cuda()] = -float("inf")
+    old = np.random.default_rng(171).random((B, d.num_kv_heads, 310)).astype(np.float32)
+    w = torch.from_numpy(old).cuda()
+    with pytest.raises(AssertionError):  # one row per request is not what this q holds
+        hb.hswa_attn_weights(h, layer, b, True, q, lse, 0.75, w)
+    with pytest.raises(AssertionError):
+        hb.hswa_cross_attn(h, layer, b, q, out, lse, ws)
+    rows = hb.Batch(ctx, dev_i32(c.table), ring, head, dev_i32(c.indptr), max_q_len=q_len, total_q=B * q_len, max_ctx_len=300)
+    hb.hswa_attn_weights(h, layer, rows, True, q, lse, 0.75, w)
+    no_error(h)
+    c.pool = to_host_bits(pool)
+    check_weights(c, 0.75, lse.cpu().numpy().reshape(B * q_len, -1), old, w.cpu().numpy())
+    # the next step begins at the accepted tokens; what a rejected draft's position held counts as 0
+    indptr = np.zeros(B + 1, np.int32)
+    indptr[1:] = np.cumsum(accepted)
+    hb.hswa_step_advance(h, B, ctx, head, dev_i32(indptr))
+    before = w.cpu().numpy().copy()
+    c.ctx = ctx0 + accepted
+    c.cached = c.ctx + 1
+    c.n[:] = 1
+    c.indptr, c.q = np.arange(B + 1, dtype=np.int32), wl.bf16_bits_normal(175, (B, d.num_q_heads, d.head_dim))
+    for r in range(B):  # room for one more token
+        if c.table[r, c.ctx[r] // d.page_size] < 0:
+            c.table[r, c.ctx[r] // d.page_size] = c.free.pop()
+    nk, nv = wl.bf16_bits_normal(176, (B, d.num_kv_heads, d.head_dim)), wl.bf16_bits_normal(177, (B, d.num_kv_heads, d.head_dim))
+    b = hb.Batch(ctx, dev_i32(c.table), ring, head, None, max_ctx_len=304)
+    out, lse = torch.zeros((B, d.num_q_heads, d.head_dim), device="cuda"), torch.zeros((B, d.num_q_heads), device="cuda")
+    hb.hswa_decode_attn(h, layer, b, to_dev_bf16(c.q), to_dev_bf16(nk), to_dev_bf16(nv), out, lse, ws)
+    hb.hswa_attn_weights(h, layer, b, True, to_dev_bf16(c.q), lse, 1.0, w)
+    no_error(h)
+    c.pool = to_host_bits(pool)
+    check_weights(c, 1.0, lse.cpu().numpy(), before, w.cpu().numpy())
