@@ -300,7 +300,9 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
  *   requests may share, are only read.  Afterwards dst_block_table and kept_len take the place of block_table and ctx_len
  *   for this layer; run it for every Full layer of the step with equal kept_len, so that one ctx_len serves all.  On the
  *   SWA layers of a hybrid stack, a ctx_len cut below W - 1 hides the window's older keys: keep at least
- *   min(ctx_len, W - 1).  Ids and positions out of range are recorded as HSWA_ERR_BOUNDS and the row is not copied. */
+ *   min(ctx_len, W - 1).  Rings and ring_head stay as they are; swa_valid_from holds positions and moves with ctx_len, to
+ *   max(0, swa_valid_from - (ctx_len - kept_len)), by the caller.  Entry i of a compacted table is no longer token i, nor the
+ *   same token for every head: such a request is no donor of a prefix, with its Full KV nor its masks.  Ids and positions out of range are recorded as HSWA_ERR_BOUNDS and the row is not copied. */
 hswa_status hswa_attn_weights(hswa_handle* h, const hswa_layer* layer, const hswa_batch* batch, int32_t causal, const void* q,
                               const float* lse, float decay, float* weights, int64_t weights_stride, void* stream);
 hswa_status hswa_evict_select(hswa_handle* h, int32_t batch, const int32_t* ctx_len, int32_t max_ctx_len, const float* weights,

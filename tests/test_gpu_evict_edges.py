@@ -277,3 +277,52 @@ def test_weights_of_drafts(d, q_len):
     no_error(h)
     c.pool = to_host_bits(pool)
     check_weights(c, 1.0, lse.cpu().numpy(), before, w.cpu().numpy())
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(4, 64, 16)], ids=str)
+@pytest.mark.parametrize("kept", [[127, 200], [128, 127]])
+def test_swa_layers_of_a_hybrid_stack_after_an_eviction(d, kept):
+    """ctx_len cut to what the Full layers keep, at least W - 1: an SWA layer's ring, head and results stay what they were, and so does
+    its bookkeeping once swa_valid_from has moved by as many positions."""
+    B, ctx0 = 2, np.array([300, 1000], np.int32)
+    h, kept = make_handle(d), np.asarray(kept, np.int32)
+    C = d.ring_slots
+    pool = torch.full((B * d.ring_pages, 2, d.num_kv_heads, d.page_size, d.head_dim), float("nan"), dtype=torch.bfloat16, device="cuda")
+    ring = dev_i32(np.random.default_rng(180).permutation(B * d.ring_pages).reshape(B, -1))
+    ctx, head = dev_i32([0, 0]), dev_i32([0, 0])
+    indptr = dev_i32([0, 300, 1300])
+    kv = [to_dev_bf16(wl.bf16_bits_normal(181 + i, (1300, d.num_kv_heads, d.head_dim))) for i in range(2)]
+    table = torch.zeros((B, 1), dtype=torch.int32, device="cuda")
+    layer = hb.Layer(pool, True)
+    hb.hswa_kv_append(h, layer, hb.Batch(ctx, table, ring, head, indptr, max_q_len=1000, total_q=1300, max_ctx_len=0), *kv)
+    hb.hswa_step_advance(h, B, ctx, head, indptr)
+    valid_from = dev_i32([0, 0])
+    hb.hswa_swa_release(h, B, ctx, None, valid_from)
+    assert valid_from.tolist() == [173, 873]
+    state = pool.clone(), head.clone()
+    results = []
+    for lens in (ctx0, kept):
+        pool.copy_(state[0])
+        head.copy_(state[1])
+        ctx.copy_(torch.from_numpy(lens))
+        for k in range(3):
+            q, kn, vn = (to_dev_bf16(wl.bf16_bits_normal(190 + 3 * k + i, (B, m, d.head_dim))) for i, m in
+                         enumerate((d.num_q_heads, d.num_kv_heads, d.num_kv_heads)))
+            out, lse = torch.zeros((B, d.num_q_heads, d.head_dim), device="cuda"), torch.zeros((B, d.num_q_heads), device="cuda")
+            hb.hswa_decode_attn(h, layer, hb.Batch(ctx, table, ring, head, None, max_ctx_len=int(lens.max()) + k), q, kn, vn, out, lse)
+            hb.hswa_step_advance(h, B, ctx, head)
+            results.append((out, lse))
+    no_error(h)
+    for a, e in zip(results[3:], results[:3]):
+        assert torch.isfinite(e[0]).all() and torch.equal(a[0], e[0]) and torch.equal(a[1], e[1])
+    # the bookkeeping, moved by the positions that went
+    ctx.copy_(torch.from_numpy(kept))
+    valid_from = (valid_from - dev_i32(ctx0 - kept)).clamp_(min=0)
+    mask = torch.zeros((B, 400), dtype=torch.uint8, device="cuda")
+    hb.hswa_swa_valid_mask(h, B, ctx, valid_from, mask)
+    assert mask.sum(dim=1).tolist() == [127, 127]
+    for r in range(B):
+        assert hb.hswa_window_safe_len(int(kept[r]), 128, mask[r].cpu().numpy()) == kept[r]
+    hb.hswa_swa_release(h, B, ctx, None, valid_from)
+    assert valid_from.tolist() == [int(k) - 127 for k in kept] and C >= 129
+    no_error(h)
