@@ -59,6 +59,12 @@ class HswaError(RuntimeError):
         super().__init__(f"{what}: {status_string(status)} (status {status})")
 
 
+def _need(ok, what: str = "tensor of a wrong type, shape or size"):
+    """A check of arguments; unlike an assert statement it stays under python -O, and the library trusts the sizes it passes."""
+    if not ok:
+        raise AssertionError(what)
+
+
 _lib = None
 
 
@@ -149,7 +155,7 @@ def status_string(status: int) -> str:
 def _ptr(t: Optional[torch.Tensor]):
     if t is None:
         return None
-    assert t.is_cuda and t.is_contiguous(), "device tensors must be contiguous CUDA tensors"
+    _need(t.is_cuda and t.is_contiguous(), "device tensors must be contiguous CUDA tensors")
     return t.data_ptr()
 
 
@@ -195,7 +201,7 @@ class Layer:
     """One layer's pool: bf16 CUDA tensor [num_pages][2][Hkv][P][D]."""
 
     def __init__(self, pool: torch.Tensor, is_swa: bool):
-        assert pool.dtype == torch.bfloat16 and pool.dim() == 5 and pool.is_contiguous()
+        _need(pool.dtype == torch.bfloat16 and pool.dim() == 5 and pool.is_contiguous())
         self.pool = pool
         self.is_swa = bool(is_swa)
         self.c = hswa_layer(pool.data_ptr(), pool.shape[0], int(self.is_swa))
@@ -207,7 +213,7 @@ class Batch:
     def __init__(self, ctx_len, block_table, ring_table, ring_head, q_indptr=None, *, max_q_len=1, total_q=None,
                  max_ctx_len=0):
         for t in (ctx_len, block_table, ring_table, ring_head):
-            assert t.dtype == torch.int32 and t.is_cuda and t.is_contiguous()
+            _need(t.dtype == torch.int32 and t.is_cuda and t.is_contiguous())
         self.ctx_len, self.block_table, self.ring_table, self.ring_head, self.q_indptr = (
             ctx_len, block_table, ring_table, ring_head, q_indptr)
         B = int(ctx_len.shape[0])
@@ -245,7 +251,7 @@ def hswa_set_block_trace(h: Handle, buf: Optional[torch.Tensor]):
     if buf is None:
         _check(load().hswa_set_block_trace(h.ptr, None, 0), "hswa_set_block_trace")
         return
-    assert buf.dtype == torch.int64 and buf.is_cuda and buf.is_contiguous() and buf.dim() == 2 and buf.shape[1] == 4
+    _need(buf.dtype == torch.int64 and buf.is_cuda and buf.is_contiguous() and buf.dim() == 2 and buf.shape[1] == 4)
     _check(load().hswa_set_block_trace(h.ptr, C.c_void_p(buf.data_ptr()), int(buf.shape[0])), "hswa_set_block_trace")
 
 
@@ -316,16 +322,16 @@ def hswa_cross_workspace_need(h: Handle, batch: int, total_q: int, max_q_len: in
 
 def _rows_are_said(batch: Batch, q):
     # [B][q_len][Hq][D], as multi-token decode takes it: without row offsets its r-th row would count as request r's
-    assert batch.q_indptr is not None or q.dim() < 4 or q.shape[1] == 1, "several rows of q per request need q_indptr"
+    _need(batch.q_indptr is not None or q.dim() < 4 or q.shape[1] == 1, "several rows of q per request need q_indptr")
 
 
 def hswa_cross_attn(h: Handle, layer: Layer, batch: Batch, q, out, lse=None, workspace=None):
     """Attention of q [T][Hq][D] to all ctx_len[r] cached states of each request (no causal mask, nothing appended)."""
-    assert q.dtype == torch.bfloat16 and out.dtype == h.out_dtype and (lse is None or lse.dtype == torch.float32)
+    _need(q.dtype == torch.bfloat16 and out.dtype == h.out_dtype and (lse is None or lse.dtype == torch.float32))
     _rows_are_said(batch, q)
     rows = batch.total_q * h.cfg.num_q_heads
     n = rows * h.cfg.head_dim
-    assert q.numel() >= n and out.numel() >= n and (lse is None or lse.numel() >= rows), "fewer rows than total_q"
+    _need(q.numel() >= n and out.numel() >= n and (lse is None or lse.numel() >= rows), "fewer rows than total_q")
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(load().hswa_cross_attn(h.ptr, C.byref(layer.c), C.byref(batch.c), _ptr(q), _ptr(out), _ptr(lse), _ptr(workspace),
                                   ws_bytes, _stream()), "hswa_cross_attn")
@@ -335,12 +341,12 @@ def hswa_attn_weights(h: Handle, layer: Layer, batch: Batch, causal: bool, q, ls
     """weights: fp32 CUDA tensor [B][Hkv][stride], updated in place with the attention weights of q's rows (lse: theirs).
 
     After hswa_decode_attn_mtp: a Batch with q_indptr = arange(B + 1) * q_len; an lse of -inf takes a draft's vote away."""
-    assert q.dtype == torch.bfloat16 and lse.dtype == torch.float32
+    _need(q.dtype == torch.bfloat16 and lse.dtype == torch.float32)
     _rows_are_said(batch, q)
     B, heads, stride = weights.shape
-    assert weights.dtype == torch.float32 and B == batch.batch and heads == h.cfg.num_kv_heads
+    _need(weights.dtype == torch.float32 and B == batch.batch and heads == h.cfg.num_kv_heads)
     rows = batch.total_q * h.cfg.num_q_heads
-    assert q.numel() >= rows * h.cfg.head_dim and lse.numel() >= rows, "fewer rows than total_q"
+    _need(q.numel() >= rows * h.cfg.head_dim and lse.numel() >= rows, "fewer rows than total_q")
     _check(load().hswa_attn_weights(h.ptr, C.byref(layer.c), C.byref(batch.c), bool(causal), _ptr(q), _ptr(lse), decay, _ptr(weights),
                                     stride, _stream()), "hswa_attn_weights")
 
@@ -349,11 +355,11 @@ def hswa_evict_select(h: Handle, batch: int, ctx_len: torch.Tensor, max_ctx_len:
                       keep_idx: torch.Tensor, kept_len: torch.Tensor, *, protect_first: int = 0, protect_last: int = 0):
     """keep_idx: int32 CUDA tensor [B][Hkv][max_keep], filled with the positions of largest weight, ascending, then -1."""
     i32, heads = torch.int32, h.cfg.num_kv_heads
-    assert ctx_len.dtype == i32 and keep_len.dtype == i32 and keep_idx.dtype == i32 and kept_len.dtype == i32
+    _need(ctx_len.dtype == i32 and keep_len.dtype == i32 and keep_idx.dtype == i32 and kept_len.dtype == i32)
     w_batch, w_heads, stride = weights.shape
     k_batch, k_heads, max_keep = keep_idx.shape
-    assert weights.dtype == torch.float32 and w_batch == k_batch == batch and w_heads == k_heads == heads
-    assert ctx_len.numel() >= batch and keep_len.numel() >= batch and kept_len.numel() >= batch
+    _need(weights.dtype == torch.float32 and w_batch == k_batch == batch and w_heads == k_heads == heads)
+    _need(ctx_len.numel() >= batch and keep_len.numel() >= batch and kept_len.numel() >= batch)
     _check(load().hswa_evict_select(h.ptr, batch, _ptr(ctx_len), max_ctx_len, _ptr(weights), stride, _ptr(keep_len), max_keep,
                                     protect_first, protect_last, _ptr(keep_idx), _ptr(kept_len), _stream()), "hswa_evict_select")
 
@@ -363,18 +369,18 @@ def hswa_evict_compact(h: Handle, layer: Layer, batch: Batch, keep_idx: torch.Te
                        weights_out: Optional[torch.Tensor] = None):
     """Copies the kept K/V rows (and weights) of batch's block table to the pages of dst_block_table [B][blocks]."""
     i32, f32 = torch.int32, torch.float32
-    assert keep_idx.dtype == i32 and kept_len.dtype == i32 and dst_block_table.dtype == i32
-    assert (weights is None or weights.dtype == f32) and (weights_out is None or weights_out.dtype == f32)
+    _need(keep_idx.dtype == i32 and kept_len.dtype == i32 and dst_block_table.dtype == i32)
+    _need((weights is None or weights.dtype == f32) and (weights_out is None or weights_out.dtype == f32))
     B, heads, max_keep = keep_idx.shape
     dst_batch, dst_blocks = dst_block_table.shape
-    assert B == dst_batch == batch.batch and heads == h.cfg.num_kv_heads and kept_len.numel() >= B
+    _need(B == dst_batch == batch.batch and heads == h.cfg.num_kv_heads and kept_len.numel() >= B)
     stride = out_stride = 0
     if weights is not None:
         w_batch, w_heads, stride = weights.shape
-        assert w_batch == B and w_heads == heads
+        _need(w_batch == B and w_heads == heads)
     if weights_out is not None:
         w_batch, w_heads, out_stride = weights_out.shape
-        assert w_batch == B and w_heads == heads
+        _need(w_batch == B and w_heads == heads)
     _check(load().hswa_evict_compact(h.ptr, C.byref(layer.c), C.byref(batch.c), _ptr(keep_idx), _ptr(kept_len), max_keep,
                                      _ptr(dst_block_table), dst_blocks, _ptr(weights), stride, _ptr(weights_out), out_stride, _stream()),
            "hswa_evict_compact")
@@ -384,12 +390,12 @@ def hswa_window_safe_len(match_len: int, window: int, swa_valid) -> int:
     """Largest usable hit length given the donor's per-position SWA validity (any uint8 buffer / numpy array)."""
     import numpy as np
     v = np.ascontiguousarray(swa_valid, dtype=np.uint8)
-    assert v.shape[0] >= match_len
+    _need(v.shape[0] >= match_len)
     return int(load().hswa_window_safe_len(int(match_len), int(window), C.c_void_p(v.ctypes.data)))
 
 
 def _any_ptr(t: torch.Tensor):
-    assert t.is_contiguous() and (t.is_cuda or t.is_pinned()), "buffer must be a CUDA tensor or pinned host memory"
+    _need(t.is_contiguous() and (t.is_cuda or t.is_pinned()), "buffer must be a CUDA tensor or pinned host memory")
     return C.c_void_p(t.data_ptr())
 
 
@@ -406,14 +412,14 @@ def hswa_swa_window_scatter(h: Handle, layer: Layer, batch: Batch, buf: torch.Te
 def hswa_swa_release(h: Handle, batch: int, ctx_len: torch.Tensor, release: Optional[torch.Tensor],
                      swa_valid_from: torch.Tensor):
     """release: uint8 CUDA tensor [B] (None: every request releases); swa_valid_from: int32 CUDA tensor [B], in place."""
-    assert swa_valid_from.dtype == torch.int32 and (release is None or release.dtype == torch.uint8)
+    _need(swa_valid_from.dtype == torch.int32 and (release is None or release.dtype == torch.uint8))
     _check(load().hswa_swa_release(h.ptr, batch, _ptr(ctx_len), _ptr(release), _ptr(swa_valid_from), _stream()),
            "hswa_swa_release")
 
 
 def hswa_swa_valid_mask(h: Handle, batch: int, ctx_len: torch.Tensor, swa_valid_from: torch.Tensor, mask: torch.Tensor):
     """mask: uint8 [B][stride], CUDA or pinned host."""
-    assert mask.dtype == torch.uint8 and mask.dim() == 2 and mask.shape[0] == batch
+    _need(mask.dtype == torch.uint8 and mask.dim() == 2 and mask.shape[0] == batch)
     _check(load().hswa_swa_valid_mask(h.ptr, batch, _ptr(ctx_len), _ptr(swa_valid_from), int(mask.shape[1]), _any_ptr(mask),
                                       _stream()), "hswa_swa_valid_mask")
 
@@ -422,7 +428,7 @@ def hswa_prefix_hit_len(match_len: int, window: int, full_valid, swa_valid) -> i
     import numpy as np
     f = np.ascontiguousarray(full_valid, dtype=np.uint8)
     s = np.ascontiguousarray(swa_valid, dtype=np.uint8)
-    assert f.shape[0] >= match_len and s.shape[0] >= match_len
+    _need(f.shape[0] >= match_len and s.shape[0] >= match_len)
     return int(load().hswa_prefix_hit_len(int(match_len), int(window), C.c_void_p(f.ctypes.data), C.c_void_p(s.ctypes.data)))
 
 
