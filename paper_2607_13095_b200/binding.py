@@ -159,9 +159,25 @@ def _ptr(t: Optional[torch.Tensor]):
     return t.data_ptr()
 
 
+_device = torch._C._cuda_getDevice
+_raw_stream = torch._C._cuda_getCurrentRawStream  # (without the Stream object around it: 0.2 us a call instead of 3.4 us)
+
+
 def _stream():
-    # (the stream's handle without the Stream object around it: 0.2 us a call instead of 3.4 us)
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return _raw_stream(_device())
+
+
+def _ptrs(dev: int, *tensors):
+    """Addresses of contiguous tensors on CUDA device `dev` (None stays None)."""
+    at = []
+    for t in tensors:
+        if t is None:
+            at.append(None)
+        elif t.get_device() != dev or not t.is_contiguous():
+            raise AssertionError("device tensors must be contiguous CUDA tensors on the current device")
+        else:
+            at.append(t.data_ptr())
+    return at
 
 
 def _check(status: int, what: str):
@@ -203,8 +219,10 @@ class Layer:
     def __init__(self, pool: torch.Tensor, is_swa: bool):
         _need(pool.dtype == torch.bfloat16 and pool.dim() == 5 and pool.is_contiguous())
         self.pool = pool
+        self.device = pool.get_device()
         self.is_swa = bool(is_swa)
         self.c = hswa_layer(pool.data_ptr(), pool.shape[0], int(self.is_swa))
+        self.ref = C.byref(self.c)
 
 
 class Batch:
@@ -218,12 +236,17 @@ class Batch:
             ctx_len, block_table, ring_table, ring_head, q_indptr)
         B = int(ctx_len.shape[0])
         self.batch = B
+        self.device = ctx_len.get_device()
+        # (what the calls on Full layers' contexts ask of the arrays besides their types)
+        self.covers_batch = block_table.dim() == 2 and block_table.shape[0] >= B and (
+            q_indptr is None or (q_indptr.dtype == torch.int32 and q_indptr.is_cuda and q_indptr.is_contiguous() and q_indptr.numel() > B))
         self.total_q = B if total_q is None else int(total_q)
         self.max_q_len = int(max_q_len)
         self.c = hswa_batch(
             B, ctx_len.data_ptr(), None if q_indptr is None else q_indptr.data_ptr(), block_table.data_ptr(),
             int(block_table.shape[1]) if block_table.dim() == 2 else 0, ring_table.data_ptr(), ring_head.data_ptr(),
             self.max_q_len, self.total_q, int(max_ctx_len))
+        self.ref = C.byref(self.c)
 
 
 def hswa_workspace_bytes(h: Handle, max_batch: int, max_total_q: int, max_ctx_len: int) -> int:
@@ -320,6 +343,16 @@ def hswa_cross_workspace_need(h: Handle, batch: int, total_q: int, max_q_len: in
     return int(load().hswa_cross_workspace_need(h.ptr, batch, total_q, max_q_len, max_ctx_len))
 
 
+def _device_of(layer: Layer, batch: Batch) -> int:
+    """The current device, which has to be that of the layer and the batch."""
+    if not batch.covers_batch:
+        raise AssertionError("block_table needs a row per request and q_indptr, int32, one entry more")
+    dev = _device()
+    if not layer.device == batch.device == dev:
+        raise AssertionError("layer or batch on another device than the current one")
+    return dev
+
+
 def _rows_are_said(batch: Batch, q):
     # [B][q_len][Hq][D], as multi-token decode takes it: without row offsets its r-th row would count as request r's
     _need(batch.q_indptr is not None or q.dim() < 4 or q.shape[1] == 1, "several rows of q per request need q_indptr")
@@ -333,8 +366,9 @@ def hswa_cross_attn(h: Handle, layer: Layer, batch: Batch, q, out, lse=None, wor
     n = rows * h.cfg.head_dim
     _need(q.numel() >= n and out.numel() >= n and (lse is None or lse.numel() >= rows), "fewer rows than total_q")
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(load().hswa_cross_attn(h.ptr, C.byref(layer.c), C.byref(batch.c), _ptr(q), _ptr(out), _ptr(lse), _ptr(workspace),
-                                  ws_bytes, _stream()), "hswa_cross_attn")
+    dev = _device_of(layer, batch)
+    _check(load().hswa_cross_attn(h.ptr, layer.ref, batch.ref, *_ptrs(dev, q, out, lse, workspace), ws_bytes, _raw_stream(dev)),
+           "hswa_cross_attn")
 
 
 def hswa_attn_weights(h: Handle, layer: Layer, batch: Batch, causal: bool, q, lse, decay: float, weights: torch.Tensor):
@@ -347,8 +381,10 @@ def hswa_attn_weights(h: Handle, layer: Layer, batch: Batch, causal: bool, q, ls
     _need(weights.dtype == torch.float32 and B == batch.batch and heads == h.cfg.num_kv_heads)
     rows = batch.total_q * h.cfg.num_q_heads
     _need(q.numel() >= rows * h.cfg.head_dim and lse.numel() >= rows, "fewer rows than total_q")
-    _check(load().hswa_attn_weights(h.ptr, C.byref(layer.c), C.byref(batch.c), bool(causal), _ptr(q), _ptr(lse), decay, _ptr(weights),
-                                    stride, _stream()), "hswa_attn_weights")
+    dev = _device_of(layer, batch)
+    q_at, lse_at, weights_at = _ptrs(dev, q, lse, weights)
+    _check(load().hswa_attn_weights(h.ptr, layer.ref, batch.ref, bool(causal), q_at, lse_at, decay, weights_at, stride,
+                                    _raw_stream(dev)), "hswa_attn_weights")
 
 
 def hswa_evict_select(h: Handle, batch: int, ctx_len: torch.Tensor, max_ctx_len: int, weights: torch.Tensor, keep_len: torch.Tensor,
@@ -360,8 +396,10 @@ def hswa_evict_select(h: Handle, batch: int, ctx_len: torch.Tensor, max_ctx_len:
     k_batch, k_heads, max_keep = keep_idx.shape
     _need(weights.dtype == torch.float32 and w_batch == k_batch == batch and w_heads == k_heads == heads)
     _need(ctx_len.numel() >= batch and keep_len.numel() >= batch and kept_len.numel() >= batch)
-    _check(load().hswa_evict_select(h.ptr, batch, _ptr(ctx_len), max_ctx_len, _ptr(weights), stride, _ptr(keep_len), max_keep,
-                                    protect_first, protect_last, _ptr(keep_idx), _ptr(kept_len), _stream()), "hswa_evict_select")
+    dev = _device()
+    ctx_at, weights_at, keep_at, idx_at, kept_at = _ptrs(dev, ctx_len, weights, keep_len, keep_idx, kept_len)
+    _check(load().hswa_evict_select(h.ptr, batch, ctx_at, max_ctx_len, weights_at, stride, keep_at, max_keep, protect_first,
+                                    protect_last, idx_at, kept_at, _raw_stream(dev)), "hswa_evict_select")
 
 
 def hswa_evict_compact(h: Handle, layer: Layer, batch: Batch, keep_idx: torch.Tensor, kept_len: torch.Tensor,
@@ -381,9 +419,10 @@ def hswa_evict_compact(h: Handle, layer: Layer, batch: Batch, keep_idx: torch.Te
     if weights_out is not None:
         w_batch, w_heads, out_stride = weights_out.shape
         _need(w_batch == B and w_heads == heads)
-    _check(load().hswa_evict_compact(h.ptr, C.byref(layer.c), C.byref(batch.c), _ptr(keep_idx), _ptr(kept_len), max_keep,
-                                     _ptr(dst_block_table), dst_blocks, _ptr(weights), stride, _ptr(weights_out), out_stride, _stream()),
-           "hswa_evict_compact")
+    dev = _device_of(layer, batch)
+    idx_at, kept_at, dst_at, weights_at, out_at = _ptrs(dev, keep_idx, kept_len, dst_block_table, weights, weights_out)
+    _check(load().hswa_evict_compact(h.ptr, layer.ref, batch.ref, idx_at, kept_at, max_keep, dst_at, dst_blocks, weights_at, stride,
+                                     out_at, out_stride, _raw_stream(dev)), "hswa_evict_compact")
 
 
 def hswa_window_safe_len(match_len: int, window: int, swa_valid) -> int:

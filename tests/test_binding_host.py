@@ -3,8 +3,10 @@ import subprocess
 import sys
 
 import pytest
+import torch
 
 from conftest import ROOT
+from paper_2607_13095_b200 import binding as hb
 
 CHECKS = """
 from types import SimpleNamespace as N
@@ -49,3 +51,38 @@ def test_wrong_tensors_are_refused(flags):
     """Also where python drops assert statements."""
     run = subprocess.run([sys.executable, *flags, "-c", CHECKS], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert run.returncode == 0 and "refused 17" in run.stdout, run.stderr[-2000:] + run.stdout
+
+
+class OnDevice:
+    """A stand-in for a contiguous CUDA tensor of a device."""
+
+    def __init__(self, t, device):
+        self.t, self.device = t, device
+        self.is_cuda, self.dtype, self.shape = True, t.dtype, t.shape
+        self.is_contiguous, self.dim, self.numel, self.element_size = t.is_contiguous, t.dim, t.numel, t.element_size
+
+    def get_device(self):
+        return self.device
+
+    def data_ptr(self):
+        return 4096
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    monkeypatch.setattr(hb, "_device", lambda: 0)
+    assert hb._ptrs(0, OnDevice(torch.zeros(4), 0), None) == [4096, None]
+    for bad in (OnDevice(torch.zeros(4), 1), OnDevice(torch.zeros(4, 4).t(), 0), torch.zeros(4)):
+        with pytest.raises(AssertionError, match="current device"):
+            hb._ptrs(0, OnDevice(torch.zeros(4), 0), bad)
+    i32 = torch.int32
+    ints = lambda *shape, device=0: OnDevice(torch.zeros(shape, dtype=i32), device)  # noqa: E731
+    pool = lambda device=0: hb.Layer(OnDevice(torch.zeros((1, 2, 1, 16, 64), dtype=torch.bfloat16), device), False)  # noqa: E731
+    batch = lambda device=0, table=(2, 3), indptr=None: hb.Batch(  # noqa: E731
+        ints(2, device=device), ints(*table, device=device), ints(2, 9), ints(2), indptr, max_ctx_len=9)
+    hb._device_of(pool(), batch())
+    hb._device_of(pool(), batch(indptr=ints(3)))
+    hb._device_of(pool(), batch(table=(4, 3), indptr=ints(7)))
+    for layer, b in ((pool(1), batch()), (pool(), batch(1)), (pool(), batch(table=(1, 3))), (pool(), batch(indptr=ints(2))),
+                     (pool(), batch(indptr=OnDevice(torch.zeros(3, dtype=torch.int64), 0)))):
+        with pytest.raises(AssertionError):
+            hb._device_of(layer, b)
