@@ -326,3 +326,167 @@ def test_swa_layers_of_a_hybrid_stack_after_an_eviction(d, kept):
     hb.hswa_swa_release(h, B, ctx, None, valid_from)
     assert valid_from.tolist() == [int(k) - 127 for k in kept] and C >= 129
     no_error(h)
+
+
+def scale_err(scale):
+    """Relative error of a probability where the score's error bound of 2^-10 (before the scale) is multiplied by `scale`."""
+    return scale * 2.0 ** -10 + S_ERR
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(5, 64, 16), dims(1, 128, 32)], ids=str)
+@pytest.mark.parametrize("n", [1, 3, 200])
+@pytest.mark.parametrize("sm_scale", [0.5, 1.0, 3.0])
+@pytest.mark.parametrize("ctx", [[3000, 500], [9000, 70, 0, 1200] * 12])
+def test_cross_of_growing_maxima(d, n, sm_scale, ctx):
+    """Scores so far apart that row maxima grow by more than the lazy rescale's slack (8 in log2 units) from tile to tile; every
+    form, with and without slices."""
+    ctx = ctx if n < 200 else ctx[:4]
+    c = Case(d, ctx, [n] * len(ctx), seed=200)
+    c.scale = sm_scale
+    S = scale_err(sm_scale)
+    K, Q = ref.rows(c.pool, c.table, 0, ctx[0], 0), wl.bits_to_f64(c.q[:n])
+    s = np.einsum("ihd,jd->ihj", Q[:, : d.group], K[:, 0]) * sm_scale * 1.4427
+    assert sm_scale < 1 or (s.max(axis=-1) - s[..., :128].max(axis=-1) > 8).any(), "no row's maximum grows enough"
+    h, b, T = make_handle(d, sm_scale=sm_scale), c.batch(), int(c.indptr[-1])
+    out, lse = torch.zeros((T, d.num_q_heads, d.head_dim), device="cuda"), torch.zeros((T, d.num_q_heads), device="cuda")
+    hb.hswa_cross_attn(h, hb.Layer(to_dev_bf16(c.pool), False), b, to_dev_bf16(c.q), out, lse, workspace(h, b))
+    no_error(h)
+    want, want_lse, mag = ref.cross_attention(c.pool, c.table, c.ctx, c.indptr, c.q, sm_scale)
+    assert (np.abs(out.double().cpu().numpy() - want) <= (2.0 ** -8 + 2 * S) * mag + 1e-7).all()
+    some = np.isfinite(want_lse)
+    got_lse = lse.double().cpu().numpy()
+    assert (np.abs(got_lse - want_lse)[some] <= S).all() and (got_lse[~some] == -np.inf).all()
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(5, 64, 16)], ids=str)
+@pytest.mark.parametrize("n", [1, 3, 60])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("sm_scale", [0.03125, 1.0])
+def test_weights_at_other_scales(d, n, causal, sm_scale):
+    c = Case(d, [900, 40, 0], [n, n, n], seed=210, causal=causal)
+    c.scale = sm_scale
+    lse, old = weights_inputs(c, 211)
+    h, w = make_handle(d, sm_scale=sm_scale), torch.from_numpy(old).cuda()
+    hb.hswa_attn_weights(h, hb.Layer(to_dev_bf16(c.pool), False), c.batch(), causal, to_dev_bf16(c.q), torch.from_numpy(lse).cuda(), 0.5, w)
+    no_error(h)
+    want = ref.attn_weights(c.pool, c.table, c.ctx, c.indptr, c.q, lse, sm_scale, causal, 0.5, old)
+    # (|lse| < 256 here: x = s log2(e) - lse log2(e) is rounded to 2^-24 of that, 2^-15 relative to 2^x, within S_ERR)
+    assert (np.abs(w.cpu().numpy() - want) <= (scale_err(sm_scale) + (n * d.group + 2) * 2.0 ** -24) * want + 1e-30).all()
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(4, 64, 16)], ids=str)
+@pytest.mark.parametrize("n", [1, 5])
+def test_cross_join_of_many_slices_in_bf16(d, n):
+    c = Case(d, [9000], [n], seed=220)
+    check_cross(c, *run_cross(c, torch.bfloat16), torch.bfloat16)
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(5, 64, 16), dims(8, 128, 32)], ids=str)
+def test_weights_with_the_lse_of_a_prefill(d):
+    """A prompt's prefill, whose lse goes into the weights; a second call lets the last tokens alone vote."""
+    ctx0, n = np.array([130, 0, 77], np.int32), np.array([200, 40, 3], np.int32)
+    c = Case(d, ctx0, n, seed=230, causal=True)
+    h, pool, b, T = make_handle(d), to_dev_bf16(c.pool), c.batch(), int(c.indptr[-1])
+    layer, q = hb.Layer(pool, False), to_dev_bf16(c.q)
+    kn, vn = (to_dev_bf16(wl.bf16_bits_normal(231 + i, (T, d.num_kv_heads, d.head_dim))) for i in range(2))
+    out, lse = torch.zeros((T, d.num_q_heads, d.head_dim), device="cuda"), torch.zeros((T, d.num_q_heads), device="cuda")
+    hb.hswa_prefill_attn(h, layer, b, q, kn, vn, True, out, lse)
+    old = np.zeros((3, d.num_kv_heads, 340), np.float32)
+    w = torch.from_numpy(old.copy()).cuda()
+    hb.hswa_attn_weights(h, layer, b, True, q, lse, 0.0, w)
+    no_error(h)
+    c.pool = to_host_bits(pool)
+    check_weights(c, 0.0, lse.cpu().numpy(), old, w.cpu().numpy())
+    total = w.double().sum(dim=-1).cpu().numpy()
+    # every row's probabilities sum to one (the prefill's lse sums rounded ones where it sums them so: 2^-8)
+    assert np.allclose(total, (n * d.group)[:, None], rtol=2.0 ** -8 + 2 * S_ERR, atol=0)
+    last = 2  # the last two tokens of each prompt, the context that much longer
+    keep = np.concatenate([np.arange(int(e) - last, int(e)) for e in c.indptr[1:]])
+    c.ctx, c.n, c.indptr, c.q = ctx0 + n - last, np.full(3, last, np.int32), np.arange(4, dtype=np.int32) * last, c.q[keep]
+    w = torch.from_numpy(old.copy()).cuda()
+    hb.hswa_attn_weights(h, layer, c.batch(), True, to_dev_bf16(c.q), lse[torch.from_numpy(keep).cuda()].contiguous(), 0.0, w)
+    no_error(h)
+    check_weights(c, 0.0, lse.cpu().numpy()[keep], old, w.cpu().numpy())
+
+
+@pytest.mark.parametrize("d", [dims(5, 128, 32), dims(8, 64, 64)], ids=str)
+def test_encoder_states_appended_then_attended(d):
+    """The states enter the pages by hswa_kv_append, in two chunks; tokens attend to all of them."""
+    c = Case(d, [150, 0, 77], [20, 3, 1], seed=240)
+    blank = np.full_like(c.pool, NAN_BITS)
+    h, pool = make_handle(d), to_dev_bf16(blank)
+    layer, table = hb.Layer(pool, False), dev_i32(c.table)
+    ctx, head = dev_i32([0, 0, 0]), dev_i32([0, 0, 0])
+    ring = torch.zeros((3, d.ring_pages), dtype=torch.int32, device="cuda")
+    done = np.zeros(3, np.int64)
+    for part in ([100, 0, 77], [50, 0, 0]):
+        kv = []
+        for which in (0, 1):
+            rows = [c.pool[c.table[r, p // d.page_size], which, :, p % d.page_size] for r in range(3) for p in range(done[r], done[r] + part[r])]
+            kv.append(to_dev_bf16(np.stack(rows)))
+        indptr = dev_i32(np.concatenate([[0], np.cumsum(part)]))
+        hb.hswa_kv_append(h, layer, hb.Batch(ctx, table, ring, head, indptr, max_q_len=max(part), total_q=sum(part), max_ctx_len=int(done.max())), *kv)
+        hb.hswa_step_advance(h, 3, ctx, head, indptr)
+        done += part
+    assert ctx.tolist() == [150, 0, 77]
+    b = hb.Batch(ctx, table, ring, head, dev_i32(c.indptr), max_q_len=20, total_q=24, max_ctx_len=150)
+    out, lse = torch.zeros((24, d.num_q_heads, d.head_dim), device="cuda"), torch.zeros((24, d.num_q_heads), device="cuda")
+    hb.hswa_cross_attn(h, layer, b, to_dev_bf16(c.q), out, lse, workspace(h, b))
+    no_error(h)
+    check_cross(c, out.double().cpu().numpy(), lse.double().cpu().numpy())
+
+
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(4, 64, 16, 1)], ids=str)
+def test_compact_of_positions_in_any_order_and_twice(d):
+    """keep_idx by the caller: descending, and one position many times."""
+    c = Case(d, [300, 70], [1, 1], seed=250)
+    kept = np.array([90, 70], np.int32)
+    idx = np.full((2, d.num_kv_heads, 90), -1, np.int32)
+    idx[0], idx[1, :, :70] = np.arange(299, 209, -1), 69
+    blocks = -(-90 // d.page_size)
+    dst = (len(c.pool) + np.arange(2 * blocks)).reshape(2, blocks)
+    c.pool = np.concatenate([c.pool, np.full((2 * blocks, *c.pool.shape[1:]), NAN_BITS, np.uint16)])
+    h, pool = make_handle(d), to_dev_bf16(c.pool)
+    hb.hswa_evict_compact(h, hb.Layer(pool, False), c.batch(), dev_i32(idx), dev_i32(kept), dev_i32(dst))
+    no_error(h)
+    assert np.array_equal(to_host_bits(pool), ref.evict_compact(c.pool, c.table, idx, kept, dst))
+
+
+def test_several_streams_at_once():
+    """Cross attention, weights and a choice of positions on several streams at a time, each with its own handle and workspace: every
+    result is that of the call by itself."""
+    jobs = []
+    for i, (d, n) in enumerate([(dims(8, 128, 64, 4), 64), (dims(8, 64, 16, 4), 5), (dims(5, 128, 32, 4), 13), (dims(8, 128, 64, 4), 1)]):
+        rng = np.random.default_rng(260 + i)
+        c = Case(d, rng.integers(1, 900, 24), [n] * 24, seed=261 + i)
+        h, b, T = make_handle(d), c.batch(), int(c.indptr[-1])
+        j = dict(h=h, b=b, layer=hb.Layer(to_dev_bf16(c.pool), False), q=to_dev_bf16(c.q), ws=workspace(h, b), keep=dev_i32([40] * 24))
+        j["out"], j["lse"] = torch.zeros((T, d.num_q_heads, d.head_dim), device="cuda"), torch.zeros((T, d.num_q_heads), device="cuda")
+        j["w"] = torch.zeros((24, 4, 900), device="cuda")
+        j["idx"], j["kept"] = torch.zeros((24, 4, 40), dtype=torch.int32, device="cuda"), torch.zeros((24,), dtype=torch.int32, device="cuda")
+        jobs.append(j)
+
+    def run(j):
+        hb.hswa_cross_attn(j["h"], j["layer"], j["b"], j["q"], j["out"], j["lse"], j["ws"])
+        hb.hswa_attn_weights(j["h"], j["layer"], j["b"], False, j["q"], j["lse"], 0.0, j["w"])
+        hb.hswa_evict_select(j["h"], 24, j["b"].ctx_len, 900, j["w"], j["keep"], j["idx"], j["kept"], protect_last=4)
+
+    names = ("out", "lse", "w", "idx", "kept")
+    for j in jobs:
+        run(j)
+    torch.cuda.synchronize()
+    want = [[j[k].clone() for k in names] for j in jobs]
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(10):
+        for j in jobs:
+            for k in names:
+                j[k].zero_()
+        torch.cuda.synchronize()
+        for j, s in zip(jobs, streams):
+            with torch.cuda.stream(s):
+                run(j)
+        torch.cuda.synchronize()
+        for j, e in zip(jobs, want):
+            assert all(torch.equal(j[k], x) for k, x in zip(names, e))
+    for j in jobs:
+        no_error(j["h"])
