@@ -316,19 +316,20 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     t0 = p.b.q_indptr[r];
     n = p.b.q_indptr[r + 1] - t0;
     const int len = p.b.ctx_len[r];
+    auto has_row = [&](int tok) { return (unsigned)t0 + (unsigned)tok < (unsigned)p.total_q; };  // q_indptr may name rows without storage
     if (threadIdx.x == 0 && blockIdx.x == 0 && kh == 0) {  // the grid was sized from the host's bounds
       if (len < 0 || len > p.max_ctx_len) record_error(p.err, HSWA_ERR_BOUNDS, r, -1, len);
       if (n < 0 || n > p.max_q_len || t0 < 0 || (int64_t)t0 + n > p.total_q) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, n);
     }
-    n = t0 < 0 ? 0 : min(n, p.total_q - t0);  // (rows past total_q have no storage)
     head = 0;
     h0 = kh * M.G;
     tok_tile = BM / M.G;
     if (p.max_splits > 1 && b == 0 && slice == 0) {
       // rows past the last row tile have no block: a mark tells the join to leave them alone
-      const int64_t first = (int64_t)max_tiles * NQ * tok_tile, last = n;
-      for (int64_t row = first * M.G + threadIdx.x; row < last * M.G; row += THREADS)
-        p.part_ml[((t0 + row / M.G) * M.Hq + h0 + row % M.G) * p.max_splits] = make_float2(-INFINITY, -1.f);
+      const int64_t last = min((int64_t)n, (int64_t)p.total_q - t0);
+      for (int64_t tok = (int64_t)max_tiles * NQ * tok_tile + threadIdx.x; tok < last; tok += THREADS)
+        if (has_row((int)tok))
+          for (int g = 0; g < M.G; ++g) p.part_ml[((t0 + tok) * M.Hq + h0 + g) * p.max_splits] = make_float2(-INFINITY, -1.f);
     }
     if (b * NQ * tok_tile >= n) return;  // uniform for the block
     nq_tiles = NQ == 2 && (b * 2 + 1) * tok_tile < n ? 2 : 1;
@@ -343,6 +344,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
       const int rows = min(NQ * tok_tile, n - b * NQ * tok_tile) * M.G;
       for (int row = threadIdx.x; row < rows; row += THREADS) {
         const int64_t orow = (int64_t)(t0 + b * NQ * tok_tile + row / M.G) * M.Hq + h0 + row % M.G;
+        if (!has_row(b * NQ * tok_tile + row / M.G)) continue;
         if (p.max_splits > 1) {
           p.part_ml[orow * p.max_splits + slice] = make_float2(-INFINITY, 0.f);
           continue;
@@ -844,7 +846,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     tc_fence_after();
     const float l_tot = l_run;
     const int tok = CROSS ? (NQ * b + i) * tok_tile + rr / M.G : 0;  // CROSS: this row's token and its output row
-    const bool tok_ok = CROSS && here && rr < tok_tile * M.G && tok < n;
+    const bool tok_ok = CROSS && here && rr < tok_tile * M.G && tok < n && (unsigned)t0 + (unsigned)tok < (unsigned)p.total_q;  // (has_row)
     const int64_t cross_row = CROSS ? (int64_t)(t0 + tok) * M.Hq + h0 + rr % M.G : 0;
     if (PREFIX || (CROSS && p.max_splits > 1)) {
       // partial for the split-K combine: row = (request, head) or (token, head), unnormalised o with its (m, l)
