@@ -460,17 +460,15 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_pool, const DecodeParams p)
   for (int idx = threadIdx.x; idx < M.G * D; idx += blockDim.x) {
     const int g = idx / D, d = idx % D;
     float mm = -INFINITY;
-    bool sums = false;  // CROSS: scores that are all NaN leave a sum of NaN without a maximum
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      mm = fmaxf(mm, sc_ml[(w * 8 + g) * 2]);
-      if constexpr (CROSS) sums |= sc_ml[(w * 8 + g) * 2 + 1] != 0.f;
-    }
+    for (int w = 0; w < NW; ++w) mm = fmaxf(mm, sc_ml[(w * 8 + g) * 2]);
     float L = 0.f, O = 0.f;
-    if (mm != -INFINITY || sums) {
+    // CROSS: scores that are all NaN leave sums of NaN without a maximum, which a factor of 0 = 2^(-inf - 0) keeps
+    const float m_ref = CROSS && mm == -INFINITY ? 0.f : mm;
+    if (CROSS || mm != -INFINITY) {
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
-        const float f = fast_exp2(sc_ml[(w * 8 + g) * 2] - mm);
+        const float f = fast_exp2(sc_ml[(w * 8 + g) * 2] - m_ref);
         L += f * sc_ml[(w * 8 + g) * 2 + 1];
         O += f * sc_o[(w * 8 + g) * D + d];
       }
@@ -522,24 +520,19 @@ __global__ void __launch_bounds__(128) combine_kernel(const DecodeParams p) {
   const float2* ml = p.part_ml + row * p.max_splits;
   const float* po = p.part_o + row * p.max_splits * D;
   float mm = -INFINITY;
-  bool sums = false;  // CROSS: as in decode_kernel
-  for (int s = lane; s < n_splits; s += 32) {
-    const float2 v = ml[s];
-    mm = fmaxf(mm, v.x);
-    if constexpr (CROSS) sums |= v.y != 0.f;
-  }
+  for (int s = lane; s < n_splits; s += 32) mm = fmaxf(mm, ml[s].x);
 #pragma unroll
   for (int sh = 16; sh >= 1; sh >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, sh));
-  if constexpr (CROSS) sums = __any_sync(0xffffffffu, sums);
+  const float m_ref = CROSS && mm == -INFINITY ? 0.f : mm;  // as in decode_kernel
   constexpr int PER = D / 32;
   float acc[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) acc[i] = 0.f;
   float L = 0.f;
-  if (mm != -INFINITY || sums) {
+  if (CROSS || mm != -INFINITY) {
     for (int s = sub; s < n_splits; s += WPR) {
       const float2 v = ml[s];
-      const float f = fast_exp2(v.x - mm);
+      const float f = fast_exp2(v.x - m_ref);
       L += f * v.y;
       if constexpr (PER == 4) {
         const float4 x = *reinterpret_cast<const float4*>(po + (int64_t)s * D + lane * 4);
