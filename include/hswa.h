@@ -244,15 +244,15 @@ hswa_status hswa_prefill_attn(hswa_handle* h, const hswa_layer* layer, const hsw
 
 /* Cross attention to an encoder's states of another length (paper Sec. 3.1.1: one logical view over paged storage; the
  * states are the cached context of a Full layer, written with hswa_kv_append).  Request r attends with its n[r] decoder
- * tokens to ALL of its ctx_len[r] cached positions: no causal mask, nothing is appended.  ctx_len[r] = 0 gives zeros and
- * an lse of minus infinity; n[r] = 0 leaves nothing to do for the request.
+ * tokens to ALL of its ctx_len[r] cached positions: no causal mask, nothing is appended.  ctx_len[r] = 0 gives zeros
+ * and an lse of minus infinity; n[r] = 0 leaves nothing to do for the request.
  * q: device bf16 [T][Hq][D]; out: device [T][Hq][D] in cfg.out_dtype; lse: device fp32 [T][Hq] or NULL.
- * batch->q_indptr may be NULL (one token per request, the serving step); with it, rows of q behind the last request's do
- * not matter and those of out and lse are left as they were (max_q_len = 0: all of them).  Probabilities enter the PV product as bf16; row sums and
- * lse are taken over the fp32 values.  Workspace: hswa_cross_workspace_need bytes (0: none needed), else
- * HSWA_ERR_WORKSPACE.  The block table must cover max_ctx_len and the layer must not be an SWA layer
- * (HSWA_ERR_INVALID_ARG); max_ctx_len is at most 2^30, for single tokens 65535 * 4096 (HSWA_ERR_UNSUPPORTED, the need is
- * then 0).  A request longer than max_ctx_len or max_q_len, or with row offsets outside [0, total_q], is recorded as
+ * batch->q_indptr may be NULL (one token per request, the serving step); with it, rows of q behind the last request's
+ * do not matter and those of out and lse are left as they were (max_q_len = 0: all of them).  Probabilities enter the
+ * PV product as bf16; row sums and lse are taken over the fp32 values.  Workspace: hswa_cross_workspace_need bytes (0:
+ * none needed), else HSWA_ERR_WORKSPACE.  The block table must cover max_ctx_len and the layer must not be an SWA layer
+ * (HSWA_ERR_INVALID_ARG); max_ctx_len is at most 2^30, for single tokens 65535 * 4096 (HSWA_ERR_UNSUPPORTED, the need
+ * is then 0).  A request longer than max_ctx_len or max_q_len, or with row offsets outside [0, total_q], is recorded as
  * HSWA_ERR_BOUNDS (index -1 / -2 / -2); what the bounds cover is computed, other rows of out and lse stay as they were.
  *
  * This call and the eviction calls below refuse a current device other than the handle's (HSWA_ERR_INVALID_ARG).
@@ -267,42 +267,45 @@ hswa_status hswa_cross_attn(hswa_handle* h, const hswa_layer* layer, const hswa_
  * (request, KV head) keeps its own positions: the cache stores rotated keys and a Full layer attends to all of them, so
  * their order and their original positions do not matter to the attention calls.
  *
- * hswa_attn_weights, after an attention call on the layer, with the q and lse of that call and the batch as it was
- * (not advanced), its new tokens appended already (fused or by hswa_kv_append):
+ * hswa_attn_weights, after an attention call on the layer, with the q and lse of that call and the batch as it was (not
+ * advanced), its new tokens appended already (fused or by hswa_kv_append):
  *   weights[r][kh][j] = decay * weights[r][kh][j] + sum over tokens i < n[r] and the G query heads h of KV head kh of
  *                       exp(sm_scale * q[r,i,h] . k[j] - lse[r,i,h])   over the rows that see position j.
  *   causal != 0 (self attention): token i sees j <= ctx[r] + i, and positions ctx[r] .. ctx[r] + n[r] - 1 are new: what
  *     their weights held before counts as 0.   causal == 0 (hswa_cross_attn): token i sees every j < ctx[r].
- *   decay = 0 reads none of the old weights.  A row whose lse is minus infinity saw nothing and adds nothing, whatever its q
- *   holds.  To judge a prompt by its last n tokens only, pass those tokens' q and lse with ctx_len reduced by n.
+ *   decay = 0 reads none of the old weights.  A row whose lse is minus infinity saw nothing and adds nothing, whatever
+ *   its q holds.  To judge a prompt by its last n tokens only, pass those tokens' q and lse with ctx_len reduced by n.
+ *   The weights inherit the lse's error: the decode calls' row sums take probabilities rounded to bf16, up to 2^-8 off
+ *   on rows of few keys.
  *   After hswa_decode_attn_mtp the batch needs row offsets, q_indptr[r] = r * q_len with max_q_len = q_len and total_q =
- *   B * q_len: the batch of that call (q_indptr = NULL) would mean one row per request.  Rejected drafts have no vote when
- *   their lse is set to minus infinity before the call; their positions lie behind the advanced ctx_len.
+ *   B * q_len: the batch of that call (q_indptr = NULL) would mean one row per request.  Rejected drafts have no vote
+ *   when their lse is set to minus infinity before the call; their positions lie behind the advanced ctx_len.
  *   q: device bf16 [T][Hq][D]; lse: device fp32 [T][Hq]; weights: device fp32 [B][Hkv][weights_stride], columns at or
  *   past the request's last position are not touched.  weights_stride and the block table must cover max_ctx_len, decay
  *   must be finite and >= 0: HSWA_ERR_INVALID_ARG; max_ctx_len + max_q_len is at most 2^30: HSWA_ERR_UNSUPPORTED.  A
  *   request longer than max_ctx_len or max_q_len, with row offsets outside [0, total_q], or whose ctx + n passes
- *   weights_stride or the block table, is recorded as HSWA_ERR_BOUNDS (index -1 / -2 / -2 / -3) and left out.  Sums are in fp32 in a fixed order: repeated calls on equal inputs
- *   agree bit for bit.
+ *   weights_stride or the block table, is recorded as HSWA_ERR_BOUNDS (index -1 / -2 / -2 / -3) and left out.  Sums are
+ *   in fp32 in a fixed order: repeated calls on equal inputs agree bit for bit.
  *
- * hswa_evict_select: keep_idx[r][kh][0 .. kept) = the kept = min(keep_len[r], ctx_len[r]) positions of largest weight, in
- *   ascending order; entries from kept to max_keep are set to -1, kept_len[r] = kept.  The first protect_first and the
- *   last protect_last positions rank above all others; equal weights are taken from the lowest position on; NaN ranks
- *   lowest.  ctx_len, keep_len, kept_len: device int32 [B]; weights as above; keep_idx: device int32 [B][Hkv][max_keep].
- *   ctx_len is the length AFTER the step (call it behind hswa_step_advance); kept_len must be another array
- *   (HSWA_ERR_INVALID_ARG), and max_ctx_len at most 2^30 (HSWA_ERR_UNSUPPORTED).  A ctx_len outside [0, max_ctx_len] or a
- *   keep_len outside [0, max_keep] is recorded as HSWA_ERR_BOUNDS (index -1 / -2) and clamped.
+ * hswa_evict_select: keep_idx[r][kh][0 .. kept) = the kept = min(keep_len[r], ctx_len[r]) positions of largest
+ *   weight, in ascending order; entries from kept to max_keep are set to -1, kept_len[r] = kept.  The first
+ *   protect_first and the last protect_last positions rank above all others; equal weights are taken from the lowest
+ *   position on; NaN ranks lowest.  ctx_len, keep_len, kept_len: device int32 [B]; weights as above; keep_idx: device
+ *   int32 [B][Hkv][max_keep].  ctx_len is the length AFTER the step (call it behind hswa_step_advance); kept_len must be
+ *   another array (HSWA_ERR_INVALID_ARG), and max_ctx_len at most 2^30 (HSWA_ERR_UNSUPPORTED).  A ctx_len outside
+ *   [0, max_ctx_len] or a keep_len outside [0, max_keep] is recorded as HSWA_ERR_BOUNDS (index -1 / -2) and clamped.
  *
  * hswa_evict_compact: copies K and V of position keep_idx[r][kh][i], i < kept_len[r], to position i behind
- *   dst_block_table (device int32 [B][dst_max_blocks], another array, pages of the same pool), and its weight (weights and weights_out
- *   both given or both NULL; different arrays) to weights_out[r][kh][i].  Nothing else is written.  The caller guarantees
- *   that the destination pages are pages of no block table in use, this batch's included: source pages, which other
- *   requests may share, are only read.  Afterwards dst_block_table and kept_len take the place of block_table and ctx_len
- *   for this layer; run it for every Full layer of the step with equal kept_len, so that one ctx_len serves all.  On the
- *   SWA layers of a hybrid stack, a ctx_len cut below W - 1 hides the window's older keys: keep at least
- *   min(ctx_len, W - 1).  Rings and ring_head stay as they are; swa_valid_from holds positions and moves with ctx_len, to
- *   max(0, swa_valid_from - (ctx_len - kept_len)), by the caller.  Entry i of a compacted table is no longer token i, nor the
- *   same token for every head: such a request is no donor of a prefix, with its Full KV nor its masks.  Ids and positions out of range are recorded as HSWA_ERR_BOUNDS and the row is not copied. */
+ *   dst_block_table (device int32 [B][dst_max_blocks], another array, pages of the same pool), and its weight (weights
+ *   and weights_out both given or both NULL; different arrays) to weights_out[r][kh][i].  Nothing else is written.  The
+ *   caller guarantees that the destination pages are pages of no block table in use, this batch's included: source
+ *   pages, which other requests may share, are only read.  Afterwards dst_block_table and kept_len take the place of
+ *   block_table and ctx_len for this layer; run it for every Full layer of the step with equal kept_len, so that one
+ *   ctx_len serves all.  On the SWA layers of a hybrid stack, a ctx_len cut below W - 1 hides the window's older keys:
+ *   keep at least min(ctx_len, W - 1).  Rings and ring_head stay as they are; swa_valid_from holds positions and moves
+ *   with ctx_len, to max(0, swa_valid_from - (ctx_len - kept_len)), by the caller.  Entry i of a compacted table is no
+ *   longer token i, nor the same token for every head: such a request is no donor of a prefix, with its Full KV nor its
+ *   masks.  Ids and positions out of range are recorded as HSWA_ERR_BOUNDS and the row is not copied. */
 hswa_status hswa_attn_weights(hswa_handle* h, const hswa_layer* layer, const hswa_batch* batch, int32_t causal, const void* q,
                               const float* lse, float decay, float* weights, int64_t weights_stride, void* stream);
 hswa_status hswa_evict_select(hswa_handle* h, int32_t batch, const int32_t* ctx_len, int32_t max_ctx_len, const float* weights,

@@ -8,8 +8,10 @@
 namespace {
 
 constexpr int kMinSplitLen = 256;
-// Cross attention of single tokens: up to this many states are one block's.  Two requests of up to 512 states: 7.2 us by one
-// launch, 8.2 with the call around it; two launches cost the host alone 10.5.
+// Cross attention of single tokens: up to this many states are one block's, one launch (two cost the host more than the
+// device: 10.5 us a call, one 8.2).  On the device, us in one block / in slices and a join: 2 requests, 4 / 1 heads of 64:
+// 300 states 5.7 / 6.6, 512 7.0 / 6.6, 600 8.2 / 6.7; 1 request, 64 / 8 heads of 128: 512 8.1 / 7.7, 600 10.0 / 8.3; 32 of them:
+// 512 16.3 / 22.5, 600 19.7 / 24.8 (what the limit costs large batches just above it).
 constexpr int kUnsplitLen = 512;
 constexpr int kMaxSplitLen = 4096;  // measured on configs 2, 4 and 5: 4096-8192 beat 2048 (fewer block prologues) and 16384 (tail)
 

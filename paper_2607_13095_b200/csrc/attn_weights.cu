@@ -3,14 +3,16 @@
 //
 // A score product whose output is summed over its ROWS: keys are the M dimension of tcgen05.mma (128 keys = 128 TMEM lanes
 // = 128 threads), the packed (token, head) rows are N, so that a thread owns a key, adds up its row sums in registers and
-// writes one number; nothing is exchanged between threads, no atomics, and the order of the sums is fixed.  Each key is
-// read from memory once.
+// writes one number.  With more than 64 rows a Q tile two threads own a key, each with one half of the columns, and their
+// two sums meet through TMEM once per key tile.  No atomics, and the order of the sums is fixed.  Each key is read from
+// memory once.
 //
 // Bounds.  One row group (a decode step) is bound by reading K: 64 requests of 4096 to 32768 keys, 8 KV heads of 128: 423 to
-// 433 us = 6.4 to 6.5 TB/s, a plain copy's rate.  With many rows the sums bound it (an observation window of 33 to 64 tokens on 8
-// prompts of up to 16384: 73 us, where the tensor core has 26 us of work and the special-function units, at 16 exponentials
-// per clock and SM, 37 us): the rest is the instructions around them.  Taking a share of the exponentials on the FMA pipes by
-// a polynomial was no faster (1, 2, 3 of 8: 78 us; 4 of 8: 83 us).
+// 437 us = 6.3 to 6.5 TB/s, a plain copy's rate.  With many rows the sums bound it (an observation window of 33 to 64 tokens
+// on 8 prompts of up to 16384: 74 us, where the tensor core has 26 us of work and the special-function units, at 16
+// exponentials per clock and SM, 37 us; they are 61 % busy, the issue slots 43 %): the rest is the instructions and the waits
+// around them.  Taking a share of the exponentials on the FMA pipes by a polynomial was slower (1, 2, 3 of 8: 78 us; 4 of 8:
+// 83 us; none: 74).
 //
 // Warp roles: two groups of summing warps (four or eight each) take the even and the odd key tiles of a segment, one warp
 // loads (TMA) and stages the rows' log-sum-exps, one issues the MMAs.  Each group has two TMEM accumulators.
@@ -27,8 +29,9 @@ using namespace hswa_dev;
 
 constexpr int TKEYS = 128;       // keys per tile
 // Summing warps per group: four cover the 128 keys of a tile.  The many-row form has twice as many, each with half of the
-// columns: two warps per scheduler leave the pipes idle too long behind TMEM reads and dependent steps (86 us on an observation
-// window of up to 64 tokens of 8 prompts of up to 16384, 78 us with four).
+// columns: two warps per scheduler leave the pipes idle too long behind TMEM reads and dependent steps (86 us on an
+// observation window of up to 64 tokens of 8 prompts of up to 16384, 78 us with four, both measured while three of eight
+// exponentials were on the FMA pipes).
 constexpr int group_warps(bool wide) { return wide ? 8 : 4; }
 constexpr int block_threads(bool wide) { return (2 * group_warps(wide) + 2) * 32; }
 constexpr int MAX_NSQ = 8, MAX_NSK = 6;
@@ -531,7 +534,8 @@ attn_weights_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_co
             const int full_cols = cols == q_rows ? mma_cols(cols, N) : cols;  // (a full tile's rows behind q_rows are zeros)
             // Columns [c_lo, cols) count: behind cols are rows of another request, before c_lo tokens that come before the
             // key.  Chunks that every lane of the warp sees whole take the short way, chunks that none sees are passed over.
-            const int c_lo = p.causal ? max(0, j - sg.ctx - tok0) * M.G : 0;  // (clamped first: G times a far context passes 32 bits)
+            // (Clamped before it is multiplied: G times a far context passes 32 bits.)
+            const int c_lo = p.causal ? max(0, j - sg.ctx - tok0) * M.G : 0;
             const int warp_lo = __shfl_sync(0xffffffffu, c_lo, 0), warp_hi = __shfl_sync(0xffffffffu, c_lo, 31);
             float2 acc[4];
 #pragma unroll
@@ -650,9 +654,9 @@ cudaError_t hswa_launch_attn_weights(const CUtensorMap& tm_pool, const CUtensorM
   const bool wide = pl.n_cols > 64;
   const int tile_kb = p.m.D / 4;  // a tile of 128 rows
   if (wide) {
-    // One block per SM, as many tiles as its shared memory holds: a Q stage more than a request has Q tiles (the next segment's first one) as long as
-    // three K stages are left; where Q tiles are streamed, four K stages (the next pair's are loaded while this one is
-    // multiplied) and the rest for Q
+    // One block per SM, as many tiles as its shared memory holds: a Q stage more than a request has Q tiles (the next
+    // segment's first one) as long as three K stages are left; where Q tiles are streamed, four K stages (the next pair's
+    // are loaded while this one is multiplied) and the rest for Q
     const int stages = p.m.D == 128 ? 7 : 13;
     pl.nsq = max_qt + 1 < MAX_NSQ ? max_qt + 1 : MAX_NSQ;
     if (pl.nsq > stages - 3) pl.nsq = stages - 3;

@@ -10,8 +10,8 @@ using namespace hswa_dev;
 // Joins the key slices: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  One warp per (token, head); slices that hold
 // no key of the row (l = 0) are passed over, and a row that no block computed (past max_q_len: l < 0 in its first slice)
 // stays as it was.  WPR = 4: four warps per row, a block's, each with every fourth slice, for more than eight of them: one
-// warp pays a memory latency for every few (8 tokens against 32000 states, 32 / 8 heads of 128, 36 slices: 43 us, with four
-// warps 35).
+// warp pays a memory latency for every few (8 tokens against 32000 states, 32 / 8 heads of 128, 36 slices: 42 us, with four
+// warps 34).
 template <int D, int WPR>
 __global__ void __launch_bounds__(128) cross_combine_kernel(const CrossParams p) {
   const int64_t row = WPR == 4 ? (int64_t)blockIdx.x : ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;

@@ -28,8 +28,9 @@ __device__ __forceinline__ uint32_t rank_key(float w, int j, int ctx, int first,
 // the positions, which puts it in order.  A list that does not fit even then (many equal weights) is done without: the
 // later passes read the row.
 //
-// Bound by what one SM can load -- a row is one block's -- and by the chain of block-wide steps around it.  512 rows of 1024 to
-// 32768 weights: 36 us for 41 MB (43 among other kernels); 128 rows of 65536 to 262144: 53 us for 83 MB, of which the longest row's 1 MB takes 32 us.
+// Bound by what one SM can load -- a row is one block's -- and by the chain of block-wide steps around it.  512 rows of 1024
+// to 32768 weights: 44 us for 41 MB (36 where launch follows launch); 128 rows of 65536 to 262144: 53 us for 83 MB, of which
+// the longest row's 1 MB takes 32 us.
 constexpr int SEL_BINS = 2048;
 constexpr int SEL_QUADS = 4;  // quads of keys a thread has in hand in a step of the whole block
 
@@ -638,8 +639,10 @@ cudaError_t launch_select_t(const SelectParams& p, int64_t rows, cudaStream_t s)
 cudaError_t hswa_launch_evict_select(const SelectParams& p, int num_sms, cudaStream_t s) {
   if (p.B == 0) return cudaSuccess;
   const int64_t rows = (int64_t)p.B * p.Hkv;
-  // Blocks.  More rows than SMs, up to 32768 positions: four small blocks per SM, whose steps overlap (512 rows, 2048 kept:
-  // 34 us; two larger blocks 41).  Else two blocks of 512 threads per SM, where their lists leave L1 the room that the data of
+  // Blocks.  More rows than SMs, up to 32768 positions: four small blocks per SM, whose steps overlap (512 rows, 2048 kept, us
+  // with four small / two larger blocks: rows of 1024 to 32768 40.4 / 42.9, 8000 to 30000 39.9 / 43.6; above the limit 1024 to
+  // 33500 40.4 / 43.4, 1024 to 65536 57.3 / 53.2, 30000 to 65536 with 4096 kept 76 / 65; 256 rows of 4000 to 30000 22.3 / 20.2,
+  // to 33500 22.8 / 20.5: fewer rows per SM would rather have the larger ones).  Else two blocks of 512 threads per SM, where their lists leave L1 the room that the data of
   // loads in flight needs (512 rows of 30000 to 60000, 4096 kept: 66 us; four small blocks 76, one block 99), or one where there
   // is one row per SM at most (128 rows of 16000 to 32000: 19 us; small blocks 25).  The longest rows and lists: one block per
   // SM with as many loads in flight as its registers hold (128 rows of 65536 to 262144, 8191 kept: 54 us; with half of them

@@ -127,7 +127,8 @@ struct CrossParams {
   int32_t batch;
   int32_t slices;
   const float* part_o;    // [T * Hq][slices][D]
-  const float2* part_ml;  // [T * Hq][slices] (m in log2 units, l; l = 0: the slice holds no key of the row; l < 0 in the first: no block has the row)
+  // [T * Hq][slices] (m in log2 units, l); l = 0: the slice holds no key of the row; l < 0 in the first: no block has the row
+  const float2* part_ml;
 };
 
 struct WeightsParams {

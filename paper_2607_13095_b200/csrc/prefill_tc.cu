@@ -226,10 +226,11 @@ __device__ __forceinline__ void linger_after_error(const int32_t* err) {
 // MODE_CROSS turns it into cross attention to cached encoder states (hswa_cross_attn): every cached key is visible to every
 // row, so the (token, head) rows of a GQA group are interchangeable, and a Q tile takes 128 / G tokens x the G query heads of
 // one KV head; the two tiles of a block follow one another in the request's tokens.  The keys may be cut into slices
-// (blockIdx.x / row tiles), which leave partials like the prefix stage's.  A block of two Q tiles whose
-// tokens fit one runs with one MMA issuer and one softmax group; NQ = 1 is for batches whose requests all do: half the
-// threads, shared memory (one K and one V stage) and TMEM columns, so that an SM holds two blocks.  8 requests, 257 to 512 tokens, up to 8192 states, 64 / 8 heads: 357 us = 981 TFLOP/s
-// under a sustained load (1140 in short bursts), 53 % of the tensor pipe; the warp-level kernel took 2137 us.
+// (blockIdx.x / row tiles), which leave partials like the prefix stage's.  A block of two Q tiles whose tokens fit one runs
+// with one MMA issuer and one softmax group; NQ = 1 is for batches whose requests all do: half the threads, shared memory
+// (one K and one V stage) and TMEM columns, so that an SM holds two blocks.  8 requests, 257 to 512 tokens, up to 8192
+// states, 64 / 8 heads: 359 us = 975 TFLOP/s under a sustained load (1130 in short bursts), 53 % of the tensor pipe; the
+// warp-level kernel took 2137 us.
 enum { MODE_PREFILL = 0, MODE_PREFIX = 1, MODE_CROSS = 2 };
 // Does cached tile j (of nA) of a request with ctx cached tokens hold rows that no row of the block can see?  On a
 // Full layer: the last tile when ctx ends inside it.  On an SWA layer: every ring tile (slots older than the window,
@@ -316,7 +317,8 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     t0 = p.b.q_indptr[r];
     n = p.b.q_indptr[r + 1] - t0;
     const int len = p.b.ctx_len[r];
-    auto has_row = [&](int tok) { return (unsigned)t0 + (unsigned)tok < (unsigned)p.total_q; };  // q_indptr may name rows without storage
+    // q_indptr may name rows without storage (tested at the stores: a shorter n here made the kernel spill registers, 2 %)
+    auto has_row = [&](int tok) { return (unsigned)t0 + (unsigned)tok < (unsigned)p.total_q; };
     if (threadIdx.x == 0 && blockIdx.x == 0 && kh == 0) {  // the grid was sized from the host's bounds
       if (len < 0 || len > p.max_ctx_len) record_error(p.err, HSWA_ERR_BOUNDS, r, -1, len);
       if (n < 0 || n > p.max_q_len || t0 < 0 || (int64_t)t0 + n > p.total_q) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, n);
@@ -443,7 +445,8 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
 
   // Registers move from the service warps (one warpgroup: producer, two MMA issuers and the patch warp; the
   // exchange is made by whole warpgroups) to the softmax warps, whose threads hold a row of 128 scores:
-  // 8 x 32 x 224 + 4 x 32 x 56 = 384 x 168 (one Q tile: 4 x 32 x 176 + 4 x 32 x 80 = 256 x 128).  Each role's branch changes its own allotment.
+  // 8 x 32 x 224 + 4 x 32 x 56 = 384 x 168 (one Q tile: 4 x 32 x 176 + 4 x 32 x 80 = 256 x 128).  Each role's branch changes
+  // its own allotment.
   if (warp == SERVICE) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER) : "memory");
     // ======================= TMA producer =======================
@@ -846,7 +849,8 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_pool, const __grid_cons
     tc_fence_after();
     const float l_tot = l_run;
     const int tok = CROSS ? (NQ * b + i) * tok_tile + rr / M.G : 0;  // CROSS: this row's token and its output row
-    const bool tok_ok = CROSS && here && rr < tok_tile * M.G && tok < n && (unsigned)t0 + (unsigned)tok < (unsigned)p.total_q;  // (has_row)
+    const bool tok_ok = CROSS && here && rr < tok_tile * M.G && tok < n &&
+                        (unsigned)t0 + (unsigned)tok < (unsigned)p.total_q;  // (has_row, above)
     const int64_t cross_row = CROSS ? (int64_t)(t0 + tok) * M.Hq + h0 + rr % M.G : 0;
     if (PREFIX || (CROSS && p.max_splits > 1)) {
       // partial for the split-K combine: row = (request, head) or (token, head), unnormalised o with its (m, l)
