@@ -284,14 +284,14 @@ def _open(s):
         _handles[key] = hb.Handle(*key, out_dtype=torch.bfloat16)
     s["hb"], s["h"] = hb, _handles[key]
     if c["op"] in ("append", "attn"):
-        s["layer"] = hb.Kv4Layer(s["pool"], c["k_scale"], c["v_scale"])
+        s["layer"] = hb.PackedLayer(s["pool"], c["k_scale"], c["v_scale"])
         ring = torch.zeros((c["batch"], s["h"].ring_pages), dtype=torch.int32, device="cuda")
         head = torch.zeros((c["batch"],), dtype=torch.int32, device="cuda")
         one = c["q_lo"] == 1 and c["q_hi"] == 1
         s["batch"] = hb.Batch(s["ctx"], s["table"], ring, head, None if one else s["indptr"], max_q_len=s["max_q"], total_q=s["total_q"],
                               max_ctx_len=s["max_ctx"])
     if c["op"] == "attn":
-        need = hb.hswa_kv4_workspace_need(s["h"], c["batch"], s["total_q"], s["max_q"], s["max_ctx"], c["causal"])
+        need = hb.hswa_packed_workspace_need(s["h"], c["batch"], s["total_q"], s["max_q"], s["max_ctx"], c["causal"])
         s["ws"] = torch.empty((max(need, 256),), dtype=torch.uint8, device="cuda")
     if c["op"] == "fork":
         s["ws"] = torch.empty((hb.hswa_pages_workspace_need(s["h"], c["pages"]),), dtype=torch.uint8, device="cuda")
@@ -302,11 +302,11 @@ def _open(s):
 def _run_own(s):
     hb, c, h = s["hb"], s["case"], s["h"]
     if c["op"] == "append":
-        hb.hswa_kv4_append(h, s["layer"], s["batch"], s["k"], s["v"])
-        hb.hswa_kv4_read(h, s["layer"], s["batch"], s["k_out"], s["v_out"])
+        hb.hswa_packed_append(h, s["layer"], s["batch"], s["k"], s["v"])
+        hb.hswa_packed_read(h, s["layer"], s["batch"], s["k_out"], s["v_out"])
         return {"k": s["k_out"], "v": s["v_out"]}
     if c["op"] == "attn":
-        hb.hswa_kv4_attn(h, s["layer"], s["batch"], c["causal"], s["q"], s["out"], s["lse"], s["ws"])
+        hb.hswa_packed_attn(h, s["layer"], s["batch"], c["causal"], s["q"], s["out"], s["lse"], s["ws"])
         return {"out": s["out"], "lse": s["lse"]}
     if c["op"] == "fork":
         hb.hswa_pages_fork(h, s["ref"], s["ref_out"], s["table"], s["held"], s["parent"], s["length"], s["need"], s["table_out"],
@@ -413,6 +413,7 @@ def _plain_fork(s):
     child = parent >= 0
     rows = torch.arange(n, device=ref.device)
     first = torch.full((held.numel(),), n, device=ref.device).scatter_reduce(0, from_row, torch.where(child, rows, n), "amin")
+    most = torch.zeros_like(first).scatter_reduce(0, from_row, torch.where(child, length // p, 0).long(), "amax")
     is_first = child & (first[from_row] == rows)
     k = torch.arange(blocks, device=ref.device)[None, :]
     full = (length // p)[:, None]
@@ -420,8 +421,8 @@ def _plain_fork(s):
     src = torch.nn.functional.pad(table, (0, max(0, blocks - table.shape[1])), value=-1)[from_row, :blocks]
     have = child[:, None] & (k < held[from_row][:, None])
     shared = have & (k < full)
-    # a page that the parent alone holds goes on to its first child
-    passed = have & ~shared & (k < held_out[:, None]) & is_first[:, None] & (ref[src.clamp(min=0).long()] == 1)
+    # a page that the parent alone holds, and that none of its children shares, goes on to its first child
+    passed = have & (k >= most[from_row][:, None]) & (k < held_out[:, None]) & is_first[:, None] & (ref[src.clamp(min=0).long()] == 1)
     fresh = (k < held_out[:, None]) & ~shared & ~passed
     free = ref == 0
     order = torch.full((pages + 1,), -1, dtype=torch.int32, device=ref.device)
