@@ -316,6 +316,100 @@ hswa_status hswa_evict_compact(hswa_handle* h, const hswa_layer* layer, const hs
                                const float* weights, int64_t weights_stride, float* weights_out, int64_t weights_out_stride,
                                void* stream);
 
+/* A Full layer's cache in 4 bits (no paper counterpart: Sec. 2.2's decode is bound by the bytes of the cache, which this
+ * makes 3.6 times fewer).  Values are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), 16 neighbouring elements of a row
+ * share an e4m3 scale, and a layer has one fp32 scale for K and one for V: an element stands for e2m1 * e4m3 * scale.
+ *
+ * Pool: uint8 [num_pages][2][Hkv][P * (D / 2 + D / 16)], 256-byte aligned.  A slab holds the P rows' values, D / 2 bytes each
+ * (element 2i in the low half of byte i), and behind them the P rows' scales, D / 16 bytes each.  Block tables, lengths and
+ * batches are those of the bf16 layers; SWA layers have no 4-bit form.  A layer of another head count, head dim or page size
+ * than the handle's cannot be told from the pointer: it is the caller's to match.
+ *
+ * hswa_packed_append: rounds the step's rows into the cache, row i of request r at position ctx_len[r] + i.  A block of largest
+ *   magnitude a gets the scale f = e4m3((a / s) / 6), at most 448, and its elements x the values e2m1(x / (f s)), at most 6 in
+ *   magnitude; all roundings go to the nearest, ties to the even code.  A block whose f rounds to 0 is held as zeros; infinities
+ *   and NaN are held as finite values.  k_new, v_new: device bf16 [T][Hkv][D].
+ * hswa_packed_read: the same rows back, k_out, v_out: device bf16 [T][Hkv][D], each element the value it stands for, rounded once
+ *   (exact where the layer's scale is a power of two).  With ctx_len = 0 and n[r] a request's length it reads the whole cache;
+ *   after an append it gives the chunk as later steps will see it.
+ *   Both: a request's rows past max_q_len, its rows outside the block table or behind a page id out of range, and a ctx_len outside
+ *   [0, max_ctx_len] are recorded as HSWA_ERR_BOUNDS and left out.  Pages that several requests share are the caller's to keep
+ *   from being written by more than one.
+ * hswa_packed_attn: softmax(sm_scale q K^T) V over the cache, any number of tokens per request.  causal != 0: token i sees
+ *   j <= ctx_len[r] + i, so the step's rows have been appended before (the cache holds ctx_len[r] + n[r] positions, and a token
+ *   sees its own row as the cache holds it).  causal == 0: every token sees all j < ctx_len[r] (an encoder's states).  A token
+ *   that sees nothing gives zeros and an lse of minus infinity.  q: device bf16 [T][Hq][D]; out: device [T][Hq][D] in
+ *   cfg.out_dtype; lse: device fp32 [T][Hq] or NULL.  Held values enter the products exactly; q enters them in fp16 after a
+ *   power of two per row (exact but for elements below 2^-28 of the row's largest); probabilities enter the PV product as
+ *   fp16, row sums and lse are taken over the fp32 values.  batch->q_indptr may be NULL (one token per request).  Slots behind a
+ *   request's last row may hold anything.  Workspace: hswa_packed_workspace_need bytes, else HSWA_ERR_WORKSPACE; 256-byte
+ *   aligned.  The block table must cover max_ctx_len (HSWA_ERR_INVALID_ARG); max_ctx_len + max_q_len is at most 2^30
+ *   (HSWA_ERR_UNSUPPORTED).  A request longer than max_ctx_len or max_q_len, with row offsets outside [0, total_q], or whose keys
+ *   pass the block table, is recorded as HSWA_ERR_BOUNDS (index -1 / -2 / -2 / -3); what the bounds cover is computed, other rows
+ *   of out and lse stay as they were.
+ * All refuse a current device other than the handle's, and scales that are not within [2^-64, 2^64] (HSWA_ERR_INVALID_ARG).
+ *
+ * hswa_packed_workspace_need: exact bytes for a call with these host-known fields; pure host arithmetic. */
+typedef struct {
+  void* pool;
+  int64_t num_pages;
+  float k_scale; /* fp32 scale of the layer's K */
+  float v_scale; /* fp32 scale of the layer's V */
+} hswa_packed_layer;
+
+hswa_status hswa_packed_append(hswa_handle* h, const hswa_packed_layer* layer, const hswa_batch* batch, const void* k_new,
+                               const void* v_new, void* stream);
+hswa_status hswa_packed_read(hswa_handle* h, const hswa_packed_layer* layer, const hswa_batch* batch, void* k_out, void* v_out,
+                             void* stream);
+size_t hswa_packed_workspace_need(const hswa_handle* h, int32_t batch, int32_t total_q, int32_t max_q_len, int32_t max_ctx_len,
+                                  int32_t causal);
+hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, const hswa_batch* batch, int32_t causal, const void* q,
+                             void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bookkeeping of pages on the device (paper Sec. 3.1.3: equal prefixes share physical pages).  ref[p] (device int32 [num_pages])
+ * is the number of holders of page p: rows of block tables, and whatever the caller counts besides (a prefix cache).  A page
+ * of count 0 is free; the lowest-numbered free pages are taken first, so results depend on the arguments alone.  Page ids are those
+ * of block tables and hold for every layer's pool; P is the handle's page size.  held[r] is the number of pages of row r, the
+ * first held[r] places of its table row.  Nothing is synchronised: counts and tables stay on the device.
+ *
+ * hswa_pages_fork: the tables of a step's rows from those of the step before, for beams, parallel samples, finished and new
+ *   requests at once.  New row r continues old row parent[r] (in [0, rows_in), or -1: a new request) at len[r] tokens (0 for a new
+ *   request, else at most held[parent] * P; fewer than the parent had takes tokens back), with room for need[r] tokens
+ *   (held_out = ceil(max(len, need) / P)).  The len / P full pages are shared with the parent.  Of the places behind them, those
+ *   whose page the parent alone holds (ref 1) and none of its children shares go on to its first child, the lowest r; every other
+ *   place gets a fresh page.  Where that replaces a partly filled page, (copy_src[r], copy_dst[r]) is the pair to be copied in
+ *   every layer's pool before the step writes (hswa_pages_copy), else -1, -1.  Old rows without a child give up their pages.
+ *   Written: ref_out (device int32 [num_pages], another array than ref), table_out (device int32 [rows_out][out_max_blocks], the
+ *   first held_out[r] places of each row), held_out, copy_src, copy_dst (device int32 [rows_out]).  Pages given up by a call are
+ *   free from the next call on, since its copies still read them.  If the free pages do not suffice, or a row's arguments are out
+ *   of range, nothing is done: ref_out becomes a copy of ref, the other arrays stay as they were, and HSWA_ERR_BOUNDS is recorded
+ *   (request -1, index = pages wanted, value = pages free; or request = row, index -1 for held, -2 for parent, len, need).  Page
+ *   ids out of range are recorded and neither counted nor copied.  Workspace: hswa_pages_workspace_need bytes.
+ *
+ * hswa_pages_compact: moves live pages into the lowest free ones, up to max_moves of them: while it lies below, the i-th lowest
+ *   free page takes the i-th highest live one.  move_src[i], move_dst[i] (device int32 [max_moves]) are the pairs to be copied in
+ *   every layer's pool, -1 behind the last; page_map (device int32 [num_pages]) gives every page's new number, for holders outside
+ *   the tables; ref_out (another array than ref) the counts under the new numbers; table_out (device int32 [rows][max_blocks], may
+ *   be table) the first held[r] places of each row under them.  After all moves the live pages are 0 .. live - 1.
+ *
+ * hswa_pages_copy: page dst[i] of every pool becomes a copy of page src[i], i < pairs (device int32 arrays; -1, -1: no pair), in
+ *   n_pools pools (host array of device pointers, 16-byte aligned) of num_pages pages of page_bytes bytes (a multiple of 16): bf16
+ *   pools 4 * Hkv * P * D bytes, 4-bit pools 2 * Hkv * P * (D / 2 + D / 16).  No page may be the destination of two pairs, or of one
+ *   and the source of another (the lists of the two calls above keep to that).  Ids out of range are recorded and not copied.
+ *
+ * All refuse a current device other than the handle's (HSWA_ERR_INVALID_ARG), more than 4096 rows or 2^23 pages
+ * (HSWA_ERR_UNSUPPORTED), and arrays that must differ but are one (HSWA_ERR_INVALID_ARG). */
+size_t hswa_pages_workspace_need(const hswa_handle* h, int64_t num_pages);
+hswa_status hswa_pages_fork(hswa_handle* h, int64_t num_pages, const int32_t* ref, int32_t* ref_out, int32_t rows_in,
+                            const int32_t* held, const int32_t* table, int32_t max_blocks, int32_t rows_out, const int32_t* parent,
+                            const int32_t* len, const int32_t* need, int32_t* table_out, int32_t out_max_blocks, int32_t* held_out,
+                            int32_t* copy_src, int32_t* copy_dst, void* workspace, size_t workspace_bytes, void* stream);
+hswa_status hswa_pages_compact(hswa_handle* h, int64_t num_pages, const int32_t* ref, int32_t* ref_out, int32_t rows,
+                               const int32_t* held, const int32_t* table, int32_t max_blocks, int32_t* table_out, int32_t* page_map,
+                               int32_t max_moves, int32_t* move_src, int32_t* move_dst, void* stream);
+hswa_status hswa_pages_copy(hswa_handle* h, int32_t n_pools, void* const* pools, int64_t num_pages, int64_t page_bytes, int32_t pairs,
+                            const int32_t* src, const int32_t* dst, void* stream);
+
 /* SWA-aware prefix reuse helpers (paper Sec. 3.1.3 "SWA-Aware Prefix Cache Tree", Sec. 3.1.1 "Data movement",
  * Sec. 3.1.2 layerwise prefetch).
  *

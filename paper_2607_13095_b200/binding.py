@@ -29,7 +29,8 @@ EXPORTS = [
     "hswa_decode_workspace_need", "hswa_selftest_wait_timeout", "hswa_set_overlap",
     "hswa_swa_release", "hswa_swa_valid_mask", "hswa_prefix_hit_len", "hswa_set_prefill_order", "hswa_set_block_trace",
     "hswa_probe_read_stream", "hswa_cross_attn", "hswa_cross_workspace_need", "hswa_attn_weights", "hswa_evict_select",
-    "hswa_evict_compact",
+    "hswa_evict_compact", "hswa_packed_append", "hswa_packed_read", "hswa_packed_workspace_need", "hswa_packed_attn",
+    "hswa_pages_workspace_need", "hswa_pages_fork", "hswa_pages_compact", "hswa_pages_copy",
 ]
 
 
@@ -43,6 +44,10 @@ class hswa_config(C.Structure):
 
 class hswa_layer(C.Structure):
     _fields_ = [("pool", C.c_void_p), ("num_pages", C.c_int64), ("is_swa", C.c_int32)]
+
+
+class hswa_packed_layer(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("num_pages", C.c_int64), ("k_scale", C.c_float), ("v_scale", C.c_float)]
 
 
 class hswa_batch(C.Structure):
@@ -126,6 +131,21 @@ def load(build_if_missing: bool = True) -> C.CDLL:
     lib.hswa_evict_select.argtypes = [vp, i32, vp, i32, vp, i64, vp, i32, i32, i32, vp, vp, vp]
     lib.hswa_evict_compact.restype = C.c_int
     lib.hswa_evict_compact.argtypes = [vp, C.POINTER(hswa_layer), C.POINTER(hswa_batch), vp, vp, i32, vp, i32, vp, i64, vp, i64, vp]
+    for name in ("hswa_packed_append", "hswa_packed_read"):
+        getattr(lib, name).restype = C.c_int
+        getattr(lib, name).argtypes = [vp, C.POINTER(hswa_packed_layer), C.POINTER(hswa_batch), vp, vp, vp]
+    lib.hswa_packed_workspace_need.restype = sz
+    lib.hswa_packed_workspace_need.argtypes = [vp, i32, i32, i32, i32, i32]
+    lib.hswa_packed_attn.restype = C.c_int
+    lib.hswa_packed_attn.argtypes = [vp, C.POINTER(hswa_packed_layer), C.POINTER(hswa_batch), i32, vp, vp, vp, vp, sz, vp]
+    lib.hswa_pages_workspace_need.restype = sz
+    lib.hswa_pages_workspace_need.argtypes = [vp, i64]
+    lib.hswa_pages_fork.restype = C.c_int
+    lib.hswa_pages_fork.argtypes = [vp, i64, vp, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+    lib.hswa_pages_compact.restype = C.c_int
+    lib.hswa_pages_compact.argtypes = [vp, i64, vp, vp, i32, vp, vp, i32, vp, vp, i32, vp, vp, vp]
+    lib.hswa_pages_copy.restype = C.c_int
+    lib.hswa_pages_copy.argtypes = [vp, i32, C.POINTER(vp), i64, i64, i32, vp, vp, vp]
     lib.hswa_window_safe_len.restype = C.c_int64
     lib.hswa_window_safe_len.argtypes = [C.c_int64, i32, vp]
     lib.hswa_swa_window_gather.restype = C.c_int
@@ -222,6 +242,17 @@ class Layer:
         self.device = pool.get_device()
         self.is_swa = bool(is_swa)
         self.c = hswa_layer(pool.data_ptr(), pool.shape[0], int(self.is_swa))
+        self.ref = C.byref(self.c)
+
+
+class PackedLayer:
+    """A Full layer's 4-bit pool: uint8 CUDA tensor [num_pages][2][Hkv][P * (D / 2 + D / 16)] and the layer's scales of K and V."""
+
+    def __init__(self, pool: torch.Tensor, k_scale: float = 1.0, v_scale: float = 1.0):
+        _need(pool.dtype == torch.uint8 and pool.dim() == 4 and pool.shape[1] == 2 and pool.is_contiguous())
+        self.pool = pool
+        self.device = pool.get_device()
+        self.c = hswa_packed_layer(pool.data_ptr(), pool.shape[0], k_scale, v_scale)
         self.ref = C.byref(self.c)
 
 
@@ -343,7 +374,7 @@ def hswa_cross_workspace_need(h: Handle, batch: int, total_q: int, max_q_len: in
     return int(load().hswa_cross_workspace_need(h.ptr, batch, total_q, max_q_len, max_ctx_len))
 
 
-def _device_of(layer: Layer, batch: Batch) -> int:
+def _device_of(layer, batch: Batch) -> int:
     """The current device, which has to be that of the layer and the batch."""
     if not batch.covers_batch:
         raise AssertionError("block_table needs a row per request and q_indptr, int32, one entry more")
@@ -423,6 +454,95 @@ def hswa_evict_compact(h: Handle, layer: Layer, batch: Batch, keep_idx: torch.Te
     idx_at, kept_at, dst_at, weights_at, out_at = _ptrs(dev, keep_idx, kept_len, dst_block_table, weights, weights_out)
     _check(load().hswa_evict_compact(h.ptr, layer.ref, batch.ref, idx_at, kept_at, max_keep, dst_at, dst_blocks, weights_at, stride,
                                      out_at, out_stride, _raw_stream(dev)), "hswa_evict_compact")
+
+
+def _packed_device_of(h: Handle, layer: PackedLayer, batch: Batch) -> int:
+    c = h.cfg
+    slab = c.page_size * (c.head_dim // 2 + c.head_dim // 16)
+    _need(tuple(layer.pool.shape[2:]) == (c.num_kv_heads, slab), "4-bit pool of another head count, head dim or page size than the handle's")
+    return _device_of(layer, batch)
+
+
+def _packed_rows(call, what, h: Handle, layer: PackedLayer, batch: Batch, k: torch.Tensor, v: torch.Tensor):
+    n = batch.total_q * h.cfg.num_kv_heads * h.cfg.head_dim
+    _need(k.dtype == v.dtype == torch.bfloat16 and k.numel() >= n and v.numel() >= n, "k and v: bf16, total_q rows")
+    dev = _packed_device_of(h, layer, batch)
+    _check(call(h.ptr, layer.ref, batch.ref, *_ptrs(dev, k, v), _raw_stream(dev)), what)
+
+
+def hswa_packed_append(h: Handle, layer: PackedLayer, batch: Batch, k_new: torch.Tensor, v_new: torch.Tensor):
+    """Rounds k_new, v_new [T][Hkv][D] to 4 bits at the positions from ctx_len[r] on."""
+    _packed_rows(load().hswa_packed_append, "hswa_packed_append", h, layer, batch, k_new, v_new)
+
+
+def hswa_packed_read(h: Handle, layer: PackedLayer, batch: Batch, k_out: torch.Tensor, v_out: torch.Tensor):
+    """The rows at the positions from ctx_len[r] on, as bf16 [T][Hkv][D]."""
+    _packed_rows(load().hswa_packed_read, "hswa_packed_read", h, layer, batch, k_out, v_out)
+
+
+def hswa_packed_workspace_need(h: Handle, batch: int, total_q: int, max_q_len: int, max_ctx_len: int, causal: bool) -> int:
+    return int(load().hswa_packed_workspace_need(h.ptr, batch, total_q, max_q_len, max_ctx_len, bool(causal)))
+
+
+def hswa_packed_attn(h: Handle, layer: PackedLayer, batch: Batch, causal: bool, q, out, lse=None, workspace=None):
+    """Attention of q [T][Hq][D] over a 4-bit cache: causal (the step's rows appended before), or to all ctx_len[r] positions."""
+    _need(q.dtype == torch.bfloat16 and out.dtype == h.out_dtype and (lse is None or lse.dtype == torch.float32))
+    _rows_are_said(batch, q)
+    rows = batch.total_q * h.cfg.num_q_heads
+    n = rows * h.cfg.head_dim
+    _need(q.numel() >= n and out.numel() >= n and (lse is None or lse.numel() >= rows), "fewer rows than total_q")
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    dev = _packed_device_of(h, layer, batch)
+    q_at, out_at, lse_at, ws_at = _ptrs(dev, q, out, lse, workspace)
+    _check(load().hswa_packed_attn(h.ptr, layer.ref, batch.ref, bool(causal), q_at, out_at, lse_at, ws_at, ws_bytes, _raw_stream(dev)),
+           "hswa_packed_attn")
+
+
+def hswa_pages_workspace_need(h: Handle, num_pages: int) -> int:
+    return int(load().hswa_pages_workspace_need(h.ptr, num_pages))
+
+
+def hswa_pages_fork(h: Handle, ref, ref_out, table, held, parent, length, need, table_out, held_out, copy_src, copy_dst, workspace):
+    """Block tables of a step's rows from their parents': int32 CUDA tensors, ref [num_pages], table [rows][blocks], the others [rows]."""
+    ints = (ref, ref_out, table, held, parent, length, need, table_out, held_out, copy_src, copy_dst)
+    _need(all(t.dtype == torch.int32 for t in ints) and ref_out.numel() == ref.numel())
+    rows_in, blocks = table.shape
+    rows_out, out_blocks = table_out.shape
+    _need(held.numel() >= rows_in and all(t.numel() >= rows_out for t in (parent, length, need, held_out, copy_src, copy_dst)),
+          "fewer entries than rows")
+    dev = _device()
+    (ref_at, ref_out_at, table_at, held_at, parent_at, len_at, need_at, table_out_at, held_out_at, src_at, dst_at, ws_at) = _ptrs(
+        dev, *ints, workspace)
+    _check(load().hswa_pages_fork(h.ptr, ref.numel(), ref_at, ref_out_at, rows_in, held_at, table_at, blocks, rows_out, parent_at, len_at,
+                                  need_at, table_out_at, out_blocks, held_out_at, src_at, dst_at, ws_at,
+                                  workspace.numel() * workspace.element_size(), _raw_stream(dev)), "hswa_pages_fork")
+
+
+def hswa_pages_compact(h: Handle, ref, ref_out, table, held, table_out, page_map, move_src, move_dst):
+    """Moves of live pages into the lowest free ones, as many as move_src has places: int32 CUDA tensors."""
+    ints = (ref, ref_out, table, held, table_out, page_map, move_src, move_dst)
+    _need(all(t.dtype == torch.int32 for t in ints) and ref_out.numel() == page_map.numel() == ref.numel())
+    rows, blocks = table.shape
+    _need(table_out.shape == table.shape and held.numel() >= rows and move_src.numel() == move_dst.numel())
+    dev = _device()
+    ref_at, ref_out_at, table_at, held_at, table_out_at, map_at, src_at, dst_at = _ptrs(dev, *ints)
+    _check(load().hswa_pages_compact(h.ptr, ref.numel(), ref_at, ref_out_at, rows, held_at, table_at, blocks, table_out_at, map_at,
+                                     move_src.numel(), src_at, dst_at, _raw_stream(dev)), "hswa_pages_compact")
+
+
+def hswa_pages_copy(h: Handle, layers, src: torch.Tensor, dst: torch.Tensor):
+    """layers: Layer or PackedLayer objects of one kind and size, any number of them; pairs of page ids, -1 where there is none."""
+    _need(src.dtype == dst.dtype == torch.int32 and src.numel() == dst.numel())
+    if not layers:
+        return
+    first = layers[0].pool
+    _need(all(x.pool.shape == first.shape and x.pool.dtype == first.dtype for x in layers), "pools of different sizes")
+    dev = _device()
+    _need(all(x.device == dev for x in layers), "layer on another device than the current one")
+    src_at, dst_at = _ptrs(dev, src, dst)
+    pools = (C.c_void_p * len(layers))(*[x.c.pool for x in layers])
+    _check(load().hswa_pages_copy(h.ptr, len(layers), pools, first.shape[0], first.stride(0) * first.element_size(), src.numel(), src_at,
+                                  dst_at, _raw_stream(dev)), "hswa_pages_copy")
 
 
 def hswa_window_safe_len(match_len: int, window: int, swa_valid) -> int:

@@ -4,6 +4,8 @@
 #include <new>
 
 #include "hswa_internal.cuh"
+#include "packed.cuh"
+#include "pages.cuh"
 
 namespace {
 
@@ -198,6 +200,33 @@ bool plan_cross(const hswa_handle* h, int batch, int total_q, int max_q_len, int
   return true;
 }
 
+// Attention over a 4-bit cache: rows of a block, blocks along a request's rows, key slices.
+struct PackedPlan {
+  int rows, row_tiles, slices, slice_len;
+  size_t o_bytes, ml_bytes;
+};
+
+bool plan_packed(const hswa_handle* h, int batch, int total_q, int max_q_len, int max_ctx_len, int causal, PackedPlan* pl) {
+  PackedPlan c = {};
+  if ((int64_t)max_ctx_len + max_q_len > kMaxPositions || h->cfg.num_kv_heads > 65535) return false;
+  const int64_t rows = (int64_t)max_q_len * h->group;
+  c.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
+  c.row_tiles = (int)((rows + c.rows - 1) / c.rows);
+  const int keys = max_ctx_len + (causal ? max_q_len : 0), last = keys > 0 ? keys - 1 : 0;
+  const int64_t blocks = (int64_t)batch * c.row_tiles;
+  if (blocks > INT32_MAX) return false;
+  c.slice_len = keys <= kUnsplitLen ? kUnsplitLen : plan_split_len(h, (int)blocks, last, 2);
+  c.slices = plan_max_splits(c.slice_len, last);
+  if (blocks * c.slices > INT32_MAX || (int64_t)total_q * h->cfg.num_q_heads > INT32_MAX / 64) return false;
+  if (c.slices > 1) {
+    const size_t n = (size_t)total_q * h->cfg.num_q_heads * c.slices;
+    c.o_bytes = (n * h->cfg.head_dim * sizeof(float) + 255) & ~size_t(255);
+    c.ml_bytes = (n * sizeof(float2) + 255) & ~size_t(255);
+  }
+  *pl = c;
+  return true;
+}
+
 // 4-D view of a pool for TMA: {D, P, 2 * Hkv, num_pages}, box {64, box_slots, 1, 1} (0: a whole page),
 // 128-byte swizzle.
 hswa_status make_pool_map(const hswa_handle* h, const hswa_layer* layer, CUtensorMap* tm, int box_slots = 0) {
@@ -226,6 +255,48 @@ hswa_status make_rows_map(const hswa_handle* h, const void* ptr, int heads, int6
                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return rc == CUDA_SUCCESS ? HSWA_OK : HSWA_ERR_CUDA;
+}
+
+// A 4-bit layer with a batch: the checks of a bf16 Full layer, and the scales.
+hswa_status check_packed(const hswa_handle* h, const hswa_packed_layer* layer, const hswa_batch* b) {
+  if (!layer) return HSWA_ERR_INVALID_ARG;
+  const hswa_layer same = {layer->pool, layer->num_pages, 0};
+  const hswa_status st = check_common(h, &same, b);
+  if (st != HSWA_OK || b->batch == 0) return st;
+  for (const float s : {layer->k_scale, layer->v_scale})
+    if (!(s >= 0x1p-64f && s <= 0x1p64f)) return HSWA_ERR_INVALID_ARG;
+  if ((int64_t)b->max_ctx_len > (int64_t)b->max_blocks * h->cfg.page_size) return HSWA_ERR_INVALID_ARG;
+  if ((int64_t)b->max_ctx_len + b->max_q_len > kMaxPositions) return HSWA_ERR_UNSUPPORTED;
+  return device_is_current(h) ? HSWA_OK : HSWA_ERR_INVALID_ARG;
+}
+
+hswa_status packed_rows(hswa_handle* h, const hswa_packed_layer* layer, const hswa_batch* b, const void* k_in, const void* v_in, void* k_out,
+                        void* v_out, void* stream) {
+  if (h) h->chain_ok = 0;
+  const hswa_status st = check_packed(h, layer, b);
+  if (st != HSWA_OK) return st;
+  if (b->batch == 0 || b->total_q == 0 || b->max_q_len == 0) return HSWA_OK;
+  const bool in = k_in || v_in;
+  const void *k = in ? k_in : k_out, *v = in ? v_in : v_out;
+  if (!k || !v || !aligned16(k) || !aligned16(v)) return HSWA_ERR_INVALID_ARG;
+  PackedCacheParams p = {};
+  p.m = model_params(h);
+  p.b = batch_params(b);
+  p.pool = static_cast<uint8_t*>(layer->pool);
+  p.num_pages = layer->num_pages;
+  p.k_scale = layer->k_scale;
+  p.v_scale = layer->v_scale;
+  p.k_in = static_cast<const __nv_bfloat16*>(k_in);
+  p.v_in = static_cast<const __nv_bfloat16*>(v_in);
+  p.k_out = static_cast<__nv_bfloat16*>(k_out);
+  p.v_out = static_cast<__nv_bfloat16*>(v_out);
+  p.total_q = b->total_q;
+  p.max_q_len = b->max_q_len;
+  p.max_ctx_len = b->max_ctx_len;
+  p.err = h->err;
+  const cudaError_t e = in ? hswa_launch_packed_append(p, h->num_sms, (cudaStream_t)stream)
+                           : hswa_launch_packed_read(p, h->num_sms, (cudaStream_t)stream);
+  return e == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
 }
 
 }  // namespace
@@ -863,6 +934,163 @@ hswa_status hswa_evict_compact(hswa_handle* h, const hswa_layer* layer, const hs
   p.out_stride = weights_out_stride;
   p.err = h->err;
   return hswa_launch_evict_compact(p, h->num_sms, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+}
+
+hswa_status hswa_packed_append(hswa_handle* h, const hswa_packed_layer* layer, const hswa_batch* b, const void* k_new, const void* v_new,
+                               void* stream) {
+  if ((k_new == nullptr) != (v_new == nullptr)) return HSWA_ERR_INVALID_ARG;
+  if (!k_new && b && b->batch > 0 && b->total_q > 0) return HSWA_ERR_INVALID_ARG;
+  return packed_rows(h, layer, b, k_new, v_new, nullptr, nullptr, stream);
+}
+
+hswa_status hswa_packed_read(hswa_handle* h, const hswa_packed_layer* layer, const hswa_batch* b, void* k_out, void* v_out, void* stream) {
+  return packed_rows(h, layer, b, nullptr, nullptr, k_out, v_out, stream);
+}
+
+size_t hswa_packed_workspace_need(const hswa_handle* h, int32_t batch, int32_t total_q, int32_t max_q_len, int32_t max_ctx_len,
+                                  int32_t causal) {
+  PackedPlan pl;
+  if (!h || batch <= 0 || total_q <= 0 || max_q_len <= 0 || max_q_len > total_q || max_ctx_len < 0 ||
+      !plan_packed(h, batch, total_q, max_q_len, max_ctx_len, causal, &pl))
+    return 0;
+  return pl.o_bytes + pl.ml_bytes;
+}
+
+hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, const hswa_batch* b, int32_t causal, const void* q, void* out,
+                             float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (h) h->chain_ok = 0;
+  const hswa_status st = check_packed(h, layer, b);
+  if (st != HSWA_OK) return st;
+  if (b->batch == 0 || b->total_q == 0 || b->max_q_len == 0) return HSWA_OK;
+  if (!q || !out || !aligned16(q) || !aligned16(out)) return HSWA_ERR_INVALID_ARG;
+  PackedPlan pl;
+  if (!plan_packed(h, b->batch, b->total_q, b->max_q_len, b->max_ctx_len, causal, &pl)) return HSWA_ERR_UNSUPPORTED;
+  if (pl.o_bytes > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < pl.o_bytes + pl.ml_bytes))
+    return HSWA_ERR_WORKSPACE;
+  PackedAttnParams p = {};
+  p.m = model_params(h);
+  p.b = batch_params(b);
+  p.pool = static_cast<const uint8_t*>(layer->pool);
+  p.num_pages = layer->num_pages;
+  p.scale_log2 = p.m.scale_log2 * layer->k_scale;
+  p.v_scale = layer->v_scale;
+  p.causal = causal != 0;
+  p.q = static_cast<const __nv_bfloat16*>(q);
+  p.out = out;
+  p.lse = lse;
+  p.total_q = b->total_q;
+  p.max_q_len = b->max_q_len;
+  p.max_ctx_len = b->max_ctx_len;
+  p.slice_len = pl.slice_len;
+  p.slices = pl.slices;
+  p.row_tiles = pl.row_tiles;
+  p.part_o = pl.o_bytes > 0 ? static_cast<float*>(workspace) : nullptr;
+  p.part_ml = pl.o_bytes > 0 ? reinterpret_cast<float2*>(static_cast<char*>(workspace) + pl.o_bytes) : nullptr;
+  p.err = h->err;
+  cudaStream_t s = (cudaStream_t)stream;
+  if (hswa_launch_packed_decode(p, pl.rows, s) != cudaSuccess) return HSWA_ERR_CUDA;
+  if (pl.slices > 1) {
+    const CrossParams join = {p.m, out, lse, b->total_q, b->q_indptr, b->batch, pl.slices, p.part_o, p.part_ml};
+    if (hswa_launch_cross_combine(join, s) != cudaSuccess) return HSWA_ERR_CUDA;
+  }
+  return HSWA_OK;
+}
+
+size_t hswa_pages_workspace_need(const hswa_handle* h, int64_t num_pages) {
+  if (!h || num_pages <= 0 || num_pages > kMaxPages) return 0;
+  return ((size_t)num_pages * sizeof(int32_t) + 255) & ~size_t(255);
+}
+
+hswa_status hswa_pages_fork(hswa_handle* h, int64_t num_pages, const int32_t* ref, int32_t* ref_out, int32_t rows_in, const int32_t* held,
+                            const int32_t* table, int32_t max_blocks, int32_t rows_out, const int32_t* parent, const int32_t* len,
+                            const int32_t* need, int32_t* table_out, int32_t out_max_blocks, int32_t* held_out, int32_t* copy_src,
+                            int32_t* copy_dst, void* workspace, size_t workspace_bytes, void* stream) {
+  if (h) h->chain_ok = 0;
+  if (!h || num_pages <= 0 || rows_in < 0 || rows_out < 0 || max_blocks < 0 || out_max_blocks < 0 || !ref || !ref_out)
+    return HSWA_ERR_INVALID_ARG;
+  if (rows_in > 0 && (!held || (max_blocks > 0 && !table))) return HSWA_ERR_INVALID_ARG;
+  if (rows_out > 0 && (!parent || !len || !need || !held_out || !copy_src || !copy_dst || (out_max_blocks > 0 && !table_out)))
+    return HSWA_ERR_INVALID_ARG;
+  if (ref_out == ref || (table && table_out == table) || (held && held_out == held) || (copy_src && copy_src == copy_dst))
+    return HSWA_ERR_INVALID_ARG;
+  if (num_pages > kMaxPages || rows_in > kMaxPageRows || rows_out > kMaxPageRows) return HSWA_ERR_UNSUPPORTED;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < hswa_pages_workspace_need(h, num_pages))
+    return HSWA_ERR_WORKSPACE;
+  if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
+  PagesForkParams p = {};
+  p.num_pages = (int32_t)num_pages;
+  p.page_size = h->cfg.page_size;
+  p.ref = ref;
+  p.ref_out = ref_out;
+  p.rows_in = rows_in;
+  p.held = held;
+  p.table = table;
+  p.max_blocks = max_blocks;
+  p.rows_out = rows_out;
+  p.parent = parent;
+  p.len = len;
+  p.need = need;
+  p.table_out = table_out;
+  p.out_max_blocks = out_max_blocks;
+  p.held_out = held_out;
+  p.copy_src = copy_src;
+  p.copy_dst = copy_dst;
+  p.fresh = static_cast<int32_t*>(workspace);
+  p.err = h->err;
+  return hswa_launch_pages_fork(p, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+}
+
+hswa_status hswa_pages_compact(hswa_handle* h, int64_t num_pages, const int32_t* ref, int32_t* ref_out, int32_t rows, const int32_t* held,
+                               const int32_t* table, int32_t max_blocks, int32_t* table_out, int32_t* page_map, int32_t max_moves,
+                               int32_t* move_src, int32_t* move_dst, void* stream) {
+  if (h) h->chain_ok = 0;
+  if (!h || num_pages <= 0 || rows < 0 || max_blocks < 0 || max_moves < 0 || !ref || !ref_out || !page_map) return HSWA_ERR_INVALID_ARG;
+  if (rows > 0 && (!held || (max_blocks > 0 && (!table || !table_out)))) return HSWA_ERR_INVALID_ARG;
+  if (max_moves > 0 && (!move_src || !move_dst || move_src == move_dst)) return HSWA_ERR_INVALID_ARG;
+  if (ref_out == ref || page_map == ref || page_map == ref_out) return HSWA_ERR_INVALID_ARG;
+  if (num_pages > kMaxPages || rows > kMaxPageRows) return HSWA_ERR_UNSUPPORTED;
+  if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
+  PagesCompactParams p = {};
+  p.num_pages = (int32_t)num_pages;
+  p.ref = ref;
+  p.ref_out = ref_out;
+  p.rows = rows;
+  p.held = held;
+  p.table = table;
+  p.max_blocks = max_blocks;
+  p.table_out = table_out;
+  p.page_map = page_map;
+  p.max_moves = max_moves;
+  p.move_src = move_src;
+  p.move_dst = move_dst;
+  p.err = h->err;
+  return hswa_launch_pages_compact(p, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+}
+
+hswa_status hswa_pages_copy(hswa_handle* h, int32_t n_pools, void* const* pools, int64_t num_pages, int64_t page_bytes, int32_t pairs,
+                            const int32_t* src, const int32_t* dst, void* stream) {
+  if (h) h->chain_ok = 0;
+  if (!h || n_pools < 0 || num_pages <= 0 || page_bytes <= 0 || page_bytes % 16 != 0 || pairs < 0) return HSWA_ERR_INVALID_ARG;
+  if (n_pools == 0 || pairs == 0) return HSWA_OK;
+  if (!pools || !src || !dst) return HSWA_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < n_pools; ++i)
+    if (!pools[i] || !aligned16(pools[i])) return HSWA_ERR_INVALID_ARG;
+  if (num_pages > INT32_MAX || page_bytes > ((int64_t)1 << 30) || (int64_t)pairs * ((page_bytes + 4095) / 4096) > INT32_MAX)
+    return HSWA_ERR_UNSUPPORTED;
+  if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < n_pools; i += kPoolsPerLaunch) {
+    PagesCopyParams p = {};
+    p.n_pools = n_pools - i < kPoolsPerLaunch ? n_pools - i : kPoolsPerLaunch;
+    for (int32_t k = 0; k < p.n_pools; ++k) p.pools[k] = pools[i + k];
+    p.num_pages = num_pages;
+    p.page_bytes = page_bytes;
+    p.pairs = pairs;
+    p.src = src;
+    p.dst = dst;
+    p.err = h->err;
+    if (hswa_launch_pages_copy(p, (cudaStream_t)stream) != cudaSuccess) return HSWA_ERR_CUDA;
+  }
+  return HSWA_OK;
 }
 
 static hswa_status window_move(hswa_handle* h, const hswa_layer* layer, const hswa_batch* b, void* buf, int gather,

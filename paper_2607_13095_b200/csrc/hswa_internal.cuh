@@ -117,13 +117,13 @@ struct PrefillParams {
   float2* part_ml;
 };
 
-// Join of the key slices of cross attention.
+// Join of the key slices of cross attention and of attention over a 4-bit cache.
 struct CrossParams {
   ModelParams m;
   void* out;   // [T][Hq][D]
   float* lse;  // [T][Hq] or null
   int32_t total_q;
-  const int32_t* q_indptr;  // [batch + 1]: rows before the first request's and behind the last one's have no partials
+  const int32_t* q_indptr;  // [batch + 1]: rows before the first request's and behind the last one's have no partials; null: all have
   int32_t batch;
   int32_t slices;
   const float* part_o;    // [T * Hq][slices][D]

@@ -1,0 +1,112 @@
+// A Full layer's cache in 4 bits: the pool's layout, kernel parameters and the conversions that its kernels share.
+//
+// A row of D elements is held as D / 2 bytes (e2m1, the even element in the low half) and D / 16 e4m3 scales; a slab, one
+// (page, K|V, head), is the P rows' bytes and then the P rows' scales.  e2m1 has at most 2 significant bits and e4m3 at most
+// 4, with products between 2^-10 and 2688: a held value e2m1 * e4m3 is exact in fp16 (and bf16), so the tensor cores multiply
+// the held values themselves; the layer's two fp32 scales are applied to scores and outputs.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "hswa_internal.cuh"
+
+struct PackedCacheParams {  // append and read-back
+  ModelParams m;
+  BatchParams b;
+  uint8_t* pool;  // [num_pages][2][Hkv][P * (D / 2 + D / 16)]
+  int64_t num_pages;
+  float k_scale, v_scale;
+  const __nv_bfloat16* k_in;  // [T][Hkv][D] (append)
+  const __nv_bfloat16* v_in;
+  __nv_bfloat16* k_out;  // [T][Hkv][D] (read-back)
+  __nv_bfloat16* v_out;
+  int32_t total_q, max_q_len, max_ctx_len;
+  int32_t* err;
+};
+
+struct PackedAttnParams {
+  ModelParams m;
+  BatchParams b;
+  const uint8_t* pool;
+  int64_t num_pages;
+  float scale_log2;  // sm_scale * log2(e) * k_scale
+  float v_scale;
+  int32_t causal;
+  const __nv_bfloat16* q;  // [T][Hq][D]
+  void* out;               // [T][Hq][D]
+  float* lse;              // [T][Hq] or null
+  int32_t total_q, max_q_len, max_ctx_len;
+  int32_t slice_len, slices;  // keys per slice, slices per row
+  int32_t row_tiles;          // blocks along a request's rows
+  float* part_o;              // [T * Hq][slices][D]
+  float2* part_ml;            // [T * Hq][slices] (m in log2 units, l)
+  int32_t* err;
+};
+
+cudaError_t hswa_launch_packed_append(const PackedCacheParams& p, int num_sms, cudaStream_t s);
+cudaError_t hswa_launch_packed_read(const PackedCacheParams& p, int num_sms, cudaStream_t s);
+// Rows (tokens x heads of a KV head) per block: 8, 16 or 32
+cudaError_t hswa_launch_packed_decode(const PackedAttnParams& p, int rows, cudaStream_t s);
+
+#ifdef __CUDACC__
+namespace hswa_dev {
+
+// Two e2m1 values (one byte) to fp16; the low half of the byte goes to the low half of the result.
+template <int BYTE>
+__device__ __forceinline__ uint32_t e2m1_to_half2(uint32_t w) {
+  uint32_t r;
+  if constexpr (BYTE == 0)
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\t}" : "=r"(r) : "r"(w));
+  else if constexpr (BYTE == 1)
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, b;\n\t}" : "=r"(r) : "r"(w));
+  else if constexpr (BYTE == 2)
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, c;\n\t}" : "=r"(r) : "r"(w));
+  else
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, d;\n\t}" : "=r"(r) : "r"(w));
+  return r;
+}
+// Two e4m3 values (the low 16 bits) to fp16.
+__device__ __forceinline__ uint32_t e4m3_to_half2(uint32_t w) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)w));
+  return r;
+}
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t low_twice(uint32_t a) { return __byte_perm(a, a, 0x1010); }
+__device__ __forceinline__ uint32_t high_twice(uint32_t a) { return __byte_perm(a, a, 0x3232); }
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// D(16x8, fp32) += A(16x16, fp16, row) * B(16x8, fp16, col)
+__device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                              uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Queries enter the products as fp16, each row times a power of two that brings its largest element to [2^14, 2^15): fp16
+// has three bits more than bf16, so only elements below 2^-28 of the largest lose any.  From the largest magnitude, the
+// power and its inverse; a row of zeros, or one with an infinity, is taken as it is (NaN are no magnitudes).
+__device__ __forceinline__ void q_powers(float amax, float* up, float* down) {
+  const int e = (int)(__float_as_uint(amax) >> 23);  // biased exponent
+  const int shift = amax > 0.f && e < 255 ? min(141 - e, 100) : 0;
+  *up = __uint_as_float((uint32_t)(127 + shift) << 23);
+  *down = __uint_as_float((uint32_t)(127 - shift) << 23);
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+}  // namespace hswa_dev
+#endif  // __CUDACC__

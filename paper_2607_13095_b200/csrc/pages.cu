@@ -1,0 +1,421 @@
+// Bookkeeping of a cache's pages on the device: hswa_pages_fork, hswa_pages_compact, hswa_pages_copy.
+//
+// Counts (how many holders a page has) are the only state: a page of count 0 is free, and the lowest-numbered free pages are
+// taken first, so results depend on the counts alone.  Fork and compact are one launch of one cluster of 16 blocks: counts of
+// pages, block tables and lists are a few MB at most, the work is a chain of dependent steps, and a cluster's barrier between
+// two steps costs a fraction of a launch.  Each block turns its share of the counts into a bitmap in shared memory on the only
+// pass over them; ranks of free and live pages come from the bitmap, and totals go around through distributed shared memory.
+#include <cooperative_groups.h>
+
+#include <utility>
+
+#include "pages.cuh"
+
+namespace {
+using namespace hswa_dev;
+namespace cg = cooperative_groups;
+
+constexpr int kBlocks = 16;     // blocks of the cluster
+constexpr int kThreads = 1024;
+constexpr int kWarps = kThreads / 32;
+
+// A block's share of the pages: words [first, first + words) of 32 pages each.
+struct Share {
+  int first, words;
+};
+__device__ __forceinline__ Share share_of(int num_pages, int block) {
+  const int all = (num_pages + 31) / 32, per = (all + kBlocks - 1) / kBlocks;
+  Share s;
+  s.first = min(block * per, all);
+  s.words = min(per, all - s.first);
+  return s;
+}
+
+// Exclusive prefix sum of `mine` over the block's threads; `total` gets the sum of all.
+__device__ __forceinline__ int block_prefix(int mine, int* s_warp, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int incl = mine;
+#pragma unroll
+  for (int sh = 1; sh < 32; sh <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, incl, sh);
+    if (lane >= sh) incl += v;
+  }
+  __syncthreads();  // (s_warp of an earlier call has been read)
+  if (lane == 31) s_warp[warp] = incl;
+  __syncthreads();
+  int w = lane < kWarps ? s_warp[lane] : 0, wi = w;
+#pragma unroll
+  for (int sh = 1; sh < 32; sh <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, wi, sh);
+    if (lane >= sh) wi += v;
+  }
+  *total = __shfl_sync(0xffffffffu, wi, 31);
+  return __shfl_sync(0xffffffffu, wi - w, warp) + incl - mine;
+}
+
+// The one pass over the counts: copies them, and sets the bit of every page with a holder.  `map`, where given, gets the
+// identity.
+__device__ __forceinline__ void scan_counts(const int32_t* ref, int32_t* ref_out, int32_t* map, int num_pages, Share sh, uint32_t* live) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  constexpr int U = 8;  // loads in flight
+  for (int w0 = warp * U; w0 < sh.words; w0 += kWarps * U) {
+    int32_t v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t page = (int64_t)(sh.first + w0 + u) * 32 + lane;
+      v[u] = w0 + u < sh.words && page < num_pages ? ref[page] : 1;  // (no page: not a free one)
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (w0 + u >= sh.words) break;
+      const int64_t page = (int64_t)(sh.first + w0 + u) * 32 + lane;
+      const uint32_t bits = __ballot_sync(0xffffffffu, page < num_pages && v[u] > 0);
+      const uint32_t none = __ballot_sync(0xffffffffu, page < num_pages && v[u] <= 0);
+      if (lane == 0) {
+        live[2 * (w0 + u)] = bits;
+        live[2 * (w0 + u) + 1] = none;
+      }
+      if (page < num_pages) {
+        ref_out[page] = v[u];
+        if (map) map[page] = (int32_t)page;
+      }
+    }
+  }
+}
+
+// Sums a per-block number over the blocks before this one and over all of them.  `started`: what the block's arrival at the
+// kernel's start gave (a block's shared memory may be written by another once it runs).
+__device__ __forceinline__ void cluster_prefix(cg::cluster_group& cluster, cg::cluster_group::arrival_token&& started, int mine,
+                                               int* s_counts, int* before, int* all) {
+  cluster.barrier_wait(std::move(started));
+  if (threadIdx.x < kBlocks) *cluster.map_shared_rank(&s_counts[cluster.block_rank()], threadIdx.x) = mine;
+  cluster.sync();
+  int b = 0, a = 0;
+  for (int i = 0; i < kBlocks; ++i) {
+    a += s_counts[i];
+    if (i < (int)cluster.block_rank()) b += s_counts[i];
+  }
+  *before = b;
+  *all = a;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Fork.  Row r of the new tables continues row parent[r] of the old ones at len[r] tokens.  Its first len / P pages are shared;
+// of the places from there on, the ones whose page the parent alone holds and no child shares go on with the parent's first
+// child, and all others get fresh pages.  What the rules need of the old counts is decided before the barrier and kept as the
+// rank of a row's first fresh page; the counts of pages change behind it, by atomic adds whose order does not matter.
+// ---------------------------------------------------------------------------------------------------------------------
+struct RowPlan {
+  int parent, full, held, parent_held;  // shared pages, pages of the row, pages of its parent
+  bool first;                           // the parent's first child
+};
+
+__global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkParams p) {
+  cg::cluster_group cluster = cg::this_cluster();
+  auto started = cluster.barrier_arrive();
+  extern __shared__ int32_t s_mem[];
+  __shared__ int s_warp[kWarps], s_counts[kBlocks], s_bad;
+  int32_t* s_first = s_mem;                // [rows_in] first child
+  int32_t* s_most = s_first + p.rows_in;   // [rows_in] most pages that a child shares
+  int32_t* s_rank = s_most + p.rows_in;    // [rows_out] rank of the row's first fresh page
+  uint32_t* s_live = reinterpret_cast<uint32_t*>(s_rank + p.rows_out);
+  const int block = (int)cluster.block_rank(), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const Share sh = share_of(p.num_pages, block);
+  if (threadIdx.x == 0) s_bad = 0;
+  for (int i = threadIdx.x; i < p.rows_in; i += kThreads) {
+    s_first[i] = INT32_MAX;
+    s_most[i] = 0;
+  }
+  __syncthreads();
+
+  auto pages_of = [&](int tokens) { return (int)(((int64_t)tokens + p.page_size - 1) / p.page_size); };
+  auto plan = [&](int r) {
+    RowPlan o;
+    o.parent = p.parent[r];
+    const int len = p.len[r];
+    o.full = len / p.page_size;
+    o.held = pages_of(max(len, p.need[r]));
+    o.parent_held = o.parent >= 0 ? p.held[o.parent] : 0;
+    o.first = o.parent >= 0 && s_first[o.parent] == r;
+    return o;
+  };
+  // does place k of the row keep the parent's page?  (k >= full)
+  auto passed = [&](const RowPlan& o, int k, int* page_out) {
+    if (!o.first || k >= o.parent_held || k < s_most[o.parent]) return false;
+    const int page = p.table[(int64_t)o.parent * p.max_blocks + k];
+    *page_out = page;
+    return page >= 0 && page < p.num_pages && p.ref[page] == 1;
+  };
+
+  // every block looks at all rows: none waits for another
+  for (int i = threadIdx.x; i < p.rows_in; i += kThreads) {
+    const int held = p.held[i];
+    if (held < 0 || held > p.max_blocks) {
+      s_bad = 1;
+      if (block == 0) record_error(p.err, HSWA_ERR_BOUNDS, i, -1, held);
+    }
+  }
+  for (int r = threadIdx.x; r < p.rows_out; r += kThreads) {
+    const int parent = p.parent[r], len = p.len[r], need = p.need[r];
+    bool ok = parent >= -1 && parent < p.rows_in && len >= 0 && pages_of(max(len, need)) <= p.out_max_blocks;
+    if (ok) ok = parent < 0 ? len == 0 : pages_of(len) <= p.held[parent];
+    if (!ok) {
+      s_bad = 1;
+      if (block == 0) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, parent);
+    } else if (parent >= 0) {
+      atomicMin(&s_first[parent], r);
+      atomicMax(&s_most[parent], len / p.page_size);
+    }
+  }
+  __syncthreads();
+  const bool rows_ok = s_bad == 0;
+  int fresh_total = 0;
+  if (rows_ok) {
+    const int per = (p.rows_out + kThreads - 1) / kThreads;
+    const int r0 = threadIdx.x * per, r1 = min(r0 + per, p.rows_out);
+    int sum = 0;
+    for (int r = r0; r < r1; ++r) {
+      const RowPlan o = plan(r);
+      int fresh = o.held - o.full, page;
+      for (int k = max(o.full, o.first ? s_most[o.parent] : 0); k < min(o.held, o.first ? o.parent_held : 0); ++k) fresh -= passed(o, k, &page);
+      s_rank[r] = sum;
+      sum += fresh;
+    }
+    const int before = block_prefix(sum, s_warp, &fresh_total);
+    for (int r = r0; r < r1; ++r) s_rank[r] += before;
+  }
+
+  // the free pages of lowest number
+  scan_counts(p.ref, p.ref_out, nullptr, p.num_pages, sh, s_live);
+  __syncthreads();
+  const int wper = (sh.words + kThreads - 1) / kThreads;
+  const int w0 = threadIdx.x * wper, w1 = min(w0 + wper, sh.words);
+  int free_mine = 0;
+  for (int w = w0; w < w1; ++w) free_mine += __popc(s_live[2 * w + 1]);
+  int free_block, base, free_all;
+  int rank = block_prefix(free_mine, s_warp, &free_block);
+  cluster_prefix(cluster, std::move(started), free_block, s_counts, &base, &free_all);
+  const bool enough = fresh_total <= free_all;
+  if (!enough && rows_ok && block == 0 && threadIdx.x == 0) record_error(p.err, HSWA_ERR_BOUNDS, -1, fresh_total, free_all);
+  if (rows_ok && enough) {
+    rank += base;
+    for (int w = w0; w < w1 && rank < fresh_total; ++w) {
+      uint32_t bits = s_live[2 * w + 1];
+      for (; bits && rank < fresh_total; bits &= bits - 1) p.fresh[rank++] = (sh.first + w) * 32 + __ffs(bits) - 1;
+    }
+  }
+  cluster.sync();  // counts copied, fresh pages listed, and nobody reads another block's shared memory any more
+  if (!rows_ok || !enough) return;
+
+  auto count = [&](int page, int by, int row, int k) {
+    if (page < 0 || page >= p.num_pages)
+      record_error(p.err, HSWA_ERR_BOUNDS, row, k, page);
+    else if (by != 0)
+      atomicAdd(&p.ref_out[page], by);
+  };
+  const int all_warps = kBlocks * kWarps, my_warp = block + kBlocks * warp;
+  constexpr int CH = 256;  // shared places per item
+  const int chunks = (max(p.max_blocks, p.out_max_blocks) + CH - 1) / CH;
+  // new rows: shared places in chunks of 256, the places behind them by the warp of chunk 0
+  for (int64_t it = my_warp; it < (int64_t)p.rows_out * chunks; it += all_warps) {
+    const int r = (int)(it / chunks), c = (int)(it % chunks);
+    const RowPlan o = plan(r);
+    int32_t* out = p.table_out + (int64_t)r * p.out_max_blocks;
+    const int32_t* in = p.table + (int64_t)max(o.parent, 0) * p.max_blocks;
+#pragma unroll
+    for (int u = 0; u < CH / 32; ++u) {
+      const int k = c * CH + u * 32 + lane;
+      if (k < o.full) {
+        const int page = in[k];
+        out[k] = page;
+        count(page, o.first ? 0 : 1, r, k);
+      }
+    }
+    if (c != 0) continue;
+    int next = s_rank[r];
+    const int len = p.len[r];
+    int src = -1, dst = -1;
+    for (int k0 = o.full; k0 < o.held; k0 += 32) {
+      const int k = k0 + lane;
+      int page = -1;
+      const bool keeps = k < o.held && passed(o, k, &page);
+      const bool fresh = k < o.held && !keeps;
+      const uint32_t who = __ballot_sync(0xffffffffu, fresh);
+      if (fresh) {
+        page = p.fresh[next + __popc(who & ((1u << lane) - 1))];
+        p.ref_out[page] = 1;
+      }
+      if (k < o.held) out[k] = page;
+      next += __popc(who);
+      if (k == o.full && fresh && len % p.page_size != 0) {
+        src = in[k];
+        dst = page;
+        if (src < 0 || src >= p.num_pages) {
+          record_error(p.err, HSWA_ERR_BOUNDS, r, k, src);
+          src = dst = -1;
+        }
+      }
+    }
+    if (lane == 0) {  // (place `full` is lane 0's)
+      p.copy_src[r] = src;
+      p.copy_dst[r] = dst;
+      p.held_out[r] = o.held;
+    }
+  }
+  // old rows: what their first child does not keep loses a holder
+  for (int64_t it = my_warp; it < (int64_t)p.rows_in * chunks; it += all_warps) {
+    const int i = (int)(it / chunks), c = (int)(it % chunks);
+    const int held = p.held[i], child = s_first[i];
+    RowPlan o = {};
+    if (child != INT32_MAX) o = plan(child);
+#pragma unroll
+    for (int u = 0; u < CH / 32; ++u) {
+      const int k = c * CH + u * 32 + lane;
+      if (k >= held || (child != INT32_MAX && k < o.full)) continue;
+      int page;
+      if (child != INT32_MAX && k < o.held && passed(o, k, &page)) continue;
+      count(p.table[(int64_t)i * p.max_blocks + k], -1, i, k);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Compact.  With L live pages, the i-th lowest free page below L takes the i-th highest live page (those lie at or past L).
+// A page's rank follows from the number of live pages before it.
+// ---------------------------------------------------------------------------------------------------------------------
+__global__ void __launch_bounds__(kThreads) pages_compact_kernel(const PagesCompactParams p) {
+  cg::cluster_group cluster = cg::this_cluster();
+  auto started = cluster.barrier_arrive();
+  extern __shared__ int32_t s_mem[];
+  __shared__ int s_warp[kWarps], s_counts[kBlocks];
+  uint32_t* s_live = reinterpret_cast<uint32_t*>(s_mem);
+  const int block = (int)cluster.block_rank(), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const Share sh = share_of(p.num_pages, block);
+  for (int i = block * kThreads + threadIdx.x; i < p.max_moves; i += kBlocks * kThreads) p.move_src[i] = p.move_dst[i] = -1;
+  scan_counts(p.ref, p.ref_out, p.page_map, p.num_pages, sh, s_live);
+  __syncthreads();
+  const int wper = (sh.words + kThreads - 1) / kThreads;
+  const int w0 = threadIdx.x * wper, w1 = min(w0 + wper, sh.words);
+  int mine = 0;
+  for (int w = w0; w < w1; ++w) mine += __popc(s_live[2 * w]);
+  int in_block, base, total;
+  int before = block_prefix(mine, s_warp, &in_block);
+  cluster_prefix(cluster, std::move(started), in_block, s_counts, &base, &total);
+  before += base;  // live pages before this thread's first
+  for (int w = w0; w < w1; ++w) {
+    const uint32_t live = s_live[2 * w];
+    const int page0 = (sh.first + w) * 32;
+    // free pages below the number of live ones
+    for (uint32_t bits = page0 < total ? s_live[2 * w + 1] : 0; bits; bits &= bits - 1) {
+      const int b = __ffs(bits) - 1, page = page0 + b;
+      const int at = page - (before + __popc(live & ((1u << b) - 1)));
+      if (page >= total || at >= p.max_moves) break;
+      p.move_dst[at] = page;
+    }
+    // live pages from there on, counted from the highest
+    if (page0 + 31 >= total)
+      for (uint32_t bits = live; bits; bits &= bits - 1) {
+        const int b = __ffs(bits) - 1, page = page0 + b;
+        const int at = total - 1 - (before + __popc(live & ((1u << b) - 1)));
+        if (page >= total && at < p.max_moves) p.move_src[at] = page;
+      }
+    before += __popc(live);
+  }
+  cluster.sync();
+  for (int i = block * kThreads + threadIdx.x; i < p.max_moves; i += kBlocks * kThreads) {
+    const int src = p.move_src[i], dst = p.move_dst[i];
+    if (src < 0) continue;
+    p.page_map[src] = dst;
+    p.ref_out[dst] = p.ref[src];
+    p.ref_out[src] = 0;
+  }
+  cluster.sync();
+  const int all_warps = kBlocks * kWarps, my_warp = block + kBlocks * warp;
+  constexpr int CH = 256;
+  const int chunks = (p.max_blocks + CH - 1) / CH;
+  for (int64_t it = my_warp; it < (int64_t)p.rows * chunks; it += all_warps) {
+    const int r = (int)(it / chunks), c = (int)(it % chunks);
+    const int held = p.held[r];
+    if (held < 0 || held > p.max_blocks) {
+      if (c == 0 && lane == 0) record_error(p.err, HSWA_ERR_BOUNDS, r, -1, held);
+      continue;
+    }
+    int page[CH / 32];
+#pragma unroll
+    for (int u = 0; u < CH / 32; ++u) {
+      const int k = c * CH + u * 32 + lane;
+      page[u] = k < held ? p.table[(int64_t)r * p.max_blocks + k] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < CH / 32; ++u) {
+      const int k = c * CH + u * 32 + lane;
+      if (k >= held) continue;
+      const bool ok = page[u] >= 0 && page[u] < p.num_pages;
+      if (!ok) record_error(p.err, HSWA_ERR_BOUNDS, r, k, page[u]);
+      p.table_out[(int64_t)r * p.max_blocks + k] = ok ? p.page_map[page[u]] : page[u];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Copy.  A block moves 32 KB of one page of one pool; bound by HBM.
+// ---------------------------------------------------------------------------------------------------------------------
+constexpr int kCopyThreads = 256, kCopyLoads = 8, kCopyBytes = kCopyThreads * kCopyLoads * 16;
+
+__global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const PagesCopyParams p, const int chunks) {
+  const int64_t pair = blockIdx.x / chunks;
+  const int chunk = (int)(blockIdx.x % chunks);
+  const int src = p.src[pair], dst = p.dst[pair];
+  if (src < 0 && dst < 0) return;  // a place without a pair
+  if (src < 0 || src >= p.num_pages || dst < 0 || dst >= p.num_pages) {
+    if (threadIdx.x == 0 && chunk == 0) record_error(p.err, HSWA_ERR_BOUNDS, (int)pair, src, dst);
+    return;
+  }
+  uint8_t* pool = static_cast<uint8_t*>(p.pools[blockIdx.y]);
+  const int64_t from = (int64_t)chunk * kCopyBytes + threadIdx.x * 16;
+  const uint4* s = reinterpret_cast<const uint4*>(pool + (int64_t)src * p.page_bytes + from);
+  uint4* d = reinterpret_cast<uint4*>(pool + (int64_t)dst * p.page_bytes + from);
+  uint4 v[kCopyLoads];
+#pragma unroll
+  for (int i = 0; i < kCopyLoads; ++i)
+    if (from + (int64_t)i * kCopyThreads * 16 < p.page_bytes) v[i] = s[i * kCopyThreads];
+#pragma unroll
+  for (int i = 0; i < kCopyLoads; ++i)
+    if (from + (int64_t)i * kCopyThreads * 16 < p.page_bytes) d[i * kCopyThreads] = v[i];
+}
+
+template <typename Kernel, typename Params>
+cudaError_t launch_cluster(Kernel kern, const Params& p, size_t smem, cudaStream_t s) {
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kBlocks, 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kBlocks;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, p);
+}
+
+size_t bitmap_bytes(int num_pages) { return (size_t)(((num_pages + 31) / 32 + kBlocks - 1) / kBlocks) * 8; }
+
+}  // namespace
+
+cudaError_t hswa_launch_pages_fork(const PagesForkParams& p, cudaStream_t s) {
+  return launch_cluster(pages_fork_kernel, p, ((size_t)p.rows_in * 2 + p.rows_out) * 4 + 8 + bitmap_bytes(p.num_pages), s);
+}
+cudaError_t hswa_launch_pages_compact(const PagesCompactParams& p, cudaStream_t s) {
+  return launch_cluster(pages_compact_kernel, p, bitmap_bytes(p.num_pages), s);
+}
+cudaError_t hswa_launch_pages_copy(const PagesCopyParams& p, cudaStream_t s) {
+  const int chunks = (int)((p.page_bytes + kCopyBytes - 1) / kCopyBytes);
+  pages_copy_kernel<<<dim3((unsigned)((int64_t)p.pairs * chunks), p.n_pools, 1), kCopyThreads, 0, s>>>(p, chunks);
+  return cudaGetLastError();
+}

@@ -1,0 +1,60 @@
+// Parameters of the page bookkeeping kernels.
+#pragma once
+
+#include "hswa_internal.cuh"
+
+// Limits of one call: rows of a table and pages of a pool whose bookkeeping fits a cluster's shared memory.
+constexpr int kMaxPageRows = 4096, kMaxPages = 1 << 23;
+constexpr int kPoolsPerLaunch = 64;
+
+struct PagesForkParams {
+  int32_t num_pages, page_size;
+  const int32_t* ref;  // [num_pages] holders of each page
+  int32_t* ref_out;
+  int32_t rows_in;
+  const int32_t* held;   // [rows_in] pages of each row
+  const int32_t* table;  // [rows_in][max_blocks]
+  int32_t max_blocks;
+  int32_t rows_out;
+  const int32_t* parent;  // [rows_out]
+  const int32_t* len;
+  const int32_t* need;
+  int32_t* table_out;  // [rows_out][out_max_blocks]
+  int32_t out_max_blocks;
+  int32_t* held_out;  // [rows_out]
+  int32_t* copy_src;
+  int32_t* copy_dst;
+  int32_t* fresh;  // scratch: [num_pages]
+  int32_t* err;
+};
+
+struct PagesCompactParams {
+  int32_t num_pages;
+  const int32_t* ref;
+  int32_t* ref_out;
+  int32_t rows;
+  const int32_t* held;
+  const int32_t* table;
+  int32_t max_blocks;
+  int32_t* table_out;
+  int32_t* page_map;  // [num_pages]
+  int32_t max_moves;
+  int32_t* move_src;
+  int32_t* move_dst;
+  int32_t* err;
+};
+
+struct PagesCopyParams {
+  void* pools[kPoolsPerLaunch];
+  int32_t n_pools;
+  int64_t page_bytes;
+  int64_t num_pages;
+  int32_t pairs;
+  const int32_t* src;
+  const int32_t* dst;
+  int32_t* err;
+};
+
+cudaError_t hswa_launch_pages_fork(const PagesForkParams& p, cudaStream_t s);
+cudaError_t hswa_launch_pages_compact(const PagesCompactParams& p, cudaStream_t s);
+cudaError_t hswa_launch_pages_copy(const PagesCopyParams& p, cudaStream_t s);
