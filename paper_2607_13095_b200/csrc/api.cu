@@ -200,28 +200,47 @@ bool plan_cross(const hswa_handle* h, int batch, int total_q, int max_q_len, int
   return true;
 }
 
-// Attention over a 4-bit cache: rows of a block, blocks along a request's rows, key slices.
+// Attention over a 4-bit cache: how one call is laid out, from host-known values only.
 struct PackedPlan {
-  int rows, row_tiles, slices, slice_len;
-  size_t o_bytes, ml_bytes;
+  int rows;                            // few rows per KV head: 8, 16 or 32 of a block; 0: the tile kernel
+  int runs;                            // few rows: runs of tiles, 0 for one block per stream
+  int row_tiles, slices, slice_len;    // the tile kernel: blocks along a request's rows, key slices
+  size_t o_bytes, ml_bytes, before_bytes;
 };
 
 bool plan_packed(const hswa_handle* h, int batch, int total_q, int max_q_len, int max_ctx_len, int causal, PackedPlan* pl) {
   PackedPlan c = {};
-  if ((int64_t)max_ctx_len + max_q_len > kMaxPositions || h->cfg.num_kv_heads > 65535) return false;
-  const int64_t rows = (int64_t)max_q_len * h->group;
-  c.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
-  c.row_tiles = (int)((rows + c.rows - 1) / c.rows);
-  const int keys = max_ctx_len + (causal ? max_q_len : 0), last = keys > 0 ? keys - 1 : 0;
-  const int64_t blocks = (int64_t)batch * c.row_tiles;
-  if (blocks > INT32_MAX) return false;
-  c.slice_len = keys <= kUnsplitLen ? kUnsplitLen : plan_split_len(h, (int)blocks, last, 2);
-  c.slices = plan_max_splits(c.slice_len, last);
-  if (blocks * c.slices > INT32_MAX || (int64_t)total_q * h->cfg.num_q_heads > INT32_MAX / 64) return false;
-  if (c.slices > 1) {
-    const size_t n = (size_t)total_q * h->cfg.num_q_heads * c.slices;
-    c.o_bytes = (n * h->cfg.head_dim * sizeof(float) + 255) & ~size_t(255);
-    c.ml_bytes = (n * sizeof(float2) + 255) & ~size_t(255);
+  if ((int64_t)max_ctx_len + max_q_len > kMaxPositions) return false;
+  const int64_t rows = (int64_t)max_q_len * h->group, streams = (int64_t)batch * h->cfg.num_kv_heads;
+  const int keys = max_ctx_len + (causal ? max_q_len : 0);
+  const auto align = [](size_t n) { return (n + 255) & ~size_t(255); };
+  if (streams > INT32_MAX) return false;
+  if (rows <= 32) {
+    c.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
+    if (keys > kUnsplitLen) {
+      // as many runs as blocks fit the SMs, of eight tiles at least (a block's seven warps take one each)
+      const int64_t fit = (int64_t)hswa_packed_decode_blocks_per_sm(c.rows) * h->num_sms, tiles = streams * ((keys + 63) / 64), most = (tiles + 7) / 8;
+      c.runs = (int)(fit < most ? fit : most);
+      c.o_bytes = align((size_t)2 * c.runs * c.rows * h->cfg.head_dim * sizeof(float));
+      c.ml_bytes = align((size_t)2 * c.runs * c.rows * sizeof(float2));
+      c.before_bytes = align(((size_t)batch + 1) * sizeof(int64_t));
+    }
+  } else {
+    const int tokens = 2 * hswa_cross_tile_tokens(model_params(h));
+    c.row_tiles = (int)(((int64_t)max_q_len + tokens - 1) / tokens);
+    const int64_t blocks = streams * c.row_tiles;
+    const int64_t want = (h->num_sms + blocks - 1) / blocks, most = ((int64_t)keys + 511) / 512;  // one wave of blocks
+    int64_t slices = want < most ? want : most;
+    if (slices < 1) slices = 1;
+    c.slice_len = (int)((((int64_t)keys + slices - 1) / slices + 127) / 128 * 128);
+    if (c.slice_len < 128) c.slice_len = 128;
+    c.slices = keys > 0 ? (keys + c.slice_len - 1) / c.slice_len : 1;
+    if (blocks * c.slices > INT32_MAX) return false;
+    if (c.slices > 1) {
+      const size_t n = (size_t)total_q * h->cfg.num_q_heads * c.slices;
+      c.o_bytes = align(n * h->cfg.head_dim * sizeof(float));
+      c.ml_bytes = align(n * sizeof(float2));
+    }
   }
   *pl = c;
   return true;
@@ -953,7 +972,7 @@ size_t hswa_packed_workspace_need(const hswa_handle* h, int32_t batch, int32_t t
   if (!h || batch <= 0 || total_q <= 0 || max_q_len <= 0 || max_q_len > total_q || max_ctx_len < 0 ||
       !plan_packed(h, batch, total_q, max_q_len, max_ctx_len, causal, &pl))
     return 0;
-  return pl.o_bytes + pl.ml_bytes;
+  return pl.o_bytes + pl.ml_bytes + pl.before_bytes;
 }
 
 hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, const hswa_batch* b, int32_t causal, const void* q, void* out,
@@ -965,8 +984,9 @@ hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, con
   if (!q || !out || !aligned16(q) || !aligned16(out)) return HSWA_ERR_INVALID_ARG;
   PackedPlan pl;
   if (!plan_packed(h, b->batch, b->total_q, b->max_q_len, b->max_ctx_len, causal, &pl)) return HSWA_ERR_UNSUPPORTED;
-  if (pl.o_bytes > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < pl.o_bytes + pl.ml_bytes))
-    return HSWA_ERR_WORKSPACE;
+  const size_t need = pl.o_bytes + pl.ml_bytes + pl.before_bytes;
+  if (need > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < need)) return HSWA_ERR_WORKSPACE;
+  char* ws = static_cast<char*>(workspace);
   PackedAttnParams p = {};
   p.m = model_params(h);
   p.b = batch_params(b);
@@ -981,14 +1001,19 @@ hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, con
   p.total_q = b->total_q;
   p.max_q_len = b->max_q_len;
   p.max_ctx_len = b->max_ctx_len;
+  p.runs = pl.runs;
+  p.row_tiles = pl.row_tiles;
   p.slice_len = pl.slice_len;
   p.slices = pl.slices;
-  p.row_tiles = pl.row_tiles;
-  p.part_o = pl.o_bytes > 0 ? static_cast<float*>(workspace) : nullptr;
-  p.part_ml = pl.o_bytes > 0 ? reinterpret_cast<float2*>(static_cast<char*>(workspace) + pl.o_bytes) : nullptr;
+  if (need > 0) {
+    p.part_o = reinterpret_cast<float*>(ws);
+    p.part_ml = reinterpret_cast<float2*>(ws + pl.o_bytes);
+    p.before = reinterpret_cast<int64_t*>(ws + pl.o_bytes + pl.ml_bytes);
+  }
   p.err = h->err;
   cudaStream_t s = (cudaStream_t)stream;
-  if (hswa_launch_packed_decode(p, pl.rows, s) != cudaSuccess) return HSWA_ERR_CUDA;
+  if (pl.rows > 0) return hswa_launch_packed_decode(p, pl.rows, s) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+  if (hswa_launch_packed_tile(p, s) != cudaSuccess) return HSWA_ERR_CUDA;
   if (pl.slices > 1) {
     const CrossParams join = {p.m, out, lse, b->total_q, b->q_indptr, b->batch, pl.slices, p.part_o, p.part_ml};
     if (hswa_launch_cross_combine(join, s) != cudaSuccess) return HSWA_ERR_CUDA;

@@ -20,8 +20,7 @@ __global__ void __launch_bounds__(128) cross_combine_kernel(const CrossParams p)
   const ModelParams& M = p.m;
   // launched early (programmatic dependent launch) behind the kernel that writes the partials
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (row >= (int64_t)p.total_q * M.Hq) return;
-  if (p.q_indptr && (row < (int64_t)p.q_indptr[0] * M.Hq || row >= (int64_t)p.q_indptr[p.batch] * M.Hq)) return;
+  if (row < (int64_t)p.q_indptr[0] * M.Hq || row >= (int64_t)min(p.q_indptr[p.batch], p.total_q) * M.Hq) return;
   const float2* ml = p.part_ml + row * p.slices;
   const float* po = p.part_o + row * p.slices * D;
   float mm = -INFINITY;

@@ -123,7 +123,7 @@ struct CrossParams {
   void* out;   // [T][Hq][D]
   float* lse;  // [T][Hq] or null
   int32_t total_q;
-  const int32_t* q_indptr;  // [batch + 1]: rows before the first request's and behind the last one's have no partials; null: all have
+  const int32_t* q_indptr;  // [batch + 1]: rows before the first request's and behind the last one's have no partials
   int32_t batch;
   int32_t slices;
   const float* part_o;    // [T * Hq][slices][D]

@@ -36,17 +36,23 @@ struct PackedAttnParams {
   void* out;               // [T][Hq][D]
   float* lse;              // [T][Hq] or null
   int32_t total_q, max_q_len, max_ctx_len;
-  int32_t slice_len, slices;  // keys per slice, slices per row
-  int32_t row_tiles;          // blocks along a request's rows
-  float* part_o;              // [T * Hq][slices][D]
-  float2* part_ml;            // [T * Hq][slices] (m in log2 units, l)
+  // few rows: runs of tiles (0: one stream per block) and the tiles of all requests before each, [B + 1]
+  int32_t runs;
+  int64_t* before;
+  // many rows: blocks along a request's rows, keys per slice (a multiple of 128), slices per row
+  int32_t row_tiles, slice_len, slices;
+  float* part_o;    // few rows: [2 runs][rows of a block][D]; many: [T * Hq][slices][D]
+  float2* part_ml;  // the same without D: (m in log2 units, l)
   int32_t* err;
 };
 
 cudaError_t hswa_launch_packed_append(const PackedCacheParams& p, int num_sms, cudaStream_t s);
 cudaError_t hswa_launch_packed_read(const PackedCacheParams& p, int num_sms, cudaStream_t s);
-// Rows (tokens x heads of a KV head) per block: 8, 16 or 32
+// Few rows (tokens x heads of a KV head): 8, 16 or 32 per block
+int hswa_packed_decode_blocks_per_sm(int rows);
 cudaError_t hswa_launch_packed_decode(const PackedAttnParams& p, int rows, cudaStream_t s);
+// Many rows: the tcgen05 tile kernel, two Q tiles of hswa_cross_tile_tokens tokens per block
+cudaError_t hswa_launch_packed_tile(const PackedAttnParams& p, cudaStream_t s);
 
 #ifdef __CUDACC__
 namespace hswa_dev {

@@ -1,23 +1,27 @@
-// Attention over a 4-bit cache for few rows per KV head (single tokens, drafts): hswa_packed_attn.
+// Attention over a 4-bit cache for few rows per KV head (single tokens, drafts: up to 32 tokens x query heads): hswa_packed_attn.
 //
-// A block takes one slice of a request's keys for one KV head and 8 NT rows (tokens x query heads).  One warp fetches the
-// pages' slabs (a bulk copy each: rows and scales lie together) into a ring of 64-key stages; every other warp takes whole
-// stages, with a softmax state of its own, and the block merges them at the end.  Bound by HBM (0.5625 bytes per element) and,
-// close behind, by the instructions that turn codes into fp16; so both products read their operands straight from the packed
-// rows, without a trip through shared memory:
+// The 64-key tiles of all (request, KV head) streams form one sequence, cut into equal runs, one for each of the blocks that the
+// SMs hold: no block ends early, whatever the lengths, and loads run on from stream to stream.  One warp fetches the pages'
+// slabs (a bulk copy each: rows and scales lie together) into a ring of stages; every other warp takes whole tiles, with a softmax
+// state of its own, and the block merges them where a stream ends.  A stream that a block has as a whole is written out there,
+// pieces of the others are joined by a second launch.
+// Bound by HBM (0.5625 bytes per element) and, close behind, by the instructions that turn codes into fp16; so both products
+// read their operands straight from the packed rows, without a trip through shared memory:
 //   S^T [keys x rows] = K Q^T: the element order along D is free as long as K and Q agree, so lane (g, t) of the fragment takes
 //     the t-th quarter of row g, contiguous: one load per row.  Scales multiply the fp16 values, which stay exact.
 //   O^T [D x rows] += V^T P^T: a lane needs neighbouring KEYS of one element side by side.  It reads 16 (D = 128) or 8
 //     neighbouring elements of two keys and exchanges nibbles: 4 logic instructions make 8 bytes of (key, key') pairs out of
 //     two words, and each converts at once.
 #include "packed.cuh"
+#include "tc_primitives.cuh"
 
 namespace {
 using namespace hswa_dev;
 
 constexpr int TK = 64;  // keys per stage
 constexpr int NW = 7;   // warps that compute: with the producer two per scheduler, so that a block's threads get 128 or 255 registers
-constexpr int NS = 12;  // stages
+// stages; with the sums of three warps, 2 blocks of up to 16 rows or one of 32 fill an SM
+constexpr int stages_of(int nt) { return nt == 1 ? 10 : nt == 2 ? 9 : 18; }
 constexpr int kThreads = (NW + 1) * 32;
 
 template <int D>
@@ -28,85 +32,42 @@ constexpr int kStageBytes = 2 * TK * (D / 2 + D / 16);
 // two of each parity, which halves the bank conflicts of 64-byte rows; K rows come in pairs of unlike parity.)
 __device__ __forceinline__ int key_of(int i) { return (i & 4) | ((i & 2) ? 3 - (i & 1) : (i & 1)); }
 
+// Keys of request r that the rows of a step see, and its tiles (one at least, if it has rows: zeros are written there too).
+struct Stream {
+  int t0, n, len, end, tiles;
+};
+__device__ __forceinline__ Stream stream_of(const PackedAttnParams& p, int r) {
+  Stream s;
+  s.t0 = p.b.q_indptr ? p.b.q_indptr[r] : r;
+  s.n = p.b.q_indptr ? min(p.b.q_indptr[r + 1] - s.t0, p.max_q_len) : 1;
+  s.len = max(0, min(p.b.ctx_len[r], p.max_ctx_len));
+  const int64_t room = (int64_t)p.b.max_blocks * p.m.P;  // positions that the block table has places for
+  s.end = (int)min((int64_t)(p.causal ? s.len + s.n : s.len), room);
+  s.tiles = s.n > 0 ? max(1, (s.end + TK - 1) / TK) : 0;
+  return s;
+}
+// First tile of run c of `runs` over `total` tiles.
+__device__ __forceinline__ int64_t run_start(int64_t total, int c, int runs) { return total * c / runs; }
+
 template <int D, int NT>
 __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kernel(const PackedAttnParams p) {
+  constexpr int NS = stages_of(NT);
   constexpr int ROW = D / 2, SC = D / 16, KS = D / 16, STAGE = kStageBytes<D>, HALF = STAGE / 2;
   constexpr int COLS = 8 * NT;
   constexpr int MT = D / 16;                // 16-row tiles of O^T
   constexpr int STEP = D == 64 && NT < 4 ? TK : TK / NT;  // keys per softmax step (registers)
   constexpr int GROUPS = STEP / 16;
   extern __shared__ __align__(128) uint8_t smem[];
-  uint2* s_q = reinterpret_cast<uint2*>(smem + NS * STAGE);                 // [NT][KS][32] fragments of Q
+  float4* box = reinterpret_cast<float4*>(smem + NS * STAGE);              // [3][MT][NT][32] sums on their way
+  uint2* s_q = reinterpret_cast<uint2*>(box + 3 * MT * NT * 32);           // [NT][KS][32] fragments of Q
   float* s_down = reinterpret_cast<float*>(s_q + NT * KS * 32);            // [COLS]
   float2* s_ml = reinterpret_cast<float2*>(s_down + COLS);                 // [NW][COLS]
   uint64_t* bars = reinterpret_cast<uint64_t*>(s_ml + NW * COLS);          // full [NS], empty [NS]
+  int64_t* s_plan = reinterpret_cast<int64_t*>(bars + 2 * NS);             // a wait ran out, first request, tiles before it, a warp's sum [8]
   const ModelParams& M = p.m;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
-
-  const int r = blockIdx.x % p.b.B, rest = blockIdx.x / p.b.B;
-  const int rt = rest % p.row_tiles, slice = rest / p.row_tiles, kh = blockIdx.y;
-  const int t0 = p.b.q_indptr ? p.b.q_indptr[r] : r;
-  const int n = p.b.q_indptr ? p.b.q_indptr[r + 1] - t0 : 1;
-  const int ctx = p.b.ctx_len[r];
-  if (threadIdx.x == 0 && rt == 0 && slice == 0 && kh == 0) {  // the grid was sized from the host's bounds
-    if (ctx < 0 || ctx > p.max_ctx_len) record_error(p.err, HSWA_ERR_BOUNDS, r, -1, ctx);
-    if (n < 0 || n > p.max_q_len || t0 < 0 || (int64_t)t0 + n > p.total_q) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, n);
-  }
-  const int len = max(0, min(ctx, p.max_ctx_len));
-  auto has_row = [&](int tok) { return (unsigned)t0 + (unsigned)tok < (unsigned)p.total_q; };
-  const int n_here = min(n, p.max_q_len);  // tokens that the grid covers
-  if (p.slices > 1 && rt == 0 && slice == 0) {
-    // rows past the host's bound have no block: a mark tells the join to leave them alone
-    for (int64_t tok = (int64_t)p.max_q_len + threadIdx.x; tok < n; tok += kThreads)
-      if (has_row((int)tok))
-        for (int h = 0; h < M.G; ++h) p.part_ml[(((int64_t)t0 + tok) * M.Hq + kh * M.G + h) * p.slices] = make_float2(-INFINITY, -1.f);
-  }
-  const int row0 = rt * COLS, rows = n_here * M.G - row0;  // rows left from this block's first on
-  if (rows <= 0) return;
-  const int last_tok = (row0 + min(rows, COLS) - 1) / M.G;
-  const int64_t room = (int64_t)p.b.max_blocks * M.P;  // positions that the block table has places for
-  int end = p.causal ? len + last_tok + 1 : len;       // keys that the block's last row sees
-  if (end > room) {
-    if (threadIdx.x == 0) record_error(p.err, HSWA_ERR_BOUNDS, r, -3, end);
-    end = (int)room;
-  }
-  const int k0 = slice * p.slice_len;
-  const int k1 = min(end, k0 + p.slice_len);
-  const int tiles = k1 > k0 ? (k1 - k0 + TK - 1) / TK : 0;
-  const int first_end = p.causal ? min(end, len + row0 / M.G + 1) : end;  // keys that its first row sees
-
-  auto store_row = [&](int col, int d, const float* v, int count) {  // count = 8 or 16 neighbouring elements of a row
-    const int row = row0 + col, tok = row / M.G;
-    if (col >= rows || !has_row(tok)) return;
-    const int64_t orow = (int64_t)(t0 + tok) * M.Hq + kh * M.G + row % M.G;
-    if (p.slices > 1 || M.out_fp32) {
-      float* dst = p.slices > 1 ? p.part_o + (orow * p.slices + slice) * D + d : reinterpret_cast<float*>(p.out) + orow * D + d;
-      for (int k = 0; k < count; k += 4) *reinterpret_cast<float4*>(dst + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
-    } else {
-      __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.out) + orow * D + d;
-      for (int k = 0; k < count; k += 8)
-        *reinterpret_cast<uint4*>(dst + k) = make_uint4(pack_bf16x2(v[k], v[k + 1]), pack_bf16x2(v[k + 2], v[k + 3]),
-                                                        pack_bf16x2(v[k + 4], v[k + 5]), pack_bf16x2(v[k + 6], v[k + 7]));
-    }
-  };
-  auto store_ml = [&](int col, float m, float l) {
-    const int row = row0 + col, tok = row / M.G;
-    if (col >= rows || !has_row(tok)) return;
-    const int64_t orow = (int64_t)(t0 + tok) * M.Hq + kh * M.G + row % M.G;
-    if (p.slices > 1)
-      p.part_ml[orow * p.slices + slice] = make_float2(m, l);
-    else if (p.lse)
-      p.lse[orow] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
-  };
-
-  if (tiles == 0) {  // no key here: zeros, or a partial that the join passes over
-    const float zero[8] = {};
-    for (int i = threadIdx.x; i < COLS; i += kThreads) store_ml(i, -INFINITY, 0.f);
-    if (p.slices == 1)
-      for (int i = threadIdx.x; i < COLS * D / 8; i += kThreads) store_row(i / (D / 8), i % (D / 8) * 8, zero, 8);
-    return;
-  }
+  const int B = p.b.B;
 
   const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + NS);
   if (threadIdx.x == 0) {
@@ -116,17 +77,147 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
     }
     mbar_fence_init();
   }
-  // Q: warp w < NT brings its eight rows into fragment order
-  if (warp < NT) {
-    const int col = warp * 8 + g, row = row0 + col, tok = row / M.G;
+  if (blockIdx.x == 0)  // the grid was sized from the host's bounds
+    for (int r = threadIdx.x; r < B; r += kThreads) {
+      const int ctx = p.b.ctx_len[r], t0 = p.b.q_indptr ? p.b.q_indptr[r] : r, n = p.b.q_indptr ? p.b.q_indptr[r + 1] - t0 : 1;
+      const Stream s = stream_of(p, r);
+      if (ctx < 0 || ctx > p.max_ctx_len) record_error(p.err, HSWA_ERR_BOUNDS, r, -1, ctx);
+      if (n < 0 || n > p.max_q_len || t0 < 0 || (int64_t)t0 + n > p.total_q) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, n);
+      if (p.causal && s.n > 0 && s.end < s.len + s.n) record_error(p.err, HSWA_ERR_BOUNDS, r, -3, s.len + s.n);
+    }
+  // the block's run of tiles [w0, w1), and the request that it starts in
+  int64_t w0, w1;
+  int r0, kh0 = 0, tile0 = 0;
+  if (p.runs == 0) {  // one stream per block
+    r0 = blockIdx.x / M.Hkv;
+    kh0 = blockIdx.x % M.Hkv;
+    w0 = 0;
+    w1 = stream_of(p, r0).tiles;
+    if (threadIdx.x == 0) s_plan[0] = 0;
+    __syncthreads();
+    if (w1 == 0) return;
+  } else {
+    const int per = (B + kThreads - 1) / kThreads, i0 = min((int)threadIdx.x * per, B), i1 = min(i0 + per, B);
+    int64_t mine = 0;
+    for (int i = i0; i < i1; ++i) mine += stream_of(p, i).tiles;
+    int64_t incl = mine;
+#pragma unroll
+    for (int sh = 1; sh < 32; sh <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, incl, sh);
+      if (lane >= sh) incl += v;
+    }
+    if (lane == 31) s_plan[3 + warp] = incl;
+    if (threadIdx.x == 0) s_plan[0] = 0;
+    __syncthreads();
+    int64_t total = 0, before = incl - mine;
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) before += s_plan[3 + w];
+      total += s_plan[3 + w];
+    }
+    total *= M.Hkv;
+    w0 = run_start(total, blockIdx.x, p.runs);
+    w1 = run_start(total, blockIdx.x + 1, p.runs);
+    for (int i = i0; i < i1; ++i) {
+      const int tiles = stream_of(p, i).tiles;
+      if (blockIdx.x == 0) p.before[i] = before;  // for the join
+      if (w0 >= before * M.Hkv && w0 < (before + tiles) * M.Hkv) {
+        s_plan[1] = i;
+        s_plan[2] = before;
+      }
+      before += tiles;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.before[B] = total / M.Hkv;
+    __syncthreads();
+    if (w0 >= w1) return;
+    r0 = (int)s_plan[1];
+    const int64_t at = w0 - s_plan[2] * M.Hkv;
+    const int tiles = stream_of(p, r0).tiles;
+    kh0 = (int)(at / tiles);
+    tile0 = (int)(at % tiles);
+  }
+  const int slab = M.P * (ROW + SC);
+  if (warp == NW) {
+    // ======================= producer =======================
+    const int ppt = TK / M.P;  // pages per stage: 1, 2 or 4
+    const int i = lane % ppt, kv = lane / ppt;
+    bool ok = true;
+    int64_t w = w0;
+    int r = r0, kh = kh0, tile = tile0;
+    int at = 0;  // stages filled
+    while (w < w1 && ok) {
+      const Stream s = stream_of(p, r);
+      const int count = (int)min((int64_t)(s.tiles - tile), w1 - w);
+      const int32_t* tbl = p.b.block_table + (int64_t)r * p.b.max_blocks;
+      const int n_pages = (s.end + M.P - 1) / M.P;  // (0: a request without keys)
+      const int page0 = tile * ppt;
+      int ids_next = page0 + lane < n_pages ? tbl[page0 + lane] : 0, ids = 0;
+      for (int j = 0; j < count; ++j, ++at) {
+        const int stage = at % NS, first = j * ppt;
+        if ((first & 31) == 0) {
+          ids = ids_next;
+          ids_next = page0 + first + 32 + lane < n_pages ? tbl[page0 + first + 32 + lane] : 0;
+        }
+        const int here = min(ppt, n_pages - page0 - first);  // pages of this tile
+        int page = __shfl_sync(0xffffffffu, ids, (first + i) & 31);
+        if (at >= NS) ok = __all_sync(0xffffffffu, mbar_wait(empty0 + 8 * stage, ((at / NS) - 1) & 1));
+        if (!ok) {
+          if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, j, 50);
+          break;
+        }
+        if (lane == 0) mbar_arrive_expect_tx(full0 + 8 * stage, 2 * max(here, 0) * slab);
+        __syncwarp();
+        if (kv < 2 && i < here) {
+          if (page < 0 || page >= p.num_pages) {
+            record_error(p.err, HSWA_ERR_BOUNDS, r, page0 + first + i, page);
+            page = 0;
+          }
+          bulk_load(smem_u32(smem + stage * STAGE + kv * HALF + i * slab), p.pool + (((int64_t)page * 2 + kv) * M.Hkv + kh) * slab, slab,
+                    full0 + 8 * stage);
+        }
+      }
+      w += count;
+      tile = 0;
+      if (++kh == M.Hkv) {
+        kh = 0;
+        do ++r; while (w < w1 && stream_of(p, r).tiles == 0);  // (requests with rows are left: w < w1)
+      }
+    }
+    if (!ok) __nanosleep(100000);  // copies that nobody will wait for land before the block's memory is handed on
+    return;
+  }
+
+  // ======================= consumers =======================
+  const int kg = key_of(g), ka = key_of(2 * t), kb = key_of(2 * t + 1);
+  // where the rows and scales of a 16-key group of a stage lie (a group is inside one page)
+  const int page_shift = 31 - __clz(M.P), scales_at = M.P * ROW;
+  auto rows_of = [&](int key0) { return (key0 >> page_shift) * slab + (key0 & (M.P - 1)) * ROW; };
+  auto scales_of = [&](int key0) { return (key0 >> page_shift) * slab + scales_at + (key0 & (M.P - 1)) * SC; };
+  auto consumers_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(NW * 32) : "memory"); };
+  int64_t w = w0;
+  int r = r0, kh = kh0, tile = tile0;
+  int at0 = 0;  // stages before this piece
+  bool ok = true;
+  while (w < w1) {
+  const Stream sm = stream_of(p, r);
+  const int count = (int)min((int64_t)(sm.tiles - tile), w1 - w);
+  const int rows = sm.n * M.G, end = sm.end;
+  const int first_end = p.causal ? min(end, sm.len + 1) : end;  // keys that the first row sees
+  auto has_row = [&](int tok) { return (unsigned)sm.t0 + (unsigned)tok < (unsigned)p.total_q; };
+
+  // Q in fragment order, each row times its power of two: by every warp for itself, or by NT warps for all
+  uint2 qf[NT == 1 ? KS : 1];
+  float down1 = 0.f;
+  if (NT == 1 || warp < NT) {
+    const int col = (NT == 1 ? 0 : warp * 8) + g, tok = col / M.G;
     const bool there = col < rows && has_row(tok);
-    uint4 w[D / 32];  // the t-th quarter of the row: D / 4 elements
-    const uint4* src = reinterpret_cast<const uint4*>(p.q + ((int64_t)(t0 + tok) * M.Hq + kh * M.G + row % M.G) * D + t * (D / 4));
+    uint4 wq[D / 32];  // the t-th quarter of the row: D / 4 elements
+    const uint4* src = reinterpret_cast<const uint4*>(p.q + ((int64_t)(sm.t0 + tok) * M.Hq + kh * M.G + col % M.G) * D + t * (D / 4));
     float amax = 0.f;
 #pragma unroll
+    for (int k = 0; k < D / 32; ++k) wq[k] = there ? src[k] : make_uint4(0, 0, 0, 0);
+#pragma unroll
     for (int k = 0; k < D / 32; ++k) {
-      w[k] = there ? src[k] : make_uint4(0, 0, 0, 0);
-      const uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+      const uint32_t u[4] = {wq[k].x, wq[k].y, wq[k].z, wq[k].w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float2 f = unpack_bf16x2(u[e]);
@@ -137,57 +228,23 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
     float up, down;
     q_powers(amax, &up, &down);
+    down = fmaxf(down * p.scale_log2, 0x1p-126f);  // (never 0: a masked score stays minus infinity)
 #pragma unroll
     for (int k = 0; k < D / 32; ++k) {
-      const uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+      const uint32_t u[4] = {wq[k].x, wq[k].y, wq[k].z, wq[k].w};
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float2 lo = unpack_bf16x2(u[2 * e]), hi = unpack_bf16x2(u[2 * e + 1]);
-        s_q[(warp * KS + 2 * k + e) * 32 + lane] = make_uint2(pack_half2(lo.x * up, lo.y * up), pack_half2(hi.x * up, hi.y * up));
+        const uint2 v = make_uint2(pack_half2(lo.x * up, lo.y * up), pack_half2(hi.x * up, hi.y * up));
+        if constexpr (NT == 1) qf[2 * k + e] = v;
+        else s_q[(warp * KS + 2 * k + e) * 32 + lane] = v;
       }
     }
-    if (t == 0) s_down[col] = down * p.scale_log2;
+    if constexpr (NT == 1) down1 = down;
+    else if (t == 0) s_down[col] = down;
   }
-  __syncthreads();
+  if constexpr (NT > 1) consumers_sync();
 
-  const int slab = M.P * (ROW + SC);
-  if (warp == NW) {
-    // ======================= producer =======================
-    const int ppt = TK / M.P;  // pages per stage: 1, 2 or 4
-    const int32_t* tbl = p.b.block_table + (int64_t)r * p.b.max_blocks + k0 / M.P;
-    const int n_pages = (k1 - k0 + M.P - 1) / M.P;
-    int ids_next = lane < n_pages ? tbl[lane] : 0, ids = 0;
-    bool ok = true;
-    for (int j = 0; j < tiles && ok; ++j) {
-      const int stage = j % NS, first = j * ppt;
-      if ((first & 31) == 0) {
-        ids = ids_next;
-        ids_next = first + 32 + lane < n_pages ? tbl[first + 32 + lane] : 0;
-      }
-      const int here = min(ppt, n_pages - first);  // pages of this stage
-      const int i = lane % ppt, kv = lane / ppt;
-      int page = __shfl_sync(0xffffffffu, ids, (first + i) & 31);
-      if (j >= NS) ok = __all_sync(0xffffffffu, mbar_wait(empty0 + 8 * stage, ((j / NS) - 1) & 1));
-      if (!ok) {
-        if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, j, 50);
-        break;
-      }
-      if (lane == 0) mbar_arrive_expect_tx(full0 + 8 * stage, 2 * here * slab);
-      __syncwarp();
-      if (kv < 2 && i < here) {
-        if (page < 0 || page >= p.num_pages) {
-          record_error(p.err, HSWA_ERR_BOUNDS, r, k0 / M.P + first + i, page);
-          page = 0;
-        }
-        bulk_load(smem_u32(smem + stage * STAGE + kv * HALF + i * slab), p.pool + (((int64_t)page * 2 + kv) * M.Hkv + kh) * slab, slab,
-                  full0 + 8 * stage);
-      }
-    }
-    if (!ok) __nanosleep(100000);  // copies that nobody will wait for land before the block's memory is handed on
-    return;
-  }
-
-  // ======================= consumers =======================
   float O[MT][NT][4];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -204,36 +261,30 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
       m[c][e] = -INFINITY;
       l[c][e] = 0.f;
       const int col = c * 8 + 2 * t + e;
-      mul[c][e] = s_down[col];
-      see[c][e] = p.causal ? min(end, len + (row0 + col) / M.G + 1) : end;
+      mul[c][e] = NT == 1 ? __shfl_sync(0xffffffffu, down1, (2 * t + e) * 4) : s_down[col];
+      see[c][e] = p.causal ? min(end, sm.len + col / M.G + 1) : end;
     }
-  uint2 qf[NT == 1 ? KS : 1];
-  if constexpr (NT == 1) {
-#pragma unroll
-    for (int s = 0; s < KS; ++s) qf[s] = s_q[s * 32 + lane];
-  }
-  const int kg = key_of(g), ka = key_of(2 * t), kb = key_of(2 * t + 1);
-  bool ok = true;
-  for (int j = warp; j < tiles; j += NW) {
-    const int stage = j % NS;
-    ok = __all_sync(0xffffffffu, mbar_wait(full0 + 8 * stage, (j / NS) & 1));
+  // the warp's tiles: every NW-th of the piece
+  for (int j = warp; j < count; j += NW) {
+    const int stage = (at0 + j) % NS;
+    ok = __all_sync(0xffffffffu, mbar_wait(full0 + 8 * stage, ((at0 + j) / NS) & 1));
     if (!ok) {
       if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, j, 51);
+      *reinterpret_cast<volatile int64_t*>(s_plan) = 1;
       __nanosleep(100000);  // (copies in flight, as above)
       break;
     }
     const uint8_t* st = smem + stage * STAGE;
-    const int pos0 = k0 + j * TK;
+    const int pos0 = (tile + j) * TK;
     const bool masked = pos0 + TK > first_end;
-#pragma unroll
+#pragma unroll 1
     for (int step = 0; step < TK / STEP; ++step) {
-      if (masked && pos0 + step * STEP >= k1) break;  // nothing of the slice behind here
+      if (masked && pos0 + step * STEP >= end) break;  // no keys behind here
       float S[GROUPS][NT][4];
 #pragma unroll
       for (int q = 0; q < GROUPS; ++q) {
-        const int key0 = step * STEP + q * 16, pg = key0 / M.P;
-        const uint8_t* rows_at = st + pg * slab + (key0 - pg * M.P) * ROW;
-        const uint8_t* sc_at = st + pg * slab + M.P * ROW + (key0 - pg * M.P) * SC;
+        const uint8_t* rows_at = st + rows_of(step * STEP + q * 16);
+        const uint8_t* sc_at = st + scales_of(step * STEP + q * 16);
         uint32_t wa[D / 32], wb[D / 32];
         uint32_t fa, fb;
         if constexpr (D == 128) {
@@ -270,25 +321,33 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
           }
         }
       }
-      // scores in log2 units, masks, the running maximum of each row (column of S^T)
+      // masks, the running maximum of each row (column of S^T) in log2 units
+      if (masked) {
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+          for (int q = 0; q < GROUPS; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (pos0 + step * STEP + q * 16 + kg + (e >> 1) * 8 >= see[c][e & 1]) S[q][c][e] = -INFINITY;
+      }
       uint32_t P[GROUPS][NT][2];
 #pragma unroll
       for (int c = 0; c < NT; ++c) {
-        float mx[2] = {-INFINITY, -INFINITY};
+        float mx[2];
 #pragma unroll
-        for (int q = 0; q < GROUPS; ++q)
+        for (int e = 0; e < 2; ++e) {
+          mx[e] = fmaxf(S[0][c][e], S[0][c][e + 2]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x = S[q][c][e] * mul[c][e & 1];
-            if (masked && pos0 + step * STEP + q * 16 + kg + (e >> 1) * 8 >= see[c][e & 1]) x = -INFINITY;
-            S[q][c][e] = x;
-            mx[e & 1] = fmaxf(mx[e & 1], x);
-          }
+          for (int q = 1; q < GROUPS; ++q) mx[e] = max3(mx[e], S[q][c][e], S[q][c][e + 2]);
+        }
 #pragma unroll
         for (int sh = 4; sh <= 16; sh <<= 1) {
           mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], sh));
           mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], sh));
         }
+        mx[0] *= mul[c][0];
+        mx[1] *= mul[c][1];
         // O moves to a new maximum only when that grew by more than 2^8 (P stays within fp16)
         const bool grow0 = mx[0] > m[c][0] + 8.f, grow1 = mx[1] > m[c][1] + 8.f;
         if (__any_sync(0xffffffffu, grow0 || grow1)) {
@@ -308,8 +367,8 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
         const float mu0 = m[c][0] == -INFINITY ? 0.f : m[c][0], mu1 = m[c][1] == -INFINITY ? 0.f : m[c][1];
 #pragma unroll
         for (int q = 0; q < GROUPS; ++q) {
-          const float e0 = fast_exp2(S[q][c][0] - mu0), e1 = fast_exp2(S[q][c][1] - mu1), e2 = fast_exp2(S[q][c][2] - mu0),
-                      e3 = fast_exp2(S[q][c][3] - mu1);
+          const float e0 = fast_exp2(fmaf(S[q][c][0], mul[c][0], -mu0)), e1 = fast_exp2(fmaf(S[q][c][1], mul[c][1], -mu1)),
+                      e2 = fast_exp2(fmaf(S[q][c][2], mul[c][0], -mu0)), e3 = fast_exp2(fmaf(S[q][c][3], mul[c][1], -mu1));
           l[c][0] += e0 + e2;
           l[c][1] += e1 + e3;
           P[q][c][0] = movmatrix_trans(pack_half2(e0, e1));
@@ -318,14 +377,13 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
       }
 #pragma unroll
       for (int q = 0; q < GROUPS; ++q) {
-        const int key0 = step * STEP + q * 16, pg = key0 / M.P;
-        const uint8_t* rows_at = st + HALF + pg * slab + (key0 - pg * M.P) * ROW;
-        const uint8_t* sc_at = st + HALF + pg * slab + M.P * ROW + (key0 - pg * M.P) * SC;
+        const uint8_t* rows_at = st + HALF + rows_of(step * STEP + q * 16);
+        const uint8_t* sc_at = st + HALF + scales_of(step * STEP + q * 16);
         const int blk = D == 128 ? g : g >> 1;
         uint32_t f0 = sc_at[ka * SC + blk] | (uint32_t)sc_at[kb * SC + blk] << 8;
         uint32_t f1 = sc_at[(ka + 8) * SC + blk] | (uint32_t)sc_at[(kb + 8) * SC + blk] << 8;
         if (masked) {  // rows behind the last visible key hold anything, scales of NaN included: zero times their codes
-          const int at = pos0 + key0;
+          const int at = pos0 + step * STEP + q * 16;
           f0 &= (at + ka < end ? 0xffu : 0u) | (at + kb < end ? 0xff00u : 0u);
           f1 &= (at + ka + 8 < end ? 0xffu : 0u) | (at + kb + 8 < end ? 0xff00u : 0u);
         }
@@ -359,7 +417,8 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
     if (lane == 0) mbar_arrive(empty0 + 8 * stage);
   }
 
-  // ---- merge of the warps' states ----
+  // ---- the piece's end: merge of the warps' states ----
+  const bool whole = tile == 0 && count == sm.tiles;
 #pragma unroll
   for (int c = 0; c < NT; ++c)
 #pragma unroll
@@ -368,8 +427,8 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
       for (int sh = 4; sh <= 16; sh <<= 1) l[c][e] += __shfl_xor_sync(0xffffffffu, l[c][e], sh);
       if (g == 0) s_ml[warp * COLS + c * 8 + 2 * t + e] = make_float2(m[c][e], l[c][e]);
     }
-  auto consumers_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(NW * 32) : "memory"); };
   consumers_sync();
+  if (*reinterpret_cast<volatile int64_t*>(s_plan) != 0) return;
   float L[NT][2], top[NT][2];
 #pragma unroll
   for (int c = 0; c < NT; ++c)
@@ -378,19 +437,19 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
       const int col = c * 8 + 2 * t + e;
       float mm = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) mm = fmaxf(mm, s_ml[w * COLS + col].x);
+      for (int k = 0; k < NW; ++k) mm = fmaxf(mm, s_ml[k * COLS + col].x);
       const float base = mm == -INFINITY ? 0.f : mm;
       float sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const float2 v = s_ml[w * COLS + col];
+      for (int k = 0; k < NW; ++k) {
+        const float2 v = s_ml[k * COLS + col];
         sum += v.y != 0.f ? v.y * fast_exp2(v.x == -INFINITY ? 0.f : v.x - base) : 0.f;  // (l of NaN scores: m says nothing)
       }
       const float f = m[c][e] == -INFINITY ? 1.f : fast_exp2(m[c][e] - base);
       top[c][e] = mm;
       L[c][e] = sum;
       // the layer's V scale, and the division where the block has all of the row's keys
-      const float out = f * (p.slices > 1 ? p.v_scale : (sum != 0.f ? p.v_scale / sum : 0.f));
+      const float out = f * (!whole ? p.v_scale : (sum != 0.f ? p.v_scale / sum : 0.f));
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         O[i][c][e] *= out;
@@ -398,8 +457,7 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
       }
     }
   // the upper half of the warps hands its sums to the lower half, three times (same lane, same registers)
-  float4* box = reinterpret_cast<float4*>(smem);
-  static_assert(NW <= 8 && 4 * MT * NT * 32 * 16 <= NS * kStageBytes<D>, "sums fit the stages");
+  static_assert(NW == 7, "three warps hand over at most");
 #pragma unroll
   for (int half = 4; half >= 1; half >>= 1) {
     if (warp >= half && warp < 2 * half) {
@@ -423,35 +481,138 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
     }
     if (half > 1) consumers_sync();
   }
-  if (warp != 0) return;
-  // a lane holds D / 8 neighbouring elements of two rows per eight
+  if (warp == 0) {
+    // a lane holds D / 8 neighbouring elements of two rows per eight
+    const int64_t piece = 2 * (int64_t)blockIdx.x + (tile == 0);  // a block has one piece at most that starts before it, and one that ends behind it
 #pragma unroll
-  for (int c = 0; c < NT; ++c)
+    for (int c = 0; c < NT; ++c)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float v[2 * MT];
+      for (int e = 0; e < 2; ++e) {
+        const int col = c * 8 + 2 * t + e, tok = col / M.G;
+        if (col >= rows || !has_row(tok)) continue;
+        const int64_t orow = (int64_t)(sm.t0 + tok) * M.Hq + kh * M.G + col % M.G;
+        if (!whole || M.out_fp32) {
+          float* dst = (!whole ? p.part_o + (piece * COLS + col) * D : reinterpret_cast<float*>(p.out) + orow * D) + g * (D / 8);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        v[2 * i] = O[i][c][e];
-        v[2 * i + 1] = O[i][c][e + 2];
+          for (int i = 0; i < MT; i += 2)
+            *reinterpret_cast<float4*>(dst + 2 * i) = make_float4(O[i][c][e], O[i][c][e + 2], O[i + 1][c][e], O[i + 1][c][e + 2]);
+        } else {
+          __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.out) + orow * D + g * (D / 8);
+#pragma unroll
+          for (int i = 0; i < MT; i += 4)
+            *reinterpret_cast<uint4*>(dst + 2 * i) =
+                make_uint4(pack_bf16x2(O[i][c][e], O[i][c][e + 2]), pack_bf16x2(O[i + 1][c][e], O[i + 1][c][e + 2]),
+                           pack_bf16x2(O[i + 2][c][e], O[i + 2][c][e + 2]), pack_bf16x2(O[i + 3][c][e], O[i + 3][c][e + 2]));
+        }
+        if (g == 0) {
+          if (!whole) p.part_ml[piece * COLS + col] = make_float2(top[c][e], L[c][e]);
+          else if (p.lse) p.lse[orow] = L[c][e] != 0.f ? (top[c][e] + log2f(L[c][e])) * 0.6931471805599453f : -INFINITY;
+        }
       }
-      const int col = c * 8 + 2 * t + e;
-      store_row(col, g * (D / 8), v, D / 8);
-      if (g == 0) store_ml(col, top[c][e], L[c][e]);
+  }
+  w += count;
+  at0 += count;
+  tile = 0;
+  if (++kh == M.Hkv) {
+    kh = 0;
+    do ++r; while (w < w1 && stream_of(p, r).tiles == 0);
+  }
+  }
+}
+
+// Joins the pieces of the streams that several blocks had: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  A block per
+// stream and row, its four warps take every fourth piece.
+template <int D>
+__global__ void __launch_bounds__(128) packed_join_kernel(const PackedAttnParams p, const int cols) {
+  const ModelParams& M = p.m;
+  const int r = blockIdx.x / M.Hkv, kh = blockIdx.x % M.Hkv, col = blockIdx.y;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const Stream s = stream_of(p, r);
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // launched early behind the kernel that writes the pieces
+  if (s.tiles == 0 || col >= s.n * M.G) return;
+  const int64_t total = p.before[p.b.B] * M.Hkv, start = p.before[r] * M.Hkv + (int64_t)kh * s.tiles;
+  // run c holds tile x: c = ceil((x + 1) runs / total) - 1
+  const int c0 = (int)(((start + 1) * p.runs - 1) / total), c1 = (int)(((start + s.tiles) * p.runs - 1) / total);
+  const int tok = col / M.G;
+  if (c0 == c1 || (unsigned)s.t0 + (unsigned)tok >= (unsigned)p.total_q) return;
+  auto piece_of = [&](int c) { return (2 * (int64_t)c + (c == c0)) * cols + col; };
+  // a run without tiles (more runs than tiles) left no piece; nor has a piece without a key of the row anything (l = 0)
+  auto ml_of = [&](int c) {
+    return run_start(total, c, p.runs) < run_start(total, c + 1, p.runs) ? p.part_ml[piece_of(c)] : make_float2(-INFINITY, 0.f);
+  };
+  float mm = -INFINITY;
+  for (int c = c0 + lane; c <= c1; c += 32) {
+    const float2 v = ml_of(c);
+    if (v.y != 0.f) mm = fmaxf(mm, v.x);
+  }
+#pragma unroll
+  for (int sh = 16; sh >= 1; sh >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, sh));
+  constexpr int PER = D / 32;
+  float acc[PER] = {}, L = 0.f;
+#pragma unroll 4
+  for (int c = c0 + warp; c <= c1; c += 4) {
+    const float2 v = ml_of(c);
+    const float f = v.y != 0.f ? fast_exp2(v.x == -INFINITY ? 0.f : v.x - mm) : 0.f;  // (l of NaN scores: m says nothing)
+    const float* o = p.part_o + piece_of(c) * D + lane * PER;
+    L += v.y != 0.f ? f * v.y : 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; i += 2) {
+      const float2 x = *reinterpret_cast<const float2*>(o + i);
+      acc[i] += v.y != 0.f ? f * x.x : 0.f;
+      acc[i + 1] += v.y != 0.f ? f * x.y : 0.f;
     }
+  }
+  __shared__ float sums[3][32][PER + 1];
+  if (warp > 0) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sums[warp - 1][lane][i] = acc[i];
+    sums[warp - 1][lane][PER] = L;
+  }
+  __syncthreads();
+  if (warp > 0) return;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) acc[i] += sums[k][lane][i];
+    L += sums[k][lane][PER];
+  }
+  const float inv = L != 0.f ? 1.f / L : 0.f;
+  const int64_t orow = (int64_t)(s.t0 + tok) * M.Hq + kh * M.G + col % M.G;
+#pragma unroll
+  for (int i = 0; i < PER; i += 2) {
+    const int64_t at = orow * D + lane * PER + i;
+    if (M.out_fp32)
+      *reinterpret_cast<float2*>(reinterpret_cast<float*>(p.out) + at) = make_float2(acc[i] * inv, acc[i + 1] * inv);
+    else
+      *reinterpret_cast<__nv_bfloat162*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at) = __floats2bfloat162_rn(acc[i] * inv, acc[i + 1] * inv);
+  }
+  if (lane == 0 && p.lse) p.lse[orow] = L != 0.f ? (mm + log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
 template <int D, int NT>
 cudaError_t launch(const PackedAttnParams& p, cudaStream_t s) {
-  constexpr int SMEM = NS * kStageBytes<D> + NT * (D / 16) * 32 * 8 + 8 * NT * 4 + NW * 8 * NT * 8 + 2 * NS * 8;
+  constexpr int NS = stages_of(NT);
+  constexpr int SMEM = NS * kStageBytes<D> + 3 * D * NT * 32 + NT * D * 16 + 32 * NT + NW * 64 * NT + 16 * NS + 8 * (3 + kThreads / 32);
   auto kern = packed_decode_kernel<D, NT>;
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
   if (e != cudaSuccess) return e;
-  kern<<<dim3((unsigned)((int64_t)p.b.B * p.row_tiles * p.slices), p.m.Hkv, 1), kThreads, SMEM, s>>>(p);
-  return cudaGetLastError();
+  kern<<<p.runs > 0 ? p.runs : p.b.B * p.m.Hkv, kThreads, SMEM, s>>>(p);
+  if ((e = cudaGetLastError()) != cudaSuccess || p.runs == 0) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.b.B * p.m.Hkv, p.max_q_len * p.m.G, 1);
+  cfg.blockDim = dim3(128, 1, 1);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, packed_join_kernel<D>, p, 8 * NT);
 }
 
 }  // namespace
+
+int hswa_packed_decode_blocks_per_sm(int rows) { return rows <= 16 ? 2 : 1; }
 
 cudaError_t hswa_launch_packed_decode(const PackedAttnParams& p, int rows, cudaStream_t s) {
   if (p.m.D == 128) return rows == 8 ? launch<128, 1>(p, s) : rows == 16 ? launch<128, 2>(p, s) : launch<128, 4>(p, s);
