@@ -2,7 +2,7 @@
 //
 // The 64-key tiles of all (request, KV head) streams form one sequence, cut into equal runs, one for each of the blocks that the
 // SMs hold: no block ends early, whatever the lengths, and loads run on from stream to stream.  One warp fetches the pages'
-// slabs (a bulk copy each: rows and scales lie together) into a ring of stages; every other warp takes whole tiles, with a softmax
+// slabs (a bulk copy each: rows and scales lie together) into a ring of slots; every other warp takes whole tiles, with a softmax
 // state of its own, and the block merges them where a stream ends.  A stream that a block has as a whole is written out there,
 // pieces of the others are joined by a second launch.
 // Bound by HBM (0.5625 bytes per element) and, close behind, by the instructions that turn codes into fp16; so both products
@@ -18,14 +18,15 @@
 namespace {
 using namespace hswa_dev;
 
-constexpr int TK = 64;  // keys per stage
+constexpr int TK = 64;  // keys per tile
 constexpr int NW = 7;   // warps that compute: with the producer two per scheduler, so that a block's threads get 128 or 255 registers
-// stages; with the sums of three warps, 2 blocks of up to 16 rows or one of 32 fill an SM
-constexpr int stages_of(int nt) { return nt == 1 ? 10 : nt == 2 ? 9 : 18; }
+// slots of the ring, each K or V of a tile (K is done with half a tile earlier); with the sums of three warps, 2 blocks of up to
+// 16 rows or one of 32 fill an SM
+constexpr int slots_of(int nt) { return nt == 1 ? 21 : nt == 2 ? 18 : 36; }
 constexpr int kThreads = (NW + 1) * 32;
 
 template <int D>
-constexpr int kStageBytes = 2 * TK * (D / 2 + D / 16);
+constexpr int kSlotBytes = TK * (D / 2 + D / 16);
 
 // Keys of a 16-key group in the order of the fragments' rows: row i of the first half holds key kKey(i), row 8 + i key 8 +
 // kKey(i).  (A lane's V rows are kKey(2t), kKey(2t + 1): this order has lanes t = 0 .. 3 on rows 0, 3, 4, 7 and 1, 2, 5, 6,
@@ -51,14 +52,14 @@ __device__ __forceinline__ int64_t run_start(int64_t total, int c, int runs) { r
 
 template <int D, int NT>
 __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kernel(const PackedAttnParams p) {
-  constexpr int NS = stages_of(NT);
-  constexpr int ROW = D / 2, SC = D / 16, KS = D / 16, STAGE = kStageBytes<D>, HALF = STAGE / 2;
+  constexpr int NS = slots_of(NT);
+  constexpr int ROW = D / 2, SC = D / 16, KS = D / 16, SLOT = kSlotBytes<D>;
   constexpr int COLS = 8 * NT;
   constexpr int MT = D / 16;                // 16-row tiles of O^T
   constexpr int STEP = D == 64 && NT < 4 ? TK : TK / NT;  // keys per softmax step (registers)
   constexpr int GROUPS = STEP / 16;
   extern __shared__ __align__(128) uint8_t smem[];
-  float4* box = reinterpret_cast<float4*>(smem + NS * STAGE);              // [3][MT][NT][32] sums on their way
+  float4* box = reinterpret_cast<float4*>(smem + NS * SLOT);               // [3][MT][NT][32] sums on their way
   uint2* s_q = reinterpret_cast<uint2*>(box + 3 * MT * NT * 32);           // [NT][KS][32] fragments of Q
   float* s_down = reinterpret_cast<float*>(s_q + NT * KS * 32);            // [COLS]
   float2* s_ml = reinterpret_cast<float2*>(s_down + COLS);                 // [NW][COLS]
@@ -138,12 +139,13 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
   const int slab = M.P * (ROW + SC);
   if (warp == NW) {
     // ======================= producer =======================
-    const int ppt = TK / M.P;  // pages per stage: 1, 2 or 4
-    const int i = lane % ppt, kv = lane / ppt;
+    const int ppt = TK / M.P;  // pages per tile: 1, 2 or 4
     bool ok = true;
     int64_t w = w0;
     int r = r0, kh = kh0, tile = tile0;
-    int at = 0;  // stages filled
+    // K and V of two tiles at a time, a lane per page: waiting for a slot costs a few hundred cycles, and these waits overlap
+    const int i = lane % ppt, kv = lane / ppt & 1, ahead = lane / (2 * ppt);
+    int at = 0;  // tiles before this piece
     while (w < w1 && ok) {
       const Stream s = stream_of(p, r);
       const int count = (int)min((int64_t)(s.tiles - tile), w1 - w);
@@ -151,30 +153,32 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
       const int n_pages = (s.end + M.P - 1) / M.P;  // (0: a request without keys)
       const int page0 = tile * ppt;
       int ids_next = page0 + lane < n_pages ? tbl[page0 + lane] : 0, ids = 0;
-      for (int j = 0; j < count; ++j, ++at) {
-        const int stage = at % NS, first = j * ppt;
-        if ((first & 31) == 0) {
+      for (int j = 0; j < count; j += 2) {
+        if ((j * ppt & 31) == 0) {
           ids = ids_next;
-          ids_next = page0 + first + 32 + lane < n_pages ? tbl[page0 + first + 32 + lane] : 0;
+          ids_next = page0 + j * ppt + 32 + lane < n_pages ? tbl[page0 + j * ppt + 32 + lane] : 0;
         }
-        const int here = min(ppt, n_pages - page0 - first);  // pages of this tile
+        const int first = (j + ahead) * ppt, here = min(ppt, n_pages - page0 - first);  // pages of the lane's tile
         int page = __shfl_sync(0xffffffffu, ids, (first + i) & 31);
-        if (at >= NS) ok = __all_sync(0xffffffffu, mbar_wait(empty0 + 8 * stage, ((at / NS) - 1) & 1));
+        const bool mine = ahead < 2 && j + ahead < count;
+        const int order = 2 * (at + j + ahead) + kv, slot = order % NS, round = order / NS;
+        if (mine && round > 0) ok = mbar_wait(empty0 + 8 * slot, (round - 1) & 1);
+        ok = __all_sync(0xffffffffu, ok);
         if (!ok) {
           if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, j, 50);
           break;
         }
-        if (lane == 0) mbar_arrive_expect_tx(full0 + 8 * stage, 2 * max(here, 0) * slab);
+        if (mine && i == 0) mbar_arrive_expect_tx(full0 + 8 * slot, max(here, 0) * slab);
         __syncwarp();
-        if (kv < 2 && i < here) {
+        if (mine && i < here) {
           if (page < 0 || page >= p.num_pages) {
             record_error(p.err, HSWA_ERR_BOUNDS, r, page0 + first + i, page);
             page = 0;
           }
-          bulk_load(smem_u32(smem + stage * STAGE + kv * HALF + i * slab), p.pool + (((int64_t)page * 2 + kv) * M.Hkv + kh) * slab, slab,
-                    full0 + 8 * stage);
+          bulk_load(smem_u32(smem + slot * SLOT + i * slab), p.pool + (((int64_t)page * 2 + kv) * M.Hkv + kh) * slab, slab, full0 + 8 * slot);
         }
       }
+      at += count;
       w += count;
       tile = 0;
       if (++kh == M.Hkv) {
@@ -188,14 +192,14 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
 
   // ======================= consumers =======================
   const int kg = key_of(g), ka = key_of(2 * t), kb = key_of(2 * t + 1);
-  // where the rows and scales of a 16-key group of a stage lie (a group is inside one page)
+  // where the rows and scales of a 16-key group of a slot lie (a group is inside one page)
   const int page_shift = 31 - __clz(M.P), scales_at = M.P * ROW;
   auto rows_of = [&](int key0) { return (key0 >> page_shift) * slab + (key0 & (M.P - 1)) * ROW; };
   auto scales_of = [&](int key0) { return (key0 >> page_shift) * slab + scales_at + (key0 & (M.P - 1)) * SC; };
   auto consumers_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(NW * 32) : "memory"); };
   int64_t w = w0;
   int r = r0, kh = kh0, tile = tile0;
-  int at0 = 0;  // stages before this piece
+  int at0 = 0;  // tiles before this piece
   bool ok = true;
   while (w < w1) {
   const Stream sm = stream_of(p, r);
@@ -266,25 +270,25 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
     }
   // the warp's tiles: every NW-th of the piece
   for (int j = warp; j < count; j += NW) {
-    const int stage = (at0 + j) % NS;
-    ok = __all_sync(0xffffffffu, mbar_wait(full0 + 8 * stage, ((at0 + j) / NS) & 1));
+    const int k_at = 2 * (at0 + j), k_slot = k_at % NS, v_slot = (k_at + 1) % NS;
+    ok = __all_sync(0xffffffffu, mbar_wait(full0 + 8 * k_slot, (k_at / NS) & 1) && mbar_wait(full0 + 8 * v_slot, ((k_at + 1) / NS) & 1));
     if (!ok) {
       if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, j, 51);
       *reinterpret_cast<volatile int64_t*>(s_plan) = 1;
       __nanosleep(100000);  // (copies in flight, as above)
       break;
     }
-    const uint8_t* st = smem + stage * STAGE;
+    const uint8_t *k_st = smem + k_slot * SLOT, *v_st = smem + v_slot * SLOT;
     const int pos0 = (tile + j) * TK;
     const bool masked = pos0 + TK > first_end;
 #pragma unroll 1
     for (int step = 0; step < TK / STEP; ++step) {
-      if (masked && pos0 + step * STEP >= end) break;  // no keys behind here
+      if (step > 0 && masked && pos0 + step * STEP >= end) break;  // no keys behind here
       float S[GROUPS][NT][4];
 #pragma unroll
       for (int q = 0; q < GROUPS; ++q) {
-        const uint8_t* rows_at = st + rows_of(step * STEP + q * 16);
-        const uint8_t* sc_at = st + scales_of(step * STEP + q * 16);
+        const uint8_t* rows_at = k_st + rows_of(step * STEP + q * 16);
+        const uint8_t* sc_at = k_st + scales_of(step * STEP + q * 16);
         uint32_t wa[D / 32], wb[D / 32];
         uint32_t fa, fb;
         if constexpr (D == 128) {
@@ -320,6 +324,10 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
             }
           }
         }
+      }
+      if (step + 1 == TK / STEP || (masked && pos0 + (step + 1) * STEP >= end)) {  // K has been read
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty0 + 8 * k_slot);
       }
       // masks, the running maximum of each row (column of S^T) in log2 units
       if (masked) {
@@ -377,8 +385,8 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
       }
 #pragma unroll
       for (int q = 0; q < GROUPS; ++q) {
-        const uint8_t* rows_at = st + HALF + rows_of(step * STEP + q * 16);
-        const uint8_t* sc_at = st + HALF + scales_of(step * STEP + q * 16);
+        const uint8_t* rows_at = v_st + rows_of(step * STEP + q * 16);
+        const uint8_t* sc_at = v_st + scales_of(step * STEP + q * 16);
         const int blk = D == 128 ? g : g >> 1;
         uint32_t f0 = sc_at[ka * SC + blk] | (uint32_t)sc_at[kb * SC + blk] << 8;
         uint32_t f1 = sc_at[(ka + 8) * SC + blk] | (uint32_t)sc_at[(kb + 8) * SC + blk] << 8;
@@ -414,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
       }
     }
     __syncwarp();
-    if (lane == 0) mbar_arrive(empty0 + 8 * stage);
+    if (lane == 0) mbar_arrive(empty0 + 8 * v_slot);
   }
 
   // ---- the piece's end: merge of the warps' states ----
@@ -591,8 +599,8 @@ __global__ void __launch_bounds__(128) packed_join_kernel(const PackedAttnParams
 
 template <int D, int NT>
 cudaError_t launch(const PackedAttnParams& p, cudaStream_t s) {
-  constexpr int NS = stages_of(NT);
-  constexpr int SMEM = NS * kStageBytes<D> + 3 * D * NT * 32 + NT * D * 16 + 32 * NT + NW * 64 * NT + 16 * NS + 8 * (3 + kThreads / 32);
+  constexpr int NS = slots_of(NT);
+  constexpr int SMEM = NS * kSlotBytes<D> + 3 * D * NT * 32 + NT * D * 16 + 32 * NT + NW * 64 * NT + 16 * NS + 8 * (3 + kThreads / 32);
   auto kern = packed_decode_kernel<D, NT>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
   if (e != cudaSuccess) return e;
