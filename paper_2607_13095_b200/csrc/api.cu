@@ -219,7 +219,9 @@ bool plan_packed(const hswa_handle* h, int batch, int total_q, int max_q_len, in
     c.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
     if (keys > kUnsplitLen) {
       // as many runs as blocks fit the SMs, of eight tiles at least (a block's seven warps take one each)
-      const int64_t fit = (int64_t)hswa_packed_decode_blocks_per_sm(c.rows) * h->num_sms, tiles = streams * ((keys + 63) / 64), most = (tiles + 7) / 8;
+      const int64_t tiles = streams * ((keys + 63) / 64);
+      const int64_t fit = (int64_t)(c.rows == 8 ? hswa_packed_stream_runs_per_sm() : hswa_packed_decode_blocks_per_sm(c.rows)) * h->num_sms;
+      const int64_t most = c.rows == 8 ? (tiles + 3) / 4 : (tiles + 7) / 8;
       c.runs = (int)(fit < most ? fit : most);
       c.o_bytes = align((size_t)2 * c.runs * c.rows * h->cfg.head_dim * sizeof(float));
       c.ml_bytes = align((size_t)2 * c.runs * c.rows * sizeof(float2));
@@ -1012,6 +1014,7 @@ hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, con
   }
   p.err = h->err;
   cudaStream_t s = (cudaStream_t)stream;
+  if (pl.rows == 8 && pl.runs > 0) return hswa_launch_packed_stream(p, s) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
   if (pl.rows > 0) return hswa_launch_packed_decode(p, pl.rows, s) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
   if (hswa_launch_packed_tile(p, s) != cudaSuccess) return HSWA_ERR_CUDA;
   if (pl.slices > 1) {

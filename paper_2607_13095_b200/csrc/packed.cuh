@@ -48,7 +48,12 @@ struct PackedAttnParams {
 
 cudaError_t hswa_launch_packed_append(const PackedCacheParams& p, int num_sms, cudaStream_t s);
 cudaError_t hswa_launch_packed_read(const PackedCacheParams& p, int num_sms, cudaStream_t s);
-// Few rows (tokens x heads of a KV head): 8, 16 or 32 per block
+// Up to eight rows (tokens x heads of a KV head), long contexts: a run per warp
+int hswa_packed_stream_runs_per_sm();
+cudaError_t hswa_launch_packed_stream(const PackedAttnParams& p, cudaStream_t s);
+// The join of runs' pieces of `cols` rows each
+cudaError_t hswa_launch_packed_join(const PackedAttnParams& p, int cols, cudaStream_t s);
+// Few rows: 8, 16 or 32 per block
 int hswa_packed_decode_blocks_per_sm(int rows);
 cudaError_t hswa_launch_packed_decode(const PackedAttnParams& p, int rows, cudaStream_t s);
 // Many rows: the tcgen05 tile kernel, two Q tiles of hswa_cross_tile_tokens tokens per block
@@ -92,7 +97,7 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 // D(16x8, fp32) += A(16x16, fp16, row) * B(16x8, fp16, col)
 __device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                               uint32_t b1) {
-  asm volatile(
+  asm(  // (not volatile: independent products may be interleaved)
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));

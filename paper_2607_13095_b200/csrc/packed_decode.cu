@@ -12,13 +12,13 @@
 //   O^T [D x rows] += V^T P^T: a lane needs neighbouring KEYS of one element side by side.  It reads 16 (D = 128) or 8
 //     neighbouring elements of two keys and exchanges nibbles: 4 logic instructions make 8 bytes of (key, key') pairs out of
 //     two words, and each converts at once.
-#include "packed.cuh"
+#include "packed_stream.cuh"
 #include "tc_primitives.cuh"
 
 namespace {
 using namespace hswa_dev;
 
-constexpr int TK = 64;  // keys per tile
+constexpr int TK = kStreamTile;
 constexpr int NW = 7;   // warps that compute: with the producer two per scheduler, so that a block's threads get 128 or 255 registers
 // slots of the ring, each K or V of a tile (K is done with half a tile earlier); with the sums of three warps, 2 blocks of up to
 // 16 rows or one of 32 fill an SM
@@ -27,28 +27,6 @@ constexpr int kThreads = (NW + 1) * 32;
 
 template <int D>
 constexpr int kSlotBytes = TK * (D / 2 + D / 16);
-
-// Keys of a 16-key group in the order of the fragments' rows: row i of the first half holds key kKey(i), row 8 + i key 8 +
-// kKey(i).  (A lane's V rows are kKey(2t), kKey(2t + 1): this order has lanes t = 0 .. 3 on rows 0, 3, 4, 7 and 1, 2, 5, 6,
-// two of each parity, which halves the bank conflicts of 64-byte rows; K rows come in pairs of unlike parity.)
-__device__ __forceinline__ int key_of(int i) { return (i & 4) | ((i & 2) ? 3 - (i & 1) : (i & 1)); }
-
-// Keys of request r that the rows of a step see, and its tiles (one at least, if it has rows: zeros are written there too).
-struct Stream {
-  int t0, n, len, end, tiles;
-};
-__device__ __forceinline__ Stream stream_of(const PackedAttnParams& p, int r) {
-  Stream s;
-  s.t0 = p.b.q_indptr ? p.b.q_indptr[r] : r;
-  s.n = p.b.q_indptr ? min(p.b.q_indptr[r + 1] - s.t0, p.max_q_len) : 1;
-  s.len = max(0, min(p.b.ctx_len[r], p.max_ctx_len));
-  const int64_t room = (int64_t)p.b.max_blocks * p.m.P;  // positions that the block table has places for
-  s.end = (int)min((int64_t)(p.causal ? s.len + s.n : s.len), room);
-  s.tiles = s.n > 0 ? max(1, (s.end + TK - 1) / TK) : 0;
-  return s;
-}
-// First tile of run c of `runs` over `total` tiles.
-__device__ __forceinline__ int64_t run_start(int64_t total, int c, int runs) { return total * c / runs; }
 
 template <int D, int NT>
 __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kernel(const PackedAttnParams p) {
@@ -78,14 +56,7 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
     }
     mbar_fence_init();
   }
-  if (blockIdx.x == 0)  // the grid was sized from the host's bounds
-    for (int r = threadIdx.x; r < B; r += kThreads) {
-      const int ctx = p.b.ctx_len[r], t0 = p.b.q_indptr ? p.b.q_indptr[r] : r, n = p.b.q_indptr ? p.b.q_indptr[r + 1] - t0 : 1;
-      const Stream s = stream_of(p, r);
-      if (ctx < 0 || ctx > p.max_ctx_len) record_error(p.err, HSWA_ERR_BOUNDS, r, -1, ctx);
-      if (n < 0 || n > p.max_q_len || t0 < 0 || (int64_t)t0 + n > p.total_q) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, n);
-      if (p.causal && s.n > 0 && s.end < s.len + s.n) record_error(p.err, HSWA_ERR_BOUNDS, r, -3, s.len + s.n);
-    }
+  if (blockIdx.x == 0) record_batch(p, kThreads);
   // the block's run of tiles [w0, w1), and the request that it starts in
   int64_t w0, w1;
   int r0, kh0 = 0, tile0 = 0;
@@ -98,23 +69,10 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
     __syncthreads();
     if (w1 == 0) return;
   } else {
-    const int per = (B + kThreads - 1) / kThreads, i0 = min((int)threadIdx.x * per, B), i1 = min(i0 + per, B);
-    int64_t mine = 0;
-    for (int i = i0; i < i1; ++i) mine += stream_of(p, i).tiles;
-    int64_t incl = mine;
-#pragma unroll
-    for (int sh = 1; sh < 32; sh <<= 1) {
-      const int64_t v = __shfl_up_sync(0xffffffffu, incl, sh);
-      if (lane >= sh) incl += v;
-    }
-    if (lane == 31) s_plan[3 + warp] = incl;
+    int i0, i1;
+    int64_t before;
     if (threadIdx.x == 0) s_plan[0] = 0;
-    __syncthreads();
-    int64_t total = 0, before = incl - mine;
-    for (int w = 0; w < kThreads / 32; ++w) {
-      if (w < warp) before += s_plan[3 + w];
-      total += s_plan[3 + w];
-    }
+    int64_t total = sum_tiles<kThreads>(p, s_plan + 3, &i0, &i1, &before);
     total *= M.Hkv;
     w0 = run_start(total, blockIdx.x, p.runs);
     w1 = run_start(total, blockIdx.x + 1, p.runs);
@@ -528,75 +486,6 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
   }
 }
 
-// Joins the pieces of the streams that several blocks had: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  A block per
-// stream and row, its four warps take every fourth piece.
-template <int D>
-__global__ void __launch_bounds__(128) packed_join_kernel(const PackedAttnParams p, const int cols) {
-  const ModelParams& M = p.m;
-  const int r = blockIdx.x / M.Hkv, kh = blockIdx.x % M.Hkv, col = blockIdx.y;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const Stream s = stream_of(p, r);
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // launched early behind the kernel that writes the pieces
-  if (s.tiles == 0 || col >= s.n * M.G) return;
-  const int64_t total = p.before[p.b.B] * M.Hkv, start = p.before[r] * M.Hkv + (int64_t)kh * s.tiles;
-  // run c holds tile x: c = ceil((x + 1) runs / total) - 1
-  const int c0 = (int)(((start + 1) * p.runs - 1) / total), c1 = (int)(((start + s.tiles) * p.runs - 1) / total);
-  const int tok = col / M.G;
-  if (c0 == c1 || (unsigned)s.t0 + (unsigned)tok >= (unsigned)p.total_q) return;
-  auto piece_of = [&](int c) { return (2 * (int64_t)c + (c == c0)) * cols + col; };
-  // a run without tiles (more runs than tiles) left no piece; nor has a piece without a key of the row anything (l = 0)
-  auto ml_of = [&](int c) {
-    return run_start(total, c, p.runs) < run_start(total, c + 1, p.runs) ? p.part_ml[piece_of(c)] : make_float2(-INFINITY, 0.f);
-  };
-  float mm = -INFINITY;
-  for (int c = c0 + lane; c <= c1; c += 32) {
-    const float2 v = ml_of(c);
-    if (v.y != 0.f) mm = fmaxf(mm, v.x);
-  }
-#pragma unroll
-  for (int sh = 16; sh >= 1; sh >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, sh));
-  constexpr int PER = D / 32;
-  float acc[PER] = {}, L = 0.f;
-#pragma unroll 4
-  for (int c = c0 + warp; c <= c1; c += 4) {
-    const float2 v = ml_of(c);
-    const float f = v.y != 0.f ? fast_exp2(v.x == -INFINITY ? 0.f : v.x - mm) : 0.f;  // (l of NaN scores: m says nothing)
-    const float* o = p.part_o + piece_of(c) * D + lane * PER;
-    L += v.y != 0.f ? f * v.y : 0.f;
-#pragma unroll
-    for (int i = 0; i < PER; i += 2) {
-      const float2 x = *reinterpret_cast<const float2*>(o + i);
-      acc[i] += v.y != 0.f ? f * x.x : 0.f;
-      acc[i + 1] += v.y != 0.f ? f * x.y : 0.f;
-    }
-  }
-  __shared__ float sums[3][32][PER + 1];
-  if (warp > 0) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) sums[warp - 1][lane][i] = acc[i];
-    sums[warp - 1][lane][PER] = L;
-  }
-  __syncthreads();
-  if (warp > 0) return;
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) acc[i] += sums[k][lane][i];
-    L += sums[k][lane][PER];
-  }
-  const float inv = L != 0.f ? 1.f / L : 0.f;
-  const int64_t orow = (int64_t)(s.t0 + tok) * M.Hq + kh * M.G + col % M.G;
-#pragma unroll
-  for (int i = 0; i < PER; i += 2) {
-    const int64_t at = orow * D + lane * PER + i;
-    if (M.out_fp32)
-      *reinterpret_cast<float2*>(reinterpret_cast<float*>(p.out) + at) = make_float2(acc[i] * inv, acc[i + 1] * inv);
-    else
-      *reinterpret_cast<__nv_bfloat162*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at) = __floats2bfloat162_rn(acc[i] * inv, acc[i + 1] * inv);
-  }
-  if (lane == 0 && p.lse) p.lse[orow] = L != 0.f ? (mm + log2f(L)) * 0.6931471805599453f : -INFINITY;
-}
-
 template <int D, int NT>
 cudaError_t launch(const PackedAttnParams& p, cudaStream_t s) {
   constexpr int NS = slots_of(NT);
@@ -606,16 +495,7 @@ cudaError_t launch(const PackedAttnParams& p, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   kern<<<p.runs > 0 ? p.runs : p.b.B * p.m.Hkv, kThreads, SMEM, s>>>(p);
   if ((e = cudaGetLastError()) != cudaSuccess || p.runs == 0) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.b.B * p.m.Hkv, p.max_q_len * p.m.G, 1);
-  cfg.blockDim = dim3(128, 1, 1);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, packed_join_kernel<D>, p, 8 * NT);
+  return hswa_launch_packed_join(p, 8 * NT, s);
 }
 
 }  // namespace
