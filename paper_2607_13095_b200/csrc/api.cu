@@ -1026,7 +1026,7 @@ hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, con
 
 size_t hswa_pages_workspace_need(const hswa_handle* h, int64_t num_pages) {
   if (!h || num_pages <= 0 || num_pages > kMaxPages) return 0;
-  return ((size_t)num_pages * sizeof(int32_t) + 255) & ~size_t(255);
+  return (((size_t)num_pages + 3 * kMaxPageRows + 1) * sizeof(int32_t) + 255) & ~size_t(255);
 }
 
 hswa_status hswa_pages_fork(hswa_handle* h, int64_t num_pages, const int32_t* ref, int32_t* ref_out, int32_t rows_in, const int32_t* held,
@@ -1064,8 +1064,12 @@ hswa_status hswa_pages_fork(hswa_handle* h, int64_t num_pages, const int32_t* re
   p.copy_src = copy_src;
   p.copy_dst = copy_dst;
   p.fresh = static_cast<int32_t*>(workspace);
+  p.first = p.fresh + num_pages;
+  p.most = p.first + kMaxPageRows;
+  p.rank = p.most + kMaxPageRows;
+  p.ok = p.rank + kMaxPageRows;
   p.err = h->err;
-  return hswa_launch_pages_fork(p, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+  return hswa_launch_pages_fork(p, h->num_sms, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
 }
 
 hswa_status hswa_pages_compact(hswa_handle* h, int64_t num_pages, const int32_t* ref, int32_t* ref_out, int32_t rows, const int32_t* held,
@@ -1092,7 +1096,7 @@ hswa_status hswa_pages_compact(hswa_handle* h, int64_t num_pages, const int32_t*
   p.move_src = move_src;
   p.move_dst = move_dst;
   p.err = h->err;
-  return hswa_launch_pages_compact(p, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+  return hswa_launch_pages_compact(p, h->num_sms, (cudaStream_t)stream) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
 }
 
 hswa_status hswa_pages_copy(hswa_handle* h, int32_t n_pools, void* const* pools, int64_t num_pages, int64_t page_bytes, int32_t pairs,

@@ -233,8 +233,6 @@ __global__ void __launch_bounds__(kThreads, 2) packed_stream_kernel(const Packed
           fb = e4m3_to_half2(sc_at[(kg + 8) * SC + t]);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) S[q][e] = 0.f;
-#pragma unroll
         for (int hf = 0; hf < D / 64; ++hf) {  // 16 elements of the lane's rows: one scale
           const uint32_t sa = hf ? high_twice(fa) : low_twice(fa), sb = hf ? high_twice(fb) : low_twice(fb);
 #pragma unroll
@@ -245,7 +243,8 @@ __global__ void __launch_bounds__(kThreads, 2) packed_stream_kernel(const Packed
             const uint32_t a1 = hmul2((s & 1) ? e2m1_to_half2<2>(ub) : e2m1_to_half2<0>(ub), sb);
             const uint32_t a2 = hmul2((s & 1) ? e2m1_to_half2<3>(ua) : e2m1_to_half2<1>(ua), sa);
             const uint32_t a3 = hmul2((s & 1) ? e2m1_to_half2<3>(ub) : e2m1_to_half2<1>(ub), sb);
-            mma_f16_16816(S[q], a0, a1, a2, a3, qf[s].x, qf[s].y);
+            if (s == 0) mma_f16_16816_zero(S[q], a0, a1, a2, a3, qf[s].x, qf[s].y);
+            else mma_f16_16816(S[q], a0, a1, a2, a3, qf[s].x, qf[s].y);
           }
         }
       }

@@ -1,10 +1,11 @@
 // Bookkeeping of a cache's pages on the device: hswa_pages_fork, hswa_pages_compact, hswa_pages_copy.
 //
 // Counts (how many holders a page has) are the only state: a page of count 0 is free, and the lowest-numbered free pages are
-// taken first, so results depend on the counts alone.  Fork and compact are one launch of one cluster of 16 blocks: counts of
-// pages, block tables and lists are a few MB at most, the work is a chain of dependent steps, and a cluster's barrier between
-// two steps costs a fraction of a launch.  Each block turns its share of the counts into a bitmap in shared memory on the only
-// pass over them; ranks of free and live pages come from the bitmap, and totals go around through distributed shared memory.
+// taken first, so results depend on the counts alone.  The steps that depend on one another (ranks of free and live pages, what each
+// row needs) are one launch of one cluster of 16 blocks, whose barrier between two steps costs a fraction of a launch: each block
+// turns its share of the counts into a bitmap in shared memory on the only pass over them, ranks come from the bitmap, and totals
+// go around through distributed shared memory.  Rewriting the tables is the cluster's work as well while they are small; large ones
+// are rewritten by a second launch of all SMs (a million entries: 66 us by 16 SMs).
 #include <cooperative_groups.h>
 
 #include <utility>
@@ -106,9 +107,107 @@ __device__ __forceinline__ void cluster_prefix(cg::cluster_group& cluster, cg::c
 // rank of a row's first fresh page; the counts of pages change behind it, by atomic adds whose order does not matter.
 // ---------------------------------------------------------------------------------------------------------------------
 struct RowPlan {
-  int parent, full, held, parent_held;  // shared pages, pages of the row, pages of its parent
-  bool first;                           // the parent's first child
+  int parent, full, held, parent_held, most;  // shared pages, pages of the row, pages of its parent, most pages that a child of it shares
+  bool first;                                 // the parent's first child
 };
+__device__ __forceinline__ int pages_of(int tokens, int page_size) { return (int)(((int64_t)tokens + page_size - 1) / page_size); }
+__device__ __forceinline__ RowPlan plan_of(const PagesForkParams& p, const int32_t* first, const int32_t* most, int r) {
+  RowPlan o;
+  o.parent = p.parent[r];
+  const int len = p.len[r];
+  o.full = len / p.page_size;
+  o.held = pages_of(max(len, p.need[r]), p.page_size);
+  o.parent_held = o.parent >= 0 ? p.held[o.parent] : 0;
+  o.first = o.parent >= 0 && first[o.parent] == r;
+  o.most = o.parent >= 0 ? most[o.parent] : 0;
+  return o;
+}
+// Does place k >= full of the row keep the parent's page?
+__device__ __forceinline__ bool passed(const PagesForkParams& p, const RowPlan& o, int k, int* page_out) {
+  if (!o.first || k >= o.parent_held || k < o.most) return false;
+  const int page = p.table[(int64_t)o.parent * p.max_blocks + k];
+  *page_out = page;
+  return page >= 0 && page < p.num_pages && p.ref[page] == 1;
+}
+
+// The new tables and counts, by warp `me` of `all`: first, most, rank as computed before, fresh pages listed, counts copied.
+__device__ __forceinline__ void apply_fork(const PagesForkParams& p, const int32_t* first, const int32_t* most, const int32_t* rank, int me, int all) {
+  const int lane = threadIdx.x & 31;
+  auto count = [&](int page, int by, int row, int k) {
+    if (page < 0 || page >= p.num_pages)
+      record_error(p.err, HSWA_ERR_BOUNDS, row, k, page);
+    else if (by != 0)
+      atomicAdd(&p.ref_out[page], by);
+  };
+  constexpr int CH = 256;  // places per item
+  const int chunks = (max(p.max_blocks, p.out_max_blocks) + CH - 1) / CH;
+  // new rows: shared places in chunks of 256, the places behind them by the warp of chunk 0
+  for (int64_t it = me; it < (int64_t)p.rows_out * chunks; it += all) {
+    const int r = (int)(it / chunks), c = (int)(it % chunks);
+    const RowPlan o = plan_of(p, first, most, r);
+    int32_t* out = p.table_out + (int64_t)r * p.out_max_blocks;
+    const int32_t* in = p.table + (int64_t)max(o.parent, 0) * p.max_blocks;
+    int page[CH / 32];
+#pragma unroll
+    for (int u = 0; u < CH / 32; ++u) {
+      const int k = c * CH + u * 32 + lane;
+      page[u] = k < o.full ? in[k] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < CH / 32; ++u) {
+      const int k = c * CH + u * 32 + lane;
+      if (k >= o.full) continue;
+      out[k] = page[u];
+      count(page[u], o.first ? 0 : 1, r, k);
+    }
+    if (c != 0) continue;
+    int next = rank[r];
+    const int len = p.len[r];
+    int src = -1, dst = -1;
+    for (int k0 = o.full; k0 < o.held; k0 += 32) {
+      const int k = k0 + lane;
+      int at = -1;
+      const bool keeps = k < o.held && passed(p, o, k, &at);
+      const bool fresh = k < o.held && !keeps;
+      const uint32_t who = __ballot_sync(0xffffffffu, fresh);
+      if (fresh) {
+        at = p.fresh[next + __popc(who & ((1u << lane) - 1))];
+        p.ref_out[at] = 1;
+      }
+      if (k < o.held) out[k] = at;
+      next += __popc(who);
+      if (k == o.full && fresh && len % p.page_size != 0) {
+        src = in[k];
+        dst = at;
+        if (src < 0 || src >= p.num_pages) {
+          record_error(p.err, HSWA_ERR_BOUNDS, r, k, src);
+          src = dst = -1;
+        }
+      }
+    }
+    if (lane == 0) {  // (place `full` is lane 0's)
+      p.copy_src[r] = src;
+      p.copy_dst[r] = dst;
+      p.held_out[r] = o.held;
+    }
+  }
+  // old rows: what their first child does not keep loses a holder
+  for (int64_t it = me; it < (int64_t)p.rows_in * chunks; it += all) {
+    const int i = (int)(it / chunks), c = (int)(it % chunks);
+    const int held = p.held[i], child = first[i];
+    RowPlan o = {};
+    if (child != INT32_MAX) o = plan_of(p, first, most, child);
+    if (child != INT32_MAX && min(held, (c + 1) * CH) <= o.full) continue;
+#pragma unroll
+    for (int u = 0; u < CH / 32; ++u) {
+      const int k = c * CH + u * 32 + lane;
+      if (k >= held || (child != INT32_MAX && k < o.full)) continue;
+      int page;
+      if (child != INT32_MAX && k < o.held && passed(p, o, k, &page)) continue;
+      count(p.table[(int64_t)i * p.max_blocks + k], -1, i, k);
+    }
+  }
+}
 
 __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkParams p) {
   cg::cluster_group cluster = cg::this_cluster();
@@ -119,33 +218,15 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
   int32_t* s_most = s_first + p.rows_in;   // [rows_in] most pages that a child shares
   int32_t* s_rank = s_most + p.rows_in;    // [rows_out] rank of the row's first fresh page
   uint32_t* s_live = reinterpret_cast<uint32_t*>(s_rank + p.rows_out);
-  const int block = (int)cluster.block_rank(), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int block = (int)cluster.block_rank(), warp = threadIdx.x >> 5;
   const Share sh = share_of(p.num_pages, block);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 0) s_bad = 0;
   for (int i = threadIdx.x; i < p.rows_in; i += kThreads) {
     s_first[i] = INT32_MAX;
     s_most[i] = 0;
   }
   __syncthreads();
-
-  auto pages_of = [&](int tokens) { return (int)(((int64_t)tokens + p.page_size - 1) / p.page_size); };
-  auto plan = [&](int r) {
-    RowPlan o;
-    o.parent = p.parent[r];
-    const int len = p.len[r];
-    o.full = len / p.page_size;
-    o.held = pages_of(max(len, p.need[r]));
-    o.parent_held = o.parent >= 0 ? p.held[o.parent] : 0;
-    o.first = o.parent >= 0 && s_first[o.parent] == r;
-    return o;
-  };
-  // does place k of the row keep the parent's page?  (k >= full)
-  auto passed = [&](const RowPlan& o, int k, int* page_out) {
-    if (!o.first || k >= o.parent_held || k < s_most[o.parent]) return false;
-    const int page = p.table[(int64_t)o.parent * p.max_blocks + k];
-    *page_out = page;
-    return page >= 0 && page < p.num_pages && p.ref[page] == 1;
-  };
 
   // every block looks at all rows: none waits for another
   for (int i = threadIdx.x; i < p.rows_in; i += kThreads) {
@@ -157,8 +238,8 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
   }
   for (int r = threadIdx.x; r < p.rows_out; r += kThreads) {
     const int parent = p.parent[r], len = p.len[r], need = p.need[r];
-    bool ok = parent >= -1 && parent < p.rows_in && len >= 0 && pages_of(max(len, need)) <= p.out_max_blocks;
-    if (ok) ok = parent < 0 ? len == 0 : pages_of(len) <= p.held[parent];
+    bool ok = parent >= -1 && parent < p.rows_in && len >= 0 && pages_of(max(len, need), p.page_size) <= p.out_max_blocks;
+    if (ok) ok = parent < 0 ? len == 0 : pages_of(len, p.page_size) <= p.held[parent];
     if (!ok) {
       s_bad = 1;
       if (block == 0) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, parent);
@@ -175,9 +256,9 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
     const int r0 = threadIdx.x * per, r1 = min(r0 + per, p.rows_out);
     int sum = 0;
     for (int r = r0; r < r1; ++r) {
-      const RowPlan o = plan(r);
+      const RowPlan o = plan_of(p, s_first, s_most, r);
       int fresh = o.held - o.full, page;
-      for (int k = max(o.full, o.first ? s_most[o.parent] : 0); k < min(o.held, o.first ? o.parent_held : 0); ++k) fresh -= passed(o, k, &page);
+      for (int k = o.most; o.first && k < min(o.held, o.parent_held); ++k) fresh -= passed(p, o, k, &page);
       s_rank[r] = sum;
       sum += fresh;
     }
@@ -204,93 +285,82 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
       for (; bits && rank < fresh_total; bits &= bits - 1) p.fresh[rank++] = (sh.first + w) * 32 + __ffs(bits) - 1;
     }
   }
+  if (p.second) {  // a second launch does the rest
+    if (block == 0) {
+      for (int i = threadIdx.x; i < p.rows_in; i += kThreads) {
+        p.first[i] = s_first[i];
+        p.most[i] = s_most[i];
+      }
+      for (int r = threadIdx.x; r < p.rows_out; r += kThreads) p.rank[r] = s_rank[r];
+      if (threadIdx.x == 0) *p.ok = rows_ok && enough;
+    }
+    cluster.sync();  // (nobody reads another block's shared memory any more)
+    return;
+  }
   cluster.sync();  // counts copied, fresh pages listed, and nobody reads another block's shared memory any more
-  if (!rows_ok || !enough) return;
+  if (rows_ok && enough) apply_fork(p, s_first, s_most, s_rank, block + kBlocks * warp, kBlocks * kWarps);
+}
 
-  auto count = [&](int page, int by, int row, int k) {
-    if (page < 0 || page >= p.num_pages)
-      record_error(p.err, HSWA_ERR_BOUNDS, row, k, page);
-    else if (by != 0)
-      atomicAdd(&p.ref_out[page], by);
-  };
-  const int all_warps = kBlocks * kWarps, my_warp = block + kBlocks * warp;
-  constexpr int CH = 256;  // shared places per item
-  const int chunks = (max(p.max_blocks, p.out_max_blocks) + CH - 1) / CH;
-  // new rows: shared places in chunks of 256, the places behind them by the warp of chunk 0
-  for (int64_t it = my_warp; it < (int64_t)p.rows_out * chunks; it += all_warps) {
-    const int r = (int)(it / chunks), c = (int)(it % chunks);
-    const RowPlan o = plan(r);
-    int32_t* out = p.table_out + (int64_t)r * p.out_max_blocks;
-    const int32_t* in = p.table + (int64_t)max(o.parent, 0) * p.max_blocks;
-#pragma unroll
-    for (int u = 0; u < CH / 32; ++u) {
-      const int k = c * CH + u * 32 + lane;
-      if (k < o.full) {
-        const int page = in[k];
-        out[k] = page;
-        count(page, o.first ? 0 : 1, r, k);
-      }
-    }
-    if (c != 0) continue;
-    int next = s_rank[r];
-    const int len = p.len[r];
-    int src = -1, dst = -1;
-    for (int k0 = o.full; k0 < o.held; k0 += 32) {
-      const int k = k0 + lane;
-      int page = -1;
-      const bool keeps = k < o.held && passed(o, k, &page);
-      const bool fresh = k < o.held && !keeps;
-      const uint32_t who = __ballot_sync(0xffffffffu, fresh);
-      if (fresh) {
-        page = p.fresh[next + __popc(who & ((1u << lane) - 1))];
-        p.ref_out[page] = 1;
-      }
-      if (k < o.held) out[k] = page;
-      next += __popc(who);
-      if (k == o.full && fresh && len % p.page_size != 0) {
-        src = in[k];
-        dst = page;
-        if (src < 0 || src >= p.num_pages) {
-          record_error(p.err, HSWA_ERR_BOUNDS, r, k, src);
-          src = dst = -1;
-        }
-      }
-    }
-    if (lane == 0) {  // (place `full` is lane 0's)
-      p.copy_src[r] = src;
-      p.copy_dst[r] = dst;
-      p.held_out[r] = o.held;
-    }
-  }
-  // old rows: what their first child does not keep loses a holder
-  for (int64_t it = my_warp; it < (int64_t)p.rows_in * chunks; it += all_warps) {
-    const int i = (int)(it / chunks), c = (int)(it % chunks);
-    const int held = p.held[i], child = s_first[i];
-    RowPlan o = {};
-    if (child != INT32_MAX) o = plan(child);
-#pragma unroll
-    for (int u = 0; u < CH / 32; ++u) {
-      const int k = c * CH + u * 32 + lane;
-      if (k >= held || (child != INT32_MAX && k < o.full)) continue;
-      int page;
-      if (child != INT32_MAX && k < o.held && passed(o, k, &page)) continue;
-      count(p.table[(int64_t)i * p.max_blocks + k], -1, i, k);
-    }
-  }
+constexpr int kWideThreads = 256;
+__global__ void __launch_bounds__(kWideThreads) pages_fork_apply_kernel(const PagesForkParams p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // launched early behind pages_fork_kernel
+  if (*p.ok == 0) return;
+  const int warps = kWideThreads / 32;
+  apply_fork(p, p.first, p.most, p.rank, blockIdx.x + gridDim.x * (threadIdx.x >> 5), gridDim.x * warps);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
 // Compact.  With L live pages, the i-th lowest free page below L takes the i-th highest live page (those lie at or past L).
 // A page's rank follows from the number of live pages before it.
 // ---------------------------------------------------------------------------------------------------------------------
+// The tables under the new numbers, by warp `me` of `all`.
+__device__ __forceinline__ void apply_compact(const PagesCompactParams& p, int me, int all) {
+  const int lane = threadIdx.x & 31;
+  constexpr int CH = 256;
+  const int chunks = (p.max_blocks + CH - 1) / CH;
+  for (int64_t it = me; it < (int64_t)p.rows * chunks; it += all) {
+    const int r = (int)(it / chunks), c = (int)(it % chunks);
+    const int held = p.held[r];
+    if (held < 0 || held > p.max_blocks) {
+      if (c == 0 && lane == 0) record_error(p.err, HSWA_ERR_BOUNDS, r, -1, held);
+      continue;
+    }
+    if (c * CH >= held) continue;
+    int page[CH / 32];
+#pragma unroll
+    for (int u = 0; u < CH / 32; ++u) {
+      const int k = c * CH + u * 32 + lane;
+      page[u] = k < held ? p.table[(int64_t)r * p.max_blocks + k] : 0;
+    }
+    int to[CH / 32];
+#pragma unroll
+    for (int u = 0; u < CH / 32; ++u) {
+      const int k = c * CH + u * 32 + lane;
+      const bool ok = page[u] >= 0 && page[u] < p.num_pages;
+      if (k < held && !ok) record_error(p.err, HSWA_ERR_BOUNDS, r, k, page[u]);
+      to[u] = ok ? p.page_map[page[u]] : page[u];
+    }
+#pragma unroll
+    for (int u = 0; u < CH / 32; ++u) {
+      const int k = c * CH + u * 32 + lane;
+      if (k < held) p.table_out[(int64_t)r * p.max_blocks + k] = to[u];
+    }
+  }
+}
+__global__ void __launch_bounds__(kWideThreads) pages_compact_apply_kernel(const PagesCompactParams p) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // launched early behind pages_compact_kernel
+  apply_compact(p, blockIdx.x + gridDim.x * (threadIdx.x >> 5), gridDim.x * (kWideThreads / 32));
+}
+
 __global__ void __launch_bounds__(kThreads) pages_compact_kernel(const PagesCompactParams p) {
   cg::cluster_group cluster = cg::this_cluster();
   auto started = cluster.barrier_arrive();
   extern __shared__ int32_t s_mem[];
   __shared__ int s_warp[kWarps], s_counts[kBlocks];
   uint32_t* s_live = reinterpret_cast<uint32_t*>(s_mem);
-  const int block = (int)cluster.block_rank(), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int block = (int)cluster.block_rank(), warp = threadIdx.x >> 5;
   const Share sh = share_of(p.num_pages, block);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   for (int i = block * kThreads + threadIdx.x; i < p.max_moves; i += kBlocks * kThreads) p.move_src[i] = p.move_dst[i] = -1;
   scan_counts(p.ref, p.ref_out, p.page_map, p.num_pages, sh, s_live);
   __syncthreads();
@@ -329,32 +399,9 @@ __global__ void __launch_bounds__(kThreads) pages_compact_kernel(const PagesComp
     p.ref_out[dst] = p.ref[src];
     p.ref_out[src] = 0;
   }
+  if (p.second) return;  // a second launch rewrites the tables
   cluster.sync();
-  const int all_warps = kBlocks * kWarps, my_warp = block + kBlocks * warp;
-  constexpr int CH = 256;
-  const int chunks = (p.max_blocks + CH - 1) / CH;
-  for (int64_t it = my_warp; it < (int64_t)p.rows * chunks; it += all_warps) {
-    const int r = (int)(it / chunks), c = (int)(it % chunks);
-    const int held = p.held[r];
-    if (held < 0 || held > p.max_blocks) {
-      if (c == 0 && lane == 0) record_error(p.err, HSWA_ERR_BOUNDS, r, -1, held);
-      continue;
-    }
-    int page[CH / 32];
-#pragma unroll
-    for (int u = 0; u < CH / 32; ++u) {
-      const int k = c * CH + u * 32 + lane;
-      page[u] = k < held ? p.table[(int64_t)r * p.max_blocks + k] : 0;
-    }
-#pragma unroll
-    for (int u = 0; u < CH / 32; ++u) {
-      const int k = c * CH + u * 32 + lane;
-      if (k >= held) continue;
-      const bool ok = page[u] >= 0 && page[u] < p.num_pages;
-      if (!ok) record_error(p.err, HSWA_ERR_BOUNDS, r, k, page[u]);
-      p.table_out[(int64_t)r * p.max_blocks + k] = ok ? p.page_map[page[u]] : page[u];
-    }
-  }
+  apply_compact(p, block + kBlocks * warp, kBlocks * kWarps);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -404,15 +451,39 @@ cudaError_t launch_cluster(Kernel kern, const Params& p, size_t smem, cudaStream
   return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
+// The second launch of all SMs, early behind the cluster.
+template <typename Kernel, typename Params>
+cudaError_t launch_wide(Kernel kern, const Params& p, int num_sms, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(4 * num_sms, 1, 1);
+  cfg.blockDim = dim3(kWideThreads, 1, 1);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, p);
+}
+
+// Table entries up to which the cluster rewrites them itself.
+constexpr int64_t kSmallTables = 32768;
+
 size_t bitmap_bytes(int num_pages) { return (size_t)(((num_pages + 31) / 32 + kBlocks - 1) / kBlocks) * 8; }
 
 }  // namespace
 
-cudaError_t hswa_launch_pages_fork(const PagesForkParams& p, cudaStream_t s) {
-  return launch_cluster(pages_fork_kernel, p, ((size_t)p.rows_in * 2 + p.rows_out) * 4 + 8 + bitmap_bytes(p.num_pages), s);
+cudaError_t hswa_launch_pages_fork(const PagesForkParams& params, int num_sms, cudaStream_t s) {
+  PagesForkParams p = params;
+  p.second = (int64_t)p.rows_in * p.max_blocks + (int64_t)p.rows_out * p.out_max_blocks > kSmallTables;
+  const cudaError_t e = launch_cluster(pages_fork_kernel, p, ((size_t)p.rows_in * 2 + p.rows_out) * 4 + 8 + bitmap_bytes(p.num_pages), s);
+  return e != cudaSuccess || !p.second ? e : launch_wide(pages_fork_apply_kernel, p, num_sms, s);
 }
-cudaError_t hswa_launch_pages_compact(const PagesCompactParams& p, cudaStream_t s) {
-  return launch_cluster(pages_compact_kernel, p, bitmap_bytes(p.num_pages), s);
+cudaError_t hswa_launch_pages_compact(const PagesCompactParams& params, int num_sms, cudaStream_t s) {
+  PagesCompactParams p = params;
+  p.second = (int64_t)p.rows * p.max_blocks > kSmallTables;
+  const cudaError_t e = launch_cluster(pages_compact_kernel, p, bitmap_bytes(p.num_pages), s);
+  return e != cudaSuccess || !p.second ? e : launch_wide(pages_compact_apply_kernel, p, num_sms, s);
 }
 cudaError_t hswa_launch_pages_copy(const PagesCopyParams& p, cudaStream_t s) {
   const int chunks = (int)((p.page_bytes + kCopyBytes - 1) / kCopyBytes);

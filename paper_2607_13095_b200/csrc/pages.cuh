@@ -24,7 +24,10 @@ struct PagesForkParams {
   int32_t* held_out;  // [rows_out]
   int32_t* copy_src;
   int32_t* copy_dst;
-  int32_t* fresh;  // scratch: [num_pages]
+  // scratch: the fresh pages [num_pages]; for a second launch [kMaxPageRows] each: first child and most pages a child shares of
+  // each old row, rank of each new row's first fresh page; whether there is anything to do
+  int32_t *fresh, *first, *most, *rank, *ok;
+  int32_t second;
   int32_t* err;
 };
 
@@ -41,6 +44,7 @@ struct PagesCompactParams {
   int32_t max_moves;
   int32_t* move_src;
   int32_t* move_dst;
+  int32_t second;  // the tables are rewritten by a second launch
   int32_t* err;
 };
 
@@ -55,6 +59,6 @@ struct PagesCopyParams {
   int32_t* err;
 };
 
-cudaError_t hswa_launch_pages_fork(const PagesForkParams& p, cudaStream_t s);
-cudaError_t hswa_launch_pages_compact(const PagesCompactParams& p, cudaStream_t s);
+cudaError_t hswa_launch_pages_fork(const PagesForkParams& p, int num_sms, cudaStream_t s);
+cudaError_t hswa_launch_pages_compact(const PagesCompactParams& p, int num_sms, cudaStream_t s);
 cudaError_t hswa_launch_pages_copy(const PagesCopyParams& p, cudaStream_t s);

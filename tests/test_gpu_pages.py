@@ -358,3 +358,26 @@ def test_calls_captured_into_a_graph_replay_on_new_counts():
         no_error(h)
         for g, w in zip((ref_out, *outs), ref.fork(counts, wide, held, pa, le, ne, P, 16, FILL)):
             assert np.array_equal(g.cpu().numpy(), w)
+
+
+def test_tables_of_many_entries():
+    """Rows times places past what the first launch rewrites itself: forked, then compacted, against the statement."""
+    rng = np.random.default_rng(11)
+    P, h, pages = 16, make_handle(dims(1, 64, 16, 1)), 50021
+    counts, table, held, lens = state(rng, P, 60, 14000, pages)
+    parent, length, need = children(rng, P, 70, held, lens, 50)
+    blocks = 880
+    assert table.size + 70 * blocks > 32768 * 2
+    ref_out, table_out, held_out, _, _ = check_fork(h, P, counts, table, held, parent, length, need, blocks)
+    dev = [dev_i32(x) for x in (ref_out, table_out, held_out)]
+    moves = 20000
+    outs = [torch.full(s, FILL, dtype=torch.int32, device="cuda") for s in ((pages,), (70, blocks), (pages,), (moves,), (moves,))]
+    hb.hswa_pages_compact(h, dev[0], outs[0], dev[1], dev[2], outs[1], outs[2], outs[3], outs[4])
+    no_error(h)
+    for g, w in zip(outs, ref.compact(ref_out, table_out, held_out, moves, FILL)):
+        assert np.array_equal(g.cpu().numpy(), w)
+    # without enough pages the second launch does nothing either
+    counts[counts == 0] = 1
+    got = fork(h, counts, table, held, parent, length, need, blocks)
+    assert hb.hswa_get_async_error(h)[:2] == (hb.HSWA_ERR_BOUNDS, -1)
+    assert np.array_equal(got[0], counts) and all((g == FILL).all() for g in got[1:])
