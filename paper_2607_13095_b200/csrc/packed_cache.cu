@@ -61,48 +61,57 @@ __device__ __forceinline__ RowAt find_row(const PackedCacheParams& p, int tok, i
   return at;
 }
 
+// Block number `it` of all tokens' rows: the 16 elements it % (D / 16) of KV head and token.
+struct Item {
+  int tok, kh, blk;
+};
+__device__ __forceinline__ Item item_of(const ModelParams& M, uint32_t it) {
+  const uint32_t shift = M.D == 128 ? 3 : 2, row = it >> shift, tok = row / (uint32_t)M.Hkv;
+  return {(int)tok, (int)(row - tok * M.Hkv), (int)(it & ((1u << shift) - 1))};
+}
+
 __global__ void __launch_bounds__(kThreads) packed_append_kernel(const PackedCacheParams p) {
   const ModelParams& M = p.m;
   const int bpr = M.D / 16;  // blocks per row: 4 or 8
-  const int shift = bpr == 8 ? 3 : 2;
-  const int64_t items = (int64_t)p.total_q * M.Hkv * bpr;
+  const uint32_t items = (uint32_t)p.total_q * M.Hkv * bpr;
   const __nv_bfloat16* in = blockIdx.y ? p.v_in : p.k_in;
   const float g = blockIdx.y ? p.v_scale : p.k_scale;
-  for (int64_t it = (int64_t)blockIdx.x * kThreads + threadIdx.x; it < items; it += (int64_t)gridDim.x * kThreads) {
-    const int64_t row = it >> shift;
-    const int blk = (int)(it & (bpr - 1)), tok = (int)(row / M.Hkv), kh = (int)(row - (int64_t)tok * M.Hkv);
-    const uint4* src = reinterpret_cast<const uint4*>(in) + it * 2;
+  for (uint32_t it = blockIdx.x * kThreads + threadIdx.x; it < items; it += gridDim.x * kThreads) {
+    const Item at_item = item_of(M, it);
+    const int blk = at_item.blk;
+    const uint4* src = reinterpret_cast<const uint4*>(in) + (int64_t)it * 2;
     const uint4 u0 = src[0], u1 = src[1];
-    const RowAt at = find_row(p, tok, kh);
+    const RowAt at = find_row(p, at_item.tok, at_item.kh);
     if (!at.ok) continue;
     const uint32_t w[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
     float x[16];
     float a = 0.f;
-    const float most = 3.3895314e38f;  // bf16's largest: infinities and NaN, which have no code, count as it
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const float2 f = unpack_bf16x2(w[k]);
-      x[2 * k] = fmaxf(fminf(f.x, most), -most);
-      x[2 * k + 1] = fmaxf(fminf(f.y, most), -most);
-      a = fmaxf(a, fmaxf(fabsf(x[2 * k]), fabsf(x[2 * k + 1])));
+      x[2 * k] = f.x;
+      x[2 * k + 1] = f.y;
+      a = fmaxf(a, fmaxf(fabsf(f.x), fabsf(f.y)));  // (NaN are no magnitudes; infinities take the largest codes)
     }
     uint16_t code;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(code) : "f"(0.f), "f"(__fdiv_rn(__fdiv_rn(a, g), 6.f)));
     const float s = __half2float(__ushort_as_half((unsigned short)(e4m3_to_half2(code) & 0xffff))) * g;
-    const float inv = s > 0.f ? __fdiv_rn(1.f, s) : 0.f;  // (a scale of 0 holds zeros)
+    const float inv = __fdiv_rn(1.f, s);
     uint32_t held[2] = {0, 0};
+    if (s > 0.f) {  // (a scale of 0 holds zeros)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      float y[2];
+      for (int k = 0; k < 8; ++k) {
+        float y[2];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        // (from 8 on the level is 6 whatever the quotient: no overflow before the residual)
-        const float y0 = fmaxf(fminf(x[2 * k + e] * inv, 8.f), -8.f);
-        y[e] = s > 0.f ? fmaf(fmaf(-y0, s, x[2 * k + e]), inv, y0) : 0.f;
+        for (int e = 0; e < 2; ++e) {
+          const float y0 = x[2 * k + e] * inv;
+          // (from 8 on the level is 6 whatever the residual)
+          y[e] = fabsf(y0) < 8.f ? fmaf(fmaf(-y0, s, x[2 * k + e]), inv, y0) : y0;
+        }
+        uint32_t b;
+        asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u32.u8 %0, t;\n\t}" : "=r"(b) : "f"(y[1]), "f"(y[0]));
+        held[k >> 2] |= b << (8 * (k & 3));
       }
-      uint32_t b;
-      asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u32.u8 %0, t;\n\t}" : "=r"(b) : "f"(y[1]), "f"(y[0]));
-      held[k >> 2] |= b << (8 * (k & 3));
     }
     uint8_t* slab = p.pool + at.slab + (blockIdx.y ? (int64_t)M.Hkv * M.P * (M.D / 2 + M.D / 16) : 0);
     *reinterpret_cast<uint2*>(slab + at.slot * (M.D / 2) + blk * 8) = make_uint2(held[0], held[1]);
@@ -112,14 +121,14 @@ __global__ void __launch_bounds__(kThreads) packed_append_kernel(const PackedCac
 
 __global__ void __launch_bounds__(kThreads) packed_read_kernel(const PackedCacheParams p) {
   const ModelParams& M = p.m;
-  const int bpr = M.D / 16, shift = bpr == 8 ? 3 : 2;
-  const int64_t items = (int64_t)p.total_q * M.Hkv * bpr;
+  const int bpr = M.D / 16;
+  const uint32_t items = (uint32_t)p.total_q * M.Hkv * bpr;
   __nv_bfloat16* out = blockIdx.y ? p.v_out : p.k_out;
   const float g = blockIdx.y ? p.v_scale : p.k_scale;
-  for (int64_t it = (int64_t)blockIdx.x * kThreads + threadIdx.x; it < items; it += (int64_t)gridDim.x * kThreads) {
-    const int64_t row = it >> shift;
-    const int blk = (int)(it & (bpr - 1)), tok = (int)(row / M.Hkv), kh = (int)(row - (int64_t)tok * M.Hkv);
-    const RowAt at = find_row(p, tok, kh);
+  for (uint32_t it = blockIdx.x * kThreads + threadIdx.x; it < items; it += gridDim.x * kThreads) {
+    const Item at_item = item_of(M, it);
+    const int blk = at_item.blk;
+    const RowAt at = find_row(p, at_item.tok, at_item.kh);
     if (!at.ok) continue;
     const uint8_t* slab = p.pool + at.slab + (blockIdx.y ? (int64_t)M.Hkv * M.P * (M.D / 2 + M.D / 16) : 0);
     const uint2 held = *reinterpret_cast<const uint2*>(slab + at.slot * (M.D / 2) + blk * 8);
@@ -137,7 +146,7 @@ __global__ void __launch_bounds__(kThreads) packed_read_kernel(const PackedCache
         o[4 * k + i] = pack_bf16x2(v.x * g, v.y * g);
       }
     }
-    uint4* dst = reinterpret_cast<uint4*>(out) + it * 2;
+    uint4* dst = reinterpret_cast<uint4*>(out) + (int64_t)it * 2;
     dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
     dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
   }

@@ -54,34 +54,58 @@ __device__ __forceinline__ int block_prefix(int mine, int* s_warp, int* total) {
   return __shfl_sync(0xffffffffu, wi - w, warp) + incl - mine;
 }
 
-// The one pass over the counts: copies them, and sets the bit of every page with a holder.  `map`, where given, gets the
-// identity.
-__device__ __forceinline__ void scan_counts(const int32_t* ref, int32_t* ref_out, int32_t* map, int num_pages, Share sh, uint32_t* live) {
+// The one pass over the counts: sets the bit of every free page and, with `copy`, copies them; `map`, where given, gets the identity.
+__device__ __forceinline__ void scan_counts(const int32_t* ref, int32_t* ref_out, int32_t* map, bool copy, int num_pages, Share sh,
+                                            uint32_t* free_bits) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  constexpr int U = 8;  // loads in flight
-  for (int w0 = warp * U; w0 < sh.words; w0 += kWarps * U) {
-    int32_t v[U];
+  constexpr int U = 4;  // loads in flight: 16 bytes, four pages, of each lane; a warp's load covers four words of the bitmap
+  const bool wide = ((reinterpret_cast<uintptr_t>(ref) | reinterpret_cast<uintptr_t>(ref_out) | reinterpret_cast<uintptr_t>(map)) & 15) == 0;
+  for (int w0 = warp * 4 * U; w0 < sh.words; w0 += kWarps * 4 * U) {
+    int4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t page = (int64_t)(sh.first + w0 + u) * 32 + lane;
-      v[u] = w0 + u < sh.words && page < num_pages ? ref[page] : 1;  // (no page: not a free one)
+      const int64_t page = (int64_t)(sh.first + w0 + 4 * u) * 32 + 4 * lane;
+      if (w0 + 4 * u + lane / 8 >= sh.words) {
+        v[u] = make_int4(1, 1, 1, 1);  // (another block's)
+      } else if (wide && page + 4 <= num_pages) {
+        v[u] = *reinterpret_cast<const int4*>(ref + page);
+      } else {
+        v[u].x = page < num_pages ? ref[page] : 1;  // (no page: not a free one)
+        v[u].y = page + 1 < num_pages ? ref[page + 1] : 1;
+        v[u].z = page + 2 < num_pages ? ref[page + 2] : 1;
+        v[u].w = page + 3 < num_pages ? ref[page + 3] : 1;
+      }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (w0 + u >= sh.words) break;
-      const int64_t page = (int64_t)(sh.first + w0 + u) * 32 + lane;
-      const uint32_t bits = __ballot_sync(0xffffffffu, page < num_pages && v[u] > 0);
-      const uint32_t none = __ballot_sync(0xffffffffu, page < num_pages && v[u] <= 0);
-      if (lane == 0) {
-        live[2 * (w0 + u)] = bits;
-        live[2 * (w0 + u) + 1] = none;
-      }
-      if (page < num_pages) {
-        ref_out[page] = v[u];
-        if (map) map[page] = (int32_t)page;
+      const int word = w0 + 4 * u + lane / 8;
+      const int64_t page = (int64_t)(sh.first + w0 + 4 * u) * 32 + 4 * lane;
+      uint32_t bits = (uint32_t)(v[u].x <= 0) | (uint32_t)(v[u].y <= 0) << 1 | (uint32_t)(v[u].z <= 0) << 2 | (uint32_t)(v[u].w <= 0) << 3;
+      bits <<= 4 * (lane & 7);
+#pragma unroll
+      for (int x = 1; x < 8; x <<= 1) bits |= __shfl_xor_sync(0xffffffffu, bits, x);
+      if (word >= sh.words) continue;
+      if ((lane & 7) == 0) free_bits[word] = bits;
+      if (!copy) continue;
+      if (wide && page + 4 <= num_pages) {
+        *reinterpret_cast<int4*>(ref_out + page) = v[u];
+        if (map) *reinterpret_cast<int4*>(map + page) = make_int4((int)page, (int)page + 1, (int)page + 2, (int)page + 3);
+      } else {
+        const int32_t each[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (page + e >= num_pages) break;
+          ref_out[page + e] = each[e];
+          if (map) map[page + e] = (int)page + e;
+        }
       }
     }
   }
+}
+// The pages of a word that are there.
+__device__ __forceinline__ uint32_t pages_of_word(int num_pages, int word) {
+  const int left = num_pages - word * 32;
+  return left >= 32 ? 0xffffffffu : (1u << left) - 1;
 }
 
 // Sums a per-block number over the blocks before this one and over all of them.  `started`: what the block's arrival at the
@@ -98,6 +122,23 @@ __device__ __forceinline__ void cluster_prefix(cg::cluster_group& cluster, cg::c
   }
   *before = b;
   *all = a;
+}
+
+// The counts of a large pool, and where given the identity, copied by all SMs while the cluster behind it looks at the rows.
+constexpr int kWideThreads = 256;
+__global__ void __launch_bounds__(kWideThreads) pages_copy_counts_kernel(const int32_t* ref, int32_t* ref_out, int32_t* map, const int num_pages) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const bool wide = ((reinterpret_cast<uintptr_t>(ref) | reinterpret_cast<uintptr_t>(ref_out) | reinterpret_cast<uintptr_t>(map)) & 15) == 0;
+  const int stride = gridDim.x * kWideThreads, me = blockIdx.x * kWideThreads + threadIdx.x;
+  const int quads = wide ? num_pages / 4 : 0;
+  for (int i = me; i < quads; i += stride) {
+    reinterpret_cast<int4*>(ref_out)[i] = reinterpret_cast<const int4*>(ref)[i];
+    if (map) reinterpret_cast<int4*>(map)[i] = make_int4(4 * i, 4 * i + 1, 4 * i + 2, 4 * i + 3);
+  }
+  for (int i = 4 * quads + me; i < num_pages; i += stride) {
+    ref_out[i] = ref[i];
+    if (map) map[i] = i;
+  }
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -217,7 +258,7 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
   int32_t* s_first = s_mem;                // [rows_in] first child
   int32_t* s_most = s_first + p.rows_in;   // [rows_in] most pages that a child shares
   int32_t* s_rank = s_most + p.rows_in;    // [rows_out] rank of the row's first fresh page
-  uint32_t* s_live = reinterpret_cast<uint32_t*>(s_rank + p.rows_out);
+  uint32_t* s_free = reinterpret_cast<uint32_t*>(s_rank + p.rows_out);
   const int block = (int)cluster.block_rank(), warp = threadIdx.x >> 5;
   const Share sh = share_of(p.num_pages, block);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -267,12 +308,12 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
   }
 
   // the free pages of lowest number
-  scan_counts(p.ref, p.ref_out, nullptr, p.num_pages, sh, s_live);
+  scan_counts(p.ref, p.ref_out, nullptr, !p.copied, p.num_pages, sh, s_free);
   __syncthreads();
   const int wper = (sh.words + kThreads - 1) / kThreads;
   const int w0 = threadIdx.x * wper, w1 = min(w0 + wper, sh.words);
   int free_mine = 0;
-  for (int w = w0; w < w1; ++w) free_mine += __popc(s_live[2 * w + 1]);
+  for (int w = w0; w < w1; ++w) free_mine += __popc(s_free[w]);
   int free_block, base, free_all;
   int rank = block_prefix(free_mine, s_warp, &free_block);
   cluster_prefix(cluster, std::move(started), free_block, s_counts, &base, &free_all);
@@ -281,10 +322,11 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
   if (rows_ok && enough) {
     rank += base;
     for (int w = w0; w < w1 && rank < fresh_total; ++w) {
-      uint32_t bits = s_live[2 * w + 1];
+      uint32_t bits = s_free[w];
       for (; bits && rank < fresh_total; bits &= bits - 1) p.fresh[rank++] = (sh.first + w) * 32 + __ffs(bits) - 1;
     }
   }
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // (with p.copied: the counts' copy, launched before, is there)
   if (p.second) {  // a second launch does the rest
     if (block == 0) {
       for (int i = threadIdx.x; i < p.rows_in; i += kThreads) {
@@ -301,7 +343,6 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
   if (rows_ok && enough) apply_fork(p, s_first, s_most, s_rank, block + kBlocks * warp, kBlocks * kWarps);
 }
 
-constexpr int kWideThreads = 256;
 __global__ void __launch_bounds__(kWideThreads) pages_fork_apply_kernel(const PagesForkParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");  // launched early behind pages_fork_kernel
   if (*p.ok == 0) return;
@@ -357,26 +398,26 @@ __global__ void __launch_bounds__(kThreads) pages_compact_kernel(const PagesComp
   auto started = cluster.barrier_arrive();
   extern __shared__ int32_t s_mem[];
   __shared__ int s_warp[kWarps], s_counts[kBlocks];
-  uint32_t* s_live = reinterpret_cast<uint32_t*>(s_mem);
+  uint32_t* s_free = reinterpret_cast<uint32_t*>(s_mem);
   const int block = (int)cluster.block_rank(), warp = threadIdx.x >> 5;
   const Share sh = share_of(p.num_pages, block);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   for (int i = block * kThreads + threadIdx.x; i < p.max_moves; i += kBlocks * kThreads) p.move_src[i] = p.move_dst[i] = -1;
-  scan_counts(p.ref, p.ref_out, p.page_map, p.num_pages, sh, s_live);
+  scan_counts(p.ref, p.ref_out, p.page_map, !p.copied, p.num_pages, sh, s_free);
   __syncthreads();
   const int wper = (sh.words + kThreads - 1) / kThreads;
   const int w0 = threadIdx.x * wper, w1 = min(w0 + wper, sh.words);
   int mine = 0;
-  for (int w = w0; w < w1; ++w) mine += __popc(s_live[2 * w]);
+  for (int w = w0; w < w1; ++w) mine += __popc(pages_of_word(p.num_pages, sh.first + w) & ~s_free[w]);
   int in_block, base, total;
   int before = block_prefix(mine, s_warp, &in_block);
   cluster_prefix(cluster, std::move(started), in_block, s_counts, &base, &total);
   before += base;  // live pages before this thread's first
   for (int w = w0; w < w1; ++w) {
-    const uint32_t live = s_live[2 * w];
+    const uint32_t live = pages_of_word(p.num_pages, sh.first + w) & ~s_free[w];
     const int page0 = (sh.first + w) * 32;
     // free pages below the number of live ones
-    for (uint32_t bits = page0 < total ? s_live[2 * w + 1] : 0; bits; bits &= bits - 1) {
+    for (uint32_t bits = page0 < total ? s_free[w] : 0; bits; bits &= bits - 1) {
       const int b = __ffs(bits) - 1, page = page0 + b;
       const int at = page - (before + __popc(live & ((1u << b) - 1)));
       if (page >= total || at >= p.max_moves) break;
@@ -391,6 +432,7 @@ __global__ void __launch_bounds__(kThreads) pages_compact_kernel(const PagesComp
       }
     before += __popc(live);
   }
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // (with p.copied: the copy and the identity, launched before, are there)
   cluster.sync();
   for (int i = block * kThreads + threadIdx.x; i < p.max_moves; i += kBlocks * kThreads) {
     const int src = p.move_src[i], dst = p.move_dst[i];
@@ -441,13 +483,15 @@ cudaError_t launch_cluster(Kernel kern, const Params& p, size_t smem, cudaStream
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = kBlocks;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = p.copied ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
@@ -466,22 +510,27 @@ cudaError_t launch_wide(Kernel kern, const Params& p, int num_sms, cudaStream_t 
   return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
-// Table entries up to which the cluster rewrites them itself.
+// Table entries up to which the cluster rewrites them itself, and pages up to which it copies the counts.
 constexpr int64_t kSmallTables = 32768;
+constexpr int kSmallPool = 65536;
 
-size_t bitmap_bytes(int num_pages) { return (size_t)(((num_pages + 31) / 32 + kBlocks - 1) / kBlocks) * 8; }
+size_t bitmap_bytes(int num_pages) { return (size_t)(((num_pages + 31) / 32 + kBlocks - 1) / kBlocks) * 4; }
 
 }  // namespace
 
 cudaError_t hswa_launch_pages_fork(const PagesForkParams& params, int num_sms, cudaStream_t s) {
   PagesForkParams p = params;
   p.second = (int64_t)p.rows_in * p.max_blocks + (int64_t)p.rows_out * p.out_max_blocks > kSmallTables;
-  const cudaError_t e = launch_cluster(pages_fork_kernel, p, ((size_t)p.rows_in * 2 + p.rows_out) * 4 + 8 + bitmap_bytes(p.num_pages), s);
+  p.copied = p.num_pages > kSmallPool;
+  if (p.copied) pages_copy_counts_kernel<<<4 * num_sms, kWideThreads, 0, s>>>(p.ref, p.ref_out, nullptr, p.num_pages);
+  const cudaError_t e = launch_cluster(pages_fork_kernel, p, ((size_t)p.rows_in * 2 + p.rows_out) * 4 + bitmap_bytes(p.num_pages), s);
   return e != cudaSuccess || !p.second ? e : launch_wide(pages_fork_apply_kernel, p, num_sms, s);
 }
 cudaError_t hswa_launch_pages_compact(const PagesCompactParams& params, int num_sms, cudaStream_t s) {
   PagesCompactParams p = params;
   p.second = (int64_t)p.rows * p.max_blocks > kSmallTables;
+  p.copied = p.num_pages > kSmallPool;
+  if (p.copied) pages_copy_counts_kernel<<<4 * num_sms, kWideThreads, 0, s>>>(p.ref, p.ref_out, p.page_map, p.num_pages);
   const cudaError_t e = launch_cluster(pages_compact_kernel, p, bitmap_bytes(p.num_pages), s);
   return e != cudaSuccess || !p.second ? e : launch_wide(pages_compact_apply_kernel, p, num_sms, s);
 }
