@@ -54,6 +54,11 @@ __device__ __forceinline__ int block_prefix(int mine, int* s_warp, int* total) {
   return __shfl_sync(0xffffffffu, wi - w, warp) + incl - mine;
 }
 
+// The block's share of the counts on its way to L2, while the rows are looked at.
+__device__ __forceinline__ void fetch_counts(const int32_t* ref, int num_pages, Share sh) {
+  for (int w = threadIdx.x; w < sh.words; w += kThreads)
+    if ((sh.first + w) * 32 < num_pages) asm volatile("prefetch.global.L2 [%0];" ::"l"(ref + (int64_t)(sh.first + w) * 32));
+}
 // The one pass over the counts: sets the bit of every free page and, with `copy`, copies them; `map`, where given, gets the identity.
 __device__ __forceinline__ void scan_counts(const int32_t* ref, int32_t* ref_out, int32_t* map, bool copy, int num_pages, Share sh,
                                             uint32_t* free_bits) {
@@ -152,15 +157,19 @@ struct RowPlan {
   bool first;                                 // the parent's first child
 };
 __device__ __forceinline__ int pages_of(int tokens, int page_size) { return (int)(((int64_t)tokens + page_size - 1) / page_size); }
-__device__ __forceinline__ RowPlan plan_of(const PagesForkParams& p, const int32_t* first, const int32_t* most, int r) {
+// The rows' arrays: the call's own, or their copies in shared memory.
+struct Rows {
+  const int32_t *parent, *len, *need, *held, *first, *most, *rank;
+};
+__device__ __forceinline__ RowPlan plan_of(const PagesForkParams& p, const Rows& rows, int r) {
   RowPlan o;
-  o.parent = p.parent[r];
-  const int len = p.len[r];
+  o.parent = rows.parent[r];
+  const int len = rows.len[r];
   o.full = len / p.page_size;
-  o.held = pages_of(max(len, p.need[r]), p.page_size);
-  o.parent_held = o.parent >= 0 ? p.held[o.parent] : 0;
-  o.first = o.parent >= 0 && first[o.parent] == r;
-  o.most = o.parent >= 0 ? most[o.parent] : 0;
+  o.held = pages_of(max(len, rows.need[r]), p.page_size);
+  o.parent_held = o.parent >= 0 ? rows.held[o.parent] : 0;
+  o.first = o.parent >= 0 && rows.first[o.parent] == r;
+  o.most = o.parent >= 0 ? rows.most[o.parent] : 0;
   return o;
 }
 // Does place k >= full of the row keep the parent's page?
@@ -171,8 +180,8 @@ __device__ __forceinline__ bool passed(const PagesForkParams& p, const RowPlan& 
   return page >= 0 && page < p.num_pages && p.ref[page] == 1;
 }
 
-// The new tables and counts, by warp `me` of `all`: first, most, rank as computed before, fresh pages listed, counts copied.
-__device__ __forceinline__ void apply_fork(const PagesForkParams& p, const int32_t* first, const int32_t* most, const int32_t* rank, int me, int all) {
+// The new tables and counts, by warp `me` of `all`: the rows' plans are made, fresh pages listed, counts copied.
+__device__ __forceinline__ void apply_fork(const PagesForkParams& p, const Rows& rows, int me, int all) {
   const int lane = threadIdx.x & 31;
   auto count = [&](int page, int by, int row, int k) {
     if (page < 0 || page >= p.num_pages)
@@ -185,7 +194,7 @@ __device__ __forceinline__ void apply_fork(const PagesForkParams& p, const int32
   // new rows: shared places in chunks of 256, the places behind them by the warp of chunk 0
   for (int64_t it = me; it < (int64_t)p.rows_out * chunks; it += all) {
     const int r = (int)(it / chunks), c = (int)(it % chunks);
-    const RowPlan o = plan_of(p, first, most, r);
+    const RowPlan o = plan_of(p, rows, r);
     int32_t* out = p.table_out + (int64_t)r * p.out_max_blocks;
     const int32_t* in = p.table + (int64_t)max(o.parent, 0) * p.max_blocks;
     int page[CH / 32];
@@ -202,8 +211,8 @@ __device__ __forceinline__ void apply_fork(const PagesForkParams& p, const int32
       count(page[u], o.first ? 0 : 1, r, k);
     }
     if (c != 0) continue;
-    int next = rank[r];
-    const int len = p.len[r];
+    int next = rows.rank[r];
+    const int len = rows.len[r];
     int src = -1, dst = -1;
     for (int k0 = o.full; k0 < o.held; k0 += 32) {
       const int k = k0 + lane;
@@ -235,9 +244,9 @@ __device__ __forceinline__ void apply_fork(const PagesForkParams& p, const int32
   // old rows: what their first child does not keep loses a holder
   for (int64_t it = me; it < (int64_t)p.rows_in * chunks; it += all) {
     const int i = (int)(it / chunks), c = (int)(it % chunks);
-    const int held = p.held[i], child = first[i];
+    const int held = rows.held[i], child = rows.first[i];
     RowPlan o = {};
-    if (child != INT32_MAX) o = plan_of(p, first, most, child);
+    if (child != INT32_MAX) o = plan_of(p, rows, child);
     if (child != INT32_MAX && min(held, (c + 1) * CH) <= o.full) continue;
 #pragma unroll
     for (int u = 0; u < CH / 32; ++u) {
@@ -255,32 +264,41 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
   auto started = cluster.barrier_arrive();
   extern __shared__ int32_t s_mem[];
   __shared__ int s_warp[kWarps], s_counts[kBlocks], s_bad;
-  int32_t* s_first = s_mem;                // [rows_in] first child
-  int32_t* s_most = s_first + p.rows_in;   // [rows_in] most pages that a child shares
-  int32_t* s_rank = s_most + p.rows_in;    // [rows_out] rank of the row's first fresh page
-  uint32_t* s_free = reinterpret_cast<uint32_t*>(s_rank + p.rows_out);
+  int32_t* s_first = s_mem;                 // [rows_in] first child
+  int32_t* s_most = s_first + p.rows_in;    // [rows_in] most pages that a child shares
+  int32_t* s_held = s_most + p.rows_in;     // [rows_in]
+  int32_t* s_rank = s_held + p.rows_in;     // [rows_out] rank of the row's first fresh page
+  int32_t* s_parent = s_rank + p.rows_out;  // [rows_out] and two more
+  int32_t* s_len = s_parent + p.rows_out;
+  int32_t* s_need = s_len + p.rows_out;
+  uint32_t* s_free = reinterpret_cast<uint32_t*>(s_need + p.rows_out);
+  const Rows rows = {s_parent, s_len, s_need, s_held, s_first, s_most, s_rank};
   const int block = (int)cluster.block_rank(), warp = threadIdx.x >> 5;
   const Share sh = share_of(p.num_pages, block);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  fetch_counts(p.ref, p.num_pages, sh);
   if (threadIdx.x == 0) s_bad = 0;
   for (int i = threadIdx.x; i < p.rows_in; i += kThreads) {
+    const int held = p.held[i];
     s_first[i] = INT32_MAX;
     s_most[i] = 0;
-  }
-  __syncthreads();
-
-  // every block looks at all rows: none waits for another
-  for (int i = threadIdx.x; i < p.rows_in; i += kThreads) {
-    const int held = p.held[i];
+    s_held[i] = held;
     if (held < 0 || held > p.max_blocks) {
       s_bad = 1;
       if (block == 0) record_error(p.err, HSWA_ERR_BOUNDS, i, -1, held);
     }
   }
   for (int r = threadIdx.x; r < p.rows_out; r += kThreads) {
-    const int parent = p.parent[r], len = p.len[r], need = p.need[r];
+    s_parent[r] = p.parent[r];
+    s_len[r] = p.len[r];
+    s_need[r] = p.need[r];
+  }
+  __syncthreads();
+  // every block looks at all rows: none waits for another
+  for (int r = threadIdx.x; r < p.rows_out; r += kThreads) {
+    const int parent = s_parent[r], len = s_len[r], need = s_need[r];
     bool ok = parent >= -1 && parent < p.rows_in && len >= 0 && pages_of(max(len, need), p.page_size) <= p.out_max_blocks;
-    if (ok) ok = parent < 0 ? len == 0 : pages_of(len, p.page_size) <= p.held[parent];
+    if (ok) ok = parent < 0 ? len == 0 : pages_of(len, p.page_size) <= s_held[parent];
     if (!ok) {
       s_bad = 1;
       if (block == 0) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, parent);
@@ -297,7 +315,7 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
     const int r0 = threadIdx.x * per, r1 = min(r0 + per, p.rows_out);
     int sum = 0;
     for (int r = r0; r < r1; ++r) {
-      const RowPlan o = plan_of(p, s_first, s_most, r);
+      const RowPlan o = plan_of(p, rows, r);
       int fresh = o.held - o.full, page;
       for (int k = o.most; o.first && k < min(o.held, o.parent_held); ++k) fresh -= passed(p, o, k, &page);
       s_rank[r] = sum;
@@ -340,14 +358,14 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
     return;
   }
   cluster.sync();  // counts copied, fresh pages listed, and nobody reads another block's shared memory any more
-  if (rows_ok && enough) apply_fork(p, s_first, s_most, s_rank, block + kBlocks * warp, kBlocks * kWarps);
+  if (rows_ok && enough) apply_fork(p, rows, block + kBlocks * warp, kBlocks * kWarps);
 }
 
 __global__ void __launch_bounds__(kWideThreads) pages_fork_apply_kernel(const PagesForkParams p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");  // launched early behind pages_fork_kernel
   if (*p.ok == 0) return;
-  const int warps = kWideThreads / 32;
-  apply_fork(p, p.first, p.most, p.rank, blockIdx.x + gridDim.x * (threadIdx.x >> 5), gridDim.x * warps);
+  const Rows rows = {p.parent, p.len, p.need, p.held, p.first, p.most, p.rank};
+  apply_fork(p, rows, blockIdx.x + gridDim.x * (threadIdx.x >> 5), gridDim.x * (kWideThreads / 32));
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -402,6 +420,7 @@ __global__ void __launch_bounds__(kThreads) pages_compact_kernel(const PagesComp
   const int block = (int)cluster.block_rank(), warp = threadIdx.x >> 5;
   const Share sh = share_of(p.num_pages, block);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  fetch_counts(p.ref, p.num_pages, sh);
   for (int i = block * kThreads + threadIdx.x; i < p.max_moves; i += kBlocks * kThreads) p.move_src[i] = p.move_dst[i] = -1;
   scan_counts(p.ref, p.ref_out, p.page_map, !p.copied, p.num_pages, sh, s_free);
   __syncthreads();
@@ -523,7 +542,7 @@ cudaError_t hswa_launch_pages_fork(const PagesForkParams& params, int num_sms, c
   p.second = (int64_t)p.rows_in * p.max_blocks + (int64_t)p.rows_out * p.out_max_blocks > kSmallTables;
   p.copied = p.num_pages > kSmallPool;
   if (p.copied) pages_copy_counts_kernel<<<4 * num_sms, kWideThreads, 0, s>>>(p.ref, p.ref_out, nullptr, p.num_pages);
-  const cudaError_t e = launch_cluster(pages_fork_kernel, p, ((size_t)p.rows_in * 2 + p.rows_out) * 4 + bitmap_bytes(p.num_pages), s);
+  const cudaError_t e = launch_cluster(pages_fork_kernel, p, ((size_t)p.rows_in * 3 + (size_t)p.rows_out * 4) * 4 + bitmap_bytes(p.num_pages), s);
   return e != cudaSuccess || !p.second ? e : launch_wide(pages_fork_apply_kernel, p, num_sms, s);
 }
 cudaError_t hswa_launch_pages_compact(const PagesCompactParams& params, int num_sms, cudaStream_t s) {
