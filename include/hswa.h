@@ -340,7 +340,7 @@ hswa_status hswa_evict_compact(hswa_handle* h, const hswa_layer* layer, const hs
  *   sees its own row as the cache holds it).  causal == 0: every token sees all j < ctx_len[r] (an encoder's states).  A token
  *   that sees nothing gives zeros and an lse of minus infinity.  q: device bf16 [T][Hq][D]; out: device [T][Hq][D] in
  *   cfg.out_dtype; lse: device fp32 [T][Hq] or NULL.  Held values enter the products exactly; q enters them in fp16 after a
- *   power of two per row (exact but for elements below 2^-28 of the row's largest); probabilities enter the PV product as
+ *   power of two (exact but for elements below 2^-28 of the largest of a KV head's rows in the step); probabilities enter the PV product as
  *   fp16, row sums and lse are taken over the fp32 values.  batch->q_indptr may be NULL (one token per request).  Slots behind a
  *   request's last row may hold anything.  Workspace: hswa_packed_workspace_need bytes, else HSWA_ERR_WORKSPACE; 256-byte
  *   aligned.  The block table must cover max_ctx_len (HSWA_ERR_INVALID_ARG); max_ctx_len + max_q_len is at most 2^30

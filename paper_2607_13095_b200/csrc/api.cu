@@ -203,7 +203,7 @@ bool plan_cross(const hswa_handle* h, int batch, int total_q, int max_q_len, int
 // Attention over a 4-bit cache: how one call is laid out, from host-known values only.
 struct PackedPlan {
   int rows;                            // few rows per KV head: 8, 16 or 32 of a block; 0: the tile kernel
-  int runs;                            // few rows: runs of tiles, 0 for one block per stream
+  int runs;                            // few rows: runs of tiles, 0: a block per stream
   int row_tiles, slices, slice_len;    // the tile kernel: blocks along a request's rows, key slices
   size_t o_bytes, ml_bytes, before_bytes;
 };
@@ -217,11 +217,14 @@ bool plan_packed(const hswa_handle* h, int batch, int total_q, int max_q_len, in
   if (streams > INT32_MAX) return false;
   if (rows <= 32) {
     c.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
-    if (keys > kUnsplitLen) {
-      // as many runs as blocks fit the SMs, of eight tiles at least (a block's seven warps take one each)
-      const int64_t tiles = streams * ((keys + 63) / 64);
-      const int64_t fit = (int64_t)(c.rows == 8 ? hswa_packed_stream_runs_per_sm() : hswa_packed_decode_blocks_per_sm(c.rows)) * h->num_sms;
-      const int64_t most = c.rows == 8 ? (tiles + 3) / 4 : (tiles + 7) / 8;
+    // Up to so many keys a block takes a stream as a whole, one launch without a join.  Measured, us in one block / in runs, 64 / 8
+    // heads of 128: a row per head, 2 requests of 2000 keys 18 / 27, of 4000 27 / 27, 32 of 2000 29 / 39, 64 of 2000 49 / 53, of 4000 80 / 86;
+    // four, 32 of 600 to 1500 57 / 66, 2 of 2000 39 / 37, 64 of 4000 193 / 141.
+    if (keys > (rows <= 8 ? 2112 : 1088)) {
+      // as many runs as fit the SMs: of a warp, four 64-key tiles at least; of a block of the tcgen05 kernel, two of 128 keys.  (Warps of
+      // two tiles leave the join twice the pieces: 1 request of 32768 keys 49 us against 37, 2 of 4000 23 against 27.)
+      const int64_t fit = (int64_t)(rows <= 8 ? hswa_packed_stream_runs_per_sm() : 1) * h->num_sms;
+      const int64_t most = (streams * ((keys + 63) / 64) + 3) / 4;
       c.runs = (int)(fit < most ? fit : most);
       c.o_bytes = align((size_t)2 * c.runs * c.rows * h->cfg.head_dim * sizeof(float));
       c.ml_bytes = align((size_t)2 * c.runs * c.rows * sizeof(float2));
@@ -1015,8 +1018,12 @@ hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, con
   }
   p.err = h->err;
   cudaStream_t s = (cudaStream_t)stream;
-  if (pl.rows == 8 && pl.runs > 0) return hswa_launch_packed_stream(p, s) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
-  if (pl.rows > 0) return hswa_launch_packed_decode(p, pl.rows, s) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+  if (pl.rows > 0) {
+    const cudaError_t e = pl.runs == 0    ? hswa_launch_packed_decode(p, pl.rows, s)
+                          : pl.rows == 8 ? hswa_launch_packed_stream(p, s)
+                                         : hswa_launch_packed_rows(p, pl.rows, s);
+    return e == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+  }
   if (hswa_launch_packed_tile(p, s) != cudaSuccess) return HSWA_ERR_CUDA;
   if (pl.slices > 1) {
     const CrossParams join = {p.m, out, lse, b->total_q, b->q_indptr, b->batch, pl.slices, p.part_o, p.part_ml};

@@ -36,7 +36,7 @@ struct PackedAttnParams {
   void* out;               // [T][Hq][D]
   float* lse;              // [T][Hq] or null
   int32_t total_q, max_q_len, max_ctx_len;
-  // few rows: runs of tiles (0: one stream per block) and the tiles of all requests before each, [B + 1]
+  // few rows: runs of tiles (0: a block per stream) and the tiles of all requests before each, [B + 1]
   int32_t runs;
   int64_t* before;
   // many rows: blocks along a request's rows, keys per slice (a multiple of 128), slices per row
@@ -51,10 +51,11 @@ cudaError_t hswa_launch_packed_read(const PackedCacheParams& p, int num_sms, cud
 // Up to eight rows (tokens x heads of a KV head), long contexts: a run per warp
 int hswa_packed_stream_runs_per_sm();
 cudaError_t hswa_launch_packed_stream(const PackedAttnParams& p, cudaStream_t s);
-// The join of runs' pieces of `cols` rows each
-cudaError_t hswa_launch_packed_join(const PackedAttnParams& p, int cols, cudaStream_t s);
-// Few rows: 8, 16 or 32 per block
-int hswa_packed_decode_blocks_per_sm(int rows);
+// Few rows, long contexts, on the 5th-generation tensor cores: up to 16 or 32 rows, a run per SM
+cudaError_t hswa_launch_packed_rows(const PackedAttnParams& p, int rows, cudaStream_t s);
+// The join of runs' pieces of `cols` rows each over key tiles of `tile`
+cudaError_t hswa_launch_packed_join(const PackedAttnParams& p, int cols, int tile, cudaStream_t s);
+// Up to 8, 16 or 32 rows, short contexts: a block per stream
 cudaError_t hswa_launch_packed_decode(const PackedAttnParams& p, int rows, cudaStream_t s);
 // Many rows: the tcgen05 tile kernel, two Q tiles of hswa_cross_tile_tokens tokens per block
 cudaError_t hswa_launch_packed_tile(const PackedAttnParams& p, cudaStream_t s);

@@ -1,10 +1,8 @@
-// Attention over a 4-bit cache for few rows per KV head (single tokens, drafts: up to 32 tokens x query heads): hswa_packed_attn.
+// Attention over a 4-bit cache for few rows per KV head (single tokens, drafts: up to 32 tokens x query heads) over contexts of up to
+// some thousand keys: hswa_packed_attn.
 //
-// The 64-key tiles of all (request, KV head) streams form one sequence, cut into equal runs, one for each of the blocks that the
-// SMs hold: no block ends early, whatever the lengths, and loads run on from stream to stream.  One warp fetches the pages'
-// slabs (a bulk copy each: rows and scales lie together) into a ring of slots; every other warp takes whole tiles, with a softmax
-// state of its own, and the block merges them where a stream ends.  A stream that a block has as a whole is written out there,
-// pieces of the others are joined by a second launch.
+// A block per (request, KV head).  One warp fetches the pages' slabs (a bulk copy each: rows and scales lie together) into a ring of
+// slots; every other warp takes whole 64-key tiles, with a softmax state of its own, and the block merges them at the end.
 // Bound by HBM (0.5625 bytes per element) and, close behind, by the instructions that turn codes into fp16; so both products
 // read their operands straight from the packed rows, without a trip through shared memory:
 //   S^T [keys x rows] = K Q^T: the element order along D is free as long as K and Q agree, so lane (g, t) of the fragment takes
@@ -42,11 +40,10 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
   float* s_down = reinterpret_cast<float*>(s_q + NT * KS * 32);            // [COLS]
   float2* s_ml = reinterpret_cast<float2*>(s_down + COLS);                 // [NW][COLS]
   uint64_t* bars = reinterpret_cast<uint64_t*>(s_ml + NW * COLS);          // full [NS], empty [NS]
-  int64_t* s_plan = reinterpret_cast<int64_t*>(bars + 2 * NS);             // a wait ran out, first request, tiles before it, a warp's sum [8]
+  int* s_stop = reinterpret_cast<int*>(bars + 2 * NS);                     // a wait ran out
   const ModelParams& M = p.m;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
-  const int B = p.b.B;
 
   const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + NS);
   if (threadIdx.x == 0) {
@@ -55,93 +52,47 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
       mbar_init(empty0 + 8 * s, 1);
     }
     mbar_fence_init();
+    *s_stop = 0;
   }
   if (blockIdx.x == 0) record_batch(p, kThreads);
-  // the block's run of tiles [w0, w1), and the request that it starts in
-  int64_t w0, w1;
-  int r0, kh0 = 0, tile0 = 0;
-  if (p.runs == 0) {  // one stream per block
-    r0 = blockIdx.x / M.Hkv;
-    kh0 = blockIdx.x % M.Hkv;
-    w0 = 0;
-    w1 = stream_of(p, r0).tiles;
-    if (threadIdx.x == 0) s_plan[0] = 0;
-    __syncthreads();
-    if (w1 == 0) return;
-  } else {
-    int i0, i1;
-    int64_t before;
-    if (threadIdx.x == 0) s_plan[0] = 0;
-    int64_t total = sum_tiles<kThreads>(p, s_plan + 3, &i0, &i1, &before);
-    total *= M.Hkv;
-    w0 = run_start(total, blockIdx.x, p.runs);
-    w1 = run_start(total, blockIdx.x + 1, p.runs);
-    for (int i = i0; i < i1; ++i) {
-      const int tiles = stream_of(p, i).tiles;
-      if (blockIdx.x == 0) p.before[i] = before;  // for the join
-      if (w0 >= before * M.Hkv && w0 < (before + tiles) * M.Hkv) {
-        s_plan[1] = i;
-        s_plan[2] = before;
-      }
-      before += tiles;
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.before[B] = total / M.Hkv;
-    __syncthreads();
-    if (w0 >= w1) return;
-    r0 = (int)s_plan[1];
-    const int64_t at = w0 - s_plan[2] * M.Hkv;
-    const int tiles = stream_of(p, r0).tiles;
-    kh0 = (int)(at / tiles);
-    tile0 = (int)(at % tiles);
-  }
+  const int r = blockIdx.x / M.Hkv, kh = blockIdx.x % M.Hkv;
+  const Stream sm = stream_of(p, r);
+  __syncthreads();
+  if (sm.tiles == 0) return;
+
   const int slab = M.P * (ROW + SC);
   if (warp == NW) {
     // ======================= producer =======================
     const int ppt = TK / M.P;  // pages per tile: 1, 2 or 4
     bool ok = true;
-    int64_t w = w0;
-    int r = r0, kh = kh0, tile = tile0;
     // K and V of two tiles at a time, a lane per page: waiting for a slot costs a few hundred cycles, and these waits overlap
     const int i = lane % ppt, kv = lane / ppt & 1, ahead = lane / (2 * ppt);
-    int at = 0;  // tiles before this piece
-    while (w < w1 && ok) {
-      const Stream s = stream_of(p, r);
-      const int count = (int)min((int64_t)(s.tiles - tile), w1 - w);
-      const int32_t* tbl = p.b.block_table + (int64_t)r * p.b.max_blocks;
-      const int n_pages = (s.end + M.P - 1) / M.P;  // (0: a request without keys)
-      const int page0 = tile * ppt;
-      int ids_next = page0 + lane < n_pages ? tbl[page0 + lane] : 0, ids = 0;
-      for (int j = 0; j < count; j += 2) {
-        if ((j * ppt & 31) == 0) {
-          ids = ids_next;
-          ids_next = page0 + j * ppt + 32 + lane < n_pages ? tbl[page0 + j * ppt + 32 + lane] : 0;
-        }
-        const int first = (j + ahead) * ppt, here = min(ppt, n_pages - page0 - first);  // pages of the lane's tile
-        int page = __shfl_sync(0xffffffffu, ids, (first + i) & 31);
-        const bool mine = ahead < 2 && j + ahead < count;
-        const int order = 2 * (at + j + ahead) + kv, slot = order % NS, round = order / NS;
-        if (mine && round > 0) ok = mbar_wait(empty0 + 8 * slot, (round - 1) & 1);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) {
-          if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, j, 50);
-          break;
-        }
-        if (mine && i == 0) mbar_arrive_expect_tx(full0 + 8 * slot, max(here, 0) * slab);
-        __syncwarp();
-        if (mine && i < here) {
-          if (page < 0 || page >= p.num_pages) {
-            record_error(p.err, HSWA_ERR_BOUNDS, r, page0 + first + i, page);
-            page = 0;
-          }
-          bulk_load(smem_u32(smem + slot * SLOT + i * slab), p.pool + (((int64_t)page * 2 + kv) * M.Hkv + kh) * slab, slab, full0 + 8 * slot);
-        }
+    const int32_t* tbl = p.b.block_table + (int64_t)r * p.b.max_blocks;
+    const int n_pages = (sm.end + M.P - 1) / M.P;  // (0: a request without keys)
+    int ids_next = lane < n_pages ? tbl[lane] : 0, ids = 0;
+    for (int j = 0; j < sm.tiles; j += 2) {
+      if ((j * ppt & 31) == 0) {
+        ids = ids_next;
+        ids_next = j * ppt + 32 + lane < n_pages ? tbl[j * ppt + 32 + lane] : 0;
       }
-      at += count;
-      w += count;
-      tile = 0;
-      if (++kh == M.Hkv) {
-        kh = 0;
-        do ++r; while (w < w1 && stream_of(p, r).tiles == 0);  // (requests with rows are left: w < w1)
+      const int first = (j + ahead) * ppt, here = min(ppt, n_pages - first);  // pages of the lane's tile
+      int page = __shfl_sync(0xffffffffu, ids, (first + i) & 31);
+      const bool mine = ahead < 2 && j + ahead < sm.tiles;
+      const int order = 2 * (j + ahead) + kv, slot = order % NS, round = order / NS;
+      if (mine && round > 0) ok = mbar_wait(empty0 + 8 * slot, (round - 1) & 1);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) {
+        if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, j, 50);
+        break;
+      }
+      if (mine && i == 0) mbar_arrive_expect_tx(full0 + 8 * slot, max(here, 0) * slab);
+      __syncwarp();
+      if (mine && i < here) {
+        if (page < 0 || page >= p.num_pages) {
+          record_error(p.err, HSWA_ERR_BOUNDS, r, first + i, page);
+          page = 0;
+        }
+        bulk_load(smem_u32(smem + slot * SLOT + i * slab), p.pool + (((int64_t)page * 2 + kv) * M.Hkv + kh) * slab, slab, full0 + 8 * slot);
       }
     }
     if (!ok) __nanosleep(100000);  // copies that nobody will wait for land before the block's memory is handed on
@@ -155,13 +106,7 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
   auto rows_of = [&](int key0) { return (key0 >> page_shift) * slab + (key0 & (M.P - 1)) * ROW; };
   auto scales_of = [&](int key0) { return (key0 >> page_shift) * slab + scales_at + (key0 & (M.P - 1)) * SC; };
   auto consumers_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(NW * 32) : "memory"); };
-  int64_t w = w0;
-  int r = r0, kh = kh0, tile = tile0;
-  int at0 = 0;  // tiles before this piece
   bool ok = true;
-  while (w < w1) {
-  const Stream sm = stream_of(p, r);
-  const int count = (int)min((int64_t)(sm.tiles - tile), w1 - w);
   const int rows = sm.n * M.G, end = sm.end;
   const int first_end = p.causal ? min(end, sm.len + 1) : end;  // keys that the first row sees
   auto has_row = [&](int tok) { return (unsigned)sm.t0 + (unsigned)tok < (unsigned)p.total_q; };
@@ -226,18 +171,18 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
       mul[c][e] = NT == 1 ? __shfl_sync(0xffffffffu, down1, (2 * t + e) * 4) : s_down[col];
       see[c][e] = p.causal ? min(end, sm.len + col / M.G + 1) : end;
     }
-  // the warp's tiles: every NW-th of the piece
-  for (int j = warp; j < count; j += NW) {
-    const int k_at = 2 * (at0 + j), k_slot = k_at % NS, v_slot = (k_at + 1) % NS;
+  // the warp's tiles: every NW-th
+  for (int j = warp; j < sm.tiles; j += NW) {
+    const int k_at = 2 * j, k_slot = k_at % NS, v_slot = (k_at + 1) % NS;
     ok = __all_sync(0xffffffffu, mbar_wait(full0 + 8 * k_slot, (k_at / NS) & 1) && mbar_wait(full0 + 8 * v_slot, ((k_at + 1) / NS) & 1));
     if (!ok) {
       if (lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, j, 51);
-      *reinterpret_cast<volatile int64_t*>(s_plan) = 1;
+      *reinterpret_cast<volatile int*>(s_stop) = 1;
       __nanosleep(100000);  // (copies in flight, as above)
       break;
     }
     const uint8_t *k_st = smem + k_slot * SLOT, *v_st = smem + v_slot * SLOT;
-    const int pos0 = (tile + j) * TK;
+    const int pos0 = j * TK;
     const bool masked = pos0 + TK > first_end;
 #pragma unroll 1
     for (int step = 0; step < TK / STEP; ++step) {
@@ -383,8 +328,7 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
     if (lane == 0) mbar_arrive(empty0 + 8 * v_slot);
   }
 
-  // ---- the piece's end: merge of the warps' states ----
-  const bool whole = tile == 0 && count == sm.tiles;
+  // ---- merge of the warps' states ----
 #pragma unroll
   for (int c = 0; c < NT; ++c)
 #pragma unroll
@@ -394,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
       if (g == 0) s_ml[warp * COLS + c * 8 + 2 * t + e] = make_float2(m[c][e], l[c][e]);
     }
   consumers_sync();
-  if (*reinterpret_cast<volatile int64_t*>(s_plan) != 0) return;
+  if (*reinterpret_cast<volatile int*>(s_stop) != 0) return;
   float L[NT][2], top[NT][2];
 #pragma unroll
   for (int c = 0; c < NT; ++c)
@@ -414,8 +358,7 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
       const float f = m[c][e] == -INFINITY ? 1.f : fast_exp2(m[c][e] - base);
       top[c][e] = mm;
       L[c][e] = sum;
-      // the layer's V scale, and the division where the block has all of the row's keys
-      const float out = f * (!whole ? p.v_scale : (sum != 0.f ? p.v_scale / sum : 0.f));
+      const float out = f * (sum != 0.f ? p.v_scale / sum : 0.f);
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         O[i][c][e] *= out;
@@ -447,60 +390,44 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
     }
     if (half > 1) consumers_sync();
   }
-  if (warp == 0) {
-    // a lane holds D / 8 neighbouring elements of two rows per eight
-    const int64_t piece = 2 * (int64_t)blockIdx.x + (tile == 0);  // a block has one piece at most that starts before it, and one that ends behind it
+  if (warp != 0) return;
+  // a lane holds D / 8 neighbouring elements of two rows per eight
 #pragma unroll
-    for (int c = 0; c < NT; ++c)
+  for (int c = 0; c < NT; ++c)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int col = c * 8 + 2 * t + e, tok = col / M.G;
-        if (col >= rows || !has_row(tok)) continue;
-        const int64_t orow = (int64_t)(sm.t0 + tok) * M.Hq + kh * M.G + col % M.G;
-        if (!whole || M.out_fp32) {
-          float* dst = (!whole ? p.part_o + (piece * COLS + col) * D : reinterpret_cast<float*>(p.out) + orow * D) + g * (D / 8);
+    for (int e = 0; e < 2; ++e) {
+      const int col = c * 8 + 2 * t + e, tok = col / M.G;
+      if (col >= rows || !has_row(tok)) continue;
+      const int64_t orow = (int64_t)(sm.t0 + tok) * M.Hq + kh * M.G + col % M.G;
+      if (M.out_fp32) {
+        float* dst = reinterpret_cast<float*>(p.out) + orow * D + g * (D / 8);
 #pragma unroll
-          for (int i = 0; i < MT; i += 2)
-            *reinterpret_cast<float4*>(dst + 2 * i) = make_float4(O[i][c][e], O[i][c][e + 2], O[i + 1][c][e], O[i + 1][c][e + 2]);
-        } else {
-          __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.out) + orow * D + g * (D / 8);
+        for (int i = 0; i < MT; i += 2)
+          *reinterpret_cast<float4*>(dst + 2 * i) = make_float4(O[i][c][e], O[i][c][e + 2], O[i + 1][c][e], O[i + 1][c][e + 2]);
+      } else {
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.out) + orow * D + g * (D / 8);
 #pragma unroll
-          for (int i = 0; i < MT; i += 4)
-            *reinterpret_cast<uint4*>(dst + 2 * i) =
-                make_uint4(pack_bf16x2(O[i][c][e], O[i][c][e + 2]), pack_bf16x2(O[i + 1][c][e], O[i + 1][c][e + 2]),
-                           pack_bf16x2(O[i + 2][c][e], O[i + 2][c][e + 2]), pack_bf16x2(O[i + 3][c][e], O[i + 3][c][e + 2]));
-        }
-        if (g == 0) {
-          if (!whole) p.part_ml[piece * COLS + col] = make_float2(top[c][e], L[c][e]);
-          else if (p.lse) p.lse[orow] = L[c][e] != 0.f ? (top[c][e] + log2f(L[c][e])) * 0.6931471805599453f : -INFINITY;
-        }
+        for (int i = 0; i < MT; i += 4)
+          *reinterpret_cast<uint4*>(dst + 2 * i) =
+              make_uint4(pack_bf16x2(O[i][c][e], O[i][c][e + 2]), pack_bf16x2(O[i + 1][c][e], O[i + 1][c][e + 2]),
+                         pack_bf16x2(O[i + 2][c][e], O[i + 2][c][e + 2]), pack_bf16x2(O[i + 3][c][e], O[i + 3][c][e + 2]));
       }
-  }
-  w += count;
-  at0 += count;
-  tile = 0;
-  if (++kh == M.Hkv) {
-    kh = 0;
-    do ++r; while (w < w1 && stream_of(p, r).tiles == 0);
-  }
-  }
+      if (g == 0 && p.lse) p.lse[orow] = L[c][e] != 0.f ? (top[c][e] + log2f(L[c][e])) * 0.6931471805599453f : -INFINITY;
+    }
 }
 
 template <int D, int NT>
 cudaError_t launch(const PackedAttnParams& p, cudaStream_t s) {
   constexpr int NS = slots_of(NT);
-  constexpr int SMEM = NS * kSlotBytes<D> + 3 * D * NT * 32 + NT * D * 16 + 32 * NT + NW * 64 * NT + 16 * NS + 8 * (3 + kThreads / 32);
+  constexpr int SMEM = NS * kSlotBytes<D> + 3 * D * NT * 32 + NT * D * 16 + 32 * NT + NW * 64 * NT + 16 * NS + 16;
   auto kern = packed_decode_kernel<D, NT>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
   if (e != cudaSuccess) return e;
-  kern<<<p.runs > 0 ? p.runs : p.b.B * p.m.Hkv, kThreads, SMEM, s>>>(p);
-  if ((e = cudaGetLastError()) != cudaSuccess || p.runs == 0) return e;
-  return hswa_launch_packed_join(p, 8 * NT, s);
+  kern<<<p.b.B * p.m.Hkv, kThreads, SMEM, s>>>(p);
+  return cudaGetLastError();
 }
 
 }  // namespace
-
-int hswa_packed_decode_blocks_per_sm(int rows) { return rows <= 16 ? 2 : 1; }
 
 cudaError_t hswa_launch_packed_decode(const PackedAttnParams& p, int rows, cudaStream_t s) {
   if (p.m.D == 128) return rows == 8 ? launch<128, 1>(p, s) : rows == 16 ? launch<128, 2>(p, s) : launch<128, 4>(p, s);

@@ -378,17 +378,20 @@ __global__ void __launch_bounds__(kThreads, 2) packed_stream_kernel(const Packed
   }
 }
 
-// Joins the pieces of the streams that several blocks had: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.  A block per
-// stream and row, its eight warps take every eighth piece.
-template <int D>
+// Joins the pieces of the streams that several warps or blocks had: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
+// WPR = 1: a warp per row, eight rows of a stream per block, for streams in few pieces; 8: the eight warps of a block take every
+// eighth piece of one row.  (32 requests of 4 tokens and 600 to 1500 keys, 64 / 8 heads, two or three pieces a stream: 30 us with eight
+// warps per row, most of whose blocks found nothing to do but to read where the runs begin.)
+template <int D, int TILE, int WPR>
 __global__ void __launch_bounds__(256) packed_join_kernel(const PackedAttnParams p, const int cols) {
   const ModelParams& M = p.m;
-  const int r = blockIdx.x / M.Hkv, kh = blockIdx.x % M.Hkv, col = blockIdx.y;
+  const int r = blockIdx.x / M.Hkv, kh = blockIdx.x % M.Hkv;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const Stream s = stream_of(p, r);
+  const int col = WPR == 1 ? blockIdx.y * 8 + warp : blockIdx.y, sub = WPR == 1 ? 0 : warp;
+  const Stream s = stream_of<TILE>(p, r);
   asm volatile("griddepcontrol.wait;" ::: "memory");  // launched early behind the kernel that writes the pieces
-  if (s.tiles == 0 || col >= s.n * M.G) return;
   const int64_t total = p.before[p.b.B] * M.Hkv, start = p.before[r] * M.Hkv + (int64_t)kh * s.tiles;
+  if (s.tiles == 0 || col >= s.n * M.G) return;
   // run c holds tile x: c = ceil((x + 1) runs / total) - 1
   const int c0 = (int)(((start + 1) * p.runs - 1) / total), c1 = (int)(((start + s.tiles) * p.runs - 1) / total);
   const int tok = col / M.G;
@@ -408,7 +411,7 @@ __global__ void __launch_bounds__(256) packed_join_kernel(const PackedAttnParams
   constexpr int PER = D / 32;
   float acc[PER] = {}, L = 0.f;
 #pragma unroll 4
-  for (int c = c0 + warp; c <= c1; c += 8) {
+  for (int c = c0 + sub; c <= c1; c += WPR) {
     const float2 v = ml_of(c);
     const float f = v.y != 0.f ? fast_exp2(v.x == -INFINITY ? 0.f : v.x - mm) : 0.f;  // (l of NaN scores: m says nothing)
     const float* o = p.part_o + piece_of(c) * D + lane * PER;
@@ -420,19 +423,21 @@ __global__ void __launch_bounds__(256) packed_join_kernel(const PackedAttnParams
       acc[i + 1] += v.y != 0.f ? f * x.y : 0.f;
     }
   }
-  __shared__ float sums[7][32][PER + 1];
-  if (warp > 0) {
+  if constexpr (WPR > 1) {
+    __shared__ float sums[7][32][PER + 1];
+    if (warp > 0) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) sums[warp - 1][lane][i] = acc[i];
-    sums[warp - 1][lane][PER] = L;
-  }
-  __syncthreads();
-  if (warp > 0) return;
+      for (int i = 0; i < PER; ++i) sums[warp - 1][lane][i] = acc[i];
+      sums[warp - 1][lane][PER] = L;
+    }
+    __syncthreads();
+    if (warp > 0) return;
 #pragma unroll
-  for (int k = 0; k < 7; ++k) {
+    for (int k = 0; k < 7; ++k) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) acc[i] += sums[k][lane][i];
-    L += sums[k][lane][PER];
+      for (int i = 0; i < PER; ++i) acc[i] += sums[k][lane][i];
+      L += sums[k][lane][PER];
+    }
   }
   const float inv = L != 0.f ? 1.f / L : 0.f;
   const int64_t orow = (int64_t)(s.t0 + tok) * M.Hq + kh * M.G + col % M.G;
@@ -466,12 +471,15 @@ int hswa_packed_stream_runs_per_sm() { return 2 * NW; }
 
 cudaError_t hswa_launch_packed_stream(const PackedAttnParams& p, cudaStream_t s) {
   const cudaError_t e = p.m.D == 128 ? launch<128>(p, s) : launch<64>(p, s);
-  return e != cudaSuccess ? e : hswa_launch_packed_join(p, 8, s);
+  return e != cudaSuccess ? e : hswa_launch_packed_join(p, 8, TK, s);
 }
 
-cudaError_t hswa_launch_packed_join(const PackedAttnParams& p, int cols, cudaStream_t s) {
+template <int D, int TILE>
+static cudaError_t launch_join(const PackedAttnParams& p, int cols, cudaStream_t s) {
+  const int streams = p.b.B * p.m.Hkv, rows = p.max_q_len * p.m.G;
+  const bool few = p.runs <= 8LL * streams;  // pieces of a stream, on the average
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.b.B * p.m.Hkv, p.max_q_len * p.m.G, 1);
+  cfg.gridDim = dim3(streams, few ? (rows + 7) / 8 : rows, 1);
   cfg.blockDim = dim3(256, 1, 1);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -479,5 +487,9 @@ cudaError_t hswa_launch_packed_join(const PackedAttnParams& p, int cols, cudaStr
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return p.m.D == 128 ? cudaLaunchKernelEx(&cfg, packed_join_kernel<128>, p, cols) : cudaLaunchKernelEx(&cfg, packed_join_kernel<64>, p, cols);
+  return few ? cudaLaunchKernelEx(&cfg, packed_join_kernel<D, TILE, 1>, p, cols) : cudaLaunchKernelEx(&cfg, packed_join_kernel<D, TILE, 8>, p, cols);
+}
+cudaError_t hswa_launch_packed_join(const PackedAttnParams& p, int cols, int tile, cudaStream_t s) {
+  if (tile == TK) return p.m.D == 128 ? launch_join<128, TK>(p, cols, s) : launch_join<64, TK>(p, cols, s);
+  return p.m.D == 128 ? launch_join<128, 128>(p, cols, s) : launch_join<64, 128>(p, cols, s);
 }

@@ -5,7 +5,7 @@
 
 namespace hswa_dev {
 
-constexpr int kStreamTile = 64;  // keys per tile
+constexpr int kStreamTile = 64;  // keys per tile of the warp-level kernels
 
 // Keys of a 16-key group in the order of the fragments' rows: row i of the first half holds key kKey(i), row 8 + i key 8 +
 // kKey(i).  (A lane's V rows are kKey(2t), kKey(2t + 1): this order has lanes t = 0 .. 3 on rows 0, 3, 4, 7 and 1, 2, 5, 6,
@@ -16,6 +16,7 @@ __device__ __forceinline__ int key_of(int i) { return (i & 4) | ((i & 2) ? 3 - (
 struct Stream {
   int t0, n, len, end, tiles;
 };
+template <int TILE = kStreamTile>
 __device__ __forceinline__ Stream stream_of(const PackedAttnParams& p, int r) {
   Stream s;
   s.t0 = p.b.q_indptr ? p.b.q_indptr[r] : r;
@@ -23,7 +24,7 @@ __device__ __forceinline__ Stream stream_of(const PackedAttnParams& p, int r) {
   s.len = max(0, min(p.b.ctx_len[r], p.max_ctx_len));
   const int64_t room = (int64_t)p.b.max_blocks * p.m.P;  // positions that the block table has places for
   s.end = (int)min((int64_t)(p.causal ? s.len + s.n : s.len), room);
-  s.tiles = s.n > 0 ? max(1, (s.end + kStreamTile - 1) / kStreamTile) : 0;
+  s.tiles = s.n > 0 ? max(1, (s.end + TILE - 1) / TILE) : 0;
   return s;
 }
 // First tile of run c of `runs` over `total` tiles.
@@ -31,13 +32,13 @@ __device__ __forceinline__ int64_t run_start(int64_t total, int c, int runs) { r
 
 // The requests' tiles summed by a block of THREADS threads: all tiles of one KV head, and this thread's first request i0, last i1
 // and the tiles before i0.  s_sums: [THREADS / 32].
-template <int THREADS>
+template <int THREADS, int TILE = kStreamTile>
 __device__ __forceinline__ int64_t sum_tiles(const PackedAttnParams& p, int64_t* s_sums, int* i0, int* i1, int64_t* before) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, B = p.b.B, per = (B + THREADS - 1) / THREADS;
   *i0 = min((int)threadIdx.x * per, B);
   *i1 = min(*i0 + per, B);
   int64_t mine = 0;
-  for (int i = *i0; i < *i1; ++i) mine += stream_of(p, i).tiles;
+  for (int i = *i0; i < *i1; ++i) mine += stream_of<TILE>(p, i).tiles;
   int64_t incl = mine;
 #pragma unroll
   for (int sh = 1; sh < 32; sh <<= 1) {

@@ -234,6 +234,132 @@ def test_offsets_past_32_bits_and_rows_left_alone():
     check(c, out[:T].double().cpu().numpy(), lse[:T].double().cpu().numpy())
 
 
+# ---- contexts past what a block takes as a whole ----
+LONG = [2500, 0, 1, 2240, 130, 4005]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("rows", [8, 16, 32])
+@pytest.mark.parametrize("d", SHAPES)
+def test_long_contexts(d, rows, causal):
+    """As many tokens as make up to 8, 16 and 32 rows for a KV head; some requests shorter by a token, one without any."""
+    n = max(1, rows // (d.num_q_heads // d.num_kv_heads))
+    c = Case(d, LONG, [n, n, max(1, n - 1), n, 0, n], seed=30 + rows, causal=causal, v_scale=3.0)
+    check(c, *run(c))
+
+
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", SHAPES)
+def test_long_single_tokens(d, out_dtype):
+    """Without row offsets; a table with places to spare, a bound far above the lengths."""
+    c = Case(d, [2113, 3000, 64, 0], [1] * 4, seed=31, spare_blocks=300, k_scale=0.046875)
+    check(c, *run(c, out_dtype), out_dtype)
+    check(c, *run(c, out_dtype, max_ctx=3000 + 100 * d.page_size), out_dtype)
+
+
+@pytest.mark.parametrize("d,n", [(dims(1, 64, 16, 1), 1), (dims(8, 128, 64, 1), 2), (dims(8, 64, 32, 1), 4), (dims(3, 128, 16, 1), 3)])
+def test_many_requests_of_all_lengths(d, n):
+    """More streams than SMs, most of them short: runs that begin and end in the middle of streams, and hold several."""
+    rng = np.random.default_rng(32)
+    B = 170
+    ctx = [int(x) for x in rng.integers(0, 400, B)]
+    ctx[3], ctx[77], ctx[B - 1] = 2600, 0, 2301
+    c = Case(d, ctx, [n if r % 5 else r % (n + 1) for r in range(B)], seed=33)
+    check(c, *run(c, single=False))
+
+
+@pytest.mark.parametrize("n", [1, 2, 4])
+def test_one_long_request(n):
+    """A stream in many pieces."""
+    c = Case(dims(8, 128, 64, 1), [20011], [n], seed=34)
+    check(c, *run(c, single=False))
+
+
+@pytest.mark.parametrize("n", [1, 2, 4])
+def test_long_rows_of_nan_and_unlike_magnitudes(n):
+    """A NaN stays in its row; a row 2^20 times smaller than its neighbour keeps its own maxima and sums."""
+    c = Case(dims(8, 128, 64, 2), [2400, 300], [n, n], seed=35)
+    q = c.q.copy()
+    q[n - 1, 5, 3] = 0x7FC0
+    q[0, 9] = to_host_bits(torch.from_numpy(wl.bits_to_f64(c.q[0, 9]) * 2.0 ** -20).to(torch.bfloat16))
+    c.q[0, 9] = q[0, 9]
+    out, lse = run(c, q=q, single=False)
+    assert np.isnan(out[n - 1, 5]).all() and np.isnan(lse[n - 1, 5])
+    out[n - 1, 5], lse[n - 1, 5] = c.want()[0][n - 1, 5], c.want()[1][n - 1, 5]
+    check(c, out, lse)
+
+
+@pytest.mark.parametrize("sm_scale", [1.0, 3.0])
+@pytest.mark.parametrize("n", [1, 3, 8])
+def test_long_peaked_rows(n, sm_scale):
+    """As test_peaked_rows_and_growing_maxima."""
+    c = Case(dims(4, 64, 32), [3500, 130], [n, n], seed=36)
+    h = make_handle(c.d, torch.float32, sm_scale=sm_scale)
+    out, lse = run(c, h=h, single=False)
+    want, want_lse, tol = c.want(sm_scale)
+    more = S_ERR * 8 * sm_scale
+    assert (np.abs(out - want) <= tol + 2 * more * np.abs(np.concatenate([v for _, v in c.kv])).max()).all()
+    assert (np.abs(lse - want_lse) <= more).all()
+
+
+@pytest.mark.parametrize("n", [1, 2, 4])
+def test_long_contexts_record_values_out_of_range(n):
+    """What the bounds do not cover is recorded and left alone; the other requests' rows are computed."""
+    d = dims(8, 64, 16, 1)
+    c = Case(d, [2300, 40, 2200], [n, n, n], seed=37)
+    good = run(c, single=False)
+    h = make_handle(d, torch.float32)
+
+    def record(ctx=None, indptr=None, table=None, max_q=n, total=3 * n):
+        b = hb.Batch(dev_i32(c.ctx if ctx is None else ctx), dev_i32(c.table if table is None else table), *no_rings(d, 3),
+                     dev_i32(c.indptr if indptr is None else indptr), max_q_len=max_q, total_q=total, max_ctx_len=2300)
+        out, lse = torch.full((3 * n, 8, 64), 7.0, device="cuda"), torch.full((3 * n, 8), 7.0, device="cuda")
+        hb.hswa_packed_attn(h, c.layer(), b, True, to_dev_bf16(c.q), out, lse, workspace(h, b, True))
+        return hb.hswa_get_async_error(h), out.double().cpu().numpy(), lse.double().cpu().numpy()
+
+    table = c.table.copy()
+    table[1, 1] = 1 << 20
+    st, out, _ = record(table=table)
+    assert st[:4] == (hb.HSWA_ERR_BOUNDS, 1, 1, 1 << 20), st
+    assert np.array_equal(out[:n], good[0][:n]) or np.abs(out[:n] - good[0][:n]).max() < 1e-2
+    for bad in (-1, 2301):
+        st, out, _ = record(ctx=[2300, bad, 2200])
+        assert st[:4] == (hb.HSWA_ERR_BOUNDS, 1, -1, bad), st
+        assert np.abs(out[2 * n:] - good[0][2 * n:]).max() < 1e-2  # (other runs, other roundings)
+    if n > 1:
+        st, out, lse = record(indptr=np.array([0, n - 1, 2 * n, 3 * n], np.int32))
+        assert st[:4] == (hb.HSWA_ERR_BOUNDS, 1, -2, n + 1), st
+        assert (out[2 * n - 1] == 7).all() and (lse[2 * n - 1] == 7).all()
+    for indptr in ([0, n, 2 * n, 3 * n + 1], [-1, n, 2 * n, 3 * n]):
+        st, _, _ = record(indptr=np.array(indptr, np.int32), max_q=n + 1 if n > 1 else 1)
+        assert (st[0], st[2]) == (hb.HSWA_ERR_BOUNDS, -2), st
+
+
+@pytest.mark.parametrize("n", [1, 4])
+def test_long_calls_captured_and_repeated(n):
+    """A captured call replayed on other data, twice: bit for bit what the call itself gives."""
+    c, other = (Case(dims(8, 128, 64, 2), [2600, 900], [n, n], seed=s) for s in (38, 39))
+    h = make_handle(c.d, torch.float32)
+    b, layer, q = c.batch(single=False), c.layer(), to_dev_bf16(c.q)
+    T = int(c.indptr[-1])
+    out, lse, ws = torch.empty((T, 16, 128), device="cuda"), torch.empty((T, 16), device="cuda"), workspace(h, b, True)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hb.hswa_packed_attn(h, layer, b, True, q, out, lse, ws)
+    layer.pool.copy_(torch.from_numpy(other.pool).cuda())
+    q.copy_(to_dev_bf16(other.q))
+    b.block_table.copy_(dev_i32(other.table))
+    seen = []
+    for _ in range(2):
+        out.fill_(7.0)
+        ws.fill_(255)
+        graph.replay()
+        no_error(h)
+        seen.append(out.double().cpu().numpy())
+        check(other, seen[-1], lse.double().cpu().numpy())
+    assert np.array_equal(*seen)
+
+
 # ---- rows in and out --------------------------------------------------------------------------------------------------
 def codes_of(pool, table, ctx, n, P, D):
     return [[ref.rows(pool, table, r, int(ctx[r] + n[r]), which, P, D, 1.0)[ctx[r]:] for which in (0, 1)] for r in range(len(ctx))]
@@ -345,8 +471,8 @@ def test_refusals():
             assert status(hb.hswa_packed_attn, hb.PackedLayer(layer.pool, *scales), b, True, q, out, None, ws) == hb.HSWA_ERR_INVALID_ARG
             assert status(hb.hswa_packed_append, hb.PackedLayer(layer.pool, *scales), b, k, k) == hb.HSWA_ERR_INVALID_ARG
     assert status(hb.hswa_packed_attn, layer, c.batch(max_ctx=1 << 20), True, q, out, None, ws) == hb.HSWA_ERR_INVALID_ARG  # table too small
-    long = Case(dims(2, 64, 16, 1), [2000], [2], seed=13)
-    need = hb.hswa_packed_workspace_need(h, 1, 2, 2, 2000, True)
+    long = Case(dims(2, 64, 16, 1), [5000], [2], seed=13)
+    need = hb.hswa_packed_workspace_need(h, 1, 2, 2, 5000, True)
     assert need > 0 and need % 256 == 0
     for w in (None, torch.empty((need - 256,), dtype=torch.uint8, device="cuda"), torch.empty((need + 16,), dtype=torch.uint8, device="cuda")[16:]):
         assert status(hb.hswa_packed_attn, long.layer(), long.batch(), True, q, out, None, w) == hb.HSWA_ERR_WORKSPACE
