@@ -215,6 +215,7 @@ class Handle:
                                1 if out_dtype == torch.float32 else 0)
         self.out_dtype = out_dtype
         _check(load().hswa_create(C.byref(self.cfg), C.byref(self._h)), "hswa_create")
+        self.packed_rows = (num_kv_heads, page_size * (head_dim // 2 + head_dim // 16))  # of a 4-bit pool: KV heads, bytes of a slab
         self.ring_pages = ring_pages or (-(-window // page_size) + 1)
 
     def close(self):
@@ -233,6 +234,12 @@ class Handle:
         return self._h
 
 
+def _pages_of(pool: torch.Tensor):
+    """Where a pool's pages lie, their number and bytes."""
+    n = int(pool.shape[0])
+    return pool.data_ptr(), n, pool.numel() // n * pool.element_size() if n else 0
+
+
 class Layer:
     """One layer's pool: bf16 CUDA tensor [num_pages][2][Hkv][P][D]."""
 
@@ -241,6 +248,7 @@ class Layer:
         self.pool = pool
         self.device = pool.get_device()
         self.is_swa = bool(is_swa)
+        self.pages = _pages_of(pool)
         self.c = hswa_layer(pool.data_ptr(), pool.shape[0], int(self.is_swa))
         self.ref = C.byref(self.c)
 
@@ -252,6 +260,8 @@ class PackedLayer:
         _need(pool.dtype == torch.uint8 and pool.dim() == 4 and pool.shape[1] == 2 and pool.is_contiguous())
         self.pool = pool
         self.device = pool.get_device()
+        self.rows = tuple(pool.shape[2:])  # KV heads, bytes of a slab
+        self.pages = _pages_of(pool)
         self.c = hswa_packed_layer(pool.data_ptr(), pool.shape[0], k_scale, v_scale)
         self.ref = C.byref(self.c)
 
@@ -457,17 +467,26 @@ def hswa_evict_compact(h: Handle, layer: Layer, batch: Batch, keep_idx: torch.Te
 
 
 def _packed_device_of(h: Handle, layer: PackedLayer, batch: Batch) -> int:
-    c = h.cfg
-    slab = c.page_size * (c.head_dim // 2 + c.head_dim // 16)
-    _need(tuple(layer.pool.shape[2:]) == (c.num_kv_heads, slab), "4-bit pool of another head count, head dim or page size than the handle's")
+    _need(layer.rows == h.packed_rows, "4-bit pool of another head count, head dim or page size than the handle's")
     return _device_of(layer, batch)
 
 
 def _packed_rows(call, what, h: Handle, layer: PackedLayer, batch: Batch, k: torch.Tensor, v: torch.Tensor):
-    n = batch.total_q * h.cfg.num_kv_heads * h.cfg.head_dim
+    n = batch.total_q * h.packed_rows[0] * h.cfg.head_dim
     _need(k.dtype == v.dtype == torch.bfloat16 and k.numel() >= n and v.numel() >= n, "k and v: bf16, total_q rows")
     dev = _packed_device_of(h, layer, batch)
-    _check(call(h.ptr, layer.ref, batch.ref, *_ptrs(dev, k, v), _raw_stream(dev)), what)
+    k_at, v_at = _ptrs(dev, k, v)
+    _check(call(h.ptr, layer.ref, batch.ref, k_at, v_at, _raw_stream(dev)), what)
+
+
+def _int_ptrs(dev: int, *tensors):
+    """_ptrs of int32 tensors."""
+    at, i32 = [], torch.int32
+    for t in tensors:
+        if t.dtype != i32 or t.get_device() != dev or not t.is_contiguous():
+            raise AssertionError("device tensors must be contiguous int32 CUDA tensors on the current device")
+        at.append(t.data_ptr())
+    return at
 
 
 def hswa_packed_append(h: Handle, layer: PackedLayer, batch: Batch, k_new: torch.Tensor, v_new: torch.Tensor):
@@ -504,45 +523,50 @@ def hswa_pages_workspace_need(h: Handle, num_pages: int) -> int:
 
 def hswa_pages_fork(h: Handle, ref, ref_out, table, held, parent, length, need, table_out, held_out, copy_src, copy_dst, workspace):
     """Block tables of a step's rows from their parents': int32 CUDA tensors, ref [num_pages], table [rows][blocks], the others [rows]."""
-    ints = (ref, ref_out, table, held, parent, length, need, table_out, held_out, copy_src, copy_dst)
-    _need(all(t.dtype == torch.int32 for t in ints) and ref_out.numel() == ref.numel())
     rows_in, blocks = table.shape
     rows_out, out_blocks = table_out.shape
-    _need(held.numel() >= rows_in and all(t.numel() >= rows_out for t in (parent, length, need, held_out, copy_src, copy_dst)),
+    pages = ref.numel()
+    _need(ref_out.numel() == pages)
+    _need(held.numel() >= rows_in and min(parent.numel(), length.numel(), need.numel(), held_out.numel(), copy_src.numel(), copy_dst.numel()) >= rows_out,
           "fewer entries than rows")
     dev = _device()
-    (ref_at, ref_out_at, table_at, held_at, parent_at, len_at, need_at, table_out_at, held_out_at, src_at, dst_at, ws_at) = _ptrs(
-        dev, *ints, workspace)
-    _check(load().hswa_pages_fork(h.ptr, ref.numel(), ref_at, ref_out_at, rows_in, held_at, table_at, blocks, rows_out, parent_at, len_at,
-                                  need_at, table_out_at, out_blocks, held_out_at, src_at, dst_at, ws_at,
-                                  workspace.numel() * workspace.element_size(), _raw_stream(dev)), "hswa_pages_fork")
+    ref_at, ref_out_at, held_at, table_at, *rest = _int_ptrs(dev, ref, ref_out, held, table, parent, length, need, table_out, held_out, copy_src, copy_dst)
+    parent_at, len_at, need_at, table_out_at, held_out_at, src_at, dst_at = rest
+    ws_at, = _ptrs(dev, workspace)
+    _check(load().hswa_pages_fork(h.ptr, pages, ref_at, ref_out_at, rows_in, held_at, table_at, blocks, rows_out, parent_at, len_at, need_at,
+                                  table_out_at, out_blocks, held_out_at, src_at, dst_at, ws_at, workspace.numel() * workspace.element_size(),
+                                  _raw_stream(dev)), "hswa_pages_fork")
 
 
 def hswa_pages_compact(h: Handle, ref, ref_out, table, held, table_out, page_map, move_src, move_dst):
     """Moves of live pages into the lowest free ones, as many as move_src has places: int32 CUDA tensors."""
-    ints = (ref, ref_out, table, held, table_out, page_map, move_src, move_dst)
-    _need(all(t.dtype == torch.int32 for t in ints) and ref_out.numel() == page_map.numel() == ref.numel())
     rows, blocks = table.shape
-    _need(table_out.shape == table.shape and held.numel() >= rows and move_src.numel() == move_dst.numel())
+    pages, moves = ref.numel(), move_src.numel()
+    _need(ref_out.numel() == page_map.numel() == pages and table_out.shape == table.shape and held.numel() >= rows and move_dst.numel() == moves)
     dev = _device()
-    ref_at, ref_out_at, table_at, held_at, table_out_at, map_at, src_at, dst_at = _ptrs(dev, *ints)
-    _check(load().hswa_pages_compact(h.ptr, ref.numel(), ref_at, ref_out_at, rows, held_at, table_at, blocks, table_out_at, map_at,
-                                     move_src.numel(), src_at, dst_at, _raw_stream(dev)), "hswa_pages_compact")
+    ref_at, ref_out_at, held_at, table_at, table_out_at, map_at, src_at, dst_at = _int_ptrs(
+        dev, ref, ref_out, held, table, table_out, page_map, move_src, move_dst)
+    _check(load().hswa_pages_compact(h.ptr, pages, ref_at, ref_out_at, rows, held_at, table_at, blocks, table_out_at, map_at, moves, src_at,
+                                     dst_at, _raw_stream(dev)), "hswa_pages_compact")
 
 
 def hswa_pages_copy(h: Handle, layers, src: torch.Tensor, dst: torch.Tensor):
     """layers: Layer or PackedLayer objects of one kind and size, any number of them; pairs of page ids, -1 where there is none."""
-    _need(src.dtype == dst.dtype == torch.int32 and src.numel() == dst.numel())
+    pairs = src.numel()
+    _need(src.dtype == dst.dtype == torch.int32 and dst.numel() == pairs)
     if not layers:
         return
-    first = layers[0].pool
-    _need(all(x.pool.shape == first.shape and x.pool.dtype == first.dtype for x in layers), "pools of different sizes")
     dev = _device()
-    _need(all(x.device == dev for x in layers), "layer on another device than the current one")
+    _, num_pages, page_bytes = layers[0].pages
+    pools = (C.c_void_p * len(layers))()
+    for i, x in enumerate(layers):
+        pools[i], n, size = x.pages
+        if n != num_pages or size != page_bytes:
+            raise AssertionError("pools of different sizes")
+        if x.device != dev:
+            raise AssertionError("layer on another device than the current one")
     src_at, dst_at = _ptrs(dev, src, dst)
-    pools = (C.c_void_p * len(layers))(*[x.c.pool for x in layers])
-    _check(load().hswa_pages_copy(h.ptr, len(layers), pools, first.shape[0], first.stride(0) * first.element_size(), src.numel(), src_at,
-                                  dst_at, _raw_stream(dev)), "hswa_pages_copy")
+    _check(load().hswa_pages_copy(h.ptr, len(layers), pools, num_pages, page_bytes, pairs, src_at, dst_at, _raw_stream(dev)), "hswa_pages_copy")
 
 
 def hswa_window_safe_len(match_len: int, window: int, swa_valid) -> int:

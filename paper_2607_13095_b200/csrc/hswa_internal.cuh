@@ -238,6 +238,23 @@ cudaError_t hswa_launch_read_probe(const void* buf, size_t bytes, int num_sms, i
 cudaError_t hswa_launch_wait_selftest(int64_t limit_clocks, int32_t* err, cudaStream_t s);
 
 #ifdef __CUDACC__
+#include <atomic>
+
+// Sets a kernel's limit of dynamic shared memory (and, with `wide`, allows clusters of 16) once per device.
+template <auto Kernel>
+cudaError_t hswa_prepare_kernel(int smem_bytes, bool wide = false) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  if (wide) e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
 namespace hswa_dev {
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }

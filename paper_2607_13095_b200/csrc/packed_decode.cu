@@ -420,10 +420,9 @@ template <int D, int NT>
 cudaError_t launch(const PackedAttnParams& p, cudaStream_t s) {
   constexpr int NS = slots_of(NT);
   constexpr int SMEM = NS * kSlotBytes<D> + 3 * D * NT * 32 + NT * D * 16 + 32 * NT + NW * 64 * NT + 16 * NS + 16;
-  auto kern = packed_decode_kernel<D, NT>;
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+  const cudaError_t e = hswa_prepare_kernel<packed_decode_kernel<D, NT>>(SMEM);
   if (e != cudaSuccess) return e;
-  kern<<<p.b.B * p.m.Hkv, kThreads, SMEM, s>>>(p);
+  packed_decode_kernel<D, NT><<<p.b.B * p.m.Hkv, kThreads, SMEM, s>>>(p);
   return cudaGetLastError();
 }
 

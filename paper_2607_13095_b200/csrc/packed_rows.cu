@@ -724,7 +724,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const PackedAt
 template <int D, int N>
 cudaError_t launch(const PackedAttnParams& p, cudaStream_t s) {
   auto kern = packed_rows_kernel<D, N>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D, N>::BYTES);
+  cudaError_t e = hswa_prepare_kernel<packed_rows_kernel<D, N>>(Smem<D, N>::BYTES);
   if (e != cudaSuccess) return e;
   // the softmax warps' request for registers is granted only if the launch gives the block 640 x 96
   static const cudaError_t budget = [&] {

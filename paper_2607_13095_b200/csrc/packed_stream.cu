@@ -454,10 +454,9 @@ __global__ void __launch_bounds__(256) packed_join_kernel(const PackedAttnParams
 
 template <int D, int PAGE>
 cudaError_t launch(const PackedAttnParams& p, cudaStream_t s) {
-  auto kern = packed_stream_kernel<D, PAGE>;
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::SMEM);
+  const cudaError_t e = hswa_prepare_kernel<packed_stream_kernel<D, PAGE>>(Cfg<D>::SMEM);
   if (e != cudaSuccess) return e;
-  kern<<<(p.runs + NW - 1) / NW, kThreads, Cfg<D>::SMEM, s>>>(p);
+  packed_stream_kernel<D, PAGE><<<(p.runs + NW - 1) / NW, kThreads, Cfg<D>::SMEM, s>>>(p);
   return cudaGetLastError();
 }
 template <int D>

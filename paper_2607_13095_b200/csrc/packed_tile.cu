@@ -495,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_tile_kernel(const PackedAt
 template <int D>
 cudaError_t launch(const PackedAttnParams& p, cudaStream_t s) {
   auto kern = packed_tile_kernel<D>;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  const cudaError_t e = hswa_prepare_kernel<packed_tile_kernel<D>>(kSmem);
   if (e != cudaSuccess) return e;
   // the softmax warps' request for registers is granted only if the launch gives the block 512 x 128
   static const cudaError_t budget = [&] {

@@ -492,10 +492,11 @@ __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const PagesCop
     if (from + (int64_t)i * kCopyThreads * 16 < p.page_bytes) d[i * kCopyThreads] = v[i];
 }
 
-template <typename Kernel, typename Params>
-cudaError_t launch_cluster(Kernel kern, const Params& p, size_t smem, cudaStream_t s) {
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+template <auto Kernel, typename Params>
+cudaError_t launch_cluster(const Params& p, size_t smem, cudaStream_t s) {
+  constexpr int most = kMaxPageRows * 7 * 4 + (kMaxPages / 32 / kBlocks) * 4;  // what the largest call needs
+  static_assert(most <= 227 * 1024 - 1024, "rows and bitmap fit a block's shared memory");
+  const cudaError_t e = hswa_prepare_kernel<Kernel>(most, true);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(kBlocks, 1, 1);
@@ -511,7 +512,7 @@ cudaError_t launch_cluster(Kernel kern, const Params& p, size_t smem, cudaStream
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = p.copied ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kern, p);
+  return cudaLaunchKernelEx(&cfg, Kernel, p);
 }
 
 // The second launch of all SMs, early behind the cluster.
@@ -542,7 +543,7 @@ cudaError_t hswa_launch_pages_fork(const PagesForkParams& params, int num_sms, c
   p.second = (int64_t)p.rows_in * p.max_blocks + (int64_t)p.rows_out * p.out_max_blocks > kSmallTables;
   p.copied = p.num_pages > kSmallPool;
   if (p.copied) pages_copy_counts_kernel<<<4 * num_sms, kWideThreads, 0, s>>>(p.ref, p.ref_out, nullptr, p.num_pages);
-  const cudaError_t e = launch_cluster(pages_fork_kernel, p, ((size_t)p.rows_in * 3 + (size_t)p.rows_out * 4) * 4 + bitmap_bytes(p.num_pages), s);
+  const cudaError_t e = launch_cluster<pages_fork_kernel>(p, ((size_t)p.rows_in * 3 + (size_t)p.rows_out * 4) * 4 + bitmap_bytes(p.num_pages), s);
   return e != cudaSuccess || !p.second ? e : launch_wide(pages_fork_apply_kernel, p, num_sms, s);
 }
 cudaError_t hswa_launch_pages_compact(const PagesCompactParams& params, int num_sms, cudaStream_t s) {
@@ -550,7 +551,7 @@ cudaError_t hswa_launch_pages_compact(const PagesCompactParams& params, int num_
   p.second = (int64_t)p.rows * p.max_blocks > kSmallTables;
   p.copied = p.num_pages > kSmallPool;
   if (p.copied) pages_copy_counts_kernel<<<4 * num_sms, kWideThreads, 0, s>>>(p.ref, p.ref_out, p.page_map, p.num_pages);
-  const cudaError_t e = launch_cluster(pages_compact_kernel, p, bitmap_bytes(p.num_pages), s);
+  const cudaError_t e = launch_cluster<pages_compact_kernel>(p, bitmap_bytes(p.num_pages), s);
   return e != cudaSuccess || !p.second ? e : launch_wide(pages_compact_apply_kernel, p, num_sms, s);
 }
 cudaError_t hswa_launch_pages_copy(const PagesCopyParams& p, cudaStream_t s) {
