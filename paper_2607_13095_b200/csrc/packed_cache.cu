@@ -1,27 +1,32 @@
-// Rows into and out of a 4-bit cache (hswa_packed_append, hswa_packed_read): one thread per block of 16 elements.
+// Rows into and out of a 4-bit cache (hswa_packed_append, hswa_packed_read): two neighbouring lanes per block of 16 elements, so that
+// a warp's 16-byte loads and stores follow one another.
 //
 // A block of 16 elements x with largest magnitude a, in a layer of scale g, is held as f = e4m3((a / g) / 6), s = f g, and
-// e2m1(x / s): both roundings to the nearest, ties to the even code, at most 448 and 6.  x / s lies halfway between two levels
-// often (both have few bits), so the quotient has to be right to the last bit: a product with 1 / s, then one Newton step on
-// its exact residual.
-// Bound by HBM: 2 bytes per element read, 0.5625 written (read-back: the reverse).
+// e2m1(x / s): both roundings to the nearest, ties to the even code, at most 448 and 6.  Quotients lie halfway between two codes
+// often (dividend and divisor have few bits), so they have to be right to the last bit: a product with the inverse, then one
+// Newton step on its exact residual, which makes every quotient exact that fits 24 bits.  (Divisions took the append from 59
+// to 79 us, once two lanes share a block.)
+// Bound by HBM: 2 bytes per element read, 0.5625 written (read-back: the reverse).  A block takes some tokens: it looks up where
+// their rows are held (a chain of dependent loads) once, and then moves their elements with several loads in flight; a thread that
+// looked up its own row was at half the rate.
 #include "packed.cuh"
 
 namespace {
 using namespace hswa_dev;
 
 constexpr int kThreads = 256;
+constexpr int kTokens = 32;  // of a block, at most
+constexpr int kAtOnce = 4;   // items that a thread has in flight
 
 struct RowAt {
-  int64_t slab;  // byte offset of the row's slab for K; V is Hkv slabs further on
+  int64_t page;  // byte offset of the row's page; -1: not to be moved
   int slot;
-  bool ok;
 };
 
 // Where the row of token `tok` (of all requests' tokens) is held; records what is out of range.
-__device__ __forceinline__ RowAt find_row(const PackedCacheParams& p, int tok, int kh) {
+__device__ __forceinline__ RowAt find_row(const PackedCacheParams& p, int tok) {
   const ModelParams& M = p.m;
-  RowAt at = {0, 0, false};
+  RowAt at = {-1, 0};
   int r = tok, i = 0;
   if (p.b.q_indptr) {
     if (tok < p.b.q_indptr[0]) return at;
@@ -54,116 +59,167 @@ __device__ __forceinline__ RowAt find_row(const PackedCacheParams& p, int tok, i
     record_error(p.err, HSWA_ERR_BOUNDS, r, block, page);
     return at;
   }
-  const int slab = M.P * (M.D / 2 + M.D / 16);
-  at.slab = ((int64_t)page * 2 * M.Hkv + kh) * slab;
+  at.page = (int64_t)page * 2 * M.Hkv * (M.P * (M.D / 2 + M.D / 16));
   at.slot = pos - block * M.P;
-  at.ok = true;
   return at;
 }
 
-// Block number `it` of all tokens' rows: the 16 elements it % (D / 16) of KV head and token.
-struct Item {
-  int tok, kh, blk;
-};
-__device__ __forceinline__ Item item_of(const ModelParams& M, uint32_t it) {
-  const uint32_t shift = M.D == 128 ? 3 : 2, row = it >> shift, tok = row / (uint32_t)M.Hkv;
-  return {(int)tok, (int)(row - tok * M.Hkv), (int)(it & ((1u << shift) - 1))};
+// The rows of the block's tokens [tok0, tok0 + n).
+__device__ __forceinline__ int find_rows(const PackedCacheParams& p, int tokens, RowAt* s_at) {
+  const int tok0 = blockIdx.x * tokens, n = min(tokens, p.total_q - tok0);
+  if (threadIdx.x < n) s_at[threadIdx.x] = find_row(p, tok0 + threadIdx.x);
+  __syncthreads();
+  return n;
 }
 
-__global__ void __launch_bounds__(kThreads) packed_append_kernel(const PackedCacheParams p) {
+// Item `it` of the block: eight elements of one token's row, half of a block of 16.
+struct Item {
+  int64_t rows, scales;  // byte offsets of its values and its scale in the pool; rows < 0: none
+};
+__device__ __forceinline__ Item item_of(const PackedCacheParams& p, const RowAt* s_at, uint32_t it, uint32_t per_head) {
   const ModelParams& M = p.m;
-  const int bpr = M.D / 16;  // blocks per row: 4 or 8
-  const uint32_t items = (uint32_t)p.total_q * M.Hkv * bpr;
-  const __nv_bfloat16* in = blockIdx.y ? p.v_in : p.k_in;
-  const float g = blockIdx.y ? p.v_scale : p.k_scale;
-  for (uint32_t it = blockIdx.x * kThreads + threadIdx.x; it < items; it += gridDim.x * kThreads) {
-    const Item at_item = item_of(M, it);
-    const int blk = at_item.blk;
-    const uint4* src = reinterpret_cast<const uint4*>(in) + (int64_t)it * 2;
-    const uint4 u0 = src[0], u1 = src[1];
-    const RowAt at = find_row(p, at_item.tok, at_item.kh);
-    if (!at.ok) continue;
-    const uint32_t w[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
-    float x[16];
-    float a = 0.f;
+  const int shift = M.D == 128 ? 4 : 3;
+  const uint32_t row = it >> shift, oct = it & ((1u << shift) - 1), tok = M.Hkv == 1 ? row : __umulhi(row, per_head), kh = row - tok * M.Hkv;
+  const RowAt at = s_at[tok];
+  const int64_t slab = at.page + (int64_t)(blockIdx.y * M.Hkv + kh) * (M.P * (M.D / 2 + M.D / 16));
+  return {at.page < 0 ? -1 : slab + at.slot * (M.D / 2) + oct * 4, slab + M.P * (M.D / 2) + at.slot * (M.D / 16) + oct / 2};
+}
+
+// x / d from inv = 1 / d to a few last places; infinite products stay what they are.
+__device__ __forceinline__ float quotient(float x, float d, float inv) {
+  const float q = x * inv;
+  return fabsf(q) < 3e38f ? fmaf(fmaf(-q, d, x), inv, q) : q;
+}
+// Eight elements to codes; the lane beside has the other half of the block.
+__device__ __forceinline__ uint32_t to_codes(const uint4 u, float g, float inv_g, uint16_t* code_out) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  float x[8];
+  float a = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 f = unpack_bf16x2(w[k]);
+    x[2 * k] = f.x;
+    x[2 * k + 1] = f.y;
+    a = fmaxf(a, fmaxf(fabsf(f.x), fabsf(f.y)));  // (NaN are no magnitudes; infinities take the largest codes)
+  }
+  a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
+  uint16_t code;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(code) : "f"(0.f), "f"(quotient(quotient(a, g, inv_g), 6.f, 1.f / 6.f)));
+  *code_out = code;
+  const float s = __half2float(__ushort_as_half((unsigned short)(e4m3_to_half2(code) & 0xffff))) * g;
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+  float y[8];
+  if (code == 0x7e) {  // 448: elements may lie far above 6 s
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] = quotient(x[k], s, inv);
+  } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float2 f = unpack_bf16x2(w[k]);
-      x[2 * k] = f.x;
-      x[2 * k + 1] = f.y;
-      a = fmaxf(a, fmaxf(fabsf(f.x), fabsf(f.y)));  // (NaN are no magnitudes; infinities take the largest codes)
+      const float q = x[k] * inv;
+      y[k] = fmaf(fmaf(-q, s, x[k]), inv, q);
     }
-    uint16_t code;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(code) : "f"(0.f), "f"(__fdiv_rn(__fdiv_rn(a, g), 6.f)));
-    const float s = __half2float(__ushort_as_half((unsigned short)(e4m3_to_half2(code) & 0xffff))) * g;
-    const float inv = __fdiv_rn(1.f, s);
-    uint32_t held[2] = {0, 0};
-    if (s > 0.f) {  // (a scale of 0 holds zeros)
+  }
+  uint32_t held;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\tmov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(held)
+      : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
+  return s > 0.f ? held : 0;  // (a scale of 0 holds zeros)
+}
+
+__global__ void __launch_bounds__(kThreads) packed_append_kernel(const PackedCacheParams p, const int tokens, const uint32_t per_head) {
+  __shared__ RowAt s_at[kTokens];
+  const ModelParams& M = p.m;
+  const int n = find_rows(p, tokens, s_at);
+  const uint32_t items = (uint32_t)n * M.Hkv * (M.D / 8);
+  const uint4* in = reinterpret_cast<const uint4*>((blockIdx.y ? p.v_in : p.k_in) + (int64_t)blockIdx.x * tokens * M.Hkv * M.D);
+  const float g = blockIdx.y ? p.v_scale : p.k_scale, inv_g = __fdiv_rn(1.f, g);
+  for (uint32_t base = 0; base < items; base += kAtOnce * kThreads) {
+    uint4 u[kAtOnce];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        float y[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float y0 = x[2 * k + e] * inv;
-          // (from 8 on the level is 6 whatever the residual)
-          y[e] = fabsf(y0) < 8.f ? fmaf(fmaf(-y0, s, x[2 * k + e]), inv, y0) : y0;
-        }
-        uint32_t b;
-        asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u32.u8 %0, t;\n\t}" : "=r"(b) : "f"(y[1]), "f"(y[0]));
-        held[k >> 2] |= b << (8 * (k & 3));
-      }
+    for (int k = 0; k < kAtOnce; ++k) {
+      const uint32_t it = base + k * kThreads + threadIdx.x;
+      u[k] = it < items ? in[it] : make_uint4(0, 0, 0, 0);
     }
-    uint8_t* slab = p.pool + at.slab + (blockIdx.y ? (int64_t)M.Hkv * M.P * (M.D / 2 + M.D / 16) : 0);
-    *reinterpret_cast<uint2*>(slab + at.slot * (M.D / 2) + blk * 8) = make_uint2(held[0], held[1]);
-    slab[M.P * (M.D / 2) + at.slot * bpr + blk] = (uint8_t)code;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (base + k * kThreads >= items) break;  // (uniform)
+      const uint32_t it = base + k * kThreads + threadIdx.x;
+      uint16_t code;
+      const uint32_t held = to_codes(u[k], g, inv_g, &code);
+      if (it >= items) continue;
+      const Item at = item_of(p, s_at, it, per_head);
+      if (at.rows < 0) continue;
+      *reinterpret_cast<uint32_t*>(p.pool + at.rows) = held;
+      if (!(it & 1)) p.pool[at.scales] = (uint8_t)code;
+    }
   }
 }
 
-__global__ void __launch_bounds__(kThreads) packed_read_kernel(const PackedCacheParams p) {
+__global__ void __launch_bounds__(kThreads) packed_read_kernel(const PackedCacheParams p, const int tokens, const uint32_t per_head) {
+  __shared__ RowAt s_at[kTokens];
   const ModelParams& M = p.m;
-  const int bpr = M.D / 16;
-  const uint32_t items = (uint32_t)p.total_q * M.Hkv * bpr;
-  __nv_bfloat16* out = blockIdx.y ? p.v_out : p.k_out;
+  const int n = find_rows(p, tokens, s_at);
+  const uint32_t items = (uint32_t)n * M.Hkv * (M.D / 8);
+  uint4* out = reinterpret_cast<uint4*>((blockIdx.y ? p.v_out : p.k_out) + (int64_t)blockIdx.x * tokens * M.Hkv * M.D);
   const float g = blockIdx.y ? p.v_scale : p.k_scale;
-  for (uint32_t it = blockIdx.x * kThreads + threadIdx.x; it < items; it += gridDim.x * kThreads) {
-    const Item at_item = item_of(M, it);
-    const int blk = at_item.blk;
-    const RowAt at = find_row(p, at_item.tok, at_item.kh);
-    if (!at.ok) continue;
-    const uint8_t* slab = p.pool + at.slab + (blockIdx.y ? (int64_t)M.Hkv * M.P * (M.D / 2 + M.D / 16) : 0);
-    const uint2 held = *reinterpret_cast<const uint2*>(slab + at.slot * (M.D / 2) + blk * 8);
-    const uint32_t f = e4m3_to_half2(slab[M.P * (M.D / 2) + at.slot * bpr + blk]);
-    const uint32_t f2 = low_twice(f);
-    uint32_t o[8];
+  for (uint32_t it0 = threadIdx.x; it0 < items; it0 += kAtOnce * kThreads) {
+    uint32_t held[kAtOnce], code[kAtOnce];
+    bool there[kAtOnce];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const uint32_t word = k ? held.y : held.x;
-      const uint32_t h[4] = {hmul2(e2m1_to_half2<0>(word), f2), hmul2(e2m1_to_half2<1>(word), f2), hmul2(e2m1_to_half2<2>(word), f2),
-                             hmul2(e2m1_to_half2<3>(word), f2)};
+    for (int k = 0; k < kAtOnce; ++k) {
+      const uint32_t it = it0 + k * kThreads;
+      there[k] = false;
+      if (it >= items) continue;
+      const Item at = item_of(p, s_at, it, per_head);
+      there[k] = at.rows >= 0;
+      if (!there[k]) continue;
+      held[k] = *reinterpret_cast<const uint32_t*>(p.pool + at.rows);
+      code[k] = p.pool[at.scales];
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (!there[k]) continue;
+      const uint32_t f2 = low_twice(e4m3_to_half2(code[k])), w = held[k];
+      const uint32_t h[4] = {hmul2(e2m1_to_half2<0>(w), f2), hmul2(e2m1_to_half2<1>(w), f2), hmul2(e2m1_to_half2<2>(w), f2),
+                             hmul2(e2m1_to_half2<3>(w), f2)};
+      uint32_t o[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-        o[4 * k + i] = pack_bf16x2(v.x * g, v.y * g);
+        o[i] = pack_bf16x2(v.x * g, v.y * g);
       }
+      out[it0 + k * kThreads] = make_uint4(o[0], o[1], o[2], o[3]);
     }
-    uint4* dst = reinterpret_cast<uint4*>(out) + (int64_t)it * 2;
-    dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
   }
 }
 
-dim3 grid_of(const PackedCacheParams& p, int num_sms) {
-  const int64_t items = (int64_t)p.total_q * p.m.Hkv * (p.m.D / 16), blocks = (items + kThreads - 1) / kThreads, most = 16LL * num_sms;
-  return dim3((unsigned)(blocks < most ? blocks : most), 2, 1);
+// Tokens of a block: enough for a few rounds of its threads, and blocks enough for the SMs.
+struct Geometry {
+  int tokens;
+  dim3 grid;
+  uint32_t per_head;  // 2^32 / Hkv, rounded up: a row's token by one multiplication (rows of a block are far below 2^16)
+};
+Geometry geometry(const PackedCacheParams& p, int num_sms) {
+  const int per_token = p.m.Hkv * (p.m.D / 8);
+  int tokens = 4 * kAtOnce * kThreads / per_token;
+  const int most = p.total_q / (2 * num_sms);
+  tokens = tokens > most ? most : tokens;
+  tokens = tokens < 1 ? 1 : tokens > kTokens ? kTokens : tokens;
+  return {tokens, dim3((unsigned)((p.total_q + tokens - 1) / tokens), 2, 1), p.m.Hkv == 1 ? 0 : (uint32_t)((1ull << 32) / p.m.Hkv + 1)};
 }
 
 }  // namespace
 
 cudaError_t hswa_launch_packed_append(const PackedCacheParams& p, int num_sms, cudaStream_t s) {
-  packed_append_kernel<<<grid_of(p, num_sms), kThreads, 0, s>>>(p);
+  const Geometry g = geometry(p, num_sms);
+  packed_append_kernel<<<g.grid, kThreads, 0, s>>>(p, g.tokens, g.per_head);
   return cudaGetLastError();
 }
 cudaError_t hswa_launch_packed_read(const PackedCacheParams& p, int num_sms, cudaStream_t s) {
-  packed_read_kernel<<<grid_of(p, num_sms), kThreads, 0, s>>>(p);
+  const Geometry g = geometry(p, num_sms);
+  packed_read_kernel<<<g.grid, kThreads, 0, s>>>(p, g.tokens, g.per_head);
   return cudaGetLastError();
 }
