@@ -267,6 +267,20 @@ hswa_status make_pool_map(const hswa_handle* h, const hswa_layer* layer, CUtenso
   return rc == CUDA_SUCCESS ? HSWA_OK : HSWA_ERR_CUDA;
 }
 
+// 5-D view of a 4-bit pool for TMA: {slab / 9, 9, Hkv, 2, num_pages} in elements of 8 bytes, box of one head's K and V of a page.  (A
+// slab is P (D / 2 + D / 16) = 9 P D / 16 bytes: too long for one dimension of a box.)
+hswa_status make_packed_map(const hswa_handle* h, const hswa_packed_layer* layer, CUtensorMap* tm) {
+  const hswa_config& c = h->cfg;
+  const cuuint64_t slab = (cuuint64_t)c.page_size * (c.head_dim / 2 + c.head_dim / 16), heads = (cuuint64_t)c.num_kv_heads;
+  cuuint64_t dims[5] = {slab / 72, 9, heads, 2, (cuuint64_t)layer->num_pages};
+  cuuint64_t strides[4] = {slab / 9, slab, heads * slab, 2 * heads * slab};
+  cuuint32_t box[5] = {(cuuint32_t)(slab / 72), 9, 1, 2, 1};
+  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  CUresult rc = h->encode_tiled(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT64, 5, layer->pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return rc == CUDA_SUCCESS ? HSWA_OK : HSWA_ERR_CUDA;
+}
+
 // 3-D view of a [T][heads][D] activation tensor for TMA: box {64, 1, box_rows}, 128-byte swizzle.
 hswa_status make_rows_map(const hswa_handle* h, const void* ptr, int heads, int64_t rows, int box_rows, CUtensorMap* tm,
                           int box_heads = 1) {
@@ -1018,10 +1032,14 @@ hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, con
   }
   p.err = h->err;
   cudaStream_t s = (cudaStream_t)stream;
+  if (pl.rows > 8 && pl.runs > 0) {
+    CUtensorMap tm;
+    const hswa_status made = make_packed_map(h, layer, &tm);
+    if (made != HSWA_OK) return made;
+    return hswa_launch_packed_rows(tm, p, pl.rows, s) == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
+  }
   if (pl.rows > 0) {
-    const cudaError_t e = pl.runs == 0    ? hswa_launch_packed_decode(p, pl.rows, s)
-                          : pl.rows == 8 ? hswa_launch_packed_stream(p, s)
-                                         : hswa_launch_packed_rows(p, pl.rows, s);
+    const cudaError_t e = pl.runs > 0 ? hswa_launch_packed_stream(p, s) : hswa_launch_packed_decode(p, pl.rows, s);
     return e == cudaSuccess ? HSWA_OK : HSWA_ERR_CUDA;
   }
   if (hswa_launch_packed_tile(p, s) != cudaSuccess) return HSWA_ERR_CUDA;

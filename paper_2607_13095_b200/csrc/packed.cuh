@@ -52,7 +52,8 @@ cudaError_t hswa_launch_packed_read(const PackedCacheParams& p, int num_sms, cud
 int hswa_packed_stream_runs_per_sm();
 cudaError_t hswa_launch_packed_stream(const PackedAttnParams& p, cudaStream_t s);
 // Few rows, long contexts, on the 5th-generation tensor cores: up to 16 or 32 rows, a run per SM
-cudaError_t hswa_launch_packed_rows(const PackedAttnParams& p, int rows, cudaStream_t s);
+// (tm_pool: the pool as {slab / 9, 9, Hkv, 2, pages}, box of a page's K and V of one head)
+cudaError_t hswa_launch_packed_rows(const CUtensorMap& tm_pool, const PackedAttnParams& p, int rows, cudaStream_t s);
 // The join of runs' pieces of `cols` rows each over key tiles of `tile`
 cudaError_t hswa_launch_packed_join(const PackedAttnParams& p, int cols, int tile, cudaStream_t s);
 // Up to 8, 16 or 32 rows, short contexts: a block per stream
@@ -121,6 +122,12 @@ __device__ __forceinline__ void q_powers(float amax, float* up, float* down) {
   *down = __uint_as_float((uint32_t)(127 - shift) << 23);
 }
 
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2, int c3, int c4) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst), "l"(tm),
+      "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
+      : "memory");
+}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
                "r"(bytes), "r"(bar)

@@ -13,8 +13,8 @@
 //   8-15   softmax, two groups of four warps with every second tile, each with maxima, sums and an accumulator of O of its own: TMEM
 //          lane = key; a lane has N scores of its key.  The rows' maxima are kept from tile to tile and moved only when a score passes
 //          one by more than 2^8, which a vote over the four warps finds out; row sums stay in the lanes to the end
-//   16-19  issue the MMAs of S, issue those of O, bring Q of the next stream, and fetch the pages' slabs of the tiles to come (a bulk
-//          copy each) into a ring
+//   16-19  issue the MMAs of S, issue those of O, bring Q of the next stream, and fetch the tiles to come into a ring (a TMA load for
+//          both slabs of a page)
 // Bound by HBM; what comes next are shared memory (V written and read as fp16) and the issue slots of the conversions.
 #include "packed_stream.cuh"
 #include "tc_primitives.cuh"
@@ -43,6 +43,7 @@ struct Smem {
   static constexpr int PACKED = TN * (D / 2 + D / 16);  // K or V of a tile
   static constexpr int OFF_V = 0, OFF_P = V_STAGES * V_BYTES, OFF_Q = OFF_P + 2 * P_BYTES, OFF_RING = OFF_Q + 2 * Q_BYTES;
   static constexpr int OFF_STATE = OFF_RING + RING * 2 * PACKED;
+  static_assert(OFF_RING % 128 == 0 && PACKED % 128 == 0, "TMA destinations");
   static constexpr int GROUP_STATE = 6 * N * 4;  // of a softmax group: maxima by warp [4][N], rows' maxima [N], factors of O [N]
   static constexpr int OFF_BARS = OFF_STATE + 2 * GROUP_STATE;
   static constexpr int OFF_PLAN = OFF_BARS + NBARS * 8;  // sums [20], first request, tiles before it
@@ -79,20 +80,20 @@ __device__ __forceinline__ void tmem_st_cols(uint32_t addr, const uint32_t* r) {
   if constexpr (N == 32) tmem_st32(addr, r);
   else tmem_st16p(addr, r);
 }
-// A wait of a warp that has nothing else to do: the thread sleeps up to the hint, in ns, instead of taking issue slots to poll.
+// A bounded wait in as few instructions as it can be polled with: twenty warps share the SM, and what the waiting ones issue the
+// others cannot (reading the clock at each poll, and a hint to sleep, took near half of all issue slots).  It gives up after 2^22
+// polls, each of which may suspend the thread: a tenth of a second at least.
 __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity) {
-  long long t0 = 0;
-  for (;;) {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(bar), "r"(parity), "r"(20000u)
-        : "memory");
-    if (done) return true;
-    if (t0 == 0) t0 = clock64();
-    else if (clock64() - t0 > kWaitLimitClocks) return false;
-  }
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 0;\n"
+      "POLL:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
+      "add.u32 n, n, 1;\n\tsetp.lt.u32 q, n, 4194304;\n\t@q bra POLL;\n"
+      "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done != 0;
 }
 // The largest over the warp (NaN are passed over).
 __device__ __forceinline__ float warp_max(float x) {
@@ -136,7 +137,7 @@ struct Walk {
 };
 
 template <int D, int N>
-__global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const PackedAttnParams p) {
+__global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const __grid_constant__ CUtensorMap tm_pool, const PackedAttnParams p) {
   using L = Smem<D, N>;
   constexpr int ROW = D / 2, SC = D / 16;
   constexpr int K_COLS = D / 2;  // TMEM columns of a K stage
@@ -232,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const PackedAt
     int at_rows[2], at_scales[2];  // where its rows and scales lie in the ring's tile
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
-      const int key = warp * 32 + hf * 16 + g, slot = key & (M.P - 1), in_page = (key - slot) / M.P * slab;
+      const int key = warp * 32 + hf * 16 + g, slot = key & (M.P - 1), in_page = (key - slot) / M.P * 2 * slab;
       at_rows[hf] = in_page + slot * ROW + t * (D / 8);
       at_scales[hf] = in_page + M.P * ROW + slot * SC + t * (D / 64);
     }
@@ -297,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const PackedAt
     int at_rows[LOADS], at_scales[LOADS];  // where its rows and scales lie in the ring's tile
 #pragma unroll
     for (int k = 0; k < LOADS; ++k) {
-      const int key = row0 + k * STEP, slot = key & (M.P - 1), in_page = (key - slot) / M.P * slab;
+      const int key = row0 + k * STEP, slot = key & (M.P - 1), in_page = (key - slot) / M.P * 2 * slab + slab;
       at_rows[k] = in_page + slot * ROW + part * 16;
       at_scales[k] = in_page + M.P * ROW + slot * SC + part * 2;
     }
@@ -305,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const PackedAt
     for (int i = 0; i < n_tiles && ok; ++i) {
       const int stage = i % V_STAGES, rs = i % RING;
       ok = __all_sync(0xffffffffu, wait_for(bar(B_RFULL + rs), (i / RING) & 1));
-      const uint8_t* packed = smem + L::OFF_RING + rs * 2 * L::PACKED + L::PACKED;
+      const uint8_t* packed = smem + L::OFF_RING + rs * 2 * L::PACKED;
       const int valid = s_valid[rs];
       uint4 data[LOADS];
       uint32_t f[LOADS];
@@ -661,51 +662,60 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const PackedAt
       if (!ok) timed_out(75, 0);
     } else {
       // ======================= pages =======================
-      // Two tiles at a time (a wait for the ring and the copies' issue cost some hundred cycles, which then overlap), a lane per page
-      // and K or V; the page ids of the two tiles behind are on their way meanwhile.
+      // Two tiles at a time (a wait for the ring costs some hundred cycles, and these overlap), a lane per page; the page ids of the two
+      // tiles behind are on their way meanwhile.  One TMA load brings K and V of a page: each load's issue takes the warp some hundred
+      // cycles, too.
       const int page_shift = 31 - __clz(M.P), ppt = TN >> page_shift;  // pages per tile: 2, 4 or 8
-      const int sub = lane & (ppt - 1), kv = lane / ppt & 1, ahead = lane / (2 * ppt);  // (idle lanes: ahead > 1)
-      const int64_t page_bytes = 2LL * M.Hkv * slab;
+      const int sub = lane & (ppt - 1), ahead = lane / ppt;            // (idle lanes: ahead > 1)
       bool ok = true;
-      // the lane's tile of the two
-      Walk next = {};
+      // the lane's tile of the two: its request, KV head, keys, pages and the page id
+      int t_r = 0, t_kh = 0, t_valid = 0, t_here = 0, t_place = 0, t_page = 0;
+      bool t_mine = false;
       auto take = [&]() {
-        next = at;
+        t_mine = false;
+#pragma unroll
         for (int k = 0; k < 2; ++k) {
-          if (at.left == 0) {
-            if (k <= ahead) next.left = 0;
-            break;
+          if (at.left == 0) break;
+          if (k == ahead) {
+            t_mine = true;
+            t_r = at.r;
+            t_kh = at.kh;
+            t_valid = min(TN, at.s.end - at.tile * TN);
+            t_here = max(0, min(ppt, (t_valid + M.P - 1) >> page_shift));
+            t_place = at.tile * ppt + sub;
+            t_page = sub < t_here ? p.b.block_table[(int64_t)at.r * p.b.max_blocks + t_place] : 0;
           }
-          if (k == ahead) next = at;
           --at.left;
           if (++at.tile == at.s.tiles && at.left > 0) at.next_stream(p);
         }
-        if (ahead > 1) next.left = 0;
-        const int place = next.tile * ppt + sub;
-        return next.left > 0 && place << page_shift < next.s.end ? p.b.block_table[(int64_t)next.r * p.b.max_blocks + place] : -1;
       };
-      int next_page = take();
+      if (lane == 0) tma_prefetch_desc(&tm_pool);
+      take();
+      int rs = ahead % RING, round = 0;  // the lane's slot of the ring, and how often it has been around
       for (int i = 0; i < n_tiles; i += 2) {
-        const Walk w = next;
-        int page = next_page;
-        next_page = take();
-        const bool mine = w.left > 0;
-        const int rs = (i + ahead) % RING, here = mine ? max(0, min(ppt, (w.s.end + M.P - 1) / M.P - w.tile * ppt)) : 0;
-        if (sub < here && (page < 0 || page >= p.num_pages)) {
-          record_error(p.err, HSWA_ERR_BOUNDS, w.r, w.tile * ppt + sub, page);
+        const bool mine = t_mine;
+        const int r = t_r, kh = t_kh, valid = t_valid, here = t_here, place = t_place;
+        int page = t_page;
+        take();
+        if (mine && sub < here && (page < 0 || page >= p.num_pages)) {
+          record_error(p.err, HSWA_ERR_BOUNDS, r, place, page);
           page = 0;
         }
-        if (mine && i + ahead >= RING) ok = wait_for(bar(B_REMPTY + rs), ((i + ahead) / RING - 1) & 1);
+        if (mine && round > 0) ok = wait_for(bar(B_REMPTY + rs), (round - 1) & 1);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        if (mine && sub == 0 && kv == 0) {
-          s_valid[rs] = min(TN, w.s.end - w.tile * TN);
+        if (mine && sub == 0) {
+          s_valid[rs] = valid;
           mbar_arrive_expect_tx(bar(B_RFULL + rs), 2 * here * slab);
         }
         __syncwarp();
-        if (sub < here)
-          bulk_load(sbase + L::OFF_RING + rs * 2 * L::PACKED + kv * L::PACKED + sub * slab,
-                    p.pool + page * page_bytes + (int64_t)(kv * M.Hkv + w.kh) * slab, slab, bar(B_RFULL + rs));
+        if (mine && sub < here)
+          tma_load_5d(sbase + L::OFF_RING + rs * 2 * L::PACKED + sub * 2 * slab, &tm_pool, bar(B_RFULL + rs), 0, 0, kh, 0, page);
+        rs += 2;
+        if (rs >= RING) {
+          rs -= RING;
+          ++round;
+        }
       }
       if (!ok) timed_out(76, 0);
     }
@@ -722,7 +732,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const PackedAt
 }
 
 template <int D, int N>
-cudaError_t launch(const PackedAttnParams& p, cudaStream_t s) {
+cudaError_t launch(const CUtensorMap& tm_pool, const PackedAttnParams& p, cudaStream_t s) {
   auto kern = packed_rows_kernel<D, N>;
   cudaError_t e = hswa_prepare_kernel<packed_rows_kernel<D, N>>(Smem<D, N>::BYTES);
   if (e != cudaSuccess) return e;
@@ -733,14 +743,14 @@ cudaError_t launch(const PackedAttnParams& p, cudaStream_t s) {
     return q != cudaSuccess ? q : attr.numRegs < 96 ? cudaErrorLaunchOutOfResources : cudaSuccess;
   }();
   if (budget != cudaSuccess) return budget;
-  kern<<<p.runs, kThreads, Smem<D, N>::BYTES, s>>>(p);
+  kern<<<p.runs, kThreads, Smem<D, N>::BYTES, s>>>(tm_pool, p);
   e = cudaGetLastError();
   return e != cudaSuccess ? e : hswa_launch_packed_join(p, N, TN, s);
 }
 
 }  // namespace
 
-cudaError_t hswa_launch_packed_rows(const PackedAttnParams& p, int rows, cudaStream_t s) {
-  if (p.m.D == 128) return rows <= 16 ? launch<128, 16>(p, s) : launch<128, 32>(p, s);
-  return rows <= 16 ? launch<64, 16>(p, s) : launch<64, 32>(p, s);
+cudaError_t hswa_launch_packed_rows(const CUtensorMap& tm_pool, const PackedAttnParams& p, int rows, cudaStream_t s) {
+  if (p.m.D == 128) return rows <= 16 ? launch<128, 16>(tm_pool, p, s) : launch<128, 32>(tm_pool, p, s);
+  return rows <= 16 ? launch<64, 16>(tm_pool, p, s) : launch<64, 32>(tm_pool, p, s);
 }
