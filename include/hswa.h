@@ -379,7 +379,7 @@ hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, con
  *   whose page the parent alone holds (ref 1) and none of its children shares go on to its first child, the lowest r; every other
  *   place gets a fresh page.  Where that replaces a partly filled page, (copy_src[r], copy_dst[r]) is the pair to be copied in
  *   every layer's pool before the step writes (hswa_pages_copy), else -1, -1.  Old rows without a child give up their pages.
- *   Written: ref_out (device int32 [num_pages], another array than ref), table_out (device int32 [rows_out][out_max_blocks], the
+ *   Written: ref_out (device int32 [num_pages]), table_out (device int32 [rows_out][out_max_blocks], the
  *   first held_out[r] places of each row), held_out, copy_src, copy_dst (device int32 [rows_out]).  Pages given up by a call are
  *   free from the next call on, since its copies still read them.  If the free pages do not suffice, or a row's arguments are out
  *   of range, nothing is done: ref_out becomes a copy of ref, the other arrays stay as they were, and HSWA_ERR_BOUNDS is recorded
@@ -389,8 +389,8 @@ hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, con
  * hswa_pages_compact: moves live pages into the lowest free ones, up to max_moves of them: while it lies below, the i-th lowest
  *   free page takes the i-th highest live one.  move_src[i], move_dst[i] (device int32 [max_moves]) are the pairs to be copied in
  *   every layer's pool, -1 behind the last; page_map (device int32 [num_pages]) gives every page's new number, for holders outside
- *   the tables; ref_out (another array than ref) the counts under the new numbers; table_out (device int32 [rows][max_blocks], may
- *   be table) the first held[r] places of each row under them.  After all moves the live pages are 0 .. live - 1.
+ *   the tables; ref_out the counts under the new numbers; table_out (device int32 [rows][max_blocks], may be table)
+ *   the first held[r] places of each row under them.  After all moves the live pages are 0 .. live - 1.
  *
  * hswa_pages_copy: page dst[i] of every pool becomes a copy of page src[i], i < pairs (device int32 arrays; -1, -1: no pair), in
  *   n_pools pools (host array of device pointers, 16-byte aligned) of num_pages pages of page_bytes bytes (a multiple of 16): bf16
@@ -398,7 +398,8 @@ hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, con
  *   and the source of another (the lists of the two calls above keep to that).  Ids out of range are recorded and not copied.
  *
  * All refuse a current device other than the handle's (HSWA_ERR_INVALID_ARG), more than 4096 rows or 2^23 pages
- * (HSWA_ERR_UNSUPPORTED), and arrays that must differ but are one (HSWA_ERR_INVALID_ARG). */
+ * (HSWA_ERR_UNSUPPORTED), and an output that is an input or another output, table_out of hswa_pages_compact and its table apart
+ * (HSWA_ERR_INVALID_ARG). */
 size_t hswa_pages_workspace_need(const hswa_handle* h, int64_t num_pages);
 hswa_status hswa_pages_fork(hswa_handle* h, int64_t num_pages, const int32_t* ref, int32_t* ref_out, int32_t rows_in,
                             const int32_t* held, const int32_t* table, int32_t max_blocks, int32_t rows_out, const int32_t* parent,

@@ -308,6 +308,19 @@ hswa_status check_packed(const hswa_handle* h, const hswa_packed_layer* layer, c
   return device_is_current(h) ? HSWA_OK : HSWA_ERR_INVALID_ARG;
 }
 
+// Is one of the outputs an input, or two of them the same array?
+template <size_t N, size_t M>
+bool aliased(const void* const (&outs)[N], const void* const (&ins)[M]) {
+  for (size_t i = 0; i < N; ++i) {
+    if (!outs[i]) continue;
+    for (const void* in : ins)
+      if (outs[i] == in) return true;
+    for (size_t k = 0; k < i; ++k)
+      if (outs[i] == outs[k]) return true;
+  }
+  return false;
+}
+
 hswa_status packed_rows(hswa_handle* h, const hswa_packed_layer* layer, const hswa_batch* b, const void* k_in, const void* v_in, void* k_out,
                         void* v_out, void* stream) {
   if (h) h->chain_ok = 0;
@@ -1065,8 +1078,7 @@ hswa_status hswa_pages_fork(hswa_handle* h, int64_t num_pages, const int32_t* re
   if (rows_in > 0 && (!held || (max_blocks > 0 && !table))) return HSWA_ERR_INVALID_ARG;
   if (rows_out > 0 && (!parent || !len || !need || !held_out || !copy_src || !copy_dst || (out_max_blocks > 0 && !table_out)))
     return HSWA_ERR_INVALID_ARG;
-  if (ref_out == ref || (table && table_out == table) || (held && held_out == held) || (copy_src && copy_src == copy_dst))
-    return HSWA_ERR_INVALID_ARG;
+  if (aliased({ref_out, table_out, held_out, copy_src, copy_dst}, {ref, table, held, parent, len, need})) return HSWA_ERR_INVALID_ARG;
   if (num_pages > kMaxPages || rows_in > kMaxPageRows || rows_out > kMaxPageRows) return HSWA_ERR_UNSUPPORTED;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < hswa_pages_workspace_need(h, num_pages))
     return HSWA_ERR_WORKSPACE;
@@ -1104,8 +1116,8 @@ hswa_status hswa_pages_compact(hswa_handle* h, int64_t num_pages, const int32_t*
   if (h) h->chain_ok = 0;
   if (!h || num_pages <= 0 || rows < 0 || max_blocks < 0 || max_moves < 0 || !ref || !ref_out || !page_map) return HSWA_ERR_INVALID_ARG;
   if (rows > 0 && (!held || (max_blocks > 0 && (!table || !table_out)))) return HSWA_ERR_INVALID_ARG;
-  if (max_moves > 0 && (!move_src || !move_dst || move_src == move_dst)) return HSWA_ERR_INVALID_ARG;
-  if (ref_out == ref || page_map == ref || page_map == ref_out) return HSWA_ERR_INVALID_ARG;
+  if (max_moves > 0 && (!move_src || !move_dst)) return HSWA_ERR_INVALID_ARG;
+  if (aliased({ref_out, page_map, move_src, move_dst}, {ref, table, held, table_out}) || (table_out && table_out == held)) return HSWA_ERR_INVALID_ARG;
   if (num_pages > kMaxPages || rows > kMaxPageRows) return HSWA_ERR_UNSUPPORTED;
   if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
   PagesCompactParams p = {};

@@ -15,7 +15,10 @@
 //          one by more than 2^8, which a vote over the four warps finds out; row sums stay in the lanes to the end
 //   16-19  issue the MMAs of S, issue those of O, bring Q of the next stream, and fetch the tiles to come into a ring (a TMA load for
 //          both slabs of a page)
-// Bound by HBM; what comes next are shared memory (V written and read as fp16) and the issue slots of the conversions.
+// HBM would allow 790 clocks a tile at a head dim of 128; a tile takes 1300 with 16 columns and 1600 with 32, bound by the chain of
+// each role's steps rather than by a pipe: every scheduler has five warps, half of its issue slots go unused.  Measured, 64 / 8 heads of
+// 128, 32 requests of 4096 to 32768 keys: 2 tokens each 185 us, 2 to 4 tokens 245 us (HBM floor 98), where warp-level MMAs took 267 and
+// 450.  Also tried: one softmax group 325 us; codes read straight from global memory 370; a descriptor ring with a prefetch to L2 328.
 #include "packed_stream.cuh"
 #include "tc_primitives.cuh"
 
@@ -25,8 +28,13 @@ using namespace hswa_dev;
 constexpr int TN = 128;  // keys per tile
 constexpr int kThreads = 640;
 constexpr int W_V = 4, W_SOFTMAX = 8, W_OTHER = 16;
-constexpr int REGS_K = 88, REGS_V = 72, REGS_SOFTMAX = 136, REGS_OTHER = 48;
-static_assert(REGS_K + REGS_V + 2 * REGS_SOFTMAX + REGS_OTHER == 5 * 96, "what the launch gave");
+// Registers per thread once the roles have split: their sum is what the launch gave (640 x 96).  32 scores of a lane want more of
+// them than 16 (drafts of 32 rows below: 259 us with the first split, 245 with the second; of 16 rows 185 and 190).
+template <int N>
+struct Regs {
+  static constexpr int K = N == 16 ? 88 : 80, V = 72, SOFTMAX = N == 16 ? 136 : 144, OTHER = N == 16 ? 48 : 40;
+  static_assert(K + V + 2 * SOFTMAX + OTHER == 5 * 96, "what the launch gave");
+};
 constexpr int K_STAGES = 3, V_STAGES = 2;
 constexpr int RING = 5;  // tiles of packed rows
 
@@ -226,7 +234,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const __grid_c
   };
 
   if (warp < W_V) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_K) : "memory");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Regs<N>::K) : "memory");
     // ======================= unpack K =======================
     // Lane (g, t) takes the t-th quarter of rows 32 warp + 16 half + {g, g + 8}.
     const int g = lane >> 2, t = lane & 3;
@@ -287,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const __grid_c
     }
     if (!ok) timed_out(70, 0);
   } else if (warp < W_SOFTMAX) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_V) : "memory");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Regs<N>::V) : "memory");
     // ======================= unpack V =======================
     // A lane takes 16 bytes (32 elements) of LOADS rows; eight neighbouring lanes are on four rows and two parts of a row: their
     // 16-byte stores fall on eight different bank groups.  Rows behind the last key are zeros.
@@ -339,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const __grid_c
     }
     if (!ok) timed_out(71, 0);
   } else if (warp < W_OTHER) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX) : "memory");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Regs<N>::SOFTMAX) : "memory");
     // ======================= softmax =======================
     const int group = (warp - W_SOFTMAX) >> 2, quad = warp & 3, me = quad * 32 + lane;  // the thread's key in the tile = its element of O
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
@@ -546,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const __grid_c
     }
     if (!ok) timed_out(72, i);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER) : "memory");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Regs<N>::OTHER) : "memory");
     if (warp == W_OTHER) {
       // ======================= S = K Q^T =======================
       bool ok = true;

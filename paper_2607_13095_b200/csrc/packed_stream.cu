@@ -379,77 +379,98 @@ __global__ void __launch_bounds__(kThreads, 2) packed_stream_kernel(const Packed
 }
 
 // Joins the pieces of the streams that several warps or blocks had: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
-// WPR = 1: a warp per row, eight rows of a stream per block, for streams in few pieces; 8: the eight warps of a block take every
-// eighth piece of one row.  (32 requests of 4 tokens and 600 to 1500 keys, 64 / 8 heads, two or three pieces a stream: 30 us with eight
-// warps per row, most of whose blocks found nothing to do but to read where the runs begin.)
-template <int D, int TILE, int WPR>
+// ROWS = 8: eight rows of a stream per block, a warp each, or all warps on one after the other where the stream is in many pieces;
+// 1: all warps on one row, for calls whose streams are all in many.  (32 requests of 4 tokens and 600 to 1500 keys, 64 / 8 heads, two or
+// three pieces a stream: 10 us; 30 us with a block per row, most of which found nothing to do but to read where the runs begin.)
+template <int D, int TILE, int ROWS>
 __global__ void __launch_bounds__(256) packed_join_kernel(const PackedAttnParams p, const int cols) {
   const ModelParams& M = p.m;
   const int r = blockIdx.x / M.Hkv, kh = blockIdx.x % M.Hkv;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int col = WPR == 1 ? blockIdx.y * 8 + warp : blockIdx.y, sub = WPR == 1 ? 0 : warp;
   const Stream s = stream_of<TILE>(p, r);
   asm volatile("griddepcontrol.wait;" ::: "memory");  // launched early behind the kernel that writes the pieces
   const int64_t total = p.before[p.b.B] * M.Hkv, start = p.before[r] * M.Hkv + (int64_t)kh * s.tiles;
-  if (s.tiles == 0 || col >= s.n * M.G) return;
+  const int rows = s.n * M.G;
+  if (s.tiles == 0 || (int)blockIdx.y * ROWS >= rows) return;
   // run c holds tile x: c = ceil((x + 1) runs / total) - 1
   const int c0 = (int)(((start + 1) * p.runs - 1) / total), c1 = (int)(((start + s.tiles) * p.runs - 1) / total);
-  const int tok = col / M.G;
-  if (c0 == c1 || (unsigned)s.t0 + (unsigned)tok >= (unsigned)p.total_q) return;
-  auto piece_of = [&](int c) { return (2 * (int64_t)c + (c == c0)) * cols + col; };
-  // a run without tiles (more runs than tiles) left no piece; nor has a piece without a key of the row anything (l = 0)
-  auto ml_of = [&](int c) {
-    return run_start(total, c, p.runs) < run_start(total, c + 1, p.runs) ? p.part_ml[piece_of(c)] : make_float2(-INFINITY, 0.f);
-  };
-  float mm = -INFINITY;
-  for (int c = c0 + lane; c <= c1; c += 32) {
-    const float2 v = ml_of(c);
-    if (v.y != 0.f) mm = fmaxf(mm, v.x);
-  }
-#pragma unroll
-  for (int sh = 16; sh >= 1; sh >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, sh));
+  if (c0 == c1) return;
   constexpr int PER = D / 32;
-  float acc[PER] = {}, L = 0.f;
+  __shared__ float sums[8][32][PER + 1];
+  // the row's pieces first, first + step, ...: their sums under the row's maximum
+  auto add_up = [&](int col, int first, int step, float (&acc)[PER], float& L) {
+    auto piece_of = [&](int c) { return (2 * (int64_t)c + (c == c0)) * cols + col; };
+    // a run without tiles (more runs than tiles) left no piece; nor has a piece without a key of the row anything (l = 0)
+    auto ml_of = [&](int c) {
+      return run_start(total, c, p.runs) < run_start(total, c + 1, p.runs) ? p.part_ml[piece_of(c)] : make_float2(-INFINITY, 0.f);
+    };
+    float mm = -INFINITY;
+    for (int c = c0 + lane; c <= c1; c += 32) {
+      const float2 v = ml_of(c);
+      if (v.y != 0.f) mm = fmaxf(mm, v.x);
+    }
+#pragma unroll
+    for (int sh = 16; sh >= 1; sh >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, sh));
+#pragma unroll
+    for (int i = 0; i < PER; ++i) acc[i] = 0.f;
+    L = 0.f;
 #pragma unroll 4
-  for (int c = c0 + sub; c <= c1; c += WPR) {
-    const float2 v = ml_of(c);
-    const float f = v.y != 0.f ? fast_exp2(v.x == -INFINITY ? 0.f : v.x - mm) : 0.f;  // (l of NaN scores: m says nothing)
-    const float* o = p.part_o + piece_of(c) * D + lane * PER;
-    L += v.y != 0.f ? f * v.y : 0.f;
+    for (int c = c0 + first; c <= c1; c += step) {
+      const float2 v = ml_of(c);
+      const float f = v.y != 0.f ? fast_exp2(v.x == -INFINITY ? 0.f : v.x - mm) : 0.f;  // (l of NaN scores: m says nothing)
+      const float* o = p.part_o + piece_of(c) * D + lane * PER;
+      L += v.y != 0.f ? f * v.y : 0.f;
+#pragma unroll
+      for (int i = 0; i < PER; i += 2) {
+        const float2 x = *reinterpret_cast<const float2*>(o + i);
+        acc[i] += v.y != 0.f ? f * x.x : 0.f;
+        acc[i + 1] += v.y != 0.f ? f * x.y : 0.f;
+      }
+    }
+    return mm;
+  };
+  auto store = [&](int col, float mm, const float (&acc)[PER], float L) {
+    const int tok = col / M.G;
+    if ((unsigned)s.t0 + (unsigned)tok >= (unsigned)p.total_q) return;
+    const float inv = L != 0.f ? 1.f / L : 0.f;
+    const int64_t orow = (int64_t)(s.t0 + tok) * M.Hq + kh * M.G + col % M.G;
 #pragma unroll
     for (int i = 0; i < PER; i += 2) {
-      const float2 x = *reinterpret_cast<const float2*>(o + i);
-      acc[i] += v.y != 0.f ? f * x.x : 0.f;
-      acc[i + 1] += v.y != 0.f ? f * x.y : 0.f;
+      const int64_t at = orow * D + lane * PER + i;
+      if (M.out_fp32)
+        *reinterpret_cast<float2*>(reinterpret_cast<float*>(p.out) + at) = make_float2(acc[i] * inv, acc[i + 1] * inv);
+      else
+        *reinterpret_cast<__nv_bfloat162*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at) = __floats2bfloat162_rn(acc[i] * inv, acc[i + 1] * inv);
     }
+    if (lane == 0 && p.lse) p.lse[orow] = L != 0.f ? (mm + log2f(L)) * 0.6931471805599453f : -INFINITY;
+  };
+  float acc[PER], L;
+  if (ROWS == 8 && c1 - c0 < 24) {
+    const int col = blockIdx.y * 8 + warp;
+    if (col >= rows) return;
+    const float mm = add_up(col, 0, 1, acc, L);
+    store(col, mm, acc, L);
+    return;
   }
-  if constexpr (WPR > 1) {
-    __shared__ float sums[7][32][PER + 1];
-    if (warp > 0) {
+  for (int k = 0; k < ROWS; ++k) {
+    const int col = blockIdx.y * ROWS + k;
+    if (col >= rows) break;  // (uniform)
+    const float mm = add_up(col, warp, 8, acc, L);
 #pragma unroll
-      for (int i = 0; i < PER; ++i) sums[warp - 1][lane][i] = acc[i];
-      sums[warp - 1][lane][PER] = L;
+    for (int i = 0; i < PER; ++i) sums[warp][lane][i] = acc[i];
+    sums[warp][lane][PER] = L;
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll
+      for (int w = 1; w < 8; ++w) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) acc[i] += sums[w][lane][i];
+        L += sums[w][lane][PER];
+      }
+      store(col, mm, acc, L);
     }
     __syncthreads();
-    if (warp > 0) return;
-#pragma unroll
-    for (int k = 0; k < 7; ++k) {
-#pragma unroll
-      for (int i = 0; i < PER; ++i) acc[i] += sums[k][lane][i];
-      L += sums[k][lane][PER];
-    }
   }
-  const float inv = L != 0.f ? 1.f / L : 0.f;
-  const int64_t orow = (int64_t)(s.t0 + tok) * M.Hq + kh * M.G + col % M.G;
-#pragma unroll
-  for (int i = 0; i < PER; i += 2) {
-    const int64_t at = orow * D + lane * PER + i;
-    if (M.out_fp32)
-      *reinterpret_cast<float2*>(reinterpret_cast<float*>(p.out) + at) = make_float2(acc[i] * inv, acc[i + 1] * inv);
-    else
-      *reinterpret_cast<__nv_bfloat162*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at) = __floats2bfloat162_rn(acc[i] * inv, acc[i + 1] * inv);
-  }
-  if (lane == 0 && p.lse) p.lse[orow] = L != 0.f ? (mm + log2f(L)) * 0.6931471805599453f : -INFINITY;
 }
 
 template <int D, int PAGE>
@@ -486,7 +507,7 @@ static cudaError_t launch_join(const PackedAttnParams& p, int cols, cudaStream_t
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return few ? cudaLaunchKernelEx(&cfg, packed_join_kernel<D, TILE, 1>, p, cols) : cudaLaunchKernelEx(&cfg, packed_join_kernel<D, TILE, 8>, p, cols);
+  return few ? cudaLaunchKernelEx(&cfg, packed_join_kernel<D, TILE, 8>, p, cols) : cudaLaunchKernelEx(&cfg, packed_join_kernel<D, TILE, 1>, p, cols);
 }
 cudaError_t hswa_launch_packed_join(const PackedAttnParams& p, int cols, int tile, cudaStream_t s) {
   if (tile == TK) return p.m.D == 128 ? launch_join<128, TK>(p, cols, s) : launch_join<64, TK>(p, cols, s);

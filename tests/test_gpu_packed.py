@@ -212,18 +212,18 @@ def test_peaked_rows_and_growing_maxima(n, sm_scale):
     assert (np.abs(lse - want_lse) <= more).all()
 
 
-def test_offsets_past_32_bits_and_rows_left_alone():
-    """A pool of more than 4 GB, a request in its last pages; rows of out behind the last request stay as they were."""
+@pytest.mark.parametrize("ctx,n", [([100, 200], [2, 3]), ([2300, 200], [1, 1]), ([2300, 200], [2, 3]), ([100, 200], [40, 3])])
+def test_offsets_past_32_bits_and_rows_left_alone(ctx, n):
+    """A pool of more than 4 GB, requests in its last pages; rows of out behind the last request stay as they were."""
     d = dims(8, 128, 64, 8)
-    c = Case(d, [100, 200], [2, 3], seed=9)
-    c.n[1] = 3
+    c = Case(d, ctx, n, seed=9)
     pages = 60000  # x 73728 bytes
     pool = torch.zeros((pages, *c.pool.shape[1:]), dtype=torch.uint8, device="cuda")
     pool[pages - c.pool.shape[0]:] = torch.from_numpy(c.pool).cuda()
     c.table = np.where(c.table >= 0, c.table + pages - c.pool.shape[0], -1).astype(np.int32)
     h = make_handle(d, torch.float32)
     T = int(c.indptr[-1])
-    b = hb.Batch(dev_i32(c.ctx), dev_i32(c.table), *no_rings(d, 2), dev_i32(c.indptr), max_q_len=3, total_q=T + 4, max_ctx_len=200)
+    b = hb.Batch(dev_i32(c.ctx), dev_i32(c.table), *no_rings(d, 2), dev_i32(c.indptr), max_q_len=max(n), total_q=T + 4, max_ctx_len=max(ctx))
     out = torch.full((T + 4, 64, 128), 7.0, device="cuda")
     lse = torch.full((T + 4, 64), 7.0, device="cuda")
     q = torch.zeros((T + 4, 64, 128), dtype=torch.bfloat16, device="cuda")
@@ -265,6 +265,15 @@ def test_many_requests_of_all_lengths(d, n):
     ctx = [int(x) for x in rng.integers(0, 400, B)]
     ctx[3], ctx[77], ctx[B - 1] = 2600, 0, 2301
     c = Case(d, ctx, [n if r % 5 else r % (n + 1) for r in range(B)], seed=33)
+    check(c, *run(c, single=False))
+
+
+@pytest.mark.parametrize("n", [1, 2])
+def test_one_long_request_among_many_short_ones(n):
+    """Most streams in a piece or two, a few in dozens."""
+    ctx = [9] * 300
+    ctx[150] = 12007
+    c = Case(dims(8, 64, 64, 1), ctx, [n] * 300, seed=40)
     check(c, *run(c, single=False))
 
 

@@ -250,7 +250,8 @@ def test_refusals():
         return e.value.status
 
     fork_args = [counts, other, table, *rows[:4], z(2, 3), *rows[4:], ws]
-    for i, same in ((1, 0), (7, 2), (8, 3), (10, 9)):  # ref_out = ref, table_out = table, held_out = held, copy_dst = copy_src
+    # ref_out = ref, table_out = table, held_out = held, copy_dst = copy_src, held_out = need, copy_src = length, copy_dst = held_out
+    for i, same in ((1, 0), (7, 2), (8, 3), (10, 9), (8, 6), (9, 5), (10, 8)):
         a = list(fork_args)
         a[i] = a[same]
         assert status(hb.hswa_pages_fork, *a) == bad
@@ -261,6 +262,7 @@ def test_refusals():
     assert status(hb.hswa_pages_compact, counts, counts, table, rows[0], table, z(8), rows[1], rows[2]) == bad
     assert status(hb.hswa_pages_compact, counts, other, table, rows[0], table, counts, rows[1], rows[2]) == bad
     assert status(hb.hswa_pages_compact, counts, other, table, rows[0], table, z(8), rows[1], rows[1]) == bad
+    assert status(hb.hswa_pages_compact, counts, other, table, rows[0], table, z(8), rows[0], rows[1]) == bad  # move_src = held
     big = torch.zeros(((1 << 23) + 1,), dtype=torch.int32, device="cuda")
     assert status(hb.hswa_pages_compact, big, torch.empty_like(big), table, rows[0], table, torch.empty_like(big), rows[1], rows[2]) == uns
     assert hb.hswa_pages_workspace_need(h, (1 << 23) + 1) == 0
