@@ -1026,6 +1026,7 @@ hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, con
   p.pool = static_cast<const uint8_t*>(layer->pool);
   p.num_pages = layer->num_pages;
   p.scale_log2 = p.m.scale_log2 * layer->k_scale;
+  if (!std::isfinite(p.scale_log2)) return HSWA_ERR_INVALID_ARG;
   p.v_scale = layer->v_scale;
   p.causal = causal != 0;
   p.q = static_cast<const __nv_bfloat16*>(q);
@@ -1079,7 +1080,9 @@ hswa_status hswa_pages_fork(hswa_handle* h, int64_t num_pages, const int32_t* re
   if (rows_out > 0 && (!parent || !len || !need || !held_out || !copy_src || !copy_dst || (out_max_blocks > 0 && !table_out)))
     return HSWA_ERR_INVALID_ARG;
   if (aliased({ref_out, table_out, held_out, copy_src, copy_dst}, {ref, table, held, parent, len, need})) return HSWA_ERR_INVALID_ARG;
-  if (num_pages > kMaxPages || rows_in > kMaxPageRows || rows_out > kMaxPageRows) return HSWA_ERR_UNSUPPORTED;
+  if (num_pages > kMaxPages || rows_in > kMaxPageRows || rows_out > kMaxPageRows || (int64_t)rows_in * max_blocks > kMaxPageEntries ||
+      (int64_t)rows_out * out_max_blocks > kMaxPageEntries)
+    return HSWA_ERR_UNSUPPORTED;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < hswa_pages_workspace_need(h, num_pages))
     return HSWA_ERR_WORKSPACE;
   if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
@@ -1118,7 +1121,7 @@ hswa_status hswa_pages_compact(hswa_handle* h, int64_t num_pages, const int32_t*
   if (rows > 0 && (!held || (max_blocks > 0 && (!table || !table_out)))) return HSWA_ERR_INVALID_ARG;
   if (max_moves > 0 && (!move_src || !move_dst)) return HSWA_ERR_INVALID_ARG;
   if (aliased({ref_out, page_map, move_src, move_dst}, {ref, table, held, table_out}) || (table_out && table_out == held)) return HSWA_ERR_INVALID_ARG;
-  if (num_pages > kMaxPages || rows > kMaxPageRows) return HSWA_ERR_UNSUPPORTED;
+  if (num_pages > kMaxPages || rows > kMaxPageRows || (int64_t)rows * max_blocks > kMaxPageEntries) return HSWA_ERR_UNSUPPORTED;
   if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
   PagesCompactParams p = {};
   p.num_pages = (int32_t)num_pages;

@@ -113,11 +113,15 @@ __device__ __forceinline__ void mma_f16_16816_zero(float (&c)[4], uint32_t a0, u
 }
 
 // Queries enter the products as fp16, each row times a power of two that brings its largest element to [2^14, 2^15): fp16
-// has three bits more than bf16, so only elements below 2^-28 of the largest lose any.  From the largest magnitude, the
-// power and its inverse; a row of zeros, or one with an infinity, is taken as it is (NaN are no magnitudes).
+// has three bits more than bf16, so only elements below 2^-28 of the largest lose any.  From the largest magnitude, infinities and
+// NaN apart, the power and its inverse.
+__device__ __forceinline__ float finite_max(float amax, float2 f) {
+  const float a = fabsf(f.x), b = fabsf(f.y);
+  return fmaxf(amax, fmaxf(a < INFINITY ? a : 0.f, b < INFINITY ? b : 0.f));
+}
 __device__ __forceinline__ void q_powers(float amax, float* up, float* down) {
   const int e = (int)(__float_as_uint(amax) >> 23);  // biased exponent
-  const int shift = amax > 0.f && e < 255 ? min(141 - e, 100) : 0;
+  const int shift = amax > 0.f ? min(141 - e, 100) : 0;
   *up = __uint_as_float((uint32_t)(127 + shift) << 23);
   *down = __uint_as_float((uint32_t)(127 - shift) << 23);
 }

@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float2 f = unpack_bf16x2(u[e]);
-        amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
+        amax = finite_max(amax, f);
       }
     }
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));

@@ -638,7 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const __grid_c
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float2 y = unpack_bf16x2(u[e]);
-            amax = fmaxf(amax, fmaxf(fabsf(y.x), fabsf(y.y)));
+            amax = finite_max(amax, y);
           }
         }
 #pragma unroll

@@ -3,9 +3,13 @@
 // The 64-key tiles of all (request, KV head) streams form one sequence, cut into equal runs, one per warp: no warp ends early,
 // whatever the lengths, none waits for another, and loads run on from stream to stream.  A warp fetches its own tiles (a bulk copy
 // per page and K or V) into a ring of its own, three half-tiles deep: V of the next tile is asked for when K of this one has been
-// read, K of the one after when V has.  (One warp that fetched for seven others could not keep up: 311 us on the batch below.)  A
-// stream that a warp has as a whole is written out there, pieces of the others are joined by a second launch.
+// read, K of the one after when V has.  A stream that a warp has as a whole is written out there, pieces of the others are joined by
+// a second launch.
 // Both products read their operands straight from the packed rows, as in packed_decode.cu, which has the fragments' layout.
+// Bound by HBM, and close behind by issue: of a 16-key group with 128 elements, the 64 conversions and 64 products that make fp16 of
+// codes and the 16 MMAs take 240 of the 390 clocks that HBM leaves a scheduler, before loads, masks and the softmax.  Measured, 64 requests of one token over 4096 to
+// 32768 keys, 64 / 8 heads of 128 (1.48 GB): 279 us, 5.3 TB/s (HBM floor 226); one warp that fetched for seven others 311, with
+// divisions by the page size 365.
 #include "packed_stream.cuh"
 #include "tc_primitives.cuh"
 
@@ -177,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, 2) packed_stream_kernel(const Packed
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float2 f = unpack_bf16x2(u[e]);
-          amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
+          amax = finite_max(amax, f);
         }
       }
       amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
@@ -400,9 +404,10 @@ __global__ void __launch_bounds__(256) packed_join_kernel(const PackedAttnParams
   // the row's pieces first, first + step, ...: their sums under the row's maximum
   auto add_up = [&](int col, int first, int step, float (&acc)[PER], float& L) {
     auto piece_of = [&](int c) { return (2 * (int64_t)c + (c == c0)) * cols + col; };
-    // a run without tiles (more runs than tiles) left no piece; nor has a piece without a key of the row anything (l = 0)
+    // a run without tiles (there may be more runs than tiles) left no piece; nor has a piece without a key of the row anything (l = 0)
     auto ml_of = [&](int c) {
-      return run_start(total, c, p.runs) < run_start(total, c + 1, p.runs) ? p.part_ml[piece_of(c)] : make_float2(-INFINITY, 0.f);
+      return p.runs <= total || run_start(total, c, p.runs) < run_start(total, c + 1, p.runs) ? p.part_ml[piece_of(c)]
+                                                                                               : make_float2(-INFINITY, 0.f);
     };
     float mm = -INFINITY;
     for (int c = c0 + lane; c <= c1; c += 32) {

@@ -7,8 +7,8 @@ namespace hswa_dev {
 
 constexpr int kStreamTile = 64;  // keys per tile of the warp-level kernels
 
-// Keys of a 16-key group in the order of the fragments' rows: row i of the first half holds key kKey(i), row 8 + i key 8 +
-// kKey(i).  (A lane's V rows are kKey(2t), kKey(2t + 1): this order has lanes t = 0 .. 3 on rows 0, 3, 4, 7 and 1, 2, 5, 6,
+// Keys of a 16-key group in the order of the fragments' rows: row i of the first half holds key key_of(i), row 8 + i key 8 +
+// key_of(i).  (A lane's V rows are key_of(2t), key_of(2t + 1): this order has lanes t = 0 .. 3 on rows 0, 3, 4, 7 and 1, 2, 5, 6,
 // two of each parity, which halves the bank conflicts of 64-byte rows; K rows come in pairs of unlike parity.)
 __device__ __forceinline__ int key_of(int i) { return (i & 4) | ((i & 2) ? 3 - (i & 1) : (i & 1)); }
 

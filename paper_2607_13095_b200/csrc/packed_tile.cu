@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_tile_kernel(const PackedAt
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float2 x = unpack_bf16x2(u[e]);
-          amax = fmaxf(amax, fmaxf(fabsf(x.x), fabsf(x.y)));
+          amax = finite_max(amax, x);
         }
       }
       float up, down;

@@ -3,8 +3,10 @@
 
 #include "hswa_internal.cuh"
 
-// Limits of one call: rows of a table and pages of a pool whose bookkeeping fits a cluster's shared memory.
+// Limits of one call: rows of a table and pages of a pool whose bookkeeping fits a cluster's shared memory, and entries of a table
+// whose number of fresh pages fits 32 bits.
 constexpr int kMaxPageRows = 4096, kMaxPages = 1 << 23;
+constexpr int64_t kMaxPageEntries = 1 << 30;
 constexpr int kPoolsPerLaunch = 64;
 
 struct PagesForkParams {

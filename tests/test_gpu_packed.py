@@ -198,6 +198,21 @@ def test_a_nan_query_shows_and_stays_in_its_row(n):
     check(c, out, lse)
 
 
+@pytest.mark.parametrize("ctx,n", [([70, 20], 1), ([70, 20], 3), ([70, 20], 40), ([2400, 300], 1), ([2400, 300], 2), ([2400, 300], 4)])
+def test_an_infinite_query_stays_in_its_row(ctx, n):
+    """Rows of elements that fp16 does not reach beside one with an infinity."""
+    c = Case(dims(8, 128, 64), ctx, [n, n], seed=41)
+    big = wl.bits_to_f64(c.q) * 2.0 ** 20
+    q = to_host_bits(torch.from_numpy(big).to(torch.bfloat16))
+    assert np.array_equal(wl.bits_to_f64(q), big)
+    q[n - 1, 5, 3] = 0x7F80
+    h = make_handle(c.d, torch.float32, sm_scale=float(np.float32(1.0 / np.sqrt(128))) * 2.0 ** -20)
+    c.scale = float(h.cfg.sm_scale) * 2.0 ** 20
+    out, lse = run(c, q=q, h=h, single=False)
+    out[n - 1, 5], lse[n - 1, 5] = c.want()[0][n - 1, 5], c.want()[1][n - 1, 5]
+    check(c, out, lse)
+
+
 @pytest.mark.parametrize("sm_scale", [1.0, 3.0])
 @pytest.mark.parametrize("n", [1, 4, 40])
 def test_peaked_rows_and_growing_maxima(n, sm_scale):
@@ -494,6 +509,10 @@ def test_refusals():
     with pytest.raises(AssertionError):
         hb.hswa_packed_attn(h, layer, b, True, q, out, None, ws.cpu())
     assert hb.hswa_packed_workspace_need(h, 1, 2, 2, 2 ** 30, True) == 0
+    steep = make_handle(dims(2, 64, 16, 1), torch.float32, sm_scale=2.0 ** 100)
+    with pytest.raises(hb.HswaError) as e:
+        hb.hswa_packed_attn(steep, hb.PackedLayer(layer.pool, 2.0 ** 40, 1.0), b, True, q, out, None, ws)
+    assert e.value.status == hb.HSWA_ERR_INVALID_ARG
     no_error(h)
 
 

@@ -259,6 +259,11 @@ def test_refusals():
     assert status(hb.hswa_pages_fork, *fork_args[:-1], torch.empty((512,), dtype=torch.uint8, device="cuda")[16:]) == hb.HSWA_ERR_WORKSPACE
     many = z(4097)
     assert status(hb.hswa_pages_fork, counts, other, z(4097, 1), many, *rows[:3], z(2, 3), *rows[3:6], ws) == uns
+    wide = torch.empty((2, (1 << 29) + 1), dtype=torch.int32, device="cuda")
+    assert status(hb.hswa_pages_fork, counts, other, wide, *rows[:4], z(2, 3), *rows[4:], ws) == uns
+    assert status(hb.hswa_pages_fork, counts, other, table, *rows[:4], wide, *rows[4:], ws) == uns
+    assert status(hb.hswa_pages_compact, counts, other, wide, rows[0], wide, z(8), rows[1], rows[2]) == uns
+    del wide
     assert status(hb.hswa_pages_compact, counts, counts, table, rows[0], table, z(8), rows[1], rows[2]) == bad
     assert status(hb.hswa_pages_compact, counts, other, table, rows[0], table, counts, rows[1], rows[2]) == bad
     assert status(hb.hswa_pages_compact, counts, other, table, rows[0], table, z(8), rows[1], rows[1]) == bad
