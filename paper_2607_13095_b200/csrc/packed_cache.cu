@@ -4,29 +4,30 @@
 // A block of 16 elements x with largest magnitude a, in a layer of scale g, is held as f = e4m3((a / g) / 6), s = f g, and
 // e2m1(x / s): both roundings to the nearest, ties to the even code, at most 448 and 6.  Quotients lie halfway between two codes
 // often (dividend and divisor have few bits), so they have to be right to the last bit: a product with the inverse, then one
-// Newton step on its exact residual, which makes every quotient exact that fits 24 bits.  (Divisions took the append from 59
-// to 79 us, once two lanes share a block.)
-// Bound by HBM: 2 bytes per element read, 0.5625 written (read-back: the reverse).  A block takes some tokens: it looks up where
-// their rows are held (a chain of dependent loads) once, and then moves their elements with several loads in flight; a thread that
-// looked up its own row was at half the rate.
+// Newton step on its exact residual, which makes every quotient exact that fits 24 bits.  (Divisions take the append from 59
+// to 79 us; a pair of elements per instruction, from 52 to 46.)
+// Bound by HBM (2 bytes per element read, 0.5625 written; read-back: the reverse) and by issue: 70 % of the slots at ten
+// instructions an element.  A block takes some tokens: it looks up where their rows are held (a chain of dependent loads) once, and then
+// moves their elements with several loads in flight; a thread that looked up its own row was at half the rate.  Measured, 8 prompts of
+// up to 8192 tokens, 8 KV heads of 128 (200 MB each way, floor 30 us): append 46 us, read-back 35; with 32 tokens a block 47 and 36 (fewer,
+// longer blocks end less evenly).
 #include "packed.cuh"
 
 namespace {
 using namespace hswa_dev;
 
 constexpr int kThreads = 256;
-constexpr int kTokens = 32;  // of a block, at most
+constexpr int kTokens = 16;  // of a block, at most
 constexpr int kAtOnce = 4;   // items that a thread has in flight
 
 struct RowAt {
-  int64_t page;  // byte offset of the row's page; -1: not to be moved
-  int slot;
+  uint8_t *values, *scales;  // of KV head 0, K or V as the block moves; null: not to be moved
 };
 
 // Where the row of token `tok` (of all requests' tokens) is held; records what is out of range.
 __device__ __forceinline__ RowAt find_row(const PackedCacheParams& p, int tok) {
   const ModelParams& M = p.m;
-  RowAt at = {-1, 0};
+  RowAt at = {nullptr, nullptr};
   int r = tok, i = 0;
   if (p.b.q_indptr) {
     if (tok < p.b.q_indptr[0]) return at;
@@ -59,8 +60,10 @@ __device__ __forceinline__ RowAt find_row(const PackedCacheParams& p, int tok) {
     record_error(p.err, HSWA_ERR_BOUNDS, r, block, page);
     return at;
   }
-  at.page = (int64_t)page * 2 * M.Hkv * (M.P * (M.D / 2 + M.D / 16));
-  at.slot = pos - block * M.P;
+  const int slot = pos - block * M.P;
+  uint8_t* slab = p.pool + ((int64_t)page * 2 + blockIdx.y) * M.Hkv * (M.P * (M.D / 2 + M.D / 16));
+  at.values = slab + slot * (M.D / 2);
+  at.scales = slab + M.P * (M.D / 2) + slot * (M.D / 16);
   return at;
 }
 
@@ -72,17 +75,26 @@ __device__ __forceinline__ int find_rows(const PackedCacheParams& p, int tokens,
   return n;
 }
 
-// Item `it` of the block: eight elements of one token's row, half of a block of 16.
-struct Item {
-  int64_t rows, scales;  // byte offsets of its values and its scale in the pool; rows < 0: none
+// What a thread's items have in common: item `it` of the block is eight elements, half of a block of 16, of row it / (D / 8) of the
+// block's tokens and KV heads; a thread's items are kThreads, a multiple of D / 8, apart, so all are the same part of their rows.
+struct Part {
+  int shift;
+  uint32_t values, scale, slab;  // byte offsets in a row and its scales, bytes of a slab
 };
-__device__ __forceinline__ Item item_of(const PackedCacheParams& p, const RowAt* s_at, uint32_t it, uint32_t per_head) {
+__device__ __forceinline__ Part part_of(const PackedCacheParams& p) {
   const ModelParams& M = p.m;
   const int shift = M.D == 128 ? 4 : 3;
-  const uint32_t row = it >> shift, oct = it & ((1u << shift) - 1), tok = M.Hkv == 1 ? row : __umulhi(row, per_head), kh = row - tok * M.Hkv;
-  const RowAt at = s_at[tok];
-  const int64_t slab = at.page + (int64_t)(blockIdx.y * M.Hkv + kh) * (M.P * (M.D / 2 + M.D / 16));
-  return {at.page < 0 ? -1 : slab + at.slot * (M.D / 2) + oct * 4, slab + M.P * (M.D / 2) + at.slot * (M.D / 16) + oct / 2};
+  const uint32_t oct = threadIdx.x & ((1u << shift) - 1);
+  return {shift, oct * 4, oct / 2, (uint32_t)(M.P * (M.D / 2 + M.D / 16))};
+}
+__device__ __forceinline__ RowAt item_of(const PackedCacheParams& p, const RowAt* s_at, const Part& part, uint32_t it, uint32_t per_head) {
+  const uint32_t heads = p.m.Hkv, row = it >> part.shift, tok = heads == 1 ? row : __umulhi(row, per_head), kh = row - tok * heads;
+  RowAt at = s_at[tok];
+  if (at.values) {
+    at.values += kh * part.slab + part.values;
+    at.scales += kh * part.slab + part.scale;
+  }
+  return at;
 }
 
 // x / d from inv = 1 / d to a few last places; infinite products stay what they are.
@@ -90,17 +102,19 @@ __device__ __forceinline__ float quotient(float x, float d, float inv) {
   const float q = x * inv;
   return fabsf(q) < 3e38f ? fmaf(fmaf(-q, d, x), inv, q) : q;
 }
+__device__ __forceinline__ float2 quotient_below_max(float2 x, float2 minus_d, float2 inv) {  // (of finite products)
+  const float2 q = __fmul2_rn(x, inv);
+  return __ffma2_rn(__ffma2_rn(q, minus_d, x), inv, q);
+}
 // Eight elements to codes; the lane beside has the other half of the block.
 __device__ __forceinline__ uint32_t to_codes(const uint4 u, float g, float inv_g, uint16_t* code_out) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-  float x[8];
+  float2 x[4];
   float a = 0.f;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const float2 f = unpack_bf16x2(w[k]);
-    x[2 * k] = f.x;
-    x[2 * k + 1] = f.y;
-    a = fmaxf(a, fmaxf(fabsf(f.x), fabsf(f.y)));  // (NaN are no magnitudes; infinities take the largest codes)
+    x[k] = unpack_bf16x2(w[k]);
+    a = fmaxf(a, fmaxf(fabsf(x[k].x), fabsf(x[k].y)));  // (NaN are no magnitudes; infinities take the largest codes)
   }
   a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
   uint16_t code;
@@ -109,23 +123,20 @@ __device__ __forceinline__ uint32_t to_codes(const uint4 u, float g, float inv_g
   const float s = __half2float(__ushort_as_half((unsigned short)(e4m3_to_half2(code) & 0xffff))) * g;
   float inv;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
-  float y[8];
+  float2 y[4];
   if (code == 0x7e) {  // 448: elements may lie far above 6 s
 #pragma unroll
-    for (int k = 0; k < 8; ++k) y[k] = quotient(x[k], s, inv);
+    for (int k = 0; k < 4; ++k) y[k] = make_float2(quotient(x[k].x, s, inv), quotient(x[k].y, s, inv));
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float q = x[k] * inv;
-      y[k] = fmaf(fmaf(-q, s, x[k]), inv, q);
-    }
+    for (int k = 0; k < 4; ++k) y[k] = quotient_below_max(x[k], make_float2(-s, -s), make_float2(inv, inv));
   }
   uint32_t held;
   asm("{\n\t.reg .b8 a, b, c, d;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\tmov.b32 %0, {a, b, c, d};\n\t}"
       : "=r"(held)
-      : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
+      : "f"(y[0].x), "f"(y[0].y), "f"(y[1].x), "f"(y[1].y), "f"(y[2].x), "f"(y[2].y), "f"(y[3].x), "f"(y[3].y));
   return s > 0.f ? held : 0;  // (a scale of 0 holds zeros)
 }
 
@@ -134,6 +145,7 @@ __global__ void __launch_bounds__(kThreads) packed_append_kernel(const PackedCac
   const ModelParams& M = p.m;
   const int n = find_rows(p, tokens, s_at);
   const uint32_t items = (uint32_t)n * M.Hkv * (M.D / 8);
+  const Part part = part_of(p);
   const uint4* in = reinterpret_cast<const uint4*>((blockIdx.y ? p.v_in : p.k_in) + (int64_t)blockIdx.x * tokens * M.Hkv * M.D);
   const float g = blockIdx.y ? p.v_scale : p.k_scale, inv_g = __fdiv_rn(1.f, g);
   for (uint32_t base = 0; base < items; base += kAtOnce * kThreads) {
@@ -150,10 +162,10 @@ __global__ void __launch_bounds__(kThreads) packed_append_kernel(const PackedCac
       uint16_t code;
       const uint32_t held = to_codes(u[k], g, inv_g, &code);
       if (it >= items) continue;
-      const Item at = item_of(p, s_at, it, per_head);
-      if (at.rows < 0) continue;
-      *reinterpret_cast<uint32_t*>(p.pool + at.rows) = held;
-      if (!(it & 1)) p.pool[at.scales] = (uint8_t)code;
+      const RowAt at = item_of(p, s_at, part, it, per_head);
+      if (!at.values) continue;
+      *reinterpret_cast<uint32_t*>(at.values) = held;
+      if (!(it & 1)) *at.scales = (uint8_t)code;
     }
   }
 }
@@ -163,6 +175,7 @@ __global__ void __launch_bounds__(kThreads) packed_read_kernel(const PackedCache
   const ModelParams& M = p.m;
   const int n = find_rows(p, tokens, s_at);
   const uint32_t items = (uint32_t)n * M.Hkv * (M.D / 8);
+  const Part part = part_of(p);
   uint4* out = reinterpret_cast<uint4*>((blockIdx.y ? p.v_out : p.k_out) + (int64_t)blockIdx.x * tokens * M.Hkv * M.D);
   const float g = blockIdx.y ? p.v_scale : p.k_scale;
   for (uint32_t it0 = threadIdx.x; it0 < items; it0 += kAtOnce * kThreads) {
@@ -173,11 +186,11 @@ __global__ void __launch_bounds__(kThreads) packed_read_kernel(const PackedCache
       const uint32_t it = it0 + k * kThreads;
       there[k] = false;
       if (it >= items) continue;
-      const Item at = item_of(p, s_at, it, per_head);
-      there[k] = at.rows >= 0;
+      const RowAt at = item_of(p, s_at, part, it, per_head);
+      there[k] = at.values != nullptr;
       if (!there[k]) continue;
-      held[k] = *reinterpret_cast<const uint32_t*>(p.pool + at.rows);
-      code[k] = p.pool[at.scales];
+      held[k] = *reinterpret_cast<const uint32_t*>(at.values);
+      code[k] = *at.scales;
     }
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
@@ -188,8 +201,8 @@ __global__ void __launch_bounds__(kThreads) packed_read_kernel(const PackedCache
       uint32_t o[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-        o[i] = pack_bf16x2(v.x * g, v.y * g);
+        const float2 v = __fmul2_rn(__half22float2(*reinterpret_cast<const __half2*>(&h[i])), make_float2(g, g));
+        o[i] = pack_bf16x2(v.x, v.y);
       }
       out[it0 + k * kThreads] = make_uint4(o[0], o[1], o[2], o[3]);
     }
@@ -204,7 +217,7 @@ struct Geometry {
 };
 Geometry geometry(const PackedCacheParams& p, int num_sms) {
   const int per_token = p.m.Hkv * (p.m.D / 8);
-  int tokens = 4 * kAtOnce * kThreads / per_token;
+  int tokens = 2 * kAtOnce * kThreads / per_token;
   const int most = p.total_q / (2 * num_sms);
   tokens = tokens > most ? most : tokens;
   tokens = tokens < 1 ? 1 : tokens > kTokens ? kTokens : tokens;
