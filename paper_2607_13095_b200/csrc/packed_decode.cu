@@ -46,18 +46,18 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
   const int g = lane >> 2, t = lane & 3;
 
   const uint32_t full0 = smem_u32(bars), empty0 = smem_u32(bars + NS);
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < NS; ++s) {
-      mbar_init(full0 + 8 * s, 1);
-      mbar_init(empty0 + 8 * s, 1);
-    }
+  if (threadIdx.x < 2 * NS) {  // (full and empty lie side by side)
+    mbar_init(full0 + 8 * threadIdx.x, 1);
     mbar_fence_init();
-    *s_stop = 0;
   }
-  if (blockIdx.x == 0) record_batch(p, kThreads);
+  if (threadIdx.x == 0) *s_stop = 0;
   const int r = blockIdx.x / M.Hkv, kh = blockIdx.x % M.Hkv;
+  // the producer's first page ids do not wait for the length (an id behind it goes unused)
+  const int32_t* tbl = p.b.block_table + (int64_t)r * p.b.max_blocks;
+  int ids_next = warp == NW && lane < p.b.max_blocks ? tbl[lane] : 0;
   const Stream sm = stream_of(p, r);
   __syncthreads();
+  if (blockIdx.x == 0 && warp < NW) record_batch(p, NW * 32);  // (while the first tiles are on their way)
   if (sm.tiles == 0) return;
 
   const int slab = M.P * (ROW + SC);
@@ -67,9 +67,8 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
     bool ok = true;
     // K and V of two tiles at a time, a lane per page: waiting for a slot costs a few hundred cycles, and these waits overlap
     const int i = lane % ppt, kv = lane / ppt & 1, ahead = lane / (2 * ppt);
-    const int32_t* tbl = p.b.block_table + (int64_t)r * p.b.max_blocks;
     const int n_pages = (sm.end + M.P - 1) / M.P;  // (0: a request without keys)
-    int ids_next = lane < n_pages ? tbl[lane] : 0, ids = 0;
+    int ids = 0;
     for (int j = 0; j < sm.tiles; j += 2) {
       if ((j * ppt & 31) == 0) {
         ids = ids_next;

@@ -442,8 +442,8 @@ __global__ void __launch_bounds__(kThreads) pages_compact_kernel(const PagesComp
       if (page >= total || at >= p.max_moves) break;
       p.move_dst[at] = page;
     }
-    // live pages from there on, counted from the highest
-    if (page0 + 31 >= total)
+    // live pages from there on, counted from the highest (most words have none of the first max_moves)
+    if (page0 + 31 >= total && total - (before + __popc(live)) < p.max_moves)
       for (uint32_t bits = live; bits; bits &= bits - 1) {
         const int b = __ffs(bits) - 1, page = page0 + b;
         const int at = total - 1 - (before + __popc(live & ((1u << b) - 1)));
