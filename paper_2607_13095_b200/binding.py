@@ -479,14 +479,14 @@ def _packed_rows(call, what, h: Handle, layer: PackedLayer, batch: Batch, k: tor
     _check(call(h.ptr, layer.ref, batch.ref, k_at, v_at, _raw_stream(dev)), what)
 
 
+_is_contiguous, _get_device, _data_ptr, _INT32 = torch.Tensor.is_contiguous, torch.Tensor.get_device, torch.Tensor.data_ptr, {torch.int32}
+
+
 def _int_ptrs(dev: int, *tensors):
     """_ptrs of int32 tensors."""
-    at, i32 = [], torch.int32
-    for t in tensors:
-        if t.dtype != i32 or t.get_device() != dev or not t.is_contiguous():
-            raise AssertionError("device tensors must be contiguous int32 CUDA tensors on the current device")
-        at.append(t.data_ptr())
-    return at
+    if not (all(map(_is_contiguous, tensors)) and set(map(_get_device, tensors)) == {dev} and {t.dtype for t in tensors} == _INT32):
+        raise AssertionError("device tensors must be contiguous int32 CUDA tensors on the current device")
+    return map(_data_ptr, tensors)
 
 
 def hswa_packed_append(h: Handle, layer: PackedLayer, batch: Batch, k_new: torch.Tensor, v_new: torch.Tensor):
@@ -530,8 +530,8 @@ def hswa_pages_fork(h: Handle, ref, ref_out, table, held, parent, length, need, 
     _need(held.numel() >= rows_in and min(parent.numel(), length.numel(), need.numel(), held_out.numel(), copy_src.numel(), copy_dst.numel()) >= rows_out,
           "fewer entries than rows")
     dev = _device()
-    ref_at, ref_out_at, held_at, table_at, *rest = _int_ptrs(dev, ref, ref_out, held, table, parent, length, need, table_out, held_out, copy_src, copy_dst)
-    parent_at, len_at, need_at, table_out_at, held_out_at, src_at, dst_at = rest
+    ref_at, ref_out_at, held_at, table_at, parent_at, len_at, need_at, table_out_at, held_out_at, src_at, dst_at = _int_ptrs(
+        dev, ref, ref_out, held, table, parent, length, need, table_out, held_out, copy_src, copy_dst)
     ws_at, = _ptrs(dev, workspace)
     _check(load().hswa_pages_fork(h.ptr, pages, ref_at, ref_out_at, rows_in, held_at, table_at, blocks, rows_out, parent_at, len_at, need_at,
                                   table_out_at, out_blocks, held_out_at, src_at, dst_at, ws_at, workspace.numel() * workspace.element_size(),
