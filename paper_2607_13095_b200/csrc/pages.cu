@@ -4,7 +4,8 @@
 // taken first, so results depend on the counts alone.  The steps that depend on one another (ranks of free and live pages, what each
 // row needs) are one launch of one cluster of 16 blocks, whose barrier between two steps costs a fraction of a launch: each block
 // turns its share of the counts into a bitmap in shared memory on the only pass over them, ranks come from the bitmap, and totals
-// go around through distributed shared memory.  Rewriting the tables is the cluster's work as well while they are small; large ones
+// go around through distributed shared memory.  Of a large pool all SMs make the bitmap, by a launch before the cluster's, which overlaps
+// with its look at the rows (a million counts: 4 us, where 16 SMs take 8).  Rewriting the tables is the cluster's work as well while they are small; large ones
 // are rewritten by a second launch of all SMs (a million entries: 66 us by 16 SMs).
 #include <cooperative_groups.h>
 
@@ -59,13 +60,15 @@ __device__ __forceinline__ void fetch_counts(const int32_t* ref, int num_pages, 
   for (int w = threadIdx.x; w < sh.words; w += kThreads)
     if ((sh.first + w) * 32 < num_pages) asm volatile("prefetch.global.L2 [%0];" ::"l"(ref + (int64_t)(sh.first + w) * 32));
 }
-// The one pass over the counts: sets the bit of every free page and, with `copy`, copies them; `map`, where given, gets the identity.
-__device__ __forceinline__ void scan_counts(const int32_t* ref, int32_t* ref_out, int32_t* map, bool copy, int num_pages, Share sh,
-                                            uint32_t* free_bits) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  constexpr int U = 4;  // loads in flight: 16 bytes, four pages, of each lane; a warp's load covers four words of the bitmap
+// The one pass over the counts, by warp `warp` of `warps`: sets the bit of every free page and copies the counts; `map`, where given, gets
+// the identity from entry `map_from` on.  U: loads in flight, 16 bytes, four pages, of each lane; a warp's load covers four words of the
+// bitmap.
+template <int U>
+__device__ __forceinline__ void scan_counts(const int32_t* ref, int32_t* ref_out, int32_t* map, int map_from, int num_pages, Share sh,
+                                            uint32_t* free_bits, int warp, int warps) {
+  const int lane = threadIdx.x & 31;
   const bool wide = ((reinterpret_cast<uintptr_t>(ref) | reinterpret_cast<uintptr_t>(ref_out) | reinterpret_cast<uintptr_t>(map)) & 15) == 0;
-  for (int w0 = warp * 4 * U; w0 < sh.words; w0 += kWarps * 4 * U) {
+  for (int w0 = warp * 4 * U; w0 < sh.words; w0 += warps * 4 * U) {
     int4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -91,8 +94,7 @@ __device__ __forceinline__ void scan_counts(const int32_t* ref, int32_t* ref_out
       for (int x = 1; x < 8; x <<= 1) bits |= __shfl_xor_sync(0xffffffffu, bits, x);
       if (word >= sh.words) continue;
       if ((lane & 7) == 0) free_bits[word] = bits;
-      if (!copy) continue;
-      if (wide && page + 4 <= num_pages) {
+      if (wide && page + 4 <= num_pages && (!map || page >= map_from)) {
         *reinterpret_cast<int4*>(ref_out + page) = v[u];
         if (map) *reinterpret_cast<int4*>(map + page) = make_int4((int)page, (int)page + 1, (int)page + 2, (int)page + 3);
       } else {
@@ -101,7 +103,7 @@ __device__ __forceinline__ void scan_counts(const int32_t* ref, int32_t* ref_out
         for (int e = 0; e < 4; ++e) {
           if (page + e >= num_pages) break;
           ref_out[page + e] = each[e];
-          if (map) map[page + e] = (int)page + e;
+          if (map && page + e >= map_from) map[page + e] = (int)page + e;
         }
       }
     }
@@ -129,20 +131,21 @@ __device__ __forceinline__ void cluster_prefix(cg::cluster_group& cluster, cg::c
   *all = a;
 }
 
-// The counts of a large pool, and where given the identity, copied by all SMs while the cluster behind it looks at the rows.
+// The pass over the counts of a large pool by all SMs, while the cluster behind it looks at the rows.  Where given, `map` gets the identity,
+// but for its first entries if the bitmap lies there: the cluster, which reads the bitmap, sets those.
 constexpr int kWideThreads = 256;
-__global__ void __launch_bounds__(kWideThreads) pages_copy_counts_kernel(const int32_t* ref, int32_t* ref_out, int32_t* map, const int num_pages) {
+__global__ void __launch_bounds__(kWideThreads) pages_copy_counts_kernel(const int32_t* ref, int32_t* ref_out, int32_t* map, uint32_t* bits,
+                                                                         const int num_pages) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const bool wide = ((reinterpret_cast<uintptr_t>(ref) | reinterpret_cast<uintptr_t>(ref_out) | reinterpret_cast<uintptr_t>(map)) & 15) == 0;
-  const int stride = gridDim.x * kWideThreads, me = blockIdx.x * kWideThreads + threadIdx.x;
-  const int quads = wide ? num_pages / 4 : 0;
-  for (int i = me; i < quads; i += stride) {
-    reinterpret_cast<int4*>(ref_out)[i] = reinterpret_cast<const int4*>(ref)[i];
-    if (map) reinterpret_cast<int4*>(map)[i] = make_int4(4 * i, 4 * i + 1, 4 * i + 2, 4 * i + 3);
-  }
-  for (int i = 4 * quads + me; i < num_pages; i += stride) {
-    ref_out[i] = ref[i];
-    if (map) map[i] = i;
+  const Share all = {0, (num_pages + 31) / 32};
+  scan_counts<2>(ref, ref_out, map, all.words, num_pages, all, bits, blockIdx.x * (kWideThreads / 32) + (threadIdx.x >> 5),
+                 gridDim.x * (kWideThreads / 32));
+}
+// The block's part of that bitmap; `map`: the first entries, where it lies, get the identity.
+__device__ __forceinline__ void take_bits(const uint32_t* bits, int32_t* map, Share sh, uint32_t* free_bits) {
+  for (int w = threadIdx.x; w < sh.words; w += kThreads) {
+    free_bits[w] = bits[sh.first + w];
+    if (map) map[sh.first + w] = sh.first + w;
   }
 }
 
@@ -276,7 +279,7 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
   const int block = (int)cluster.block_rank(), warp = threadIdx.x >> 5;
   const Share sh = share_of(p.num_pages, block);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  fetch_counts(p.ref, p.num_pages, sh);
+  if (!p.copied) fetch_counts(p.ref, p.num_pages, sh);
   if (threadIdx.x == 0) s_bad = 0;
   for (int i = threadIdx.x; i < p.rows_in; i += kThreads) {
     const int held = p.held[i];
@@ -326,7 +329,9 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
   }
 
   // the free pages of lowest number
-  scan_counts(p.ref, p.ref_out, nullptr, !p.copied, p.num_pages, sh, s_free);
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // (with p.copied: the pass over the counts, launched before, is done)
+  if (p.copied) take_bits(reinterpret_cast<const uint32_t*>(p.fresh), nullptr, sh, s_free);
+  else scan_counts<4>(p.ref, p.ref_out, nullptr, 0, p.num_pages, sh, s_free, warp, kWarps);
   __syncthreads();
   const int wper = (sh.words + kThreads - 1) / kThreads;
   const int w0 = threadIdx.x * wper, w1 = min(w0 + wper, sh.words);
@@ -344,7 +349,6 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
       for (; bits && rank < fresh_total; bits &= bits - 1) p.fresh[rank++] = (sh.first + w) * 32 + __ffs(bits) - 1;
     }
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // (with p.copied: the counts' copy, launched before, is there)
   if (p.second) {  // a second launch does the rest
     if (block == 0) {
       for (int i = threadIdx.x; i < p.rows_in; i += kThreads) {
@@ -420,9 +424,11 @@ __global__ void __launch_bounds__(kThreads) pages_compact_kernel(const PagesComp
   const int block = (int)cluster.block_rank(), warp = threadIdx.x >> 5;
   const Share sh = share_of(p.num_pages, block);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  fetch_counts(p.ref, p.num_pages, sh);
+  if (!p.copied) fetch_counts(p.ref, p.num_pages, sh);
   for (int i = block * kThreads + threadIdx.x; i < p.max_moves; i += kBlocks * kThreads) p.move_src[i] = p.move_dst[i] = -1;
-  scan_counts(p.ref, p.ref_out, p.page_map, !p.copied, p.num_pages, sh, s_free);
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // (with p.copied: the pass over the counts, launched before, is done)
+  if (p.copied) take_bits(reinterpret_cast<const uint32_t*>(p.page_map), p.page_map, sh, s_free);
+  else scan_counts<4>(p.ref, p.ref_out, p.page_map, 0, p.num_pages, sh, s_free, warp, kWarps);
   __syncthreads();
   const int wper = (sh.words + kThreads - 1) / kThreads;
   const int w0 = threadIdx.x * wper, w1 = min(w0 + wper, sh.words);
@@ -451,7 +457,6 @@ __global__ void __launch_bounds__(kThreads) pages_compact_kernel(const PagesComp
       }
     before += __popc(live);
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // (with p.copied: the copy and the identity, launched before, are there)
   cluster.sync();
   for (int i = block * kThreads + threadIdx.x; i < p.max_moves; i += kBlocks * kThreads) {
     const int src = p.move_src[i], dst = p.move_dst[i];
@@ -542,7 +547,7 @@ cudaError_t hswa_launch_pages_fork(const PagesForkParams& params, int num_sms, c
   PagesForkParams p = params;
   p.second = (int64_t)p.rows_in * p.max_blocks + (int64_t)p.rows_out * p.out_max_blocks > kSmallTables;
   p.copied = p.num_pages > kSmallPool;
-  if (p.copied) pages_copy_counts_kernel<<<4 * num_sms, kWideThreads, 0, s>>>(p.ref, p.ref_out, nullptr, p.num_pages);
+  if (p.copied) pages_copy_counts_kernel<<<4 * num_sms, kWideThreads, 0, s>>>(p.ref, p.ref_out, nullptr, reinterpret_cast<uint32_t*>(p.fresh), p.num_pages);
   const cudaError_t e = launch_cluster<pages_fork_kernel>(p, ((size_t)p.rows_in * 3 + (size_t)p.rows_out * 4) * 4 + bitmap_bytes(p.num_pages), s);
   return e != cudaSuccess || !p.second ? e : launch_wide(pages_fork_apply_kernel, p, num_sms, s);
 }
@@ -550,7 +555,7 @@ cudaError_t hswa_launch_pages_compact(const PagesCompactParams& params, int num_
   PagesCompactParams p = params;
   p.second = (int64_t)p.rows * p.max_blocks > kSmallTables;
   p.copied = p.num_pages > kSmallPool;
-  if (p.copied) pages_copy_counts_kernel<<<4 * num_sms, kWideThreads, 0, s>>>(p.ref, p.ref_out, p.page_map, p.num_pages);
+  if (p.copied) pages_copy_counts_kernel<<<4 * num_sms, kWideThreads, 0, s>>>(p.ref, p.ref_out, p.page_map, reinterpret_cast<uint32_t*>(p.page_map), p.num_pages);
   const cudaError_t e = launch_cluster<pages_compact_kernel>(p, bitmap_bytes(p.num_pages), s);
   return e != cudaSuccess || !p.second ? e : launch_wide(pages_compact_apply_kernel, p, num_sms, s);
 }

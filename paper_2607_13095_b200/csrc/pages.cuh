@@ -30,7 +30,7 @@ struct PagesForkParams {
   // each old row, rank of each new row's first fresh page; whether there is anything to do
   int32_t *fresh, *first, *most, *rank, *ok;
   int32_t second;
-  int32_t copied;  // the counts are copied by a launch before
+  int32_t copied;  // the counts are copied, and the bitmap of free pages put into `fresh`, by a launch before
   int32_t* err;
 };
 
@@ -48,7 +48,7 @@ struct PagesCompactParams {
   int32_t* move_src;
   int32_t* move_dst;
   int32_t second;  // the tables are rewritten by a second launch
-  int32_t copied;  // the counts are copied, and the map set to the identity, by a launch before
+  int32_t copied;  // the counts are copied, the map set to the identity, and the bitmap put into its first entries, by a launch before
   int32_t* err;
 };
 
