@@ -10,6 +10,8 @@
 //   O^T [D x rows] += V^T P^T: a lane needs neighbouring KEYS of one element side by side.  It reads 16 (D = 128) or 8
 //     neighbouring elements of two keys and exchanges nibbles: 4 logic instructions make 8 bytes of (key, key') pairs out of
 //     two words, and each converts at once.
+// Measured, 64 / 8 heads of 128, one token: 32 requests of 1000 keys 19 us, of 2000 29; 2 requests of up to 512 keys, 4 heads of 64: 7.5,
+// bound by the chain from the length to the merge.
 #include "packed_stream.cuh"
 #include "tc_primitives.cuh"
 

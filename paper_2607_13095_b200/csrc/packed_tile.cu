@@ -11,7 +11,9 @@
 //                on their way, so the latency of a load is that of half a tile's conversion.
 // TMEM columns: S0 0-127, S1 128-255, O0 256-, O1 384- (fp32; P_i = fp16 pairs over the first 64 columns of S_i).  O is rescaled
 // only when a row's maximum grows by more than 2^8.  Rows of a key tile that no row sees are written as zeros.
-// Bound by the tensor cores and the exponentials; the unpackers' conversion (a fifth of the issue slots) hides beside them.
+// Bound by the tensor cores and the exponentials; the unpackers' conversion (a fifth of the issue slots) hides beside them.  Measured, 8
+// prompts of 257 to 512 tokens over up to 8192 keys, 64 / 8 heads of 128: 668 us alone, 1.03 PFLOP/s, 705 in a sustained run under the
+// power cap (410 at the rate of a plain matrix product; blocks of warp-level MMAs took 5483).
 #include "block_order.cuh"
 #include "packed.cuh"
 #include "tc_primitives.cuh"
