@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
   cg::cluster_group cluster = cg::this_cluster();
   auto started = cluster.barrier_arrive();
   extern __shared__ int32_t s_mem[];
-  __shared__ int s_warp[kWarps], s_counts[kBlocks], s_bad;
+  __shared__ int s_warp[kWarps], s_counts[kBlocks];
   int32_t* s_first = s_mem;                 // [rows_in] first child
   int32_t* s_most = s_first + p.rows_in;    // [rows_in] most pages that a child shares
   int32_t* s_held = s_most + p.rows_in;     // [rows_in]
@@ -282,14 +282,14 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
   const Share sh = share_of(p.num_pages, block);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (!p.copied) fetch_counts(p.ref, p.num_pages, sh);
-  if (threadIdx.x == 0) s_bad = 0;
+  bool bad = false;
   for (int i = threadIdx.x; i < p.rows_in; i += kThreads) {
     const int held = p.held[i];
     s_first[i] = INT32_MAX;
     s_most[i] = 0;
     s_held[i] = held;
     if (held < 0 || held > p.max_blocks) {
-      s_bad = 1;
+      bad = true;
       if (block == 0) record_error(p.err, HSWA_ERR_BOUNDS, i, -1, held);
     }
   }
@@ -298,22 +298,21 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
     s_len[r] = p.len[r];
     s_need[r] = p.need[r];
   }
-  __syncthreads();
-  // every block looks at all rows: none waits for another
+  // every block looks at all rows, so none waits for another, and all come to the same answer: the votes are barriers as well
+  bad = __syncthreads_or(bad);
   for (int r = threadIdx.x; r < p.rows_out; r += kThreads) {
     const int parent = s_parent[r], len = s_len[r], need = s_need[r];
     bool ok = parent >= -1 && parent < p.rows_in && len >= 0 && pages_of(max(len, need), p.page_size) <= p.out_max_blocks;
     if (ok) ok = parent < 0 ? len == 0 : pages_of(len, p.page_size) <= s_held[parent];
     if (!ok) {
-      s_bad = 1;
+      bad = true;
       if (block == 0) record_error(p.err, HSWA_ERR_BOUNDS, r, -2, parent);
     } else if (parent >= 0) {
       atomicMin(&s_first[parent], r);
       atomicMax(&s_most[parent], len / p.page_size);
     }
   }
-  __syncthreads();
-  const bool rows_ok = s_bad == 0;
+  const bool rows_ok = !__syncthreads_or(bad);
   int fresh_total = 0;
   if (rows_ok) {
     const int per = (p.rows_out + kThreads - 1) / kThreads;

@@ -1,0 +1,34 @@
+"""Page calls where they can go wrong: arguments out of range anywhere among many rows, tables without places, the launches of large pools and
+large tables together, arrays off 16 bytes, handles side by side."""
+import numpy as np
+import pytest
+import torch
+
+import packed_reference as ref
+from gpu_utils import dev_i32, make_handle
+from paper_2607_13095_b200 import binding as hb
+from test_gpu_packed import dims, no_error
+from test_gpu_pages import FILL, check_fork, children, fork, state
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("pages", [5003, 70001])
+@pytest.mark.parametrize("rows,hi", [(100, 40), (1500, 30), (100, 8000)])
+def test_fork_refuses_a_bad_number_of_pages_in_any_row(rows, hi, pages):
+    """A row that claims more pages than its table has places, or fewer than none, wherever it stands: nothing is done."""
+    P, h = 16, make_handle(dims(1, 64, 16, 1))
+    rng = np.random.default_rng(rows)
+    blocks = -(-hi // P) + 1
+    table = rng.integers(0, pages, (rows, blocks)).astype(np.int32)
+    counts = np.bincount(table.ravel(), minlength=pages).astype(np.int32)
+    parent = np.arange(rows, dtype=np.int32)[::-1].copy()
+    length = np.full(rows, P, np.int32)
+    for row in (0, 31, 33, 64, rows // 2, rows - 1):
+        for bad in (blocks + 1, 1 << 30, -1):
+            held = np.full(rows, blocks, np.int32)
+            held[row] = bad
+            got = fork(h, counts, table, held, parent, length, length + 1, blocks)
+            st = hb.hswa_get_async_error(h)
+            assert st == (hb.HSWA_ERR_BOUNDS, row, -1, bad), st
+            assert np.array_equal(got[0], counts) and all((g == FILL).all() for g in got[1:])
