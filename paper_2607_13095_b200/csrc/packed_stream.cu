@@ -149,9 +149,9 @@ __global__ void __launch_bounds__(kThreads, 2) packed_stream_kernel(const Packed
       phase ^= 1;
     }
   };
-  auto arrived = [&]() {  // (one poll where the copy has landed)
+  auto arrived = [&]() {  // (one poll where the copy has landed; the lanes may see it land at different polls, so each is voted on)
     const uint32_t bar = bar0 + 8 * slot;
-    if (mbar_try_wait(bar, phase)) return true;
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, phase))) return true;
     return __all_sync(0xffffffffu, mbar_wait(bar, phase)) != 0;
   };
   auto give_up = [&]() {
