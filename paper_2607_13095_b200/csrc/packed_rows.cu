@@ -366,9 +366,11 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const __grid_c
 #pragma unroll
       for (int n = 0; n < N / 2; ++n) m[n] = l[n] = make_float2(0.f, 0.f);
       const int j0 = (i + group) & 1;  // the group's first tile of the piece
-      for (int j = j0; j < count && ok; j += 2) {
+      // A wait runs out for a warp, not for its group: the loop is left at the group's votes alone, where all four warps agree, or a
+      // warp would wait at one named barrier and the others at another.
+      for (int j = j0; j < count; j += 2) {
         const int b = group, it = i + j, key = (at.tile + j) * TN + me;
-        if (ok) ok = __all_sync(0xffffffffu, wait_for(bar(B_SFULL + b), (it >> 1) & 1));
+        ok = ok & (bool)__all_sync(0xffffffffu, wait_for(bar(B_SFULL + b), (it >> 1) & 1));
         if (j == j0) mul = s_mul[pc & 3];  // (written before the MMAs that this barrier waits for)
         uint32_t v[N];
         tc_fence_after();
@@ -441,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const __grid_c
           pk[n] = pack_half2(ex.x, ex.y);
           l[n] = __fadd2_rn(l[n], ex);
         }
-        if (it >= 2 && ok) ok = __all_sync(0xffffffffu, wait_for(bar(B_PEMPTY + b), ((it >> 1) - 1) & 1));
+        if (it >= 2) ok = ok & (bool)__all_sync(0xffffffffu, wait_for(bar(B_PEMPTY + b), ((it >> 1) - 1) & 1));
         uint8_t* prow = smem + L::OFF_P + b * P_BYTES;
 #pragma unroll
         for (int q = 0; q < N / 8; ++q)

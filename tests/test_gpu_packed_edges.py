@@ -15,7 +15,7 @@ pytestmark = pytest.mark.gpu
 class Filled:
     """A cache of many requests whose pages are filled on the GPU: random codes, scales between 2^-3 and 2^2."""
 
-    def __init__(self, d, ctx, n, seed):
+    def __init__(self, d, ctx, n, seed, sm_scale=0.0):
         P, D, H = d.page_size, d.head_dim, d.num_kv_heads
         g = torch.Generator(device="cuda").manual_seed(seed)
         used = [-(-(c + n) // P) for c in ctx]
@@ -28,7 +28,7 @@ class Filled:
         for r, u in enumerate(used):
             table[r, :u] = perm[at:at + u]
             at += u
-        self.h, self.n, self.B = make_handle(d, torch.float32), n, B
+        self.h, self.n, self.B = make_handle(d, torch.float32, sm_scale), n, B
         self.layer = hb.PackedLayer(pool, 0.5, 1.0)
         self.q = torch.randn((B * n, d.num_q_heads, D), generator=g, device="cuda", dtype=torch.bfloat16)
         self.batch = hb.Batch(dev_i32(ctx), table, *no_rings(d, B), dev_i32(np.arange(B + 1) * n), max_q_len=n, total_q=B * n, max_ctx_len=max(ctx))
@@ -47,6 +47,21 @@ def test_full_machines_of_single_tokens_repeat_themselves(d):
     with several copies a tile, give the same bits whenever they run."""
     rng = np.random.default_rng(1)
     c = Filled(d, [int(x) for x in rng.integers(1000, 9000, 48)], 1, seed=2)
+    first = c.run()
+    assert torch.isfinite(first[0]).all() and torch.isfinite(first[1]).all()
+    for _ in range(20):
+        again = c.run()
+        assert all(torch.equal(x, y) for x, y in zip(first, again))
+    no_error(c.h)
+
+
+@pytest.mark.parametrize("sm_scale", [0.0, 2.0])
+@pytest.mark.parametrize("d,n", [(dims(8, 128, 64, 4), 2), (dims(8, 128, 16, 4), 4), (dims(8, 64, 32, 4), 4), (dims(3, 64, 64, 4), 5)])
+def test_full_machines_of_drafts_repeat_themselves(d, n, sm_scale):
+    """Runs of many pieces, in which two groups of warps take turns and vote on their maxima tile by tile (with the larger scale, maxima grow
+    all along): the same bits whenever they run, and no wait runs out."""
+    rng = np.random.default_rng(3)
+    c = Filled(d, [int(x) for x in rng.integers(100, 9000, 48)], n, seed=4, sm_scale=sm_scale)
     first = c.run()
     assert torch.isfinite(first[0]).all() and torch.isfinite(first[1]).all()
     for _ in range(20):
