@@ -563,7 +563,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const __grid_c
       int i = 0;
       for (int pc = 0; at.left > 0 && ok; ++pc) {
         const int count = at.count(), buf = pc & 1;
-        ok = wait_for(bar(B_QFULL + buf), (pc >> 1) & 1);
+        ok = __all_sync(0xffffffffu, wait_for(bar(B_QFULL + buf), (pc >> 1) & 1));
         const uint64_t dq = smem_desc(sbase + L::OFF_Q + buf * L::Q_BYTES, 16);
         for (int j = 0; j < count && ok; ++j, ++i) {
           const int stage = i % K_STAGES, b = i & 1;
@@ -594,7 +594,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const __grid_c
       const uint64_t dv0 = smem_desc(sbase + L::OFF_V, HALF_BYTES), dp0 = smem_desc(sbase + L::OFF_P, HALF_BYTES);
       for (int pc = 0; at.left > 0 && ok; ++pc) {
         const int count = at.count(), buf = pc & 1;
-        if (pc >= 2) ok = wait_for(bar(B_OFREE + 2 * buf), ((pc >> 1) - 1) & 1) && wait_for(bar(B_OFREE + 2 * buf + 1), ((pc >> 1) - 1) & 1);
+        if (pc >= 2)
+          ok = __all_sync(0xffffffffu, wait_for(bar(B_OFREE + 2 * buf), ((pc >> 1) - 1) & 1) && wait_for(bar(B_OFREE + 2 * buf + 1), ((pc >> 1) - 1) & 1));
         for (int j = 0; j < count && ok; ++j, ++i) {
           const int stage = i % V_STAGES, b = i & 1;
           ok = wait_for(bar(B_VFULL + stage), (i / V_STAGES) & 1) && wait_for(bar(B_PFULL + b), (i >> 1) & 1);

@@ -48,8 +48,9 @@ __global__ void __launch_bounds__(kThreads, 1) packed_tile_kernel(const PackedAt
   constexpr uint32_t IDESC_O = (IDESC_S & ~(0x3fu << 17)) | ((uint32_t)(D >> 3) << 17) | (1u << 16);  // B (= V) is [key][d], d contiguous
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + OFF_STATE);
   uint32_t& tmem_base_slot = *reinterpret_cast<uint32_t*>(smem + OFF_STATE + 160);
-  int& mma_abort = *reinterpret_cast<int*>(smem + OFF_STATE + 164);
+  int& failed = *reinterpret_cast<int*>(smem + OFF_STATE + 164);
   int* picked = reinterpret_cast<int*>(smem + OFF_STATE + 168);
+  int* issuer_stop = reinterpret_cast<int*>(smem + OFF_STATE + 176);  // [2] an MMA issuer is to stop: a wait ran out
   const uint32_t sbase = smem_u32(smem);
   const ModelParams& M = p.m;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -79,17 +80,18 @@ __global__ void __launch_bounds__(kThreads, 1) packed_tile_kernel(const PackedAt
     if (lane == 0) {
       picked[0] = pr;
       picked[1] = pb;
+      issuer_stop[0] = issuer_stop[1] = 0;
       // an earlier block gave up: do not queue behind it
-      mma_abort = *reinterpret_cast<volatile int32_t*>(p.err) == HSWA_ERR_TIMEOUT;
+      failed = *reinterpret_cast<volatile int32_t*>(p.err) == HSWA_ERR_TIMEOUT;
       if (sbase & 1023u) {  // the swizzled tiles need a 1 KB-aligned window
         record_error(p.err, HSWA_ERR_CUDA, -1, (int)(sbase & 1023u), 15);
-        mma_abort = 1;
+        failed = 1;
       }
     }
   }
   __syncthreads();
   const int r = picked[0], b = picked[1];
-  if (r < 0 || mma_abort) return;  // uniform for the block
+  if (r < 0 || failed) return;  // uniform for the block
   const int t0 = p.b.q_indptr[r], n_all = p.b.q_indptr[r + 1] - t0, n = min(n_all, p.max_q_len);
   auto has_row = [&](int tok) { return (unsigned)t0 + (unsigned)tok < (unsigned)p.total_q; };
   const int tok0 = b * 2 * tok_tile, tok_end = min(n, tok0 + 2 * tok_tile);
@@ -237,7 +239,17 @@ __global__ void __launch_bounds__(kThreads, 1) packed_tile_kernel(const PackedAt
     // ======================= MMA issuers =======================
     if (warp - W_MMA < q_tiles) {
       const int i = warp - W_MMA;
-      bool ok = mbar_wait(bar(BAR_Q), 0);
+      // A wait may run out for some lanes of the warp alone, so none leaves by itself: it sets its warp's flag, and the warp leaves
+      // behind the next barrier, where all lanes read the same.  The other issuer's flag is set with the token in hand.  (Votes on
+      // the waits: 697 us against 672.)
+      volatile int *stop = &issuer_stop[i], *stop_other = &issuer_stop[1 - i];
+      auto await = [&](int which, uint32_t parity) {
+        if (mbar_wait(bar(which), parity)) return true;
+        record_error(p.err, HSWA_ERR_TIMEOUT, r, b, 62 + i);
+        *stop = 1;
+        return false;  // (of use to leave out waits behind it)
+      };
+      const bool q_here = await(BAR_Q, 0);
       const uint64_t dQ = smem_desc(sbase + OFF_Q + i * TILE_BYTES, 16);
       const uint64_t dK0 = smem_desc(sbase + OFF_K, 16), dV0 = smem_desc(sbase + OFF_V, HALF_BYTES);
       auto issue_S = [&](int stage) {
@@ -267,51 +279,45 @@ __global__ void __launch_bounds__(kThreads, 1) packed_tile_kernel(const PackedAt
         __syncwarp();
       };
       // [PV0(j), S0(j+1)] [PV1(j), S1(j+1)] ...: a token goes around through two named barriers.  An issuer leaves the loop only
-      // right after passing the token, and passes it whenever it finds the abort flag set, so neither waits forever.
+      // right after passing the token, and passes it when it finds its flag set, so neither waits forever.  (A wait that runs
+      // out with the token in hand is found at the next turn; the products until then are of a call that has failed.)
       const int tok_in = i == 0 ? 2 : 1, tok_out = i == 0 ? 1 : 2;
       auto token_wait = [&]() {
         if (q_tiles == 2) asm volatile("bar.sync %0, 64;" ::"r"(tok_in) : "memory");
+        else __syncwarp();
       };
       auto token_pass = [&]() {
         if (q_tiles == 1) return;
         __threadfence_block();
         asm volatile("bar.arrive %0, 64;" ::"r"(tok_out) : "memory");
       };
-      volatile int* abort_flag = &mma_abort;
-      if (ok) ok = mbar_wait(bar(BAR_KFULL + 0), 0);
+      if (q_here) await(BAR_KFULL + 0, 0);
       if (i == 1) token_wait();
-      if (!ok) *abort_flag = 1;
-      if (ok && *abort_flag == 0) issue_S(0);
+      else __syncwarp();
+      if (*stop != 0) *stop_other = 1;
+      else issue_S(0);
       token_pass();
-      bool done = !ok || *abort_flag != 0;
-      for (int j = 0; j < n_tiles && !done; ++j) {
+      for (int j = 0; j < n_tiles; ++j) {
         const int stage = j % STAGES, nstage = (j + 1) % STAGES;
         const bool more = j + 1 < n_tiles;
         // polled during the other issuer's turn
-        ok = mbar_wait(bar(BAR_VFULL + stage), (j / STAGES) & 1) && mbar_wait(bar(BAR_PFULL + P_PARTS * i), j & 1);
-        if (ok && more) ok = mbar_wait(bar(BAR_KFULL + nstage), ((j + 1) / STAGES) & 1);
+        if (await(BAR_VFULL + stage, (j / STAGES) & 1) && await(BAR_PFULL + P_PARTS * i, j & 1) && more) await(BAR_KFULL + nstage, ((j + 1) / STAGES) & 1);
         token_wait();
-        if (!ok) *abort_flag = 1;
-        if (*abort_flag != 0) {
+        if (*stop != 0) {
+          *stop_other = 1;
           token_pass();
           break;
         }
 #pragma unroll
         for (int q = 0; q < P_PARTS; ++q) {
-          if (q > 0 && ok) ok = mbar_wait(bar(BAR_PFULL + P_PARTS * i + q), j & 1);
-          if (ok) issue_PV(stage, q, j == 0);
+          if (q > 0) await(BAR_PFULL + P_PARTS * i + q, j & 1);
+          issue_PV(stage, q, j == 0);
         }
-        if (ok) {
-          if (elect_one()) tc_commit(bar(BAR_VEMPTY + stage));
-          __syncwarp();
-          if (more) issue_S(nstage);
-        } else {
-          *abort_flag = 1;
-          done = true;
-        }
+        if (elect_one()) tc_commit(bar(BAR_VEMPTY + stage));
+        __syncwarp();
+        if (more) issue_S(nstage);
         token_pass();
       }
-      if (!ok && lane == 0) record_error(p.err, HSWA_ERR_TIMEOUT, r, b, 62 + i);
       if (elect_one()) tc_commit(bar(BAR_OFINAL + i));
       __syncwarp();
     }
@@ -488,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_tile_kernel(const PackedAt
   tc_fence_before();
   __syncthreads();
   if (warp == W_MMA) {
-    if (mma_abort) __nanosleep(100000);  // (MMAs in flight that nobody waited for)
+    if (issuer_stop[0] || issuer_stop[1]) __nanosleep(100000);  // (MMAs in flight that nobody waited for)
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TM_COLS) : "memory");
   }

@@ -68,3 +68,16 @@ def test_full_machines_of_drafts_repeat_themselves(d, n, sm_scale):
         again = c.run()
         assert all(torch.equal(x, y) for x, y in zip(first, again))
     no_error(c.h)
+
+
+@pytest.mark.parametrize("d,n", [(dims(8, 128, 64, 4), 150), (dims(5, 64, 16, 4), 70)])
+def test_full_machines_of_prompts_repeat_themselves(d, n):
+    """Blocks of one and of two Q tiles, whose MMA issuers pass a token: the same bits whenever they run, and no wait runs out."""
+    rng = np.random.default_rng(5)
+    c = Filled(d, [int(x) for x in rng.integers(0, 3000, 24)], n, seed=6)
+    first = c.run()
+    assert torch.isfinite(first[0]).all() and torch.isfinite(first[1]).all()
+    for _ in range(10):
+        again = c.run()
+        assert all(torch.equal(x, y) for x, y in zip(first, again))
+    no_error(c.h)
