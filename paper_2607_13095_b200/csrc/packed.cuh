@@ -112,6 +112,17 @@ __device__ __forceinline__ void mma_f16_16816_zero(float (&c)[4], uint32_t a0, u
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
+// Probabilities enter the PV product as fp16, whose 11 bits are rounding enough for outputs in bf16, but whose exponents end at 2^-24: they
+// are taken relative to a base 2^7 below the row's maximum, and the base moves when a score passes it by more than 2^15, the most that
+// fp16 holds.  What a key adds is then off by 2^-11 of itself or, below 2^-21 of the row's largest, by 2^-32 of that.  (Relative to the
+// maximum itself, 2^-25: a million keys 25 bits below one of them would lose 3 % of the row's weight.)  The base of a tile's largest score `top`
+// (times `mul`, in log2 units), and whether a row moves to it; the 2^-22 covers the roundings of large scores.
+constexpr float kBaseBelowMax = 7.f, kMostAboveBase = 15.f;
+__device__ __forceinline__ float base_of(float top, float mul) { return fmaf(top, mul, -kBaseBelowMax); }
+__device__ __forceinline__ bool base_moves(float to, float from) {
+  return fmaf(fabsf(to), 0x1p-22f, to) > from + (kMostAboveBase - kBaseBelowMax);  // (never to minus infinity)
+}
+
 // Queries enter the products as fp16, each row times a power of two that brings its largest element to [2^14, 2^15): fp16
 // has three bits more than bf16, so only elements below 2^-28 of the largest lose any.  From the largest magnitude, infinities and
 // NaN apart, the power and its inverse.

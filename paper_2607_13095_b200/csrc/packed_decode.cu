@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
         __syncwarp();
         if (lane == 0) mbar_arrive(empty0 + 8 * k_slot);
       }
-      // masks, the running maximum of each row (column of S^T) in log2 units
+      // masks, the running base of each row (column of S^T) in log2 units
       if (masked) {
 #pragma unroll
         for (int c = 0; c < NT; ++c)
@@ -258,10 +258,9 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 1 : 2) packed_decode_kerne
           mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], sh));
           mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], sh));
         }
-        mx[0] *= mul[c][0];
-        mx[1] *= mul[c][1];
-        // O moves to a new maximum only when that grew by more than 2^8 (P stays within fp16)
-        const bool grow0 = mx[0] > m[c][0] + 8.f, grow1 = mx[1] > m[c][1] + 8.f;
+        mx[0] = base_of(mx[0], mul[c][0]);
+        mx[1] = base_of(mx[1], mul[c][1]);
+        const bool grow0 = base_moves(mx[0], m[c][0]), grow1 = base_moves(mx[1], m[c][1]);
         if (__any_sync(0xffffffffu, grow0 || grow1)) {
           const float al0 = grow0 ? fast_exp2(m[c][0] - mx[0]) : 1.f, al1 = grow1 ? fast_exp2(m[c][1] - mx[1]) : 1.f;
           if (grow0) m[c][0] = mx[0];

@@ -11,8 +11,8 @@
 //          the same)
 //   4-7    unpack V into swizzled shared memory
 //   8-15   softmax, two groups of four warps with every second tile, each with maxima, sums and an accumulator of O of its own: TMEM
-//          lane = key; a lane has N scores of its key.  The rows' maxima are kept from tile to tile and moved only when a score passes
-//          one by more than 2^8, which a vote over the four warps finds out; row sums stay in the lanes to the end
+//          lane = key; a lane has N scores of its key.  The rows' bases (packed.cuh) are kept from tile to tile and moved only when a score passes
+//          one by more than 2^15, which a vote over the four warps finds out; row sums stay in the lanes to the end
 //   16-19  issue the MMAs of S, issue those of O, bring Q of the next stream, and fetch the tiles to come into a ring (a TMA load for
 //          both slabs of a page)
 // HBM would allow 790 clocks a tile at a head dim of 128; a tile takes 1300 with 16 columns and 1600 with 32, bound by the chain of
@@ -52,7 +52,7 @@ struct Smem {
   static constexpr int OFF_V = 0, OFF_P = V_STAGES * V_BYTES, OFF_Q = OFF_P + 2 * P_BYTES, OFF_RING = OFF_Q + 2 * Q_BYTES;
   static constexpr int OFF_STATE = OFF_RING + RING * 2 * PACKED;
   static_assert(OFF_RING % 128 == 0 && PACKED % 128 == 0, "TMA destinations");
-  static constexpr int GROUP_STATE = 6 * N * 4;  // of a softmax group: maxima by warp [4][N], rows' maxima [N], factors of O [N]
+  static constexpr int GROUP_STATE = 6 * N * 4;  // of a softmax group: bases by warp [4][N], of the rows [N], factors of O [N]
   static constexpr int OFF_BARS = OFF_STATE + 2 * GROUP_STATE;
   static constexpr int OFF_PLAN = OFF_BARS + NBARS * 8;  // sums [20], first request, tiles before it
   static constexpr int OFF_MISC = OFF_PLAN + 22 * 8;     // TMEM base, a spare word, multiplier [4], keys of the ring's tiles [RING]
@@ -352,9 +352,9 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const __grid_c
     const int group = (warp - W_SOFTMAX) >> 2, quad = warp & 3, me = quad * 32 + lane;  // the thread's key in the tile = its element of O
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     float* s_max = reinterpret_cast<float*>(smem + L::OFF_STATE + group * L::GROUP_STATE);  // [4][N]
-    float* s_m = s_max + 4 * N;                                                              // [N] the rows' maxima
+    float* s_m = s_max + 4 * N;                                                              // [N] the rows' bases
     float* s_alpha = s_m + N;                                                                // [N] factors of O
-    float2 m[N / 2];  // added to the scores: the rows' maxima, negative, 0 for rows without a key
+    float2 m[N / 2];  // added to the scores: the rows' bases, negative, 0 for rows without a key
     float2 l[N / 2];  // sums over the thread's keys
     bool ok = true;
     int i = 0;  // tile of the run
@@ -396,8 +396,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const __grid_c
           const float2 e = __ffma2_rn(x[n], mul2, m[n]);
           top = max3(top, e.x, e.y);
         }
-        if (softmax_any(group, j == j0 || top > 8.f || !ok)) {
-          // a row's maximum moves (or the first tile sets it): the tile's maxima over all its keys
+        if (softmax_any(group, j == j0 || top > kMostAboveBase || !ok)) {
+          // a row's base moves (or the first tile sets it): the tile's over all its keys
           if (softmax_any(group, !ok)) {
             ok = false;
             break;
@@ -405,13 +405,13 @@ __global__ void __launch_bounds__(kThreads, 1) packed_rows_kernel(const __grid_c
 #pragma unroll
           for (int n = 0; n < N; ++n) {
             const float c = warp_max(n & 1 ? x[n / 2].y : x[n / 2].x);
-            if (lane == 0) s_max[quad * N + n] = c * mul;
+            if (lane == 0) s_max[quad * N + n] = base_of(c, mul);
           }
           softmax_sync(group);
           if (quad == 0 && lane < N) {
             const float c = fmaxf(fmaxf(s_max[lane], s_max[N + lane]), fmaxf(s_max[2 * N + lane], s_max[3 * N + lane]));
             const float old = j == j0 ? -INFINITY : s_m[lane];
-            const bool grow = c > old + 8.f || j == j0;
+            const bool grow = base_moves(c, old) || j == j0;
             s_alpha[lane] = grow ? (j == j0 || c == -INFINITY ? 1.f : fast_exp2(old - c)) : 1.f;
             s_m[lane] = grow ? c : old;
           }

@@ -10,7 +10,7 @@
 //                rings of two tiles.  A lane holds 32 elements at a time; while it converts them, the same lane's next 32 are
 //                on their way, so the latency of a load is that of half a tile's conversion.
 // TMEM columns: S0 0-127, S1 128-255, O0 256-, O1 384- (fp32; P_i = fp16 pairs over the first 64 columns of S_i).  O is rescaled
-// only when a row's maximum grows by more than 2^8.  Rows of a key tile that no row sees are written as zeros.
+// only when a row's base moves (packed.cuh).  Rows of a key tile that no row sees are written as zeros.
 // Bound by the tensor cores and the exponentials; the unpackers' conversion (a fifth of the issue slots) hides beside them.  Measured, 8
 // prompts of 257 to 512 tokens over up to 8192 keys, 64 / 8 heads of 128: 668 us alone, 1.03 PFLOP/s, 705 in a sustained run under the
 // power cap (410 at the rate of a plain matrix product; blocks of warp-level MMAs took 5483).
@@ -397,11 +397,11 @@ __global__ void __launch_bounds__(kThreads, 1) packed_tile_kernel(const PackedAt
         for (int c = 0; c < 8; ++c) mx8[c] = max3(mx8[c], __uint_as_float(v[k + 2 * c]), __uint_as_float(v[k + 2 * c + 1]));
       }
       const float mx = fmaxf(fmaxf(max3(mx8[0], mx8[1], mx8[2]), max3(mx8[3], mx8[4], mx8[5])), fmaxf(mx8[6], mx8[7]));
-      const float mx_s = mx * mul;
+      const float mx_s = base_of(mx, mul);
       if (j == 0) {
         m_st = mx_s;
       } else {
-        const bool grow = mx_s > m_st + 8.f;
+        const bool grow = base_moves(mx_s, m_st);
         if (__any_sync(0xffffffffu, grow)) {
           const float m_new = grow ? mx_s : m_st;
           const float alpha = (m_new == -INFINITY) ? 1.f : fast_exp2(m_st - m_new);

@@ -81,3 +81,69 @@ def test_full_machines_of_prompts_repeat_themselves(d, n):
         again = c.run()
         assert all(torch.equal(x, y) for x, y in zip(first, again))
     no_error(c.h)
+
+
+# ---- probabilities far below the row's largest ----
+def levelled(d, L, n, k_of, v_of, sm_scale, ones=1.0):
+    """One request of L cached keys (the step's n among them) whose K and V rows are constant, k_of[j] and v_of[j] (values of e2m1), and queries
+    of ones: the score of key j is sm_scale * D * ones * k_of[j] for every row.  -> out, lse of the call."""
+    P, D, H = d.page_size, d.head_dim, d.num_kv_heads
+    pages = -(-L // P)
+    pad = np.zeros(pages * P - L)
+    codes = [np.searchsorted(ref.LEVELS, np.concatenate([x, pad])).astype(np.uint8) * 17 for x in (k_of, v_of)]
+    pool = torch.full((pages, 2, H, P * (D // 2 + D // 16)), 0x38, dtype=torch.uint8, device="cuda")  # scales of 1
+    for which, c in enumerate(codes):
+        rows = torch.from_numpy(c).cuda().reshape(pages, 1, P, 1).expand(pages, H, P, D // 2)
+        pool[:, which, :, : P * D // 2] = rows.reshape(pages, H, -1)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").flip(0)[None].contiguous()
+    pool = pool.flip(0).contiguous()
+    h = make_handle(d, torch.float32, sm_scale=float(np.float32(sm_scale)))
+    q = torch.full((n, d.num_q_heads, D), ones, dtype=torch.bfloat16, device="cuda")
+    b = hb.Batch(dev_i32([L - n]), table, *no_rings(d, 1), dev_i32([0, n]), max_q_len=n, total_q=n, max_ctx_len=L - n)
+    out, lse = torch.full(q.shape, 7.0, device="cuda"), torch.full(q.shape[:2], 7.0, device="cuda")
+    ws = workspace(h, b, True)
+    ws.fill_(255)
+    hb.hswa_packed_attn(h, hb.PackedLayer(pool), b, True, q, out, lse, ws)
+    no_error(h)
+    return out.double().cpu().numpy(), lse.double().cpu().numpy()
+
+
+LEVEL_SHAPES = [(dims(8, 128, 64, 1), 1, 2000), (dims(8, 128, 64, 1), 1, 131072), (dims(4, 64, 16, 1), 1, 100000), (dims(8, 128, 64, 1), 2, 131072),
+                (dims(8, 128, 32, 1), 4, 1000), (dims(8, 128, 64, 1), 4, 131072), (dims(8, 64, 64, 1), 4, 131072), (dims(8, 128, 64, 1), 40, 20000),
+                (dims(5, 64, 32, 1), 30, 20000)]
+
+
+@pytest.mark.parametrize("bits", [7.9, 8.1, 14.9, 25.1, 27.0])
+@pytest.mark.parametrize("where", ["first", "middle", "late"])
+@pytest.mark.parametrize("d,n,L", LEVEL_SHAPES)
+def test_one_key_far_above_all_others_leaves_them_their_weight(d, n, L, where, bits):
+    """One key `bits` powers of two above all others, whose V is 0 where theirs is 1: what comes out is their weight.  A score off by S = 2^-12
+    (as in test_gpu_packed.py), fp16's 2^-11 and 2^-32 of the largest for each key, and sums of L terms."""
+    at = {"first": 0, "middle": L // 2, "late": L - n - 1}[where]
+    k, v = np.zeros(L), np.ones(L)
+    k[at], v[at] = 1.0, 0.0
+    scale = np.float32(bits * np.log(2.0) / d.head_dim)
+    out, lse = levelled(d, L, n, k, v, scale)
+    s = float(scale) * d.head_dim
+    for i in range(n):
+        others = L - n + i
+        want = others * np.exp(-s) / (1.0 + others * np.exp(-s))
+        tol = want * (2.0 ** -11 + 2 * S_ERR + L * 2.0 ** -24) + L * 2.0 ** -32
+        assert np.abs(out[i] - want).max() <= tol, (i, out[i].min(), out[i].max(), want)
+        assert np.abs(lse[i] - (s + np.log1p(others * np.exp(-s)))).max() <= S_ERR
+
+
+@pytest.mark.parametrize("bits", [2.0 ** 12, 2.0 ** 20, 2.0 ** 24, 2.0 ** 26])
+@pytest.mark.parametrize("d,n,L", LEVEL_SHAPES)
+def test_scores_of_any_size_that_grow_from_key_to_key(d, n, L, bits):
+    """Scores that grow in steps along the keys, up to sizes where a score's own rounding is several powers of two: the largest, one key, takes all."""
+    k, v = np.zeros(L), np.full(L, 3.0)
+    steps = [0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
+    for i, x in enumerate(steps):
+        k[(L - n) * (i + 1) // 8] = x
+    v[(L - n) * 7 // 8] = 1.0
+    scale = np.float32(bits * np.log(2.0) / d.head_dim / 6.0)
+    out, lse = levelled(d, L, n, k, v, scale)
+    assert (np.abs(out - 1.0) <= 2.0 ** -10).all()
+    want = float(scale) * d.head_dim * 6.0
+    assert (np.abs(lse - want) <= want * 2.0 ** -21).all()
