@@ -124,15 +124,16 @@ __device__ __forceinline__ bool base_moves(float to, float from) {
 }
 
 // Queries enter the products as fp16, each row times a power of two that brings its largest element to [2^14, 2^15): fp16
-// has three bits more than bf16, so only elements below 2^-28 of the largest lose any.  From the largest magnitude, infinities and
-// NaN apart, the power and its inverse.
+// has three bits more than bf16, so only elements below 2^-28 of the largest lose any.  (Rows below 2^-112 are multiplied by 2^126, the
+// largest whose inverse is a normal number: their elements, down to bf16's smallest, stay normal in fp16.)  From the largest magnitude,
+// infinities and NaN apart, the power and its inverse.
 __device__ __forceinline__ float finite_max(float amax, float2 f) {
   const float a = fabsf(f.x), b = fabsf(f.y);
   return fmaxf(amax, fmaxf(a < INFINITY ? a : 0.f, b < INFINITY ? b : 0.f));
 }
 __device__ __forceinline__ void q_powers(float amax, float* up, float* down) {
   const int e = (int)(__float_as_uint(amax) >> 23);  // biased exponent
-  const int shift = amax > 0.f ? min(141 - e, 100) : 0;
+  const int shift = amax > 0.f ? min(141 - e, 126) : 0;
   *up = __uint_as_float((uint32_t)(127 + shift) << 23);
   *down = __uint_as_float((uint32_t)(127 - shift) << 23);
 }

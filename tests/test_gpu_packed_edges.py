@@ -147,3 +147,14 @@ def test_scores_of_any_size_that_grow_from_key_to_key(d, n, L, bits):
     assert (np.abs(out - 1.0) <= 2.0 ** -10).all()
     want = float(scale) * d.head_dim * 6.0
     assert (np.abs(lse - want) <= want * 2.0 ** -21).all()
+
+
+@pytest.mark.parametrize("n,ctx", [(1, [40, 70]), (1, [2400, 70]), (2, [2400, 70]), (4, [40, 70]), (4, [2400, 70]), (50, [40, 70])])
+@pytest.mark.parametrize("mag", [2.0 ** -90, 2.0 ** -112, 2.0 ** -118, 2.0 ** -121])
+def test_queries_of_tiny_elements_and_a_large_scale(n, ctx, mag):
+    """Elements around `mag` with a scale that makes scores of order 1: no element within 2^28 of the largest loses a bit on its way to fp16."""
+    c = Case(dims(8, 128, 32), ctx, [n, n], seed=50)
+    c.q = to_host_bits((torch.from_numpy(wl.bits_to_f64(c.q)) * mag).to(torch.bfloat16))
+    h = make_handle(c.d, torch.float32, sm_scale=float(np.float32(1.0 / np.sqrt(128) / mag)))
+    c.scale = float(h.cfg.sm_scale)
+    check(c, *run(c, h=h, single=False))
