@@ -195,7 +195,7 @@ __device__ __forceinline__ void apply_fork(const PagesForkParams& p, const Rows&
       atomicAdd(&p.ref_out[page], by);
   };
   constexpr int CH = 256;  // places per item
-  const int chunks = (max(p.max_blocks, p.out_max_blocks) + CH - 1) / CH;
+  const int chunks = max(1, (max(p.max_blocks, p.out_max_blocks) + CH - 1) / CH);  // (tables without places have rows all the same)
   // new rows: shared places in chunks of 256, the places behind them by the warp of chunk 0
   for (int64_t it = me; it < (int64_t)p.rows_out * chunks; it += all) {
     const int r = (int)(it / chunks), c = (int)(it % chunks);

@@ -32,3 +32,24 @@ def test_fork_refuses_a_bad_number_of_pages_in_any_row(rows, hi, pages):
             st = hb.hswa_get_async_error(h)
             assert st == (hb.HSWA_ERR_BOUNDS, row, -1, bad), st
             assert np.array_equal(got[0], counts) and all((g == FILL).all() for g in got[1:])
+
+
+@pytest.mark.parametrize("pages", [9, 70001])
+@pytest.mark.parametrize("blocks,out_blocks", [(0, 0), (0, 2), (2, 0)])
+def test_fork_of_tables_without_places(blocks, out_blocks, pages):
+    """Rows that hold no page, from or into tables of width 0: their numbers of pages and copies are written like any others."""
+    P, h = 16, make_handle(dims(1, 64, 16, 1))
+    counts = np.zeros(pages, np.int32)
+    counts[3] = 2
+    need = [0, 0, P + 1 if out_blocks else 0]
+    got = check_fork(h, P, counts, np.zeros((2, blocks), np.int32), np.zeros(2, np.int32), [0, -1, -1], [0, 0, 0], need, out_blocks)
+    assert got[2].tolist() == [0, 0, out_blocks]
+
+
+def test_compact_of_tables_without_places():
+    h = make_handle(dims(1, 64, 16, 1))
+    counts = dev_i32([0, 1, 0, 2])
+    o = [torch.full(s, FILL, dtype=torch.int32, device="cuda") for s in ((4,), (2, 0), (4,), (2,), (2,))]
+    hb.hswa_pages_compact(h, counts, o[0], torch.zeros((2, 0), dtype=torch.int32, device="cuda"), dev_i32([0, 0]), o[1], o[2], o[3], o[4])
+    no_error(h)
+    assert [x.tolist() for x in (o[0], o[2], o[3], o[4])] == [[2, 1, 0, 0], [0, 1, 2, 0], [3, -1], [0, -1]]
