@@ -1120,7 +1120,8 @@ hswa_status hswa_pages_compact(hswa_handle* h, int64_t num_pages, const int32_t*
   if (!h || num_pages <= 0 || rows < 0 || max_blocks < 0 || max_moves < 0 || !ref || !ref_out || !page_map) return HSWA_ERR_INVALID_ARG;
   if (rows > 0 && (!held || (max_blocks > 0 && (!table || !table_out)))) return HSWA_ERR_INVALID_ARG;
   if (max_moves > 0 && (!move_src || !move_dst)) return HSWA_ERR_INVALID_ARG;
-  if (aliased({ref_out, page_map, move_src, move_dst}, {ref, table, held, table_out}) || (table_out && table_out == held)) return HSWA_ERR_INVALID_ARG;
+  if (aliased({ref_out, page_map, move_src, move_dst}, {ref, table, held, table_out}) || (table_out && (table_out == held || table_out == ref)))
+    return HSWA_ERR_INVALID_ARG;
   if (num_pages > kMaxPages || rows > kMaxPageRows || (int64_t)rows * max_blocks > kMaxPageEntries) return HSWA_ERR_UNSUPPORTED;
   if (!device_is_current(h)) return HSWA_ERR_INVALID_ARG;
   PagesCompactParams p = {};

@@ -53,3 +53,15 @@ def test_compact_of_tables_without_places():
     hb.hswa_pages_compact(h, counts, o[0], torch.zeros((2, 0), dtype=torch.int32, device="cuda"), dev_i32([0, 0]), o[1], o[2], o[3], o[4])
     no_error(h)
     assert [x.tolist() for x in (o[0], o[2], o[3], o[4])] == [[2, 1, 0, 0], [0, 1, 2, 0], [3, -1], [0, -1]]
+
+
+def test_compact_refuses_a_table_over_the_counts():
+    h = make_handle(dims(1, 64, 16, 1))
+    counts = dev_i32([0, 1, 0, 2, 1, 0])
+    before = counts.clone()
+    o = [torch.full(s, FILL, dtype=torch.int32, device="cuda") for s in ((6,), (6,), (2,), (2,))]
+    with pytest.raises(hb.HswaError) as e:
+        hb.hswa_pages_compact(h, counts, o[0], dev_i32([[1, 3, 0], [4, 0, 0]]), dev_i32([2, 1]), counts.reshape(2, 3), o[1], o[2], o[3])
+    assert e.value.status == hb.HSWA_ERR_INVALID_ARG
+    assert torch.equal(counts, before) and all((x == FILL).all() for x in o)
+    no_error(h)
