@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kThreads) pages_fork_kernel(const PagesForkPar
   const Rows rows = {s_parent, s_len, s_need, s_held, s_first, s_most, s_rank};
   const int block = (int)cluster.block_rank(), warp = threadIdx.x >> 5;
   const Share sh = share_of(p.num_pages, block);
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (p.second) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (else another handle's decode may follow, and read early)
   if (!p.copied) fetch_counts(p.ref, p.num_pages, sh);
   bool bad = false;
   for (int i = threadIdx.x; i < p.rows_in; i += kThreads) {
@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(kThreads) pages_compact_kernel(const PagesComp
   const Share sh = share_of(p.num_pages, block);
   uint32_t* s_free = reinterpret_cast<uint32_t*>(s_mem);
   int32_t* s_before = s_mem + sh.words;  // live pages before each word's
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (p.second) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (else another handle's decode may follow, and read early)
   if (!p.copied) fetch_counts(p.ref, p.num_pages, sh);
   for (int i = block * kThreads + threadIdx.x; i < p.max_moves; i += kBlocks * kThreads) p.move_src[i] = p.move_dst[i] = -1;
   asm volatile("griddepcontrol.wait;" ::: "memory");  // (with p.copied: the pass over the counts, launched before, is done)

@@ -5,9 +5,10 @@ import pytest
 import torch
 
 import packed_reference as ref
-from gpu_utils import dev_i32, make_handle
+from gpu_utils import dev_i32, make_handle, to_dev_bf16
 from paper_2607_13095_b200 import binding as hb
-from test_gpu_packed import dims, no_error
+from paper_2607_13095_b200 import workloads as wl
+from test_gpu_packed import dims, no_error, no_rings
 from test_gpu_pages import FILL, check_fork, children, fork, state
 
 pytestmark = pytest.mark.gpu
@@ -65,3 +66,45 @@ def test_compact_refuses_a_table_over_the_counts():
     assert e.value.status == hb.HSWA_ERR_INVALID_ARG
     assert torch.equal(counts, before) and all((x == FILL).all() for x in o)
     no_error(h)
+
+
+@pytest.mark.parametrize("what", ["fork", "compact"])
+def test_tables_written_through_another_handle_between_decode_calls(what):
+    """Decode calls of one handle may overlap; a table that another handle's call writes between two of them is whole before the second reads it."""
+    d, B, L = dims(4, 64, 16, 1), 8, 300
+    P, blocks = 16, 20
+    pages = 1 + B * blocks
+    h, other = make_handle(d, torch.float32), make_handle(d, torch.float32)
+    table = dev_i32(1 + np.random.default_rng(12).permutation(B * blocks).reshape(B, blocks))
+    pools = [to_dev_bf16(wl.bf16_bits_normal(60 + i, (pages, 2, 1, P, 64))) for i in range(2)]
+    q, k, v = (to_dev_bf16(wl.bf16_bits_normal(62 + i, (B, n, 64))) for i, n in enumerate((4, 1, 1)))
+    ref_in, held = torch.ones((pages,), dtype=torch.int32, device="cuda"), dev_i32([blocks] * B)
+    ref_out, page_map = torch.empty_like(ref_in), torch.empty_like(ref_in)
+    seen = torch.zeros((B, blocks), dtype=torch.int32, device="cuda")  # the table that the decode calls read
+    batch = hb.Batch(dev_i32([L] * B), seen, *no_rings(d, B), max_ctx_len=L)
+    parent, length, need = dev_i32(np.arange(B)), dev_i32([L] * B), dev_i32([blocks * P] * B)
+    small = [torch.empty((B,), dtype=torch.int32, device="cuda") for _ in range(3)]
+    ws_pages = torch.empty((hb.hswa_pages_workspace_need(h, pages),), dtype=torch.uint8, device="cuda")
+    ws = torch.empty((hb.hswa_workspace_bytes(h, B, B, L),), dtype=torch.uint8, device="cuda")
+    layers = [hb.Layer(p, False) for p in pools]
+
+    def step():
+        seen.zero_()  # page 0: nobody's
+        out = [torch.empty((B, 4, 64), device="cuda") for _ in range(2)]
+        hb.hswa_decode_attn(h, layers[0], batch, q, k, v, out[0], None, ws)
+        if what == "fork":
+            hb.hswa_pages_fork(other, ref_in, ref_out, table, held, parent, length, need, seen, *small, ws_pages)
+        else:
+            hb.hswa_pages_compact(other, ref_in, ref_out, table, held, seen, page_map, small[0], small[1])
+        hb.hswa_decode_attn(h, layers[1], batch, q, k, v, out[1], None, ws)
+        return out[1]
+
+    hb.hswa_set_overlap(h, False)
+    want = step()
+    hb.hswa_set_overlap(h, True)
+    assert torch.isfinite(want).all()
+    for _ in range(50):
+        assert torch.equal(step(), want)
+    assert torch.equal(seen, table)
+    no_error(h)
+    no_error(other)
