@@ -327,10 +327,12 @@ hswa_status hswa_evict_compact(hswa_handle* h, const hswa_layer* layer, const hs
  *
  * hswa_packed_append: rounds the step's rows into the cache, row i of request r at position ctx_len[r] + i.  A block of largest
  *   magnitude a gets the scale f = e4m3((a / s) / 6), at most 448, and its elements x the values e2m1(x / (f s)), at most 6 in
- *   magnitude; all roundings go to the nearest, ties to the even code.  A block whose f rounds to 0 is held as zeros; infinities
+ *   magnitude; all roundings go to the nearest, ties to the even code.  Quotients are taken in fp32: with a scale s of at most 14
+ *   significant bits the codes are those of exact arithmetic; with a longer one, where an exact quotient lies within 2^-22 (relative) of the
+ *   middle between two codes, either may be held.  A block whose f rounds to 0 is held as zeros; infinities
  *   and NaN are held as finite values.  k_new, v_new: device bf16 [T][Hkv][D].
- * hswa_packed_read: the same rows back, k_out, v_out: device bf16 [T][Hkv][D], each element the value it stands for, rounded once
- *   (exact where the layer's scale is a power of two).  With ctx_len = 0 and n[r] a request's length it reads the whole cache;
+ * hswa_packed_read: the same rows back, k_out, v_out: device bf16 [T][Hkv][D], each element the value it stands for, rounded to fp32
+ *   and then to bf16 (exact where the layer's scale is a power of two).  With ctx_len = 0 and n[r] a request's length it reads the whole cache;
  *   after an append it gives the chunk as later steps will see it.
  *   Both: a request's rows past max_q_len, its rows outside the block table or behind a page id out of range, and a ctx_len outside
  *   [0, max_ctx_len] are recorded as HSWA_ERR_BOUNDS and left out.  Pages that several requests share are the caller's to keep

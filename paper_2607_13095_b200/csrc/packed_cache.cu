@@ -4,7 +4,8 @@
 // A block of 16 elements x with largest magnitude a, in a layer of scale g, is held as f = e4m3((a / g) / 6), s = f g, and
 // e2m1(x / s): both roundings to the nearest, ties to the even code, at most 448 and 6.  Quotients lie halfway between two codes
 // often (dividend and divisor have few bits), so they have to be right to the last bit: a product with the inverse, then one
-// Newton step on its exact residual, which makes every quotient exact that fits 24 bits.  (Divisions take the append from 59
+// Newton step on its exact residual, which makes every quotient exact that fits 24 bits.  (Layer scales of more than 14 bits make other
+// quotients, which 32 bits may round to a half: within 2^-22 of one either code may be held.)  (Divisions take the append from 59
 // to 79 us; a pair of elements per instruction, from 52 to 46.)
 // Bound by HBM (2 bytes per element read, 0.5625 written; read-back: the reverse) and by issue: 70 % of the slots at ten
 // instructions an element.  A block takes some tokens: it looks up where their rows are held (a chain of dependent loads) once, and then

@@ -158,3 +158,58 @@ def test_queries_of_tiny_elements_and_a_large_scale(n, ctx, mag):
     h = make_handle(c.d, torch.float32, sm_scale=float(np.float32(1.0 / np.sqrt(128) / mag)))
     c.scale = float(h.cfg.sm_scale)
     check(c, *run(c, h=h, single=False))
+
+
+# ---- layer scales of many bits ----
+BORDERS = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])
+
+
+@pytest.mark.parametrize("scale", [0.7001953125, 1.4998779296875 * 2.0 ** -9, 5.2119140625, 0.7, 4.0 / 3.0, 3.3895 / 2688.0, 1.9999998807907104, 2.0 ** -63 * 1.1])
+def test_layer_scales_of_any_number_of_bits(scale):
+    """Scales of up to 14 bits round as in exact arithmetic.  Longer ones make quotients that 32 bits round, two of them (2^-23 each) for the
+    scale of a block, a product and one quotient for an element: within 2^-22 of a border either neighbour may be held.  The read-back rounds to
+    32 bits, then to bf16."""
+    d = dims(1, 128, 64, 1)
+    s32 = float(np.float32(scale))
+    exact = (np.float32(scale).view(np.uint32) & 0x3FF) == 0
+    rng = np.random.default_rng(13)
+    tops = np.concatenate([[0x3F80, 0x4049, 0x7F7F, 0x2345], rng.integers(0x3000, 0x4800, 4000)]).astype(np.uint16)
+    x = np.stack([tops] + [np.maximum(tops.astype(int) - rng.integers(0, 700, len(tops)), 0).astype(np.uint16) for _ in range(15)], axis=1)
+    x[:, 1:] |= rng.integers(0, 2, (len(tops), 15)).astype(np.uint16) << 15
+    # elements next to the borders of their block's quotients
+    f = ref.round_rows(wl.bits_to_f64(x), s32)[1]
+    near = (BORDERS[rng.integers(0, 7, len(tops))] * ref.SCALES[f[:, 0]] * s32).astype(np.float32)
+    near_bits = to_host_bits(torch.from_numpy(near).to(torch.bfloat16))
+    x[:, 1] = np.minimum(near_bits, tops)
+    flat = x.reshape(-1)
+    T = -(-len(flat) // 128)
+    flat = np.concatenate([flat, np.zeros(T * 128 - len(flat), np.uint16)]).reshape(T, 1, 128)
+    pages = -(-T // 64)
+    h = make_handle(d)
+    b = hb.Batch(dev_i32([0]), dev_i32(np.arange(pages)[None]), *no_rings(d, 1), dev_i32([0, T]), max_q_len=T, total_q=T, max_ctx_len=0)
+    layer = hb.PackedLayer(torch.zeros((pages, 2, 1, 64 * 72), dtype=torch.uint8, device="cuda"), scale, scale)
+    data = to_dev_bf16(flat)
+    hb.hswa_packed_append(h, layer, b, data, data)
+    k, v = torch.empty_like(data), torch.empty_like(data)
+    hb.hswa_packed_read(h, layer, b, k, v)
+    no_error(h)
+    pool, table = layer.pool.cpu().numpy(), np.arange(pages)[None]
+    held = ref.rows(pool, table, 0, T, 1, 64, 128, 1.0)
+    n4, f = ref.round_rows(wl.bits_to_f64(flat), s32)
+    want = ref.values(n4, f, 1.0)
+    if exact:
+        assert np.array_equal(held, want)
+    else:
+        # a block's scale: the statement's, or its neighbour where the quotient is that near to the middle between them
+        pos = np.arange(T)
+        codes = pool[pos // 64, 1, 0][:, 64 * 64:].reshape(T, 64, 8)[pos, pos % 64]
+        a = np.abs(wl.bits_to_f64(flat)).reshape(T, 8, 16).max(axis=-1) / s32 / 6.0
+        other = codes != f[:, 0]
+        middle = (ref.SCALES[codes] + ref.SCALES[f[:, 0]]) / 2
+        assert (np.abs(a / np.where(other, middle, a + 1e-300) - 1)[other] < 2.0 ** -22).all() and (np.abs(codes.astype(int) - f[:, 0])[other] == 1).all()
+        y = np.abs(wl.bits_to_f64(flat[:, 0])) / np.repeat(ref.SCALES[f[:, 0]] * s32 + 1e-300, 16, axis=-1)
+        close = np.abs(y[..., None] / BORDERS - 1).min(axis=-1) < 2.0 ** -22
+        differ = (held != want)[:, 0]
+        assert (close | np.repeat(other, 16, axis=-1) | ~differ).all()
+    got, stands_for = v.double().cpu().numpy(), held * s32
+    assert (np.abs(got - stands_for) <= (2.0 ** -8 + 2.0 ** -24) * np.abs(stands_for)).all() and torch.equal(k, v)
