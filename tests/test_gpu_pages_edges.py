@@ -108,3 +108,146 @@ def test_tables_written_through_another_handle_between_decode_calls(what):
     assert torch.equal(seen, table)
     no_error(h)
     no_error(other)
+
+
+# ---- large pools and large tables together: counts copied by a launch before the cluster's, tables rewritten by one behind it ----
+PAGES, BLOCKS = 70001, 900
+
+
+def large(seed, rows_in=66, rows_out=70):
+    rng = np.random.default_rng(seed)
+    P = 16
+    counts, table, held, lens = state(rng, P, rows_in, 14000, PAGES)
+    parent, length, need = children(rng, P, rows_out, held, lens, 50)
+    parent[3], parent[4], parent[5] = parent[2], parent[2], -1  # several children of one row, a new request of many pages
+    length[2:5] = np.minimum([int(lens[max(parent[2], 0)])] * 3, [14000, 9999, 14000]) if parent[2] >= 0 else 0
+    need[2:5] = length[2:5] + 20
+    length[5], need[5] = 0, 13900
+    assert rows_in * table.shape[1] + rows_out * BLOCKS > 32768 and PAGES > 65536
+    return P, make_handle(dims(1, 64, P, 1)), counts, table, held, parent, length, need
+
+
+@pytest.mark.parametrize("seed", [21, 22, 23])
+def test_large_pools_with_large_tables(seed):
+    """Forked, then compacted, entry for entry: shared, passed on, copied, fresh and freed pages, some of a prefix cache."""
+    P, h, counts, table, held, parent, length, need = large(seed)
+    ref_out, table_out, held_out, src, _ = check_fork(h, P, counts, table, held, parent, length, need, BLOCKS)
+    assert (src >= 0).any() and (counts == 2).any()
+    for moves in (7, 30000):
+        dev = [dev_i32(x) for x in (ref_out, table_out, held_out)]
+        rows = len(held_out)
+        outs = [torch.full(s, FILL, dtype=torch.int32, device="cuda") for s in ((PAGES,), (rows, BLOCKS), (PAGES,), (moves,), (moves,))]
+        want = ref.compact(ref_out, table_out, held_out, moves, FILL)
+        hb.hswa_pages_compact(h, dev[0], outs[0], dev[1], dev[2], outs[1], outs[2], outs[3], outs[4])
+        no_error(h)
+        for g, w in zip(outs, want):
+            assert np.array_equal(g.cpu().numpy(), w)
+        hb.hswa_pages_compact(h, dev[0], outs[0], dev[1], dev[2], dev[1], outs[2], outs[3], outs[4])  # in place
+        no_error(h)
+        assert np.array_equal(dev[1].cpu().numpy()[want[1] != FILL], want[1][want[1] != FILL])
+
+
+def test_large_forks_that_are_refused_do_nothing():
+    P, h, counts, table, held, parent, length, need = large(24)
+
+    def refused(*what, **change):
+        a = dict(counts=counts, held=held, parent=parent, length=length, need=need)
+        a.update(change)
+        got = fork(h, a["counts"], table, a["held"], a["parent"], a["length"], a["need"], BLOCKS)
+        st = hb.hswa_get_async_error(h)
+        assert st[: len(what)] == what, st
+        assert np.array_equal(got[0], a["counts"]) and all((g == FILL).all() for g in got[1:])
+
+    def at(x, i, v):
+        y = np.array(x)
+        y[i] = v
+        return y
+
+    few = np.where(counts == 0, 1, counts)
+    few[[5, 69998]] = 0
+    refused(hb.HSWA_ERR_BOUNDS, -1, counts=few)
+    refused(hb.HSWA_ERR_BOUNDS, 50, -1, held=at(held, 50, table.shape[1] + 1))
+    refused(hb.HSWA_ERR_BOUNDS, 61, -2, parent=at(parent, 61, 66))
+    refused(hb.HSWA_ERR_BOUNDS, 62, -2, length=at(length, 62, -1))
+    refused(hb.HSWA_ERR_BOUNDS, 63, -2, need=at(need, 63, BLOCKS * P + 1))
+    # as many as there are: enough
+    check_fork(h, P, counts, table, held, parent, length, need, BLOCKS)
+
+
+def test_large_fork_replayed_from_a_graph():
+    P, h, counts, table, held, parent, length, need = large(25)
+    dev = [dev_i32(x) for x in (np.zeros_like(counts), table, held, parent, length, need)]
+    n = len(parent)
+    outs = [torch.full(s, FILL, dtype=torch.int32, device="cuda") for s in ((PAGES,), (n, BLOCKS), (n,), (n,), (n,))]
+    ws = torch.empty((hb.hswa_pages_workspace_need(h, PAGES),), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hb.hswa_pages_fork(h, dev[0], outs[0], dev[1], dev[2], dev[3], dev[4], dev[5], *outs[1:], ws)
+    dev[0].copy_(dev_i32(counts))
+    want = ref.fork(counts, table, held, parent, length, need, P, BLOCKS, FILL)
+    for _ in range(3):
+        for o in outs:
+            o.fill_(FILL)
+        ws.fill_(255)
+        graph.replay()
+        no_error(h)
+        for g, w in zip(outs, want):
+            assert np.array_equal(g.cpu().numpy(), w)
+
+
+def off_by(x, places):
+    """The same values in memory that starts `places` entries behind a 16-byte border."""
+    buf = torch.full((x.numel() + 8,), FILL, dtype=torch.int32, device="cuda")
+    view = buf[places:places + x.numel()].reshape(x.shape)
+    view.copy_(x)
+    return view
+
+
+@pytest.mark.parametrize("pages", [1, 31, 5003, 70001])
+@pytest.mark.parametrize("shift", [(1, 1, 1), (0, 3, 0), (2, 0, 1), (0, 0, 3)])
+def test_arrays_off_16_bytes(pages, shift):
+    """Counts, their copy and the map anywhere on 4 bytes, next to memory that stays as it was."""
+    rng = np.random.default_rng(pages)
+    P, h = 16, make_handle(dims(1, 64, 16, 1))
+    counts, table, held, lens = state(rng, P, 3 if pages > 1000 else 0, 300, pages)
+    parent, length, need = children(rng, P, 4 if pages > 1000 else 0, held, lens, 40)
+    a, b, c = (off_by(dev_i32(x), s) for x, s in zip((counts, np.full(pages, FILL), np.full(pages, FILL)), shift))
+    n, blocks = len(parent), 25
+    outs = [torch.full(s, FILL, dtype=torch.int32, device="cuda") for s in ((n, blocks), (n,), (n,), (n,))]
+    ws = torch.empty((hb.hswa_pages_workspace_need(h, pages),), dtype=torch.uint8, device="cuda")
+    dev = [off_by(dev_i32(x), 1) for x in (table, held, parent, length, need)]
+    hb.hswa_pages_fork(h, a, b, *dev, *outs, ws)
+    no_error(h)
+    want = ref.fork(counts, table, held, parent, length, need, P, blocks, FILL)
+    for g, w in zip((b, *outs), want):
+        assert np.array_equal(g.cpu().numpy(), w)
+    moves = 50
+    outs = [torch.full(s, FILL, dtype=torch.int32, device="cuda") for s in (tuple(table.shape), (moves,), (moves,))]
+    hb.hswa_pages_compact(h, a, b, dev[0], dev[1], outs[0], c, outs[1], outs[2])
+    no_error(h)
+    for g, w in zip((b, outs[0], c, outs[1], outs[2]), ref.compact(counts, table, held, moves, FILL)):
+        assert np.array_equal(g.cpu().numpy(), w)
+    for x, s in ((b, shift[1]), (c, shift[2])):
+        whole = torch.as_strided(x, (pages + 8,), (1,), 0)
+        assert (whole[:s] == FILL).all() and (whole[s + pages:] == FILL).all()
+
+
+def test_fresh_pages_at_the_limits_are_the_lowest():
+    """8388608 pages, 4096 rows: fresh pages in the order of rows and places are the lowest free ones in order, whoever lists them."""
+    P, pages, n = 16, 1 << 23, 4096
+    h = make_handle(dims(1, 64, P, 1))
+    counts = (torch.rand((pages,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(7)) < 0.7).to(torch.int32)
+    places = torch.arange(n, device="cuda") % 9  # pages of each new request
+    need = (places * P).to(torch.int32)
+    ref_out = torch.empty_like(counts)
+    outs = [torch.full(s, FILL, dtype=torch.int32, device="cuda") for s in ((n, 8), (n,), (n,), (n,))]
+    ws = torch.empty((hb.hswa_pages_workspace_need(h, pages),), dtype=torch.uint8, device="cuda")
+    hb.hswa_pages_fork(h, counts, ref_out, torch.zeros((0, 1), dtype=torch.int32, device="cuda"), dev_i32([]), dev_i32([-1] * n), dev_i32([0] * n), need,
+                       *outs, ws)
+    no_error(h)
+    inside = torch.arange(8, device="cuda")[None] < places[:, None]
+    total = int(places.sum())
+    fresh = torch.nonzero(counts == 0)[:total, 0]
+    assert torch.equal(outs[0][inside].long(), fresh) and (outs[0][~inside] == FILL).all()
+    counts[fresh] = 1
+    assert torch.equal(ref_out, counts) and torch.equal(outs[1].long(), places)
