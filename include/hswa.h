@@ -388,6 +388,11 @@ hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, con
  *   of range, nothing is done: ref_out becomes a copy of ref, the other arrays stay as they were, and HSWA_ERR_BOUNDS is recorded
  *   (request -1, index = pages wanted, value = pages free; or request = row, index -1 for held, -2 for parent, len, need).  Page
  *   ids out of range are recorded and neither counted nor copied.  Workspace: hswa_pages_workspace_need bytes.
+ *   On a hybrid stack these are the Full layers' pages.  A row's ring on the SWA layers is its own: one child takes over its parent's ring
+ *   pages, every other child needs R of its own, filled by hswa_pages_copy on each SWA layer's pool (the pairs of the parent's and the
+ *   child's ring_table entries, place by place) before the step writes.  ring_head goes with them, moved back (mod C) by as many slots
+ *   as the child takes tokens back.  Copies of a ring that has been L tokens long, taken back or not, hold the keys from position L - C
+ *   on, and a child at len tokens needs those from len - W + 1 on: from a row as long as it has been, C - W + 1 tokens at most.
  *
  * hswa_pages_compact: moves live pages into the lowest free ones, up to max_moves of them: while it lies below, the i-th lowest
  *   free page takes the i-th highest live one.  move_src[i], move_dst[i] (device int32 [max_moves]) are the pairs to be copied in

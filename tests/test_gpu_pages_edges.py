@@ -8,7 +8,7 @@ import packed_reference as ref
 from gpu_utils import dev_i32, make_handle, to_dev_bf16
 from paper_2607_13095_b200 import binding as hb
 from paper_2607_13095_b200 import workloads as wl
-from test_gpu_packed import dims, no_error, no_rings
+from test_gpu_packed import S_ERR, dims, no_error, no_rings
 from test_gpu_pages import FILL, check_fork, children, fork, state
 
 pytestmark = pytest.mark.gpu
@@ -251,3 +251,78 @@ def test_fresh_pages_at_the_limits_are_the_lowest():
     assert torch.equal(outs[0][inside].long(), fresh) and (outs[0][~inside] == FILL).all()
     counts[fresh] = 1
     assert torch.equal(ref_out, counts) and torch.equal(outs[1].long(), places)
+
+
+@pytest.mark.parametrize("d", [dims(4, 64, 16, 1), dims(8, 128, 64, 2)])
+def test_beams_on_a_hybrid_stack(d):
+    """Steps of forking over a Full and an SWA layer: tables by the fork, rings taken over by one child and copied for the others, heads moved back
+    by the tokens that a child takes back, as many as the ring still covers.  Every row's attention is that over its own history."""
+    P, D, H, W, R, C = d.page_size, d.head_dim, d.num_kv_heads, d.window, d.ring_pages, d.ring_slots
+    h = make_handle(d, torch.float32)
+    pages, blocks, rings = 400, 700 // P + 3, 40
+    pools = [hb.Layer(torch.full((n, 2, H, P, D), float("nan"), dtype=torch.bfloat16, device="cuda"), swa) for n, swa in ((pages, False), (rings * R, True))]
+    counts = torch.zeros((pages,), dtype=torch.int32, device="cuda")
+    table, held = torch.zeros((0, blocks), dtype=torch.int32, device="cuda"), dev_i32([])
+    ws_pages = torch.empty((hb.hswa_pages_workspace_need(h, pages),), dtype=torch.uint8, device="cuda")
+    past, ring_of, head_of, free = [], [], [], list(range(rings))  # of each row: per layer K and V; its ring; its head
+    since = []  # of each row: the first position that its ring still holds
+    most = C - W + 1
+    steps = [([-1, -1], [300, 40], [0, 0]), ([0, 0, 1], [1] * 3, [0, most, 5]), ([0, 1, 1, 2], [1] * 4, [0, 0, 1, 0]), ([1, 1, 3], [30, 150, 7], [most, 1, 0]),
+             ([0, 0, 1, 2, -1], [1] * 5, [0, 1, most, 3, 0]), ([4, 0, 2], [1] * 3, [0, 0, 1])]
+    for step, (parent, n, back) in enumerate(steps):
+        B, T = len(parent), sum(n)
+        back = [x if p < 0 else min(x, len(past[p][0][0]) - (W - 1) - since[p] if since[p] else x) for p, x in zip(parent, back)]
+        assert min(back) >= 0 and (step != 1 or back[1] == most)
+        length = [0 if p < 0 else len(past[p][0][0]) - x for p, x in zip(parent, back)]
+        since = [max(0 if p < 0 else since[p], a + b - C) for p, a, b in zip(parent, length, n)]
+        table_out = torch.full((B, blocks), -1, dtype=torch.int32, device="cuda")
+        held_out, src, dst = (torch.empty((B,), dtype=torch.int32, device="cuda") for _ in range(3))
+        new = torch.empty_like(counts)
+        hb.hswa_pages_fork(h, counts, new, table, held, dev_i32(parent), dev_i32(length), dev_i32([a + b for a, b in zip(length, n)]), table_out,
+                           held_out, src, dst, ws_pages)
+        hb.hswa_pages_copy(h, pools[:1], src, dst)
+        counts, table, held = new, table_out, held_out
+        # rings: fresh ones from those that no row of the step before holds
+        spare = [x for x in free if x not in ring_of]
+        mine, pairs, heads, taken = [], [], [], set()
+        for p, x in zip(parent, back):
+            if p >= 0 and p not in taken:
+                mine.append(ring_of[p])
+                taken.add(p)
+            else:
+                mine.append(spare.pop())
+                if p >= 0:
+                    pairs += [(ring_of[p] * R + i, mine[-1] * R + i) for i in range(R)]
+            heads.append(0 if p < 0 else (head_of[p] - x) % C)
+        if pairs:
+            hb.hswa_pages_copy(h, pools[1:], dev_i32([a for a, _ in pairs]), dev_i32([b for _, b in pairs]))
+        ring_of, head_of = mine, heads
+        past = [[[x[:keep] for x in kv] for kv in past[p]] if p >= 0 else [[np.zeros((0, H, D))] * 2 for _ in range(2)] for p, keep in zip(parent, length)]
+        indptr = np.concatenate([[0], np.cumsum(n)]).astype(np.int32)
+        ring_table = dev_i32([[x * R + i for i in range(R)] for x in ring_of])
+        ctx, head = dev_i32(length), dev_i32(head_of)
+        single = max(n) == 1
+        b = hb.Batch(ctx, table, ring_table, head, None if single else dev_i32(indptr), max_q_len=max(n), total_q=T, max_ctx_len=max(length))
+        for layer in range(2):
+            bits = [wl.bf16_bits_normal(3000 + 100 * step + 10 * layer + i, (T, heads_, D)) for i, heads_ in ((0, H), (1, H), (2, d.num_q_heads))]
+            k, v, q = (to_dev_bf16(x) for x in bits)
+            for r in range(B):
+                for which in (0, 1):
+                    past[r][layer][which] = np.concatenate([past[r][layer][which], wl.bits_to_f64(bits[which][indptr[r]:indptr[r + 1]])])
+            if not single:  # (prompts: their rows are cached, and read by the steps behind)
+                hb.hswa_kv_append(h, pools[layer], b, k, v)
+                no_error(h)
+                continue
+            out = torch.empty((T, d.num_q_heads, D), device="cuda")
+            ws = torch.empty((max(256, hb.hswa_workspace_bytes(h, B, T, max(length))),), dtype=torch.uint8, device="cuda")
+            hb.hswa_decode_attn(h, pools[layer], b, q, k, v, out, None, ws)
+            no_error(h)
+            o = out.double().cpu().numpy()
+            for r in range(B):
+                K, V = (x[-W:] if layer else x for x in past[r][layer])
+                want, _, mag = ref.attention(K, V, wl.bits_to_f64(bits[2][r:r + 1]), [len(K)], 1.0 / np.sqrt(D))
+                # probabilities in bf16, 2^-8 of their value; scores as in test_gpu_packed.py
+                tol = (2.0 ** -8 + 2 * S_ERR + len(K) * 2.0 ** -24) * mag
+                assert (np.abs(o[r:r + 1] - want) <= tol + 1e-7).all(), (step, layer, r, np.abs(o[r:r + 1] - want).max())
+        hb.hswa_step_advance(h, B, ctx, head, b.q_indptr)
+        head_of = head.tolist()
