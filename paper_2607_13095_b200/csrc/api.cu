@@ -217,10 +217,14 @@ bool plan_packed(const hswa_handle* h, int batch, int total_q, int max_q_len, in
   if (streams > INT32_MAX) return false;
   if (rows <= 32) {
     c.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
-    // Up to so many keys a block takes a stream as a whole, one launch without a join.  Measured, us in one block / in runs, 64 / 8
-    // heads of 128: a row per head, 2 requests of 2000 keys 18 / 27, of 4000 27 / 27, 32 of 2000 29 / 39, 64 of 2000 49 / 53, of 4000 80 / 86;
-    // four, 32 of 600 to 1500 57 / 66, 2 of 2000 39 / 37, 64 of 4000 193 / 141.
-    if (keys > (rows <= 8 ? 2112 : 1088)) {
+    // Up to so many keys a block takes a stream as a whole, one launch without a join; about where the two meet for few requests.  Measured, us in
+    // one block / in runs, captured calls among others, 64 / 8 heads of 128: a row per head, 2 requests of 2048 keys 14.5 / 21.4, of 4000
+    // 22.8 / 22.6, of 6000 31 / 23; 32 of 2048 23 / 35, of 4000 39 / 50; 64 of 4000 72 / 74 (8 / 1 heads of 64: 8 of 2048 18.6 / 18.6, of 4000
+    // 33 / 19); two, 2 of 1536 22.6 / 22.7, of 3000 35 / 23; 32 of 1536 32 / 41, of 4000 70 / 64; four, 2 of 1536 28.8 / 28.9, of 3000 47 / 29; 32 of
+    // 600 to 1500 50 / 58, of 2048 68 / 63; 64 of 200 to 2048 98 / 140, of 600 to 1500 88 / 95, of 1536 112 / 101 (mixed lengths leave blocks
+    // better off, many of one length runs; the lengths are the device's).
+    const int whole = rows > 8 ? 1600 : h->cfg.head_dim == 128 ? 4096 : 2112;
+    if (keys > whole) {
       // as many runs as fit the SMs: of a warp, four 64-key tiles at least; of a block of the tcgen05 kernel, two of 128 keys.  (Warps of
       // two tiles leave the join twice the pieces: 1 request of 32768 keys 49 us against 37, 2 of 4000 23 against 27.)
       const int64_t fit = (int64_t)(rows <= 8 ? hswa_packed_stream_runs_per_sm() : 1) * h->num_sms;

@@ -213,3 +213,89 @@ def test_layer_scales_of_any_number_of_bits(scale):
         assert (close | np.repeat(other, 16, axis=-1) | ~differ).all()
     got, stands_for = v.double().cpu().numpy(), held * s32
     assert (np.abs(got - stands_for) <= (2.0 ** -8 + 2.0 ** -24) * np.abs(stands_for)).all() and torch.equal(k, v)
+
+
+# ---- on both sides of the lengths up to which a block takes a stream as a whole ----
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d,n,keys", [(dims(8, 128, 64, 1), 1, 4096), (dims(1, 128, 16, 1), 8, 4096), (dims(8, 64, 32, 1), 1, 2112), (dims(8, 128, 32, 1), 2, 1600),
+                                      (dims(8, 128, 64, 1), 4, 1600), (dims(4, 64, 16, 1), 8, 1600)])
+def test_lengths_where_streams_begin_to_be_cut(d, n, keys, causal):
+    step = n if causal else 0
+    c = Case(d, [keys - step - 1, 70, keys - 300], [n] * 3, seed=60, causal=causal, spare_blocks=4)
+    for bound in (keys - step - 1, keys - step, keys - step + 1):  # (host-known: it decides, whatever the lengths)
+        check(c, *run(c, single=False, max_ctx=bound))
+
+
+LONGER = [4500, 0, 1, 4240, 130, 6005]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [dims(8, 128, 64), dims(1, 128, 32, 3), dims(5, 128, 16), dims(3, 128, 64, 1), dims(2, 64, 32)])
+def test_single_tokens_over_longer_contexts(d, causal, out_dtype):
+    c = Case(d, LONGER, [1] * 6, seed=61, causal=causal, v_scale=3.0)
+    check(c, *run(c, out_dtype), out_dtype)
+
+
+def test_single_tokens_of_nan_over_longer_contexts():
+    """As test_long_rows_of_nan_and_unlike_magnitudes."""
+    c = Case(dims(8, 128, 64, 2), [4400, 300], [1, 1], seed=62)
+    q = c.q.copy()
+    q[0, 5, 3] = 0x7FC0
+    q[0, 9] = to_host_bits(torch.from_numpy(wl.bits_to_f64(c.q[0, 9]) * 2.0 ** -20).to(torch.bfloat16))
+    c.q[0, 9] = q[0, 9]
+    out, lse = run(c, q=q, single=False)
+    assert np.isnan(out[0, 5]).all() and np.isnan(lse[0, 5])
+    out[0, 5], lse[0, 5] = c.want()[0][0, 5], c.want()[1][0, 5]
+    check(c, out, lse)
+
+
+def test_single_tokens_over_longer_contexts_record_values_out_of_range():
+    """As test_long_contexts_record_values_out_of_range."""
+    d = dims(8, 128, 16, 1)
+    c = Case(d, [4300, 40, 4200], [1] * 3, seed=63)
+    good = run(c, single=False)
+    h = make_handle(d, torch.float32)
+
+    def record(ctx=None, indptr=None, table=None):
+        b = hb.Batch(dev_i32(c.ctx if ctx is None else ctx), dev_i32(c.table if table is None else table), *no_rings(d, 3),
+                     dev_i32(c.indptr if indptr is None else indptr), max_q_len=1, total_q=3, max_ctx_len=4300)
+        out, lse = torch.full((3, 8, 128), 7.0, device="cuda"), torch.full((3, 8), 7.0, device="cuda")
+        hb.hswa_packed_attn(h, c.layer(), b, True, to_dev_bf16(c.q), out, lse, workspace(h, b, True))
+        return hb.hswa_get_async_error(h), out.double().cpu().numpy()
+
+    table = c.table.copy()
+    table[1, 1] = 1 << 20
+    st, out = record(table=table)
+    assert st[:4] == (hb.HSWA_ERR_BOUNDS, 1, 1, 1 << 20), st
+    assert np.abs(out[0] - good[0][0]).max() < 1e-2
+    for bad in (-1, 4301):
+        st, out = record(ctx=[4300, bad, 4200])
+        assert st[:4] == (hb.HSWA_ERR_BOUNDS, 1, -1, bad), st
+        assert np.abs(out[2] - good[0][2]).max() < 1e-2  # (other runs, other roundings)
+    for indptr in ([0, 1, 2, 4], [-1, 1, 2, 3]):
+        st, _ = record(indptr=np.array(indptr, np.int32))
+        assert (st[0], st[2]) == (hb.HSWA_ERR_BOUNDS, -2), st
+
+
+def test_single_tokens_over_longer_contexts_captured_and_repeated():
+    """As test_long_calls_captured_and_repeated."""
+    c, other = (Case(dims(8, 128, 64, 2), [4600, 900], [1, 1], seed=s) for s in (64, 65))
+    h = make_handle(c.d, torch.float32)
+    b, layer, q = c.batch(single=False), c.layer(), to_dev_bf16(c.q)
+    out, lse, ws = torch.empty((2, 16, 128), device="cuda"), torch.empty((2, 16), device="cuda"), workspace(h, b, True)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hb.hswa_packed_attn(h, layer, b, True, q, out, lse, ws)
+    layer.pool.copy_(torch.from_numpy(other.pool).cuda())
+    q.copy_(to_dev_bf16(other.q))
+    b.block_table.copy_(dev_i32(other.table))
+    seen = []
+    for _ in range(2):
+        out.fill_(7.0)
+        ws.fill_(255)
+        graph.replay()
+        no_error(h)
+        seen.append(out.double().cpu().numpy())
+        check(other, seen[-1], lse.double().cpu().numpy())
+    assert np.array_equal(*seen)
