@@ -299,3 +299,50 @@ def test_single_tokens_over_longer_contexts_captured_and_repeated():
         seen.append(out.double().cpu().numpy())
         check(other, seen[-1], lse.double().cpu().numpy())
     assert np.array_equal(*seen)
+
+
+@pytest.mark.parametrize("ctx,n", [([100, 200], [1, 1]), ([4500, 200], [1, 1]), ([100, 200], [2, 3]), ([2300, 200], [2, 3]), ([100, 200], [4, 4]), ([2300, 200], [4, 4]),
+                                   ([100, 200], [40, 3]), ([3000, 200], [40, 30])])
+def test_rows_before_the_first_request_and_calls_without_lse(ctx, n):
+    """Row offsets that begin behind 0: rows before them and behind the last stay as they were, in the cache's calls too; no lse asked for."""
+    d = dims(8, 128, 64)
+    c = Case(d, ctx, n, seed=70)
+    T, lead = int(c.indptr[-1]), 5
+    h = make_handle(d, torch.float32)
+    b = hb.Batch(dev_i32(c.ctx), dev_i32(c.table), *no_rings(d, 2), dev_i32(c.indptr + lead), max_q_len=max(n), total_q=T + lead + 3, max_ctx_len=max(ctx))
+    q = torch.zeros((T + lead + 3, 16, 128), dtype=torch.bfloat16, device="cuda")
+    q[lead:lead + T] = to_dev_bf16(c.q)
+    outs = []
+    for lse in (torch.full((T + lead + 3, 16), 7.0, device="cuda"), None):
+        out, ws = torch.full(q.shape, 7.0, device="cuda"), workspace(h, b, True)
+        ws.fill_(255)
+        hb.hswa_packed_attn(h, c.layer(), b, True, q, out, lse, ws)
+        no_error(h)
+        assert (out[:lead] == 7).all() and (out[lead + T:] == 7).all()
+        if lse is not None:
+            assert (lse[:lead] == 7).all() and (lse[lead + T:] == 7).all()
+            check(c, out[lead:lead + T].double().cpu().numpy(), lse[lead:lead + T].double().cpu().numpy())
+        outs.append(out)
+    assert torch.equal(*outs)
+    # the step's rows back, and in again: nothing changes
+    layer = c.layer()
+    before = layer.pool.clone()
+    k, v = (torch.full((T + lead + 3, 2, 128), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    hb.hswa_packed_read(h, layer, b, k, v)
+    no_error(h)
+    for x in (k, v):
+        assert (x[:lead] == 9).all() and (x[lead + T:] == 9).all() and (x[lead:lead + T] != 9).any(dim=(1, 2)).all()
+    hb.hswa_packed_append(h, layer, b, k, v)
+    no_error(h)
+    again = [torch.empty_like(k) for _ in range(2)]
+    hb.hswa_packed_read(h, layer, b, *again)
+    no_error(h)
+    assert all(torch.equal(x[lead:lead + T], y[lead:lead + T]) for x, y in zip((k, v), again))
+    untouched = torch.ones_like(before, dtype=torch.bool)
+    P, D = 64, 128
+    for r in range(2):
+        for i in range(n[r]):
+            page, slot = int(c.table[r, (ctx[r] + i) // P]), (ctx[r] + i) % P
+            untouched[page, :, :, slot * D // 2:(slot + 1) * D // 2] = False
+            untouched[page, :, :, P * D // 2 + slot * D // 16:P * D // 2 + (slot + 1) * D // 16] = False
+    assert torch.equal(layer.pool[untouched], before[untouched])
