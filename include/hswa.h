@@ -343,14 +343,15 @@ hswa_status hswa_evict_compact(hswa_handle* h, const hswa_layer* layer, const hs
  *   that sees nothing gives zeros and an lse of minus infinity.  q: device bf16 [T][Hq][D]; out: device [T][Hq][D] in
  *   cfg.out_dtype; lse: device fp32 [T][Hq] or NULL.  Held values enter the products exactly; q enters them in fp16 after a
  *   power of two (exact but for elements below 2^-28 of the largest finite one of a KV head's rows in the step); probabilities enter the PV product as
- *   fp16, row sums and lse are taken over the fp32 values.  batch->q_indptr may be NULL (one token per request).  Slots behind a
+ *   fp16 (each off by 2^-11 of itself or, below 2^-21 of the row's largest so far, by 2^-32 of that, at most), row sums and lse are taken over the
+ *   fp32 values.  batch->q_indptr may be NULL (one token per request).  Slots behind a
  *   request's last row may hold anything.  Workspace: hswa_packed_workspace_need bytes, else HSWA_ERR_WORKSPACE; 256-byte
- *   aligned.  The block table must cover max_ctx_len (HSWA_ERR_INVALID_ARG); max_ctx_len + max_q_len is at most 2^30
- *   (HSWA_ERR_UNSUPPORTED).  A request longer than max_ctx_len or max_q_len, with row offsets outside [0, total_q], or whose keys
+ *   aligned.  A request longer than max_ctx_len or max_q_len, with row offsets outside [0, total_q], or whose keys
  *   pass the block table, is recorded as HSWA_ERR_BOUNDS (index -1 / -2 / -2 / -3); what the bounds cover is computed, other rows
  *   of out and lse stay as they were.
- * All refuse a current device other than the handle's, scales that are not within [2^-64, 2^64], and an sm_scale whose product with
- * k_scale is past fp32 (HSWA_ERR_INVALID_ARG); append and read 2^30 blocks of 16 or more at once (HSWA_ERR_UNSUPPORTED).
+ * All refuse a current device other than the handle's, scales that are not within [2^-64, 2^64], a block table that does not cover
+ * max_ctx_len (HSWA_ERR_INVALID_ARG), and max_ctx_len + max_q_len above 2^30 (HSWA_ERR_UNSUPPORTED); hswa_packed_attn an sm_scale whose
+ * product with k_scale is past fp32 (HSWA_ERR_INVALID_ARG); append and read 2^30 blocks of 16 or more at once (HSWA_ERR_UNSUPPORTED).
  *
  * hswa_packed_workspace_need: exact bytes for a call with these host-known fields; pure host arithmetic. */
 typedef struct {
@@ -405,9 +406,10 @@ hswa_status hswa_packed_attn(hswa_handle* h, const hswa_packed_layer* layer, con
  *   pools 4 * Hkv * P * D bytes, 4-bit pools 2 * Hkv * P * (D / 2 + D / 16).  No page may be the destination of two pairs, or of one
  *   and the source of another (the lists of the two calls above keep to that).  Ids out of range are recorded and not copied.
  *
- * All refuse a current device other than the handle's (HSWA_ERR_INVALID_ARG), more than 4096 rows, 2^23 pages or 2^30
- * entries of a table (HSWA_ERR_UNSUPPORTED), and an output that is an input or another output, table_out of hswa_pages_compact and its table apart
- * (HSWA_ERR_INVALID_ARG). */
+ * All refuse a current device other than the handle's (HSWA_ERR_INVALID_ARG).  Fork and compact refuse more than 4096 rows, 2^23 pages
+ * or 2^30 entries of a table (HSWA_ERR_UNSUPPORTED), and an output that is an input or another output, table_out of hswa_pages_compact
+ * and its table apart (HSWA_ERR_INVALID_ARG); copy 2^31 pages or more, pages of more than 2^30 bytes, and as many pairs as make 2^31 pieces
+ * of 4 KB of one pool (HSWA_ERR_UNSUPPORTED). */
 size_t hswa_pages_workspace_need(const hswa_handle* h, int64_t num_pages);
 hswa_status hswa_pages_fork(hswa_handle* h, int64_t num_pages, const int32_t* ref, int32_t* ref_out, int32_t rows_in,
                             const int32_t* held, const int32_t* table, int32_t max_blocks, int32_t rows_out, const int32_t* parent,

@@ -326,3 +326,13 @@ def test_beams_on_a_hybrid_stack(d):
                 assert (np.abs(o[r:r + 1] - want) <= tol + 1e-7).all(), (step, layer, r, np.abs(o[r:r + 1] - want).max())
         hb.hswa_step_advance(h, B, ctx, head, b.q_indptr)
         head_of = head.tolist()
+
+
+def test_copy_refuses_what_its_grid_cannot_hold():
+    d = dims(1, 64, 16, 1)
+    h, lib = make_handle(d), hb.load()
+    pool, ids = torch.zeros((4, 2, 1, 16, 64), dtype=torch.bfloat16, device="cuda"), dev_i32([0, 1])
+    at = (hb.C.c_void_p * 1)(pool.data_ptr())
+    for pages, size, pairs in ((1 << 31, 4096, 2), (4, (1 << 30) + 16, 2), (4, 1 << 30, 1 << 13)):
+        assert lib.hswa_pages_copy(h.ptr, 1, at, pages, size, pairs, ids.data_ptr(), ids.data_ptr(), None) == hb.HSWA_ERR_UNSUPPORTED
+    no_error(h)
