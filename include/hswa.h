@@ -351,7 +351,8 @@ hswa_status hswa_evict_compact(hswa_handle* h, const hswa_layer* layer, const hs
  *   of out and lse stay as they were.
  * All refuse a current device other than the handle's, scales that are not within [2^-64, 2^64], a block table that does not cover
  * max_ctx_len (HSWA_ERR_INVALID_ARG), and max_ctx_len + max_q_len above 2^30 (HSWA_ERR_UNSUPPORTED); hswa_packed_attn an sm_scale whose
- * product with k_scale is past fp32 (HSWA_ERR_INVALID_ARG); append and read 2^30 blocks of 16 or more at once (HSWA_ERR_UNSUPPORTED).
+ * product with k_scale is past fp32 (HSWA_ERR_INVALID_ARG); append and read 2^30 blocks of 16 or more at once and more than
+ * 65535 KV heads (HSWA_ERR_UNSUPPORTED).
  *
  * hswa_packed_workspace_need: exact bytes for a call with these host-known fields; pure host arithmetic. */
 typedef struct {

@@ -335,6 +335,7 @@ hswa_status packed_rows(hswa_handle* h, const hswa_packed_layer* layer, const hs
   const void *k = in ? k_in : k_out, *v = in ? v_in : v_out;
   if (!k || !v || !aligned16(k) || !aligned16(v)) return HSWA_ERR_INVALID_ARG;
   if ((int64_t)b->total_q * h->cfg.num_kv_heads * (h->cfg.head_dim / 16) > INT32_MAX / 2) return HSWA_ERR_UNSUPPORTED;
+  if (h->cfg.num_kv_heads > 65535) return HSWA_ERR_UNSUPPORTED;  // (the kernels divide by it with a 32-bit product)
   PackedCacheParams p = {};
   p.m = model_params(h);
   p.b = batch_params(b);

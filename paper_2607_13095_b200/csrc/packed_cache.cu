@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kThreads) packed_read_kernel(const PackedCache
 struct Geometry {
   int tokens;
   dim3 grid;
-  uint32_t per_head;  // 2^32 / Hkv, rounded up: a row's token by one multiplication (rows of a block are far below 2^16)
+  uint32_t per_head;  // 2^32 / Hkv, rounded up: a row's token by one multiplication (exact while row and Hkv are below 2^16)
 };
 Geometry geometry(const PackedCacheParams& p, int num_sms) {
   const int per_token = p.m.Hkv * (p.m.D / 8);

@@ -346,3 +346,35 @@ def test_rows_before_the_first_request_and_calls_without_lse(ctx, n):
             untouched[page, :, :, slot * D // 2:(slot + 1) * D // 2] = False
             untouched[page, :, :, P * D // 2 + slot * D // 16:P * D // 2 + (slot + 1) * D // 16] = False
     assert torch.equal(layer.pool[untouched], before[untouched])
+
+
+def test_append_and_read_refuse_more_heads_than_they_divide_by():
+    for heads in (65536, 70001):
+        d = dims(1, 64, 16, heads)
+        h = make_handle(d)
+        layer = hb.PackedLayer(torch.zeros((1, 2, heads, 16 * 36), dtype=torch.uint8, device="cuda"))
+        k, v = (torch.zeros((1, heads, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        b = hb.Batch(dev_i32([0]), dev_i32([[0]]), *no_rings(d, 1), max_ctx_len=0)
+        for call in (hb.hswa_packed_append, hb.hswa_packed_read):
+            with pytest.raises(hb.HswaError) as e:
+                call(h, layer, b, k, v)
+            assert e.value.status == hb.HSWA_ERR_UNSUPPORTED
+        no_error(h)
+
+
+def test_append_and_read_of_many_heads():
+    """The most heads that are taken: each head's row goes to its own slab and comes back."""
+    heads = 65535
+    d = dims(1, 64, 16, heads)
+    h = make_handle(d)
+    layer = hb.PackedLayer(torch.zeros((1, 2, heads, 16 * 36), dtype=torch.uint8, device="cuda"))
+    g = torch.Generator(device="cuda").manual_seed(14)
+    k, v = (torch.randint(0, 2, (2, heads, 64), generator=g, device="cuda").mul(12).sub(6).to(torch.bfloat16) for _ in range(2))
+    b = hb.Batch(dev_i32([3]), dev_i32([[0]]), *no_rings(d, 1), dev_i32([0, 2]), max_q_len=2, total_q=2, max_ctx_len=3)
+    hb.hswa_packed_append(h, layer, b, k, v)
+    back = [torch.empty_like(k) for _ in range(2)]
+    hb.hswa_packed_read(h, layer, b, *back)
+    no_error(h)
+    assert torch.equal(back[0], k) and torch.equal(back[1], v)
+    touched = layer.pool.reshape(2, heads, -1)[:, :, : 16 * 32].reshape(2, heads, 16, 32).ne(0).any(dim=3)
+    assert (touched[:, :, 3:5]).all() and not touched[:, :, :3].any() and not touched[:, :, 5:].any()
