@@ -89,14 +89,14 @@ __device__ __forceinline__ void tmem_st_cols(uint32_t addr, const uint32_t* r) {
   else tmem_st16p(addr, r);
 }
 // A bounded wait in as few instructions as it can be polled with: twenty warps share the SM, and what the waiting ones issue the
-// others cannot (reading the clock at each poll, and a hint to sleep, took near half of all issue slots).  It gives up after 2^22
-// polls, each of which may suspend the thread: a tenth of a second at least.
+// others cannot (reading the clock at each poll, and a hint to sleep, took near half of all issue slots).  It gives up after 2^19
+// polls, each of which suspends the thread for some 8000 clocks (measured on a barrier that nothing completes): two seconds.
 __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity) {
   uint32_t done;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 0;\n"
       "POLL:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
-      "add.u32 n, n, 1;\n\tsetp.lt.u32 q, n, 4194304;\n\t@q bra POLL;\n"
+      "add.u32 n, n, 1;\n\tsetp.lt.u32 q, n, 524288;\n\t@q bra POLL;\n"
       "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(done)
       : "r"(bar), "r"(parity)
